@@ -413,6 +413,156 @@ quasar_status quasar_tensor_amax(const float* w, int64_t n, float* amax_out,
                                  quasar_stream_t stream);
 
 /*
+ * Operators around the reconstruction.  A training step reads the
+ * reconstructed weights r in matrix products, compares the student's logits
+ * with a teacher's (the forward KL the paper distils with, Sec. 6.1), and
+ * differentiates both; the weight gradient is the g the next reconstruction
+ * reads.  The conventions at the top of this file hold, with these
+ * differences: matrices are row-major with a row stride (`ld`, in elements,
+ * at least the row's length), and only pointers that are said to be are
+ * 16-byte aligned; the others need their element's alignment.  Sums and
+ * softmax statistics are fp32; an output of fewer bits is rounded once.
+ */
+
+/* y = z (none), max(z, 0), z / (1 + e^-z), z Phi(z) */
+typedef enum {
+    QUASAR_ACT_NONE = 0,
+    QUASAR_ACT_RELU = 1,
+    QUASAR_ACT_SILU = 2,
+    QUASAR_ACT_GELU = 3
+} quasar_activation;
+
+/*
+ * quasar_linear -- z = x r^T + bias, y = activation(z) + residual.
+ *
+ *   x         [tokens, inputs] bf16, 16-byte aligned, ld_x % 8 == 0.
+ *   r         [features, inputs] bf16 (a reconstruction with bf16 r), 16-byte
+ *             aligned, ld_r % 8 == 0.
+ *   bias      [features] fp32, or NULL.
+ *   residual  [tokens, features] of y's dtype, or NULL; it may be y itself
+ *             (same pointer and stride).
+ *   y         [tokens, features], dtype y_dtype (written).
+ *   pre       [tokens, features] bf16, receives z (what the activation's
+ *             gradient needs), or NULL.
+ * Any number of tokens, from one up; features may be odd, rows of y, pre and
+ * residual may start anywhere.  tokens or features 0 is a no-op; inputs 0
+ * gives z = bias.  Products are exact bf16 x bf16, accumulated in fp32.
+ * Outputs must not overlap inputs, but for the residual.
+ */
+quasar_status quasar_linear(const void* x, int64_t ld_x, const void* r, int64_t ld_r,
+                            const float* bias, quasar_activation activation, const void* residual,
+                            int64_t ld_residual, int64_t tokens, int64_t features, int64_t inputs,
+                            void* y, quasar_dtype y_dtype, int64_t ld_y, void* pre, int64_t ld_pre,
+                            quasar_stream_t stream);
+
+/*
+ * quasar_linear_grad_input -- dx = (dz r) * activation_in'(pre_in) + residual.
+ *
+ *   dz        [tokens, features] bf16, the gradient at z, 16-byte aligned,
+ *             ld_dz % 8 == 0.
+ *   r         as in quasar_linear.
+ *   pre_in    [tokens, inputs] bf16: the z that the layer's input was
+ *             activated from, with activation_in; NULL (with
+ *             QUASAR_ACT_NONE) if the input was not an activation.  Then dx
+ *             is the gradient at that z: the dz of the layer below.
+ *   residual  [tokens, inputs] of dx's dtype, added last, or NULL.
+ *   dx        [tokens, inputs], dtype dx_dtype (written); it may be residual
+ *             or a bf16 pre_in itself.
+ */
+quasar_status quasar_linear_grad_input(const void* dz, int64_t ld_dz, const void* r, int64_t ld_r,
+                                       const void* pre_in, int64_t ld_pre_in,
+                                       quasar_activation activation_in, const void* residual,
+                                       int64_t ld_residual, int64_t tokens, int64_t features,
+                                       int64_t inputs, void* dx, quasar_dtype dx_dtype,
+                                       int64_t ld_dx, quasar_stream_t stream);
+
+/*
+ * quasar_linear_grad_weight -- dr = dz^T x and dbias = the column sums of dz.
+ *
+ *   dz, x     as above (x is not read when dr is NULL).
+ *   dr        [features, inputs], dtype dr_dtype (written), or NULL: the g of
+ *             the reconstruction entry points.
+ *   dbias     [features] fp32 (written), or NULL.
+ * tokens 0 gives zeros.  The order of every sum is fixed: the same inputs
+ * give the same bits.
+ */
+quasar_status quasar_linear_grad_weight(const void* dz, int64_t ld_dz, const void* x, int64_t ld_x,
+                                        int64_t tokens, int64_t features, int64_t inputs, void* dr,
+                                        quasar_dtype dr_dtype, int64_t ld_dr, float* dbias,
+                                        quasar_stream_t stream);
+
+/*
+ * quasar_activation_grad -- dz = dy * activation'(pre) in bf16 (all bf16,
+ * [rows, cols]): the gradient at z of a layer whose own output was activated.
+ * With QUASAR_ACT_NONE pre is not read and dz is a copy, which brings dy to
+ * the row stride the products need.  dz may be dy or pre itself.
+ */
+quasar_status quasar_activation_grad(const void* dy, int64_t ld_dy, const void* pre, int64_t ld_pre,
+                                     quasar_activation activation, int64_t rows, int64_t cols,
+                                     void* dz, int64_t ld_dz, quasar_stream_t stream);
+
+/*
+ * quasar_top_logits -- each row's k largest logits, largest first.
+ *
+ *   logits       [rows, vocab] bf16 or fp32 (dtype); rows may start anywhere.
+ *   k            1 .. min(256, vocab).
+ *   temperature  > 0.
+ *   values       [rows, k] fp32: the logits themselves (not scaled).
+ *   indices      [rows, k] int32.  Equal values rank by the lowest index.
+ *   lse          [rows] fp32: log sum exp(logits / temperature) over the
+ *                vocabulary (-inf for a row of -inf), or NULL.
+ * -inf logits are ordinary values (masked entries).  A row may take up to
+ * 8 x 208 KB less the lists (UNSUPPORTED beyond).
+ */
+quasar_status quasar_top_logits(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows,
+                                int64_t vocab, int k, float temperature, float* values,
+                                int32_t* indices, float* lse, quasar_stream_t stream);
+
+/*
+ * quasar_distill_top -- forward KL divergence of the student from a teacher
+ * of whom each row keeps k logits, with its gradient if asked.
+ *
+ * With z = logits / temperature and q = softmax(z):
+ *   teacher_lse given: p_k = exp(values_k / temperature - teacher_lse) and
+ *     everything not listed is one further outcome, the rest, of teacher mass
+ *     p_r = max(0, 1 - sum p_k) and student mass q_r;
+ *   teacher_lse NULL: p = softmax of the listed values / temperature, p_r = 0.
+ *   loss = sum_k p_k log(p_k / q_k) + p_r log(p_r / q_r)
+ *   grad = row_weight * d loss / d logits
+ *
+ *   logits       [rows, vocab] bf16 or fp32; rows may start anywhere.
+ *   indices      [rows, k] int32, distinct within a row.  An index outside
+ *                [0, vocab) marks an absent entry (a row with fewer than k).
+ *   values       [rows, k] fp32, 1 <= k <= 256.
+ *   row_weight   [rows] fp32 (what the row counts in the total), or NULL for
+ *                1.  A row of weight 0 is not read: loss, statistics and
+ *                gradient 0, whatever its logits hold.
+ *   loss         [rows] fp32, not weighted (written).
+ *   stats        [rows, 2] fp32: log sum exp z over the vocabulary and over
+ *                the unlisted entries, for the backward call; or NULL.
+ *   grad         [rows, vocab] of the logits' dtype, or NULL; it may be the
+ *                logits themselves (same pointer and stride).
+ * -inf logits are ordinary values (q = 0; a listed one with p > 0 makes the
+ * loss inf).  Without a single entry of mass, teacher_lse NULL gives loss and
+ * gradient 0.  Rows up to 8 x 208 KB (UNSUPPORTED beyond).
+ */
+quasar_status quasar_distill_top(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows,
+                                 int64_t vocab, const int32_t* indices, const float* values, int k,
+                                 const float* teacher_lse, const float* row_weight,
+                                 float temperature, float* loss, float* stats, void* grad,
+                                 int64_t ld_grad, quasar_stream_t stream);
+
+/* quasar_distill_top_backward -- the gradient alone, from the statistics a
+ * forward call kept, where the rows' weights (the gradient that reaches each
+ * row's loss) are known only later.  Arguments as above; stats is read. */
+quasar_status quasar_distill_top_backward(const void* logits, quasar_dtype dtype, int64_t ld,
+                                          int64_t rows, int64_t vocab, const int32_t* indices,
+                                          const float* values, int k, const float* teacher_lse,
+                                          const float* stats, const float* row_weight,
+                                          float temperature, void* grad, int64_t ld_grad,
+                                          quasar_stream_t stream);
+
+/*
  * quasar_get_device_status -- synchronises `stream`, then returns
  * QUASAR_ERR_TIMEOUT if any kernel of this library on the current device
  * recorded a timed-out wait since the previous query (and clears the record),

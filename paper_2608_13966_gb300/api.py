@@ -10,13 +10,18 @@ clears that word after synchronising the stream, and callers that must know
 their outputs are whole call it once after their last reconstruction."""
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
-from .quasar import (BF16, F32, QuasarError, QuasarStatus, adamw_nvfp4_tensor_array,
+from .quasar import (ACTIVATIONS, BF16, F32, QuasarError, QuasarStatus, adamw_nvfp4_tensor_array,
                      adamw_tensor_array, int_tensor_array, lut_tensor_array, nvfp4_tensor_array,
                      options, quasar_adamw_recon_int_batch, quasar_get_device_status, quasar_adamw_recon_nvfp4_batch,
                      quasar_recon_int, quasar_recon_int_batch_ex, quasar_recon_lut_batch,
-                     quasar_recon_nvfp4, quasar_recon_nvfp4_batch_ex, quasar_tensor_amax)
+                     quasar_recon_nvfp4, quasar_recon_nvfp4_batch_ex, quasar_tensor_amax,
+                     quasar_activation_grad, quasar_distill_top, quasar_distill_top_backward,
+                     quasar_linear, quasar_linear_grad_input, quasar_linear_grad_weight,
+                     quasar_top_logits)
 
 
 def _check(st):
@@ -284,4 +289,239 @@ def recon_lut_batch(items, *, clip, beta2=0.999, r_dtype=torch.bfloat16, codes=F
 def tensor_amax(w, stream=None):
     out = torch.empty(1, dtype=torch.float32, device=w.device)
     _check(quasar_tensor_amax(w, w.numel(), out, stream=stream))
+    return out
+
+
+# -- operators around the reconstruction -----------------------------------------
+#
+# Matrices are 2-D CUDA tensors whose rows are contiguous (any row stride).
+# Outputs and scratch are allocated on the stream the call runs on: pass
+# ``stream`` as a torch stream, or run under ``torch.cuda.stream``.
+
+def _matrix(t, name, shape=None, dtypes=(torch.bfloat16,)):
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a 2-D tensor with contiguous rows")
+    if not t.is_cuda or t.dtype not in dtypes:
+        raise ValueError(f"{name} must be a CUDA tensor of dtype {' or '.join(map(str, dtypes))}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    return _ld(t)
+
+
+def _ld(t):
+    """Row stride; a single row's is whatever a whole number of 8 elements needs."""
+    rows, cols = t.shape
+    return t.stride(0) if rows > 1 else -(-cols // 8) * 8
+
+
+def _vector(t, name, n, dtype=torch.float32):
+    if t.dim() != 1 or t.shape[0] != n or not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous CUDA tensor of {n} values of {dtype}")
+
+
+_FLOATS = (torch.bfloat16, torch.float32)
+_CODES = {torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _float_code(dtype, name):
+    if dtype not in _CODES:
+        raise ValueError(f"{name} must be torch.bfloat16 or torch.float32")
+    return _CODES[dtype]
+
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}")
+
+
+def _on(stream):
+    """Allocations made inside belong to the stream the call runs on."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
+
+
+def _for_products(t, stream):
+    """t itself if the products can read it, else a copy whose rows start at
+    16-byte boundaries."""
+    if t.data_ptr() % 16 == 0 and _ld(t) % 8 == 0:
+        return t
+    return activation_grad(t, None, "none", stream=stream)
+
+
+def linear(x, r, *, bias=None, activation="none", residual=None, out_dtype=torch.bfloat16,
+           save_pre=False, stream=None):
+    """z = x r^T + bias, y = activation(z) + residual.
+
+    x: bf16 [tokens, inputs]; r: bf16 [features, inputs] (a reconstruction);
+    bias: fp32 [features]; residual: [tokens, features] of out_dtype;
+    activation: "none", "relu", "silu" or "gelu".  Returns a dict with y and,
+    with save_pre, pre (z in bf16, in storage whose rows the products can
+    read)."""
+    ld_x = _matrix(x, "x")
+    tokens, inputs = x.shape
+    ld_r = _matrix(r, "r")
+    features = r.shape[0]
+    if r.shape[1] != inputs:
+        raise ValueError(f"x has {inputs} inputs, r {r.shape[1]}")
+    code = _float_code(out_dtype, "out_dtype")
+    _activation(activation)
+    if bias is not None:
+        _vector(bias, "bias", features)
+    ld_res = 0 if residual is None else _matrix(residual, "residual", (tokens, features), (out_dtype,))
+    with _on(stream):
+        y = torch.empty((tokens, features), dtype=out_dtype, device=x.device)
+        pre = _rows_of_8(tokens, features, x.device) if save_pre else None
+    _check(quasar_linear(x, ld_x, r, ld_r, bias, activation, residual, ld_res, tokens, features,
+                         inputs, y, code, features, pre, _ld(pre) if save_pre else 0, stream=stream))
+    return {"y": y, "pre": pre} if save_pre else {"y": y}
+
+
+def _rows_of_8(rows, cols, device):
+    """An empty bf16 [rows, cols] whose rows start at 16-byte boundaries."""
+    wide = torch.empty((rows, -(-cols // 8) * 8), dtype=torch.bfloat16, device=device)
+    return wide if wide.shape[1] == cols else wide[:, :cols]
+
+
+def activation_grad(dy, pre, activation, *, stream=None):
+    """dz = dy * activation'(pre) in bf16, in storage whose rows the products
+    can read ("none": a copy; pre is not used)."""
+    ld_dy = _matrix(dy, "dy")
+    _activation(activation)
+    ld_pre = 0 if activation == "none" else _matrix(pre, "pre", dy.shape)
+    rows, cols = dy.shape
+    with _on(stream):
+        dz = _rows_of_8(rows, cols, dy.device)
+    _check(quasar_activation_grad(dy, ld_dy, pre if activation != "none" else None, ld_pre,
+                                  activation, rows, cols, dz, _ld(dz), stream=stream))
+    return dz
+
+
+def linear_backward(dz, x, r, *, dx=True, dr=True, bias=False, pre_in=None, activation_in="none",
+                    residual=None, dx_dtype=torch.bfloat16, dr_dtype=torch.bfloat16, stream=None):
+    """Gradients of ``linear`` from dz (bf16 [tokens, features], the gradient
+    at z; see ``activation_grad`` for a layer whose own output is activated).
+
+    dx = (dz r) * activation_in'(pre_in) + residual, the gradient at the z the
+    input x was activated from (pre_in None: at x itself); dr = dz^T x, the g
+    the next reconstruction reads; dbias = the column sums of dz (with bias).
+    Returns a dict of those asked for."""
+    _matrix(dz, "dz")
+    tokens, features = dz.shape
+    ld_x = _matrix(x, "x")
+    inputs = x.shape[1]
+    if x.shape[0] != tokens:
+        raise ValueError(f"dz has {tokens} tokens, x {x.shape[0]}")
+    ld_r = _matrix(r, "r", (features, inputs))
+    _activation(activation_in)
+    if (pre_in is None) != (activation_in == "none"):
+        raise ValueError("pre_in and activation_in go together")
+    ld_pre = 0 if pre_in is None else _matrix(pre_in, "pre_in", (tokens, inputs))
+    ld_res = 0 if residual is None else _matrix(residual, "residual", (tokens, inputs), (dx_dtype,))
+    dx_code, dr_code = _float_code(dx_dtype, "dx_dtype"), _float_code(dr_dtype, "dr_dtype")
+    dz = _for_products(dz, stream)
+    ld_dz = _ld(dz)
+    out = {}
+    with _on(stream):
+        if dx:
+            out["dx"] = torch.empty((tokens, inputs), dtype=dx_dtype, device=dz.device)
+        if dr:
+            out["dr"] = torch.empty((features, inputs), dtype=dr_dtype, device=dz.device)
+        if bias:
+            out["dbias"] = torch.empty(features, dtype=torch.float32, device=dz.device)
+    if dx:
+        _check(quasar_linear_grad_input(dz, ld_dz, r, ld_r, pre_in, ld_pre, activation_in, residual,
+                                        ld_res, tokens, features, inputs, out["dx"], dx_code, inputs,
+                                        stream=stream))
+    if dr or bias:
+        _check(quasar_linear_grad_weight(dz, ld_dz, x, ld_x, tokens, features, inputs,
+                                         out.get("dr"), dr_code, inputs, out.get("dbias"),
+                                         stream=stream))
+    return out
+
+
+def top_logits(logits, k, *, temperature=1.0, lse=True, stream=None):
+    """Each row's k largest logits (bf16 or fp32 [rows, vocab]), largest
+    first, equal values by the lowest index.  Returns a dict with values
+    (fp32 [rows, k]), indices (int32) and, with lse, the row's
+    log sum exp(logits / temperature)."""
+    ld = _matrix(logits, "logits", dtypes=_FLOATS)
+    rows, vocab = logits.shape
+    with _on(stream):
+        values = torch.empty((rows, k), dtype=torch.float32, device=logits.device)
+        indices = torch.empty((rows, k), dtype=torch.int32, device=logits.device)
+        sums = torch.empty(rows, dtype=torch.float32, device=logits.device) if lse else None
+    _check(quasar_top_logits(logits, _CODES[logits.dtype], max(ld, vocab), rows, vocab, k, temperature,
+                             values, indices, sums, stream=stream))
+    out = {"values": values, "indices": indices}
+    if lse:
+        out["lse"] = sums
+    return out
+
+
+def _teacher(logits, indices, values, teacher_lse, row_weight):
+    ld = _matrix(logits, "logits", dtypes=_FLOATS)
+    rows = logits.shape[0]
+    k = indices.shape[1] if indices.dim() == 2 else 0
+    for t, name, dtype in ((indices, "indices", torch.int32), (values, "values", torch.float32)):
+        _matrix(t, name, (rows, k), (dtype,))
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    if teacher_lse is not None:
+        _vector(teacher_lse, "teacher_lse", rows)
+    if row_weight is not None:
+        _vector(row_weight, "row_weight", rows)
+    return ld, k
+
+
+def distill_top(logits, indices, values, *, teacher_lse=None, row_weight=None, temperature=1.0,
+                grad=True, stats=False, out=None, stream=None):
+    """Forward KL divergence of the student's logits (bf16 or fp32 [rows,
+    vocab]) from a teacher's top entries (``top_logits``: indices, values and,
+    for the mass outside them, its lse), and the gradient of
+    sum(row_weight * loss) with respect to the logits.
+
+    Returns a dict with loss (fp32 [rows], not weighted) and, as asked, grad
+    (of the logits' dtype; written to ``out`` if given, which may be the
+    logits) and stats (for ``distill_top_backward``).  Rows of weight 0 are
+    skipped: loss and gradient 0."""
+    ld, k = _teacher(logits, indices, values, teacher_lse, row_weight)
+    rows, vocab = logits.shape
+    if out is not None:
+        _matrix(out, "out", logits.shape, (logits.dtype,))
+    with _on(stream):
+        loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
+        kept = torch.empty((rows, 2), dtype=torch.float32, device=logits.device) if stats else None
+        if grad and out is None:
+            out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+    _check(quasar_distill_top(logits, _CODES[logits.dtype], ld, rows, vocab, indices, values, k,
+                              teacher_lse, row_weight, temperature, loss, kept,
+                              out if grad else None, _ld(out) if grad else 0, stream=stream))
+    made = {"loss": loss}
+    if grad:
+        made["grad"] = out
+    if stats:
+        made["stats"] = kept
+    return made
+
+
+def distill_top_backward(logits, indices, values, stats, row_weight, *, teacher_lse=None,
+                         temperature=1.0, out=None, stream=None):
+    """The gradient of sum(row_weight * loss) from the statistics a
+    ``distill_top(..., stats=True)`` call kept."""
+    ld, k = _teacher(logits, indices, values, teacher_lse, row_weight)
+    rows, vocab = logits.shape
+    _matrix(stats, "stats", (rows, 2), (torch.float32,))
+    if not stats.is_contiguous():
+        raise ValueError("stats must be contiguous")
+    if out is None:
+        with _on(stream):
+            out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+    else:
+        _matrix(out, "out", logits.shape, (logits.dtype,))
+    _check(quasar_distill_top_backward(logits, _CODES[logits.dtype], ld, rows, vocab, indices,
+                                       values, k, teacher_lse, stats, row_weight, temperature, out,
+                                       _ld(out), stream=stream))
     return out

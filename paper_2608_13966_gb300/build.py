@@ -37,6 +37,9 @@ UNITS = [
     ("kernels_nvfp4.cu", [], "kernels_nvfp4.o"),
     ("kernels_lut.cu", [], "kernels_lut.o"),
     ("kernels_sym.cu", [], "kernels_sym.o"),
+    ("train_abi.cu", [], "train_abi.o"),
+    ("kernels_linear.cu", [], "kernels_linear.o"),
+    ("kernels_logits.cu", [], "kernels_logits.o"),
 ]
 
 

@@ -1,0 +1,294 @@
+// Distillation from a teacher's top logits: the forward KL divergence of a
+// row of student logits and its gradient.
+//
+// With z = logits / temperature, q = softmax(z) over the vocabulary, p the
+// teacher's probabilities of its k listed entries, and the "rest" everything
+// that is not listed (student mass q_r, teacher mass p_r):
+//
+//   loss = sum_k p_k log(p_k / q_k) + p_r log(p_r / q_r)
+//        = sum of p log(p / q) - p + q over the entries and the rest,
+//
+// the second form because both sides sum to one: no term is negative, so
+// nothing cancels.  With P = sum p_k + p_r and u_j = e^{z_j} / sum over the
+// rest of e^z, the student's share of unlisted entry j within the rest,
+//
+//   dloss/dz_k = P q_k - p_k            (listed)
+//   dloss/dz_j = u_j (P q_r - p_r)      (unlisted),
+//
+// which never divides by q_r.  The rest's sum is formed on its own (a listed
+// logit is replaced by -inf in shared memory once it has been read), not as
+// the difference of two sums.
+#pragma once
+
+#include "row_slice.cuh"
+
+namespace quasar {
+
+constexpr int kDistillThreads = 512;
+constexpr float kLog2e = 1.44269504f;
+
+// x / tau - y: the quotient is not rounded before the subtraction (inv_tau is
+// 1 / tau rounded, the second step its remainder)
+__device__ __forceinline__ float scaled_less(float x, float tau, float inv_tau, float y)
+{
+    const float low = fmaf(-tau, inv_tau, 1.0f) * inv_tau;
+    const float d = fmaf(x, inv_tau, -y);
+    return low == 0.0f ? d : fmaf(x, low, d);
+}
+
+// p log(p / q) - p + q from p, log p and log q
+__device__ __forceinline__ float kl_term(float p, float log_p, float log_q)
+{
+    if (!(p > 0.0f)) return expf(log_q);
+    const float d = log_p - log_q;
+    return d > -1.0f ? p * (d + expm1f(-d)) : p * (d - 1.0f) + expf(log_q);
+}
+
+// Teacher side of a row, by one warp: log p of each entry into logp[] (-inf
+// where absent), returns sum p; n_listed counts the entries present.
+__device__ __forceinline__ float teacher_side(const DistillParams& p, int64_t r, float inv_tau,
+                                              float* logp, int32_t* entry, int* n_listed)
+{
+    const int lane = threadIdx.x & 31;
+    const int32_t* idx = p.indices + r * p.k;
+    const float* val = p.values + r * p.k;
+    float top = neg_inf();
+    int n = 0;
+    for (int k = lane; k < p.k; k += 32) {
+        const int32_t e = idx[k];
+        const bool here = e >= 0 && e < p.row.vocab;
+        const float t = here ? val[k] * inv_tau : neg_inf();
+        entry[k] = here ? e : -1;
+        logp[k] = t;
+        top = fmaxf(top, t);
+        n += here;
+    }
+    *n_listed = __reduce_add_sync(0xffffffffu, n);
+    float norm;
+    if (p.teacher_lse) {
+        norm = p.teacher_lse[r];
+    } else {
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        float s = 0.0f;
+        for (int k = lane; k < p.k; k += 32) s += top == neg_inf() ? 0.0f : expf(logp[k] - top);
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        norm = s > 0.0f ? top + logf(s) : 0.0f;
+    }
+    float sum = 0.0f;
+    for (int k = lane; k < p.k; k += 32) {
+        logp[k] -= norm;
+        sum += expf(logp[k]);
+    }
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    return sum;
+}
+
+// Maximum over the CTA's threads; `scratch` holds a float per warp.
+__device__ __forceinline__ float block_max(float x, float* scratch)
+{
+    x = lanes_max(x, 0xffffffffu);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
+    __syncthreads();
+    x = scratch[0];
+    for (int w = 1; w < (int)blockDim.x / 32; ++w) x = fmaxf(x, scratch[w]);
+    return x;
+}
+
+__device__ __forceinline__ float block_sum(float x, float* scratch)
+{
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
+    __syncthreads();
+    x = scratch[0];
+    for (int w = 1; w < (int)blockDim.x / 32; ++w) x += scratch[w];
+    return x;
+}
+
+// BACKWARD: the gradient from kept statistics (log-sum-exp of z over the
+// vocabulary and over the rest).  Otherwise the loss, the statistics and, if
+// asked, the gradient, the row staying in shared memory in between.
+template <typename T, bool BACKWARD>
+__global__ void __launch_bounds__(kDistillThreads) k_distill_top(const __grid_constant__ DistillParams p)
+{
+    using V = Vec16<T>;
+    constexpr int kN = V::kN;
+    extern __shared__ __align__(128) uint8_t smem_raw[];
+    T* slice = reinterpret_cast<T*>(smem_raw);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem_raw + (size_t)p.row.vecs * 16);
+    uint64_t* never = bars + kRowChunks;
+    float* logp = reinterpret_cast<float*>(never + 1);      // [kMaxTop]
+    float* own = logp + kMaxTop;                            // student logits of the entries held here
+    float* all = own + kMaxTop;                             // rank 0: of every entry
+    float(*parts)[4] = reinterpret_cast<float(*)[4]>(all + kMaxTop);  // [kRowCtas]
+    float* scratch = reinterpret_cast<float*>(parts + kRowCtas);      // [warps]
+    float* teacher = scratch + 32;                          // P, p_r, listed
+    int32_t* entry = reinterpret_cast<int32_t*>(teacher + 4);  // [kMaxTop]
+
+    const int t = threadIdx.x;
+    const int rank = (int)(blockIdx.x % p.row.ctas);
+    const int64_t r = blockIdx.x / p.row.ctas;
+    const RowSlice<T> S(p.row, r, rank);
+    const float weight = p.row_weight ? p.row_weight[r] : 1.0f;
+    T* grad = p.grad ? static_cast<T*>(p.grad) + r * p.ld_grad : nullptr;
+
+    if (weight == 0.0f) {  // a row that counts nothing is not read
+        if (grad)
+            for (int64_t s = S.begin + t; s < S.end; s += kDistillThreads) grad[s - S.lead] = V::from_f32(0.0f);
+        if (!BACKWARD && rank == 0 && t == 0) {
+            p.loss[r] = 0.0f;
+            if (p.stats) p.stats[2 * r] = p.stats[2 * r + 1] = 0.0f;
+        }
+        return;
+    }
+
+    if (t == 0) {
+        for (int c = 0; c < kRowChunks; ++c) mbar_init(bars + c, 1);
+        mbar_init(never, 1);
+        mbar_init_fence();
+    }
+    if (!BACKWARD) cluster_arrive();
+    __syncthreads();
+    S.load(slice, bars);
+    const float inv_tau = 1.0f / p.temperature;
+    if (t < 32) {
+        int n_listed;
+        const float sum = teacher_side(p, r, inv_tau, logp, entry, &n_listed);
+        if (t == 0) {
+            float rest = p.teacher_lse && n_listed < p.row.vocab ? fmaxf(1.0f - sum, 0.0f) : 0.0f;
+            teacher[0] = sum + rest;
+            teacher[1] = rest;
+        }
+    }
+    if (t == 0 && p.row.force_timeout_ns && !mbar_wait_bounded(never, 0, p.row.force_timeout_ns))
+        record_timeout(p.row.status);
+    for (int c = 0; c < kRowChunks; ++c)
+        if (!mbar_wait_bounded(bars + c, 0, p.row.timeout_ns)) record_timeout(p.row.status);
+    __syncthreads();
+    if (!BACKWARD) cluster_wait();  // every CTA of the row has started: its shared memory may be written
+
+    const float mass = teacher[0], p_rest = teacher[1];
+    const float c2 = kLog2e * inv_tau;
+    // take the listed entries out of the slice
+    for (int k = t; k < p.k; k += kDistillThreads) {
+        const int s = entry[k] >= 0 ? S.slot_of(entry[k]) : -1;
+        if (s >= 0) {
+            own[k] = V::to_f32(slice[s]);
+            if (!BACKWARD) st_peer(peer_addr(smem_u32(all + k), 0), own[k]);
+        }
+    }
+    __syncthreads();
+    for (int k = t; k < p.k; k += kDistillThreads) {
+        const int s = entry[k] >= 0 ? S.slot_of(entry[k]) : -1;
+        if (s >= 0) slice[s] = V::from_f32(neg_inf());
+    }
+    __syncthreads();
+
+    float m_rest, coef, q_rest, lse;     // of the whole row
+    float m_all = 0.0f, log_s = 0.0f;    // lse = m_all / tau + log_s
+    if constexpr (!BACKWARD) {
+        float m = neg_inf(), s = 0.0f;
+        for (int v = t; v < S.n_vecs; v += kDistillThreads) {
+            float x[kN];
+            V::unpack(reinterpret_cast<const uint4*>(slice)[v], x);
+            float top = x[0];
+#pragma unroll
+            for (int j = 1; j < kN; ++j) top = fmaxf(top, x[j]);
+            if (top > m) {
+                s *= ex2((m - top) * c2);
+                m = top;
+            }
+            const float base = m == neg_inf() ? 0.0f : m;
+#pragma unroll
+            for (int j = 0; j < kN; ++j) s += ex2((x[j] - base) * c2);
+        }
+        // the listed entries held here, as a second sum
+        float m_in = neg_inf(), s_in = 0.0f;
+        for (int k = t; k < p.k; k += kDistillThreads) {
+            const int at = entry[k] >= 0 ? S.slot_of(entry[k]) : -1;
+            if (at >= 0) merge_sum(m_in, s_in, own[k], own[k] == neg_inf() ? 0.0f : 1.0f, c2);
+        }
+        const float top = block_max(m, scratch), top_in = block_max(m_in, scratch);
+        s = block_sum(top == neg_inf() ? s : s * ex2((m - top) * c2), scratch);
+        s_in = block_sum(m_in == neg_inf() ? 0.0f : s_in * ex2((m_in - top_in) * c2), scratch);
+        if (t < p.row.ctas) {
+            const uint32_t to = peer_addr(smem_u32(&parts[rank][0]), (uint32_t)t);
+            st_peer(to, top);
+            st_peer(to + 4, s);
+            st_peer(to + 8, top_in);
+            st_peer(to + 12, s_in);
+        }
+        cluster_sync();
+        float m_listed = neg_inf(), s_listed = 0.0f, s_rest = 0.0f;
+        m_rest = neg_inf();
+        for (int c = 0; c < p.row.ctas; ++c) {
+            merge_sum(m_rest, s_rest, parts[c][0], parts[c][1], c2);
+            merge_sum(m_listed, s_listed, parts[c][2], parts[c][3], c2);
+        }
+        float s_all = s_rest;
+        m_all = m_rest;
+        merge_sum(m_all, s_all, m_listed, s_listed, c2);
+        log_s = logf(s_all);
+        lse = m_all * inv_tau + log_s;
+        const bool some = m_rest != neg_inf();
+        const float log_q_rest = some ? (m_rest - m_all) * inv_tau + (logf(s_rest) - log_s) : neg_inf();
+        q_rest = expf(log_q_rest);
+        coef = some ? (mass * q_rest - p_rest) / s_rest : 0.0f;
+        if (rank == 0 && t < 32) {
+            float loss = 0.0f;
+            for (int k = t; k < p.k; k += 32)
+                if (entry[k] >= 0)
+                    loss += kl_term(expf(logp[k]), logp[k], (all[k] - m_all) * inv_tau - log_s);
+            for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
+            if (t == 0) {
+                loss += kl_term(p_rest, logf(p_rest), log_q_rest);
+                p.loss[r] = mass > 0.0f ? loss : 0.0f;
+                if (p.stats) {
+                    p.stats[2 * r] = lse;
+                    p.stats[2 * r + 1] = some ? m_rest * inv_tau + logf(s_rest) : neg_inf();
+                }
+            }
+        }
+        if (!grad) return;
+        if (!some) m_rest = 0.0f;
+    } else {
+        lse = p.stats[2 * r];
+        const float lse_rest = p.stats[2 * r + 1];
+        const bool some = lse_rest != neg_inf();
+        q_rest = some ? expf(lse_rest - lse) : 0.0f;
+        coef = some ? mass * q_rest - p_rest : 0.0f;
+        m_rest = some ? lse_rest : 0.0f;
+    }
+    const float scale = mass > 0.0f ? weight * inv_tau : 0.0f;
+    coef *= scale;
+
+    // the unlisted entries: coef e^(z - base)
+    const bool vectors = (reinterpret_cast<uintptr_t>(grad - S.lead) & 15) == 0;
+    for (int v = t; v < S.n_vecs; v += kDistillThreads) {
+        float x[kN];
+        V::unpack(reinterpret_cast<const uint4*>(slice)[v], x);
+#pragma unroll
+        for (int j = 0; j < kN; ++j)
+            x[j] = coef * (BACKWARD ? ex2(scaled_less(x[j], p.temperature, inv_tau, m_rest) * kLog2e)
+                                    : ex2((x[j] - m_rest) * c2));
+        const int64_t s = S.first + (int64_t)v * kN;
+        if (vectors && S.whole(v)) {
+            __stcs(reinterpret_cast<uint4*>(grad + (s - S.lead)), V::pack(x));
+        } else {
+#pragma unroll
+            for (int j = 0; j < kN; ++j)
+                if (s + j >= S.begin && s + j < S.end) grad[s + j - S.lead] = V::from_f32(x[j]);
+        }
+    }
+    __syncthreads();
+    // then the listed ones over the zeros left in their places
+    for (int k = t; k < p.k; k += kDistillThreads) {
+        const int s = entry[k] >= 0 ? S.slot_of(entry[k]) : -1;
+        if (s < 0) continue;
+        const float q = BACKWARD ? expf(scaled_less(own[k], p.temperature, inv_tau, lse)) : expf((own[k] - m_all) * inv_tau - log_s);
+        grad[entry[k]] = V::from_f32(scale * (mass * q - expf(logp[k])));
+    }
+}
+
+}  // namespace quasar

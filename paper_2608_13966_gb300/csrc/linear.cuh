@@ -1,0 +1,352 @@
+// Matrix products with the reconstructed weights: y = act(x r^T + bias) +
+// residual and the two products of its backward pass, on the 5th-generation
+// tensor cores.
+//
+// Every product is written as D[i][j] = sum_k A[i][k] B[j][k] with i the
+// coordinate that is contiguous in the result's memory:
+//
+//   forward          i = feature, j = token, k = input    A = r,  B = x
+//   input gradient   i = input,   j = token, k = feature  A = r^T, B = dz
+//   weight gradient  i = input,   j = feature, k = token  A = x^T, B = dz^T
+//
+// so that an accumulator lane (a row of D in tensor memory) is a memory
+// column: one accumulator column stored by a warp is 32 consecutive results.
+// No result is staged through shared memory, and results may start at any
+// element and have any row stride.  A transposed operand is read as it lies
+// in memory (an MN-major tile); nothing is transposed on the way.
+#pragma once
+
+#include "cluster.cuh"
+#include "linear.h"
+#include "quasar.h"
+#include "tensor_core.cuh"
+
+namespace quasar {
+
+constexpr int kTileRows = 128;          // rows of D a CTA owns: the lanes of tensor memory
+constexpr int kTileK = 64;              // 128 bytes of bf16: one swizzled row
+constexpr uint32_t kTileABytes = kTileRows * kTileK * 2;
+
+// -- activations -------------------------------------------------------------
+
+// fp32 throughout; exp and erf are CUDA's accurate functions (the epilogue is
+// hidden behind the next tile's product, so the faster ones buy nothing).
+__device__ __forceinline__ float activation(float z, int act)
+{
+    switch (act) {
+    case QUASAR_ACT_RELU: return fmaxf(z, 0.0f);
+    case QUASAR_ACT_SILU: return z / (1.0f + expf(-z));
+    case QUASAR_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+    default: return z;
+    }
+}
+
+__device__ __forceinline__ float activation_slope(float z, int act)
+{
+    switch (act) {
+    case QUASAR_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
+    case QUASAR_ACT_SILU: {
+        const float s = 1.0f / (1.0f + expf(-z));
+        return s * (1.0f + z * (1.0f - s));
+    }
+    case QUASAR_ACT_GELU:
+        return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z);
+    default: return 1.0f;
+    }
+}
+
+// -- epilogue ----------------------------------------------------------------
+
+__device__ __forceinline__ float load_as_f32(const void* p, int64_t i, bool f32)
+{
+    return f32 ? static_cast<const float*>(p)[i]
+               : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+}
+
+__device__ __forceinline__ void store_from_f32(void* p, int64_t i, bool f32, float v)
+{
+    if (f32)
+        static_cast<float*>(p)[i] = v;
+    else
+        static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+}
+
+// N consecutive columns j0.. of one row i: bias, activation (or the input
+// activation's slope), residual, one rounding to the output's type.
+template <int N>
+__device__ __forceinline__ void finish(const Epilogue& e, float (&v)[N], int64_t i, int64_t j0,
+                                       int64_t rows, int64_t cols, float bias)
+{
+    if (i >= rows) return;
+    const int n = (int)(cols - j0 < N ? cols - j0 : N);
+    const bool f32 = e.out_f32;
+    float res[N];
+#pragma unroll
+    for (int c = 0; c < N; ++c)
+        res[c] = e.residual && c < n ? load_as_f32(e.residual, (j0 + c) * e.ld_res + i, f32) : 0.0f;
+    if (e.scale_pre) {
+        float z[N];
+#pragma unroll
+        for (int c = 0; c < N; ++c)
+            z[c] = c < n ? load_as_f32(e.scale_pre, (j0 + c) * e.ld_scale + i, false) : 0.0f;
+#pragma unroll
+        for (int c = 0; c < N; ++c) v[c] *= activation_slope(z[c], e.act);
+    } else {
+#pragma unroll
+        for (int c = 0; c < N; ++c) v[c] += bias;
+        if (e.pre) {
+#pragma unroll
+            for (int c = 0; c < N; ++c)
+                if (c < n) store_from_f32(e.pre, (j0 + c) * e.ld_pre + i, false, v[c]);
+        }
+        if (e.act != QUASAR_ACT_NONE) {
+#pragma unroll
+            for (int c = 0; c < N; ++c) v[c] = activation(v[c], e.act);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < N; ++c)
+        if (c < n) store_from_f32(e.out, (j0 + c) * e.ld_out + i, f32, v[c] + res[c]);
+}
+
+// -- waits -------------------------------------------------------------------
+
+// Wait for a phase of `bar`; gives up when limit_ns have passed or another
+// role of this CTA gave up (`*gone`), and then says so to the others.
+__device__ __forceinline__ bool role_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* gone,
+                                          uint64_t limit_ns, unsigned int* status)
+{
+    if (mbar_try_wait(bar, parity)) return true;
+    const uint64_t t0 = global_timer_ns();
+    for (;;) {
+#pragma unroll 1
+        for (int i = 0; i < 16; ++i)
+            if (mbar_try_wait(bar, parity)) return true;
+        if (*gone) return false;
+        if (global_timer_ns() - t0 > limit_ns) {
+            *gone = 1;
+            record_timeout(status);
+            return false;
+        }
+    }
+}
+
+// -- one tile per cluster ------------------------------------------------------
+
+// BN columns (tokens, for the forward product) by 128 rows per cluster, the
+// reduction split over the cluster's CTAs.  Each CTA multiplies its share
+// into its own tensor memory; the partial tiles are then exchanged through
+// distributed shared memory and summed in rank order (always the same order,
+// so the result does not depend on timing), each CTA finishing BN / split of
+// the columns.
+//
+// Warps: 0-3 epilogue (one per 32 lanes of tensor memory), 4 copies, 5
+// matrix instructions.
+template <int BN, bool A_MN, bool B_MN>
+__global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ ProductParams p)
+{
+    constexpr uint32_t kBBytes = BN * kTileK * 2;
+    constexpr uint32_t kStageBytes = kTileABytes + kBBytes;
+    constexpr uint32_t kColumns = BN < 32 ? 32 : BN;
+    static_assert(!B_MN || BN % 64 == 0, "an MN-major tile is made of 64-wide blocks");
+
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    const int stages = p.stages;
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + (size_t)stages * kStageBytes);
+    uint64_t* empty = full + stages;
+    uint64_t* done = empty + stages;
+    uint64_t* never = done + 1;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(never + 1);
+    volatile uint32_t* gone = tmem_slot + 1;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = p.split > 1 ? (int)cluster_rank() : 0;
+    const int64_t tile = blockIdx.x / p.split;
+    const int64_t row0 = (tile % p.tiles_row) * kTileRows;
+    const int64_t col0 = (tile / p.tiles_row) * BN;
+    const int kb0 = (int)((int64_t)p.k_blocks * rank / p.split);
+    const int nkb = (int)((int64_t)p.k_blocks * (rank + 1) / p.split) - kb0;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < stages; ++s) {
+            mbar_init(full + s, 1);
+            mbar_init(empty + s, 1);
+        }
+        mbar_init(done, 1);
+        mbar_init(never, 1);
+        *gone = 0;
+        mbar_init_fence();
+    }
+    if (warp == 5) tmem_alloc<1>(tmem_slot, kColumns);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == 4 && lane == 0) {
+        if (p.force_timeout_ns) role_wait(never, 0, gone, p.force_timeout_ns, p.status);
+        int it = 0;
+        for (; it < nkb; ++it) {
+            const int s = it % stages;
+            if (it >= stages && !role_wait(empty + s, (it / stages - 1) & 1, gone, p.timeout_ns, p.status)) break;
+            if (*gone) break;
+            const uint32_t a = smem_u32(smem + (size_t)s * kStageBytes), b = a + kTileABytes;
+            const uint32_t bar = smem_u32(full + s);
+            mbar_arrive_expect_tx(full + s, kStageBytes);
+            const int k = (kb0 + it) * kTileK;
+            if (A_MN) {
+#pragma unroll
+                for (int q = 0; q < kTileRows / 64; ++q) tile_g2s(a + q * 8192, &p.a, (int)row0 + 64 * q, k, bar);
+            } else {
+                tile_g2s(a, &p.a, k, (int)row0, bar);
+            }
+            if (B_MN) {
+#pragma unroll
+                for (int q = 0; q < BN / 64; ++q) tile_g2s(b + q * 8192, &p.b, (int)col0 + 64 * q, k, bar);
+            } else {
+                tile_g2s(b, &p.b, k, (int)col0, bar);
+            }
+        }
+        // given up: the copies in flight still land in this CTA's memory
+        if (it < nkb)
+            for (int j = it > stages ? it - stages : 0; j < it; ++j)
+                mbar_wait_bounded(full + j % stages, (j / stages) & 1, p.timeout_ns);
+    } else if (warp == 5 && lane == 0) {
+        constexpr uint32_t desc = mma_desc(kTileRows, BN, A_MN, B_MN);
+        for (int it = 0; it < nkb; ++it) {
+            const int s = it % stages;
+            if (!role_wait(full + s, (it / stages) & 1, gone, p.timeout_ns, p.status)) break;
+            tc_fence_after();
+            const uint32_t a = smem_u32(smem + (size_t)s * kStageBytes);
+            uint64_t da = operand_desc(a, A_MN), db = operand_desc(a + kTileABytes, B_MN);
+#pragma unroll
+            for (int k = 0; k < kTileK / 16; ++k) {
+                mma_bf16<1>(tmem, da, db, desc, it > 0 || k > 0);
+                da += k_step(A_MN);
+                db += k_step(B_MN);
+            }
+            mma_commit(smem_u32(empty + s));
+        }
+        mma_commit(smem_u32(done));
+        // everything issued is finished before tensor memory is freed
+        mbar_wait_bounded(done, 0, p.timeout_ns);
+    }
+    __syncwarp();
+    if (warp < 4) {
+        role_wait(done, 0, gone, p.timeout_ns, p.status);
+        __syncwarp();
+        tc_fence_after();
+        const int64_t i = row0 + 32 * warp + lane;
+        const float bias = p.e.bias && i < p.rows ? p.e.bias[i] : 0.0f;
+        const uint32_t mine = tmem + ((uint32_t)(32 * warp) << 16);
+        float* part = reinterpret_cast<float*>(smem);
+        for (int c = 0; c < BN; c += 16) {
+            float v[16];
+            if (nkb > 0) {
+                tmem_ld16(mine + c, v);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 16; ++q) v[q] = 0.0f;
+            }
+            if (p.split == 1) {
+                if (col0 + c < p.cols) finish(p.e, v, i, col0 + c, p.rows, p.cols, bias);
+            } else {
+                // the operands' memory is free: every product is done
+#pragma unroll
+                for (int q = 0; q < 16; ++q) part[(c + q) * kTileRows + 32 * warp + lane] = v[q];
+            }
+        }
+    }
+    if (p.split > 1) {
+        __syncthreads();
+        cluster_sync();
+        if (warp < 4) {
+            const int64_t i = row0 + 32 * warp + lane;
+            const float bias = p.e.bias && i < p.rows ? p.e.bias[i] : 0.0f;
+            const int per = BN / p.split;
+            const uint32_t base = smem_u32(smem) + (uint32_t)(32 * warp + lane) * 4;
+            for (int c = rank * per; c < (rank + 1) * per; c += 2) {
+                if (col0 + c >= p.cols) break;
+                float v[2] = {0.0f, 0.0f};
+                for (int r = 0; r < p.split; ++r) {
+                    const uint32_t from = peer_addr(base, (uint32_t)r);
+                    v[0] += ld_peer(from + (uint32_t)c * kTileRows * 4);
+                    v[1] += ld_peer(from + (uint32_t)(c + 1) * kTileRows * 4);
+                }
+                finish(p.e, v, i, col0 + c, p.rows, p.cols, bias);
+            }
+        }
+        cluster_sync();
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 5) tmem_free<1>(tmem, kColumns);
+}
+
+// -- column sums and activation gradients --------------------------------------
+
+// dbias[j] = sum over rows of dz[row][j] in fp32.  64 columns per cluster of 8
+// CTAs of 8 warps; warp w of CTA c takes the rows c + 8 w + 64 q, and the 64
+// partial sums of a column are added in a fixed order.
+__global__ void __launch_bounds__(256) k_column_sum(const __grid_constant__ ColumnSumParams p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    float2* part = reinterpret_cast<float2*>(smem_raw);  // [8 warps][32 lanes]
+    float2* peers = part + 256;                          // [8 CTAs][32 lanes], used by rank 0
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)cluster_rank();
+    const int64_t col = (int64_t)(blockIdx.x / 8) * 64 + 2 * lane;
+    const __nv_bfloat16* in = static_cast<const __nv_bfloat16*>(p.in) + col;
+    float2 s = make_float2(0.0f, 0.0f);
+    cluster_arrive();
+    if (col + 1 < p.cols) {
+#pragma unroll 8
+        for (int64_t r = rank + 8 * warp; r < p.rows; r += 64) {
+            const uint32_t x = *reinterpret_cast<const uint32_t*>(in + r * p.ld);
+            s.x += bf16lo(x);
+            s.y += bf16hi(x);
+        }
+    } else if (col < p.cols) {
+        for (int64_t r = rank + 8 * warp; r < p.rows; r += 64) s.x += __bfloat162float(in[r * p.ld]);
+    }
+    part[warp * 32 + lane] = s;
+    __syncthreads();
+    cluster_wait();
+    if (warp == 0) {
+        for (int w = 1; w < 8; ++w) {
+            s.x += part[w * 32 + lane].x;
+            s.y += part[w * 32 + lane].y;
+        }
+        const uint32_t to = peer_addr(smem_u32(peers + rank * 32 + lane), 0);
+        st_peer(to, s.x);
+        st_peer(to + 4, s.y);
+    }
+    cluster_sync();
+    if (rank == 0 && warp == 0) {
+        s = peers[lane];
+        for (int c = 1; c < 8; ++c) {
+            s.x += peers[c * 32 + lane].x;
+            s.y += peers[c * 32 + lane].y;
+        }
+        if (col < p.cols) p.out[col] = s.x;
+        if (col + 1 < p.cols) p.out[col + 1] = s.y;
+    }
+}
+
+// dz = dy act'(pre), rounded once to bf16 (pre NULL: a strided copy).
+__global__ void __launch_bounds__(256) k_activation_grad(const __grid_constant__ ActGradParams p)
+{
+    const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (col >= p.cols) return;
+    const __nv_bfloat16* dy = static_cast<const __nv_bfloat16*>(p.dy);
+    const __nv_bfloat16* pre = static_cast<const __nv_bfloat16*>(p.pre);
+    __nv_bfloat16* dz = static_cast<__nv_bfloat16*>(p.dz);
+    for (int64_t r = blockIdx.y; r < p.rows; r += gridDim.y) {
+        float d = __bfloat162float(dy[r * p.ld_dy + col]);
+        if (pre) d *= activation_slope(__bfloat162float(pre[r * p.ld_pre + col]), p.act);
+        dz[r * p.ld_dz + col] = __float2bfloat16_rn(d);
+    }
+}
+
+}  // namespace quasar

@@ -1,0 +1,50 @@
+// Launch parameters of the kernels over rows of logits (shared by host and
+// device).
+#pragma once
+
+#include <cstdint>
+
+namespace quasar {
+
+constexpr int kMaxTop = 256;          // most entries of a row's top list
+constexpr int kRowCtas = 8;           // most CTAs (one cluster) a row is spread over
+constexpr int kRowChunks = 4;         // copies a CTA's slice arrives in
+
+// A row of logits spread over a cluster: each CTA holds a slice in shared
+// memory, `vecs` vectors of 16 bytes at most.
+struct RowParams {
+    const void* logits;
+    int64_t ld;
+    int64_t rows;
+    int64_t vocab;
+    int ctas;       // of a cluster
+    int vecs;       // of a slice
+    uint64_t timeout_ns;
+    uint64_t force_timeout_ns;
+    unsigned int* status;
+};
+
+struct TopParams {
+    RowParams row;
+    int k;
+    float temperature;
+    float* values;
+    int32_t* indices;
+    float* lse;     // or NULL
+};
+
+struct DistillParams {
+    RowParams row;
+    int k;
+    const int32_t* indices;
+    const float* values;
+    const float* teacher_lse;  // or NULL: renormalise over the k
+    const float* row_weight;   // or NULL: 1
+    float temperature;
+    float* loss;               // forward
+    float* stats;              // forward: written if given; backward: read
+    void* grad;                // or NULL
+    int64_t ld_grad;
+};
+
+}  // namespace quasar

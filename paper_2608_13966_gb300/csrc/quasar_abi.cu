@@ -11,6 +11,7 @@
 #include <cstring>
 #include <mutex>
 
+#include "host.h"
 #include "params.h"
 #include "quasar.h"
 
@@ -258,6 +259,7 @@ int g_ncfg = 0;
 struct SmemLimit {
     const void* fn = nullptr;
     int dev = -1;
+    size_t optin = 0;
 };
 constexpr int kMaxLimits = 256;
 SmemLimit g_limit[kMaxLimits];
@@ -296,6 +298,23 @@ quasar_status status_ptr(unsigned int** p)
     return QUASAR_OK;
 }
 
+// Raise fn's dynamic shared-memory limit to the device's opt-in maximum, once
+// per device (the caller holds g_mu).
+quasar_status allow_smem(const void* fn, size_t smem, int dev)
+{
+    for (int i = 0; i < g_nlimit; ++i)
+        if (g_limit[i].fn == fn && g_limit[i].dev == dev)
+            return smem <= g_limit[i].optin ? QUASAR_OK : QUASAR_ERR_UNSUPPORTED;
+    int optin = 0;
+    if (cudaDeviceGetAttribute(&optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev) != cudaSuccess)
+        return QUASAR_ERR_CUDA;
+    if (smem > (size_t)optin) return QUASAR_ERR_UNSUPPORTED;
+    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, optin) != cudaSuccess)
+        return QUASAR_ERR_CUDA;
+    if (g_nlimit < kMaxLimits) g_limit[g_nlimit++] = SmemLimit{fn, dev, (size_t)optin};
+    return QUASAR_OK;
+}
+
 // Resident CTAs per SM for (fn, smem) on device dev.  The kernel's dynamic
 // shared-memory limit is set once per device, to the device's opt-in
 // maximum, so every configuration cached earlier stays launchable.
@@ -307,17 +326,8 @@ quasar_status occupancy(const void* fn, size_t smem, int threads, int dev, int* 
             *occ = g_cfg[i].occupancy;
             return QUASAR_OK;
         }
-    bool raised = false;
-    for (int i = 0; i < g_nlimit && !raised; ++i) raised = g_limit[i].fn == fn && g_limit[i].dev == dev;
-    if (!raised) {
-        int optin = 0;
-        if (cudaDeviceGetAttribute(&optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev) != cudaSuccess)
-            return QUASAR_ERR_CUDA;
-        if (smem > (size_t)optin) return QUASAR_ERR_UNSUPPORTED;
-        if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, optin) != cudaSuccess)
-            return QUASAR_ERR_CUDA;
-        if (g_nlimit < kMaxLimits) g_limit[g_nlimit++] = SmemLimit{fn, dev};
-    }
+    quasar_status st;
+    if ((st = allow_smem(fn, smem, dev)) != QUASAR_OK) return st;
     int o = 0;
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&o, fn, threads, smem) != cudaSuccess)
         return QUASAR_ERR_CUDA;
@@ -670,6 +680,33 @@ quasar_status nvfp4_run(Nvfp4Launch<MAXT>& Lp, AmaxBatch<MAXT>& B, int n_clip, c
 }
 
 }  // namespace
+
+namespace quasar {
+
+quasar_status host_device(int* n_sm, unsigned int** status)
+{
+    int dev;
+    const DeviceInfo* info;
+    const quasar_status st = device_info(&dev, &info);
+    if (st != QUASAR_OK) return st;
+    *n_sm = info->nsm;
+    *status = info->status;
+    return QUASAR_OK;
+}
+
+quasar_status host_allow_smem(const void* fn, size_t smem)
+{
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return QUASAR_ERR_CUDA;
+    std::lock_guard<std::mutex> lock(g_mu);
+    return allow_smem(fn, smem, dev);
+}
+
+uint64_t host_timeout_ns() { return kDefaultTimeoutNs; }
+
+uint64_t host_forced_timeout_ns() { return (uint64_t)std::max<int64_t>(0, g_force_timeout_ns.load()); }
+
+}  // namespace quasar
 
 extern "C" {
 
@@ -1114,6 +1151,6 @@ const char* quasar_status_string(quasar_status status)
     }
 }
 
-int quasar_version(void) { return 100; }
+int quasar_version(void) { return 200; }
 
 }  // extern "C"

@@ -1,0 +1,148 @@
+// 5th-generation tensor-core building blocks (sm_103a): tile copies by tensor
+// map (TMA), shared-memory matrix descriptors, tcgen05.mma with accumulators
+// in tensor memory, and their completion on mbarriers.
+#pragma once
+
+#include <cstdint>
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include "device_common.cuh"
+
+namespace quasar {
+
+// 2-D tile copy global -> shared.  x (the contiguous coordinate) is a
+// multiple of 8 bf16 elements everywhere in this library (the 16-byte rule of
+// tiled copies); elements outside the tensor arrive as zero and count toward
+// the barrier's bytes.
+__device__ __forceinline__ void tile_g2s(uint32_t dst, const CUtensorMap* map, int x, int y,
+                                         uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+
+// The same by one CTA of a pair: `bar` may lie in the pair's other CTA.
+__device__ __forceinline__ void tile_g2s_pair(uint32_t dst, const CUtensorMap* map, int x, int y,
+                                              uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map)
+{
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
+// Matrix descriptor of an operand tile in shared memory, 128-byte swizzle,
+// base 1024-byte aligned.  K-major tiles are rows of 64 elements (128 bytes)
+// and repeat every 8 rows (stride 1024; the leading offset is not used).
+// MN-major tiles are blocks of 64 (M or N) x 64 (K) elements: 8 K-rows to the
+// next 1024 bytes, the next 64 M or N at the leading offset of 8192 bytes.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool mn_major)
+{
+    const uint64_t leading = mn_major ? (8192u >> 4) : 1u;
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | (leading << 16) | ((uint64_t)(1024u >> 4) << 32) |
+           (1ull << 46) | (2ull << 61);
+}
+
+// Descriptor advance for the next 16 elements of K: 32 bytes along a K-major
+// row, 16 rows of 128 bytes in an MN-major block.
+__device__ __forceinline__ uint64_t k_step(bool mn_major) { return mn_major ? (2048u >> 4) : (32u >> 4); }
+
+// Instruction descriptor of kind::f16: bf16 operands, fp32 accumulators.
+__device__ __forceinline__ constexpr uint32_t mma_desc(int m, int n, bool a_mn, bool b_mn)
+{
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
+           ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+template <int CTAS>
+__device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add)
+{
+    if constexpr (CTAS == 1)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
+            : "memory");
+}
+
+// Arrive on `bar` when every tcgen05.mma this thread issued so far is done.
+__device__ __forceinline__ void mma_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
+                 : "memory");
+}
+
+// The same on the barrier at this offset in both CTAs of the pair.
+__device__ __forceinline__ void mma_commit_pair(uint32_t bar)
+{
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 "
+        "[%0], %1;" ::"r"(bar),
+        "h"((uint16_t)3)
+        : "memory");
+}
+
+// Tensor memory: whole-warp calls.  `slot` receives the first column.
+template <int CTAS>
+__device__ __forceinline__ void tmem_alloc(uint32_t* slot, uint32_t columns)
+{
+    if constexpr (CTAS == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                         smem_u32(slot)),
+                     "r"(columns)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                         smem_u32(slot)),
+                     "r"(columns)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+}
+
+template <int CTAS>
+__device__ __forceinline__ void tmem_free(uint32_t base, uint32_t columns)
+{
+    if constexpr (CTAS == 1)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns));
+    else
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns));
+}
+
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// 16 accumulator columns of this warp's 32 lanes, one lane a thread.
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16])
+{
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+          "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+}  // namespace quasar

@@ -1,0 +1,427 @@
+// C ABI of the operators around the reconstruction: matrix products with the
+// reconstructed weights, a teacher's top logits, and distillation from them.
+// Argument validation, launch plans and launches; declarations and contracts
+// are in include/quasar.h.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <mutex>
+
+#include "host.h"
+#include "linear.h"
+#include "logits.h"
+#include "quasar.h"
+
+namespace quasar {
+const void* product_tile_kernel(int bn, bool a_mn, bool b_mn);
+const void* column_sum_kernel();
+const void* activation_grad_kernel();
+const void* distill_kernel(bool f32, bool backward);
+const void* top_logits_kernel(bool f32);
+}  // namespace quasar
+
+namespace {
+
+using namespace quasar;
+
+bool valid_dtype(quasar_dtype d) { return d == QUASAR_F32 || d == QUASAR_BF16; }
+int64_t dtype_size(quasar_dtype d) { return d == QUASAR_BF16 ? 2 : 4; }
+bool valid_act(quasar_activation a) { return a >= QUASAR_ACT_NONE && a <= QUASAR_ACT_GELU; }
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// Bytes a strided [rows, cols] view spans.
+size_t span(int64_t rows, int64_t cols, int64_t ld, int64_t size)
+{
+    return rows == 0 || cols == 0 ? 0 : (size_t)(((rows - 1) * ld + cols) * size);
+}
+
+bool overlaps(const void* a, size_t na, const void* b, size_t nb)
+{
+    if (!a || !b || na == 0 || nb == 0) return false;
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + nb && y < x + na;
+}
+
+// Sizes a 2-D view may have: coordinates are 32-bit on the device, offsets 64.
+bool valid_shape(int64_t rows, int64_t cols, int64_t ld)
+{
+    constexpr int64_t kMax = (int64_t(1) << 31) - 256;
+    return rows >= 0 && cols >= 0 && rows <= kMax && cols <= kMax && ld >= cols &&
+           ld <= (int64_t(1) << 36) && (rows == 0 || ld <= (int64_t(1) << 58) / rows);
+}
+
+// -- launches ------------------------------------------------------------------
+
+quasar_status launch(const void* fn, void* params, dim3 grid, int threads, int cluster, size_t smem,
+                     quasar_stream_t stream)
+{
+    const quasar_status st = host_allow_smem(fn, smem);
+    if (st != QUASAR_OK) return st;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = reinterpret_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cluster;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 1 : 0;
+    void* args[] = {params};
+    return cudaLaunchKernelExC(&cfg, fn, args) == cudaSuccess ? QUASAR_OK : QUASAR_ERR_CUDA;
+}
+
+// -- matrix products -------------------------------------------------------------
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                 CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled()
+{
+    static const EncodeTiled fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) !=
+                cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return fn;
+}
+
+// An operand as it lies in memory: bf16 [outer, inner], 64 x box_outer tiles.
+struct Operand {
+    const void* p;
+    int64_t ld;
+    int64_t outer, inner;
+    bool mn_major;  // inner is the coordinate of D's rows (or columns), not the reduction
+};
+
+quasar_status tile_map(const Operand& o, int box_outer, CUtensorMap* map)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return QUASAR_ERR_UNSUPPORTED;
+    const cuuint64_t dims[2] = {(cuuint64_t)o.inner, (cuuint64_t)o.outer};
+    const cuuint64_t strides[1] = {(cuuint64_t)o.ld * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_outer};
+    const cuuint32_t step[2] = {1, 1};
+    const CUresult r =
+        encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(o.p), dims, strides, box, step,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? QUASAR_OK : QUASAR_ERR_INVALID_ARG;
+}
+
+// An operand's rows start at 16-byte boundaries (the rule of tiled copies).
+bool valid_operand(const void* p, int64_t rows, int64_t cols, int64_t ld)
+{
+    return valid_shape(rows, cols, ld) && (rows == 0 || cols == 0 || (p && aligned(p, 16) && ld % 8 == 0));
+}
+
+// D (rows x cols, rows contiguous) = A B^T over `depth`, then the epilogue.
+quasar_status product(const Operand& a, const Operand& b, int64_t rows, int64_t cols, int64_t depth,
+                      const Epilogue& e, quasar_stream_t stream)
+{
+    if (rows == 0 || cols == 0) return QUASAR_OK;
+    ProductParams p{};
+    int n_sm = 0;
+    quasar_status st = host_device(&n_sm, &p.status);
+    if (st != QUASAR_OK) return st;
+    p.e = e;
+    p.rows = rows;
+    p.cols = cols;
+    p.k_blocks = (int)((depth + 63) / 64);
+    p.timeout_ns = host_timeout_ns();
+    p.force_timeout_ns = host_forced_timeout_ns();
+
+    int bn = cols <= 16 ? 16 : (cols <= 32 ? 32 : (cols <= 64 ? 64 : 128));
+    if (b.mn_major) bn = std::max(bn, 64);
+    p.tiles_row = (int)((rows + 127) / 128);
+    p.tiles_col = (int)((cols + bn - 1) / bn);
+    const int64_t tiles = (int64_t)p.tiles_row * p.tiles_col;
+    p.split = 1;
+    while (p.split < 8 && tiles * p.split * 2 <= 2 * n_sm && p.k_blocks >= p.split * 4) p.split *= 2;
+    const size_t stage = 128 * 128 + (size_t)bn * 128;
+    p.stages = (int)std::min<size_t>(8, (size_t)100 * 1024 / stage);
+    // exchange of partial tiles through the stages' memory
+    const size_t smem = 1024 + p.stages * stage + (2 * p.stages + 2) * 8 + 16;
+    if (tiles * p.split > (int64_t(1) << 31) - 1) return QUASAR_ERR_UNSUPPORTED;
+    if (depth > 0) {
+        if ((st = tile_map(a, a.mn_major ? 64 : 128, &p.a)) != QUASAR_OK) return st;
+        if ((st = tile_map(b, b.mn_major ? 64 : bn, &p.b)) != QUASAR_OK) return st;
+    }
+    const void* fn = product_tile_kernel(bn, a.mn_major, b.mn_major);
+    if (!fn) return QUASAR_ERR_UNSUPPORTED;
+    return launch(fn, &p, dim3((unsigned)(tiles * p.split)), 192, p.split, smem, stream);
+}
+
+// -- rows of logits ----------------------------------------------------------------
+
+// How a row is spread: the fewest CTAs (a power of two) whose slices leave
+// room for three of them on an SM, then more while the rows alone leave SMs
+// idle and slices stay above 4 KB.
+quasar_status plan_rows(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows, int64_t vocab,
+                        size_t extra, RowParams* row, size_t* smem)
+{
+    int n_sm = 0;
+    quasar_status st = host_device(&n_sm, &row->status);
+    if (st != QUASAR_OK) return st;
+    row->logits = logits;
+    row->ld = ld;
+    row->rows = rows;
+    row->vocab = vocab;
+    row->timeout_ns = host_timeout_ns();
+    row->force_timeout_ns = host_forced_timeout_ns();
+    const int64_t per = 16 / dtype_size(dtype);
+    const int64_t vecs = (vocab + per - 1 + per - 1) / per;  // for any start within 16 bytes
+    auto slice = [&](int c) { return (vecs + c - 1) / c * 16; };
+    constexpr int64_t kThree = 75 * 1024;
+    int c = 1;
+    while (c < kRowCtas && slice(c) + (int64_t)extra > kThree) c *= 2;
+    while (c < kRowCtas && rows * c < n_sm && slice(2 * c) >= 4096) c *= 2;
+    row->ctas = c;
+    row->vecs = (int)(slice(c) / 16);
+    *smem = (size_t)slice(c) + extra;
+    if (*smem > 226 * 1024) return QUASAR_ERR_UNSUPPORTED;
+    if (rows * c > (int64_t(1) << 31) - 1) return QUASAR_ERR_UNSUPPORTED;
+    return QUASAR_OK;
+}
+
+quasar_status check_rows(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows, int64_t vocab,
+                         int k, float temperature)
+{
+    if (!valid_dtype(dtype) || !valid_shape(rows, vocab, ld)) return QUASAR_ERR_INVALID_ARG;
+    if (!(temperature > 0.0f) || !std::isfinite(temperature)) return QUASAR_ERR_INVALID_ARG;
+    if (vocab < 1 || k < 1 || k > vocab) return QUASAR_ERR_INVALID_ARG;
+    if (k > kMaxTop) return QUASAR_ERR_UNSUPPORTED;
+    if (rows > 0 && (!logits || !aligned(logits, (uintptr_t)dtype_size(dtype)))) return QUASAR_ERR_INVALID_ARG;
+    return QUASAR_OK;
+}
+
+constexpr size_t kDistillExtra = (kRowChunks + 1) * 8 + 3 * kMaxTop * 4 + kRowCtas * 16 + 32 * 4 + 16 + kMaxTop * 4;
+
+quasar_status run_distill(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows, int64_t vocab,
+                          const int32_t* indices, const float* values, int k, const float* teacher_lse,
+                          const float* row_weight, float temperature, float* loss, float* stats, void* grad,
+                          int64_t ld_grad, bool backward, quasar_stream_t stream)
+{
+    quasar_status st = check_rows(logits, dtype, ld, rows, vocab, k, temperature);
+    if (st != QUASAR_OK) return st;
+    if (grad && !valid_shape(rows, vocab, ld_grad)) return QUASAR_ERR_INVALID_ARG;
+    if (rows == 0) return QUASAR_OK;
+    if (!indices || !values || !aligned(indices, 4) || !aligned(values, 4)) return QUASAR_ERR_INVALID_ARG;
+    if (!aligned(teacher_lse, 4) || !aligned(row_weight, 4) || !aligned(loss, 4) || !aligned(stats, 4))
+        return QUASAR_ERR_INVALID_ARG;
+    if (backward ? (!stats || !grad) : !loss) return QUASAR_ERR_INVALID_ARG;
+    if (!aligned(grad, (uintptr_t)dtype_size(dtype))) return QUASAR_ERR_INVALID_ARG;
+    const size_t n_log = span(rows, vocab, ld, dtype_size(dtype));
+    const size_t n_grad = grad ? span(rows, vocab, ld_grad, dtype_size(dtype)) : 0;
+    const size_t n_row = (size_t)rows * 4, n_top = (size_t)rows * k * 4;
+    // the gradient may replace the logits, in exactly their place
+    const bool in_place = grad == logits && ld_grad == ld;
+    if (!in_place && overlaps(grad, n_grad, logits, n_log)) return QUASAR_ERR_INVALID_ARG;
+    const void* outs[] = {grad, backward ? nullptr : loss, backward ? nullptr : stats};
+    const size_t out_n[] = {n_grad, n_row, 2 * n_row};
+    const void* ins[] = {indices, values, teacher_lse, row_weight, backward ? stats : nullptr};
+    const size_t in_n[] = {n_top, n_top, n_row, n_row, 2 * n_row};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < 5; ++j)
+            if (overlaps(outs[i], out_n[i], ins[j], in_n[j])) return QUASAR_ERR_INVALID_ARG;
+        if (i > 0 && overlaps(outs[i], out_n[i], logits, n_log)) return QUASAR_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (overlaps(outs[i], out_n[i], outs[j], out_n[j])) return QUASAR_ERR_INVALID_ARG;
+    }
+    DistillParams p{};
+    size_t smem = 0;
+    if ((st = plan_rows(logits, dtype, ld, rows, vocab, kDistillExtra, &p.row, &smem)) != QUASAR_OK) return st;
+    p.k = k;
+    p.indices = indices;
+    p.values = values;
+    p.teacher_lse = teacher_lse;
+    p.row_weight = row_weight;
+    p.temperature = temperature;
+    p.loss = loss;
+    p.stats = stats;
+    p.grad = grad;
+    p.ld_grad = ld_grad;
+    return launch(distill_kernel(dtype == QUASAR_F32, backward), &p, dim3((unsigned)(rows * p.row.ctas)), 512,
+                  backward ? 1 : p.row.ctas, smem, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+quasar_status quasar_linear(const void* x, int64_t ld_x, const void* r, int64_t ld_r, const float* bias,
+                            quasar_activation activation, const void* residual, int64_t ld_residual,
+                            int64_t tokens, int64_t features, int64_t inputs, void* y, quasar_dtype y_dtype,
+                            int64_t ld_y, void* pre, int64_t ld_pre, quasar_stream_t stream)
+{
+    if (!valid_act(activation) || !valid_dtype(y_dtype)) return QUASAR_ERR_INVALID_ARG;
+    if (!valid_operand(x, tokens, inputs, ld_x) || !valid_operand(r, features, inputs, ld_r))
+        return QUASAR_ERR_INVALID_ARG;
+    if (!valid_shape(tokens, features, ld_y)) return QUASAR_ERR_INVALID_ARG;
+    if (residual && !valid_shape(tokens, features, ld_residual)) return QUASAR_ERR_INVALID_ARG;
+    if (pre && !valid_shape(tokens, features, ld_pre)) return QUASAR_ERR_INVALID_ARG;
+    if (tokens == 0 || features == 0) return QUASAR_OK;
+    const int64_t size = dtype_size(y_dtype);
+    if (!y || !aligned(y, size) || !aligned(residual, size) || !aligned(bias, 4) || !aligned(pre, 2))
+        return QUASAR_ERR_INVALID_ARG;
+    const size_t n_y = span(tokens, features, ld_y, size);
+    const size_t n_pre = pre ? span(tokens, features, ld_pre, 2) : 0;
+    const size_t n_res = residual ? span(tokens, features, ld_residual, size) : 0;
+    const size_t n_x = span(tokens, inputs, ld_x, 2), n_r = span(features, inputs, ld_r, 2);
+    const size_t n_bias = bias ? (size_t)features * 4 : 0;
+    // y may replace the residual, in exactly its place
+    const bool in_place = residual == y && ld_residual == ld_y;
+    if (overlaps(y, n_y, x, n_x) || overlaps(y, n_y, r, n_r) || overlaps(y, n_y, bias, n_bias) ||
+        (!in_place && overlaps(y, n_y, residual, n_res)) || overlaps(pre, n_pre, x, n_x) ||
+        overlaps(pre, n_pre, r, n_r) || overlaps(pre, n_pre, bias, n_bias) ||
+        overlaps(pre, n_pre, residual, n_res) || overlaps(pre, n_pre, y, n_y))
+        return QUASAR_ERR_INVALID_ARG;
+    const Epilogue e{bias, pre, ld_pre, nullptr, 0, residual, ld_residual, y, ld_y, activation,
+                     y_dtype == QUASAR_F32};
+    return product(Operand{r, ld_r, features, inputs, false}, Operand{x, ld_x, tokens, inputs, false}, features,
+                   tokens, inputs, e, stream);
+}
+
+quasar_status quasar_linear_grad_input(const void* dz, int64_t ld_dz, const void* r, int64_t ld_r,
+                                       const void* pre_in, int64_t ld_pre_in, quasar_activation activation_in,
+                                       const void* residual, int64_t ld_residual, int64_t tokens,
+                                       int64_t features, int64_t inputs, void* dx, quasar_dtype dx_dtype,
+                                       int64_t ld_dx, quasar_stream_t stream)
+{
+    if (!valid_act(activation_in) || !valid_dtype(dx_dtype)) return QUASAR_ERR_INVALID_ARG;
+    if (!valid_operand(dz, tokens, features, ld_dz) || !valid_operand(r, features, inputs, ld_r))
+        return QUASAR_ERR_INVALID_ARG;
+    if (!valid_shape(tokens, inputs, ld_dx)) return QUASAR_ERR_INVALID_ARG;
+    if (residual && !valid_shape(tokens, inputs, ld_residual)) return QUASAR_ERR_INVALID_ARG;
+    const bool slope = activation_in != QUASAR_ACT_NONE;
+    if (pre_in && !valid_shape(tokens, inputs, ld_pre_in)) return QUASAR_ERR_INVALID_ARG;
+    if (tokens == 0 || inputs == 0) return QUASAR_OK;
+    const int64_t size = dtype_size(dx_dtype);
+    if (!dx || !aligned(dx, size) || !aligned(residual, size) || !aligned(pre_in, 2)) return QUASAR_ERR_INVALID_ARG;
+    if (slope && !pre_in) return QUASAR_ERR_INVALID_ARG;
+    const size_t n_dx = span(tokens, inputs, ld_dx, size);
+    const size_t n_pre = pre_in ? span(tokens, inputs, ld_pre_in, 2) : 0;
+    const size_t n_res = residual ? span(tokens, inputs, ld_residual, size) : 0;
+    const bool res_in_place = residual == dx && ld_residual == ld_dx;
+    const bool pre_in_place = pre_in == dx && ld_pre_in == ld_dx && size == 2;
+    if (overlaps(dx, n_dx, dz, span(tokens, features, ld_dz, 2)) ||
+        overlaps(dx, n_dx, r, span(features, inputs, ld_r, 2)) ||
+        (!pre_in_place && overlaps(dx, n_dx, pre_in, n_pre)) ||
+        (!res_in_place && overlaps(dx, n_dx, residual, n_res)))
+        return QUASAR_ERR_INVALID_ARG;
+    const Epilogue e{nullptr, nullptr, 0, slope ? pre_in : nullptr, ld_pre_in, residual, ld_residual, dx, ld_dx,
+                     activation_in, dx_dtype == QUASAR_F32};
+    return product(Operand{r, ld_r, features, inputs, true}, Operand{dz, ld_dz, tokens, features, false}, inputs,
+                   tokens, features, e, stream);
+}
+
+quasar_status quasar_linear_grad_weight(const void* dz, int64_t ld_dz, const void* x, int64_t ld_x,
+                                        int64_t tokens, int64_t features, int64_t inputs, void* dr,
+                                        quasar_dtype dr_dtype, int64_t ld_dr, float* dbias,
+                                        quasar_stream_t stream)
+{
+    if (!valid_dtype(dr_dtype) || !valid_operand(dz, tokens, features, ld_dz)) return QUASAR_ERR_INVALID_ARG;
+    if (dr && (!valid_operand(x, tokens, inputs, ld_x) || !valid_shape(features, inputs, ld_dr)))
+        return QUASAR_ERR_INVALID_ARG;
+    if (features == 0) return QUASAR_OK;
+    if ((dr && !aligned(dr, dtype_size(dr_dtype))) || !aligned(dbias, 4)) return QUASAR_ERR_INVALID_ARG;
+    const size_t n_dz = span(tokens, features, ld_dz, 2);
+    const size_t n_dr = dr ? span(features, inputs, ld_dr, dtype_size(dr_dtype)) : 0;
+    const size_t n_x = dr ? span(tokens, inputs, ld_x, 2) : 0, n_db = dbias ? (size_t)features * 4 : 0;
+    if (overlaps(dr, n_dr, dz, n_dz) || overlaps(dr, n_dr, x, n_x) || overlaps(dbias, n_db, dz, n_dz) ||
+        overlaps(dbias, n_db, x, n_x) || overlaps(dbias, n_db, dr, n_dr))
+        return QUASAR_ERR_INVALID_ARG;
+    if (dbias) {
+        ColumnSumParams c{dz, ld_dz, tokens, features, dbias};
+        const int64_t blocks = (features + 63) / 64;
+        const quasar_status st =
+            launch(column_sum_kernel(), &c, dim3((unsigned)(blocks * 8)), 256, 8, (256 + 256) * 8, stream);
+        if (st != QUASAR_OK) return st;
+    }
+    if (!dr) return QUASAR_OK;
+    const Epilogue e{nullptr, nullptr, 0, nullptr, 0, nullptr, 0, dr, ld_dr, QUASAR_ACT_NONE,
+                     dr_dtype == QUASAR_F32};
+    return product(Operand{x, ld_x, tokens, inputs, true}, Operand{dz, ld_dz, tokens, features, true}, inputs,
+                   features, tokens, e, stream);
+}
+
+quasar_status quasar_activation_grad(const void* dy, int64_t ld_dy, const void* pre, int64_t ld_pre,
+                                     quasar_activation activation, int64_t rows, int64_t cols, void* dz,
+                                     int64_t ld_dz, quasar_stream_t stream)
+{
+    const bool slope = activation != QUASAR_ACT_NONE;
+    if (!valid_act(activation) || !valid_shape(rows, cols, ld_dy) || !valid_shape(rows, cols, ld_dz))
+        return QUASAR_ERR_INVALID_ARG;
+    if (slope && !valid_shape(rows, cols, ld_pre)) return QUASAR_ERR_INVALID_ARG;
+    if (rows == 0 || cols == 0) return QUASAR_OK;
+    if (!dy || !dz || (slope && !pre) || !aligned(dy, 2) || !aligned(dz, 2) || !aligned(pre, 2))
+        return QUASAR_ERR_INVALID_ARG;
+    const size_t n_dz = span(rows, cols, ld_dz, 2);
+    if ((!(dz == dy && ld_dz == ld_dy) && overlaps(dz, n_dz, dy, span(rows, cols, ld_dy, 2))) ||
+        (slope && !(dz == pre && ld_dz == ld_pre) && overlaps(dz, n_dz, pre, span(rows, cols, ld_pre, 2))))
+        return QUASAR_ERR_INVALID_ARG;
+    ActGradParams p{dy, ld_dy, slope ? pre : nullptr, ld_pre, dz, ld_dz, rows, cols, activation};
+    return launch(activation_grad_kernel(), &p,
+                  dim3((unsigned)((cols + 255) / 256), (unsigned)std::min<int64_t>(rows, 65535)), 256, 1, 0, stream);
+}
+
+quasar_status quasar_top_logits(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows, int64_t vocab,
+                                int k, float temperature, float* values, int32_t* indices, float* lse,
+                                quasar_stream_t stream)
+{
+    quasar_status st = check_rows(logits, dtype, ld, rows, vocab, k, temperature);
+    if (st != QUASAR_OK) return st;
+    if (rows == 0) return QUASAR_OK;
+    if (!values || !indices || !aligned(values, 4) || !aligned(indices, 4) || !aligned(lse, 4))
+        return QUASAR_ERR_INVALID_ARG;
+    const size_t n_log = span(rows, vocab, ld, dtype_size(dtype)), n_top = (size_t)rows * k * 4;
+    const size_t n_lse = lse ? (size_t)rows * 4 : 0;
+    if (overlaps(values, n_top, logits, n_log) || overlaps(indices, n_top, logits, n_log) ||
+        overlaps(lse, n_lse, logits, n_log) || overlaps(values, n_top, indices, n_top) ||
+        overlaps(lse, n_lse, values, n_top) || overlaps(lse, n_lse, indices, n_top))
+        return QUASAR_ERR_INVALID_ARG;
+    TopParams p{};
+    const size_t extra =
+        (kRowChunks + 1) * 8 + 1024 * 8 + (size_t)kRowCtas * k * 8 + kRowCtas * 8 + 32 * 4 + 16;
+    size_t smem = 0;
+    if ((st = plan_rows(logits, dtype, ld, rows, vocab, extra, &p.row, &smem)) != QUASAR_OK) return st;
+    p.k = k;
+    p.temperature = temperature;
+    p.values = values;
+    p.indices = indices;
+    p.lse = lse;
+    return launch(top_logits_kernel(dtype == QUASAR_F32), &p, dim3((unsigned)(rows * p.row.ctas)), 512,
+                  p.row.ctas, smem, stream);
+}
+
+quasar_status quasar_distill_top(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows, int64_t vocab,
+                                 const int32_t* indices, const float* values, int k, const float* teacher_lse,
+                                 const float* row_weight, float temperature, float* loss, float* stats,
+                                 void* grad, int64_t ld_grad, quasar_stream_t stream)
+{
+    return run_distill(logits, dtype, ld, rows, vocab, indices, values, k, teacher_lse, row_weight, temperature,
+                       loss, stats, grad, ld_grad, false, stream);
+}
+
+quasar_status quasar_distill_top_backward(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows,
+                                          int64_t vocab, const int32_t* indices, const float* values, int k,
+                                          const float* teacher_lse, const float* stats, const float* row_weight,
+                                          float temperature, void* grad, int64_t ld_grad,
+                                          quasar_stream_t stream)
+{
+    return run_distill(logits, dtype, ld, rows, vocab, indices, values, k, teacher_lse, row_weight, temperature,
+                       nullptr, const_cast<float*>(stats), grad, ld_grad, true, stream);
+}
+
+}  // extern "C"

@@ -52,6 +52,18 @@ PROTOTYPES = {
     "quasar_adamw_recon_nvfp4_batch": (_I, [_P, _I, _I, _F, _F, _F, _F, _F, _I64, _P, _I, _I, _P,
                                             _P]),
     "quasar_tensor_amax": (_I, [_P, _I64, _P, _P]),
+    "quasar_linear": (_I, [_P, _I64, _P, _I64, _P, _I, _P, _I64, _I64, _I64, _I64, _P, _I, _I64,
+                           _P, _I64, _P]),
+    "quasar_linear_grad_input": (_I, [_P, _I64, _P, _I64, _P, _I64, _I, _P, _I64, _I64, _I64, _I64,
+                                      _P, _I, _I64, _P]),
+    "quasar_linear_grad_weight": (_I, [_P, _I64, _P, _I64, _I64, _I64, _I64, _P, _I, _I64, _P,
+                                       _P]),
+    "quasar_activation_grad": (_I, [_P, _I64, _P, _I64, _I, _I64, _I64, _P, _I64, _P]),
+    "quasar_top_logits": (_I, [_P, _I, _I64, _I64, _I64, _I, _F, _P, _P, _P, _P]),
+    "quasar_distill_top": (_I, [_P, _I, _I64, _I64, _I64, _P, _P, _I, _P, _P, _F, _P, _P, _P, _I64,
+                                _P]),
+    "quasar_distill_top_backward": (_I, [_P, _I, _I64, _I64, _I64, _P, _P, _I, _P, _P, _P, _F, _P,
+                                         _I64, _P]),
     "quasar_get_device_status": (_I, [_P]),
     "quasar_debug_force_timeout": (None, [_I64]),
     "quasar_debug_set_stats": (None, [_P]),
@@ -367,6 +379,71 @@ def quasar_recon_nvfp4(w, g, v, beta2, clip, rows, cols, tensor_amax, r, codes, 
 
 def quasar_tensor_amax(w, n, amax_out, stream=None) -> QuasarStatus:
     return QuasarStatus(load().quasar_tensor_amax(_ptr(w), n, _ptr(amax_out), _stream(stream)))
+
+
+# quasar_activation
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+
+
+def _act_code(activation):
+    """The enumerator of an activation's name (raw integers pass through
+    unchecked, for the library's own validation)."""
+    return ACTIVATIONS[activation] if isinstance(activation, str) else int(activation)
+
+
+def quasar_linear(x, ld_x, r, ld_r, bias, activation, residual, ld_residual, tokens, features,
+                  inputs, y, y_dtype, ld_y, pre=None, ld_pre=0, stream=None) -> QuasarStatus:
+    return QuasarStatus(load().quasar_linear(
+        _ptr(x), ld_x, _ptr(r), ld_r, _ptr(bias), _act_code(activation), _ptr(residual),
+        ld_residual, tokens, features, inputs, _ptr(y), y_dtype, ld_y, _ptr(pre), ld_pre,
+        _stream(stream)))
+
+
+def quasar_linear_grad_input(dz, ld_dz, r, ld_r, pre_in, ld_pre_in, activation_in, residual,
+                             ld_residual, tokens, features, inputs, dx, dx_dtype, ld_dx,
+                             stream=None) -> QuasarStatus:
+    return QuasarStatus(load().quasar_linear_grad_input(
+        _ptr(dz), ld_dz, _ptr(r), ld_r, _ptr(pre_in), ld_pre_in, _act_code(activation_in),
+        _ptr(residual), ld_residual, tokens, features, inputs, _ptr(dx), dx_dtype, ld_dx,
+        _stream(stream)))
+
+
+def quasar_linear_grad_weight(dz, ld_dz, x, ld_x, tokens, features, inputs, dr, dr_dtype, ld_dr,
+                              dbias=None, stream=None) -> QuasarStatus:
+    return QuasarStatus(load().quasar_linear_grad_weight(
+        _ptr(dz), ld_dz, _ptr(x), ld_x, tokens, features, inputs, _ptr(dr), dr_dtype, ld_dr,
+        _ptr(dbias), _stream(stream)))
+
+
+def quasar_activation_grad(dy, ld_dy, pre, ld_pre, activation, rows, cols, dz, ld_dz,
+                           stream=None) -> QuasarStatus:
+    return QuasarStatus(load().quasar_activation_grad(
+        _ptr(dy), ld_dy, _ptr(pre), ld_pre, _act_code(activation), rows, cols, _ptr(dz), ld_dz,
+        _stream(stream)))
+
+
+def quasar_top_logits(logits, dtype, ld, rows, vocab, k, temperature, values, indices, lse=None,
+                      stream=None) -> QuasarStatus:
+    return QuasarStatus(load().quasar_top_logits(
+        _ptr(logits), dtype, ld, rows, vocab, k, temperature, _ptr(values), _ptr(indices),
+        _ptr(lse), _stream(stream)))
+
+
+def quasar_distill_top(logits, dtype, ld, rows, vocab, indices, values, k, teacher_lse, row_weight,
+                       temperature, loss, stats=None, grad=None, ld_grad=0,
+                       stream=None) -> QuasarStatus:
+    return QuasarStatus(load().quasar_distill_top(
+        _ptr(logits), dtype, ld, rows, vocab, _ptr(indices), _ptr(values), k, _ptr(teacher_lse),
+        _ptr(row_weight), temperature, _ptr(loss), _ptr(stats), _ptr(grad), ld_grad,
+        _stream(stream)))
+
+
+def quasar_distill_top_backward(logits, dtype, ld, rows, vocab, indices, values, k, teacher_lse,
+                                stats, row_weight, temperature, grad, ld_grad,
+                                stream=None) -> QuasarStatus:
+    return QuasarStatus(load().quasar_distill_top_backward(
+        _ptr(logits), dtype, ld, rows, vocab, _ptr(indices), _ptr(values), k, _ptr(teacher_lse),
+        _ptr(stats), _ptr(row_weight), temperature, _ptr(grad), ld_grad, _stream(stream)))
 
 
 def quasar_get_device_status(stream=None) -> QuasarStatus:
