@@ -10,7 +10,7 @@ clears that word after synchronising the stream, and callers that must know
 their outputs are whole call it once after their last reconstruction."""
 from __future__ import annotations
 
-import contextlib
+import functools
 
 import torch
 
@@ -295,13 +295,34 @@ def tensor_amax(w, stream=None):
 # -- operators around the reconstruction -----------------------------------------
 #
 # Matrices are 2-D CUDA tensors whose rows are contiguous (any row stride).
-# Outputs and scratch are allocated on the stream the call runs on: pass
-# ``stream`` as a torch stream, or run under ``torch.cuda.stream``.
+# Each call takes a ``stream`` (a torch stream or a handle; None: the current
+# one); its outputs and scratch are allocated on the stream it runs on.  The
+# checks are kept to a few attribute reads: a call with a handful of tokens
+# runs for less time on the GPU than a careless one takes on the host.
+
+_FLOATS = (torch.bfloat16, torch.float32)
+_CODES = {torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _on_stream(call):
+    """Run ``call`` with the stream it is given as the current one."""
+    @functools.wraps(call)
+    def run(*args, stream=None, **kwargs):
+        if stream is None:
+            return call(*args, **kwargs)
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+        with torch.cuda.stream(stream):
+            return call(*args, **kwargs)
+    return run
+
 
 def _matrix(t, name, shape=None, dtypes=(torch.bfloat16,)):
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    """Check a matrix; returns its row stride (a single row's: its length
+    rounded up to what the products' operands need)."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
         raise ValueError(f"{name} must be a 2-D tensor with contiguous rows")
-    if not t.is_cuda or t.dtype not in dtypes:
+    if t.dtype not in dtypes or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor of dtype {' or '.join(map(str, dtypes))}")
     if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
@@ -309,18 +330,13 @@ def _matrix(t, name, shape=None, dtypes=(torch.bfloat16,)):
 
 
 def _ld(t):
-    """Row stride; a single row's is whatever a whole number of 8 elements needs."""
     rows, cols = t.shape
     return t.stride(0) if rows > 1 else -(-cols // 8) * 8
 
 
-def _vector(t, name, n, dtype=torch.float32):
-    if t.dim() != 1 or t.shape[0] != n or not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous CUDA tensor of {n} values of {dtype}")
-
-
-_FLOATS = (torch.bfloat16, torch.float32)
-_CODES = {torch.bfloat16: BF16, torch.float32: F32}
+def _vector(t, name, n):
+    if t.dim() != 1 or t.shape[0] != n or t.dtype != torch.float32 or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous fp32 CUDA tensor of {n} values")
 
 
 def _float_code(dtype, name):
@@ -329,54 +345,10 @@ def _float_code(dtype, name):
     return _CODES[dtype]
 
 
-def _activation(name):
+def _act_code(name):
     if name not in ACTIVATIONS:
         raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}")
-
-
-def _on(stream):
-    """Allocations made inside belong to the stream the call runs on."""
-    if stream is None:
-        return contextlib.nullcontext()
-    if isinstance(stream, int):
-        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
-    return torch.cuda.stream(stream)
-
-
-def _for_products(t, stream):
-    """t itself if the products can read it, else a copy whose rows start at
-    16-byte boundaries."""
-    if t.data_ptr() % 16 == 0 and _ld(t) % 8 == 0:
-        return t
-    return activation_grad(t, None, "none", stream=stream)
-
-
-def linear(x, r, *, bias=None, activation="none", residual=None, out_dtype=torch.bfloat16,
-           save_pre=False, stream=None):
-    """z = x r^T + bias, y = activation(z) + residual.
-
-    x: bf16 [tokens, inputs]; r: bf16 [features, inputs] (a reconstruction);
-    bias: fp32 [features]; residual: [tokens, features] of out_dtype;
-    activation: "none", "relu", "silu" or "gelu".  Returns a dict with y and,
-    with save_pre, pre (z in bf16, in storage whose rows the products can
-    read)."""
-    ld_x = _matrix(x, "x")
-    tokens, inputs = x.shape
-    ld_r = _matrix(r, "r")
-    features = r.shape[0]
-    if r.shape[1] != inputs:
-        raise ValueError(f"x has {inputs} inputs, r {r.shape[1]}")
-    code = _float_code(out_dtype, "out_dtype")
-    _activation(activation)
-    if bias is not None:
-        _vector(bias, "bias", features)
-    ld_res = 0 if residual is None else _matrix(residual, "residual", (tokens, features), (out_dtype,))
-    with _on(stream):
-        y = torch.empty((tokens, features), dtype=out_dtype, device=x.device)
-        pre = _rows_of_8(tokens, features, x.device) if save_pre else None
-    _check(quasar_linear(x, ld_x, r, ld_r, bias, activation, residual, ld_res, tokens, features,
-                         inputs, y, code, features, pre, _ld(pre) if save_pre else 0, stream=stream))
-    return {"y": y, "pre": pre} if save_pre else {"y": y}
+    return ACTIVATIONS[name]
 
 
 def _rows_of_8(rows, cols, device):
@@ -385,99 +357,135 @@ def _rows_of_8(rows, cols, device):
     return wide if wide.shape[1] == cols else wide[:, :cols]
 
 
-def activation_grad(dy, pre, activation, *, stream=None):
+@_on_stream
+def linear(x, r, *, bias=None, activation="none", residual=None, out_dtype=torch.bfloat16,
+           save_pre=False):
+    """z = x r^T + bias, y = activation(z) + residual.
+
+    x: bf16 [tokens, inputs]; r: bf16 [features, inputs] (a reconstruction);
+    both 16-byte aligned with row strides of a multiple of 8; bias: fp32
+    [features]; residual: [tokens, features] of out_dtype; activation: "none",
+    "relu", "silu" or "gelu".  Returns a dict with y and, with save_pre, pre
+    (z in bf16, in storage whose rows the products can read)."""
+    ld_x, ld_r = _matrix(x, "x"), _matrix(r, "r")
+    tokens, inputs = x.shape
+    features = r.shape[0]
+    if r.shape[1] != inputs:
+        raise ValueError(f"x has {inputs} inputs, r {r.shape[1]}")
+    code, act = _float_code(out_dtype, "out_dtype"), _act_code(activation)
+    ld_res = ld_pre = 0
+    if bias is not None:
+        _vector(bias, "bias", features)
+    if residual is not None:
+        ld_res = _matrix(residual, "residual", (tokens, features), (out_dtype,))
+    y = torch.empty((tokens, features), dtype=out_dtype, device=x.device)
+    out = {"y": y}
+    pre = None
+    if save_pre:
+        out["pre"] = pre = _rows_of_8(tokens, features, x.device)
+        ld_pre = _ld(pre)
+    _check(quasar_linear(x, ld_x, r, ld_r, bias, act, residual, ld_res, tokens, features, inputs, y,
+                         code, features, pre, ld_pre))
+    return out
+
+
+@_on_stream
+def activation_grad(dy, pre, activation):
     """dz = dy * activation'(pre) in bf16, in storage whose rows the products
     can read ("none": a copy; pre is not used)."""
     ld_dy = _matrix(dy, "dy")
-    _activation(activation)
-    ld_pre = 0 if activation == "none" else _matrix(pre, "pre", dy.shape)
+    act = _act_code(activation)
+    if activation == "none":
+        pre = None
+    ld_pre = 0 if pre is None else _matrix(pre, "pre", dy.shape)
     rows, cols = dy.shape
-    with _on(stream):
-        dz = _rows_of_8(rows, cols, dy.device)
-    _check(quasar_activation_grad(dy, ld_dy, pre if activation != "none" else None, ld_pre,
-                                  activation, rows, cols, dz, _ld(dz), stream=stream))
+    dz = _rows_of_8(rows, cols, dy.device)
+    _check(quasar_activation_grad(dy, ld_dy, pre, ld_pre, act, rows, cols, dz, _ld(dz)))
     return dz
 
 
+@_on_stream
 def linear_backward(dz, x, r, *, dx=True, dr=True, bias=False, pre_in=None, activation_in="none",
-                    residual=None, dx_dtype=torch.bfloat16, dr_dtype=torch.bfloat16, stream=None):
+                    residual=None, dx_dtype=torch.bfloat16, dr_dtype=torch.bfloat16):
     """Gradients of ``linear`` from dz (bf16 [tokens, features], the gradient
     at z; see ``activation_grad`` for a layer whose own output is activated).
 
     dx = (dz r) * activation_in'(pre_in) + residual, the gradient at the z the
     input x was activated from (pre_in None: at x itself); dr = dz^T x, the g
     the next reconstruction reads; dbias = the column sums of dz (with bias).
-    Returns a dict of those asked for."""
-    _matrix(dz, "dz")
+    Returns a dict of those asked for.  A dz whose rows the products cannot
+    read is copied first."""
+    ld_dz, ld_x = _matrix(dz, "dz"), _matrix(x, "x")
     tokens, features = dz.shape
-    ld_x = _matrix(x, "x")
     inputs = x.shape[1]
     if x.shape[0] != tokens:
         raise ValueError(f"dz has {tokens} tokens, x {x.shape[0]}")
     ld_r = _matrix(r, "r", (features, inputs))
-    _activation(activation_in)
+    act = _act_code(activation_in)
     if (pre_in is None) != (activation_in == "none"):
         raise ValueError("pre_in and activation_in go together")
     ld_pre = 0 if pre_in is None else _matrix(pre_in, "pre_in", (tokens, inputs))
     ld_res = 0 if residual is None else _matrix(residual, "residual", (tokens, inputs), (dx_dtype,))
     dx_code, dr_code = _float_code(dx_dtype, "dx_dtype"), _float_code(dr_dtype, "dr_dtype")
-    dz = _for_products(dz, stream)
-    ld_dz = _ld(dz)
+    if ld_dz % 8 or dz.data_ptr() % 16:
+        dz = activation_grad(dz, None, "none")
+        ld_dz = _ld(dz)
+    device = dz.device
     out = {}
-    with _on(stream):
-        if dx:
-            out["dx"] = torch.empty((tokens, inputs), dtype=dx_dtype, device=dz.device)
-        if dr:
-            out["dr"] = torch.empty((features, inputs), dtype=dr_dtype, device=dz.device)
-        if bias:
-            out["dbias"] = torch.empty(features, dtype=torch.float32, device=dz.device)
     if dx:
-        _check(quasar_linear_grad_input(dz, ld_dz, r, ld_r, pre_in, ld_pre, activation_in, residual,
-                                        ld_res, tokens, features, inputs, out["dx"], dx_code, inputs,
-                                        stream=stream))
+        out["dx"] = to = torch.empty((tokens, inputs), dtype=dx_dtype, device=device)
+        _check(quasar_linear_grad_input(dz, ld_dz, r, ld_r, pre_in, ld_pre, act, residual, ld_res,
+                                        tokens, features, inputs, to, dx_code, inputs))
     if dr or bias:
-        _check(quasar_linear_grad_weight(dz, ld_dz, x, ld_x, tokens, features, inputs,
-                                         out.get("dr"), dr_code, inputs, out.get("dbias"),
-                                         stream=stream))
+        to = dbias = None
+        if dr:
+            out["dr"] = to = torch.empty((features, inputs), dtype=dr_dtype, device=device)
+        if bias:
+            out["dbias"] = dbias = torch.empty(features, dtype=torch.float32, device=device)
+        _check(quasar_linear_grad_weight(dz, ld_dz, x, ld_x, tokens, features, inputs, to, dr_code,
+                                         inputs, dbias))
     return out
 
 
-def top_logits(logits, k, *, temperature=1.0, lse=True, stream=None):
-    """Each row's k largest logits (bf16 or fp32 [rows, vocab]), largest
-    first, equal values by the lowest index.  Returns a dict with values
-    (fp32 [rows, k]), indices (int32) and, with lse, the row's
+@_on_stream
+def top_logits(logits, k, *, temperature=1.0, lse=True):
+    """Each row's k largest logits (bf16 or fp32 [rows, vocab], k up to 256),
+    largest first, equal values by the lowest index.  Returns a dict with
+    values (fp32 [rows, k]), indices (int32) and, with lse, the row's
     log sum exp(logits / temperature)."""
-    ld = _matrix(logits, "logits", dtypes=_FLOATS)
+    ld = _matrix(logits, "logits", None, _FLOATS)
     rows, vocab = logits.shape
-    with _on(stream):
-        values = torch.empty((rows, k), dtype=torch.float32, device=logits.device)
-        indices = torch.empty((rows, k), dtype=torch.int32, device=logits.device)
-        sums = torch.empty(rows, dtype=torch.float32, device=logits.device) if lse else None
-    _check(quasar_top_logits(logits, _CODES[logits.dtype], max(ld, vocab), rows, vocab, k, temperature,
-                             values, indices, sums, stream=stream))
+    device = logits.device
+    values = torch.empty((rows, k), dtype=torch.float32, device=device)
+    indices = torch.empty((rows, k), dtype=torch.int32, device=device)
     out = {"values": values, "indices": indices}
+    sums = None
     if lse:
-        out["lse"] = sums
+        out["lse"] = sums = torch.empty(rows, dtype=torch.float32, device=device)
+    _check(quasar_top_logits(logits, _CODES[logits.dtype], ld, rows, vocab, k, temperature, values,
+                             indices, sums))
     return out
 
 
 def _teacher(logits, indices, values, teacher_lse, row_weight):
-    ld = _matrix(logits, "logits", dtypes=_FLOATS)
+    ld = _matrix(logits, "logits", None, _FLOATS)
     rows = logits.shape[0]
-    k = indices.shape[1] if indices.dim() == 2 else 0
-    for t, name, dtype in ((indices, "indices", torch.int32), (values, "values", torch.float32)):
-        _matrix(t, name, (rows, k), (dtype,))
-        if not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
+    if indices.dim() != 2 or indices.shape[0] != rows or indices.dtype != torch.int32 or \
+            not indices.is_cuda or not indices.is_contiguous():
+        raise ValueError("indices must be a contiguous int32 CUDA tensor [rows, k]")
+    if values.shape != indices.shape or values.dtype != torch.float32 or not values.is_cuda or \
+            not values.is_contiguous():
+        raise ValueError("values must be a contiguous fp32 CUDA tensor of the shape of indices")
     if teacher_lse is not None:
         _vector(teacher_lse, "teacher_lse", rows)
     if row_weight is not None:
         _vector(row_weight, "row_weight", rows)
-    return ld, k
+    return ld, indices.shape[1]
 
 
+@_on_stream
 def distill_top(logits, indices, values, *, teacher_lse=None, row_weight=None, temperature=1.0,
-                grad=True, stats=False, out=None, stream=None):
+                grad=True, stats=False, out=None):
     """Forward KL divergence of the student's logits (bf16 or fp32 [rows,
     vocab]) from a teacher's top entries (``top_logits``: indices, values and,
     for the mass outside them, its lse), and the gradient of
@@ -489,26 +497,28 @@ def distill_top(logits, indices, values, *, teacher_lse=None, row_weight=None, t
     skipped: loss and gradient 0."""
     ld, k = _teacher(logits, indices, values, teacher_lse, row_weight)
     rows, vocab = logits.shape
-    if out is not None:
-        _matrix(out, "out", logits.shape, (logits.dtype,))
-    with _on(stream):
-        loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
-        kept = torch.empty((rows, 2), dtype=torch.float32, device=logits.device) if stats else None
-        if grad and out is None:
-            out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
-    _check(quasar_distill_top(logits, _CODES[logits.dtype], ld, rows, vocab, indices, values, k,
-                              teacher_lse, row_weight, temperature, loss, kept,
-                              out if grad else None, _ld(out) if grad else 0, stream=stream))
+    device = logits.device
+    loss = torch.empty(rows, dtype=torch.float32, device=device)
     made = {"loss": loss}
+    kept, ld_out = None, 0
     if grad:
+        if out is None:
+            out, ld_out = torch.empty((rows, vocab), dtype=logits.dtype, device=device), vocab
+        else:
+            ld_out = _matrix(out, "out", logits.shape, (logits.dtype,))
         made["grad"] = out
+    else:
+        out = None
     if stats:
-        made["stats"] = kept
+        made["stats"] = kept = torch.empty((rows, 2), dtype=torch.float32, device=device)
+    _check(quasar_distill_top(logits, _CODES[logits.dtype], ld, rows, vocab, indices, values, k,
+                              teacher_lse, row_weight, temperature, loss, kept, out, ld_out))
     return made
 
 
+@_on_stream
 def distill_top_backward(logits, indices, values, stats, row_weight, *, teacher_lse=None,
-                         temperature=1.0, out=None, stream=None):
+                         temperature=1.0, out=None):
     """The gradient of sum(row_weight * loss) from the statistics a
     ``distill_top(..., stats=True)`` call kept."""
     ld, k = _teacher(logits, indices, values, teacher_lse, row_weight)
@@ -517,11 +527,10 @@ def distill_top_backward(logits, indices, values, stats, row_weight, *, teacher_
     if not stats.is_contiguous():
         raise ValueError("stats must be contiguous")
     if out is None:
-        with _on(stream):
-            out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+        out, ld_out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device), vocab
     else:
-        _matrix(out, "out", logits.shape, (logits.dtype,))
+        ld_out = _matrix(out, "out", logits.shape, (logits.dtype,))
     _check(quasar_distill_top_backward(logits, _CODES[logits.dtype], ld, rows, vocab, indices,
                                        values, k, teacher_lse, stats, row_weight, temperature, out,
-                                       _ld(out), stream=stream))
+                                       ld_out))
     return out

@@ -22,6 +22,23 @@ const void* product_tile_kernel(int bn, bool a_mn, bool b_mn)
     return nullptr;
 }
 
+// The kernel of paired 256 x 256 tiles; nullptr if there is none.
+const void* product_pair_kernel(bool a_mn, bool b_mn, bool promote)
+{
+#define QUASAR_PAIR(am, bm, pr) \
+    if (a_mn == am && b_mn == bm && promote == pr) return reinterpret_cast<const void*>(&k_product_pair<am, bm, pr>);
+    QUASAR_PAIR(false, false, false)
+    QUASAR_PAIR(false, false, true)
+    QUASAR_PAIR(true, false, false)
+    QUASAR_PAIR(true, false, true)
+    QUASAR_PAIR(true, true, false)
+    QUASAR_PAIR(true, true, true)
+#undef QUASAR_PAIR
+    return nullptr;
+}
+
+size_t product_pair_smem() { return 1024 + kPairStages * kPairStageBytes + (2 * kPairStages + 6) * 8 + 16; }
+
 const void* column_sum_kernel() { return reinterpret_cast<const void*>(&k_column_sum); }
 const void* activation_grad_kernel() { return reinterpret_cast<const void*>(&k_activation_grad); }
 

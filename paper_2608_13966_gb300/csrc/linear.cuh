@@ -244,6 +244,7 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ Pr
         for (int c = 0; c < BN; c += 16) {
             float v[16];
             if (nkb > 0) {
+                __syncwarp();
                 tmem_ld16(mine + c, v);
             } else {
 #pragma unroll
@@ -282,6 +283,225 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ Pr
     tc_fence_before();
     __syncthreads();
     if (warp == 5) tmem_free<1>(tmem, kColumns);
+}
+
+// -- pairs of CTAs ---------------------------------------------------------------
+
+// 256 x 256 tiles, two CTAs (one on each SM of a pair) a tile, persistent.
+// Each CTA keeps its 128 rows of A and half of B's columns in shared memory;
+// one thread of the pair's first CTA issues the matrix instructions of both,
+// which read the two halves of B from both memories, so an operand byte is
+// fetched from L2 once for 256 rows or columns.  The accumulators (128 lanes x
+// 256 columns a CTA) use half of tensor memory: the next tile is multiplied
+// into the other half while the epilogue drains this one.
+//
+// PROMOTE: fp32 results.  The tensor core truncates as it accumulates, an
+// error that grows with the number of instructions; so every kPromoteBlocks
+// blocks of the reduction go to a fresh accumulator, and the epilogue adds
+// the parts up in registers, rounding to nearest.
+//
+// Warps: 0-7 epilogue (lane quadrant w % 4, column half w / 4), 8 copies, 9
+// matrix instructions.
+constexpr int kPairCols = 256;
+constexpr int kPairThreads = 320;
+constexpr int kPairStages = 6;
+constexpr int kPromoteBlocks = 4;
+constexpr int kPairGroup = 8;  // column tiles walked together, for operand reuse in L2
+constexpr uint32_t kPairStageBytes = 2 * kTileABytes;
+
+__device__ __forceinline__ void arrive_peer(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+template <bool A_MN, bool B_MN, bool PROMOTE>
+__global__ void __launch_bounds__(kPairThreads, 1) k_product_pair(const __grid_constant__ ProductParams p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + kPairStages * kPairStageBytes);  // first CTA's: both halves landed
+    uint64_t* empty = full + kPairStages;   // each CTA's
+    uint64_t* acc_full = empty + kPairStages;  // [2], each CTA's
+    uint64_t* acc_empty = acc_full + 2;        // [2], first CTA's: 16 epilogue warps
+    uint64_t* drained = acc_empty + 2;
+    uint64_t* never = drained + 1;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(never + 1);
+    volatile uint32_t* gone = tmem_slot + 1;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int pair = (int)(blockIdx.x >> 1), n_pairs = (int)(gridDim.x >> 1);
+    const int64_t n_tiles = (int64_t)p.tiles_row * p.tiles_col;
+    const int nkb = p.k_blocks;
+    const int per_part = PROMOTE ? kPromoteBlocks : nkb;
+    const int n_parts = (nkb + per_part - 1) / per_part;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kPairStages; ++s) {
+            mbar_init(full + s, 1);
+            mbar_init(empty + s, 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(acc_full + b, 1);
+            mbar_init(acc_empty + b, 16);
+        }
+        mbar_init(drained, 1);
+        mbar_init(never, 1);
+        *gone = 0;
+        mbar_init_fence();
+    }
+    if (warp == 9) tmem_alloc<2>(tmem_slot, 512);
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    // tile t: groups of kPairGroup column tiles, row tiles within a group
+    auto tile_at = [&](int64_t t, int64_t& row0, int64_t& col0) {
+        const int64_t group = t / ((int64_t)kPairGroup * p.tiles_row);
+        const int64_t in = t - group * kPairGroup * p.tiles_row;
+        const int64_t left = p.tiles_col - group * kPairGroup;
+        const int wide = (int)(left < kPairGroup ? left : kPairGroup);
+        row0 = in / wide * 256 + 128 * rank;  // of this CTA
+        col0 = (group * kPairGroup + in % wide) * kPairCols;
+    };
+
+    if (warp == 8 && lane == 0) {
+        if (p.force_timeout_ns) role_wait(never, 0, gone, p.force_timeout_ns, p.status);
+        uint32_t it = 0;
+        for (int64_t t = pair; t < n_tiles && !*gone; t += n_pairs) {
+            int64_t row0, col0;
+            tile_at(t, row0, col0);
+            const int bcol = (int)col0 + 128 * (int)rank;
+            for (int kb = 0; kb < nkb; ++kb, ++it) {
+                const int s = it % kPairStages;
+                if (it >= kPairStages &&
+                    !role_wait(empty + s, (it / kPairStages - 1) & 1, gone, p.timeout_ns, p.status))
+                    break;
+                const uint32_t a = smem_u32(smem + (size_t)s * kPairStageBytes), b = a + kTileABytes;
+                const uint32_t bar = peer_addr(smem_u32(full + s), 0);
+                if (rank == 0) mbar_arrive_expect_tx(full + s, 2 * kPairStageBytes);
+                const int k = kb * kTileK;
+                if (A_MN) {
+                    tile_g2s_pair(a, &p.a, (int)row0, k, bar);
+                    tile_g2s_pair(a + 8192, &p.a, (int)row0 + 64, k, bar);
+                } else {
+                    tile_g2s_pair(a, &p.a, k, (int)row0, bar);
+                }
+                if (B_MN) {
+                    tile_g2s_pair(b, &p.b, bcol, k, bar);
+                    tile_g2s_pair(b + 8192, &p.b, bcol + 64, k, bar);
+                } else {
+                    tile_g2s_pair(b, &p.b, k, bcol, bar);
+                }
+            }
+        }
+        // given up: what is in flight lands before the memory is let go (the
+        // second CTA's copies report to the first, which waits for both)
+        if (*gone && rank == 0)
+            for (uint32_t j = it > kPairStages ? it - kPairStages : 0; j < it; ++j)
+                mbar_wait_bounded(full + j % kPairStages, (j / kPairStages) & 1, p.timeout_ns);
+    } else if (warp == 9 && lane == 0 && rank == 0) {
+        constexpr uint32_t desc = mma_desc(256, kPairCols, A_MN, B_MN);
+        uint32_t it = 0, part = 0;
+        bool ok = true;
+        for (int64_t t = pair; t < n_tiles && ok; t += n_pairs) {
+            for (int kb = 0; kb < nkb && ok; ++part) {
+                const uint32_t buf = part & 1;
+                if (part >= 2 && !role_wait(acc_empty + buf, (part / 2 - 1) & 1, gone, p.timeout_ns, p.status)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t d = tmem + buf * kPairCols;
+                const int end = kb + per_part < nkb ? kb + per_part : nkb;
+                for (bool add = false; kb < end; ++kb, ++it) {
+                    const int s = it % kPairStages;
+                    if (!role_wait(full + s, (it / kPairStages) & 1, gone, p.timeout_ns, p.status)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t a = smem_u32(smem + (size_t)s * kPairStageBytes);
+                    uint64_t da = operand_desc(a, A_MN), db = operand_desc(a + kTileABytes, B_MN);
+#pragma unroll
+                    for (int k = 0; k < kTileK / 16; ++k) {
+                        mma_bf16<2>(d, da, db, desc, add);
+                        add = true;
+                        da += k_step(A_MN);
+                        db += k_step(B_MN);
+                    }
+                    mma_commit_pair(smem_u32(empty + s));
+                }
+                if (ok) mma_commit_pair(smem_u32(acc_full + buf));
+            }
+        }
+        mma_commit_local_pair(smem_u32(drained));
+        mbar_wait_bounded(drained, 0, p.timeout_ns);
+    } else if (warp < 8) {
+        const int quad = warp & 3, half = warp >> 2;
+        const uint32_t mine = tmem + ((uint32_t)(32 * quad) << 16) + 128 * half;
+        uint32_t part = 0;
+        for (int64_t t = pair; t < n_tiles; t += n_pairs) {
+            int64_t row0, col0;
+            tile_at(t, row0, col0);
+            col0 += 128 * half;
+            const int64_t i = row0 + 32 * quad + lane;
+            const float bias = p.e.bias && i < p.rows ? p.e.bias[i] : 0.0f;
+            float acc[PROMOTE ? 128 : 1];
+            bool ok = true;
+            for (int q = 0; q < n_parts && ok; ++q, ++part) {
+                const uint32_t buf = part & 1;
+                ok = role_wait(acc_full + buf, (part / 2) & 1, gone, p.timeout_ns, p.status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                if constexpr (PROMOTE) {
+#pragma unroll
+                    for (int c = 0; c < 128; c += 16) {
+                        float v[16];
+                        __syncwarp();
+                        tmem_ld16(mine + buf * kPairCols + c, v);
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) acc[c + x] = q == 0 ? v[x] : acc[c + x] + v[x];
+                    }
+                } else {
+                    for (int c = 0; c < 128; c += 32) {
+                        float v[32];
+                        __syncwarp();
+                        tmem_ld32(mine + buf * kPairCols + c, v);
+                        if (c == 96) {  // drained: the next part may be multiplied into it
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) arrive_peer(peer_addr(smem_u32(acc_empty + buf), 0));
+                        }
+                        if (col0 + c < p.cols) finish(p.e, v, i, col0 + c, p.rows, p.cols, bias);
+                    }
+                }
+                if constexpr (PROMOTE) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive_peer(peer_addr(smem_u32(acc_empty + buf), 0));
+                }
+            }
+            if (!ok) break;
+            if constexpr (PROMOTE) {
+#pragma unroll
+                for (int c = 0; c < 128; c += 8) {
+                    float v[8];
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) v[x] = acc[c + x];
+                    if (col0 + c < p.cols) finish(p.e, v, i, col0 + c, p.rows, p.cols, bias);
+                }
+            }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();  // neither CTA leaves while the other may still signal it
+    if (warp == 9) tmem_free<2>(tmem, 512);
 }
 
 // -- column sums and activation gradients --------------------------------------

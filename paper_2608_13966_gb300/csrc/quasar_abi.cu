@@ -242,7 +242,8 @@ struct DeviceInfo {
 DeviceInfo g_dev[kMaxDevices];
 std::mutex g_mu;
 
-// Launch configuration of one kernel at one shared-memory size, per device.
+// Launch configuration of one kernel at one shared-memory size, per device
+// (occupancy: CTAs per SM, or clusters on the device for a clustered kernel).
 struct KernelConfig {
     const void* fn = nullptr;
     size_t smem = 0;
@@ -700,6 +701,37 @@ quasar_status host_allow_smem(const void* fn, size_t smem)
     if (cudaGetDevice(&dev) != cudaSuccess) return QUASAR_ERR_CUDA;
     std::lock_guard<std::mutex> lock(g_mu);
     return allow_smem(fn, smem, dev);
+}
+
+quasar_status host_max_clusters(const void* fn, int size, int threads, size_t smem, int* clusters)
+{
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return QUASAR_ERR_CUDA;
+    std::lock_guard<std::mutex> lock(g_mu);
+    for (int i = 0; i < g_ncfg; ++i)
+        if (g_cfg[i].fn == fn && g_cfg[i].dev == dev && g_cfg[i].smem == smem) {
+            *clusters = g_cfg[i].occupancy;
+            return QUASAR_OK;
+        }
+    const quasar_status st = allow_smem(fn, smem, dev);
+    if (st != QUASAR_OK) return st;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)size);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)size;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, fn, &cfg) != cudaSuccess) return QUASAR_ERR_CUDA;
+    if (n < 1) return QUASAR_ERR_UNSUPPORTED;
+    if (g_ncfg < kMaxConfigs) g_cfg[g_ncfg++] = KernelConfig{fn, smem, dev, n};
+    *clusters = n;
+    return QUASAR_OK;
 }
 
 uint64_t host_timeout_ns() { return kDefaultTimeoutNs; }

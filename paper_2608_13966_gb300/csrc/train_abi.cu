@@ -17,6 +17,8 @@
 
 namespace quasar {
 const void* product_tile_kernel(int bn, bool a_mn, bool b_mn);
+const void* product_pair_kernel(bool a_mn, bool b_mn, bool promote);
+size_t product_pair_smem();
 const void* column_sum_kernel();
 const void* activation_grad_kernel();
 const void* distill_kernel(bool f32, bool backward);
@@ -142,6 +144,19 @@ quasar_status product(const Operand& a, const Operand& b, int64_t rows, int64_t 
     p.timeout_ns = host_timeout_ns();
     p.force_timeout_ns = host_forced_timeout_ns();
 
+    const int64_t pair_tiles = ((rows + 255) / 256) * ((cols + 255) / 256);
+    if (depth > 0 && pair_tiles * 2 >= n_sm) {
+        p.tiles_row = (int)((rows + 255) / 256);
+        p.tiles_col = (int)((cols + 255) / 256);
+        if ((st = tile_map(a, a.mn_major ? 64 : 128, &p.a)) != QUASAR_OK) return st;
+        if ((st = tile_map(b, b.mn_major ? 64 : 128, &p.b)) != QUASAR_OK) return st;
+        const void* fn = product_pair_kernel(a.mn_major, b.mn_major, e.out_f32);
+        if (!fn) return QUASAR_ERR_UNSUPPORTED;
+        int pairs = 0;
+        if ((st = host_max_clusters(fn, 2, 320, product_pair_smem(), &pairs)) != QUASAR_OK) return st;
+        pairs = (int)std::min<int64_t>(pair_tiles, pairs);
+        return launch(fn, &p, dim3((unsigned)pairs * 2), 320, 2, product_pair_smem(), stream);
+    }
     int bn = cols <= 16 ? 16 : (cols <= 32 ? 32 : (cols <= 64 ? 64 : 128));
     if (b.mn_major) bn = std::max(bn, 64);
     p.tiles_row = (int)((rows + 127) / 128);

@@ -82,6 +82,8 @@ def load(build_if_missing: bool = True):
     environment variable QUASAR_LIBRARY names another build of the same
     library to load instead (no build step then)."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is not None:
             return _lib
@@ -103,9 +105,7 @@ def load(build_if_missing: bool = True):
 
 def _ptr(x):
     """Device pointer of a tensor, an int, or None."""
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or type(x) is int:
         return x
     return x.data_ptr()
 
@@ -125,11 +125,25 @@ def _dtype_code(t, default=F32):
 
 def _stream(stream):
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
+
+
+def _current_stream():
+    """Handle of the current device's current stream."""
+    global _current_stream
+    import torch
+    try:  # without building a Stream object for every call (2.7 us on the GPU's host)
+        raw, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+        torch.cuda.init()
+        handle = lambda: raw(device())  # noqa: E731
+        handle()
+    except AttributeError:
+        handle = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+    _current_stream = handle
+    return handle()
 
 
 def _clip_array(clip):

@@ -113,6 +113,52 @@ def test_linear_backward(tokens, features, inputs, activation, residual, dx_type
     close(made["dbias"], dz.double().sum(0), dz.double().abs().sum(0), tokens, False)
 
 
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens,features,inputs", [(2311, 2497, 72), (2500, 2304, 1032), (4097, 2200, 8)])
+def test_linear_of_many_tiles(tokens, features, inputs, out):
+    """Enough 256 x 256 tiles for every pair of SMs, with ragged edges."""
+    x, r = rand(tokens, inputs, seed=1), rand(features, inputs, scale=0.05, seed=2)
+    b, res = rand(features, seed=3, dtype=torch.float32), rand(tokens, features, seed=4, dtype=out)
+    made = api.linear(x, r, bias=b, activation="gelu", residual=res, out_dtype=out, save_pre=True)
+    z = x.double() @ r.double().t() + b.double()
+    mag = x.double().abs() @ r.double().abs().t() + b.double().abs()
+    api.check_device()
+    close(made["pre"], z, mag, inputs, True)
+    close(made["y"], ACT["gelu"](z) + res.double(), mag + res.double().abs(), inputs,
+          out == torch.bfloat16)
+
+
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens,features,inputs", [(2311, 2497, 2312), (2305, 2560, 4104)])
+def test_linear_backward_of_many_tiles(tokens, features, inputs, out):
+    dz, x = rand(tokens, features, seed=5), rand(tokens, inputs, seed=6)
+    r = rand(features, inputs, scale=0.05, seed=7)
+    pre, res = rand(tokens, inputs, seed=8), rand(tokens, inputs, seed=9, dtype=out)
+    made = api.linear_backward(dz, x, r, bias=True, pre_in=pre, activation_in="silu", residual=res,
+                               dx_dtype=out, dr_dtype=out)
+    api.check_device()
+    dx = dz.double() @ r.double() * slope(pre.double(), "silu") + res.double()
+    mag = 1.2 * (dz.double().abs() @ r.double().abs()) + res.double().abs()
+    close(made["dx"], dx, mag, features, out == torch.bfloat16)
+    close(made["dr"], dz.double().t() @ x.double(), dz.double().abs().t() @ x.double().abs(),
+          tokens, out == torch.bfloat16)
+    close(made["dbias"], dz.double().sum(0), dz.double().abs().sum(0), tokens, False)
+
+
+def test_a_large_product_whose_wait_runs_out_is_reported():
+    x, r = rand(2311, 72, seed=1), rand(2497, 72, seed=2)
+    want = api.linear(x, r, out_dtype=torch.float32)["y"]
+    api.check_device()
+    Q.quasar_debug_force_timeout(1_000_000)
+    try:
+        api.linear(x, r, out_dtype=torch.float32)
+        assert Q.quasar_get_device_status() == Q.QuasarStatus.ERR_TIMEOUT
+    finally:
+        Q.quasar_debug_force_timeout(0)
+    assert torch.equal(api.linear(x, r, out_dtype=torch.float32)["y"], want)
+    api.check_device()
+
+
 @pytest.mark.parametrize("tokens,features,inputs", [(5, 77, 200), (90, 300, 1032), (513, 640, 128)])
 def test_strides_and_guards(tokens, features, inputs):
     """Strided operands and results; nothing outside the results is written,
