@@ -25,7 +25,6 @@
 namespace quasar {
 
 constexpr int kDistillThreads = 512;
-constexpr float kLog2e = 1.44269504f;
 
 // x / tau - y: the quotient is not rounded before the subtraction (inv_tau is
 // 1 / tau rounded, the second step its remainder)
@@ -68,10 +67,10 @@ __device__ __forceinline__ float teacher_side(const DistillParams& p, int64_t r,
     if (p.teacher_lse) {
         norm = p.teacher_lse[r];
     } else {
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        top = lanes_max(top, 0xffffffffu);
         float s = 0.0f;
         for (int k = lane; k < p.k; k += 32) s += top == neg_inf() ? 0.0f : expf(logp[k] - top);
-        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        s = warp_sum(s);
         norm = s > 0.0f ? top + logf(s) : 0.0f;
     }
     float sum = 0.0f;
@@ -79,31 +78,7 @@ __device__ __forceinline__ float teacher_side(const DistillParams& p, int64_t r,
         logp[k] -= norm;
         sum += expf(logp[k]);
     }
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    return sum;
-}
-
-// Maximum over the CTA's threads; `scratch` holds a float per warp.
-__device__ __forceinline__ float block_max(float x, float* scratch)
-{
-    x = lanes_max(x, 0xffffffffu);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
-    __syncthreads();
-    x = scratch[0];
-    for (int w = 1; w < (int)blockDim.x / 32; ++w) x = fmaxf(x, scratch[w]);
-    return x;
-}
-
-__device__ __forceinline__ float block_sum(float x, float* scratch)
-{
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
-    __syncthreads();
-    x = scratch[0];
-    for (int w = 1; w < (int)blockDim.x / 32; ++w) x += scratch[w];
-    return x;
+    return warp_sum(sum);
 }
 
 // BACKWARD: the gradient from kept statistics (log-sum-exp of z over the
@@ -122,8 +97,8 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill_top(const __grid_co
     float* own = logp + kMaxTop;                            // student logits of the entries held here
     float* all = own + kMaxTop;                             // rank 0: of every entry
     float(*parts)[4] = reinterpret_cast<float(*)[4]>(all + kMaxTop);  // [kRowCtas]
-    float* scratch = reinterpret_cast<float*>(parts + kRowCtas);      // [warps]
-    float* teacher = scratch + 32;                          // P, p_r, listed
+    float* scratch = reinterpret_cast<float*>(parts + kRowCtas);      // [4][warps]
+    float* teacher = scratch + 64;                          // P, p_r
     int32_t* entry = reinterpret_cast<int32_t*>(teacher + 4);  // [kMaxTop]
 
     const int t = threadIdx.x;
@@ -185,39 +160,41 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill_top(const __grid_co
     }
     __syncthreads();
 
-    float m_rest, coef, q_rest, lse;     // of the whole row
-    float m_all = 0.0f, log_s = 0.0f;    // lse = m_all / tau + log_s
+    float m_rest, coef, q_rest;          // of the whole row (backward: m_rest is the rest's lse)
+    float m_all, log_s = 0.0f;           // lse = m_all / tau + log_s (backward: lse = m_all)
     if constexpr (!BACKWARD) {
-        float m = neg_inf(), s = 0.0f;
-        for (int v = t; v < S.n_vecs; v += kDistillThreads) {
-            float x[kN];
-            V::unpack(reinterpret_cast<const uint4*>(slice)[v], x);
-            float top = x[0];
-#pragma unroll
-            for (int j = 1; j < kN; ++j) top = fmaxf(top, x[j]);
-            if (top > m) {
-                s *= ex2((m - top) * c2);
-                m = top;
-            }
-            const float base = m == neg_inf() ? 0.0f : m;
-#pragma unroll
-            for (int j = 0; j < kN; ++j) s += ex2((x[j] - base) * c2);
-        }
-        // the listed entries held here, as a second sum
+        const uint4* vecs = reinterpret_cast<const uint4*>(slice);
+        const int warp = t >> 5, lane = t & 31;
+        const float m = block_max(largest<T>(vecs, S.n_vecs), scratch);
+        const ExpBase at(m, c2);
+        const float s = warp_sum(sum_exponentials<T>(vecs, S.n_vecs, c2, at)) * at.fix;
+        // the listed entries held here, as a second sum (one a thread)
         float m_in = neg_inf(), s_in = 0.0f;
-        for (int k = t; k < p.k; k += kDistillThreads) {
-            const int at = entry[k] >= 0 ? S.slot_of(entry[k]) : -1;
-            if (at >= 0) merge_sum(m_in, s_in, own[k], own[k] == neg_inf() ? 0.0f : 1.0f, c2);
+        if (t < kMaxTop) {
+            const bool here = t < p.k && entry[t] >= 0 && S.slot_of(entry[t]) >= 0;
+            const float x = here ? own[t] : neg_inf();
+            m_in = lanes_max(x, 0xffffffffu);
+            s_in = warp_sum(x == neg_inf() ? 0.0f : exp2f((x - m_in) * c2));
         }
-        const float top = block_max(m, scratch), top_in = block_max(m_in, scratch);
-        s = block_sum(top == neg_inf() ? s : s * ex2((m - top) * c2), scratch);
-        s_in = block_sum(m_in == neg_inf() ? 0.0f : s_in * ex2((m_in - top_in) * c2), scratch);
-        if (t < p.row.ctas) {
-            const uint32_t to = peer_addr(smem_u32(&parts[rank][0]), (uint32_t)t);
-            st_peer(to, top);
-            st_peer(to + 4, s);
-            st_peer(to + 8, top_in);
-            st_peer(to + 12, s_in);
+        if (lane == 0) {
+            scratch[16 + warp] = s;
+            scratch[32 + warp] = m_in;
+            scratch[48 + warp] = s_in;
+        }
+        __syncthreads();
+        if (warp == 0) {
+            constexpr int kW = kDistillThreads / 32;
+            const float sum = warp_sum(lane < kW ? scratch[16 + lane] : 0.0f);
+            const float x = lane < kW ? scratch[32 + lane] : neg_inf();
+            m_in = lanes_max(x, 0xffffffffu);
+            s_in = warp_sum(x == neg_inf() ? 0.0f : scratch[48 + lane] * exp2f((x - m_in) * c2));
+            if (lane < p.row.ctas) {
+                const uint32_t to = peer_addr(smem_u32(&parts[rank][0]), (uint32_t)lane);
+                st_peer(to, m);
+                st_peer(to + 4, sum);
+                st_peer(to + 8, m_in);
+                st_peer(to + 12, s_in);
+            }
         }
         cluster_sync();
         float m_listed = neg_inf(), s_listed = 0.0f, s_rest = 0.0f;
@@ -230,7 +207,6 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill_top(const __grid_co
         m_all = m_rest;
         merge_sum(m_all, s_all, m_listed, s_listed, c2);
         log_s = logf(s_all);
-        lse = m_all * inv_tau + log_s;
         const bool some = m_rest != neg_inf();
         const float log_q_rest = some ? (m_rest - m_all) * inv_tau + (logf(s_rest) - log_s) : neg_inf();
         q_rest = expf(log_q_rest);
@@ -240,45 +216,59 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill_top(const __grid_co
             for (int k = t; k < p.k; k += 32)
                 if (entry[k] >= 0)
                     loss += kl_term(expf(logp[k]), logp[k], (all[k] - m_all) * inv_tau - log_s);
-            for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
+            loss = warp_sum(loss);
             if (t == 0) {
                 loss += kl_term(p_rest, logf(p_rest), log_q_rest);
+                if (m_all == neg_inf()) loss = __int_as_float(0x7F800000);  // q is 0 everywhere
                 p.loss[r] = mass > 0.0f ? loss : 0.0f;
                 if (p.stats) {
-                    p.stats[2 * r] = lse;
-                    p.stats[2 * r + 1] = some ? m_rest * inv_tau + logf(s_rest) : neg_inf();
+                    p.stats[2 * r] = m_all / p.temperature + log_s;
+                    p.stats[2 * r + 1] = some ? m_rest / p.temperature + logf(s_rest) : neg_inf();
                 }
             }
         }
         if (!grad) return;
-        if (!some) m_rest = 0.0f;
     } else {
-        lse = p.stats[2 * r];
+        m_all = p.stats[2 * r];
         const float lse_rest = p.stats[2 * r + 1];
         const bool some = lse_rest != neg_inf();
-        q_rest = some ? expf(lse_rest - lse) : 0.0f;
+        q_rest = some ? expf(lse_rest - m_all) : 0.0f;
         coef = some ? mass * q_rest - p_rest : 0.0f;
         m_rest = some ? lse_rest : 0.0f;
     }
-    const float scale = mass > 0.0f ? weight * inv_tau : 0.0f;
+    // a row without teacher mass, or without a finite logit, has no gradient
+    const bool none = !(mass > 0.0f) || m_all == neg_inf();
+    const float scale = none ? 0.0f : weight * inv_tau;
     coef *= scale;
 
-    // the unlisted entries: coef e^(z - base)
+    // the unlisted entries: coef 2^(x c - base), or coef e^(z - lse) from
+    // kept statistics
     const bool vectors = (reinterpret_cast<uintptr_t>(grad - S.lead) & 15) == 0;
+    const ExpBase at(BACKWARD ? 0.0f : m_rest, c2);
+    coef *= at.fix;
+    const float2 kk = make_float2(coef, coef);
     for (int v = t; v < S.n_vecs; v += kDistillThreads) {
-        float x[kN];
+        constexpr int kP = kN / 2;
+        float2 x[kP];
         V::unpack(reinterpret_cast<const uint4*>(slice)[v], x);
+        if constexpr (BACKWARD) {
 #pragma unroll
-        for (int j = 0; j < kN; ++j)
-            x[j] = coef * (BACKWARD ? ex2(scaled_less(x[j], p.temperature, inv_tau, m_rest) * kLog2e)
-                                    : ex2((x[j] - m_rest) * c2));
+            for (int j = 0; j < kP; ++j)
+                x[j] = make_float2(ex2(scaled_less(x[j].x, p.temperature, inv_tau, m_rest) * kLog2e),
+                                   ex2(scaled_less(x[j].y, p.temperature, inv_tau, m_rest) * kLog2e));
+        } else {
+            at.apply(x, c2);
+        }
+#pragma unroll
+        for (int j = 0; j < kP; ++j) x[j] = __fmul2_rn(kk, x[j]);
         const int64_t s = S.first + (int64_t)v * kN;
         if (vectors && S.whole(v)) {
             __stcs(reinterpret_cast<uint4*>(grad + (s - S.lead)), V::pack(x));
         } else {
 #pragma unroll
             for (int j = 0; j < kN; ++j)
-                if (s + j >= S.begin && s + j < S.end) grad[s + j - S.lead] = V::from_f32(x[j]);
+                if (s + j >= S.begin && s + j < S.end)
+                    grad[s + j - S.lead] = V::from_f32(j & 1 ? x[j / 2].y : x[j / 2].x);
         }
     }
     __syncthreads();
@@ -286,8 +276,9 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill_top(const __grid_co
     for (int k = t; k < p.k; k += kDistillThreads) {
         const int s = entry[k] >= 0 ? S.slot_of(entry[k]) : -1;
         if (s < 0) continue;
-        const float q = BACKWARD ? expf(scaled_less(own[k], p.temperature, inv_tau, lse)) : expf((own[k] - m_all) * inv_tau - log_s);
-        grad[entry[k]] = V::from_f32(scale * (mass * q - expf(logp[k])));
+        const float log_q = BACKWARD ? scaled_less(own[k], p.temperature, inv_tau, m_all)
+                                     : (own[k] - m_all) * inv_tau - log_s;
+        grad[entry[k]] = V::from_f32(none ? 0.0f : scale * (mass * expf(log_q) - expf(logp[k])));
     }
 }
 

@@ -17,24 +17,41 @@ namespace quasar {
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xFF800000); }
 
+// max that keeps a NaN
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// 16 bytes of T: as pairs of floats, and their maximum (bf16: two at a time,
+// four instructions a vector).
 template <typename T>
-struct Vec16;  // 16 bytes of T as floats
+struct Vec16;
 
 template <>
 struct Vec16<float> {
     static constexpr int kN = 4;
-    static __device__ __forceinline__ void unpack(const uint4& x, float (&v)[4])
+    using Max = float;
+    static __device__ __forceinline__ void unpack(const uint4& x, float2 (&v)[2])
     {
-        v[0] = __uint_as_float(x.x);
-        v[1] = __uint_as_float(x.y);
-        v[2] = __uint_as_float(x.z);
-        v[3] = __uint_as_float(x.w);
+        v[0] = make_float2(__uint_as_float(x.x), __uint_as_float(x.y));
+        v[1] = make_float2(__uint_as_float(x.z), __uint_as_float(x.w));
     }
-    static __device__ __forceinline__ uint4 pack(const float (&v)[4])
+    static __device__ __forceinline__ uint4 pack(const float2 (&v)[2])
     {
-        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
-                          __float_as_uint(v[3]));
+        return make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x),
+                          __float_as_uint(v[1].y));
     }
+    static __device__ __forceinline__ Max lowest() { return neg_inf(); }
+    static __device__ __forceinline__ Max larger(const uint4& x)
+    {
+        return max_nan(max_nan(__uint_as_float(x.x), __uint_as_float(x.y)),
+                       max_nan(__uint_as_float(x.z), __uint_as_float(x.w)));
+    }
+    static __device__ __forceinline__ Max larger(Max m, Max n) { return max_nan(m, n); }
+    static __device__ __forceinline__ float value(Max m) { return m; }
     static __device__ __forceinline__ float to_f32(float x) { return x; }
     static __device__ __forceinline__ float from_f32(float x) { return x; }
 };
@@ -42,17 +59,30 @@ struct Vec16<float> {
 template <>
 struct Vec16<__nv_bfloat16> {
     static constexpr int kN = 8;
-    static __device__ __forceinline__ void unpack(const uint4& x, float (&v)[8])
+    using Max = __nv_bfloat162;
+    static __device__ __forceinline__ Max pair(uint32_t x) { return *reinterpret_cast<const Max*>(&x); }
+    static __device__ __forceinline__ void unpack(const uint4& x, float2 (&v)[4])
     {
-        v[0] = bf16lo(x.x), v[1] = bf16hi(x.x);
-        v[2] = bf16lo(x.y), v[3] = bf16hi(x.y);
-        v[4] = bf16lo(x.z), v[5] = bf16hi(x.z);
-        v[6] = bf16lo(x.w), v[7] = bf16hi(x.w);
+        v[0] = make_float2(bf16lo(x.x), bf16hi(x.x));
+        v[1] = make_float2(bf16lo(x.y), bf16hi(x.y));
+        v[2] = make_float2(bf16lo(x.z), bf16hi(x.z));
+        v[3] = make_float2(bf16lo(x.w), bf16hi(x.w));
     }
-    static __device__ __forceinline__ uint4 pack(const float (&v)[8])
+    static __device__ __forceinline__ uint4 pack(const float2 (&v)[4])
     {
-        return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
-                          pack_bf16x2(v[6], v[7]));
+        return make_uint4(pack_bf16x2(v[0].x, v[0].y), pack_bf16x2(v[1].x, v[1].y),
+                          pack_bf16x2(v[2].x, v[2].y), pack_bf16x2(v[3].x, v[3].y));
+    }
+    static __device__ __forceinline__ Max lowest() { return pair(0xFF80FF80u); }
+    static __device__ __forceinline__ Max larger(const uint4& x)
+    {
+        return __hmax2_nan(__hmax2_nan(pair(x.x), pair(x.y)), __hmax2_nan(pair(x.z), pair(x.w)));
+    }
+    static __device__ __forceinline__ Max larger(Max m, Max n) { return __hmax2_nan(m, n); }
+    static __device__ __forceinline__ float value(Max m)
+    {
+        const uint32_t x = *reinterpret_cast<const uint32_t*>(&m);
+        return max_nan(bf16lo(x), bf16hi(x));
     }
     static __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
     static __device__ __forceinline__ __nv_bfloat16 from_f32(float x) { return __float2bfloat16_rn(x); }
@@ -129,7 +159,12 @@ struct RowSlice {
     }
 };
 
-// Larger-of-maxima merge of two (maximum, sum of exp2((x - maximum) c)).
+constexpr float kLog2e = 1.44269504f;
+constexpr float kLn2 = 0.69314718f;
+
+// Sums of exponentials are kept as (m, s), meaning sum e^(x / tau) = s e^(m /
+// tau) with m one of the logits; c = log2(e) / tau.  m = -inf: nothing was
+// added.
 __device__ __forceinline__ void merge_sum(float& m, float& s, float m2, float s2, float c)
 {
     const float top = fmaxf(m, m2);
@@ -143,6 +178,85 @@ __device__ __forceinline__ float ex2(float x)
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// Maximum and sum over the CTA.  `scratch` holds a float per warp and is not
+// reused without a barrier in between.
+__device__ __forceinline__ float block_max(float x, float* scratch)
+{
+    x = lanes_max(x, 0xffffffffu);
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
+    __syncthreads();
+    return lanes_max(scratch[threadIdx.x & (blockDim.x / 32 - 1)], 0xffffffffu);
+}
+
+__device__ __forceinline__ float warp_sum(float x)
+{
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+
+// 2^((x - m) c) as one multiply-add and one exponential: 2^(x c - base) times
+// fix, with base = m c as rounded and fix = 2^(base - m c), what that rounding
+// took away.  m = -inf (nothing to add): base 0.  Where m c leaves fp32's
+// range (a row masked with the type's lowest value) the subtraction comes
+// first instead.
+struct ExpBase {
+    float base, fix, shift;
+    __device__ __forceinline__ ExpBase(float m, float c)
+    {
+        base = m == neg_inf() ? 0.0f : m * c;
+        fix = m == neg_inf() ? 1.0f : exp2f(-fmaf(m, c, -base));
+        shift = 0.0f;
+        if (isinf(base)) {
+            base = 0.0f;
+            fix = 1.0f;
+            shift = -m;
+        }
+    }
+
+    // the pairs x -> 2^(x c - base)
+    template <int N>
+    __device__ __forceinline__ void apply(float2 (&x)[N], float c) const
+    {
+        const float2 cc = make_float2(c, c), mm = make_float2(-base, -base);
+        if (shift != 0.0f) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) x[j] = __fadd2_rn(x[j], make_float2(shift, shift));
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            x[j] = __ffma2_rn(x[j], cc, mm);
+            x[j] = make_float2(ex2(x[j].x), ex2(x[j].y));
+        }
+    }
+};
+
+// The sum of 2^(x c - base) over this thread's vectors v = t, t + threads, ...
+template <typename T>
+__device__ __forceinline__ float sum_exponentials(const uint4* slice, int n_vecs, float c, const ExpBase& at)
+{
+    float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll 2
+    for (int v = threadIdx.x; v < n_vecs; v += blockDim.x) {
+        float2 x[Vec16<T>::kN / 2];
+        Vec16<T>::unpack(slice[v], x);
+        at.apply(x, c);
+#pragma unroll
+        for (int j = 0; j < Vec16<T>::kN / 2; ++j) s = __fadd2_rn(s, x[j]);
+    }
+    return s.x + s.y;
+}
+
+// This thread's largest logit in the slice.
+template <typename T>
+__device__ __forceinline__ float largest(const uint4* slice, int n_vecs)
+{
+    typename Vec16<T>::Max m = Vec16<T>::lowest();
+#pragma unroll 4
+    for (int v = threadIdx.x; v < n_vecs; v += blockDim.x)
+        m = Vec16<T>::larger(m, Vec16<T>::larger(slice[v]));
+    return Vec16<T>::value(m);
 }
 
 }  // namespace quasar

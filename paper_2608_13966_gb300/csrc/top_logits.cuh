@@ -6,13 +6,16 @@
 // so that equal values rank by the lowest index and no two keys are equal.
 //
 // Each CTA of a row's cluster finds the k largest of its slice.  A bound on
-// the k-th comes from the threads' own maxima: the k-th largest of the 512
-// maxima has at least k elements at or above it, and not many more unless
-// the row is made of ties.  The elements at or above the bound are gathered
-// and ranked by counting.  A slice with more of them than the list holds is
-// settled by bisection on the 64-bit keys, which is exact for any data.  The
-// slices' lists, sorted, are merged by rank 0: an entry's rank is its place
-// in its own list plus, by binary search, the entries above it in the others.
+// the k-th comes from the threads' own maxima: the k-th largest of them (in
+// 16 bits, rounded down) has at least k elements at or above it, and not many
+// more unless the row is made of ties.  One warp settles the bound; then, in
+// the pass that sums the exponentials, each 16-byte vector's maximum is
+// compared with it, and the few vectors that reach it are looked into
+// afterwards, an element a thread.  The elements found are ranked by counting.
+// A slice with more of them than the lists hold is settled by bisection on
+// the 64-bit keys, which is exact for any data.  The slices' lists, sorted,
+// are merged by rank 0: an entry's rank is its place in its own list plus, by
+// binary search, the entries above it in the others.
 #pragma once
 
 #include "distill.cuh"
@@ -20,7 +23,8 @@
 namespace quasar {
 
 constexpr int kTopThreads = 512;
-constexpr int kTopList = 1024;  // elements a slice may gather before bisection
+constexpr int kTopList = 512;  // vectors or elements a slice may gather before bisection
+constexpr int kTopBounds = kTopThreads;  // maxima the bound is taken from
 
 // Both zeros are one value, and NaN ranks above everything.
 __device__ __forceinline__ uint32_t ordered_bits(float x)
@@ -39,6 +43,27 @@ __device__ __forceinline__ uint64_t top_key(float x, int64_t e)
     return ((uint64_t)ordered_bits(x) << 32) | (uint32_t)~(uint32_t)e;
 }
 
+// The want-th largest of the kTopBounds 16-bit maxima (0 if there are fewer),
+// by one warp, a bit a step.
+__device__ __forceinline__ uint32_t kth_largest(const uint16_t* maxima, int want)
+{
+    constexpr int kEach = kTopBounds / 32;
+    const int lane = threadIdx.x & 31;
+    uint32_t key[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) key[i] = maxima[32 * i + lane];
+    uint32_t bound = 0;
+#pragma unroll 1
+    for (int b = 15; b >= 0; --b) {
+        const uint32_t trial = bound | (1u << b);
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) c += key[i] >= trial;
+        if (__reduce_add_sync(0xffffffffu, c) >= want) bound = trial;
+    }
+    return bound;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kTopThreads) k_top_logits(const __grid_constant__ TopParams p)
 {
@@ -49,10 +74,13 @@ __global__ void __launch_bounds__(kTopThreads) k_top_logits(const __grid_constan
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem_raw + (size_t)p.row.vecs * 16);
     uint64_t* never = bars + kRowChunks;
     uint64_t* list = never + 1;                        // [kTopList]
-    uint64_t* merged = list + kTopList;                // rank 0: [kRowCtas][k]
-    float(*parts)[2] = reinterpret_cast<float(*)[2]>(merged + (size_t)kRowCtas * p.k);
-    float* scratch = reinterpret_cast<float*>(parts + kRowCtas);
-    int* count = reinterpret_cast<int*>(scratch + 32);
+    uint64_t* merged = list + kTopList;                // rank 0: [ctas][k]
+    float(*parts)[2] = reinterpret_cast<float(*)[2]>(merged + (size_t)p.row.ctas * p.k);
+    float* scratch = reinterpret_cast<float*>(parts + kRowCtas);      // [2][warps]
+    uint16_t* maxima = reinterpret_cast<uint16_t*>(scratch + 32);     // [kTopBounds]
+    uint16_t* found = maxima + kTopBounds;                            // [kTopList] vectors
+    int* count = reinterpret_cast<int*>(found + kTopList);  // elements, vectors
+    uint32_t* shared_bound = reinterpret_cast<uint32_t*>(count + 2);
 
     const int t = threadIdx.x;
     const int rank = (int)(blockIdx.x % p.row.ctas);
@@ -62,7 +90,7 @@ __global__ void __launch_bounds__(kTopThreads) k_top_logits(const __grid_constan
         for (int c = 0; c < kRowChunks; ++c) mbar_init(bars + c, 1);
         mbar_init(never, 1);
         mbar_init_fence();
-        *count = 0;
+        count[0] = count[1] = 0;
     }
     cluster_arrive();
     __syncthreads();
@@ -74,74 +102,73 @@ __global__ void __launch_bounds__(kTopThreads) k_top_logits(const __grid_constan
     __syncthreads();
     cluster_wait();  // every CTA of the row has started: its shared memory may be written
 
-    // maximum and sum of this thread's elements, and its largest element
     const float c2 = kLog2e / p.temperature;
-    float m = neg_inf(), s = 0.0f;
-    bool any = false;
-    for (int v = t; v < S.n_vecs; v += kTopThreads) {
-        float x[kN];
-        V::unpack(reinterpret_cast<const uint4*>(slice)[v], x);
-        float top = x[0];
+    const uint4* vecs = reinterpret_cast<const uint4*>(slice);
+    const int warp = t >> 5, lane = t & 31;
+    const int have = (int)(S.end - S.begin);
+    const int want = have < p.k ? have : p.k;
+    const float mine = largest<T>(vecs, S.n_vecs);
+    maxima[t] = (uint16_t)(t < S.n_vecs ? ordered_bits(mine) >> 16 : 0);
+    const float m = block_max(mine, scratch);
+    if (warp == 0) *shared_bound = kth_largest(maxima, want) << 16;
+    const ExpBase at(m, c2);
+    __syncthreads();
+    const uint32_t bound = *shared_bound;
+    const float least = from_ordered(bound);
+
+    // the exponentials' sum, and the vectors that hold an element at or above
+    // the bound (a NaN compares as if it did)
+    {
+        constexpr int kP = kN / 2;
+        float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll 2
+        for (int v = t; v < S.n_vecs; v += kTopThreads) {
+            const uint4 raw = vecs[v];
+            if (!(V::value(V::larger(raw)) < least)) {
+                const int i = atomicAdd(count + 1, 1);
+                if (i < kTopList) found[i] = (uint16_t)v;
+            }
+            if (p.lse) {
+                float2 x[kP];
+                V::unpack(raw, x);
+                at.apply(x, c2);
 #pragma unroll
-        for (int j = 1; j < kN; ++j) top = fmaxf(top, x[j]);
-        if (top > m) {
-            s *= ex2((m - top) * c2);
-            m = top;
+                for (int j = 0; j < kP; ++j) s = __fadd2_rn(s, x[j]);
+            }
         }
-        const float base = m == neg_inf() ? 0.0f : m;
-#pragma unroll
-        for (int j = 0; j < kN; ++j) s += ex2((x[j] - base) * c2);
-        any = true;
+        const float sum = warp_sum(s.x + s.y);
+        if (lane == 0) scratch[16 + warp] = sum;
     }
-    if (p.lse) {
-        const float top = block_max(m, scratch);
-        const float sum = block_sum(top == neg_inf() ? s : s * ex2((m - top) * c2), scratch);
-        if (t == 0) {
+    __syncthreads();
+    if (p.lse && warp == 0) {
+        const float sum = warp_sum(lane < kTopThreads / 32 ? scratch[16 + lane] : 0.0f) * at.fix;
+        if (lane == 0) {
             const uint32_t to = peer_addr(smem_u32(&parts[rank][0]), 0);
-            st_peer(to, top);
+            st_peer(to, m);
             st_peer(to + 4, sum);
         }
     }
-    // this thread's largest element (or less): a NaN leaves its mark in the sum
-    uint32_t best = 0;
-    if (any) best = s != s && m != __int_as_float(0x7F800000) ? 0xFFFFFFFFu : ordered_bits(m);
-
-    const int have = (int)(S.end - S.begin);
-    const int want = have < p.k ? have : p.k;
-    // the want-th largest of the threads' maxima, bit by bit
-    uint32_t bound = 0;
-    if (have > kTopThreads)
-        for (int b = 31; b >= 0; --b) {
-            const uint32_t trial = bound | (1u << b);
-            if (__syncthreads_count(best >= trial) >= want) bound = trial;
+    // an element a thread of the vectors found
+    const int n_found = count[1];
+    for (int i = t; i < min(n_found, kTopList) * kN; i += kTopThreads) {
+        const int at_slot = found[i / kN] * kN + i % kN;
+        const int64_t e = S.first + at_slot;
+        const float x = V::to_f32(slice[at_slot]);
+        if (ordered_bits(x) >= bound && e >= S.begin && e < S.end) {
+            const int j = atomicAdd(count, 1);
+            if (j < kTopList) list[j] = top_key(x, e - S.lead);
         }
-    for (int v = t; v < S.n_vecs; v += kTopThreads) {
-        float x[kN];
-        V::unpack(reinterpret_cast<const uint4*>(slice)[v], x);
-        const int64_t at = S.first + (int64_t)v * kN;
-#pragma unroll
-        for (int j = 0; j < kN; ++j)
-            if (ordered_bits(x[j]) >= bound && at + j >= S.begin && at + j < S.end) {
-                const int n = atomicAdd(count, 1);
-                if (n < kTopList) list[n] = top_key(x[j], at + j - S.lead);
-            }
     }
     __syncthreads();
-    int n = *count;
+    int n = n_found > kTopList ? kTopList + 1 : *count;
     if (n > kTopList) {
         // exact: the want-th largest key, and the keys from it up
         uint64_t floor_key = 0;
         for (int b = 63; b >= 0; --b) {
             const uint64_t trial = floor_key | (1ull << b);
             int c = 0;
-            for (int v = t; v < S.n_vecs; v += kTopThreads) {
-                float x[kN];
-                V::unpack(reinterpret_cast<const uint4*>(slice)[v], x);
-                const int64_t at = S.first + (int64_t)v * kN;
-#pragma unroll
-                for (int j = 0; j < kN; ++j)
-                    c += at + j >= S.begin && at + j < S.end && top_key(x[j], at + j - S.lead) >= trial;
-            }
+            for (int i = t; i < have; i += kTopThreads)
+                c += top_key(V::to_f32(slice[S.begin - S.first + i]), S.begin - S.lead + i) >= trial;
             c = __reduce_add_sync(0xffffffffu, c);
             __syncthreads();
             if (t == 0) *count = 0;
@@ -153,17 +180,11 @@ __global__ void __launch_bounds__(kTopThreads) k_top_logits(const __grid_constan
         __syncthreads();
         if (t == 0) *count = 0;
         __syncthreads();
-        for (int v = t; v < S.n_vecs; v += kTopThreads) {
-            float x[kN];
-            V::unpack(reinterpret_cast<const uint4*>(slice)[v], x);
-            const int64_t at = S.first + (int64_t)v * kN;
-#pragma unroll
-            for (int j = 0; j < kN; ++j) {
-                const uint64_t key = top_key(x[j], at + j - S.lead);
-                if (at + j >= S.begin && at + j < S.end && key >= floor_key) {
-                    const int i = atomicAdd(count, 1);
-                    if (i < kTopList) list[i] = key;
-                }
+        for (int i = t; i < have; i += kTopThreads) {
+            const uint64_t key = top_key(V::to_f32(slice[S.begin - S.first + i]), S.begin - S.lead + i);
+            if (key >= floor_key) {
+                const int j = atomicAdd(count, 1);
+                if (j < kTopList) list[j] = key;
             }
         }
         __syncthreads();
@@ -207,7 +228,7 @@ __global__ void __launch_bounds__(kTopThreads) k_top_logits(const __grid_constan
     if (p.lse && t == 0) {
         float top = neg_inf(), sum = 0.0f;
         for (int c = 0; c < p.row.ctas; ++c) merge_sum(top, sum, parts[c][0], parts[c][1], c2);
-        p.lse[r] = sum > 0.0f || sum != sum ? top / p.temperature + logf(sum) : neg_inf();
+        p.lse[r] = top == neg_inf() && sum == 0.0f ? neg_inf() : top / p.temperature + logf(sum);
     }
 }
 

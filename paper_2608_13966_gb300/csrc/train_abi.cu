@@ -221,7 +221,7 @@ quasar_status check_rows(const void* logits, quasar_dtype dtype, int64_t ld, int
     return QUASAR_OK;
 }
 
-constexpr size_t kDistillExtra = (kRowChunks + 1) * 8 + 3 * kMaxTop * 4 + kRowCtas * 16 + 32 * 4 + 16 + kMaxTop * 4;
+constexpr size_t kDistillExtra = (kRowChunks + 1) * 8 + 3 * kMaxTop * 4 + kRowCtas * 16 + 64 * 4 + 16 + kMaxTop * 4;
 
 quasar_status run_distill(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows, int64_t vocab,
                           const int32_t* indices, const float* values, int k, const float* teacher_lse,
@@ -407,8 +407,8 @@ quasar_status quasar_top_logits(const void* logits, quasar_dtype dtype, int64_t 
         overlaps(lse, n_lse, values, n_top) || overlaps(lse, n_lse, indices, n_top))
         return QUASAR_ERR_INVALID_ARG;
     TopParams p{};
-    const size_t extra =
-        (kRowChunks + 1) * 8 + 1024 * 8 + (size_t)kRowCtas * k * 8 + kRowCtas * 8 + 32 * 4 + 16;
+    const size_t extra = (kRowChunks + 1) * 8 + 512 * 8 + (size_t)kRowCtas * k * 8 + kRowCtas * 8 + 32 * 4 +
+                         2 * 512 * 2 + 16;
     size_t smem = 0;
     if ((st = plan_rows(logits, dtype, ld, rows, vocab, extra, &p.row, &smem)) != QUASAR_OK) return st;
     p.k = k;
