@@ -94,8 +94,7 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill_top(const __grid_co
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem_raw + (size_t)p.row.vecs * 16);
     uint64_t* never = bars + kRowChunks;
     float* logp = reinterpret_cast<float*>(never + 1);      // [kMaxTop]
-    float* own = logp + kMaxTop;                            // student logits of the entries held here
-    float* all = own + kMaxTop;                             // rank 0: of every entry
+    float* all = logp + kMaxTop;                            // rank 0: the entries' student logits
     float(*parts)[4] = reinterpret_cast<float(*)[4]>(all + kMaxTop);  // [kRowCtas]
     float* scratch = reinterpret_cast<float*>(parts + kRowCtas);      // [4][warps]
     float* teacher = scratch + 64;                          // P, p_r
@@ -110,7 +109,7 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill_top(const __grid_co
 
     if (weight == 0.0f) {  // a row that counts nothing is not read
         if (grad)
-            for (int64_t s = S.begin + t; s < S.end; s += kDistillThreads) grad[s - S.lead] = V::from_f32(0.0f);
+            for (int s = S.begin + t; s < S.end; s += kDistillThreads) grad[S.element0 + s] = V::from_f32(0.0f);
         if (!BACKWARD && rank == 0 && t == 0) {
             p.loss[r] = 0.0f;
             if (p.stats) p.stats[2 * r] = p.stats[2 * r + 1] = 0.0f;
@@ -118,14 +117,8 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill_top(const __grid_co
         return;
     }
 
-    if (t == 0) {
-        for (int c = 0; c < kRowChunks; ++c) mbar_init(bars + c, 1);
-        mbar_init(never, 1);
-        mbar_init_fence();
-    }
     if (!BACKWARD) cluster_arrive();
-    __syncthreads();
-    S.load(slice, bars);
+    S.load(slice, bars, never);
     const float inv_tau = 1.0f / p.temperature;
     if (t < 32) {
         int n_listed;
@@ -136,45 +129,44 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill_top(const __grid_co
             teacher[1] = rest;
         }
     }
+    __syncthreads();
     if (t == 0 && p.row.force_timeout_ns && !mbar_wait_bounded(never, 0, p.row.force_timeout_ns))
         record_timeout(p.row.status);
-    for (int c = 0; c < kRowChunks; ++c)
-        if (!mbar_wait_bounded(bars + c, 0, p.row.timeout_ns)) record_timeout(p.row.status);
-    __syncthreads();
-    if (!BACKWARD) cluster_wait();  // every CTA of the row has started: its shared memory may be written
 
     const float mass = teacher[0], p_rest = teacher[1];
     const float c2 = kLog2e * inv_tau;
-    // take the listed entries out of the slice
-    for (int k = t; k < p.k; k += kDistillThreads) {
-        const int s = entry[k] >= 0 ? S.slot_of(entry[k]) : -1;
-        if (s >= 0) {
-            own[k] = V::to_f32(slice[s]);
-            if (!BACKWARD) st_peer(peer_addr(smem_u32(all + k), 0), own[k]);
-        }
+    float mine = 0.0f;  // this thread's largest logit, listed or not
+    if (BACKWARD) {
+        for (int c = 0; c < kRowChunks; ++c)
+            if (!mbar_wait_bounded(bars + c, 0, p.row.timeout_ns)) record_timeout(p.row.status);
+    } else {
+        mine = S.largest(slice, bars, p.row);
+        cluster_wait();  // every CTA of the row has started: its shared memory may be written
+        __syncthreads();
     }
-    __syncthreads();
-    for (int k = t; k < p.k; k += kDistillThreads) {
-        const int s = entry[k] >= 0 ? S.slot_of(entry[k]) : -1;
-        if (s >= 0) slice[s] = V::from_f32(neg_inf());
+    // take the listed entry of this thread out of the slice
+    const int listed = t < p.k && entry[t] >= 0 ? S.slot_of(entry[t]) : -1;
+    float own = neg_inf();
+    if (listed >= 0) {
+        own = V::to_f32(slice[listed]);
+        slice[listed] = V::from_f32(neg_inf());
+        if (!BACKWARD) st_peer(peer_addr(smem_u32(all + t), 0), own);
     }
-    __syncthreads();
 
     float m_rest, coef, q_rest;          // of the whole row (backward: m_rest is the rest's lse)
     float m_all, log_s = 0.0f;           // lse = m_all / tau + log_s (backward: lse = m_all)
     if constexpr (!BACKWARD) {
-        const uint4* vecs = reinterpret_cast<const uint4*>(slice);
         const int warp = t >> 5, lane = t & 31;
-        const float m = block_max(largest<T>(vecs, S.n_vecs), scratch);
-        const ExpBase at(m, c2);
-        const float s = warp_sum(sum_exponentials<T>(vecs, S.n_vecs, c2, at)) * at.fix;
+        // the base is the largest logit, even a listed one: the rest's sum is
+        // fine about it unless the rest lies far below, which is then redone
+        float m = block_max(mine, scratch);
+        ExpBase at(m, c2);
+        float s = warp_sum(sum_exponentials(slice, S.n_vecs, t, kDistillThreads, c2, at)) * at.fix;
         // the listed entries held here, as a second sum (one a thread)
         float m_in = neg_inf(), s_in = 0.0f;
         if (t < kMaxTop) {
-            const bool here = t < p.k && entry[t] >= 0 && S.slot_of(entry[t]) >= 0;
-            const float x = here ? own[t] : neg_inf();
-            m_in = lanes_max(x, 0xffffffffu);
-            s_in = warp_sum(x == neg_inf() ? 0.0f : exp2f((x - m_in) * c2));
+            m_in = lanes_max(own, 0xffffffffu);
+            s_in = warp_sum(own == neg_inf() ? 0.0f : exp2f((own - m_in) * c2));
         }
         if (lane == 0) {
             scratch[16 + warp] = s;
@@ -182,9 +174,17 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill_top(const __grid_co
             scratch[48 + warp] = s_in;
         }
         __syncthreads();
+        constexpr int kW = kDistillThreads / 32;
+        float sum = warp_sum(lane < kW ? scratch[16 + lane] : 0.0f);
+        if (sum < 1e-20f) {
+            m = block_max(largest(slice, S.n_vecs), scratch);
+            at = ExpBase(m, c2);
+            s = warp_sum(sum_exponentials(slice, S.n_vecs, t, kDistillThreads, c2, at)) * at.fix;
+            if (lane == 0) scratch[16 + warp] = s;
+            __syncthreads();
+            sum = warp_sum(lane < kW ? scratch[16 + lane] : 0.0f);
+        }
         if (warp == 0) {
-            constexpr int kW = kDistillThreads / 32;
-            const float sum = warp_sum(lane < kW ? scratch[16 + lane] : 0.0f);
             const float x = lane < kW ? scratch[32 + lane] : neg_inf();
             m_in = lanes_max(x, 0xffffffffu);
             s_in = warp_sum(x == neg_inf() ? 0.0f : scratch[48 + lane] * exp2f((x - m_in) * c2));
@@ -243,10 +243,13 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill_top(const __grid_co
 
     // the unlisted entries: coef 2^(x c - base), or coef e^(z - lse) from
     // kept statistics
-    const bool vectors = (reinterpret_cast<uintptr_t>(grad - S.lead) & 15) == 0;
+    T* out = grad + S.element0;  // of slot 0
+    const bool vectors = (reinterpret_cast<uintptr_t>(out) & 15) == 0;
     const ExpBase at(BACKWARD ? 0.0f : m_rest, c2);
     coef *= at.fix;
     const float2 kk = make_float2(coef, coef);
+    if (BACKWARD) __syncthreads();
+#pragma unroll 2
     for (int v = t; v < S.n_vecs; v += kDistillThreads) {
         constexpr int kP = kN / 2;
         float2 x[kP];
@@ -261,24 +264,22 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill_top(const __grid_co
         }
 #pragma unroll
         for (int j = 0; j < kP; ++j) x[j] = __fmul2_rn(kk, x[j]);
-        const int64_t s = S.first + (int64_t)v * kN;
         if (vectors && S.whole(v)) {
-            __stcs(reinterpret_cast<uint4*>(grad + (s - S.lead)), V::pack(x));
+            __stcs(reinterpret_cast<uint4*>(out) + v, V::pack(x));
         } else {
 #pragma unroll
-            for (int j = 0; j < kN; ++j)
-                if (s + j >= S.begin && s + j < S.end)
-                    grad[s + j - S.lead] = V::from_f32(j & 1 ? x[j / 2].y : x[j / 2].x);
+            for (int j = 0; j < kN; ++j) {
+                const int s = v * kN + j;
+                if (s >= S.begin && s < S.end) out[s] = V::from_f32(j & 1 ? x[j / 2].y : x[j / 2].x);
+            }
         }
     }
     __syncthreads();
     // then the listed ones over the zeros left in their places
-    for (int k = t; k < p.k; k += kDistillThreads) {
-        const int s = entry[k] >= 0 ? S.slot_of(entry[k]) : -1;
-        if (s < 0) continue;
-        const float log_q = BACKWARD ? scaled_less(own[k], p.temperature, inv_tau, m_all)
-                                     : (own[k] - m_all) * inv_tau - log_s;
-        grad[entry[k]] = V::from_f32(none ? 0.0f : scale * (mass * expf(log_q) - expf(logp[k])));
+    if (listed >= 0) {
+        const float log_q = BACKWARD ? scaled_less(own, p.temperature, inv_tau, m_all)
+                                     : (own - m_all) * inv_tau - log_s;
+        out[listed] = V::from_f32(none ? 0.0f : scale * (mass * expf(log_q) - expf(logp[t])));
     }
 }
 

@@ -89,73 +89,98 @@ struct Vec16<__nv_bfloat16> {
 };
 
 // Where a CTA's slice of one row lies.  Slots count elements from the 16-byte
-// boundary at or before the row's start: element e of the row is slot lead + e.
+// boundary at or before the slice's first element.
 template <typename T>
 struct RowSlice {
     static constexpr int kN = Vec16<T>::kN;
-    const T* row;      // element 0 of the row
-    int lead;          // slots before the row in its first vector
-    int64_t first;     // first slot of the slice
+    const T* base;     // slot 0 (the row itself may start after it)
+    int64_t element0;  // element of the row at slot 0 (negative: the row starts after it)
     int n_vecs;        // vectors of the slice (may be 0)
-    int64_t begin;     // slots [begin, end) of the slice hold elements
-    int64_t end;
+    int begin, end;    // slots that hold elements
+    int whole0, whole1;  // vectors the row fills
+    int per_chunk;     // whole vectors a copy brings
 
     __device__ __forceinline__ RowSlice(const RowParams& p, int64_t r, int rank)
     {
-        row = static_cast<const T*>(p.logits) + r * p.ld;
-        lead = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+        const T* row = static_cast<const T*>(p.logits) + r * p.ld;
+        const int lead = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
         const int64_t slots = lead + p.vocab;
         const int64_t vecs = (slots + kN - 1) / kN;
         const int64_t v0 = (int64_t)rank * p.vecs;
         n_vecs = (int)(v0 >= vecs ? 0 : (vecs - v0 < p.vecs ? vecs - v0 : p.vecs));
-        first = v0 * kN;
-        begin = first < lead ? lead : first;
-        end = first + (int64_t)n_vecs * kN < slots ? first + (int64_t)n_vecs * kN : slots;
-        if (end < begin) end = begin;
+        element0 = v0 * kN - lead;
+        base = row + element0;
+        begin = element0 < 0 ? (int)-element0 : 0;
+        const int64_t left = p.vocab - element0;
+        end = left < (int64_t)n_vecs * kN ? (int)left : n_vecs * kN;
+        if (n_vecs == 0) begin = end = 0;
+        whole0 = begin > 0 ? 1 : 0;
+        whole1 = end < n_vecs * kN ? n_vecs - 1 : n_vecs;
+        if (whole1 < whole0) whole1 = whole0;
+        per_chunk = (whole1 - whole0 + kRowChunks - 1) / kRowChunks;
     }
 
-    // slot, relative to the slice, of element e; -1 if another CTA holds it
-    __device__ __forceinline__ int slot_of(int64_t e) const
+    // slot of element e; -1 if another CTA holds it
+    __device__ __forceinline__ int slot_of(int e) const
     {
-        const int64_t s = lead + e;
-        return s >= begin && s < end ? (int)(s - first) : -1;
+        const int64_t s = e - element0;
+        return s >= begin && s < end ? (int)s : -1;
     }
 
     __device__ __forceinline__ bool whole(int v) const
     {
-        const int64_t s = first + (int64_t)v * kN;
-        return s >= begin && s + kN <= end;
+        return (unsigned)(v - whole0) < (unsigned)(whole1 - whole0);
     }
 
-    // Start loading the slice.  Bulk copies for the whole vectors, chunk c of
-    // them on bars[c]; the (at most two) partial vectors by thread 0's warp.
-    // Every thread of the CTA calls it, after the barriers' initialisation.
-    __device__ __forceinline__ void load(T* smem, uint64_t* bars) const
+    // whether largest() gives thread t any element
+    __device__ __forceinline__ bool holds(int t) const
     {
-        int v0 = 0, v1 = n_vecs;
-        if (v0 < v1 && !whole(v0)) ++v0;
-        if (v0 < v1 && !whole(v1 - 1)) --v1;
-        if (threadIdx.x == 0) {
-            const int per = (v1 - v0 + kRowChunks - 1) / kRowChunks;
+        return t < min(per_chunk, whole1 - whole0) || (t == 0 && whole0 == 1 && n_vecs > 0) ||
+               (t == 1 && whole1 < n_vecs);
+    }
+
+    // Start loading the slice; every thread calls it, and a barrier follows
+    // before the slice is touched.  Thread 0 initialises the chunks' barriers
+    // and issues the copies of the whole vectors; the (at most two) partial
+    // ones are loaded and completed with -inf by the first warp.
+    __device__ __forceinline__ void load(T* smem, uint64_t* bars, uint64_t* never) const
+    {
+        const int t = threadIdx.x;
+        if (t == 0) {
+            for (int c = 0; c < kRowChunks; ++c) mbar_init(bars + c, 1);
+            mbar_init(never, 1);
+            mbar_init_fence();
             for (int c = 0; c < kRowChunks; ++c) {
-                const int a = v0 + c * per < v1 ? v0 + c * per : v1;
-                const int b = a + per < v1 ? a + per : v1;
+                const int a = min(whole0 + c * per_chunk, whole1), b = min(a + per_chunk, whole1);
                 mbar_arrive_expect_tx(bars + c, (uint32_t)(b - a) * 16u);
-                if (b > a)
-                    bulk_g2s(smem + (size_t)a * kN, row + (first + (int64_t)a * kN - lead),
-                             (uint32_t)(b - a) * 16u, bars + c);
+                if (b > a) bulk_g2s(smem + (size_t)a * kN, base + (size_t)a * kN, (uint32_t)(b - a) * 16u, bars + c);
             }
         }
-        const int t = threadIdx.x;
         if (t < 2 * kN) {
             const int v = t < kN ? 0 : n_vecs - 1;
-            const bool second = t >= kN;
-            if (v >= 0 && v < n_vecs && !whole(v) && !(second && v == 0)) {
-                const int64_t s = first + (int64_t)v * kN + t % kN;
-                smem[v * kN + t % kN] =
-                    s >= begin && s < end ? row[s - lead] : Vec16<T>::from_f32(neg_inf());
+            if (v >= 0 && v < n_vecs && !whole(v) && !(t >= kN && v == 0)) {
+                const int s = v * kN + t % kN;
+                smem[s] = s >= begin && s < end ? base[s] : Vec16<T>::from_f32(neg_inf());
             }
         }
+    }
+
+    // This thread's largest logit, chunk by chunk as the copies land.
+    // Records a timeout where one does not.
+    __device__ __forceinline__ float largest(const T* smem, uint64_t* bars, const RowParams& p) const
+    {
+        const uint4* vecs = reinterpret_cast<const uint4*>(smem);
+        typename Vec16<T>::Max m = Vec16<T>::lowest();
+        for (int c = 0; c < kRowChunks; ++c) {
+            if (!mbar_wait_bounded(bars + c, 0, p.timeout_ns)) record_timeout(p.status);
+            const int stop = min(whole0 + (c + 1) * per_chunk, whole1);
+#pragma unroll 4
+            for (int v = whole0 + c * per_chunk + threadIdx.x; v < stop; v += blockDim.x)
+                m = Vec16<T>::larger(m, Vec16<T>::larger(vecs[v]));
+        }
+        if (threadIdx.x == 0 && whole0 == 1 && n_vecs > 0) m = Vec16<T>::larger(m, Vec16<T>::larger(vecs[0]));
+        if (threadIdx.x == 1 && whole1 < n_vecs) m = Vec16<T>::larger(m, Vec16<T>::larger(vecs[n_vecs - 1]));
+        return Vec16<T>::value(m);
     }
 };
 
@@ -232,15 +257,17 @@ struct ExpBase {
     }
 };
 
-// The sum of 2^(x c - base) over this thread's vectors v = t, t + threads, ...
+// The sum of 2^(x c - base) over this thread's vectors v = first, first + step, ...
 template <typename T>
-__device__ __forceinline__ float sum_exponentials(const uint4* slice, int n_vecs, float c, const ExpBase& at)
+__device__ __forceinline__ float sum_exponentials(const T* slice, int n_vecs, int first, int step, float c,
+                                                  const ExpBase& at)
 {
+    const uint4* vecs = reinterpret_cast<const uint4*>(slice);
     float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll 2
-    for (int v = threadIdx.x; v < n_vecs; v += blockDim.x) {
+    for (int v = first; v < n_vecs; v += step) {
         float2 x[Vec16<T>::kN / 2];
-        Vec16<T>::unpack(slice[v], x);
+        Vec16<T>::unpack(vecs[v], x);
         at.apply(x, c);
 #pragma unroll
         for (int j = 0; j < Vec16<T>::kN / 2; ++j) s = __fadd2_rn(s, x[j]);
@@ -248,14 +275,15 @@ __device__ __forceinline__ float sum_exponentials(const uint4* slice, int n_vecs
     return s.x + s.y;
 }
 
-// This thread's largest logit in the slice.
+// This thread's largest logit of a slice that has landed.
 template <typename T>
-__device__ __forceinline__ float largest(const uint4* slice, int n_vecs)
+__device__ __forceinline__ float largest(const T* slice, int n_vecs)
 {
+    const uint4* vecs = reinterpret_cast<const uint4*>(slice);
     typename Vec16<T>::Max m = Vec16<T>::lowest();
 #pragma unroll 4
     for (int v = threadIdx.x; v < n_vecs; v += blockDim.x)
-        m = Vec16<T>::larger(m, Vec16<T>::larger(slice[v]));
+        m = Vec16<T>::larger(m, Vec16<T>::larger(vecs[v]));
     return Vec16<T>::value(m);
 }
 

@@ -52,9 +52,19 @@ __device__ __forceinline__ uint32_t kth_largest(const uint16_t* maxima, int want
     uint32_t key[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) key[i] = maxima[32 * i + lane];
-    uint32_t bound = 0;
+    // the bits above the highest in which any two differ are settled already
+    uint32_t high = key[0], low = key[0];
+#pragma unroll
+    for (int i = 1; i < kEach; ++i) {
+        high = max(high, key[i]);
+        low = min(low, key[i]);
+    }
+    high = __reduce_max_sync(0xffffffffu, high);
+    low = __reduce_min_sync(0xffffffffu, low);
+    int b = 31 - __clz(high ^ low);
+    uint32_t bound = high >> (b + 1) << (b + 1);
 #pragma unroll 1
-    for (int b = 15; b >= 0; --b) {
+    for (; b >= 0; --b) {
         const uint32_t trial = bound | (1u << b);
         int c = 0;
 #pragma unroll
@@ -86,77 +96,60 @@ __global__ void __launch_bounds__(kTopThreads) k_top_logits(const __grid_constan
     const int rank = (int)(blockIdx.x % p.row.ctas);
     const int64_t r = blockIdx.x / p.row.ctas;
     const RowSlice<T> S(p.row, r, rank);
-    if (t == 0) {
-        for (int c = 0; c < kRowChunks; ++c) mbar_init(bars + c, 1);
-        mbar_init(never, 1);
-        mbar_init_fence();
-        count[0] = count[1] = 0;
-    }
     cluster_arrive();
+    if (t == 0) count[0] = count[1] = 0;
+    S.load(slice, bars, never);
     __syncthreads();
-    S.load(slice, bars);
     if (t == 0 && p.row.force_timeout_ns && !mbar_wait_bounded(never, 0, p.row.force_timeout_ns))
         record_timeout(p.row.status);
-    for (int c = 0; c < kRowChunks; ++c)
-        if (!mbar_wait_bounded(bars + c, 0, p.row.timeout_ns)) record_timeout(p.row.status);
-    __syncthreads();
-    cluster_wait();  // every CTA of the row has started: its shared memory may be written
 
     const float c2 = kLog2e / p.temperature;
     const uint4* vecs = reinterpret_cast<const uint4*>(slice);
     const int warp = t >> 5, lane = t & 31;
-    const int have = (int)(S.end - S.begin);
+    const int have = S.end - S.begin;
     const int want = have < p.k ? have : p.k;
-    const float mine = largest<T>(vecs, S.n_vecs);
-    maxima[t] = (uint16_t)(t < S.n_vecs ? ordered_bits(mine) >> 16 : 0);
+    const float mine = S.largest(slice, bars, p.row);
+    cluster_wait();  // every CTA of the row has started: its shared memory may be written
+    // 0 where a thread held nothing: it must not count towards the bound
+    maxima[t] = (uint16_t)(S.holds(t) ? ordered_bits(mine) >> 16 : 0);
     const float m = block_max(mine, scratch);
-    if (warp == 0) *shared_bound = kth_largest(maxima, want) << 16;
-    const ExpBase at(m, c2);
-    __syncthreads();
-    const uint32_t bound = *shared_bound;
-    const float least = from_ordered(bound);
-
-    // the exponentials' sum, and the vectors that hold an element at or above
-    // the bound (a NaN compares as if it did)
-    {
-        constexpr int kP = kN / 2;
-        float2 s = make_float2(0.0f, 0.0f);
-#pragma unroll 2
-        for (int v = t; v < S.n_vecs; v += kTopThreads) {
-            const uint4 raw = vecs[v];
-            if (!(V::value(V::larger(raw)) < least)) {
-                const int i = atomicAdd(count + 1, 1);
-                if (i < kTopList) found[i] = (uint16_t)v;
-            }
-            if (p.lse) {
-                float2 x[kP];
-                V::unpack(raw, x);
-                at.apply(x, c2);
-#pragma unroll
-                for (int j = 0; j < kP; ++j) s = __fadd2_rn(s, x[j]);
-            }
-        }
-        const float sum = warp_sum(s.x + s.y);
-        if (lane == 0) scratch[16 + warp] = sum;
+    // one warp settles the bound while the others sum the exponentials
+    if (warp == 0) {
+        const uint32_t b = kth_largest(maxima, want) << 16;
+        if (lane == 0) *shared_bound = b;
+    } else if (p.lse) {
+        const ExpBase at(m, c2);
+        const float s = warp_sum(sum_exponentials(slice, S.n_vecs, t - 32, kTopThreads - 32, c2, at)) * at.fix;
+        if (lane == 0) scratch[16 + warp] = s;
     }
     __syncthreads();
-    if (p.lse && warp == 0) {
-        const float sum = warp_sum(lane < kTopThreads / 32 ? scratch[16 + lane] : 0.0f) * at.fix;
+    if (p.lse && warp == 1) {
+        const float sum = warp_sum(lane > 0 && lane < kTopThreads / 32 ? scratch[16 + lane] : 0.0f);
         if (lane == 0) {
             const uint32_t to = peer_addr(smem_u32(&parts[rank][0]), 0);
             st_peer(to, m);
             st_peer(to + 4, sum);
         }
     }
+    // the vectors that hold an element at or above the bound (a NaN compares
+    // as if it did)
+    const uint32_t bound = *shared_bound;
+    const float least = from_ordered(bound);
+#pragma unroll 4
+    for (int v = t; v < S.n_vecs; v += kTopThreads)
+        if (!(V::value(V::larger(vecs[v])) < least)) {
+            const int i = atomicAdd(count + 1, 1);
+            if (i < kTopList) found[i] = (uint16_t)v;
+        }
+    __syncthreads();
     // an element a thread of the vectors found
     const int n_found = count[1];
     for (int i = t; i < min(n_found, kTopList) * kN; i += kTopThreads) {
         const int at_slot = found[i / kN] * kN + i % kN;
-        const int64_t e = S.first + at_slot;
         const float x = V::to_f32(slice[at_slot]);
-        if (ordered_bits(x) >= bound && e >= S.begin && e < S.end) {
+        if (ordered_bits(x) >= bound && at_slot >= S.begin && at_slot < S.end) {
             const int j = atomicAdd(count, 1);
-            if (j < kTopList) list[j] = top_key(x, e - S.lead);
+            if (j < kTopList) list[j] = top_key(x, S.element0 + at_slot);
         }
     }
     __syncthreads();
@@ -168,7 +161,7 @@ __global__ void __launch_bounds__(kTopThreads) k_top_logits(const __grid_constan
             const uint64_t trial = floor_key | (1ull << b);
             int c = 0;
             for (int i = t; i < have; i += kTopThreads)
-                c += top_key(V::to_f32(slice[S.begin - S.first + i]), S.begin - S.lead + i) >= trial;
+                c += top_key(V::to_f32(slice[S.begin + i]), S.element0 + S.begin + i) >= trial;
             c = __reduce_add_sync(0xffffffffu, c);
             __syncthreads();
             if (t == 0) *count = 0;
@@ -181,7 +174,7 @@ __global__ void __launch_bounds__(kTopThreads) k_top_logits(const __grid_constan
         if (t == 0) *count = 0;
         __syncthreads();
         for (int i = t; i < have; i += kTopThreads) {
-            const uint64_t key = top_key(V::to_f32(slice[S.begin - S.first + i]), S.begin - S.lead + i);
+            const uint64_t key = top_key(V::to_f32(slice[S.begin + i]), S.element0 + S.begin + i);
             if (key >= floor_key) {
                 const int j = atomicAdd(count, 1);
                 if (j < kTopList) list[j] = key;
