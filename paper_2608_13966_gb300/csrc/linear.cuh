@@ -29,84 +29,163 @@ constexpr uint32_t kTileABytes = kTileRows * kTileK * 2;
 
 // -- activations -------------------------------------------------------------
 
-// fp32 throughout; exp and erf are CUDA's accurate functions (the epilogue is
-// hidden behind the next tile's product, so the faster ones buy nothing).
-__device__ __forceinline__ float activation(float z, int act)
+__device__ __forceinline__ float ex2_approx(float x)
 {
-    switch (act) {
-    case QUASAR_ACT_RELU: return fmaxf(z, 0.0f);
-    case QUASAR_ACT_SILU: return z / (1.0f + expf(-z));
-    case QUASAR_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678f));
-    default: return z;
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ float rcp_approx(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// 1 / (1 + e^-z), to 2^-22 of itself where it is not small: with the accurate
+// exponential and division instead, the epilogue of a 256 x 256 tile took
+// longer than its product at 4096 inputs.
+__device__ __forceinline__ float sigmoid(float z) { return rcp_approx(1.0f + ex2_approx(-1.44269504f * z)); }
+
+// The normal distribution Phi(z) and its density, from erfc(x) = e^(-x^2) t
+// (a1 + t (a2 + ...)), t = 1 / (1 + 0.3275911 x), x >= 0 (Abramowitz and
+// Stegun, Handbook of Mathematical Functions, 7.1.26: error 1.5e-7).
+__device__ __forceinline__ void normal(float z, float& phi, float& density)
+{
+    const float x = fabsf(z) * 0.70710678f;
+    const float t = rcp_approx(fmaf(0.3275911f, x, 1.0f));
+    const float e = ex2_approx(-0.72134752f * z * z);
+    float q = fmaf(1.061405429f, t, -1.453152027f);
+    q = fmaf(q, t, 1.421413741f);
+    q = fmaf(q, t, -0.284496736f);
+    q = fmaf(q, t, 0.254829592f);
+    const float tail = 0.5f * q * t * e;  // beyond |z|
+    phi = z < 0.0f ? tail : 1.0f - tail;
+    density = 0.39894228f * e;
+}
+
+template <int N>
+__device__ __forceinline__ void activate(float (&v)[N], int act)
+{
+    if (act == QUASAR_ACT_RELU) {
+#pragma unroll
+        for (int c = 0; c < N; ++c) v[c] = fmaxf(v[c], 0.0f);
+    } else if (act == QUASAR_ACT_SILU) {
+#pragma unroll
+        for (int c = 0; c < N; ++c) v[c] *= sigmoid(v[c]);
+    } else if (act == QUASAR_ACT_GELU) {
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            float phi, density;
+            normal(v[c], phi, density);
+            v[c] *= phi;
+        }
     }
 }
 
-__device__ __forceinline__ float activation_slope(float z, int act)
+// v *= act'(z)
+template <int N>
+__device__ __forceinline__ void times_slope(float (&v)[N], const float (&z)[N], int act)
 {
-    switch (act) {
-    case QUASAR_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
-    case QUASAR_ACT_SILU: {
-        const float s = 1.0f / (1.0f + expf(-z));
-        return s * (1.0f + z * (1.0f - s));
-    }
-    case QUASAR_ACT_GELU:
-        return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z);
-    default: return 1.0f;
+    if (act == QUASAR_ACT_RELU) {
+#pragma unroll
+        for (int c = 0; c < N; ++c) v[c] = z[c] > 0.0f ? v[c] : 0.0f;
+    } else if (act == QUASAR_ACT_SILU) {
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            const float s = sigmoid(z[c]);
+            v[c] *= s * fmaf(z[c], 1.0f - s, 1.0f);
+        }
+    } else if (act == QUASAR_ACT_GELU) {
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            float phi, density;
+            normal(z[c], phi, density);
+            v[c] *= fmaf(z[c], density, phi);
+        }
     }
 }
 
 // -- epilogue ----------------------------------------------------------------
 
-__device__ __forceinline__ float load_as_f32(const void* p, int64_t i, bool f32)
+// Element (row j, column i) of a row-major matrix, walked down a column: the
+// address is one addition a row.
+template <typename T, int N, bool FULL>
+__device__ __forceinline__ void load_column(const void* base, int64_t ld, int64_t j0, int64_t i, int n, float (&v)[N])
 {
-    return f32 ? static_cast<const float*>(p)[i]
-               : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+    const T* p = static_cast<const T*>(base) + j0 * ld + i;
+#pragma unroll
+    for (int c = 0; c < N; ++c, p += ld) {
+        v[c] = 0.0f;
+        if (FULL || c < n) {
+            if constexpr (sizeof(T) == 2)
+                v[c] = __bfloat162float(*p);
+            else
+                v[c] = *p;
+        }
+    }
 }
 
-__device__ __forceinline__ void store_from_f32(void* p, int64_t i, bool f32, float v)
+template <typename T, int N, bool FULL>
+__device__ __forceinline__ void store_column(void* base, int64_t ld, int64_t j0, int64_t i, int n, const float (&v)[N])
 {
-    if (f32)
-        static_cast<float*>(p)[i] = v;
+    T* p = static_cast<T*>(base) + j0 * ld + i;
+#pragma unroll
+    for (int c = 0; c < N; ++c, p += ld)
+        if (FULL || c < n) {
+            if constexpr (sizeof(T) == 2)
+                *p = __float2bfloat16_rn(v[c]);
+            else
+                *p = v[c];
+        }
+}
+
+template <int N, bool FULL>
+__device__ __forceinline__ void finish_columns(const Epilogue& e, float (&v)[N], int64_t i, int64_t j0, int n, float bias)
+{
+    using bf16 = __nv_bfloat16;
+    float res[N];
+    if (e.residual) {
+        if (e.out_f32)
+            load_column<float, N, FULL>(e.residual, e.ld_res, j0, i, n, res);
+        else
+            load_column<bf16, N, FULL>(e.residual, e.ld_res, j0, i, n, res);
+    }
+    if (e.scale_pre) {
+        float z[N];
+        load_column<bf16, N, FULL>(e.scale_pre, e.ld_scale, j0, i, n, z);
+        times_slope(v, z, e.act);
+    } else {
+        if (e.bias) {
+#pragma unroll
+            for (int c = 0; c < N; ++c) v[c] += bias;
+        }
+        if (e.pre) store_column<bf16, N, FULL>(e.pre, e.ld_pre, j0, i, n, v);
+        activate(v, e.act);
+    }
+    if (e.residual) {
+#pragma unroll
+        for (int c = 0; c < N; ++c) v[c] += res[c];
+    }
+    if (e.out_f32)
+        store_column<float, N, FULL>(e.out, e.ld_out, j0, i, n, v);
     else
-        static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+        store_column<bf16, N, FULL>(e.out, e.ld_out, j0, i, n, v);
 }
 
-// N consecutive columns j0.. of one row i: bias, activation (or the input
-// activation's slope), residual, one rounding to the output's type.
+// N consecutive columns j0.. (rows of memory) of one row i: bias, activation
+// (or the input activation's slope), residual, one rounding to the output's
+// type.
 template <int N>
 __device__ __forceinline__ void finish(const Epilogue& e, float (&v)[N], int64_t i, int64_t j0,
                                        int64_t rows, int64_t cols, float bias)
 {
-    if (i >= rows) return;
-    const int n = (int)(cols - j0 < N ? cols - j0 : N);
-    const bool f32 = e.out_f32;
-    float res[N];
-#pragma unroll
-    for (int c = 0; c < N; ++c)
-        res[c] = e.residual && c < n ? load_as_f32(e.residual, (j0 + c) * e.ld_res + i, f32) : 0.0f;
-    if (e.scale_pre) {
-        float z[N];
-#pragma unroll
-        for (int c = 0; c < N; ++c)
-            z[c] = c < n ? load_as_f32(e.scale_pre, (j0 + c) * e.ld_scale + i, false) : 0.0f;
-#pragma unroll
-        for (int c = 0; c < N; ++c) v[c] *= activation_slope(z[c], e.act);
-    } else {
-#pragma unroll
-        for (int c = 0; c < N; ++c) v[c] += bias;
-        if (e.pre) {
-#pragma unroll
-            for (int c = 0; c < N; ++c)
-                if (c < n) store_from_f32(e.pre, (j0 + c) * e.ld_pre + i, false, v[c]);
-        }
-        if (e.act != QUASAR_ACT_NONE) {
-#pragma unroll
-            for (int c = 0; c < N; ++c) v[c] = activation(v[c], e.act);
-        }
-    }
-#pragma unroll
-    for (int c = 0; c < N; ++c)
-        if (c < n) store_from_f32(e.out, (j0 + c) * e.ld_out + i, f32, v[c] + res[c]);
+    if (i >= rows || j0 >= cols) return;
+    if (cols - j0 >= N)
+        finish_columns<N, true>(e, v, i, j0, N, bias);
+    else
+        finish_columns<N, false>(e, v, i, j0, (int)(cols - j0), bias);
 }
 
 // -- waits -------------------------------------------------------------------
@@ -263,19 +342,26 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ Pr
         __syncthreads();
         cluster_sync();
         if (warp < 4) {
-            const int64_t i = row0 + 32 * warp + lane;
-            const float bias = p.e.bias && i < p.rows ? p.e.bias[i] : 0.0f;
+            // 4 rows of one column a thread: 16 bytes from each CTA
             const int per = BN / p.split;
-            const uint32_t base = smem_u32(smem) + (uint32_t)(32 * warp + lane) * 4;
-            for (int c = rank * per; c < (rank + 1) * per; c += 2) {
+            const uint32_t base = smem_u32(smem) + (uint32_t)lane * 16;
+            for (int c = rank * per + warp; c < (rank + 1) * per; c += 4) {
                 if (col0 + c >= p.cols) break;
-                float v[2] = {0.0f, 0.0f};
-                for (int r = 0; r < p.split; ++r) {
-                    const uint32_t from = peer_addr(base, (uint32_t)r);
-                    v[0] += ld_peer(from + (uint32_t)c * kTileRows * 4);
-                    v[1] += ld_peer(from + (uint32_t)(c + 1) * kTileRows * 4);
+                float4 v[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (r < p.split) v[r] = ld_peer4(peer_addr(base, (uint32_t)r) + (uint32_t)c * kTileRows * 4);
+                float s[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+                for (int r = 1; r < 8; ++r)
+                    if (r < p.split) s[0] += v[r].x, s[1] += v[r].y, s[2] += v[r].z, s[3] += v[r].w;
+                const int64_t i = row0 + 4 * lane;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float one[1] = {s[q]};
+                    finish(p.e, one, i + q, col0 + c, p.rows, p.cols,
+                           p.e.bias && i + q < p.rows ? p.e.bias[i + q] : 0.0f);
                 }
-                finish(p.e, v, i, col0 + c, p.rows, p.cols, bias);
             }
         }
         cluster_sync();
@@ -451,49 +537,46 @@ __global__ void __launch_bounds__(kPairThreads, 1) k_product_pair(const __grid_c
             const float bias = p.e.bias && i < p.rows ? p.e.bias[i] : 0.0f;
             float acc[PROMOTE ? 128 : 1];
             bool ok = true;
+            uint32_t from = mine;
             for (int q = 0; q < n_parts && ok; ++q, ++part) {
                 const uint32_t buf = part & 1;
                 ok = role_wait(acc_full + buf, (part / 2) & 1, gone, p.timeout_ns, p.status);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
+                from = mine + buf * kPairCols;
                 if constexpr (PROMOTE) {
 #pragma unroll
                     for (int c = 0; c < 128; c += 16) {
                         float v[16];
-                        __syncwarp();
-                        tmem_ld16(mine + buf * kPairCols + c, v);
+                        tmem_ld16(from + c, v);
 #pragma unroll
                         for (int x = 0; x < 16; ++x) acc[c + x] = q == 0 ? v[x] : acc[c + x] + v[x];
                     }
-                } else {
-                    for (int c = 0; c < 128; c += 32) {
-                        float v[32];
+                    if (q + 1 < n_parts) {
+                        tc_fence_before();
                         __syncwarp();
-                        tmem_ld32(mine + buf * kPairCols + c, v);
-                        if (c == 96) {  // drained: the next part may be multiplied into it
-                            tc_fence_before();
-                            __syncwarp();
-                            if (lane == 0) arrive_peer(peer_addr(smem_u32(acc_empty + buf), 0));
-                        }
-                        if (col0 + c < p.cols) finish(p.e, v, i, col0 + c, p.rows, p.cols, bias);
+                        if (lane == 0) arrive_peer(peer_addr(smem_u32(acc_empty + buf), 0));
                     }
-                }
-                if constexpr (PROMOTE) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) arrive_peer(peer_addr(smem_u32(acc_empty + buf), 0));
                 }
             }
             if (!ok) break;
             if constexpr (PROMOTE) {
+                // the sums back where the last part lay, for the epilogue's loop
 #pragma unroll
-                for (int c = 0; c < 128; c += 8) {
-                    float v[8];
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) v[x] = acc[c + x];
-                    if (col0 + c < p.cols) finish(p.e, v, i, col0 + c, p.rows, p.cols, bias);
+                for (int c = 0; c < 128; c += 16) tmem_st16(from + c, acc + c);
+                tmem_wait_st();
+            }
+            for (int c = 0; c < 128; c += 32) {
+                float v[32];
+                __syncwarp();
+                tmem_ld32(from + c, v);
+                if (c == 96) {  // drained: the next part may be multiplied into it
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive_peer(peer_addr(smem_u32(acc_empty + ((part - 1) & 1)), 0));
                 }
+                finish(p.e, v, i, col0 + c, p.rows, p.cols, bias);
             }
         }
     }
@@ -563,9 +646,12 @@ __global__ void __launch_bounds__(256) k_activation_grad(const __grid_constant__
     const __nv_bfloat16* pre = static_cast<const __nv_bfloat16*>(p.pre);
     __nv_bfloat16* dz = static_cast<__nv_bfloat16*>(p.dz);
     for (int64_t r = blockIdx.y; r < p.rows; r += gridDim.y) {
-        float d = __bfloat162float(dy[r * p.ld_dy + col]);
-        if (pre) d *= activation_slope(__bfloat162float(pre[r * p.ld_pre + col]), p.act);
-        dz[r * p.ld_dz + col] = __float2bfloat16_rn(d);
+        float d[1] = {__bfloat162float(dy[r * p.ld_dy + col])};
+        if (pre) {
+            const float z[1] = {__bfloat162float(pre[r * p.ld_pre + col])};
+            times_slope(d, z, p.act);
+        }
+        dz[r * p.ld_dz + col] = __float2bfloat16_rn(d[0]);
     }
 }
 
