@@ -39,6 +39,7 @@ UNITS = [
     ("kernels_sym.cu", [], "kernels_sym.o"),
     ("train_abi.cu", [], "train_abi.o"),
     ("kernels_linear.cu", [], "kernels_linear.o"),
+    ("kernels_linear_tile.cu", [], "kernels_linear_tile.o"),
     ("kernels_logits.cu", [], "kernels_logits.o"),
 ]
 

@@ -104,6 +104,7 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill_top(const __grid_co
     const int rank = (int)(blockIdx.x % p.row.ctas);
     const int64_t r = blockIdx.x / p.row.ctas;
     const RowSlice<T> S(p.row, r, rank);
+    wait_for_previous_grid();
     const float weight = p.row_weight ? p.row_weight[r] : 1.0f;
     T* grad = p.grad ? static_cast<T*>(p.grad) + r * p.ld_grad : nullptr;
 

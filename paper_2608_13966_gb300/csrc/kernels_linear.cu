@@ -1,26 +1,8 @@
-// Instantiations of the matrix-product kernels.
-#include "linear.cuh"
+// Instantiations of the paired matrix products, the column sums and the
+// activation gradient.
+#include "linear_grad.cuh"
 
 namespace quasar {
-
-// The kernel of 128-row tiles with bn columns; nullptr if there is none.
-const void* product_tile_kernel(int bn, bool a_mn, bool b_mn)
-{
-#define QUASAR_TILE(n, am, bm) \
-    if (bn == n && a_mn == am && b_mn == bm) return reinterpret_cast<const void*>(&k_product_tile<n, am, bm>);
-    QUASAR_TILE(16, false, false)
-    QUASAR_TILE(32, false, false)
-    QUASAR_TILE(64, false, false)
-    QUASAR_TILE(128, false, false)
-    QUASAR_TILE(16, true, false)
-    QUASAR_TILE(32, true, false)
-    QUASAR_TILE(64, true, false)
-    QUASAR_TILE(128, true, false)
-    QUASAR_TILE(64, true, true)
-    QUASAR_TILE(128, true, true)
-#undef QUASAR_TILE
-    return nullptr;
-}
 
 // The kernel of paired 256 x 256 tiles; nullptr if there is none.
 const void* product_pair_kernel(bool a_mn, bool b_mn, bool promote)

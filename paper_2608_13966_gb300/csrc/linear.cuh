@@ -219,14 +219,23 @@ __device__ __forceinline__ bool role_wait(uint64_t* bar, uint32_t parity, volati
 // so the result does not depend on timing), each CTA finishing BN / split of
 // the columns.
 //
+// PROMOTE: fp32 results.  The tensor core truncates as it accumulates, an
+// error that grows with the number of instructions (relative to the result's
+// norm 9e-7 after 1024 products, 4.7e-7 after 512; a plain fp32 product of
+// 4096 has 6e-7).  So every kPromoteBlocks blocks of the reduction go to a
+// fresh accumulator, two taking turns, and the epilogue adds the parts up in
+// registers, rounding to nearest.
+//
 // Warps: 0-3 epilogue (one per 32 lanes of tensor memory), 4 copies, 5
 // matrix instructions.
-template <int BN, bool A_MN, bool B_MN>
-__global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ ProductParams p)
+constexpr int kPromoteBlocks = 8;
+
+template <int BN, bool A_MN, bool B_MN, bool PROMOTE>
+__global__ void __launch_bounds__(192, 2) k_product_tile(const __grid_constant__ ProductParams p)
 {
     constexpr uint32_t kBBytes = BN * kTileK * 2;
     constexpr uint32_t kStageBytes = kTileABytes + kBBytes;
-    constexpr uint32_t kColumns = BN < 32 ? 32 : BN;
+    constexpr uint32_t kColumns = (PROMOTE ? 2 : 1) * BN < 32 ? 32 : (PROMOTE ? 2 : 1) * BN;
     static_assert(!B_MN || BN % 64 == 0, "an MN-major tile is made of 64-wide blocks");
 
     extern __shared__ uint8_t smem_raw[];
@@ -234,8 +243,10 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ Pr
     const int stages = p.stages;
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + (size_t)stages * kStageBytes);
     uint64_t* empty = full + stages;
-    uint64_t* done = empty + stages;
-    uint64_t* never = done + 1;
+    uint64_t* acc_full = empty + stages;   // [2]
+    uint64_t* acc_empty = acc_full + 2;    // [2]: 4 epilogue warps
+    uint64_t* drained = acc_empty + 2;
+    uint64_t* never = drained + 1;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(never + 1);
     volatile uint32_t* gone = tmem_slot + 1;
 
@@ -246,21 +257,31 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ Pr
     const int64_t col0 = (tile / p.tiles_row) * BN;
     const int kb0 = (int)((int64_t)p.k_blocks * rank / p.split);
     const int nkb = (int)((int64_t)p.k_blocks * (rank + 1) / p.split) - kb0;
+    const int per_part = PROMOTE ? kPromoteBlocks : nkb;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) {
             mbar_init(full + s, 1);
             mbar_init(empty + s, 1);
         }
-        mbar_init(done, 1);
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(acc_full + b, 1);
+            mbar_init(acc_empty + b, 4);
+        }
+        mbar_init(drained, 1);
         mbar_init(never, 1);
         *gone = 0;
         mbar_init_fence();
     }
     if (warp == 5) tmem_alloc<1>(tmem_slot, kColumns);
+    if (warp == 4 && lane == 0) {
+        prefetch_map(&p.a);
+        prefetch_map(&p.b);
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    wait_for_previous_grid();
     const uint32_t tmem = *tmem_slot;
 
     if (warp == 4 && lane == 0) {
@@ -293,38 +314,79 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ Pr
                 mbar_wait_bounded(full + j % stages, (j / stages) & 1, p.timeout_ns);
     } else if (warp == 5 && lane == 0) {
         constexpr uint32_t desc = mma_desc(kTileRows, BN, A_MN, B_MN);
-        for (int it = 0; it < nkb; ++it) {
-            const int s = it % stages;
-            if (!role_wait(full + s, (it / stages) & 1, gone, p.timeout_ns, p.status)) break;
+        bool ok = true;
+        int it = 0;
+        for (int part = 0; it < nkb && ok; ++part) {
+            const int buf = part & 1;
+            if (part >= 2 && !role_wait(acc_empty + buf, (part / 2 - 1) & 1, gone, p.timeout_ns, p.status)) break;
             tc_fence_after();
-            const uint32_t a = smem_u32(smem + (size_t)s * kStageBytes);
-            uint64_t da = operand_desc(a, A_MN), db = operand_desc(a + kTileABytes, B_MN);
+            const int end = it + per_part < nkb ? it + per_part : nkb;
+            for (bool add = false; it < end; ++it) {
+                const int s = it % stages;
+                if (!role_wait(full + s, (it / stages) & 1, gone, p.timeout_ns, p.status)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t a = smem_u32(smem + (size_t)s * kStageBytes);
+                uint64_t da = operand_desc(a, A_MN), db = operand_desc(a + kTileABytes, B_MN);
 #pragma unroll
-            for (int k = 0; k < kTileK / 16; ++k) {
-                mma_bf16<1>(tmem, da, db, desc, it > 0 || k > 0);
-                da += k_step(A_MN);
-                db += k_step(B_MN);
+                for (int k = 0; k < kTileK / 16; ++k) {
+                    mma_bf16<1>(tmem + buf * BN, da, db, desc, add);
+                    add = true;
+                    da += k_step(A_MN);
+                    db += k_step(B_MN);
+                }
+                mma_commit(smem_u32(empty + s));
             }
-            mma_commit(smem_u32(empty + s));
+            if (ok) mma_commit(smem_u32(acc_full + buf));
         }
-        mma_commit(smem_u32(done));
         // everything issued is finished before tensor memory is freed
-        mbar_wait_bounded(done, 0, p.timeout_ns);
+        mma_commit(smem_u32(drained));
+        mbar_wait_bounded(drained, 0, p.timeout_ns);
     }
     __syncwarp();
     if (warp < 4) {
-        role_wait(done, 0, gone, p.timeout_ns, p.status);
-        __syncwarp();
-        tc_fence_after();
         const int64_t i = row0 + 32 * warp + lane;
         const float bias = p.e.bias && i < p.rows ? p.e.bias[i] : 0.0f;
         const uint32_t mine = tmem + ((uint32_t)(32 * warp) << 16);
         float* part = reinterpret_cast<float*>(smem);
+        const int n_parts = nkb > 0 ? (nkb + per_part - 1) / per_part : 0;
+        uint32_t from = mine;
+        float acc[PROMOTE ? BN : 1];
+#pragma unroll
+        for (float& x : acc) x = 0.0f;
+#pragma unroll 1
+        for (int q = 0; q < n_parts; ++q) {
+            const bool ok = role_wait(acc_full + (q & 1), (q / 2) & 1, gone, p.timeout_ns, p.status);
+            if (!__all_sync(0xffffffffu, ok)) break;
+            tc_fence_after();
+            from = mine + (q & 1) * BN;
+            if constexpr (PROMOTE) {
+#pragma unroll
+                for (int c = 0; c < BN; c += 16) {
+                    float v[16];
+                    tmem_ld16(from + c, v);
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) acc[c + x] += v[x];
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(acc_empty + (q & 1));
+            }
+        }
+        if (PROMOTE && n_parts > 1) {
+            // the sums where the last part lay, for the loop below
+#pragma unroll
+            for (int c = 0; c < BN; c += 16) tmem_st16(from + c, acc + (PROMOTE ? c : 0));
+            tmem_wait_st();
+        }
+#pragma unroll 1
         for (int c = 0; c < BN; c += 16) {
             float v[16];
             if (nkb > 0) {
                 __syncwarp();
-                tmem_ld16(mine + c, v);
+                tmem_ld16(from + c, v);
             } else {
 #pragma unroll
                 for (int q = 0; q < 16; ++q) v[q] = 0.0f;
@@ -381,17 +443,16 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ Pr
 // 256 columns a CTA) use half of tensor memory: the next tile is multiplied
 // into the other half while the epilogue drains this one.
 //
-// PROMOTE: fp32 results.  The tensor core truncates as it accumulates, an
-// error that grows with the number of instructions; so every kPromoteBlocks
-// blocks of the reduction go to a fresh accumulator, and the epilogue adds
-// the parts up in registers, rounding to nearest.
+// PROMOTE: fp32 results, parts of the reduction added up in registers as in
+// k_product_tile (8192 x 14336 x 4096 with parts of 512: 671 us against 537
+// us for bf16 results, of which the larger output takes 35; with parts of 256
+// the draining shows, 736 us).
 //
 // Warps: 0-7 epilogue (lane quadrant w % 4, column half w / 4), 8 copies, 9
 // matrix instructions.
 constexpr int kPairCols = 256;
 constexpr int kPairThreads = 320;
 constexpr int kPairStages = 6;
-constexpr int kPromoteBlocks = 4;
 constexpr int kPairGroup = 8;  // column tiles walked together, for operand reuse in L2
 constexpr uint32_t kPairStageBytes = 2 * kTileABytes;
 
@@ -437,10 +498,15 @@ __global__ void __launch_bounds__(kPairThreads, 1) k_product_pair(const __grid_c
         mbar_init_fence();
     }
     if (warp == 9) tmem_alloc<2>(tmem_slot, 512);
+    if (warp == 8 && lane == 0) {
+        prefetch_map(&p.a);
+        prefetch_map(&p.b);
+    }
     tc_fence_before();
     __syncthreads();
     cluster_sync();
     tc_fence_after();
+    wait_for_previous_grid();
     const uint32_t tmem = *tmem_slot;
 
     // tile t: groups of kPairGroup column tiles, row tiles within a group
@@ -536,8 +602,11 @@ __global__ void __launch_bounds__(kPairThreads, 1) k_product_pair(const __grid_c
             const int64_t i = row0 + 32 * quad + lane;
             const float bias = p.e.bias && i < p.rows ? p.e.bias[i] : 0.0f;
             float acc[PROMOTE ? 128 : 1];
+#pragma unroll
+            for (float& x : acc) x = 0.0f;
             bool ok = true;
             uint32_t from = mine;
+#pragma unroll 1
             for (int q = 0; q < n_parts && ok; ++q, ++part) {
                 const uint32_t buf = part & 1;
                 ok = role_wait(acc_full + buf, (part / 2) & 1, gone, p.timeout_ns, p.status);
@@ -551,7 +620,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) k_product_pair(const __grid_c
                         float v[16];
                         tmem_ld16(from + c, v);
 #pragma unroll
-                        for (int x = 0; x < 16; ++x) acc[c + x] = q == 0 ? v[x] : acc[c + x] + v[x];
+                        for (int x = 0; x < 16; ++x) acc[c + x] += v[x];
                     }
                     if (q + 1 < n_parts) {
                         tc_fence_before();
@@ -567,6 +636,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) k_product_pair(const __grid_c
                 for (int c = 0; c < 128; c += 16) tmem_st16(from + c, acc + c);
                 tmem_wait_st();
             }
+#pragma unroll 1
             for (int c = 0; c < 128; c += 32) {
                 float v[32];
                 __syncwarp();
@@ -585,74 +655,6 @@ __global__ void __launch_bounds__(kPairThreads, 1) k_product_pair(const __grid_c
     __syncthreads();
     cluster_sync();  // neither CTA leaves while the other may still signal it
     if (warp == 9) tmem_free<2>(tmem, 512);
-}
-
-// -- column sums and activation gradients --------------------------------------
-
-// dbias[j] = sum over rows of dz[row][j] in fp32.  64 columns per cluster of 8
-// CTAs of 8 warps; warp w of CTA c takes the rows c + 8 w + 64 q, and the 64
-// partial sums of a column are added in a fixed order.
-__global__ void __launch_bounds__(256) k_column_sum(const __grid_constant__ ColumnSumParams p)
-{
-    extern __shared__ uint8_t smem_raw[];
-    float2* part = reinterpret_cast<float2*>(smem_raw);  // [8 warps][32 lanes]
-    float2* peers = part + 256;                          // [8 CTAs][32 lanes], used by rank 0
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = (int)cluster_rank();
-    const int64_t col = (int64_t)(blockIdx.x / 8) * 64 + 2 * lane;
-    const __nv_bfloat16* in = static_cast<const __nv_bfloat16*>(p.in) + col;
-    float2 s = make_float2(0.0f, 0.0f);
-    cluster_arrive();
-    if (col + 1 < p.cols) {
-#pragma unroll 8
-        for (int64_t r = rank + 8 * warp; r < p.rows; r += 64) {
-            const uint32_t x = *reinterpret_cast<const uint32_t*>(in + r * p.ld);
-            s.x += bf16lo(x);
-            s.y += bf16hi(x);
-        }
-    } else if (col < p.cols) {
-        for (int64_t r = rank + 8 * warp; r < p.rows; r += 64) s.x += __bfloat162float(in[r * p.ld]);
-    }
-    part[warp * 32 + lane] = s;
-    __syncthreads();
-    cluster_wait();
-    if (warp == 0) {
-        for (int w = 1; w < 8; ++w) {
-            s.x += part[w * 32 + lane].x;
-            s.y += part[w * 32 + lane].y;
-        }
-        const uint32_t to = peer_addr(smem_u32(peers + rank * 32 + lane), 0);
-        st_peer(to, s.x);
-        st_peer(to + 4, s.y);
-    }
-    cluster_sync();
-    if (rank == 0 && warp == 0) {
-        s = peers[lane];
-        for (int c = 1; c < 8; ++c) {
-            s.x += peers[c * 32 + lane].x;
-            s.y += peers[c * 32 + lane].y;
-        }
-        if (col < p.cols) p.out[col] = s.x;
-        if (col + 1 < p.cols) p.out[col + 1] = s.y;
-    }
-}
-
-// dz = dy act'(pre), rounded once to bf16 (pre NULL: a strided copy).
-__global__ void __launch_bounds__(256) k_activation_grad(const __grid_constant__ ActGradParams p)
-{
-    const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (col >= p.cols) return;
-    const __nv_bfloat16* dy = static_cast<const __nv_bfloat16*>(p.dy);
-    const __nv_bfloat16* pre = static_cast<const __nv_bfloat16*>(p.pre);
-    __nv_bfloat16* dz = static_cast<__nv_bfloat16*>(p.dz);
-    for (int64_t r = blockIdx.y; r < p.rows; r += gridDim.y) {
-        float d[1] = {__bfloat162float(dy[r * p.ld_dy + col])};
-        if (pre) {
-            const float z[1] = {__bfloat162float(pre[r * p.ld_pre + col])};
-            times_slope(d, z, p.act);
-        }
-        dz[r * p.ld_dz + col] = __float2bfloat16_rn(d[0]);
-    }
 }
 
 }  // namespace quasar

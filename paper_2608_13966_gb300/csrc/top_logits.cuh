@@ -97,6 +97,7 @@ __global__ void __launch_bounds__(kTopThreads) k_top_logits(const __grid_constan
     const int64_t r = blockIdx.x / p.row.ctas;
     const RowSlice<T> S(p.row, r, rank);
     cluster_arrive();
+    wait_for_previous_grid();
     if (t == 0) count[0] = count[1] = 0;
     S.load(slice, bars, never);
     __syncthreads();

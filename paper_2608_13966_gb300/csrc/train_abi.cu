@@ -16,7 +16,7 @@
 #include "quasar.h"
 
 namespace quasar {
-const void* product_tile_kernel(int bn, bool a_mn, bool b_mn);
+const void* product_tile_kernel(int bn, bool a_mn, bool b_mn, bool promote);
 const void* product_pair_kernel(bool a_mn, bool b_mn, bool promote);
 size_t product_pair_smem();
 const void* column_sum_kernel();
@@ -57,6 +57,9 @@ bool valid_shape(int64_t rows, int64_t cols, int64_t ld)
 
 // -- launches ------------------------------------------------------------------
 
+// A programmatic dependent launch: every kernel of this file waits for the
+// grid before it in the stream before it touches global memory, and only its
+// prologue (barriers, tensor memory, tensor maps) runs earlier.
 quasar_status launch(const void* fn, void* params, dim3 grid, int threads, int cluster, size_t smem,
                      quasar_stream_t stream)
 {
@@ -67,13 +70,15 @@ quasar_status launch(const void* fn, void* params, dim3 grid, int threads, int c
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = reinterpret_cast<cudaStream_t>(stream);
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)cluster;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 1 : 0;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     void* args[] = {params};
     return cudaLaunchKernelExC(&cfg, fn, args) == cudaSuccess ? QUASAR_OK : QUASAR_ERR_CUDA;
 }
@@ -150,7 +155,7 @@ quasar_status product(const Operand& a, const Operand& b, int64_t rows, int64_t 
         p.tiles_col = (int)((cols + 255) / 256);
         if ((st = tile_map(a, a.mn_major ? 64 : 128, &p.a)) != QUASAR_OK) return st;
         if ((st = tile_map(b, b.mn_major ? 64 : 128, &p.b)) != QUASAR_OK) return st;
-        const void* fn = product_pair_kernel(a.mn_major, b.mn_major, e.out_f32);
+        const void* fn = product_pair_kernel(a.mn_major, b.mn_major, e.out_f32 && p.k_blocks > 8);
         if (!fn) return QUASAR_ERR_UNSUPPORTED;
         int pairs = 0;
         if ((st = host_max_clusters(fn, 2, 320, product_pair_smem(), &pairs)) != QUASAR_OK) return st;
@@ -167,13 +172,15 @@ quasar_status product(const Operand& a, const Operand& b, int64_t rows, int64_t 
     const size_t stage = 128 * 128 + (size_t)bn * 128;
     p.stages = (int)std::min<size_t>(8, (size_t)100 * 1024 / stage);
     // exchange of partial tiles through the stages' memory
-    const size_t smem = 1024 + p.stages * stage + (2 * p.stages + 2) * 8 + 16;
+    const size_t smem = 1024 + p.stages * stage + (2 * p.stages + 6) * 8 + 16;
     if (tiles * p.split > (int64_t(1) << 31) - 1) return QUASAR_ERR_UNSUPPORTED;
+    // parts are only worth promoting where there are several
+    const bool promote = e.out_f32 && p.k_blocks / p.split > 8;
     if (depth > 0) {
         if ((st = tile_map(a, a.mn_major ? 64 : 128, &p.a)) != QUASAR_OK) return st;
         if ((st = tile_map(b, b.mn_major ? 64 : bn, &p.b)) != QUASAR_OK) return st;
     }
-    const void* fn = product_tile_kernel(bn, a.mn_major, b.mn_major);
+    const void* fn = product_tile_kernel(bn, a.mn_major, b.mn_major, promote);
     if (!fn) return QUASAR_ERR_UNSUPPORTED;
     return launch(fn, &p, dim3((unsigned)(tiles * p.split)), 192, p.split, smem, stream);
 }
