@@ -506,13 +506,13 @@ quasar_status quasar_activation_grad(const void* dy, int64_t ld_dy, const void* 
  *
  *   logits       [rows, vocab] bf16 or fp32 (dtype); rows may start anywhere.
  *   k            1 .. min(256, vocab).
- *   temperature  > 0.
+ *   temperature  1e-6 .. 1e6.
  *   values       [rows, k] fp32: the logits themselves (not scaled).
  *   indices      [rows, k] int32.  Equal values rank by the lowest index.
  *   lse          [rows] fp32: log sum exp(logits / temperature) over the
  *                vocabulary (-inf for a row of -inf), or NULL.
- * -inf logits are ordinary values (masked entries).  A row may take up to
- * 8 x 208 KB less the lists (UNSUPPORTED beyond).
+ * -inf logits are ordinary values (masked entries), and a NaN ranks above
+ * everything.
  */
 quasar_status quasar_top_logits(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows,
                                 int64_t vocab, int k, float temperature, float* values,
@@ -533,7 +533,7 @@ quasar_status quasar_top_logits(const void* logits, quasar_dtype dtype, int64_t 
  *   logits       [rows, vocab] bf16 or fp32; rows may start anywhere.
  *   indices      [rows, k] int32, distinct within a row.  An index outside
  *                [0, vocab) marks an absent entry (a row with fewer than k).
- *   values       [rows, k] fp32, 1 <= k <= 256.
+ *   values       [rows, k] fp32, 1 <= k <= 256; temperature 1e-6 .. 1e6.
  *   row_weight   [rows] fp32 (what the row counts in the total), or NULL for
  *                1.  A row of weight 0 is not read: loss, statistics and
  *                gradient 0, whatever its logits hold.
@@ -543,8 +543,10 @@ quasar_status quasar_top_logits(const void* logits, quasar_dtype dtype, int64_t 
  *   grad         [rows, vocab] of the logits' dtype, or NULL; it may be the
  *                logits themselves (same pointer and stride).
  * -inf logits are ordinary values (q = 0; a listed one with p > 0 makes the
- * loss inf).  Without a single entry of mass, teacher_lse NULL gives loss and
- * gradient 0.  Rows up to 8 x 208 KB (UNSUPPORTED beyond).
+ * loss inf; a row of nothing else has loss inf and gradient 0).  Without a
+ * single entry of mass, teacher_lse NULL gives loss and gradient 0.  A byte
+ * of shared memory is kept for each 16 bytes of a CTA's share of the row:
+ * a million logits fit whatever the number of rows (UNSUPPORTED beyond 227 KB).
  */
 quasar_status quasar_distill_top(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows,
                                  int64_t vocab, const int32_t* indices, const float* values, int k,

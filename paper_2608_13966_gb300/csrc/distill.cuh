@@ -16,15 +16,17 @@
 //   dloss/dz_j = u_j (P q_r - p_r)      (unlisted),
 //
 // which never divides by q_r.  The rest's sum is formed on its own (a listed
-// logit is replaced by -inf in shared memory once it has been read), not as
-// the difference of two sums.
+// logit counts as -inf there), not as the difference of two sums.
+//
+// The row is passed over twice: the rest's sum of exponentials about a running
+// maximum, then the gradient; the second time it comes from L2.  The listed
+// logits, k scattered elements, are read first.  A byte a vector in shared
+// memory says which of its elements are listed.
 #pragma once
 
-#include "row_slice.cuh"
+#include "row_stream.cuh"
 
 namespace quasar {
-
-constexpr int kDistillThreads = 512;
 
 // x / tau - y: the quotient is not rounded before the subtraction (inv_tau is
 // 1 / tau rounded, the second step its remainder)
@@ -43,39 +45,26 @@ __device__ __forceinline__ float kl_term(float p, float log_p, float log_q)
     return d > -1.0f ? p * (d + expm1f(-d)) : p * (d - 1.0f) + expf(log_q);
 }
 
-// Teacher side of a row, by one warp: log p of each entry into logp[] (-inf
-// where absent), returns sum p; n_listed counts the entries present.
-__device__ __forceinline__ float teacher_side(const DistillParams& p, int64_t r, float inv_tau,
-                                              float* logp, int32_t* entry, int* n_listed)
+// Teacher side of a row, by one warp: log p of each entry replaces its value
+// in logp[] (-inf where absent); returns sum p.
+__device__ __forceinline__ float teacher_side(const DistillParams& p, int64_t r, float inv_tau, float* logp)
 {
     const int lane = threadIdx.x & 31;
-    const int32_t* idx = p.indices + r * p.k;
-    const float* val = p.values + r * p.k;
-    float top = neg_inf();
-    int n = 0;
-    for (int k = lane; k < p.k; k += 32) {
-        const int32_t e = idx[k];
-        const bool here = e >= 0 && e < p.row.vocab;
-        const float t = here ? val[k] * inv_tau : neg_inf();
-        entry[k] = here ? e : -1;
-        logp[k] = t;
-        top = fmaxf(top, t);
-        n += here;
-    }
-    *n_listed = __reduce_add_sync(0xffffffffu, n);
     float norm;
     if (p.teacher_lse) {
         norm = p.teacher_lse[r];
     } else {
+        float top = neg_inf();
+        for (int k = lane; k < p.k; k += 32) top = fmaxf(top, logp[k] * inv_tau);
         top = lanes_max(top, 0xffffffffu);
         float s = 0.0f;
-        for (int k = lane; k < p.k; k += 32) s += top == neg_inf() ? 0.0f : expf(logp[k] - top);
+        for (int k = lane; k < p.k; k += 32) s += top == neg_inf() ? 0.0f : expf(logp[k] * inv_tau - top);
         s = warp_sum(s);
         norm = s > 0.0f ? top + logf(s) : 0.0f;
     }
     float sum = 0.0f;
     for (int k = lane; k < p.k; k += 32) {
-        logp[k] -= norm;
+        logp[k] = logp[k] * inv_tau - norm;
         sum += expf(logp[k]);
     }
     return warp_sum(sum);
@@ -83,34 +72,44 @@ __device__ __forceinline__ float teacher_side(const DistillParams& p, int64_t r,
 
 // BACKWARD: the gradient from kept statistics (log-sum-exp of z over the
 // vocabulary and over the rest).  Otherwise the loss, the statistics and, if
-// asked, the gradient, the row staying in shared memory in between.
-template <typename T, bool BACKWARD>
-__global__ void __launch_bounds__(kDistillThreads) k_distill_top(const __grid_constant__ DistillParams p)
+// asked, the gradient.
+template <typename T, int THREADS, bool BACKWARD>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const __grid_constant__ DistillParams p)
 {
     using V = Vec16<T>;
-    constexpr int kN = V::kN;
+    constexpr int kN = V::kN, kP = kN / 2;
     extern __shared__ __align__(128) uint8_t smem_raw[];
-    T* slice = reinterpret_cast<T*>(smem_raw);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem_raw + (size_t)p.row.vecs * 16);
-    uint64_t* never = bars + kRowChunks;
-    float* logp = reinterpret_cast<float*>(never + 1);      // [kMaxTop]
-    float* all = logp + kMaxTop;                            // rank 0: the entries' student logits
-    float(*parts)[4] = reinterpret_cast<float(*)[4]>(all + kMaxTop);  // [kRowCtas]
-    float* scratch = reinterpret_cast<float*>(parts + kRowCtas);      // [4][warps]
-    float* teacher = scratch + 64;                          // P, p_r
-    int32_t* entry = reinterpret_cast<int32_t*>(teacher + 4);  // [kMaxTop]
+    uint8_t* mask = smem_raw;  // of each vector, its listed elements
+    const int mask_words = (p.row.vecs + 15) / 16 * 4;
+    float* logp = reinterpret_cast<float*>(mask + (size_t)mask_words * 4);  // [kMaxTop]
+    float* own = logp + kMaxTop;                              // the entries' student logits
+    int32_t* entry = reinterpret_cast<int32_t*>(own + kMaxTop);  // -1: absent
+    float* scratch = reinterpret_cast<float*>(entry + kMaxTop);  // [2][32]
+    float* teacher = scratch + 64;                            // P, p_r, listed (m, s)
+    float(*parts)[2] = reinterpret_cast<float(*)[2]>(teacher + 4);  // [kRowCtas]
+    uint64_t* never = reinterpret_cast<uint64_t*>(parts + kRowCtas);  // nothing signals it: see quasar_debug_force_timeout
+    int* n_listed = reinterpret_cast<int*>(never + 1);
 
-    const int t = threadIdx.x;
-    const int rank = (int)(blockIdx.x % p.row.ctas);
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+    const int rank = p.row.ctas > 1 ? (int)(blockIdx.x % p.row.ctas) : 0;
     const int64_t r = blockIdx.x / p.row.ctas;
-    const RowSlice<T> S(p.row, r, rank);
+    const RowStream<T, THREADS> S(p.row, r, rank);
+    const bool exchange = !BACKWARD && p.row.ctas > 1;
     wait_for_previous_grid();
     const float weight = p.row_weight ? p.row_weight[r] : 1.0f;
-    T* grad = p.grad ? static_cast<T*>(p.grad) + r * p.ld_grad : nullptr;
+    T* grad = p.grad ? static_cast<T*>(p.grad) + r * p.ld_grad - S.begin : nullptr;  // of slot 0
+    const bool vectors = (reinterpret_cast<uintptr_t>(grad) & 15) == 0;
 
     if (weight == 0.0f) {  // a row that counts nothing is not read
         if (grad)
-            for (int s = S.begin + t; s < S.end; s += kDistillThreads) grad[S.element0 + s] = V::from_f32(0.0f);
+            for (int v = S.v0 + t; v < S.v1; v += THREADS) {
+                if (vectors && S.whole(v)) {
+                    __stcs(reinterpret_cast<uint4*>(grad) + v, make_uint4(0, 0, 0, 0));
+                } else {
+                    for (int j = 0; j < kN; ++j)
+                        if (S.holds((int64_t)v * kN + j)) grad[(int64_t)v * kN + j] = V::from_f32(0.0f);
+                }
+            }
         if (!BACKWARD && rank == 0 && t == 0) {
             p.loss[r] = 0.0f;
             if (p.stats) p.stats[2 * r] = p.stats[2 * r + 1] = 0.0f;
@@ -118,107 +117,117 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill_top(const __grid_co
         return;
     }
 
-    if (!BACKWARD) cluster_arrive();
-    S.load(slice, bars, never);
-    const float inv_tau = 1.0f / p.temperature;
-    if (t < 32) {
-        int n_listed;
-        const float sum = teacher_side(p, r, inv_tau, logp, entry, &n_listed);
-        if (t == 0) {
-            float rest = p.teacher_lse && n_listed < p.row.vocab ? fmaxf(1.0f - sum, 0.0f) : 0.0f;
-            teacher[0] = sum + rest;
-            teacher[1] = rest;
-        }
+    if (exchange) cluster_arrive();
+    uint4 raw[kHand];
+    S.load_group(raw, 0);
+    for (int w = t; w < mask_words; w += THREADS) reinterpret_cast<uint32_t*>(mask)[w] = 0;
+    if (t == 0) *n_listed = 0;
+    for (int k = t; k < p.k; k += THREADS) {
+        const int32_t e = p.indices[r * p.k + k];
+        const bool here = e >= 0 && e < p.row.vocab;
+        entry[k] = here ? e : -1;
+        logp[k] = here ? p.values[r * p.k + k] : neg_inf();
+        // a backward call needs only its own share's (another CTA may already
+        // have put the gradient in the place of the others)
+        const int64_t s = (int64_t)S.begin + e;
+        own[k] = here && (!BACKWARD || (s >= (int64_t)S.v0 * kN && s < (int64_t)S.v1 * kN)) ? V::to_f32(S.slot0[s])
+                                                                                           : neg_inf();
     }
     __syncthreads();
-    if (t == 0 && p.row.force_timeout_ns && !mbar_wait_bounded(never, 0, p.row.force_timeout_ns))
-        record_timeout(p.row.status);
-
-    const float mass = teacher[0], p_rest = teacher[1];
+    const float inv_tau = 1.0f / p.temperature;
     const float c2 = kLog2e * inv_tau;
-    float mine = 0.0f;  // this thread's largest logit, listed or not
-    if (BACKWARD) {
-        for (int c = 0; c < kRowChunks; ++c)
-            if (!mbar_wait_bounded(bars + c, 0, p.row.timeout_ns)) record_timeout(p.row.status);
-    } else {
-        mine = S.largest(slice, bars, p.row);
-        cluster_wait();  // every CTA of the row has started: its shared memory may be written
-        __syncthreads();
-    }
-    // take the listed entry of this thread out of the slice
-    const int listed = t < p.k && entry[t] >= 0 ? S.slot_of(entry[t]) : -1;
-    float own = neg_inf();
-    if (listed >= 0) {
-        own = V::to_f32(slice[listed]);
-        slice[listed] = V::from_f32(neg_inf());
-        if (!BACKWARD) st_peer(peer_addr(smem_u32(all + t), 0), own);
-    }
-
-    float m_rest, coef, q_rest;          // of the whole row (backward: m_rest is the rest's lse)
-    float m_all, log_s = 0.0f;           // lse = m_all / tau + log_s (backward: lse = m_all)
-    if constexpr (!BACKWARD) {
-        const int warp = t >> 5, lane = t & 31;
-        // the base is the largest logit, even a listed one: the rest's sum is
-        // fine about it unless the rest lies far below, which is then redone
-        float m = block_max(mine, scratch);
-        ExpBase at(m, c2);
-        float s = warp_sum(sum_exponentials(slice, S.n_vecs, t, kDistillThreads, c2, at)) * at.fix;
-        // the listed entries held here, as a second sum (one a thread)
-        float m_in = neg_inf(), s_in = 0.0f;
-        if (t < kMaxTop) {
-            m_in = lanes_max(own, 0xffffffffu);
-            s_in = warp_sum(own == neg_inf() ? 0.0f : exp2f((own - m_in) * c2));
+    for (int k = t; k < p.k; k += THREADS)
+        if (entry[k] >= 0) {
+            atomicAdd(n_listed, 1);
+            const int64_t s = (int64_t)S.begin + entry[k];
+            const int v = (int)(s / kN) - S.v0;
+            if (v >= 0 && v < S.v1 - S.v0)
+                atomicOr(reinterpret_cast<uint32_t*>(mask) + v / 4, 1u << ((v % 4) * 8 + (int)(s % kN)));
         }
+    if (warp == THREADS / 32 - 1) {
+        const float sum = teacher_side(p, r, inv_tau, logp);
+        // the listed entries' own sum of exponentials
+        float m_in = neg_inf();
+        for (int k = lane; k < p.k; k += 32) m_in = fmaxf(m_in, own[k]);
+        m_in = lanes_max(m_in, 0xffffffffu);
+        float s_in = 0.0f;
+        for (int k = lane; k < p.k; k += 32) s_in += m_in == neg_inf() ? 0.0f : exp2f((own[k] - m_in) * c2);
+        s_in = warp_sum(s_in);
         if (lane == 0) {
-            scratch[16 + warp] = s;
-            scratch[32 + warp] = m_in;
-            scratch[48 + warp] = s_in;
+            teacher[0] = sum;
+            teacher[2] = m_in;
+            teacher[3] = s_in;
         }
-        __syncthreads();
-        constexpr int kW = kDistillThreads / 32;
-        float sum = warp_sum(lane < kW ? scratch[16 + lane] : 0.0f);
-        if (sum < 1e-20f) {
-            m = block_max(largest(slice, S.n_vecs), scratch);
-            at = ExpBase(m, c2);
-            s = warp_sum(sum_exponentials(slice, S.n_vecs, t, kDistillThreads, c2, at)) * at.fix;
-            if (lane == 0) scratch[16 + warp] = s;
-            __syncthreads();
-            sum = warp_sum(lane < kW ? scratch[16 + lane] : 0.0f);
+    }
+    if (t == 0 && p.row.force_timeout_ns) {
+        mbar_init(never, 1);
+        if (!mbar_wait_bounded(never, 0, p.row.force_timeout_ns)) record_timeout(p.row.status);
+    }
+    __syncthreads();
+    const float sum_p = teacher[0];
+    const float p_rest = p.teacher_lse && *n_listed < p.row.vocab ? fmaxf(1.0f - sum_p, 0.0f) : 0.0f;
+    const float mass = sum_p + p_rest;
+    const int groups = S.groups();
+
+    // -inf in the places of a vector's listed elements
+    auto drop = [&](uint4& x, int v) {
+        const unsigned listed = v < S.v1 ? mask[v - S.v0] : 0;
+        if (listed) {
+            uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int j = 0; j < kN; ++j)
+                if (listed >> j & 1) V::put(w, j, V::from_f32(neg_inf()));
+            x = make_uint4(w[0], w[1], w[2], w[3]);
         }
-        if (warp == 0) {
-            const float x = lane < kW ? scratch[32 + lane] : neg_inf();
-            m_in = lanes_max(x, 0xffffffffu);
-            s_in = warp_sum(x == neg_inf() ? 0.0f : scratch[48 + lane] * exp2f((x - m_in) * c2));
-            if (lane < p.row.ctas) {
-                const uint32_t to = peer_addr(smem_u32(&parts[rank][0]), (uint32_t)lane);
-                st_peer(to, m);
-                st_peer(to + 4, sum);
-                st_peer(to + 8, m_in);
-                st_peer(to + 12, s_in);
+    };
+
+    float m_rest, coef, q_rest;  // of the whole row (backward: m_rest is the rest's lse)
+    float m_all, log_s = 0.0f;   // lse = m_all / tau + log_s (backward: lse = m_all)
+    if constexpr (!BACKWARD) {
+        RunningSum run;
+        for (int g = 0; g < groups; ++g) {
+            uint4 next[kHand];
+            if (g + 1 < groups) S.load_group(next, g + 1);
+            typename V::Max top = V::lowest();
+#pragma unroll
+            for (int u = 0; u < kHand; ++u) {
+                drop(raw[u], S.vec(g, u));
+                top = V::larger(top, V::larger(raw[u]));
             }
+            run.template add<T>(raw, top, c2);
+#pragma unroll
+            for (int u = 0; u < kHand; ++u) raw[u] = next[u];
         }
-        cluster_sync();
-        float m_listed = neg_inf(), s_listed = 0.0f, s_rest = 0.0f;
-        m_rest = neg_inf();
-        for (int c = 0; c < p.row.ctas; ++c) {
-            merge_sum(m_rest, s_rest, parts[c][0], parts[c][1], c2);
-            merge_sum(m_listed, s_listed, parts[c][2], parts[c][3], c2);
+        if (p.grad) S.load_group(raw, 0);  // for the second pass
+        float s_rest;
+        block_sum<THREADS>(run, c2, scratch, m_rest, s_rest);
+        if (is_low(m_rest, c2)) s_rest = low_sum(S, m_rest, c2, scratch, drop);
+        if (exchange) {
+            cluster_wait();  // every CTA of the row has started: its shared memory may be written
+            if (t < p.row.ctas) {
+                const uint32_t to = peer_addr(smem_u32(&parts[rank][0]), (uint32_t)t);
+                st_peer(to, m_rest);
+                st_peer(to + 4, s_rest);
+            }
+            cluster_sync();
+            m_rest = neg_inf();
+            s_rest = 0.0f;
+            for (int c = 0; c < p.row.ctas; ++c) merge_sum(m_rest, s_rest, parts[c][0], parts[c][1], c2);
         }
-        float s_all = s_rest;
         m_all = m_rest;
-        merge_sum(m_all, s_all, m_listed, s_listed, c2);
+        float s_all = s_rest;
+        merge_sum(m_all, s_all, teacher[2], teacher[3], c2);
         log_s = logf(s_all);
         const bool some = m_rest != neg_inf();
         const float log_q_rest = some ? (m_rest - m_all) * inv_tau + (logf(s_rest) - log_s) : neg_inf();
         q_rest = expf(log_q_rest);
         coef = some ? (mass * q_rest - p_rest) / s_rest : 0.0f;
-        if (rank == 0 && t < 32) {
+        if (rank == 0 && warp == 0) {
             float loss = 0.0f;
-            for (int k = t; k < p.k; k += 32)
-                if (entry[k] >= 0)
-                    loss += kl_term(expf(logp[k]), logp[k], (all[k] - m_all) * inv_tau - log_s);
+            for (int k = lane; k < p.k; k += 32)
+                if (entry[k] >= 0) loss += kl_term(expf(logp[k]), logp[k], (own[k] - m_all) * inv_tau - log_s);
             loss = warp_sum(loss);
-            if (t == 0) {
+            if (lane == 0) {
                 loss += kl_term(p_rest, logf(p_rest), log_q_rest);
                 if (m_all == neg_inf()) loss = __int_as_float(0x7F800000);  // q is 0 everywhere
                 p.loss[r] = mass > 0.0f ? loss : 0.0f;
@@ -242,45 +251,62 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill_top(const __grid_co
     const float scale = none ? 0.0f : weight * inv_tau;
     coef *= scale;
 
-    // the unlisted entries: coef 2^(x c - base), or coef e^(z - lse) from
-    // kept statistics
-    T* out = grad + S.element0;  // of slot 0
-    const bool vectors = (reinterpret_cast<uintptr_t>(out) & 15) == 0;
-    const ExpBase at(BACKWARD ? 0.0f : m_rest, c2);
-    coef *= at.fix;
-    const float2 kk = make_float2(coef, coef);
-    if (BACKWARD) __syncthreads();
-#pragma unroll 2
-    for (int v = t; v < S.n_vecs; v += kDistillThreads) {
-        constexpr int kP = kN / 2;
-        float2 x[kP];
-        V::unpack(reinterpret_cast<const uint4*>(slice)[v], x);
-        if constexpr (BACKWARD) {
+    // the unlisted entries: coef 2^(x c - base), or coef e^(z - lse) from kept
+    // statistics
+    const float base = m_rest == neg_inf() ? 0.0f : exp_base(m_rest, c2);
+    const bool low = !BACKWARD && base == kFloor;  // the subtraction first: see exp_base
+    if (!BACKWARD && !low) coef *= m_rest == neg_inf() ? 1.0f : exp_fix(m_rest, c2, base);
+    const float2 cc = make_float2(c2, c2), bb = make_float2(-base, -base), kk = make_float2(coef, coef);
+    for (int g = 0; g < groups; ++g) {
+        uint4 next[kHand];
+        if (g + 1 < groups) S.load_group(next, g + 1);
 #pragma unroll
-            for (int j = 0; j < kP; ++j)
-                x[j] = make_float2(ex2(scaled_less(x[j].x, p.temperature, inv_tau, m_rest) * kLog2e),
-                                   ex2(scaled_less(x[j].y, p.temperature, inv_tau, m_rest) * kLog2e));
-        } else {
-            at.apply(x, c2);
-        }
+        for (int u = 0; u < kHand; ++u) {
+            const int v = S.vec(g, u);
+            if (v >= S.v1) break;
+            if (BACKWARD || low) drop(raw[u], v);
+            float2 x[kP];
+            V::unpack(raw[u], x);
+            if constexpr (BACKWARD) {
 #pragma unroll
-        for (int j = 0; j < kP; ++j) x[j] = __fmul2_rn(kk, x[j]);
-        if (vectors && S.whole(v)) {
-            __stcs(reinterpret_cast<uint4*>(out) + v, V::pack(x));
-        } else {
+                for (int j = 0; j < kP; ++j)
+                    x[j] = make_float2(ex2(scaled_less(x[j].x, p.temperature, inv_tau, m_rest) * kLog2e),
+                                       ex2(scaled_less(x[j].y, p.temperature, inv_tau, m_rest) * kLog2e));
+            } else if (low) {
 #pragma unroll
-            for (int j = 0; j < kN; ++j) {
-                const int s = v * kN + j;
-                if (s >= S.begin && s < S.end) out[s] = V::from_f32(j & 1 ? x[j / 2].y : x[j / 2].x);
+                for (int j = 0; j < kP; ++j)
+                    x[j] = make_float2(ex2((x[j].x - m_rest) * c2), ex2((x[j].y - m_rest) * c2));
+            } else {
+#pragma unroll
+                for (int j = 0; j < kP; ++j) {
+                    x[j] = __ffma2_rn(x[j], cc, bb);
+                    x[j] = make_float2(ex2(x[j].x), ex2(x[j].y));
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kP; ++j) x[j] = __fmul2_rn(kk, x[j]);
+            if (vectors && S.whole(v)) {
+                __stcs(reinterpret_cast<uint4*>(grad) + v, V::pack(x));
+            } else {
+#pragma unroll
+                for (int j = 0; j < kN; ++j) {
+                    const int64_t s = (int64_t)v * kN + j;
+                    if (S.holds(s)) grad[s] = V::from_f32(j & 1 ? x[j / 2].y : x[j / 2].x);
+                }
             }
         }
+#pragma unroll
+        for (int u = 0; u < kHand; ++u) raw[u] = next[u];
     }
     __syncthreads();
-    // then the listed ones over the zeros left in their places
-    if (listed >= 0) {
-        const float log_q = BACKWARD ? scaled_less(own, p.temperature, inv_tau, m_all)
-                                     : (own - m_all) * inv_tau - log_s;
-        out[listed] = V::from_f32(none ? 0.0f : scale * (mass * expf(log_q) - expf(logp[t])));
+    // then the listed ones over what was left in their places
+    for (int k = t; k < p.k; k += THREADS) {
+        if (entry[k] < 0) continue;
+        const int64_t s = (int64_t)S.begin + entry[k];
+        if (s / kN < S.v0 || s / kN >= S.v1) continue;
+        const float log_q = BACKWARD ? scaled_less(own[k], p.temperature, inv_tau, m_all)
+                                     : (own[k] - m_all) * inv_tau - log_s;
+        grad[s] = V::from_f32(none ? 0.0f : scale * (mass * expf(log_q) - expf(logp[k])));
     }
 }
 

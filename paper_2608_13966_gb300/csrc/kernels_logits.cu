@@ -1,21 +1,45 @@
 // Instantiations of the kernels over rows of logits.
+#include "distill.cuh"
 #include "top_logits.cuh"
 
 namespace quasar {
 
-const void* distill_kernel(bool f32, bool backward)
+namespace {
+
+template <typename T, int THREADS>
+const void* distill(bool backward)
 {
-    if (f32)
-        return backward ? reinterpret_cast<const void*>(&k_distill_top<float, true>)
-                        : reinterpret_cast<const void*>(&k_distill_top<float, false>);
-    return backward ? reinterpret_cast<const void*>(&k_distill_top<__nv_bfloat16, true>)
-                    : reinterpret_cast<const void*>(&k_distill_top<__nv_bfloat16, false>);
+    return backward ? reinterpret_cast<const void*>(&k_distill_top<T, THREADS, true>)
+                    : reinterpret_cast<const void*>(&k_distill_top<T, THREADS, false>);
 }
 
-const void* top_logits_kernel(bool f32)
+}  // namespace
+
+const void* distill_kernel(bool f32, int threads, bool backward)
 {
-    return f32 ? reinterpret_cast<const void*>(&k_top_logits<float>)
-               : reinterpret_cast<const void*>(&k_top_logits<__nv_bfloat16>);
+    if (f32) return threads == kFewThreads ? distill<float, kFewThreads>(backward) : distill<float, kRowThreads>(backward);
+    return threads == kFewThreads ? distill<__nv_bfloat16, kFewThreads>(backward)
+                                  : distill<__nv_bfloat16, kRowThreads>(backward);
+}
+
+const void* top_logits_kernel(bool f32, int threads)
+{
+    if (f32)
+        return threads == kFewThreads ? reinterpret_cast<const void*>(&k_top_logits<float, kFewThreads>)
+                                      : reinterpret_cast<const void*>(&k_top_logits<float, kRowThreads>);
+    return threads == kFewThreads ? reinterpret_cast<const void*>(&k_top_logits<__nv_bfloat16, kFewThreads>)
+                                  : reinterpret_cast<const void*>(&k_top_logits<__nv_bfloat16, kRowThreads>);
+}
+
+size_t top_logits_smem(int threads, int ctas, int k)
+{
+    return (size_t)kTopVectors * 20 + (size_t)kTopKeys * 8 + (ctas > 1 ? (size_t)ctas * k * 8 : 0) + 8 + kRowCtas * 8 +
+           64 * 4 + 6 * 4 + (size_t)threads * 2;
+}
+
+size_t distill_smem(int vecs)
+{
+    return (size_t)(vecs + 15) / 16 * 16 + 3 * kMaxTop * 4 + 64 * 4 + 4 * 4 + kRowCtas * 8 + 8 + 8;
 }
 
 }  // namespace quasar

@@ -8,18 +8,18 @@ namespace quasar {
 
 constexpr int kMaxTop = 256;          // most entries of a row's top list
 constexpr int kRowCtas = 8;           // most CTAs (one cluster) a row is spread over
-constexpr int kRowChunks = 4;         // copies a CTA's slice arrives in
+constexpr int kRowThreads = 512;      // of a CTA
+constexpr int kFewThreads = 128;      // ... whose share is no more than kFewVectors
+constexpr int kFewVectors = 1024;
 
-// A row of logits spread over a cluster: each CTA holds a slice in shared
-// memory, `vecs` vectors of 16 bytes at most.
+// A row is shared out to `ctas` CTAs, `vecs` 16-byte vectors each.
 struct RowParams {
     const void* logits;
     int64_t ld;
     int64_t rows;
     int64_t vocab;
     int ctas;       // of a cluster
-    int vecs;       // of a slice
-    uint64_t timeout_ns;
+    int vecs;       // of a CTA's share
     uint64_t force_timeout_ns;
     unsigned int* status;
 };

@@ -5,26 +5,29 @@
 // unsigned comparison follows the floats', above the complement of the index,
 // so that equal values rank by the lowest index and no two keys are equal.
 //
-// Each CTA of a row's cluster finds the k largest of its slice.  A bound on
-// the k-th comes from the threads' own maxima: the k-th largest of them (in
-// 16 bits, rounded down) has at least k elements at or above it, and not many
-// more unless the row is made of ties.  One warp settles the bound; then, in
-// the pass that sums the exponentials, each 16-byte vector's maximum is
-// compared with it, and the few vectors that reach it are looked into
-// afterwards, an element a thread.  The elements found are ranked by counting.
-// A slice with more of them than the lists hold is settled by bisection on
-// the 64-bit keys, which is exact for any data.  The slices' lists, sorted,
-// are merged by rank 0: an entry's rank is its place in its own list plus, by
-// binary search, the entries above it in the others.
+// A row is read once.  The threads' maxima over the first vectors they hold (8
+// each; in fours where k <= 64) bound the k-th largest: the k-th largest of
+// those maxima, in 16 bits rounded down, has at least k elements at or above
+// it.  A vector of the rest
+// is looked into only if its maximum reaches the bound; with 131,072 bf16
+// logits, k = 64 and values in no particular order that is about 350 of 16,384
+// vectors.  Those are put aside, their elements at or above the bound are
+// gathered, a second bound among the gathered (a bit a step, by the whole CTA)
+// leaves little more than k, and they are ranked by counting.  A row
+// that puts aside more than the lists hold (rising order, ties, fewer than k
+// that are not -inf) is settled by bisection on the 64-bit keys, which is
+// exact for any data and reads the row once more for each bit.  Where a
+// cluster shares a row, its lists, sorted, are merged by rank 0: an entry's
+// rank is its place in its own list plus, by binary search, the entries above
+// it in the others.
 #pragma once
 
-#include "distill.cuh"
+#include "row_stream.cuh"
 
 namespace quasar {
 
-constexpr int kTopThreads = 512;
-constexpr int kTopList = 512;  // vectors or elements a slice may gather before bisection
-constexpr int kTopBounds = kTopThreads;  // maxima the bound is taken from
+constexpr int kTopVectors = 1024;  // vectors a share may put aside before bisection
+constexpr int kTopKeys = 2048;     // elements of them at or above the bound
 
 // Both zeros are one value, and NaN ranks above everything.
 __device__ __forceinline__ uint32_t ordered_bits(float x)
@@ -43,19 +46,19 @@ __device__ __forceinline__ uint64_t top_key(float x, int64_t e)
     return ((uint64_t)ordered_bits(x) << 32) | (uint32_t)~(uint32_t)e;
 }
 
-// The want-th largest of the kTopBounds 16-bit maxima (0 if there are fewer),
-// by one warp, a bit a step.
-__device__ __forceinline__ uint32_t kth_largest(const uint16_t* maxima, int want)
+// The largest 16-bit value that at least `want` of 32 EACH values reach (the
+// want-th largest), by one warp, a bit a step from the highest in which any
+// two differ.
+template <int EACH>
+__device__ __forceinline__ uint32_t kth_largest(const uint16_t* values, int want)
 {
-    constexpr int kEach = kTopBounds / 32;
     const int lane = threadIdx.x & 31;
-    uint32_t key[kEach];
+    uint32_t key[EACH];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) key[i] = maxima[32 * i + lane];
-    // the bits above the highest in which any two differ are settled already
+    for (int i = 0; i < EACH; ++i) key[i] = values[32 * i + lane];
     uint32_t high = key[0], low = key[0];
 #pragma unroll
-    for (int i = 1; i < kEach; ++i) {
+    for (int i = 1; i < EACH; ++i) {
         high = max(high, key[i]);
         low = min(low, key[i]);
     }
@@ -68,135 +71,261 @@ __device__ __forceinline__ uint32_t kth_largest(const uint16_t* maxima, int want
         const uint32_t trial = bound | (1u << b);
         int c = 0;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) c += key[i] >= trial;
+        for (int i = 0; i < EACH; ++i) c += key[i] >= trial;
         if (__reduce_add_sync(0xffffffffu, c) >= want) bound = trial;
     }
     return bound;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kTopThreads) k_top_logits(const __grid_constant__ TopParams p)
+// A place in a list for each lane with `want`, one atomic a warp; the lanes
+// of the warp that call it do so together.
+__device__ __forceinline__ int take_place(int* count, bool want)
+{
+    const unsigned active = __activemask();
+    const unsigned who = __ballot_sync(active, want);
+    if (who == 0) return 0;
+    const int lane = threadIdx.x & 31, leader = __ffs(who) - 1;
+    int first = 0;
+    if (lane == leader) first = atomicAdd(count, __popc(who));
+    return __shfl_sync(active, first, leader) + __popc(who & ((1u << lane) - 1));
+}
+
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_top_logits(const __grid_constant__ TopParams p)
 {
     using V = Vec16<T>;
     constexpr int kN = V::kN;
     extern __shared__ __align__(128) uint8_t smem_raw[];
-    T* slice = reinterpret_cast<T*>(smem_raw);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem_raw + (size_t)p.row.vecs * 16);
-    uint64_t* never = bars + kRowChunks;
-    uint64_t* list = never + 1;                        // [kTopList]
-    uint64_t* merged = list + kTopList;                // rank 0: [ctas][k]
-    float(*parts)[2] = reinterpret_cast<float(*)[2]>(merged + (size_t)p.row.ctas * p.k);
-    float* scratch = reinterpret_cast<float*>(parts + kRowCtas);      // [2][warps]
-    uint16_t* maxima = reinterpret_cast<uint16_t*>(scratch + 32);     // [kTopBounds]
-    uint16_t* found = maxima + kTopBounds;                            // [kTopList] vectors
-    int* count = reinterpret_cast<int*>(found + kTopList);  // elements, vectors
-    uint32_t* shared_bound = reinterpret_cast<uint32_t*>(count + 2);
+    uint4* aside = reinterpret_cast<uint4*>(smem_raw);               // [kTopVectors]
+    uint64_t* list = reinterpret_cast<uint64_t*>(aside + kTopVectors);  // [kTopKeys]
+    uint64_t* few = reinterpret_cast<uint64_t*>(aside);              // [kTopKeys], once the vectors are done with
+    int32_t* aside_at = reinterpret_cast<int32_t*>(list + kTopKeys);  // [kTopVectors]
+    uint64_t* merged = reinterpret_cast<uint64_t*>(aside_at + kTopVectors);  // rank 0: [ctas][k]
+    uint64_t* never = merged + (p.row.ctas > 1 ? (size_t)p.row.ctas * p.k : 0);
+    float(*parts)[2] = reinterpret_cast<float(*)[2]>(never + 1);     // [kRowCtas]
+    float* scratch = reinterpret_cast<float*>(parts + kRowCtas);     // [2][32]
+    int* count = reinterpret_cast<int*>(scratch + 64);               // vectors, keys, survivors
+    uint32_t* bounds = reinterpret_cast<uint32_t*>(count + 3);       // [2]
+    uint16_t* maxima = reinterpret_cast<uint16_t*>(bounds + 3);      // [THREADS]
 
-    const int t = threadIdx.x;
-    const int rank = (int)(blockIdx.x % p.row.ctas);
+    const int t = threadIdx.x, warp = t >> 5;
+    const int rank = p.row.ctas > 1 ? (int)(blockIdx.x % p.row.ctas) : 0;
     const int64_t r = blockIdx.x / p.row.ctas;
-    const RowSlice<T> S(p.row, r, rank);
-    cluster_arrive();
+    const RowStream<T, THREADS> S(p.row, r, rank);
+    if (p.row.ctas > 1) cluster_arrive();
     wait_for_previous_grid();
-    if (t == 0) count[0] = count[1] = 0;
-    S.load(slice, bars, never);
-    __syncthreads();
-    if (t == 0 && p.row.force_timeout_ns && !mbar_wait_bounded(never, 0, p.row.force_timeout_ns))
-        record_timeout(p.row.status);
+    uint4 raw[kHand], next[kHand];
+    S.load_group(raw, 0);
+    S.load_group(next, 1);
+    if (t < 3) count[t] = 0;
+    if (t == 3) bounds[1] = 0;
+    if (t == 0 && p.row.force_timeout_ns) {
+        mbar_init(never, 1);
+        if (!mbar_wait_bounded(never, 0, p.row.force_timeout_ns)) record_timeout(p.row.status);
+    }
 
     const float c2 = kLog2e / p.temperature;
-    const uint4* vecs = reinterpret_cast<const uint4*>(slice);
-    const int warp = t >> 5, lane = t & 31;
-    const int have = S.end - S.begin;
-    const int want = have < p.k ? have : p.k;
-    const float mine = S.largest(slice, bars, p.row);
-    cluster_wait();  // every CTA of the row has started: its shared memory may be written
-    // 0 where a thread held nothing: it must not count towards the bound
-    maxima[t] = (uint16_t)(S.holds(t) ? ordered_bits(mine) >> 16 : 0);
-    const float m = block_max(mine, scratch);
-    // one warp settles the bound while the others sum the exponentials
+    const int groups = S.groups();
+    // elements of this share, and how many of its largest are wanted
+    const int64_t first = max((int64_t)S.v0 * kN, (int64_t)S.begin);
+    const int have = (int)max((int64_t)0, min((int64_t)S.v1 * kN, S.end) - first);
+    const int want = min(have, p.k);
+
+    auto top_of = [](const uint4 (&x)[kHand]) {
+        typename V::Max m = V::larger(x[0]);
+#pragma unroll
+        for (int u = 1; u < kHand; ++u) m = V::larger(m, V::larger(x[u]));
+        return m;
+    };
+    const typename V::Max top0 = top_of(raw), top1 = top_of(next);
+    // (0 from a thread that holds nothing: it must not count)
+    uint32_t best = t < S.v1 - S.v0 ? ordered_bits(V::value(V::larger(top0, top1))) >> 16 : 0;
+    const bool fours = THREADS > 128 && p.k <= 64;
+    if (fours) {
+        best = max(best, __shfl_xor_sync(0xffffffffu, best, 1));
+        best = max(best, __shfl_xor_sync(0xffffffffu, best, 2));
+        if ((t & 3) == 0) maxima[t / 4] = (uint16_t)best;
+    } else {
+        maxima[t] = (uint16_t)best;
+    }
+    __syncthreads();
+    // one warp settles the bound while the others begin the sum
     if (warp == 0) {
-        const uint32_t b = kth_largest(maxima, want) << 16;
-        if (lane == 0) *shared_bound = b;
-    } else if (p.lse) {
-        const ExpBase at(m, c2);
-        const float s = warp_sum(sum_exponentials(slice, S.n_vecs, t - 32, kTopThreads - 32, c2, at)) * at.fix;
-        if (lane == 0) scratch[16 + warp] = s;
+        const uint32_t b = fours ? kth_largest<THREADS / 128>(maxima, want) : kth_largest<THREADS / 32>(maxima, want);
+        if (t == 0) bounds[0] = b << 16;
+    }
+    RunningSum run;
+    if (p.lse) {
+        run.template add<T>(raw, top0, c2);
+        run.template add<T>(next, top1, c2);
     }
     __syncthreads();
-    if (p.lse && warp == 1) {
-        const float sum = warp_sum(lane > 0 && lane < kTopThreads / 32 ? scratch[16 + lane] : 0.0f);
-        if (lane == 0) {
-            const uint32_t to = peer_addr(smem_u32(&parts[rank][0]), 0);
-            st_peer(to, m);
-            st_peer(to + 4, sum);
-        }
-    }
-    // the vectors that hold an element at or above the bound (a NaN compares
-    // as if it did)
-    const uint32_t bound = *shared_bound;
+    const uint32_t bound = bounds[0];
     const float least = from_ordered(bound);
-#pragma unroll 4
-    for (int v = t; v < S.n_vecs; v += kTopThreads)
-        if (!(V::value(V::larger(vecs[v])) < least)) {
-            const int i = atomicAdd(count + 1, 1);
-            if (i < kTopList) found[i] = (uint16_t)v;
-        }
-    __syncthreads();
-    // an element a thread of the vectors found
-    const int n_found = count[1];
-    for (int i = t; i < min(n_found, kTopList) * kN; i += kTopThreads) {
-        const int at_slot = found[i / kN] * kN + i % kN;
-        const float x = V::to_f32(slice[at_slot]);
-        if (ordered_bits(x) >= bound && at_slot >= S.begin && at_slot < S.end) {
-            const int j = atomicAdd(count, 1);
-            if (j < kTopList) list[j] = top_key(x, S.element0 + at_slot);
-        }
-    }
-    __syncthreads();
-    int n = n_found > kTopList ? kTopList + 1 : *count;
-    if (n > kTopList) {
-        // exact: the want-th largest key, and the keys from it up
-        uint64_t floor_key = 0;
-        for (int b = 63; b >= 0; --b) {
-            const uint64_t trial = floor_key | (1ull << b);
-            int c = 0;
-            for (int i = t; i < have; i += kTopThreads)
-                c += top_key(V::to_f32(slice[S.begin + i]), S.element0 + S.begin + i) >= trial;
-            c = __reduce_add_sync(0xffffffffu, c);
-            __syncthreads();
-            if (t == 0) *count = 0;
-            __syncthreads();
-            if ((t & 31) == 0) atomicAdd(count, c);
-            __syncthreads();
-            if (*count >= want) floor_key = trial;
-        }
-        __syncthreads();
-        if (t == 0) *count = 0;
-        __syncthreads();
-        for (int i = t; i < have; i += kTopThreads) {
-            const uint64_t key = top_key(V::to_f32(slice[S.begin + i]), S.element0 + S.begin + i);
-            if (key >= floor_key) {
-                const int j = atomicAdd(count, 1);
-                if (j < kTopList) list[j] = key;
+
+    // put a vector aside if its maximum reaches the bound (a NaN, or a bound
+    // that is none, compares as if it did)
+    auto keep = [&](const uint4& x, int v) {
+        if (!(V::value(V::larger(x)) < least) && v < S.v1) {
+            const int i = atomicAdd(count, 1);
+            if (i < kTopVectors) {
+                aside[i] = x;
+                aside_at[i] = v;
             }
         }
+    };
+#pragma unroll
+    for (int u = 0; u < kHand; ++u) keep(raw[u], S.vec(0, u));
+#pragma unroll
+    for (int u = 0; u < kHand; ++u) keep(next[u], S.vec(1, u));
+    if (groups > 2) S.load_group(raw, 2);
+    for (int g = 2; g < groups; ++g) {
+        if (g + 1 < groups) S.load_group(next, g + 1);
+#pragma unroll
+        for (int u = 0; u < kHand; ++u) keep(raw[u], S.vec(g, u));
+        if (p.lse) run.template add<T>(raw, top_of(raw), c2);
+#pragma unroll
+        for (int u = 0; u < kHand; ++u) raw[u] = next[u];
+    }
+    float m = neg_inf(), s = 0.0f;
+    if (p.lse) {
+        block_sum<THREADS>(run, c2, scratch, m, s);
+        if (is_low(m, c2)) s = low_sum(S, m, c2, scratch, [](uint4&, int) {});
+        if (p.row.ctas == 1 && t == 0)
+            p.lse[r] = m == neg_inf() && s == 0.0f ? neg_inf() : m / p.temperature + logf(s);
+    }
+    __syncthreads();
+
+    const int n_aside = count[0];
+    int n = kTopKeys + 1;
+    if (n_aside <= kTopVectors) {
+        // an element a thread
+        for (int i = t; i < (n_aside * kN + 31) / 32 * 32; i += THREADS) {
+            bool in = i < n_aside * kN;
+            const int at = in ? i / kN : 0;
+            const int64_t slot = (int64_t)aside_at[at] * kN + i % kN;
+            const float f = V::get(aside[at], i % kN);
+            in = in && ordered_bits(f) >= bound && S.holds(slot);
+            const int j = take_place(count + 1, in);
+            if (in && j < kTopKeys) list[j] = top_key(f, slot - S.begin);
+        }
         __syncthreads();
-        n = *count < kTopList ? *count : kTopList;
+        n = count[1];
     }
-    // sorted into rank 0's row of the merge: the place is the number above
-    const uint32_t to = peer_addr(smem_u32(merged + (size_t)rank * p.k), 0);
-    for (int i = t; i < n; i += kTopThreads) {
-        const uint64_t key = list[i];
+    if (n <= kTopKeys) {
+        // the want-th largest in 16 bits, a thread a key where they suffice
+        uint32_t key16[kTopKeys / THREADS];
+#pragma unroll
+        for (int q = 0; q < kTopKeys / THREADS; ++q) key16[q] = q * THREADS + t < n ? (uint32_t)(list[q * THREADS + t] >> 48) : 0;
+        uint32_t high = 0;
+#pragma unroll
+        for (int q = 0; q < kTopKeys / THREADS; ++q) high = max(high, key16[q]);
+        high = __reduce_max_sync(0xffffffffu, high);
+        if ((t & 31) == 0) atomicMax(bounds + 1, high);
+        __syncthreads();
+        // what is common to the bound and the largest is settled
+        int b = 31 - __clz(bounds[1] ^ (bound >> 16));
+        uint32_t second = bounds[1] >> (b + 1) << (b + 1);
+        for (; b >= 0; --b) {
+            const uint32_t trial = second | (1u << b);
+            int c;
+            if (n <= THREADS) {
+                c = __syncthreads_count(key16[0] >= trial);
+            } else {
+                c = 0;
+#pragma unroll
+                for (int q = 0; q < kTopKeys / THREADS; ++q) c += __syncthreads_count(key16[q] >= trial);
+            }
+            if (c >= want) second = trial;
+        }
+        const uint64_t least_key = (uint64_t)second << 48;
+        for (int i = t; i < (n + 31) / 32 * 32; i += THREADS) {
+            const uint64_t key = i < n ? list[i] : 0;
+            const bool in = i < n && key >= least_key;
+            const int j = take_place(count + 2, in);
+            if (in) few[j] = key;
+        }
+        __syncthreads();
+        n = count[2];
+    } else {
+        // exact: the want-th largest key of the share, a bit a pass, and the
+        // keys from it up
+        auto each = [&](auto use) {
+            for (int g = 0; g < groups; ++g)
+                for (int u = 0; u < kHand; ++u) {
+                    const int v = S.vec(g, u);
+                    if (v >= S.v1) break;
+                    const uint4 x = S.load(v);
+                    for (int j = 0; j < kN; ++j) {
+                        const int64_t slot = (int64_t)v * kN + j;
+                        if (S.holds(slot)) use(top_key(V::get(x, j), slot - S.begin));
+                    }
+                }
+        };
+        uint64_t floor_key = 0;
+        // every index is below the vocabulary: the bits above its length are
+        // set in every complement
+        const int index_bits = 32 - __clz((int)p.row.vocab);
+        for (int b = 63; b >= 0; --b) {
+            const uint64_t trial = floor_key | (1ull << b);
+            if (b < 32 && b >= index_bits) {
+                floor_key = trial;
+                continue;
+            }
+            int c = 0;
+            each([&](uint64_t key) { c += key >= trial; });
+            c = __reduce_add_sync(0xffffffffu, c);
+            __syncthreads();
+            if (t == 0) count[2] = 0;
+            __syncthreads();
+            if ((t & 31) == 0) atomicAdd(count + 2, c);
+            __syncthreads();
+            if (count[2] >= want) floor_key = trial;
+        }
+        __syncthreads();
+        if (t == 0) count[2] = 0;
+        __syncthreads();
+        each([&](uint64_t key) {
+            if (key >= floor_key) {
+                const int i = atomicAdd(count + 2, 1);
+                if (i < kTopKeys) few[i] = key;
+            }
+        });
+        __syncthreads();
+        n = min(count[2], kTopKeys);
+    }
+
+    // in order: a key's place is the number above it
+    const bool alone = p.row.ctas == 1;
+    if (!alone) cluster_wait();  // every CTA of the row has started: its shared memory may be written
+    const uint32_t to = alone ? 0 : peer_addr(smem_u32(merged + (size_t)rank * p.k), 0);
+    for (int i = t; i < (4 * n + 31) / 32 * 32; i += THREADS) {
+        // four threads a key, a quarter of the others each
+        const uint64_t key = i < 4 * n ? few[i / 4] : ~0ull;
         int above = 0;
-        for (int j = 0; j < n; ++j) above += list[j] > key;
-        if (above < p.k) st_peer(to + (uint32_t)above * 8, key);
+#pragma unroll 4
+        for (int j = i & 3; j < n; j += 4) above += few[j] > key;
+        above += __shfl_xor_sync(0xffffffffu, above, 1);
+        above += __shfl_xor_sync(0xffffffffu, above, 2);
+        if (i >= 4 * n || (i & 3) != 0 || above >= p.k) continue;
+        if (alone) {
+            p.values[r * p.k + above] = from_ordered((uint32_t)(key >> 32));
+            p.indices[r * p.k + above] = (int32_t)~(uint32_t)key;
+        } else {
+            st_peer(to + (uint32_t)above * 8, key);
+        }
     }
-    for (int i = n + t; i < p.k; i += kTopThreads) st_peer(to + (uint32_t)i * 8, (uint64_t)0);
+    if (alone) return;
+    for (int i = n + t; i < p.k; i += THREADS) st_peer(to + (uint32_t)i * 8, (uint64_t)0);
+    if (p.lse && t == 0) {
+        const uint32_t part = peer_addr(smem_u32(&parts[rank][0]), 0);
+        st_peer(part, m);
+        st_peer(part + 4, s);
+    }
     cluster_sync();
     if (rank != 0) return;
 
-    for (int i = t; i < p.row.ctas * p.k; i += kTopThreads) {
+    for (int i = t; i < p.row.ctas * p.k; i += THREADS) {
         const int c = i / p.k;
         const uint64_t key = merged[i];
         if (key == 0) continue;

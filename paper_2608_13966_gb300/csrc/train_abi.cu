@@ -21,8 +21,10 @@ const void* product_pair_kernel(bool a_mn, bool b_mn, bool promote);
 size_t product_pair_smem();
 const void* column_sum_kernel();
 const void* activation_grad_kernel();
-const void* distill_kernel(bool f32, bool backward);
-const void* top_logits_kernel(bool f32);
+const void* distill_kernel(bool f32, int threads, bool backward);
+const void* top_logits_kernel(bool f32, int threads);
+size_t distill_smem(int vecs);
+size_t top_logits_smem(int threads, int ctas, int k);
 }  // namespace quasar
 
 namespace {
@@ -187,11 +189,11 @@ quasar_status product(const Operand& a, const Operand& b, int64_t rows, int64_t 
 
 // -- rows of logits ----------------------------------------------------------------
 
-// How a row is spread: the fewest CTAs (a power of two) whose slices leave
-// room for three of them on an SM, then more while the rows alone leave SMs
-// idle and slices stay above 4 KB.
+// How a row is spread: one CTA, or more (a power of two, one cluster) while
+// the rows alone leave SMs idle and a share keeps at least 1,024 vectors (16
+// KB: below that the exchange costs more than the reading).
 quasar_status plan_rows(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows, int64_t vocab,
-                        size_t extra, RowParams* row, size_t* smem)
+                        RowParams* row, int* threads)
 {
     int n_sm = 0;
     quasar_status st = host_device(&n_sm, &row->status);
@@ -200,19 +202,14 @@ quasar_status plan_rows(const void* logits, quasar_dtype dtype, int64_t ld, int6
     row->ld = ld;
     row->rows = rows;
     row->vocab = vocab;
-    row->timeout_ns = host_timeout_ns();
     row->force_timeout_ns = host_forced_timeout_ns();
     const int64_t per = 16 / dtype_size(dtype);
     const int64_t vecs = (vocab + per - 1 + per - 1) / per;  // for any start within 16 bytes
-    auto slice = [&](int c) { return (vecs + c - 1) / c * 16; };
-    constexpr int64_t kThree = 75 * 1024;
     int c = 1;
-    while (c < kRowCtas && slice(c) + (int64_t)extra > kThree) c *= 2;
-    while (c < kRowCtas && rows * c < n_sm && slice(2 * c) >= 4096) c *= 2;
+    while (c < kRowCtas && rows * c < n_sm && vecs / (2 * c) >= 1024) c *= 2;
     row->ctas = c;
-    row->vecs = (int)(slice(c) / 16);
-    *smem = (size_t)slice(c) + extra;
-    if (*smem > 226 * 1024) return QUASAR_ERR_UNSUPPORTED;
+    row->vecs = (int)((vecs + c - 1) / c);
+    *threads = row->vecs <= kFewVectors ? kFewThreads : kRowThreads;
     if (rows * c > (int64_t(1) << 31) - 1) return QUASAR_ERR_UNSUPPORTED;
     return QUASAR_OK;
 }
@@ -221,14 +218,12 @@ quasar_status check_rows(const void* logits, quasar_dtype dtype, int64_t ld, int
                          int k, float temperature)
 {
     if (!valid_dtype(dtype) || !valid_shape(rows, vocab, ld)) return QUASAR_ERR_INVALID_ARG;
-    if (!(temperature > 0.0f) || !std::isfinite(temperature)) return QUASAR_ERR_INVALID_ARG;
+    if (!(temperature >= 1e-6f && temperature <= 1e6f)) return QUASAR_ERR_INVALID_ARG;
     if (vocab < 1 || k < 1 || k > vocab) return QUASAR_ERR_INVALID_ARG;
     if (k > kMaxTop) return QUASAR_ERR_UNSUPPORTED;
     if (rows > 0 && (!logits || !aligned(logits, (uintptr_t)dtype_size(dtype)))) return QUASAR_ERR_INVALID_ARG;
     return QUASAR_OK;
 }
-
-constexpr size_t kDistillExtra = (kRowChunks + 1) * 8 + 3 * kMaxTop * 4 + kRowCtas * 16 + 64 * 4 + 16 + kMaxTop * 4;
 
 quasar_status run_distill(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows, int64_t vocab,
                           const int32_t* indices, const float* values, int k, const float* teacher_lse,
@@ -262,8 +257,8 @@ quasar_status run_distill(const void* logits, quasar_dtype dtype, int64_t ld, in
             if (overlaps(outs[i], out_n[i], outs[j], out_n[j])) return QUASAR_ERR_INVALID_ARG;
     }
     DistillParams p{};
-    size_t smem = 0;
-    if ((st = plan_rows(logits, dtype, ld, rows, vocab, kDistillExtra, &p.row, &smem)) != QUASAR_OK) return st;
+    int threads = 0;
+    if ((st = plan_rows(logits, dtype, ld, rows, vocab, &p.row, &threads)) != QUASAR_OK) return st;
     p.k = k;
     p.indices = indices;
     p.values = values;
@@ -274,8 +269,8 @@ quasar_status run_distill(const void* logits, quasar_dtype dtype, int64_t ld, in
     p.stats = stats;
     p.grad = grad;
     p.ld_grad = ld_grad;
-    return launch(distill_kernel(dtype == QUASAR_F32, backward), &p, dim3((unsigned)(rows * p.row.ctas)), 512,
-                  backward ? 1 : p.row.ctas, smem, stream);
+    return launch(distill_kernel(dtype == QUASAR_F32, threads, backward), &p, dim3((unsigned)(rows * p.row.ctas)),
+                  threads, backward ? 1 : p.row.ctas, distill_smem(p.row.vecs), stream);
 }
 
 }  // namespace
@@ -414,17 +409,15 @@ quasar_status quasar_top_logits(const void* logits, quasar_dtype dtype, int64_t 
         overlaps(lse, n_lse, values, n_top) || overlaps(lse, n_lse, indices, n_top))
         return QUASAR_ERR_INVALID_ARG;
     TopParams p{};
-    const size_t extra = (kRowChunks + 1) * 8 + 512 * 8 + (size_t)kRowCtas * k * 8 + kRowCtas * 8 + 32 * 4 +
-                         2 * 512 * 2 + 16;
-    size_t smem = 0;
-    if ((st = plan_rows(logits, dtype, ld, rows, vocab, extra, &p.row, &smem)) != QUASAR_OK) return st;
+    int threads = 0;
+    if ((st = plan_rows(logits, dtype, ld, rows, vocab, &p.row, &threads)) != QUASAR_OK) return st;
     p.k = k;
     p.temperature = temperature;
     p.values = values;
     p.indices = indices;
     p.lse = lse;
-    return launch(top_logits_kernel(dtype == QUASAR_F32), &p, dim3((unsigned)(rows * p.row.ctas)), 512,
-                  p.row.ctas, smem, stream);
+    return launch(top_logits_kernel(dtype == QUASAR_F32, threads), &p, dim3((unsigned)(rows * p.row.ctas)), threads,
+                  p.row.ctas, top_logits_smem(threads, p.row.ctas, k), stream);
 }
 
 quasar_status quasar_distill_top(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows, int64_t vocab,

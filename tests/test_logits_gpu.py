@@ -376,11 +376,24 @@ def test_the_same_bits_every_time():
         assert torch.equal(api.top_logits(z, 100)["lse"], t["lse"])
 
 
-def test_rows_too_long_are_refused():
-    z = torch.zeros(1, 1 << 20, device="cuda")
-    assert Q.quasar_top_logits(z, Q.F32, 1 << 20, 1, 1 << 20, 4, 1.0, z, z, None) == Q.QuasarStatus.ERR_INVALID_ARG
-    v, i = torch.empty(1, 4, device="cuda"), torch.empty(1, 4, dtype=torch.int32, device="cuda")
-    assert Q.quasar_top_logits(z, Q.F32, 1 << 20, 1, 1 << 20, 4, 1.0, v, i, None) == Q.QuasarStatus.ERR_UNSUPPORTED
+@pytest.mark.parametrize("dtype,vocab", [(F32, 1 << 20), (BF16, 1500007)])
+def test_long_rows(dtype, vocab):
+    z = (torch.randn(2, vocab, generator=gen(27), device="cuda") * 3.0).to(dtype)
+    check_top(z, 200)
+    indices, values, lse = teacher_of(z, 200, 1.0, 28)
+    check_distill(z, indices, values, lse, None, 1.0)
+
+
+def test_a_row_without_a_finite_logit():
+    z = torch.full((2, 5000), -INF, device="cuda")
+    z[1] = torch.randn(5000, generator=gen(29), device="cuda")
+    indices = torch.arange(20, dtype=torch.int32, device="cuda").expand(2, 20).contiguous()
+    values = torch.randn(2, 20, generator=gen(30), device="cuda")
+    made = api.distill_top(z, indices, values, stats=True)
+    assert float(made["loss"][0]) == INF and math.isfinite(float(made["loss"][1]))
+    assert not made["grad"][0].any() and torch.isfinite(made["grad"]).all()
+    back = api.distill_top_backward(z, indices, values, made["stats"], None)
+    assert not back[0].any() and torch.isfinite(back).all()
 
 
 def test_a_wait_that_runs_out_is_reported():
