@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
     const int groups = S.groups();
 
     // -inf in the places of a vector's listed elements
-    auto drop = [&](uint4& x, int v) {
+    auto drop = [=](uint4& x, int v) {
         const unsigned listed = v < S.v1 ? mask[v - S.v0] : 0;
         if (listed) {
             uint32_t w[4] = {x.x, x.y, x.z, x.w};

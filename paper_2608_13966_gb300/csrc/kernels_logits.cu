@@ -34,7 +34,7 @@ const void* top_logits_kernel(bool f32, int threads)
 size_t top_logits_smem(int threads, int ctas, int k)
 {
     return (size_t)kTopVectors * 20 + (size_t)kTopKeys * 8 + (ctas > 1 ? (size_t)ctas * k * 8 : 0) + 8 + kRowCtas * 8 +
-           64 * 4 + 6 * 4 + (size_t)threads * 2;
+           64 * 4 + 6 * 4 + ((size_t)threads + kTopVectors) * 2;
 }
 
 size_t distill_smem(int vecs)

@@ -110,6 +110,15 @@ struct Vec16<__nv_bfloat16> {
     static __device__ __forceinline__ __nv_bfloat16 from_f32(float x) { return __float2bfloat16_rn(x); }
 };
 
+// A load that is issued where it stands (the compiler would move it down to
+// its use, and the next vectors would no longer be on their way).
+__device__ __forceinline__ uint4 load_now(const uint4* p)
+{
+    uint4 x;
+    asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p));
+    return x;
+}
+
 constexpr float kLog2e = 1.44269504f;
 constexpr int kHand = 4;  // vectors a thread works on at a time
 
@@ -155,7 +164,7 @@ struct RowStream {
     // A vector of the row, what lies outside it as -inf.
     __device__ __forceinline__ uint4 load(int v) const
     {
-        if (whole(v)) return __ldg(reinterpret_cast<const uint4*>(slot0) + v);
+        if (whole(v)) return load_now(reinterpret_cast<const uint4*>(slot0) + v);
         uint32_t w[4] = {Vec16<T>::kNone, Vec16<T>::kNone, Vec16<T>::kNone, Vec16<T>::kNone};
         if (v >= v0 && v < v1) {
 #pragma unroll
@@ -262,8 +271,10 @@ __device__ __forceinline__ void block_sum(const RunningSum& r, float c, float* s
 
 // Where every logit lies so far down that the base stopped at kFloor: the sum
 // again, the subtraction first.  `drop` replaces what a vector must not count.
+// (Out of line, and its arguments by value: a reference would keep the caller's
+// variables in memory.)
 template <typename T, int THREADS, typename Drop>
-__device__ __noinline__ float low_sum(const RowStream<T, THREADS>& S, float m, float c, float* scratch, Drop drop)
+__device__ __noinline__ float low_sum(const RowStream<T, THREADS> S, float m, float c, float* scratch, Drop drop)
 {
     constexpr int kP = Vec16<T>::kN / 2;
     float s = 0.0f;

@@ -6,20 +6,20 @@
 // so that equal values rank by the lowest index and no two keys are equal.
 //
 // A row is read once.  The threads' maxima over the first vectors they hold (8
-// each; in fours where k <= 64) bound the k-th largest: the k-th largest of
-// those maxima, in 16 bits rounded down, has at least k elements at or above
-// it.  A vector of the rest
-// is looked into only if its maximum reaches the bound; with 131,072 bf16
-// logits, k = 64 and values in no particular order that is about 350 of 16,384
-// vectors.  Those are put aside, their elements at or above the bound are
-// gathered, a second bound among the gathered (a bit a step, by the whole CTA)
-// leaves little more than k, and they are ranked by counting.  A row
-// that puts aside more than the lists hold (rising order, ties, fewer than k
-// that are not -inf) is settled by bisection on the 64-bit keys, which is
-// exact for any data and reads the row once more for each bit.  Where a
-// cluster shares a row, its lists, sorted, are merged by rank 0: an entry's
-// rank is its place in its own list plus, by binary search, the entries above
-// it in the others.
+// each; in fours where an eighth of the threads is k or more) bound the k-th
+// largest: the k-th largest of those maxima, in 16 bits rounded down, has at
+// least k elements at or above it.  A vector of the rest is put aside only if
+// its maximum reaches the bound; with 131,072 bf16 logits, k = 64 and values
+// in no particular order that is about 350 of 16,384 vectors.  Over a long row
+// the bound is renewed, each time the part read has doubled, from the maxima
+// of what lies aside.  In the end the elements at or above the bound are
+// gathered, a second bound among them (a bit a step) leaves little more than
+// k, and those are ranked by counting.  A row that puts aside more than the
+// lists hold (rising order, ties, fewer than k that are not -inf) is settled
+// by bisection on the k-th value, which is exact for any data and reads the
+// row once more for each bit.  Where a cluster shares a row, its lists,
+// sorted, are merged by rank 0: an entry's rank is its place in its own list
+// plus, by binary search, the entries above it in the others.
 #pragma once
 
 #include "row_stream.cuh"
@@ -28,6 +28,7 @@ namespace quasar {
 
 constexpr int kTopVectors = 1024;  // vectors a share may put aside before bisection
 constexpr int kTopKeys = 2048;     // elements of them at or above the bound
+constexpr int kTopShort = 512;     // ... that one warp finds the second bound of
 
 // Both zeros are one value, and NaN ranks above everything.
 __device__ __forceinline__ uint32_t ordered_bits(float x)
@@ -47,34 +48,53 @@ __device__ __forceinline__ uint64_t top_key(float x, int64_t e)
 }
 
 // The largest 16-bit value that at least `want` of 32 EACH values reach (the
-// want-th largest), by one warp, a bit a step from the highest in which any
-// two differ.
+// want-th largest), by one warp, a bit a step from the highest in which the
+// largest differs from `low`: a value that many are known to reach, or 0 (then
+// from the smallest present).
 template <int EACH>
-__device__ __forceinline__ uint32_t kth_largest(const uint16_t* values, int want)
+__device__ __forceinline__ uint32_t kth_largest(const uint16_t* values, int want, uint32_t low)
 {
     const int lane = threadIdx.x & 31;
     uint32_t key[EACH];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) key[i] = values[32 * i + lane];
-    uint32_t high = key[0], low = key[0];
+    uint32_t high = key[0], least = key[0];
 #pragma unroll
     for (int i = 1; i < EACH; ++i) {
         high = max(high, key[i]);
-        low = min(low, key[i]);
+        least = min(least, key[i]);
     }
     high = __reduce_max_sync(0xffffffffu, high);
-    low = __reduce_min_sync(0xffffffffu, low);
+    low = max(low, __reduce_min_sync(0xffffffffu, least));
     int b = 31 - __clz(high ^ low);
     uint32_t bound = high >> (b + 1) << (b + 1);
 #pragma unroll 1
     for (; b >= 0; --b) {
         const uint32_t trial = bound | (1u << b);
-        int c = 0;
+        int c[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) c += key[i] >= trial;
-        if (__reduce_add_sync(0xffffffffu, c) >= want) bound = trial;
+        for (int i = 0; i < EACH; ++i) c[i & 3] += key[i] >= trial;
+        if (__reduce_add_sync(0xffffffffu, (c[0] + c[1]) + (c[2] + c[3])) >= want) bound = trial;
     }
     return bound;
+}
+
+// The same of n values, get(i) each, by the whole CTA: for the longer lists.
+template <int THREADS, typename Get>
+__device__ __noinline__ uint32_t block_kth_largest(int n, int want, uint32_t low, Get get)
+{
+    uint32_t bound = 0;
+    for (int b = 15; b >= 0; --b) {
+        const uint32_t trial = bound | (1u << b);
+        int c = want;
+        if (trial > low) {
+            c = 0;
+            for (int i = threadIdx.x; i < (n + THREADS - 1) / THREADS * THREADS; i += THREADS)
+                c += __syncthreads_count(i < n && get(i) >= trial);
+        }
+        if (c >= want) bound = trial;
+    }
+    return max(bound, low);
 }
 
 // A place in a list for each lane with `want`, one atomic a warp; the lanes
@@ -88,6 +108,101 @@ __device__ __forceinline__ int take_place(int* count, bool want)
     int first = 0;
     if (lane == leader) first = atomicAdd(count, __popc(who));
     return __shfl_sync(active, first, leader) + __popc(who & ((1u << lane) - 1));
+}
+
+// The keys of the share's `want` largest elements into few[], unordered, by
+// bisection on the value: exact for any data, a pass over the row a bit.
+// `list` and `scratch` are room to work in; returns how many there are.  (Kept
+// out of line: inlined, its registers were spilled in the loops that run.)
+template <typename T, int THREADS>
+__device__ __noinline__ int exact_top(const RowStream<T, THREADS> S, int want, uint64_t* few, uint64_t* list,
+                                      int* found, float* scratch)
+{
+    using V = Vec16<T>;
+    constexpr int kN = V::kN;
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+    const int groups = S.groups();
+    constexpr int kLow = sizeof(T) == 2 ? 16 : 0;  // a bf16 is its 16 high bits
+    auto count_from = [&](uint32_t trial) {
+        const float f = from_ordered(trial);
+        int c = 0;
+        for (int g = 0; g < groups; ++g)
+#pragma unroll
+            for (int u = 0; u < kHand; ++u) {
+                const int v = S.vec(g, u);
+                if (v >= S.v1) break;
+                const uint4 x = S.load(v);
+                if (V::value(V::larger(x)) < f) continue;
+#pragma unroll
+                for (int j = 0; j < kN; ++j)
+                    c += ordered_bits(V::get(x, j)) >= trial && S.holds((int64_t)v * kN + j);
+            }
+        c = __reduce_add_sync(0xffffffffu, c);
+        __syncthreads();
+        if (t == 0) *found = 0;
+        __syncthreads();
+        if (lane == 0) atomicAdd(found, c);
+        __syncthreads();
+        return *found;
+    };
+    uint32_t value = 0;
+    for (int b = 31; b >= kLow; --b)
+        if (count_from(value | (1u << b)) >= want) value |= 1u << b;
+    // (bf16: the bits below, as ordered_bits leaves them)
+    if (kLow && (!(value & 0x80000000u) || value == 0xFFFF0000u)) value |= 0xFFFFu;
+    // the keys above it, and of those that tie the lowest indices: the
+    // threads' vectors of one step lie in order, so the ties of a step
+    // are numbered by a scan over the CTA
+    __syncthreads();
+    if (t == 0) *found = 0;
+    __syncthreads();
+    int ties = 0;  // found so far
+    int32_t* warps = reinterpret_cast<int32_t*>(scratch);
+    for (int g = 0; g < groups; ++g)
+        for (int u = 0; u < kHand; ++u) {
+            const int v = S.vec(g, u);
+            const uint4 x = S.load(v);
+            unsigned equal = 0;
+            for (int j = 0; j < kN; ++j) {
+                const int64_t slot = (int64_t)v * kN + j;
+                if (v >= S.v1 || !S.holds(slot)) continue;
+                const float f = V::get(x, j);
+                const uint32_t o = ordered_bits(f);
+                if (o > value) {
+                    const int i = atomicAdd(found, 1);
+                    if (i < kTopKeys / 2) few[i] = top_key(f, slot - S.begin);
+                } else if (o == value) {
+                    equal |= 1u << j;
+                }
+            }
+            if (ties >= want) continue;
+            const int mine = __popc(equal);
+            int upto = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const int y = __shfl_up_sync(0xffffffffu, upto, o);
+                upto += lane >= o ? y : 0;
+            }
+            __syncthreads();
+            if (lane == 31) warps[warp] = upto;
+            __syncthreads();
+            int at = ties + upto - mine;
+            for (int w = 0; w < THREADS / 32; ++w) {
+                if (w < warp) at += warps[w];
+                ties += warps[w];
+            }
+            for (; equal; equal &= equal - 1, ++at) {
+                const int j = __ffs(equal) - 1;
+                if (at < want) list[at] = top_key(V::get(x, j), (int64_t)v * kN + j - S.begin);
+            }
+        }
+    __syncthreads();
+    // fewer than `want` are above; the first ties complete them
+    const int above = min(*found, want);
+    ties = min(ties, want - above);
+    for (int i = t; i < ties; i += THREADS) few[above + i] = list[i];
+    __syncthreads();
+    return above + ties;
 }
 
 template <typename T, int THREADS>
@@ -107,40 +222,42 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_top_logits(const __
     int* count = reinterpret_cast<int*>(scratch + 64);               // vectors, keys, survivors
     uint32_t* bounds = reinterpret_cast<uint32_t*>(count + 3);       // [2]
     uint16_t* maxima = reinterpret_cast<uint16_t*>(bounds + 3);      // [THREADS]
+    // [kTopVectors]: maxima of what lies aside, then the keys' values, in 16 bits
+    uint16_t* high16 = maxima + THREADS;
 
-    const int t = threadIdx.x, warp = t >> 5;
-    const int rank = p.row.ctas > 1 ? (int)(blockIdx.x % p.row.ctas) : 0;
-    const int64_t r = blockIdx.x / p.row.ctas;
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+    const bool alone = p.row.ctas == 1;
+    const int rank = alone ? 0 : (int)(blockIdx.x % p.row.ctas);
+    const int64_t r = alone ? blockIdx.x : blockIdx.x / p.row.ctas;
     const RowStream<T, THREADS> S(p.row, r, rank);
-    if (p.row.ctas > 1) cluster_arrive();
+    if (!alone) cluster_arrive();
     wait_for_previous_grid();
     uint4 raw[kHand], next[kHand];
     S.load_group(raw, 0);
     S.load_group(next, 1);
-    if (t < 3) count[t] = 0;
-    if (t == 3) bounds[1] = 0;
     if (t == 0 && p.row.force_timeout_ns) {
         mbar_init(never, 1);
         if (!mbar_wait_bounded(never, 0, p.row.force_timeout_ns)) record_timeout(p.row.status);
     }
 
     const float c2 = kLog2e / p.temperature;
-    const int groups = S.groups();
-    // elements of this share, and how many of its largest are wanted
-    const int64_t first = max((int64_t)S.v0 * kN, (int64_t)S.begin);
-    const int have = (int)max((int64_t)0, min((int64_t)S.v1 * kN, S.end) - first);
-    const int want = min(have, p.k);
-
     auto top_of = [](const uint4 (&x)[kHand]) {
         typename V::Max m = V::larger(x[0]);
 #pragma unroll
         for (int u = 1; u < kHand; ++u) m = V::larger(m, V::larger(x[u]));
         return m;
     };
+
+    const int groups = S.groups();
+    // elements of this share, and how many of its largest are wanted
+    const int64_t first = max((int64_t)S.v0 * kN, (int64_t)S.begin);
+    const int have = (int)max((int64_t)0, min((int64_t)S.v1 * kN, S.end) - first);
+    const int want = min(have, p.k);
+
     const typename V::Max top0 = top_of(raw), top1 = top_of(next);
     // (0 from a thread that holds nothing: it must not count)
     uint32_t best = t < S.v1 - S.v0 ? ordered_bits(V::value(V::larger(top0, top1))) >> 16 : 0;
-    const bool fours = THREADS > 128 && p.k <= 64;
+    const bool fours = p.k * 8 <= THREADS;
     if (fours) {
         best = max(best, __shfl_xor_sync(0xffffffffu, best, 1));
         best = max(best, __shfl_xor_sync(0xffffffffu, best, 2));
@@ -148,10 +265,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_top_logits(const __
     } else {
         maxima[t] = (uint16_t)best;
     }
+    if (t < 3) count[t] = 0;
     __syncthreads();
     // one warp settles the bound while the others begin the sum
     if (warp == 0) {
-        const uint32_t b = fours ? kth_largest<THREADS / 128>(maxima, want) : kth_largest<THREADS / 32>(maxima, want);
+        const uint32_t b = fours ? kth_largest<THREADS / 128>(maxima, want, 0) : kth_largest<THREADS / 32>(maxima, want, 0);
         if (t == 0) bounds[0] = b << 16;
     }
     RunningSum run;
@@ -160,8 +278,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_top_logits(const __
         run.template add<T>(next, top1, c2);
     }
     __syncthreads();
-    const uint32_t bound = bounds[0];
-    const float least = from_ordered(bound);
+    uint32_t bound = bounds[0];
+    float least = from_ordered(bound);
 
     // put a vector aside if its maximum reaches the bound (a NaN, or a bound
     // that is none, compares as if it did)
@@ -178,65 +296,85 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_top_logits(const __
     for (int u = 0; u < kHand; ++u) keep(raw[u], S.vec(0, u));
 #pragma unroll
     for (int u = 0; u < kHand; ++u) keep(next[u], S.vec(1, u));
-    if (groups > 2) S.load_group(raw, 2);
-    for (int g = 2; g < groups; ++g) {
-        if (g + 1 < groups) S.load_group(next, g + 1);
+    // each doubling of the part read puts some k vectors more aside
+    const bool renew = p.k * groups > 1200;
+    for (int g = 2, stop = renew ? 4 : groups;; stop = min(2 * stop, groups)) {
+        stop = min(stop, groups);
+        if (g < stop) S.load_group(raw, g);
+        for (; g < stop; ++g) {
+            if (g + 1 < stop) S.load_group(next, g + 1);
 #pragma unroll
-        for (int u = 0; u < kHand; ++u) keep(raw[u], S.vec(g, u));
-        if (p.lse) run.template add<T>(raw, top_of(raw), c2);
+            for (int u = 0; u < kHand; ++u) keep(raw[u], S.vec(g, u));
+            if (p.lse) run.template add<T>(raw, top_of(raw), c2);
 #pragma unroll
-        for (int u = 0; u < kHand; ++u) raw[u] = next[u];
+            for (int u = 0; u < kHand; ++u) raw[u] = next[u];
+        }
+        if (g >= groups) break;
+        __syncthreads();
+        const int n = count[0];
+        for (int i = t; i < min(n, kTopVectors); i += THREADS)
+            high16[i] = (uint16_t)(ordered_bits(V::value(V::larger(aside[i]))) >> 16);
+        __syncthreads();
+        if (n <= kTopVectors)
+            bound = block_kth_largest<THREADS>(n, want, bound >> 16, [=](int i) { return (uint32_t)high16[i]; }) << 16;
+        least = from_ordered(bound);
     }
     float m = neg_inf(), s = 0.0f;
     if (p.lse) {
         block_sum<THREADS>(run, c2, scratch, m, s);
         if (is_low(m, c2)) s = low_sum(S, m, c2, scratch, [](uint4&, int) {});
-        if (p.row.ctas == 1 && t == 0)
+        if (alone && t == 0)
             p.lse[r] = m == neg_inf() && s == 0.0f ? neg_inf() : m / p.temperature + logf(s);
     }
     __syncthreads();
 
     const int n_aside = count[0];
     int n = kTopKeys + 1;
+    for (int i = t; i < kTopShort; i += THREADS) high16[i] = 0;
+    __syncthreads();
     if (n_aside <= kTopVectors) {
-        // an element a thread
-        for (int i = t; i < (n_aside * kN + 31) / 32 * 32; i += THREADS) {
-            bool in = i < n_aside * kN;
-            const int at = in ? i / kN : 0;
-            const int64_t slot = (int64_t)aside_at[at] * kN + i % kN;
-            const float f = V::get(aside[at], i % kN);
-            in = in && ordered_bits(f) >= bound && S.holds(slot);
-            const int j = take_place(count + 1, in);
-            if (in && j < kTopKeys) list[j] = top_key(f, slot - S.begin);
+        // a vector a thread: its elements at or above the bound
+        for (int i = t; i < (n_aside + 31) / 32 * 32; i += THREADS) {
+            const uint4 x = aside[i < n_aside ? i : 0];
+            const int64_t slot = (int64_t)aside_at[i < n_aside ? i : 0] * kN;
+            unsigned hits = 0;
+            if (i < n_aside) {
+#pragma unroll
+                for (int j = 0; j < kN; ++j)
+                    hits |= (unsigned)(ordered_bits(V::get(x, j)) >= bound && S.holds(slot + j)) << j;
+            }
+            const int mine = __popc(hits);
+            int upto = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const int y = __shfl_up_sync(0xffffffffu, upto, o);
+                upto += lane >= o ? y : 0;
+            }
+            int at = 0;
+            if (lane == 31) at = atomicAdd(count + 1, upto);
+            at = __shfl_sync(0xffffffffu, at, 31) + upto - mine;
+            for (; hits; hits &= hits - 1, ++at) {
+                const int j = __ffs(hits) - 1;
+                const uint64_t key = top_key(V::get(x, j), slot + j - S.begin);
+                if (at < kTopKeys) list[at] = key;
+                if (at < kTopShort) high16[at] = (uint16_t)(key >> 48);
+            }
         }
         __syncthreads();
         n = count[1];
     }
     if (n <= kTopKeys) {
-        // the want-th largest in 16 bits, a thread a key where they suffice
-        uint32_t key16[kTopKeys / THREADS];
-#pragma unroll
-        for (int q = 0; q < kTopKeys / THREADS; ++q) key16[q] = q * THREADS + t < n ? (uint32_t)(list[q * THREADS + t] >> 48) : 0;
-        uint32_t high = 0;
-#pragma unroll
-        for (int q = 0; q < kTopKeys / THREADS; ++q) high = max(high, key16[q]);
-        high = __reduce_max_sync(0xffffffffu, high);
-        if ((t & 31) == 0) atomicMax(bounds + 1, high);
-        __syncthreads();
-        // what is common to the bound and the largest is settled
-        int b = 31 - __clz(bounds[1] ^ (bound >> 16));
-        uint32_t second = bounds[1] >> (b + 1) << (b + 1);
-        for (; b >= 0; --b) {
-            const uint32_t trial = second | (1u << b);
-            int c;
-            if (n <= THREADS) {
-                c = __syncthreads_count(key16[0] >= trial);
-            } else {
-                c = 0;
-#pragma unroll
-                for (int q = 0; q < kTopKeys / THREADS; ++q) c += __syncthreads_count(key16[q] >= trial);
+        // the want-th largest in 16 bits
+        uint32_t second;
+        if (n <= kTopShort) {
+            if (warp == 0) {
+                const uint32_t b = kth_largest<kTopShort / 32>(high16, want, bound >> 16);
+                if (t == 0) bounds[1] = b;
             }
-            if (c >= want) second = trial;
+            __syncthreads();
+            second = bounds[1];
+        } else {
+            second = block_kth_largest<THREADS>(n, want, bound >> 16, [=](int i) { return (uint32_t)(list[i] >> 48); });
         }
         const uint64_t least_key = (uint64_t)second << 48;
         for (int i = t; i < (n + 31) / 32 * 32; i += THREADS) {
@@ -248,55 +386,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_top_logits(const __
         __syncthreads();
         n = count[2];
     } else {
-        // exact: the want-th largest key of the share, a bit a pass, and the
-        // keys from it up
-        auto each = [&](auto use) {
-            for (int g = 0; g < groups; ++g)
-                for (int u = 0; u < kHand; ++u) {
-                    const int v = S.vec(g, u);
-                    if (v >= S.v1) break;
-                    const uint4 x = S.load(v);
-                    for (int j = 0; j < kN; ++j) {
-                        const int64_t slot = (int64_t)v * kN + j;
-                        if (S.holds(slot)) use(top_key(V::get(x, j), slot - S.begin));
-                    }
-                }
-        };
-        uint64_t floor_key = 0;
-        // every index is below the vocabulary: the bits above its length are
-        // set in every complement
-        const int index_bits = 32 - __clz((int)p.row.vocab);
-        for (int b = 63; b >= 0; --b) {
-            const uint64_t trial = floor_key | (1ull << b);
-            if (b < 32 && b >= index_bits) {
-                floor_key = trial;
-                continue;
-            }
-            int c = 0;
-            each([&](uint64_t key) { c += key >= trial; });
-            c = __reduce_add_sync(0xffffffffu, c);
-            __syncthreads();
-            if (t == 0) count[2] = 0;
-            __syncthreads();
-            if ((t & 31) == 0) atomicAdd(count + 2, c);
-            __syncthreads();
-            if (count[2] >= want) floor_key = trial;
-        }
-        __syncthreads();
-        if (t == 0) count[2] = 0;
-        __syncthreads();
-        each([&](uint64_t key) {
-            if (key >= floor_key) {
-                const int i = atomicAdd(count + 2, 1);
-                if (i < kTopKeys) few[i] = key;
-            }
-        });
-        __syncthreads();
-        n = min(count[2], kTopKeys);
+        n = exact_top<T, THREADS>(S, want, few, list, count + 2, scratch);
     }
 
     // in order: a key's place is the number above it
-    const bool alone = p.row.ctas == 1;
     if (!alone) cluster_wait();  // every CTA of the row has started: its shared memory may be written
     const uint32_t to = alone ? 0 : peer_addr(smem_u32(merged + (size_t)rank * p.k), 0);
     for (int i = t; i < (4 * n + 31) / 32 * 32; i += THREADS) {

@@ -99,6 +99,26 @@ def test_top_logits_of_masked_rows(dtype):
     check_top(z, 64)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_top_logits_of_rows_that_keep_rising(dtype):
+    """Rows whose first part says little about the rest: more is put aside
+    than the lists hold."""
+    g = gen(31)
+    vocab = 100003
+    ramp = torch.linspace(-300.0, 300.0, vocab, device="cuda").expand(2, -1)
+    check_top((ramp + torch.randn(2, vocab, generator=g, device="cuda")).to(dtype), 100)
+    check_top((ramp.flip(1) + torch.randn(2, vocab, generator=g, device="cuda")).to(dtype), 100)
+    late = torch.randn(2, vocab, generator=g, device="cuda")
+    late[:, 70000:] += 50.0
+    check_top(late.to(dtype), 256)
+    few = torch.randn(3, vocab, generator=g, device="cuda")
+    few[:, 9000:] = few[:, 9000:].round()           # ties of a handful of values
+    check_top(few.to(dtype), 200)
+    down = -torch.randn(2, vocab, generator=g, device="cuda").abs() - 1.0   # negative values only
+    down[1, 30000:] = -1.0
+    check_top(down.to(dtype), 77)
+
+
 def test_top_logits_never_leaves_the_row():
     """NaN and inf give unspecified values, but places inside the row, and
     outputs that end where they should."""
