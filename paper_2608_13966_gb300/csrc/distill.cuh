@@ -20,8 +20,9 @@
 //
 // The row is passed over twice: the rest's sum of exponentials about a running
 // maximum, then the gradient; the second time it comes from L2.  The listed
-// logits, k scattered elements, are read first.  A byte a vector in shared
-// memory says which of its elements are listed.
+// logits, k scattered elements, are read on the way.  A byte a vector in
+// shared memory says which of its elements are listed; the four vectors a
+// thread has in hand have theirs in one word.
 #pragma once
 
 #include "row_stream.cuh"
@@ -29,12 +30,12 @@
 namespace quasar {
 
 // x / tau - y: the quotient is not rounded before the subtraction (inv_tau is
-// 1 / tau rounded, the second step its remainder)
-__device__ __forceinline__ float scaled_less(float x, float tau, float inv_tau, float y)
+// 1 / tau rounded, inv_low what that leaves out; x = -inf must not meet an
+// inv_low of the other sign)
+__device__ __forceinline__ float scaled_less(float x, float inv_tau, float inv_low, float y)
 {
-    const float low = fmaf(-tau, inv_tau, 1.0f) * inv_tau;
     const float d = fmaf(x, inv_tau, -y);
-    return low == 0.0f ? d : fmaf(x, low, d);
+    return fmaf(fmaxf(x, -1e30f), inv_low, d);
 }
 
 // p log(p / q) - p + q from p, log p and log q
@@ -79,13 +80,14 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
     using V = Vec16<T>;
     constexpr int kN = V::kN, kP = kN / 2;
     extern __shared__ __align__(128) uint8_t smem_raw[];
-    uint8_t* mask = smem_raw;  // of each vector, its listed elements
-    const int mask_words = (p.row.vecs + 15) / 16 * 4;
-    float* logp = reinterpret_cast<float*>(mask + (size_t)mask_words * 4);  // [kMaxTop]
+    // a word for each thread's group: of its vectors, the listed elements
+    uint32_t* mask = reinterpret_cast<uint32_t*>(smem_raw);
+    const int mask_words = (p.row.vecs + kHand * THREADS - 1) / (kHand * THREADS) * THREADS;
+    float* logp = reinterpret_cast<float*>(mask + mask_words);  // [kMaxTop]
     float* own = logp + kMaxTop;                              // the entries' student logits
     int32_t* entry = reinterpret_cast<int32_t*>(own + kMaxTop);  // -1: absent
     float* scratch = reinterpret_cast<float*>(entry + kMaxTop);  // [2][32]
-    float* teacher = scratch + 64;                            // P, p_r, listed (m, s)
+    float* teacher = scratch + 64;                            // sum p
     float(*parts)[2] = reinterpret_cast<float(*)[2]>(teacher + 4);  // [kRowCtas]
     uint64_t* never = reinterpret_cast<uint64_t*>(parts + kRowCtas);  // nothing signals it: see quasar_debug_force_timeout
     int* n_listed = reinterpret_cast<int*>(never + 1);
@@ -119,45 +121,41 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
 
     if (exchange) cluster_arrive();
     uint4 raw[kHand];
-    S.load_group(raw, 0);
-    for (int w = t; w < mask_words; w += THREADS) reinterpret_cast<uint32_t*>(mask)[w] = 0;
+    S.template load_group<!BACKWARD>(raw, 0);
+    for (int w = t; w < mask_words; w += THREADS) mask[w] = 0;
     if (t == 0) *n_listed = 0;
     for (int k = t; k < p.k; k += THREADS) {
         const int32_t e = p.indices[r * p.k + k];
         const bool here = e >= 0 && e < p.row.vocab;
         entry[k] = here ? e : -1;
         logp[k] = here ? p.values[r * p.k + k] : neg_inf();
-        // a backward call needs only its own share's (another CTA may already
-        // have put the gradient in the place of the others)
-        const int64_t s = (int64_t)S.begin + e;
-        own[k] = here && (!BACKWARD || (s >= (int64_t)S.v0 * kN && s < (int64_t)S.v1 * kN)) ? V::to_f32(S.slot0[s])
-                                                                                           : neg_inf();
     }
     __syncthreads();
     const float inv_tau = 1.0f / p.temperature;
+    const float inv_low = fmaf(-p.temperature, inv_tau, 1.0f) * inv_tau;
     const float c2 = kLog2e * inv_tau;
-    for (int k = t; k < p.k; k += THREADS)
-        if (entry[k] >= 0) {
-            atomicAdd(n_listed, 1);
-            const int64_t s = (int64_t)S.begin + entry[k];
-            const int v = (int)(s / kN) - S.v0;
-            if (v >= 0 && v < S.v1 - S.v0)
-                atomicOr(reinterpret_cast<uint32_t*>(mask) + v / 4, 1u << ((v % 4) * 8 + (int)(s % kN)));
-        }
+    // the student's logits of the entries are on their way during the first
+    // pass (a backward call needs only its own share's: another CTA may already
+    // have put the gradient in the place of the others)
+    constexpr int kMine = kMaxTop / THREADS > 0 ? kMaxTop / THREADS : 1;
+    T own_mine[kMine];
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) {
+        const int k = q * THREADS + t;
+        own_mine[q] = V::from_f32(neg_inf());
+        if (k >= p.k || entry[k] < 0) continue;
+        const int64_t s = (int64_t)S.begin + entry[k];
+        const int v = (int)(s / kN) - S.v0;
+        const bool held = v >= 0 && v < S.v1 - S.v0;
+        if (!BACKWARD || held) own_mine[q] = load_one(S.slot0 + s);
+        atomicAdd(n_listed, 1);
+        if (held)  // vector v of the share is vector v / THREADS % kHand of a group of thread v % THREADS
+            atomicOr(mask + v / (kHand * THREADS) * THREADS + v % THREADS,
+                     1u << (v / THREADS % kHand * 8 + (int)(s % kN)));
+    }
     if (warp == THREADS / 32 - 1) {
         const float sum = teacher_side(p, r, inv_tau, logp);
-        // the listed entries' own sum of exponentials
-        float m_in = neg_inf();
-        for (int k = lane; k < p.k; k += 32) m_in = fmaxf(m_in, own[k]);
-        m_in = lanes_max(m_in, 0xffffffffu);
-        float s_in = 0.0f;
-        for (int k = lane; k < p.k; k += 32) s_in += m_in == neg_inf() ? 0.0f : exp2f((own[k] - m_in) * c2);
-        s_in = warp_sum(s_in);
-        if (lane == 0) {
-            teacher[0] = sum;
-            teacher[2] = m_in;
-            teacher[3] = s_in;
-        }
+        if (lane == 0) teacher[0] = sum;
     }
     if (t == 0 && p.row.force_timeout_ns) {
         mbar_init(never, 1);
@@ -170,15 +168,26 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
     const int groups = S.groups();
 
     // -inf in the places of a vector's listed elements
-    auto drop = [=](uint4& x, int v) {
-        const unsigned listed = v < S.v1 ? mask[v - S.v0] : 0;
-        if (listed) {
-            uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    auto drop_from = [](uint4& x, unsigned listed) {
+        uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-            for (int j = 0; j < kN; ++j)
-                if (listed >> j & 1) V::put(w, j, V::from_f32(neg_inf()));
-            x = make_uint4(w[0], w[1], w[2], w[3]);
+        for (int j = 0; j < kN; ++j)
+            if (listed >> j & 1) V::put(w, j, V::from_f32(neg_inf()));
+        x = make_uint4(w[0], w[1], w[2], w[3]);
+    };
+    auto drop_group = [=](uint4 (&x)[kHand], int g) {
+        const uint32_t listed = mask[g * THREADS + t];
+        if (listed) {
+#pragma unroll
+            for (int u = 0; u < kHand; ++u) drop_from(x[u], listed >> 8 * u);
         }
+    };
+    auto drop = [=](uint4& x, int g, int u) { drop_from(x, mask[g * THREADS + t] >> 8 * u); };
+
+    auto put_own = [&] {
+#pragma unroll
+        for (int q = 0; q < kMine; ++q)
+            if (q * THREADS + t < p.k) own[q * THREADS + t] = V::to_f32(own_mine[q]);
     };
 
     float m_rest, coef, q_rest;  // of the whole row (backward: m_rest is the rest's lse)
@@ -187,20 +196,27 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
         RunningSum run;
         for (int g = 0; g < groups; ++g) {
             uint4 next[kHand];
-            if (g + 1 < groups) S.load_group(next, g + 1);
-            typename V::Max top = V::lowest();
+            if (g + 1 < groups) S.template load_group<!BACKWARD>(next, g + 1);
+            drop_group(raw, g);
+            typename V::Max top = V::larger(raw[0]);
 #pragma unroll
-            for (int u = 0; u < kHand; ++u) {
-                drop(raw[u], S.vec(g, u));
-                top = V::larger(top, V::larger(raw[u]));
-            }
+            for (int u = 1; u < kHand; ++u) top = V::larger(top, V::larger(raw[u]));
             run.template add<T>(raw, top, c2);
+            if (g + 1 < groups) {
 #pragma unroll
-            for (int u = 0; u < kHand; ++u) raw[u] = next[u];
+                for (int u = 0; u < kHand; ++u) raw[u] = next[u];
+            }
         }
-        if (p.grad) S.load_group(raw, 0);  // for the second pass
+        // (the last group stays in hand for the second pass)
         float s_rest;
+        put_own();
         block_sum<THREADS>(run, c2, scratch, m_rest, s_rest);
+        // the listed entries' own sum of exponentials, by every warp
+        float m_in = neg_inf(), s_in = 0.0f;
+        for (int k = lane; k < p.k; k += 32) m_in = fmaxf(m_in, own[k]);
+        m_in = lanes_max(m_in, 0xffffffffu);
+        for (int k = lane; k < p.k; k += 32) s_in += m_in == neg_inf() ? 0.0f : exp2f((own[k] - m_in) * c2);
+        s_in = warp_sum(s_in);
         if (is_low(m_rest, c2)) s_rest = low_sum(S, m_rest, c2, scratch, drop);
         if (exchange) {
             cluster_wait();  // every CTA of the row has started: its shared memory may be written
@@ -216,7 +232,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
         }
         m_all = m_rest;
         float s_all = s_rest;
-        merge_sum(m_all, s_all, teacher[2], teacher[3], c2);
+        merge_sum(m_all, s_all, m_in, s_in, c2);
         log_s = logf(s_all);
         const bool some = m_rest != neg_inf();
         const float log_q_rest = some ? (m_rest - m_all) * inv_tau + (logf(s_rest) - log_s) : neg_inf();
@@ -256,27 +272,40 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
     const float base = m_rest == neg_inf() ? 0.0f : exp_base(m_rest, c2);
     const bool low = !BACKWARD && base == kFloor;  // the subtraction first: see exp_base
     if (!BACKWARD && !low) coef *= m_rest == neg_inf() ? 1.0f : exp_fix(m_rest, c2, base);
-    const float2 cc = make_float2(c2, c2), bb = make_float2(-base, -base), kk = make_float2(coef, coef);
-    for (int g = 0; g < groups; ++g) {
+    const float2 cc = make_float2(c2, c2), bb = make_float2(low ? 0.0f : -base, low ? 0.0f : -base),
+                 kk = make_float2(coef, coef);
+    // from the end of the row: what was read last is the likeliest to be in L2
+    if (BACKWARD) {
+        put_own();
+        if (groups > 1) S.load_group(raw, groups - 1);
+    }
+    for (int g = groups - 1; g >= 0; --g) {
         uint4 next[kHand];
-        if (g + 1 < groups) S.load_group(next, g + 1);
+        if (g > 0) S.load_group(next, g - 1);
+        if (BACKWARD || low) drop_group(raw, g);
+        const bool whole = vectors && S.whole_group(g);
+        uint4* to = reinterpret_cast<uint4*>(grad) + S.vec(g, 0);
 #pragma unroll
         for (int u = 0; u < kHand; ++u) {
-            const int v = S.vec(g, u);
-            if (v >= S.v1) break;
-            if (BACKWARD || low) drop(raw[u], v);
             float2 x[kP];
             V::unpack(raw[u], x);
             if constexpr (BACKWARD) {
+                // scaled_less, two at a time
 #pragma unroll
-                for (int j = 0; j < kP; ++j)
-                    x[j] = make_float2(ex2(scaled_less(x[j].x, p.temperature, inv_tau, m_rest) * kLog2e),
-                                       ex2(scaled_less(x[j].y, p.temperature, inv_tau, m_rest) * kLog2e));
-            } else if (low) {
-#pragma unroll
-                for (int j = 0; j < kP; ++j)
-                    x[j] = make_float2(ex2((x[j].x - m_rest) * c2), ex2((x[j].y - m_rest) * c2));
+                for (int j = 0; j < kP; ++j) {
+                    const float2 z = x[j];
+                    x[j] = __ffma2_rn(z, make_float2(inv_tau, inv_tau), make_float2(-m_rest, -m_rest));
+                    if (inv_low != 0.0f)
+                        x[j] = __ffma2_rn(make_float2(fmaxf(z.x, -1e30f), fmaxf(z.y, -1e30f)),
+                                          make_float2(inv_low, inv_low), x[j]);
+                    x[j] = __fmul2_rn(x[j], make_float2(kLog2e, kLog2e));
+                    x[j] = make_float2(ex2(x[j].x), ex2(x[j].y));
+                }
             } else {
+                if (low) {
+#pragma unroll
+                    for (int j = 0; j < kP; ++j) x[j] = __fadd2_rn(x[j], make_float2(-m_rest, -m_rest));
+                }
 #pragma unroll
                 for (int j = 0; j < kP; ++j) {
                     x[j] = __ffma2_rn(x[j], cc, bb);
@@ -285,9 +314,15 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
             }
 #pragma unroll
             for (int j = 0; j < kP; ++j) x[j] = __fmul2_rn(kk, x[j]);
-            if (vectors && S.whole(v)) {
-                __stcs(reinterpret_cast<uint4*>(grad) + v, V::pack(x));
+            if (whole) {
+                __stcs(to + u * THREADS, V::pack(x));
             } else {
+                const int v = S.vec(g, u);
+                if (v >= S.v1) continue;
+                if (vectors && S.whole(v)) {
+                    __stcs(to + u * THREADS, V::pack(x));
+                    continue;
+                }
 #pragma unroll
                 for (int j = 0; j < kN; ++j) {
                     const int64_t s = (int64_t)v * kN + j;
@@ -304,7 +339,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
         if (entry[k] < 0) continue;
         const int64_t s = (int64_t)S.begin + entry[k];
         if (s / kN < S.v0 || s / kN >= S.v1) continue;
-        const float log_q = BACKWARD ? scaled_less(own[k], p.temperature, inv_tau, m_all)
+        const float log_q = BACKWARD ? scaled_less(own[k], inv_tau, inv_low, m_all)
                                      : (own[k] - m_all) * inv_tau - log_s;
         grad[s] = V::from_f32(none ? 0.0f : scale * (mass * expf(log_q) - expf(logp[k])));
     }

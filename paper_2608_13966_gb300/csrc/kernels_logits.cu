@@ -37,9 +37,10 @@ size_t top_logits_smem(int threads, int ctas, int k)
            64 * 4 + 6 * 4 + ((size_t)threads + kTopVectors) * 2;
 }
 
-size_t distill_smem(int vecs)
+size_t distill_smem(int vecs, int threads)
 {
-    return (size_t)(vecs + 15) / 16 * 16 + 3 * kMaxTop * 4 + 64 * 4 + 4 * 4 + kRowCtas * 8 + 8 + 8;
+    const size_t words = (size_t)(vecs + kHand * threads - 1) / (kHand * threads) * threads;
+    return words * 4 + 3 * kMaxTop * 4 + 64 * 4 + 4 * 4 + kRowCtas * 8 + 8 + 8;
 }
 
 }  // namespace quasar

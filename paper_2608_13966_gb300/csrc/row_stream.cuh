@@ -40,6 +40,7 @@ struct Vec16<float> {
     static constexpr int kN = 4;
     static constexpr uint32_t kNone = 0xFF800000u;  // -inf
     using Max = float;
+    static __device__ __forceinline__ uint32_t replace(uint32_t, int, float x) { return __float_as_uint(x); }
     static __device__ __forceinline__ void put(uint32_t (&w)[4], int j, float x) { w[j] = __float_as_uint(x); }
     static __device__ __forceinline__ float get(const uint4& x, int j)
     {
@@ -72,10 +73,14 @@ struct Vec16<__nv_bfloat16> {
     static constexpr int kN = 8;
     static constexpr uint32_t kNone = 0xFF80FF80u;  // two of -inf
     using Max = __nv_bfloat162;
-    static __device__ __forceinline__ void put(uint32_t (&w)[4], int j, __nv_bfloat16 x)
+    static __device__ __forceinline__ uint32_t replace(uint32_t word, int j, __nv_bfloat16 x)
     {
         const uint32_t bits = __bfloat16_as_ushort(x);
-        w[j / 2] = j & 1 ? (w[j / 2] & 0xFFFFu) | bits << 16 : (w[j / 2] & 0xFFFF0000u) | bits;
+        return j & 1 ? (word & 0xFFFFu) | bits << 16 : (word & 0xFFFF0000u) | bits;
+    }
+    static __device__ __forceinline__ void put(uint32_t (&w)[4], int j, __nv_bfloat16 x)
+    {
+        w[j / 2] = replace(w[j / 2], j, x);
     }
     static __device__ __forceinline__ float get(const uint4& x, int j)
     {
@@ -112,11 +117,39 @@ struct Vec16<__nv_bfloat16> {
 
 // A load that is issued where it stands (the compiler would move it down to
 // its use, and the next vectors would no longer be on their way).
+// KEEP: the line is wanted again, and stays in L2 before others; otherwise it
+// goes first.
+template <bool KEEP>
 __device__ __forceinline__ uint4 load_now(const uint4* p)
 {
     uint4 x;
-    asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p));
+    if constexpr (KEEP)
+        asm volatile(
+            "{\n\t.reg .b64 keep;\n\tcreatepolicy.fractional.L2::evict_last.b64 keep, 1.0;\n\t"
+            "ld.global.nc.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], keep;\n\t}"
+            : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
+            : "l"(p));
+    else
+        asm volatile(
+            "{\n\t.reg .b64 drop;\n\tcreatepolicy.fractional.L2::evict_first.b64 drop, 1.0;\n\t"
+            "ld.global.nc.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], drop;\n\t}"
+            : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
+            : "l"(p));
     return x;
+}
+
+__device__ __forceinline__ float load_one(const float* p)
+{
+    float x;
+    asm volatile("ld.global.f32 %0, [%1];" : "=f"(x) : "l"(p));
+    return x;
+}
+
+__device__ __forceinline__ __nv_bfloat16 load_one(const __nv_bfloat16* p)
+{
+    unsigned short x;
+    asm volatile("ld.global.u16 %0, [%1];" : "=h"(x) : "l"(p));
+    return __ushort_as_bfloat16(x);
 }
 
 constexpr float kLog2e = 1.44269504f;
@@ -131,6 +164,7 @@ struct RowStream {
     int64_t end;         // slot after the last element
     int v0, v1;          // this CTA's vectors
     int whole0, whole1;  // of those, the ones the row fills
+    bool ragged;         // not all
 
     __device__ __forceinline__ RowStream(const RowParams& p, int64_t r, int rank)
     {
@@ -144,6 +178,7 @@ struct RowStream {
         whole0 = v0 == 0 && begin > 0 ? 1 : v0;
         whole1 = v1 == vecs && end < (int64_t)vecs * kN ? v1 - 1 : v1;
         if (whole1 < whole0) whole1 = whole0;
+        ragged = whole0 > v0 || whole1 < v1;
     }
 
     __device__ __forceinline__ bool whole(int v) const
@@ -161,25 +196,68 @@ struct RowStream {
 
     __device__ __forceinline__ int groups() const { return (v1 - v0 + kHand * THREADS - 1) / (kHand * THREADS); }
 
-    // A vector of the row, what lies outside it as -inf.
-    __device__ __forceinline__ uint4 load(int v) const
+    // A vector that the row fills in part: what lies outside it as -inf.  (A
+    // loop, inlined: a call from the loops over groups would spill their
+    // registers, and unrolled it is most of their code.)
+    __device__ __forceinline__ uint4 load_part(int v) const
     {
-        if (whole(v)) return load_now(reinterpret_cast<const uint4*>(slot0) + v);
-        uint32_t w[4] = {Vec16<T>::kNone, Vec16<T>::kNone, Vec16<T>::kNone, Vec16<T>::kNone};
-        if (v >= v0 && v < v1) {
-#pragma unroll
-            for (int j = 0; j < kN; ++j) {
-                const int64_t s = (int64_t)v * kN + j;
-                if (holds(s)) Vec16<T>::put(w, j, slot0[s]);
-            }
+        uint4 x = none();
+#pragma unroll 1
+        for (int j = 0; j < kN; ++j) {
+            const int64_t s = (int64_t)v * kN + j;
+            if (!holds(s)) continue;
+            const int word = j * (int)sizeof(T) / 4;
+            uint32_t old = word == 0 ? x.x : word == 1 ? x.y : word == 2 ? x.z : x.w;
+            old = Vec16<T>::replace(old, j, slot0[s]);
+            if (word == 0) x.x = old;
+            if (word == 1) x.y = old;
+            if (word == 2) x.z = old;
+            if (word == 3) x.w = old;
         }
-        return make_uint4(w[0], w[1], w[2], w[3]);
+        return x;
     }
 
+    __device__ __forceinline__ static uint4 none()
+    {
+        return make_uint4(Vec16<T>::kNone, Vec16<T>::kNone, Vec16<T>::kNone, Vec16<T>::kNone);
+    }
+
+    __device__ __forceinline__ uint4 load(int v) const
+    {
+        if (whole(v)) return load_now<false>(reinterpret_cast<const uint4*>(slot0) + v);
+        return v >= v0 && v < v1 ? load_part(v) : none();
+    }
+
+    template <bool KEEP = false>
     __device__ __forceinline__ void load_group(uint4 (&raw)[kHand], int g) const
     {
+        const int v = vec(g, 0);
+        const uint4* p = reinterpret_cast<const uint4*>(slot0) + v;
+        const unsigned at = (unsigned)(v - whole0), n = (unsigned)(whole1 - whole0);
+        if (at < n && at + (kHand - 1) * THREADS < n) {
 #pragma unroll
-        for (int u = 0; u < kHand; ++u) raw[u] = load(vec(g, u));
+            for (int u = 0; u < kHand; ++u) raw[u] = load_now<KEEP>(p + u * THREADS);
+            return;
+        }
+#pragma unroll
+        for (int u = 0; u < kHand; ++u) {
+            raw[u] = none();
+            if (at + u * THREADS < n) raw[u] = load_now<KEEP>(p + u * THREADS);
+        }
+        if (ragged) {
+#pragma unroll
+            for (int u = 0; u < kHand; ++u) {
+                const int w = v + u * THREADS;
+                if (at + u * THREADS >= n && w >= v0 && w < v1) raw[u] = load_part(w);
+            }
+        }
+    }
+
+    // Where the vectors of this thread's group all lie within the row.
+    __device__ __forceinline__ bool whole_group(int g) const
+    {
+        const unsigned at = (unsigned)(vec(g, 0) - whole0), n = (unsigned)(whole1 - whole0);
+        return at < n && at + (kHand - 1) * THREADS < n;
     }
 };
 
@@ -270,7 +348,8 @@ __device__ __forceinline__ void block_sum(const RunningSum& r, float c, float* s
 }
 
 // Where every logit lies so far down that the base stopped at kFloor: the sum
-// again, the subtraction first.  `drop` replaces what a vector must not count.
+// again, the subtraction first.  `drop` replaces what a thread's vector (g, u) must
+// not count.
 // (Out of line, and its arguments by value: a reference would keep the caller's
 // variables in memory.)
 template <typename T, int THREADS, typename Drop>
@@ -281,7 +360,7 @@ __device__ __noinline__ float low_sum(const RowStream<T, THREADS> S, float m, fl
     for (int g = 0; g < S.groups(); ++g)
         for (int u = 0; u < kHand; ++u) {
             uint4 raw = S.load(S.vec(g, u));
-            drop(raw, S.vec(g, u));
+            drop(raw, g, u);
             float2 x[kP];
             Vec16<T>::unpack(raw, x);
 #pragma unroll

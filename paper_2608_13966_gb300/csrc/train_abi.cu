@@ -23,7 +23,7 @@ const void* column_sum_kernel();
 const void* activation_grad_kernel();
 const void* distill_kernel(bool f32, int threads, bool backward);
 const void* top_logits_kernel(bool f32, int threads);
-size_t distill_smem(int vecs);
+size_t distill_smem(int vecs, int threads);
 size_t top_logits_smem(int threads, int ctas, int k);
 }  // namespace quasar
 
@@ -270,7 +270,7 @@ quasar_status run_distill(const void* logits, quasar_dtype dtype, int64_t ld, in
     p.grad = grad;
     p.ld_grad = ld_grad;
     return launch(distill_kernel(dtype == QUASAR_F32, threads, backward), &p, dim3((unsigned)(rows * p.row.ctas)),
-                  threads, backward ? 1 : p.row.ctas, distill_smem(p.row.vecs), stream);
+                  threads, backward ? 1 : p.row.ctas, distill_smem(p.row.vecs, threads), stream);
 }
 
 }  // namespace

@@ -325,6 +325,17 @@ def test_distill_masked_logits(dtype, tail):
     assert torch.isfinite(made["grad"]).all()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("tau", [0.7, 1.3, 2.5, 3.0])
+def test_distill_masked_logits_at_any_temperature(dtype, tau):
+    z = (torch.randn(3, 2005, generator=gen(32), device="cuda") * 3.0).to(dtype)
+    indices, values, lse = teacher_of(z, 20, tau, 33)
+    rest = torch.ones(3, 2005, dtype=torch.bool, device="cuda").scatter_(1, indices.long(), False)
+    z[:, 900:][rest[:, 900:]] = -INF
+    made = check_distill(z, indices, values, lse, None, tau)
+    assert torch.isfinite(made["grad"]).all()
+
+
 def test_distill_with_everything_listed():
     z = torch.randn(4, 200, generator=gen(16), device="cuda") * 3.0
     indices, values, lse = teacher_of(z, 200, 1.0, 17)
