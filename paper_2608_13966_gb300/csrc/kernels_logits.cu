@@ -6,20 +6,21 @@ namespace quasar {
 
 namespace {
 
-template <typename T, int THREADS>
-const void* distill(bool backward)
+template <typename T>
+const void* distill(int threads, bool backward)
 {
-    return backward ? reinterpret_cast<const void*>(&k_distill_top<T, THREADS, true>)
-                    : reinterpret_cast<const void*>(&k_distill_top<T, THREADS, false>);
+    if (threads == kFewThreads)
+        return backward ? reinterpret_cast<const void*>(&k_distill_top<T, kFewThreads, true>)
+                        : reinterpret_cast<const void*>(&k_distill_top<T, kFewThreads, false>);
+    return backward ? reinterpret_cast<const void*>(&k_distill_top<T, kBackThreads, true>)
+                    : reinterpret_cast<const void*>(&k_distill_top<T, kRowThreads, false>);
 }
 
 }  // namespace
 
 const void* distill_kernel(bool f32, int threads, bool backward)
 {
-    if (f32) return threads == kFewThreads ? distill<float, kFewThreads>(backward) : distill<float, kRowThreads>(backward);
-    return threads == kFewThreads ? distill<__nv_bfloat16, kFewThreads>(backward)
-                                  : distill<__nv_bfloat16, kRowThreads>(backward);
+    return f32 ? distill<float>(threads, backward) : distill<__nv_bfloat16>(threads, backward);
 }
 
 const void* top_logits_kernel(bool f32, int threads)

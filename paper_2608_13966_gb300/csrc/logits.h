@@ -9,6 +9,7 @@ namespace quasar {
 constexpr int kMaxTop = 256;          // most entries of a row's top list
 constexpr int kRowCtas = 8;           // most CTAs (one cluster) a row is spread over
 constexpr int kRowThreads = 512;      // of a CTA
+constexpr int kBackThreads = 256;     // ... of a backward call, whose rows pass only once
 constexpr int kFewThreads = 128;      // ... whose share is no more than kFewVectors
 constexpr int kFewVectors = 1024;
 

@@ -259,6 +259,7 @@ quasar_status run_distill(const void* logits, quasar_dtype dtype, int64_t ld, in
     DistillParams p{};
     int threads = 0;
     if ((st = plan_rows(logits, dtype, ld, rows, vocab, &p.row, &threads)) != QUASAR_OK) return st;
+    if (backward && threads == kRowThreads) threads = kBackThreads;
     p.k = k;
     p.indices = indices;
     p.values = values;
