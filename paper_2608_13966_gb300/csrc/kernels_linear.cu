@@ -1,5 +1,6 @@
-// Instantiations of the paired matrix products, the column sums and the
-// activation gradient.
+// Instantiations of the paired matrix products, the product of one token,
+// the column sums and the activation gradient.
+#include "linear_one.cuh"
 #include "linear_grad.cuh"
 
 namespace quasar {
@@ -21,6 +22,7 @@ const void* product_pair_kernel(bool a_mn, bool b_mn, bool promote)
 
 size_t product_pair_smem() { return 1024 + kPairStages * kPairStageBytes + (2 * kPairStages + 6) * 8 + 16; }
 
+const void* linear_one_kernel() { return reinterpret_cast<const void*>(&k_linear_one); }
 const void* column_sum_kernel() { return reinterpret_cast<const void*>(&k_column_sum); }
 const void* activation_grad_kernel() { return reinterpret_cast<const void*>(&k_activation_grad); }
 

@@ -16,6 +16,8 @@
 // in memory (an MN-major tile); nothing is transposed on the way.
 #pragma once
 
+#include <type_traits>
+
 #include "cluster.cuh"
 #include "linear.h"
 #include "quasar.h"
@@ -186,6 +188,73 @@ __device__ __forceinline__ void finish(const Epilogue& e, float (&v)[N], int64_t
         finish_columns<N, true>(e, v, i, j0, N, bias);
     else
         finish_columns<N, false>(e, v, i, j0, (int)(cols - j0), bias);
+}
+
+// 4 consecutive rows i.. (consecutive in memory) of one column j: as finish,
+// with one access for the four where they are aligned.
+template <typename T>
+__device__ __forceinline__ void finish_four(const Epilogue& e, float (&v)[4], int64_t i, int64_t j)
+{
+    using bf16 = __nv_bfloat16;
+    auto vector = [](const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; };
+    auto load = [&](auto* p, float (&x)[4]) {
+        using E = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
+        if (vector(p, 4 * sizeof(E))) {
+            if constexpr (sizeof(E) == 2) {
+                const uint2 w = *reinterpret_cast<const uint2*>(p);
+                x[0] = bf16lo(w.x), x[1] = bf16hi(w.x), x[2] = bf16lo(w.y), x[3] = bf16hi(w.y);
+            } else {
+                const float4 w = *reinterpret_cast<const float4*>(p);
+                x[0] = w.x, x[1] = w.y, x[2] = w.z, x[3] = w.w;
+            }
+        } else {
+            for (int q = 0; q < 4; ++q) x[q] = (float)p[q];
+        }
+    };
+    auto store = [&](auto* p, const float (&x)[4]) {
+        using E = std::remove_pointer_t<decltype(p)>;
+        if (vector(p, 4 * sizeof(E))) {
+            if constexpr (sizeof(E) == 2)
+                *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+            else
+                *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+        } else {
+            for (int q = 0; q < 4; ++q) p[q] = (E)x[q];
+        }
+    };
+    float res[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (e.residual) load(static_cast<const T*>(e.residual) + j * e.ld_res + i, res);
+    if (e.scale_pre) {
+        float z[4];
+        load(static_cast<const bf16*>(e.scale_pre) + j * e.ld_scale + i, z);
+        times_slope(v, z, e.act);
+    } else {
+        if (e.bias) {
+            float b[4];
+            load(e.bias + i, b);
+            for (int q = 0; q < 4; ++q) v[q] += b[q];
+        }
+        if (e.pre) store(static_cast<bf16*>(e.pre) + j * e.ld_pre + i, v);
+        activate(v, e.act);
+    }
+    for (int q = 0; q < 4; ++q) v[q] += res[q];
+    store(static_cast<T*>(e.out) + j * e.ld_out + i, v);
+}
+
+__device__ __forceinline__ void finish_rows(const Epilogue& e, const float4& x, int64_t i, int64_t j, int64_t rows)
+{
+    float v[4] = {x.x, x.y, x.z, x.w};
+    if (i + 4 <= rows) {
+        if (e.out_f32)
+            finish_four<float>(e, v, i, j);
+        else
+            finish_four<__nv_bfloat16>(e, v, i, j);
+    } else {
+        for (int q = 0; q < 4; ++q) {
+            float one[1] = {v[q]};
+            finish(e, one, i + q, j, rows, j + 1, e.bias && i + q < rows ? e.bias[i + q] : 0.0f);
+        }
+    }
 }
 
 // -- waits -------------------------------------------------------------------
@@ -404,26 +473,27 @@ __global__ void __launch_bounds__(192, 2) k_product_tile(const __grid_constant__
         __syncthreads();
         cluster_sync();
         if (warp < 4) {
-            // 4 rows of one column a thread: 16 bytes from each CTA
-            const int per = BN / p.split;
+            // 4 rows of two columns a thread at a time: 16 bytes from each CTA
+            const int stop = (rank + 1) * (BN / p.split);
             const uint32_t base = smem_u32(smem) + (uint32_t)lane * 16;
-            for (int c = rank * per + warp; c < (rank + 1) * per; c += 4) {
-                if (col0 + c >= p.cols) break;
-                float4 v[8];
+            for (int c = rank * (BN / p.split) + warp; c < stop && col0 + c < p.cols; c += 8) {
+                const bool two = c + 4 < stop && col0 + c + 4 < p.cols;
+                float4 a[8], b[8];
 #pragma unroll
                 for (int r = 0; r < 8; ++r)
-                    if (r < p.split) v[r] = ld_peer4(peer_addr(base, (uint32_t)r) + (uint32_t)c * kTileRows * 4);
-                float s[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+                    if (r < p.split) {
+                        const uint32_t from = peer_addr(base, (uint32_t)r) + (uint32_t)c * kTileRows * 4;
+                        a[r] = ld_peer4(from);
+                        if (two) b[r] = ld_peer4(from + 4 * kTileRows * 4);
+                    }
 #pragma unroll
                 for (int r = 1; r < 8; ++r)
-                    if (r < p.split) s[0] += v[r].x, s[1] += v[r].y, s[2] += v[r].z, s[3] += v[r].w;
-                const int64_t i = row0 + 4 * lane;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float one[1] = {s[q]};
-                    finish(p.e, one, i + q, col0 + c, p.rows, p.cols,
-                           p.e.bias && i + q < p.rows ? p.e.bias[i + q] : 0.0f);
-                }
+                    if (r < p.split) {
+                        a[0].x += a[r].x, a[0].y += a[r].y, a[0].z += a[r].z, a[0].w += a[r].w;
+                        if (two) b[0].x += b[r].x, b[0].y += b[r].y, b[0].z += b[r].z, b[0].w += b[r].w;
+                    }
+                finish_rows(p.e, a[0], row0 + 4 * lane, col0 + c, p.rows);
+                if (two) finish_rows(p.e, b[0], row0 + 4 * lane, col0 + c + 4, p.rows);
             }
         }
         cluster_sync();

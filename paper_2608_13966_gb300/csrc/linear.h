@@ -38,6 +38,15 @@ struct ProductParams {
     unsigned int* status;
 };
 
+struct OneParams {
+    const void* x;
+    const void* r;
+    int64_t ld_r;
+    int64_t features;
+    int64_t inputs;
+    Epilogue e;
+};
+
 struct ColumnSumParams {
     const void* in;  // bf16 [rows, cols]
     int64_t ld;

@@ -19,6 +19,7 @@ namespace quasar {
 const void* product_tile_kernel(int bn, bool a_mn, bool b_mn, bool promote);
 const void* product_pair_kernel(bool a_mn, bool b_mn, bool promote);
 size_t product_pair_smem();
+const void* linear_one_kernel();
 const void* column_sum_kernel();
 const void* activation_grad_kernel();
 const void* distill_kernel(bool f32, int threads, bool backward);
@@ -151,8 +152,14 @@ quasar_status product(const Operand& a, const Operand& b, int64_t rows, int64_t 
     p.timeout_ns = host_timeout_ns();
     p.force_timeout_ns = host_forced_timeout_ns();
 
+    // Paired 256 x 256 tiles or one 128-row tile a cluster, by what they take
+    // (measured, 512 to 14336 a side): a pair works through a block of 64 of
+    // the reduction in 315 ns, 76 pairs side by side; the smaller tiles are
+    // bound by L2, 2.1 ns a tile and block in all, and start 3 us dearer.
     const int64_t pair_tiles = ((rows + 255) / 256) * ((cols + 255) / 256);
-    if (depth > 0 && pair_tiles * 2 >= n_sm) {
+    const int64_t small_tiles = ((rows + 127) / 128) * ((cols + 127) / 128);
+    const double pair_ns = (double)((pair_tiles + n_sm / 2 - 1) / (n_sm / 2)) * p.k_blocks * 315.0;
+    if (depth > 0 && cols > 64 && rows > 128 && pair_ns < 3000.0 + 2.1 * (double)small_tiles * p.k_blocks) {
         p.tiles_row = (int)((rows + 255) / 256);
         p.tiles_col = (int)((cols + 255) / 256);
         if ((st = tile_map(a, a.mn_major ? 64 : 128, &p.a)) != QUASAR_OK) return st;
@@ -307,6 +314,13 @@ quasar_status quasar_linear(const void* x, int64_t ld_x, const void* r, int64_t 
         return QUASAR_ERR_INVALID_ARG;
     const Epilogue e{bias, pre, ld_pre, nullptr, 0, residual, ld_residual, y, ld_y, activation,
                      y_dtype == QUASAR_F32};
+    // one token: 22 us through 14336 x 4096, 24 by the tensor cores' kernel; two
+    // already take 29 there against 24
+    if (tokens == 1 && inputs > 0) {
+        OneParams f{x, r, ld_r, features, inputs, e};
+        return launch(linear_one_kernel(), &f, dim3((unsigned)((features + 3) / 4)), 256, 1,
+                      8 * 4 * 4, stream);
+    }
     return product(Operand{r, ld_r, features, inputs, false}, Operand{x, ld_x, tokens, inputs, false}, features,
                    tokens, inputs, e, stream);
 }
