@@ -25,7 +25,7 @@ from .quasar import (ACTIVATIONS, BF16, F32, QuasarError, QuasarStatus, adamw_nv
 
 
 def _check(st):
-    if st != QuasarStatus.OK:
+    if st:  # QuasarStatus.OK is 0
         raise QuasarError(st)
 
 
@@ -320,13 +320,14 @@ def _on_stream(call):
 def _matrix(t, name, shape=None, dtypes=(torch.bfloat16,)):
     """Check a matrix; returns its row stride (a single row's: its length
     rounded up to what the products' operands need)."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+    sizes, strides = t.shape, t.stride()
+    if len(sizes) != 2 or (strides[1] != 1 and sizes[1] > 1):
         raise ValueError(f"{name} must be a 2-D tensor with contiguous rows")
     if t.dtype not in dtypes or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor of dtype {' or '.join(map(str, dtypes))}")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-    return _ld(t)
+    if shape is not None and sizes != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(sizes)}")
+    return strides[0] if sizes[0] > 1 else -(-sizes[1] // 8) * 8
 
 
 def _ld(t):

@@ -405,9 +405,13 @@ def _act_code(activation):
     return ACTIVATIONS[activation] if isinstance(activation, str) else int(activation)
 
 
+def _status(st):
+    return QuasarStatus(st) if st else QuasarStatus.OK
+
+
 def quasar_linear(x, ld_x, r, ld_r, bias, activation, residual, ld_residual, tokens, features,
                   inputs, y, y_dtype, ld_y, pre=None, ld_pre=0, stream=None) -> QuasarStatus:
-    return QuasarStatus(load().quasar_linear(
+    return _status((_lib or load()).quasar_linear(
         _ptr(x), ld_x, _ptr(r), ld_r, _ptr(bias), _act_code(activation), _ptr(residual),
         ld_residual, tokens, features, inputs, _ptr(y), y_dtype, ld_y, _ptr(pre), ld_pre,
         _stream(stream)))
@@ -416,7 +420,7 @@ def quasar_linear(x, ld_x, r, ld_r, bias, activation, residual, ld_residual, tok
 def quasar_linear_grad_input(dz, ld_dz, r, ld_r, pre_in, ld_pre_in, activation_in, residual,
                              ld_residual, tokens, features, inputs, dx, dx_dtype, ld_dx,
                              stream=None) -> QuasarStatus:
-    return QuasarStatus(load().quasar_linear_grad_input(
+    return _status((_lib or load()).quasar_linear_grad_input(
         _ptr(dz), ld_dz, _ptr(r), ld_r, _ptr(pre_in), ld_pre_in, _act_code(activation_in),
         _ptr(residual), ld_residual, tokens, features, inputs, _ptr(dx), dx_dtype, ld_dx,
         _stream(stream)))
@@ -424,21 +428,21 @@ def quasar_linear_grad_input(dz, ld_dz, r, ld_r, pre_in, ld_pre_in, activation_i
 
 def quasar_linear_grad_weight(dz, ld_dz, x, ld_x, tokens, features, inputs, dr, dr_dtype, ld_dr,
                               dbias=None, stream=None) -> QuasarStatus:
-    return QuasarStatus(load().quasar_linear_grad_weight(
+    return _status((_lib or load()).quasar_linear_grad_weight(
         _ptr(dz), ld_dz, _ptr(x), ld_x, tokens, features, inputs, _ptr(dr), dr_dtype, ld_dr,
         _ptr(dbias), _stream(stream)))
 
 
 def quasar_activation_grad(dy, ld_dy, pre, ld_pre, activation, rows, cols, dz, ld_dz,
                            stream=None) -> QuasarStatus:
-    return QuasarStatus(load().quasar_activation_grad(
+    return _status((_lib or load()).quasar_activation_grad(
         _ptr(dy), ld_dy, _ptr(pre), ld_pre, _act_code(activation), rows, cols, _ptr(dz), ld_dz,
         _stream(stream)))
 
 
 def quasar_top_logits(logits, dtype, ld, rows, vocab, k, temperature, values, indices, lse=None,
                       stream=None) -> QuasarStatus:
-    return QuasarStatus(load().quasar_top_logits(
+    return _status((_lib or load()).quasar_top_logits(
         _ptr(logits), dtype, ld, rows, vocab, k, temperature, _ptr(values), _ptr(indices),
         _ptr(lse), _stream(stream)))
 
@@ -446,7 +450,7 @@ def quasar_top_logits(logits, dtype, ld, rows, vocab, k, temperature, values, in
 def quasar_distill_top(logits, dtype, ld, rows, vocab, indices, values, k, teacher_lse, row_weight,
                        temperature, loss, stats=None, grad=None, ld_grad=0,
                        stream=None) -> QuasarStatus:
-    return QuasarStatus(load().quasar_distill_top(
+    return _status((_lib or load()).quasar_distill_top(
         _ptr(logits), dtype, ld, rows, vocab, _ptr(indices), _ptr(values), k, _ptr(teacher_lse),
         _ptr(row_weight), temperature, _ptr(loss), _ptr(stats), _ptr(grad), ld_grad,
         _stream(stream)))
@@ -455,7 +459,7 @@ def quasar_distill_top(logits, dtype, ld, rows, vocab, indices, values, k, teach
 def quasar_distill_top_backward(logits, dtype, ld, rows, vocab, indices, values, k, teacher_lse,
                                 stats, row_weight, temperature, grad, ld_grad,
                                 stream=None) -> QuasarStatus:
-    return QuasarStatus(load().quasar_distill_top_backward(
+    return _status((_lib or load()).quasar_distill_top_backward(
         _ptr(logits), dtype, ld, rows, vocab, _ptr(indices), _ptr(values), k, _ptr(teacher_lse),
         _ptr(stats), _ptr(row_weight), temperature, _ptr(grad), ld_grad, _stream(stream)))
 
