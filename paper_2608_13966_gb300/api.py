@@ -10,8 +10,6 @@ clears that word after synchronising the stream, and callers that must know
 their outputs are whole call it once after their last reconstruction."""
 from __future__ import annotations
 
-import functools
-
 import torch
 
 from .quasar import (ACTIVATIONS, BF16, F32, QuasarError, QuasarStatus, adamw_nvfp4_tensor_array,
@@ -297,46 +295,46 @@ def tensor_amax(w, stream=None):
 # Matrices are 2-D CUDA tensors whose rows are contiguous (any row stride).
 # Each call takes a ``stream`` (a torch stream or a handle; None: the current
 # one); its outputs and scratch are allocated on the stream it runs on.  The
-# checks are kept to a few attribute reads: a call with a handful of tokens
-# runs for less time on the GPU than a careless one takes on the host.
+# checks read each attribute once: a call with a handful of tokens runs for
+# less time on the GPU than a careless one takes on the host.
 
+_BF16S = (torch.bfloat16,)
 _FLOATS = (torch.bfloat16, torch.float32)
 _CODES = {torch.bfloat16: BF16, torch.float32: F32}
 
 
-def _on_stream(call):
-    """Run ``call`` with the stream it is given as the current one."""
-    @functools.wraps(call)
-    def run(*args, stream=None, **kwargs):
-        if stream is None:
-            return call(*args, **kwargs)
-        if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
-        with torch.cuda.stream(stream):
-            return call(*args, **kwargs)
-    return run
+def _on(stream, call, *args, **kwargs):
+    """``call`` with ``stream`` as the current one."""
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    with torch.cuda.stream(stream):
+        return call(*args, **kwargs)
 
 
-def _matrix(t, name, shape=None, dtypes=(torch.bfloat16,)):
-    """Check a matrix; returns its row stride (a single row's: its length
-    rounded up to what the products' operands need)."""
-    sizes, strides = t.shape, t.stride()
-    if len(sizes) != 2 or (strides[1] != 1 and sizes[1] > 1):
-        raise ValueError(f"{name} must be a 2-D tensor with contiguous rows")
+def _matrix(t, name, dtypes=_BF16S):
+    """(rows, columns, row stride) of a matrix; a single row's stride is its
+    length rounded up to what the products' operands need."""
+    try:
+        (rows, cols), (ld, step) = t.shape, t.stride()
+    except ValueError:
+        raise ValueError(f"{name} must be a 2-D tensor") from None
+    if step != 1 and cols > 1:
+        raise ValueError(f"{name} must have contiguous rows")
     if t.dtype not in dtypes or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor of dtype {' or '.join(map(str, dtypes))}")
-    if shape is not None and sizes != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(sizes)}")
-    return strides[0] if sizes[0] > 1 else -(-sizes[1] // 8) * 8
+    return rows, cols, ld if rows > 1 else -(-cols // 8) * 8
 
 
-def _ld(t):
-    rows, cols = t.shape
-    return t.stride(0) if rows > 1 else -(-cols // 8) * 8
+def _like(t, name, rows, cols, dtypes=_BF16S):
+    """The row stride of a matrix that must have this shape."""
+    r, c, ld = _matrix(t, name, dtypes)
+    if r != rows or c != cols:
+        raise ValueError(f"{name} must have shape ({rows}, {cols}), not ({r}, {c})")
+    return ld
 
 
 def _vector(t, name, n):
-    if t.dim() != 1 or t.shape[0] != n or t.dtype != torch.float32 or not t.is_cuda or not t.is_contiguous():
+    if t.shape != (n,) or t.dtype != torch.float32 or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous fp32 CUDA tensor of {n} values")
 
 
@@ -353,14 +351,15 @@ def _act_code(name):
 
 
 def _rows_of_8(rows, cols, device):
-    """An empty bf16 [rows, cols] whose rows start at 16-byte boundaries."""
-    wide = torch.empty((rows, -(-cols // 8) * 8), dtype=torch.bfloat16, device=device)
-    return wide if wide.shape[1] == cols else wide[:, :cols]
+    """An empty bf16 [rows, cols] whose rows start at 16-byte boundaries, and
+    its row stride."""
+    ld = -(-cols // 8) * 8
+    wide = torch.empty((rows, ld), dtype=torch.bfloat16, device=device)
+    return (wide if ld == cols else wide[:, :cols]), ld
 
 
-@_on_stream
 def linear(x, r, *, bias=None, activation="none", residual=None, out_dtype=torch.bfloat16,
-           save_pre=False):
+           save_pre=False, stream=None):
     """z = x r^T + bias, y = activation(z) + residual.
 
     x: bf16 [tokens, inputs]; r: bf16 [features, inputs] (a reconstruction);
@@ -368,46 +367,45 @@ def linear(x, r, *, bias=None, activation="none", residual=None, out_dtype=torch
     [features]; residual: [tokens, features] of out_dtype; activation: "none",
     "relu", "silu" or "gelu".  Returns a dict with y and, with save_pre, pre
     (z in bf16, in storage whose rows the products can read)."""
-    ld_x, ld_r = _matrix(x, "x"), _matrix(r, "r")
-    tokens, inputs = x.shape
-    features = r.shape[0]
-    if r.shape[1] != inputs:
-        raise ValueError(f"x has {inputs} inputs, r {r.shape[1]}")
+    if stream is not None:
+        return _on(stream, linear, x, r, bias=bias, activation=activation, residual=residual,
+                   out_dtype=out_dtype, save_pre=save_pre)
+    tokens, inputs, ld_x = _matrix(x, "x")
+    features, r_inputs, ld_r = _matrix(r, "r")
+    if r_inputs != inputs:
+        raise ValueError(f"x has {inputs} inputs, r {r_inputs}")
     code, act = _float_code(out_dtype, "out_dtype"), _act_code(activation)
     ld_res = ld_pre = 0
     if bias is not None:
         _vector(bias, "bias", features)
     if residual is not None:
-        ld_res = _matrix(residual, "residual", (tokens, features), (out_dtype,))
+        ld_res = _like(residual, "residual", tokens, features, (out_dtype,))
     y = torch.empty((tokens, features), dtype=out_dtype, device=x.device)
-    out = {"y": y}
     pre = None
     if save_pre:
-        out["pre"] = pre = _rows_of_8(tokens, features, x.device)
-        ld_pre = _ld(pre)
+        pre, ld_pre = _rows_of_8(tokens, features, x.device)
     _check(quasar_linear(x, ld_x, r, ld_r, bias, act, residual, ld_res, tokens, features, inputs, y,
                          code, features, pre, ld_pre))
-    return out
+    return {"y": y, "pre": pre} if save_pre else {"y": y}
 
 
-@_on_stream
-def activation_grad(dy, pre, activation):
+def activation_grad(dy, pre, activation, *, stream=None):
     """dz = dy * activation'(pre) in bf16, in storage whose rows the products
     can read ("none": a copy; pre is not used)."""
-    ld_dy = _matrix(dy, "dy")
+    if stream is not None:
+        return _on(stream, activation_grad, dy, pre, activation)
+    rows, cols, ld_dy = _matrix(dy, "dy")
     act = _act_code(activation)
     if activation == "none":
         pre = None
-    ld_pre = 0 if pre is None else _matrix(pre, "pre", dy.shape)
-    rows, cols = dy.shape
-    dz = _rows_of_8(rows, cols, dy.device)
-    _check(quasar_activation_grad(dy, ld_dy, pre, ld_pre, act, rows, cols, dz, _ld(dz)))
+    ld_pre = 0 if pre is None else _like(pre, "pre", rows, cols)
+    dz, ld_dz = _rows_of_8(rows, cols, dy.device)
+    _check(quasar_activation_grad(dy, ld_dy, pre, ld_pre, act, rows, cols, dz, ld_dz))
     return dz
 
 
-@_on_stream
 def linear_backward(dz, x, r, *, dx=True, dr=True, bias=False, pre_in=None, activation_in="none",
-                    residual=None, dx_dtype=torch.bfloat16, dr_dtype=torch.bfloat16):
+                    residual=None, dx_dtype=torch.bfloat16, dr_dtype=torch.bfloat16, stream=None):
     """Gradients of ``linear`` from dz (bf16 [tokens, features], the gradient
     at z; see ``activation_grad`` for a layer whose own output is activated).
 
@@ -416,18 +414,21 @@ def linear_backward(dz, x, r, *, dx=True, dr=True, bias=False, pre_in=None, acti
     the next reconstruction reads; dbias = the column sums of dz (with bias).
     Returns a dict of those asked for.  A dz whose rows the products cannot
     read is copied first."""
-    ld_dz, ld_x = _matrix(dz, "dz"), _matrix(x, "x")
-    tokens, features = dz.shape
-    inputs = x.shape[1]
-    if x.shape[0] != tokens:
-        raise ValueError(f"dz has {tokens} tokens, x {x.shape[0]}")
-    ld_r = _matrix(r, "r", (features, inputs))
+    if stream is not None:
+        return _on(stream, linear_backward, dz, x, r, dx=dx, dr=dr, bias=bias, pre_in=pre_in,
+                   activation_in=activation_in, residual=residual, dx_dtype=dx_dtype,
+                   dr_dtype=dr_dtype)
+    tokens, features, ld_dz = _matrix(dz, "dz")
+    x_tokens, inputs, ld_x = _matrix(x, "x")
+    if x_tokens != tokens:
+        raise ValueError(f"dz has {tokens} tokens, x {x_tokens}")
+    ld_r = _like(r, "r", features, inputs)
     act = _act_code(activation_in)
     if (pre_in is None) != (activation_in == "none"):
         raise ValueError("pre_in and activation_in go together")
-    ld_pre = 0 if pre_in is None else _matrix(pre_in, "pre_in", (tokens, inputs))
-    ld_res = 0 if residual is None else _matrix(residual, "residual", (tokens, inputs), (dx_dtype,))
     dx_code, dr_code = _float_code(dx_dtype, "dx_dtype"), _float_code(dr_dtype, "dr_dtype")
+    ld_pre = 0 if pre_in is None else _like(pre_in, "pre_in", tokens, inputs)
+    ld_res = 0 if residual is None else _like(residual, "residual", tokens, inputs, (dx_dtype,))
     if ld_dz % 8 or dz.data_ptr() % 16:
         dz = activation_grad(dz, None, "none")
         ld_dz = _ld(dz)
@@ -448,14 +449,19 @@ def linear_backward(dz, x, r, *, dx=True, dr=True, bias=False, pre_in=None, acti
     return out
 
 
-@_on_stream
-def top_logits(logits, k, *, temperature=1.0, lse=True):
+def _ld(t):
+    rows, cols = t.shape
+    return t.stride(0) if rows > 1 else -(-cols // 8) * 8
+
+
+def top_logits(logits, k, *, temperature=1.0, lse=True, stream=None):
     """Each row's k largest logits (bf16 or fp32 [rows, vocab], k up to 256),
     largest first, equal values by the lowest index.  Returns a dict with
     values (fp32 [rows, k]), indices (int32) and, with lse, the row's
     log sum exp(logits / temperature)."""
-    ld = _matrix(logits, "logits", None, _FLOATS)
-    rows, vocab = logits.shape
+    if stream is not None:
+        return _on(stream, top_logits, logits, k, temperature=temperature, lse=lse)
+    rows, vocab, ld = _matrix(logits, "logits", _FLOATS)
     device = logits.device
     values = torch.empty((rows, k), dtype=torch.float32, device=device)
     indices = torch.empty((rows, k), dtype=torch.int32, device=device)
@@ -468,25 +474,24 @@ def top_logits(logits, k, *, temperature=1.0, lse=True):
     return out
 
 
-def _teacher(logits, indices, values, teacher_lse, row_weight):
-    ld = _matrix(logits, "logits", None, _FLOATS)
-    rows = logits.shape[0]
-    if indices.dim() != 2 or indices.shape[0] != rows or indices.dtype != torch.int32 or \
+def _teacher(rows, indices, values, teacher_lse, row_weight):
+    """k, of a teacher's lists for this many rows."""
+    shape = indices.shape
+    if len(shape) != 2 or shape[0] != rows or indices.dtype != torch.int32 or \
             not indices.is_cuda or not indices.is_contiguous():
         raise ValueError("indices must be a contiguous int32 CUDA tensor [rows, k]")
-    if values.shape != indices.shape or values.dtype != torch.float32 or not values.is_cuda or \
+    if values.shape != shape or values.dtype != torch.float32 or not values.is_cuda or \
             not values.is_contiguous():
         raise ValueError("values must be a contiguous fp32 CUDA tensor of the shape of indices")
     if teacher_lse is not None:
         _vector(teacher_lse, "teacher_lse", rows)
     if row_weight is not None:
         _vector(row_weight, "row_weight", rows)
-    return ld, indices.shape[1]
+    return shape[1]
 
 
-@_on_stream
 def distill_top(logits, indices, values, *, teacher_lse=None, row_weight=None, temperature=1.0,
-                grad=True, stats=False, out=None):
+                grad=True, stats=False, out=None, stream=None):
     """Forward KL divergence of the student's logits (bf16 or fp32 [rows,
     vocab]) from a teacher's top entries (``top_logits``: indices, values and,
     for the mass outside them, its lse), and the gradient of
@@ -496,8 +501,11 @@ def distill_top(logits, indices, values, *, teacher_lse=None, row_weight=None, t
     (of the logits' dtype; written to ``out`` if given, which may be the
     logits) and stats (for ``distill_top_backward``).  Rows of weight 0 are
     skipped: loss and gradient 0."""
-    ld, k = _teacher(logits, indices, values, teacher_lse, row_weight)
-    rows, vocab = logits.shape
+    if stream is not None:
+        return _on(stream, distill_top, logits, indices, values, teacher_lse=teacher_lse,
+                   row_weight=row_weight, temperature=temperature, grad=grad, stats=stats, out=out)
+    rows, vocab, ld = _matrix(logits, "logits", _FLOATS)
+    k = _teacher(rows, indices, values, teacher_lse, row_weight)
     device = logits.device
     loss = torch.empty(rows, dtype=torch.float32, device=device)
     made = {"loss": loss}
@@ -506,7 +514,7 @@ def distill_top(logits, indices, values, *, teacher_lse=None, row_weight=None, t
         if out is None:
             out, ld_out = torch.empty((rows, vocab), dtype=logits.dtype, device=device), vocab
         else:
-            ld_out = _matrix(out, "out", logits.shape, (logits.dtype,))
+            ld_out = _like(out, "out", rows, vocab, (logits.dtype,))
         made["grad"] = out
     else:
         out = None
@@ -517,20 +525,22 @@ def distill_top(logits, indices, values, *, teacher_lse=None, row_weight=None, t
     return made
 
 
-@_on_stream
 def distill_top_backward(logits, indices, values, stats, row_weight, *, teacher_lse=None,
-                         temperature=1.0, out=None):
+                         temperature=1.0, out=None, stream=None):
     """The gradient of sum(row_weight * loss) from the statistics a
     ``distill_top(..., stats=True)`` call kept."""
-    ld, k = _teacher(logits, indices, values, teacher_lse, row_weight)
-    rows, vocab = logits.shape
-    _matrix(stats, "stats", (rows, 2), (torch.float32,))
+    if stream is not None:
+        return _on(stream, distill_top_backward, logits, indices, values, stats, row_weight,
+                   teacher_lse=teacher_lse, temperature=temperature, out=out)
+    rows, vocab, ld = _matrix(logits, "logits", _FLOATS)
+    k = _teacher(rows, indices, values, teacher_lse, row_weight)
+    _like(stats, "stats", rows, 2, (torch.float32,))
     if not stats.is_contiguous():
         raise ValueError("stats must be contiguous")
     if out is None:
         out, ld_out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device), vocab
     else:
-        ld_out = _matrix(out, "out", logits.shape, (logits.dtype,))
+        ld_out = _like(out, "out", rows, vocab, (logits.dtype,))
     _check(quasar_distill_top_backward(logits, _CODES[logits.dtype], ld, rows, vocab, indices,
                                        values, k, teacher_lse, stats, row_weight, temperature, out,
                                        ld_out))
