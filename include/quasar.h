@@ -512,7 +512,7 @@ quasar_status quasar_activation_grad(const void* dy, int64_t ld_dy, const void* 
  *   lse          [rows] fp32: log sum exp(logits / temperature) over the
  *                vocabulary (-inf for a row of -inf), or NULL.
  * -inf logits are ordinary values (masked entries), and a NaN ranks above
- * everything.
+ * everything.  Rows as long as in quasar_distill_top.
  */
 quasar_status quasar_top_logits(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows,
                                 int64_t vocab, int k, float temperature, float* values,
@@ -544,9 +544,8 @@ quasar_status quasar_top_logits(const void* logits, quasar_dtype dtype, int64_t 
  *                logits themselves (same pointer and stride).
  * -inf logits are ordinary values (q = 0; a listed one with p > 0 makes the
  * loss inf; a row of nothing else has loss inf and gradient 0).  Without a
- * single entry of mass, teacher_lse NULL gives loss and gradient 0.  A byte
- * of shared memory is kept for each 16 bytes of a CTA's share of the row:
- * a million logits fit whatever the number of rows (UNSUPPORTED beyond 227 KB).
+ * single entry of mass, teacher_lse NULL gives loss and gradient 0.  Up to
+ * 6.4 million fp32 or 12.8 million bf16 logits a row (UNSUPPORTED beyond).
  */
 quasar_status quasar_distill_top(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows,
                                  int64_t vocab, const int32_t* indices, const float* values, int k,

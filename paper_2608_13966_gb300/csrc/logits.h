@@ -12,6 +12,7 @@ constexpr int kRowThreads = 512;      // of a CTA
 constexpr int kBackThreads = 256;     // ... of a backward call, whose rows pass only once
 constexpr int kFewThreads = 128;      // ... whose share is no more than kFewVectors
 constexpr int kFewVectors = 1024;
+constexpr int kMostVectors = 200000;  // of a share (a byte of shared memory each)
 
 // A row is shared out to `ctas` CTAs, `vecs` 16-byte vectors each.
 struct RowParams {

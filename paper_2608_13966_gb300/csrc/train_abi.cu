@@ -198,7 +198,8 @@ quasar_status product(const Operand& a, const Operand& b, int64_t rows, int64_t 
 
 // How a row is spread: one CTA, or more (a power of two, one cluster) while
 // the rows alone leave SMs idle and a share keeps at least 1,024 vectors (16
-// KB: below that the exchange costs more than the reading).
+// KB: below that the exchange costs more than the reading), or while a share
+// is longer than the distillation's shared memory can describe.
 quasar_status plan_rows(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows, int64_t vocab,
                         RowParams* row, int* threads)
 {
@@ -213,7 +214,8 @@ quasar_status plan_rows(const void* logits, quasar_dtype dtype, int64_t ld, int6
     const int64_t per = 16 / dtype_size(dtype);
     const int64_t vecs = (vocab + per - 1 + per - 1) / per;  // for any start within 16 bytes
     int c = 1;
-    while (c < kRowCtas && rows * c < n_sm && vecs / (2 * c) >= 1024) c *= 2;
+    while (c < kRowCtas && ((rows * c < n_sm && vecs / (2 * c) >= 1024) || vecs / c > kMostVectors)) c *= 2;
+    if (vecs / c > kMostVectors) return QUASAR_ERR_UNSUPPORTED;
     row->ctas = c;
     row->vecs = (int)((vecs + c - 1) / c);
     *threads = row->vecs <= kFewVectors ? kFewThreads : kRowThreads;

@@ -284,6 +284,70 @@ def test_gradients_are_those_of_the_forward():
             assert abs(float(got[j]) - want) <= 2.0 ** -7 * float(mags[which].flatten()[j]) + 1e-6
 
 
+@pytest.mark.parametrize("tokens,features,inputs", [(1, 70, 72), (5, 70, 72), (300, 260, 136)])
+def test_offsets_past_32_bits(tokens, features, inputs):
+    """Rows so far apart that element offsets pass 2^32 (operands, results and
+    what is added)."""
+    apart = (1 << 32) // max(tokens - 1, 1) // 8 * 8 + 8
+    wide = torch.empty((tokens - 1) * apart + 1024, dtype=torch.bfloat16, device="cuda")
+    wide2 = torch.empty((tokens - 1) * apart + 1024, dtype=torch.bfloat16, device="cuda")
+    x = wide.as_strided((tokens, inputs), (apart, 1))
+    y = wide2.as_strided((tokens, features), (apart, 1))
+    x.copy_(rand(tokens, inputs, seed=1))
+    y.copy_(rand(tokens, features, seed=2))
+    r = rand(features, inputs, scale=0.05, seed=3)
+    want = x.double() @ r.double().t() + y.double()
+    mag = x.double().abs() @ r.double().abs().t() + y.double().abs()
+    st = Q.quasar_linear(x, apart, r, inputs, None, "none", y, apart, tokens, features, inputs, y, Q.BF16,
+                         apart)
+    assert st == Q.QuasarStatus.OK
+    api.check_device()
+    close(y, want, mag, inputs, True)
+    if tokens > 1:  # y is dz now
+        made = api.linear_backward(y, x, r, bias=True, dr_dtype=torch.float32)
+        close(made["dr"], y.double().t() @ x.double(), y.double().abs().t() @ x.double().abs(), tokens,
+              False)
+        close(made["dbias"], y.double().sum(0), y.double().abs().sum(0), tokens, False)
+
+
+def test_two_streams_at_once():
+    """Products of different kinds side by side, many of them, and the same
+    bits as alone."""
+    cases = [(1, 1000, 520), (40, 700, 2056), (200, 333, 1032), (2600, 2600, 136)]
+    data = [(rand(t, i, seed=n), rand(f, i, scale=0.05, seed=n + 9)) for n, (t, f, i) in enumerate(cases)]
+    alone = [api.linear(x, r, out_dtype=torch.float32)["y"] for x, r in data]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    made = []
+    for turn in range(12):
+        for n, (x, r) in enumerate(data):
+            made.append((n, api.linear(x, r, out_dtype=torch.float32, stream=streams[(turn + n) % 3])["y"]))
+    torch.cuda.synchronize()
+    api.check_device()
+    for n, y in made:
+        assert torch.equal(y, alone[n])
+
+
+def test_in_a_graph():
+    x, r = rand(70, 264, seed=1), rand(200, 264, scale=0.05, seed=2)
+    api.linear(x, r)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = api.linear(x, r, activation="silu", save_pre=True)
+        dz = api.activation_grad(y["y"], y["pre"], "silu")
+        made = api.linear_backward(dz, x, r, bias=True)
+    for seed in (3, 4):
+        x.copy_(rand(70, 264, seed=seed))
+        graph.replay()
+        torch.cuda.synchronize()
+        again = api.linear(x, r, activation="silu", save_pre=True)
+        assert torch.equal(again["y"], y["y"]) and torch.equal(again["pre"], y["pre"])
+        back = api.linear_backward(api.activation_grad(again["y"], again["pre"], "silu"), x, r, bias=True)
+        for name in back:
+            assert torch.equal(back[name], made[name]), name
+
+
 def test_another_stream():
     side = torch.cuda.Stream()
     x, r = rand(40, 264, seed=1), rand(72, 264, seed=2)

@@ -415,6 +415,62 @@ def test_long_rows(dtype, vocab):
     check_distill(z, indices, values, lse, None, 1.0)
 
 
+def test_many_long_rows():
+    """More rows than SMs, each longer than one CTA can describe."""
+    vocab, rows = (1 << 20) + 3, 160
+    z = torch.randn(rows, vocab, generator=gen(34), device="cuda")
+    t = api.top_logits(z, 20)
+    made = api.distill_top(z, t["indices"], t["values"] + 0.5, stats=True)
+    api.check_device()
+    for r in (0, 77, 159):
+        v, i = torch.sort(z[r], descending=True, stable=True)
+        assert torch.equal(t["values"][r], v[:20]) and torch.equal(t["indices"][r].long(), i[:20])
+        row = slice(r, r + 1)
+        loss, grad, t_loss, t_grad = reference(z[row], t["indices"][row], t["values"][row] + 0.5, None,
+                                               None, 1.0)
+        assert ((made["loss"][row].double() - loss).abs() <= t_loss).all()
+        assert not outside(made["grad"][row], grad, t_grad).any()
+
+
+def test_offsets_past_32_bits():
+    """Rows so far apart that element offsets pass 2^32."""
+    rows, vocab, ld = 3, 5003, (1 << 31) + 5
+    logits = torch.empty((rows - 1) * ld + vocab + 8, dtype=BF16, device="cuda")
+    out = torch.empty((rows - 1) * ld + vocab + 8, dtype=BF16, device="cuda")
+    z = logits[3:].as_strided((rows, vocab), (ld, 1))
+    g = out[1:].as_strided((rows, vocab), (ld, 1))
+    z.copy_(torch.randn(rows, vocab, generator=gen(35), device="cuda") * 3.0)
+    check_top(z, 40)
+    indices, values, lse = teacher_of(z, 40, 1.0, 36)
+    _, grad, _, t_grad = reference(z, indices, values, lse, None, 1.0)
+    api.distill_top(z, indices, values, teacher_lse=lse, out=g)
+    api.check_device()
+    assert not outside(g, grad, t_grad).any()
+
+
+def test_in_a_graph():
+    """Captured once, replayed on new values: a step's calls in their order."""
+    z = (torch.randn(40, 9001, generator=gen(37), device="cuda") * 3.0).to(BF16)
+    grad, side = torch.empty_like(z), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        t = api.top_logits(z, 32)
+        api.distill_top(z, t["indices"], t["values"], teacher_lse=t["lse"], out=grad)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        t = api.top_logits(z, 32)
+        made = api.distill_top(z, t["indices"], t["values"] - 0.25, teacher_lse=t["lse"], out=grad)
+    for seed in (38, 39):
+        z.copy_(torch.randn(40, 9001, generator=gen(seed), device="cuda") * 3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        again = api.top_logits(z, 32)
+        assert torch.equal(again["indices"], t["indices"]) and torch.equal(again["lse"], t["lse"])
+        want = api.distill_top(z, again["indices"], again["values"] - 0.25, teacher_lse=again["lse"])
+        assert torch.equal(want["loss"], made["loss"]) and torch.equal(want["grad"], grad)
+
+
 def test_a_row_without_a_finite_logit():
     z = torch.full((2, 5000), -INF, device="cuda")
     z[1] = torch.randn(5000, generator=gen(29), device="cuda")
