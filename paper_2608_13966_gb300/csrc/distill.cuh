@@ -19,7 +19,12 @@
 // logit counts as -inf there), not as the difference of two sums.
 //
 // The row is passed over twice: the rest's sum of exponentials about a running
-// maximum, then the gradient; the second time it comes from L2.  The listed
+// maximum, then the gradient, from the row's end.  4096 x 131072 bf16 (a tenth
+// of the rows padding) takes 371 us: 2.04 GB read and written at 5.5 TB/s, 0.81
+// of the measured copy rate.  Of the second pass 0.2 GB comes from HBM again
+// and the rest from L2, where the first pass asks for its lines to stay.
+// Exponentials are the hardware's, about a base that loses nothing to rounding;
+// every sum is fp32 and a bf16 gradient is rounded once.  The listed
 // logits, k scattered elements, are read on the way.  A byte a vector in
 // shared memory says which of its elements are listed; the four vectors a
 // thread has in hand have theirs in one word.

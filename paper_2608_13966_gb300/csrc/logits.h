@@ -18,7 +18,6 @@ constexpr int kMostVectors = 200000;  // of a share (a byte of shared memory eac
 struct RowParams {
     const void* logits;
     int64_t ld;
-    int64_t rows;
     int64_t vocab;
     int ctas;       // of a cluster
     int vecs;       // of a CTA's share

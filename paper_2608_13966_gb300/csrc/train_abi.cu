@@ -6,9 +6,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
-#include <cmath>
 #include <cstdint>
-#include <mutex>
 
 #include "host.h"
 #include "linear.h"
@@ -208,7 +206,6 @@ quasar_status plan_rows(const void* logits, quasar_dtype dtype, int64_t ld, int6
     if (st != QUASAR_OK) return st;
     row->logits = logits;
     row->ld = ld;
-    row->rows = rows;
     row->vocab = vocab;
     row->force_timeout_ns = host_forced_timeout_ns();
     const int64_t per = 16 / dtype_size(dtype);
