@@ -23,6 +23,24 @@ const void* product_pair_kernel(bool a_mn, bool b_mn, bool promote)
 size_t product_pair_smem() { return 1024 + kPairStages * kPairStageBytes + (2 * kPairStages + 6) * 8 + 16; }
 
 const void* linear_one_kernel() { return reinterpret_cast<const void*>(&k_linear_one); }
+// The kernel of up to 8 tokens' outer products; `padded`: the tokens it is
+// built for.
+const void* outer_kernel(int64_t tokens, bool f32, int* padded)
+{
+#define QUASAR_OUTER(n)                                                       \
+    if (tokens <= n) {                                                        \
+        *padded = n;                                                          \
+        return f32 ? reinterpret_cast<const void*>(&k_outer<n, true>)         \
+                   : reinterpret_cast<const void*>(&k_outer<n, false>);       \
+    }
+    QUASAR_OUTER(1)
+    QUASAR_OUTER(2)
+    QUASAR_OUTER(4)
+    QUASAR_OUTER(8)
+#undef QUASAR_OUTER
+    return nullptr;
+}
+
 const void* column_sum_kernel() { return reinterpret_cast<const void*>(&k_column_sum); }
 const void* activation_grad_kernel() { return reinterpret_cast<const void*>(&k_activation_grad); }
 

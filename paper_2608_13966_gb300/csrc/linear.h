@@ -47,6 +47,19 @@ struct OneParams {
     Epilogue e;
 };
 
+struct OuterParams {
+    const void* dz;  // bf16 [tokens, features]
+    int64_t ld_dz;
+    const void* x;   // bf16 [tokens, inputs]
+    int64_t ld_x;
+    int tokens;
+    int64_t features;
+    int64_t inputs;
+    void* dr;
+    int64_t ld_dr;
+    float* dbias;    // or NULL
+};
+
 struct ColumnSumParams {
     const void* in;  // bf16 [rows, cols]
     int64_t ld;

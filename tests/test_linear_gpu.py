@@ -187,6 +187,30 @@ def test_strides_and_guards(tokens, features, inputs):
             assert (whole[off + tokens * ld:] == 12345.0).all()
 
 
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens", [1, 2, 3, 4, 7, 8, 9])
+@pytest.mark.parametrize("features,inputs,ld", [(33, 13, 13), (70, 2061, 2064), (31, 4104, 4107), (100, 2048, 2048)])
+def test_weight_gradient_of_a_few_tokens(tokens, features, inputs, ld, out):
+    """Also with inputs that end inside a vector and rows of dr that start
+    anywhere; nothing outside dr is written."""
+    dz = strided(rand(tokens, features, seed=1), features // 8 * 8 + 8)
+    x = strided(rand(tokens, inputs, seed=2), inputs // 8 * 8 + 16)
+    flat = torch.full((features * ld + 40,), 12345.0, dtype=out, device="cuda")
+    off = 3 if ld % 8 else 0
+    dbias = torch.full((features + 8,), 12345.0, device="cuda")
+    st = Q.quasar_linear_grad_weight(dz, dz.stride(0), x, x.stride(0), tokens, features, inputs,
+                                     flat.data_ptr() + off * flat.element_size(),
+                                     Q.F32 if out == torch.float32 else Q.BF16, ld, dbias)
+    assert st == Q.QuasarStatus.OK
+    api.check_device()
+    dr = flat[off:off + features * ld].view(features, ld)
+    close(dr[:, :inputs], dz.double().t() @ x.double(), dz.double().abs().t() @ x.double().abs(),
+          tokens, out == torch.bfloat16)
+    close(dbias[:features], dz.double().sum(0), dz.double().abs().sum(0), tokens, False)
+    assert (dr[:, inputs:] == 12345.0).all() and (flat[:off] == 12345.0).all()
+    assert (flat[off + features * ld:] == 12345.0).all() and (dbias[features:] == 12345.0).all()
+
+
 def test_results_in_place_of_what_they_add():
     tokens, features, inputs = 70, 200, 136
     x, r = rand(tokens, inputs, seed=1), rand(features, inputs, scale=0.05, seed=2)
