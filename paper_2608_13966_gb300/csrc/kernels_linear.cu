@@ -20,7 +20,9 @@ const void* product_pair_kernel(bool a_mn, bool b_mn, bool promote)
     return nullptr;
 }
 
-size_t product_pair_smem() { return 1024 + kPairStages * kPairStageBytes + (2 * kPairStages + 6) * 8 + 16; }
+int product_pair_threads() { return kPairThreads; }
+
+size_t product_pair_smem() { return 1024 + kPairStages * kPairStageBytes + (2 * kPairStages + 8) * 8 + 16; }
 
 const void* linear_one_kernel() { return reinterpret_cast<const void*>(&k_linear_one); }
 // The kernel of up to 8 tokens' outer products; `padded`: the tokens it is

@@ -113,9 +113,30 @@ __device__ __forceinline__ void times_slope(float (&v)[N], const float (&z)[N], 
 
 // Element (row j, column i) of a row-major matrix, walked down a column: the
 // address is one addition a row.
-template <typename T, int N, bool FULL>
+//
+// WARP: every lane of the warp holds a column of the matrix (i = a multiple of
+// 32 + lane).  bf16 is then moved two columns of memory at a time where rows
+// are 4-byte aligned: of memory rows c and c + 1 the even lane takes its own
+// and its neighbour's element of row c, the odd lane those of row c + 1, and
+// one exchange between the two lanes puts them in place.  That halves the
+// accesses, which bound an epilogue whose product is short.
+template <typename T, int N, bool FULL, bool WARP>
 __device__ __forceinline__ void load_column(const void* base, int64_t ld, int64_t j0, int64_t i, int n, float (&v)[N])
 {
+    if constexpr (sizeof(T) == 2 && N % 2 == 0 && FULL && WARP) {
+        if ((reinterpret_cast<uintptr_t>(base) & 3) == 0 && ld % 2 == 0) {
+            const bool odd = i & 1;
+            const T* p = static_cast<const T*>(base) + (j0 + odd) * ld + (i - odd);
+#pragma unroll
+            for (int c = 0; c < N; c += 2, p += 2 * ld) {
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+                const float got = __shfl_xor_sync(0xffffffffu, odd ? bf16lo(w) : bf16hi(w), 1);
+                v[c] = odd ? got : bf16lo(w);
+                v[c + 1] = odd ? bf16hi(w) : got;
+            }
+            return;
+        }
+    }
     const T* p = static_cast<const T*>(base) + j0 * ld + i;
 #pragma unroll
     for (int c = 0; c < N; ++c, p += ld) {
@@ -129,9 +150,21 @@ __device__ __forceinline__ void load_column(const void* base, int64_t ld, int64_
     }
 }
 
-template <typename T, int N, bool FULL>
+template <typename T, int N, bool FULL, bool WARP>
 __device__ __forceinline__ void store_column(void* base, int64_t ld, int64_t j0, int64_t i, int n, const float (&v)[N])
 {
+    if constexpr (sizeof(T) == 2 && N % 2 == 0 && FULL && WARP) {
+        if ((reinterpret_cast<uintptr_t>(base) & 3) == 0 && ld % 2 == 0) {
+            const bool odd = i & 1;
+            T* p = static_cast<T*>(base) + (j0 + odd) * ld + (i - odd);
+#pragma unroll
+            for (int c = 0; c < N; c += 2, p += 2 * ld) {
+                const float got = __shfl_xor_sync(0xffffffffu, odd ? v[c] : v[c + 1], 1);
+                *reinterpret_cast<uint32_t*>(p) = pack_bf16x2(odd ? got : v[c], odd ? v[c + 1] : got);
+            }
+            return;
+        }
+    }
     T* p = static_cast<T*>(base) + j0 * ld + i;
 #pragma unroll
     for (int c = 0; c < N; ++c, p += ld)
@@ -143,27 +176,27 @@ __device__ __forceinline__ void store_column(void* base, int64_t ld, int64_t j0,
         }
 }
 
-template <int N, bool FULL>
+template <int N, bool FULL, bool WARP>
 __device__ __forceinline__ void finish_columns(const Epilogue& e, float (&v)[N], int64_t i, int64_t j0, int n, float bias)
 {
     using bf16 = __nv_bfloat16;
     float res[N];
     if (e.residual) {
         if (e.out_f32)
-            load_column<float, N, FULL>(e.residual, e.ld_res, j0, i, n, res);
+            load_column<float, N, FULL, WARP>(e.residual, e.ld_res, j0, i, n, res);
         else
-            load_column<bf16, N, FULL>(e.residual, e.ld_res, j0, i, n, res);
+            load_column<bf16, N, FULL, WARP>(e.residual, e.ld_res, j0, i, n, res);
     }
     if (e.scale_pre) {
         float z[N];
-        load_column<bf16, N, FULL>(e.scale_pre, e.ld_scale, j0, i, n, z);
+        load_column<bf16, N, FULL, WARP>(e.scale_pre, e.ld_scale, j0, i, n, z);
         times_slope(v, z, e.act);
     } else {
         if (e.bias) {
 #pragma unroll
             for (int c = 0; c < N; ++c) v[c] += bias;
         }
-        if (e.pre) store_column<bf16, N, FULL>(e.pre, e.ld_pre, j0, i, n, v);
+        if (e.pre) store_column<bf16, N, FULL, WARP>(e.pre, e.ld_pre, j0, i, n, v);
         activate(v, e.act);
     }
     if (e.residual) {
@@ -171,23 +204,24 @@ __device__ __forceinline__ void finish_columns(const Epilogue& e, float (&v)[N],
         for (int c = 0; c < N; ++c) v[c] += res[c];
     }
     if (e.out_f32)
-        store_column<float, N, FULL>(e.out, e.ld_out, j0, i, n, v);
+        store_column<float, N, FULL, WARP>(e.out, e.ld_out, j0, i, n, v);
     else
-        store_column<bf16, N, FULL>(e.out, e.ld_out, j0, i, n, v);
+        store_column<bf16, N, FULL, WARP>(e.out, e.ld_out, j0, i, n, v);
 }
 
 // N consecutive columns j0.. (rows of memory) of one row i: bias, activation
 // (or the input activation's slope), residual, one rounding to the output's
-// type.
+// type.  With N > 1 by a whole warp whose lanes hold consecutive rows.
 template <int N>
 __device__ __forceinline__ void finish(const Epilogue& e, float (&v)[N], int64_t i, int64_t j0,
                                        int64_t rows, int64_t cols, float bias)
 {
-    if (i >= rows || j0 >= cols) return;
-    if (cols - j0 >= N)
-        finish_columns<N, true>(e, v, i, j0, N, bias);
-    else
-        finish_columns<N, false>(e, v, i, j0, (int)(cols - j0), bias);
+    if (j0 >= cols) return;
+    if (N > 1 && cols - j0 >= N && (i | 31) < rows) {
+        finish_columns<N, true, true>(e, v, i, j0, N, bias);
+        return;
+    }
+    if (i < rows) finish_columns<N, false, false>(e, v, i, j0, (int)(cols - j0 < N ? cols - j0 : N), bias);
 }
 
 // 4 consecutive rows i.. (consecutive in memory) of one column j: as finish,
@@ -529,10 +563,12 @@ __global__ void __launch_bounds__(192, 2) k_product_tile(const __grid_constant__
 // bias, SiLU and kept pre-activation takes 611 us, 1.58 PFLOP/s, 0.84 of the
 // measured burst rate and 0.92 of the sustained.
 //
-// Warps: 0-7 epilogue (lane quadrant w % 4, column half w / 4), 8 copies, 9
+// Warps: 0-15 epilogue (lane quadrant w % 4, 64 columns w / 4), 16 copies, 17
 // matrix instructions.
 constexpr int kPairCols = 256;
-constexpr int kPairThreads = 320;
+constexpr int kPairEpilogue = 16;  // warps
+constexpr int kPairThreads = (kPairEpilogue + 2) * 32;
+constexpr int kPairSpan = 4 * kPairCols / kPairEpilogue;  // columns of an epilogue warp
 constexpr int kPairStages = 6;
 constexpr int kPairGroup = 8;  // column tiles walked together, for operand reuse in L2
 constexpr uint32_t kPairStageBytes = 2 * kTileABytes;
@@ -550,8 +586,9 @@ __global__ void __launch_bounds__(kPairThreads, 1) k_product_pair(const __grid_c
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + kPairStages * kPairStageBytes);  // first CTA's: both halves landed
     uint64_t* empty = full + kPairStages;   // each CTA's
     uint64_t* acc_full = empty + kPairStages;  // [2], each CTA's
-    uint64_t* acc_empty = acc_full + 2;        // [2], first CTA's: 16 epilogue warps
-    uint64_t* drained = acc_empty + 2;
+    uint64_t* acc_empty = acc_full + 2;        // [2], each CTA's: its epilogue warps
+    uint64_t* peer_empty = acc_empty + 2;      // [2], first CTA's: the second's acc_empty, passed on
+    uint64_t* drained = peer_empty + 2;
     uint64_t* never = drained + 1;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(never + 1);
     volatile uint32_t* gone = tmem_slot + 1;
@@ -571,15 +608,16 @@ __global__ void __launch_bounds__(kPairThreads, 1) k_product_pair(const __grid_c
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full + b, 1);
-            mbar_init(acc_empty + b, 16);
+            mbar_init(acc_empty + b, kPairEpilogue);
+            mbar_init(peer_empty + b, 1);
         }
         mbar_init(drained, 1);
         mbar_init(never, 1);
         *gone = 0;
         mbar_init_fence();
     }
-    if (warp == 9) tmem_alloc<2>(tmem_slot, 512);
-    if (warp == 8 && lane == 0) {
+    if (warp == kPairEpilogue + 1) tmem_alloc<2>(tmem_slot, 512);
+    if (warp == kPairEpilogue && lane == 0) {
         prefetch_map(&p.a);
         prefetch_map(&p.b);
     }
@@ -600,7 +638,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) k_product_pair(const __grid_c
         col0 = (group * kPairGroup + in % wide) * kPairCols;
     };
 
-    if (warp == 8 && lane == 0) {
+    if (warp == kPairEpilogue && lane == 0) {
         if (p.force_timeout_ns) role_wait(never, 0, gone, p.force_timeout_ns, p.status);
         uint32_t it = 0;
         for (int64_t t = pair; t < n_tiles && !*gone; t += n_pairs) {
@@ -639,14 +677,16 @@ __global__ void __launch_bounds__(kPairThreads, 1) k_product_pair(const __grid_c
                 role_wait(empty + j % kPairStages, (j / kPairStages) & 1, gone, p.timeout_ns, p.status);
             else if (rank == 0)
                 mbar_wait_bounded(full + j % kPairStages, (j / kPairStages) & 1, p.timeout_ns);
-    } else if (warp == 9 && lane == 0 && rank == 0) {
+    } else if (warp == kPairEpilogue + 1 && lane == 0 && rank == 0) {
         constexpr uint32_t desc = mma_desc(256, kPairCols, A_MN, B_MN);
         uint32_t it = 0, part = 0;
         bool ok = true;
         for (int64_t t = pair; t < n_tiles && ok; t += n_pairs) {
             for (int kb = 0; kb < nkb && ok; ++part) {
                 const uint32_t buf = part & 1;
-                if (part >= 2 && !role_wait(acc_empty + buf, (part / 2 - 1) & 1, gone, p.timeout_ns, p.status)) {
+                const uint32_t before = (part / 2 - 1) & 1;
+                if (part >= 2 && !(role_wait(acc_empty + buf, before, gone, p.timeout_ns, p.status) &&
+                                   role_wait(peer_empty + buf, before, gone, p.timeout_ns, p.status))) {
                     ok = false;
                     break;
                 }
@@ -676,17 +716,30 @@ __global__ void __launch_bounds__(kPairThreads, 1) k_product_pair(const __grid_c
         }
         mma_commit_local_pair(smem_u32(drained));
         mbar_wait_bounded(drained, 0, p.timeout_ns);
-    } else if (warp < 8) {
-        const int quad = warp & 3, half = warp >> 2;
-        const uint32_t mine = tmem + ((uint32_t)(32 * quad) << 16) + 128 * half;
+    } else if (warp == kPairEpilogue + 1 && lane == 0) {
+        // The second CTA's drained accumulators, passed on.  (An arrival at the
+        // other CTA waits for its thread's earlier stores to global memory: done
+        // by the epilogue's warps it cost 2 us a tile.)
+        uint32_t part = 0;
+        bool ok = true;
+        for (int64_t t = pair; t < n_tiles && ok; t += n_pairs)
+            for (int q = 0; q < n_parts && ok; ++q, ++part) {
+                ok = role_wait(acc_empty + (part & 1), (part / 2) & 1, gone, p.timeout_ns, p.status);
+                tc_fence_after();
+                tc_fence_before();
+                if (ok) arrive_peer(peer_addr(smem_u32(peer_empty + (part & 1)), 0));
+            }
+    } else if (warp < kPairEpilogue) {
+        const int quad = warp & 3, span = warp >> 2;
+        const uint32_t mine = tmem + ((uint32_t)(32 * quad) << 16) + kPairSpan * span;
         uint32_t part = 0;
         for (int64_t t = pair; t < n_tiles; t += n_pairs) {
             int64_t row0, col0;
             tile_at(t, row0, col0);
-            col0 += 128 * half;
+            col0 += kPairSpan * span;
             const int64_t i = row0 + 32 * quad + lane;
             const float bias = p.e.bias && i < p.rows ? p.e.bias[i] : 0.0f;
-            float acc[PROMOTE ? 128 : 1];
+            float acc[PROMOTE ? kPairSpan : 1];
 #pragma unroll
             for (float& x : acc) x = 0.0f;
             bool ok = true;
@@ -701,7 +754,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) k_product_pair(const __grid_c
                 from = mine + buf * kPairCols;
                 if constexpr (PROMOTE) {
 #pragma unroll
-                    for (int c = 0; c < 128; c += 16) {
+                    for (int c = 0; c < kPairSpan; c += 16) {
                         float v[16];
                         tmem_ld16(from + c, v);
 #pragma unroll
@@ -710,7 +763,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) k_product_pair(const __grid_c
                     if (q + 1 < n_parts) {
                         tc_fence_before();
                         __syncwarp();
-                        if (lane == 0) arrive_peer(peer_addr(smem_u32(acc_empty + buf), 0));
+                        if (lane == 0) mbar_arrive(acc_empty + buf);
                     }
                 }
             }
@@ -718,18 +771,18 @@ __global__ void __launch_bounds__(kPairThreads, 1) k_product_pair(const __grid_c
             if constexpr (PROMOTE) {
                 // the sums back where the last part lay, for the epilogue's loop
 #pragma unroll
-                for (int c = 0; c < 128; c += 16) tmem_st16(from + c, acc + c);
+                for (int c = 0; c < kPairSpan; c += 16) tmem_st16(from + c, acc + c);
                 tmem_wait_st();
             }
 #pragma unroll 1
-            for (int c = 0; c < 128; c += 32) {
-                float v[32];
+            for (int c = 0; c < kPairSpan; c += 16) {
+                float v[16];
                 __syncwarp();
-                tmem_ld32(from + c, v);
-                if (c == 96) {  // drained: the next part may be multiplied into it
+                tmem_ld16(from + c, v);
+                if (c == kPairSpan - 16) {  // drained: the next part may be multiplied into it
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) arrive_peer(peer_addr(smem_u32(acc_empty + ((part - 1) & 1)), 0));
+                    if (lane == 0) mbar_arrive(acc_empty + ((part - 1) & 1));
                 }
                 finish(p.e, v, i, col0 + c, p.rows, p.cols, bias);
             }
@@ -739,7 +792,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) k_product_pair(const __grid_c
     tc_fence_before();
     __syncthreads();
     cluster_sync();  // neither CTA leaves while the other may still signal it
-    if (warp == 9) tmem_free<2>(tmem, 512);
+    if (warp == kPairEpilogue + 1) tmem_free<2>(tmem, 512);
 }
 
 }  // namespace quasar

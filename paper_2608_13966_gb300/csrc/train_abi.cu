@@ -16,6 +16,7 @@
 namespace quasar {
 const void* product_tile_kernel(int bn, bool a_mn, bool b_mn, bool promote);
 const void* product_pair_kernel(bool a_mn, bool b_mn, bool promote);
+int product_pair_threads();
 size_t product_pair_smem();
 const void* linear_one_kernel();
 const void* outer_kernel(int64_t tokens, bool f32, int* padded);
@@ -166,9 +167,10 @@ quasar_status product(const Operand& a, const Operand& b, int64_t rows, int64_t 
         const void* fn = product_pair_kernel(a.mn_major, b.mn_major, e.out_f32 && p.k_blocks > 8);
         if (!fn) return QUASAR_ERR_UNSUPPORTED;
         int pairs = 0;
-        if ((st = host_max_clusters(fn, 2, 320, product_pair_smem(), &pairs)) != QUASAR_OK) return st;
+        if ((st = host_max_clusters(fn, 2, product_pair_threads(), product_pair_smem(), &pairs)) != QUASAR_OK) return st;
         pairs = (int)std::min<int64_t>(pair_tiles, pairs);
-        return launch(fn, &p, dim3((unsigned)pairs * 2), 320, 2, product_pair_smem(), stream);
+        return launch(fn, &p, dim3((unsigned)pairs * 2), product_pair_threads(), 2, product_pair_smem(),
+                      stream);
     }
     int bn = cols <= 16 ? 16 : (cols <= 32 ? 32 : (cols <= 64 ? 64 : 128));
     if (b.mn_major) bn = std::max(bn, 64);
