@@ -113,30 +113,9 @@ __device__ __forceinline__ void times_slope(float (&v)[N], const float (&z)[N], 
 
 // Element (row j, column i) of a row-major matrix, walked down a column: the
 // address is one addition a row.
-//
-// WARP: every lane of the warp holds a column of the matrix (i = a multiple of
-// 32 + lane).  bf16 is then moved two columns of memory at a time where rows
-// are 4-byte aligned: of memory rows c and c + 1 the even lane takes its own
-// and its neighbour's element of row c, the odd lane those of row c + 1, and
-// one exchange between the two lanes puts them in place.  That halves the
-// accesses, which bound an epilogue whose product is short.
-template <typename T, int N, bool FULL, bool WARP>
+template <typename T, int N, bool FULL>
 __device__ __forceinline__ void load_column(const void* base, int64_t ld, int64_t j0, int64_t i, int n, float (&v)[N])
 {
-    if constexpr (sizeof(T) == 2 && N % 2 == 0 && FULL && WARP) {
-        if ((reinterpret_cast<uintptr_t>(base) & 3) == 0 && ld % 2 == 0) {
-            const bool odd = i & 1;
-            const T* p = static_cast<const T*>(base) + (j0 + odd) * ld + (i - odd);
-#pragma unroll
-            for (int c = 0; c < N; c += 2, p += 2 * ld) {
-                const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
-                const float got = __shfl_xor_sync(0xffffffffu, odd ? bf16lo(w) : bf16hi(w), 1);
-                v[c] = odd ? got : bf16lo(w);
-                v[c + 1] = odd ? bf16hi(w) : got;
-            }
-            return;
-        }
-    }
     const T* p = static_cast<const T*>(base) + j0 * ld + i;
 #pragma unroll
     for (int c = 0; c < N; ++c, p += ld) {
@@ -150,21 +129,9 @@ __device__ __forceinline__ void load_column(const void* base, int64_t ld, int64_
     }
 }
 
-template <typename T, int N, bool FULL, bool WARP>
+template <typename T, int N, bool FULL>
 __device__ __forceinline__ void store_column(void* base, int64_t ld, int64_t j0, int64_t i, int n, const float (&v)[N])
 {
-    if constexpr (sizeof(T) == 2 && N % 2 == 0 && FULL && WARP) {
-        if ((reinterpret_cast<uintptr_t>(base) & 3) == 0 && ld % 2 == 0) {
-            const bool odd = i & 1;
-            T* p = static_cast<T*>(base) + (j0 + odd) * ld + (i - odd);
-#pragma unroll
-            for (int c = 0; c < N; c += 2, p += 2 * ld) {
-                const float got = __shfl_xor_sync(0xffffffffu, odd ? v[c] : v[c + 1], 1);
-                *reinterpret_cast<uint32_t*>(p) = pack_bf16x2(odd ? got : v[c], odd ? v[c + 1] : got);
-            }
-            return;
-        }
-    }
     T* p = static_cast<T*>(base) + j0 * ld + i;
 #pragma unroll
     for (int c = 0; c < N; ++c, p += ld)
@@ -176,27 +143,27 @@ __device__ __forceinline__ void store_column(void* base, int64_t ld, int64_t j0,
         }
 }
 
-template <int N, bool FULL, bool WARP>
+template <int N, bool FULL>
 __device__ __forceinline__ void finish_columns(const Epilogue& e, float (&v)[N], int64_t i, int64_t j0, int n, float bias)
 {
     using bf16 = __nv_bfloat16;
     float res[N];
     if (e.residual) {
         if (e.out_f32)
-            load_column<float, N, FULL, WARP>(e.residual, e.ld_res, j0, i, n, res);
+            load_column<float, N, FULL>(e.residual, e.ld_res, j0, i, n, res);
         else
-            load_column<bf16, N, FULL, WARP>(e.residual, e.ld_res, j0, i, n, res);
+            load_column<bf16, N, FULL>(e.residual, e.ld_res, j0, i, n, res);
     }
     if (e.scale_pre) {
         float z[N];
-        load_column<bf16, N, FULL, WARP>(e.scale_pre, e.ld_scale, j0, i, n, z);
+        load_column<bf16, N, FULL>(e.scale_pre, e.ld_scale, j0, i, n, z);
         times_slope(v, z, e.act);
     } else {
         if (e.bias) {
 #pragma unroll
             for (int c = 0; c < N; ++c) v[c] += bias;
         }
-        if (e.pre) store_column<bf16, N, FULL, WARP>(e.pre, e.ld_pre, j0, i, n, v);
+        if (e.pre) store_column<bf16, N, FULL>(e.pre, e.ld_pre, j0, i, n, v);
         activate(v, e.act);
     }
     if (e.residual) {
@@ -204,24 +171,23 @@ __device__ __forceinline__ void finish_columns(const Epilogue& e, float (&v)[N],
         for (int c = 0; c < N; ++c) v[c] += res[c];
     }
     if (e.out_f32)
-        store_column<float, N, FULL, WARP>(e.out, e.ld_out, j0, i, n, v);
+        store_column<float, N, FULL>(e.out, e.ld_out, j0, i, n, v);
     else
-        store_column<bf16, N, FULL, WARP>(e.out, e.ld_out, j0, i, n, v);
+        store_column<bf16, N, FULL>(e.out, e.ld_out, j0, i, n, v);
 }
 
 // N consecutive columns j0.. (rows of memory) of one row i: bias, activation
 // (or the input activation's slope), residual, one rounding to the output's
-// type.  With N > 1 by a whole warp whose lanes hold consecutive rows.
+// type.
 template <int N>
 __device__ __forceinline__ void finish(const Epilogue& e, float (&v)[N], int64_t i, int64_t j0,
                                        int64_t rows, int64_t cols, float bias)
 {
-    if (j0 >= cols) return;
-    if (N > 1 && cols - j0 >= N && (i | 31) < rows) {
-        finish_columns<N, true, true>(e, v, i, j0, N, bias);
-        return;
-    }
-    if (i < rows) finish_columns<N, false, false>(e, v, i, j0, (int)(cols - j0 < N ? cols - j0 : N), bias);
+    if (i >= rows || j0 >= cols) return;
+    if (cols - j0 >= N)
+        finish_columns<N, true>(e, v, i, j0, N, bias);
+    else
+        finish_columns<N, false>(e, v, i, j0, (int)(cols - j0), bias);
 }
 
 // 4 consecutive rows i.. (consecutive in memory) of one column j: as finish,
@@ -515,9 +481,9 @@ __global__ void __launch_bounds__(192, 2) k_product_tile(const __grid_constant__
         cluster_sync();
         if (warp < 4) {
             // 4 rows of two columns a thread at a time: 16 bytes from each CTA
-            const int stop = (rank + 1) * (BN / p.split);
+            const int stop = BN * (rank + 1) / p.split;
             const uint32_t base = smem_u32(smem) + (uint32_t)lane * 16;
-            for (int c = rank * (BN / p.split) + warp; c < stop && col0 + c < p.cols; c += 8) {
+            for (int c = BN * rank / p.split + warp; c < stop && col0 + c < p.cols; c += 8) {
                 const bool two = c + 4 < stop && col0 + c + 4 < p.cols;
                 float4 a[8], b[8];
 #pragma unroll
@@ -555,16 +521,20 @@ __global__ void __launch_bounds__(192, 2) k_product_tile(const __grid_constant__
 // into the other half while the epilogue drains this one.
 //
 // PROMOTE: fp32 results, parts of the reduction added up in registers as in
-// k_product_tile (8192 x 14336 x 4096 with parts of 512: 671 us against 537
-// us for bf16 results, of which the larger output takes 35; with parts of 256
-// the draining shows, 736 us).
+// k_product_tile (8192 x 14336 x 4096 with parts of 512: 660 us against 515
+// us for bf16 results, of which the larger output takes 35).
 //
 // Bound by the tensor cores and the power they draw: 8192 x 14336 x 4096 with
-// bias, SiLU and kept pre-activation takes 611 us, 1.58 PFLOP/s, 0.84 of the
-// measured burst rate and 0.92 of the sustained.
+// bias, SiLU and kept pre-activation takes 632 us, 1.52 PFLOP/s, 0.81 of the
+// measured burst rate and 0.89 of the sustained (535 to 557 us, 1.76 PFLOP/s,
+// where one input set is used over and over).  With a short reduction, by the
+// epilogue: the weight gradient of 32 tokens, 14336 x 4096, takes 36.5 us, 3.2
+// TB/s.
 //
-// Warps: 0-15 epilogue (lane quadrant w % 4, 64 columns w / 4), 16 copies, 17
-// matrix instructions.
+// Warps: 0-15 epilogue (lane quadrant w % 4, 64 columns w / 4; with 8 warps of
+// 128 columns 32 tokens' gradient took 42 us, 2560 x 2560 x 1024 with SiLU 22.5
+// against 20.9, the large products 0 to 3% less), 16 copies, 17 matrix
+// instructions and, in the second CTA, the drained accumulators' messages.
 constexpr int kPairCols = 256;
 constexpr int kPairEpilogue = 16;  // warps
 constexpr int kPairThreads = (kPairEpilogue + 2) * 32;
@@ -719,7 +689,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) k_product_pair(const __grid_c
     } else if (warp == kPairEpilogue + 1 && lane == 0) {
         // The second CTA's drained accumulators, passed on.  (An arrival at the
         // other CTA waits for its thread's earlier stores to global memory: done
-        // by the epilogue's warps it cost 2 us a tile.)
+        // by the epilogue's warps it cost the gradient of 32 tokens 10 us.)
         uint32_t part = 0;
         bool ok = true;
         for (int64_t t = pair; t < n_tiles && ok; t += n_pairs)

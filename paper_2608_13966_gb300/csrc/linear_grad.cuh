@@ -11,8 +11,8 @@ namespace quasar {
 // products, bound by writing dr.  A thread keeps 8 inputs of every token in
 // registers (in fp32 results two runs of 4, so that a warp's stores are 512
 // consecutive bytes either way) and walks kOuterFeatures features.  1 to 4
-// tokens through 14336 x 4096: 20 us in bf16, 5.9 TB/s, where the tensor cores'
-// kernels store 64 bytes a warp and step and take 43.
+// tokens through 14336 x 4096: 20 us in bf16, 5.9 TB/s, 8 tokens 24, where the
+// tensor cores' kernels store 64 bytes a warp and step and take 36.
 constexpr int kOuterThreads = 256;
 constexpr int kOuterFeatures = 32;
 

@@ -243,11 +243,13 @@ DeviceInfo g_dev[kMaxDevices];
 std::mutex g_mu;
 
 // Launch configuration of one kernel at one shared-memory size, per device
-// (occupancy: CTAs per SM, or clusters on the device for a clustered kernel).
+// (occupancy: CTAs per SM, or clusters of `cluster` CTAs on the device for a
+// clustered kernel).
 struct KernelConfig {
     const void* fn = nullptr;
     size_t smem = 0;
     int dev = -1;
+    int cluster = 0;
     int occupancy = 0;
 };
 constexpr int kMaxConfigs = 256;
@@ -323,7 +325,7 @@ quasar_status occupancy(const void* fn, size_t smem, int threads, int dev, int* 
 {
     std::lock_guard<std::mutex> lock(g_mu);
     for (int i = 0; i < g_ncfg; ++i)
-        if (g_cfg[i].fn == fn && g_cfg[i].dev == dev && g_cfg[i].smem == smem) {
+        if (g_cfg[i].fn == fn && g_cfg[i].dev == dev && g_cfg[i].smem == smem && g_cfg[i].cluster == 0) {
             *occ = g_cfg[i].occupancy;
             return QUASAR_OK;
         }
@@ -332,7 +334,7 @@ quasar_status occupancy(const void* fn, size_t smem, int threads, int dev, int* 
     int o = 0;
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&o, fn, threads, smem) != cudaSuccess)
         return QUASAR_ERR_CUDA;
-    if (g_ncfg < kMaxConfigs) g_cfg[g_ncfg++] = KernelConfig{fn, smem, dev, o};
+    if (g_ncfg < kMaxConfigs) g_cfg[g_ncfg++] = KernelConfig{fn, smem, dev, 0, o};
     *occ = o;
     return QUASAR_OK;
 }
@@ -709,7 +711,7 @@ quasar_status host_max_clusters(const void* fn, int size, int threads, size_t sm
     if (cudaGetDevice(&dev) != cudaSuccess) return QUASAR_ERR_CUDA;
     std::lock_guard<std::mutex> lock(g_mu);
     for (int i = 0; i < g_ncfg; ++i)
-        if (g_cfg[i].fn == fn && g_cfg[i].dev == dev && g_cfg[i].smem == smem) {
+        if (g_cfg[i].fn == fn && g_cfg[i].dev == dev && g_cfg[i].smem == smem && g_cfg[i].cluster == size) {
             *clusters = g_cfg[i].occupancy;
             return QUASAR_OK;
         }
@@ -729,7 +731,7 @@ quasar_status host_max_clusters(const void* fn, int size, int threads, size_t sm
     int n = 0;
     if (cudaOccupancyMaxActiveClusters(&n, fn, &cfg) != cudaSuccess) return QUASAR_ERR_CUDA;
     if (n < 1) return QUASAR_ERR_UNSUPPORTED;
-    if (g_ncfg < kMaxConfigs) g_cfg[g_ncfg++] = KernelConfig{fn, smem, dev, n};
+    if (g_ncfg < kMaxConfigs) g_cfg[g_ncfg++] = KernelConfig{fn, smem, dev, size, n};
     *clusters = n;
     return QUASAR_OK;
 }

@@ -136,6 +136,48 @@ bool valid_operand(const void* p, int64_t rows, int64_t cols, int64_t ld)
     return valid_shape(rows, cols, ld) && (rows == 0 || cols == 0 || (p && aligned(p, 16) && ld % 8 == 0));
 }
 
+// Stages of k_product_tile for bn columns: what two CTAs an SM leave each.
+int tile_stages(int bn, size_t* smem)
+{
+    const size_t stage = 128 * 128 + (size_t)bn * 128;
+    const int stages = (int)std::min<size_t>(8, (size_t)100 * 1024 / stage);
+    // exchange of partial tiles through the stages' memory
+    *smem = 1024 + stages * stage + (2 * stages + 6) * 8 + 16;
+    return stages;
+}
+
+// CTAs that share a tile's reduction: as many as leave each two blocks, while
+// all clusters run at once.  A CTA's copies bound it, so a split shortens the
+// call until the SMs are full (2 against 3 CTAs a tile: 128 x 11008 x 4096
+// 23.9 and 19.5 us, 5012 x 160 x 12544 55 and 41), but clusters left over
+// start when the rest is done (5012 x 128 x 12544: 40 clusters of 6 CTAs 29.6
+// us, of 7, more than fit, 45.8, of 4 33.2).
+//
+// How many clusters fit does not follow from the SM count, as one lies within
+// a part of the device.  The device's answer counts one CTA an SM; the kernel
+// runs two, so a cluster of s takes the place of half one, or of one of half
+// the size.  That holds for every variant: one kernel is asked for all.
+quasar_status tile_split(int64_t tiles, int k_blocks, int n_sm, int* split)
+{
+    *split = 1;
+    size_t smem = 0;
+    tile_stages(128, &smem);
+    const void* fn = product_tile_kernel(128, false, false, false);
+    for (int s = std::min(8, k_blocks / 2); s > 1; --s) {
+        if (tiles * s > 2 * (int64_t)n_sm) continue;
+        int whole = 0, half = n_sm;
+        quasar_status st = host_max_clusters(fn, s, 192, smem, &whole);
+        if (st == QUASAR_OK && s > 2) st = host_max_clusters(fn, (s + 1) / 2, 192, smem, &half);
+        if (st != QUASAR_OK) return st;
+        if (tiles > std::max(2 * whole, half)) continue;
+        // no more CTAs than the longest share needs
+        while ((k_blocks + s - 2) / (s - 1) == (k_blocks + s - 1) / s) --s;
+        *split = s;
+        break;
+    }
+    return QUASAR_OK;
+}
+
 // D (rows x cols, rows contiguous) = A B^T over `depth`, then the epilogue.
 quasar_status product(const Operand& a, const Operand& b, int64_t rows, int64_t cols, int64_t depth,
                       const Epilogue& e, quasar_stream_t stream)
@@ -178,14 +220,12 @@ quasar_status product(const Operand& a, const Operand& b, int64_t rows, int64_t 
     p.tiles_col = (int)((cols + bn - 1) / bn);
     const int64_t tiles = (int64_t)p.tiles_row * p.tiles_col;
     p.split = 1;
-    while (p.split < 8 && tiles * p.split * 2 <= 2 * n_sm && p.k_blocks >= p.split * 4) p.split *= 2;
-    const size_t stage = 128 * 128 + (size_t)bn * 128;
-    p.stages = (int)std::min<size_t>(8, (size_t)100 * 1024 / stage);
-    // exchange of partial tiles through the stages' memory
-    const size_t smem = 1024 + p.stages * stage + (2 * p.stages + 6) * 8 + 16;
+    if ((st = tile_split(tiles, p.k_blocks, n_sm, &p.split)) != QUASAR_OK) return st;
+    size_t smem = 0;
+    p.stages = tile_stages(bn, &smem);
     if (tiles * p.split > (int64_t(1) << 31) - 1) return QUASAR_ERR_UNSUPPORTED;
     // parts are only worth promoting where there are several
-    const bool promote = e.out_f32 && p.k_blocks / p.split > 8;
+    const bool promote = e.out_f32 && (p.k_blocks + p.split - 1) / p.split > 8;
     if (depth > 0) {
         if ((st = tile_map(a, a.mn_major ? 64 : 128, &p.a)) != QUASAR_OK) return st;
         if ((st = tile_map(b, b.mn_major ? 64 : bn, &p.b)) != QUASAR_OK) return st;
@@ -377,7 +417,7 @@ quasar_status quasar_linear_grad_weight(const void* dz, int64_t ld_dz, const voi
         overlaps(dbias, n_db, x, n_x) || overlaps(dbias, n_db, dr, n_dr))
         return QUASAR_ERR_INVALID_ARG;
     // a few tokens: writing dr is what it takes, 20 us against the tensor cores'
-    // 43 for 4 tokens and 14336 x 4096, 24 for 8; at 12 they are equal
+    // 36 for 4 tokens and 14336 x 4096, 24 for 8 (12 would take 43)
     const int64_t outer_blocks = (features + 31) / 32;
     if (tokens <= 8 && outer_blocks <= 65535) {
         OuterParams o{dz, ld_dz, x, ld_x, (int)tokens, features, dr ? inputs : 0, dr, ld_dr, dbias};

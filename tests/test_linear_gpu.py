@@ -145,6 +145,19 @@ def test_linear_backward_of_many_tiles(tokens, features, inputs, out):
     close(made["dbias"], dz.double().sum(0), dz.double().abs().sum(0), tokens, False)
 
 
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens,features,inputs", [
+    (4999, 200, 1976), (2299, 333, 1600), (2500, 130, 2376), (2300, 141, 2688), (2300, 130, 2632), (60, 3001, 1352)])
+def test_linear_of_tiles_several_ctas_share(tokens, features, inputs, out):
+    """2 to 8 CTAs a tile, by what the device holds at once."""
+    x, r = rand(tokens, inputs, seed=32), rand(features, inputs, scale=0.05, seed=33)
+    b = rand(features, seed=34, dtype=torch.float32)
+    made = api.linear(x, r, bias=b, out_dtype=out)
+    api.check_device()
+    close(made["y"], x.double() @ r.double().t() + b.double(),
+          x.double().abs() @ r.double().abs().t() + b.double().abs(), inputs, out == torch.bfloat16)
+
+
 def test_a_large_product_whose_wait_runs_out_is_reported():
     x, r = rand(2311, 72, seed=1), rand(2497, 72, seed=2)
     want = api.linear(x, r, out_dtype=torch.float32)["y"]
