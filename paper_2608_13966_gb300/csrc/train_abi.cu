@@ -416,6 +416,7 @@ quasar_status quasar_linear_grad_weight(const void* dz, int64_t ld_dz, const voi
     if (overlaps(dr, n_dr, dz, n_dz) || overlaps(dr, n_dr, x, n_x) || overlaps(dbias, n_db, dz, n_dz) ||
         overlaps(dbias, n_db, x, n_x) || overlaps(dbias, n_db, dr, n_dr))
         return QUASAR_ERR_INVALID_ARG;
+    if ((!dr || inputs == 0) && !dbias) return QUASAR_OK;
     // a few tokens: writing dr is what it takes, 20 us against the tensor cores'
     // 36 for 4 tokens and 14336 x 4096, 24 for 8 (12 would take 43)
     const int64_t outer_blocks = (features + 31) / 32;
