@@ -10,7 +10,7 @@ constexpr int kMaxTop = 256;          // most entries of a row's top list
 constexpr int kRowCtas = 8;           // most CTAs (one cluster) a row is spread over
 constexpr int kRowThreads = 512;      // of a CTA
 constexpr int kBackThreads = 256;     // ... of a backward call, whose rows pass only once
-constexpr int kFewThreads = 128;      // ... whose share is no more than kFewVectors
+constexpr int kFewThreads = 128;      // ... whose share is no more than kFewVectors (top lists: k no more than 128)
 constexpr int kFewVectors = 1024;
 constexpr int kMostVectors = 200000;  // of a share (a byte of shared memory each)
 

@@ -7,8 +7,8 @@
 //
 // A row is read once.  The threads' maxima over the first vectors they hold (8
 // each; in fours where an eighth of the threads is k or more) bound the k-th
-// largest: the k-th largest of those maxima, in 16 bits rounded down, has at
-// least k elements at or above it.  A vector of the rest is put aside only if
+// largest: the k-th largest of those maxima (a CTA has k threads or more), in
+// 16 bits rounded down, has at least k elements at or above it.  A vector of the rest is put aside only if
 // its maximum reaches the bound; with 131,072 bf16 logits, k = 64 and values
 // in no particular order that is about 350 of 16,384 vectors.  Over a long row
 // the bound is renewed, each time the part read has doubled, from the maxima
@@ -53,7 +53,7 @@ __device__ __forceinline__ uint64_t top_key(float x, int64_t e)
 // The largest 16-bit value that at least `want` of 32 EACH values reach (the
 // want-th largest), by one warp, a bit a step from the highest in which the
 // largest differs from `low`: a value that many are known to reach, or 0 (then
-// from the smallest present).
+// from the smallest present, which takes want <= 32 EACH).
 template <int EACH>
 __device__ __forceinline__ uint32_t kth_largest(const uint16_t* values, int want, uint32_t low)
 {
@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_top_logits(const __
         __syncthreads();
         n = count[1];
     }
-    if (n <= kTopKeys) {
+    if (n >= want && n <= kTopKeys) {
         // the want-th largest in 16 bits
         uint32_t second;
         if (n <= kTopShort) {

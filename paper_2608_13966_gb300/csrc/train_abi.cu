@@ -479,6 +479,8 @@ quasar_status quasar_top_logits(const void* logits, quasar_dtype dtype, int64_t 
     TopParams p{};
     int threads = 0;
     if ((st = plan_rows(logits, dtype, ld, rows, vocab, &p.row, &threads)) != QUASAR_OK) return st;
+    // the bound is the k-th largest of the threads' maxima: it takes k of them
+    if (k > kFewThreads) threads = kRowThreads;
     p.k = k;
     p.temperature = temperature;
     p.values = values;
