@@ -43,16 +43,17 @@ __device__ __forceinline__ float scaled_less(float x, float inv_tau, float inv_l
     return fmaf(fmaxf(x, -1e30f), inv_low, d);
 }
 
-// p log(p / q) - p + q from p, log p and log q
+// p log(p / q) - p + q from p, log p and log q (a NaN stays one)
 __device__ __forceinline__ float kl_term(float p, float log_p, float log_q)
 {
-    if (!(p > 0.0f)) return expf(log_q);
+    if (p == 0.0f) return expf(log_q);
     const float d = log_p - log_q;
     return d > -1.0f ? p * (d + expm1f(-d)) : p * (d - 1.0f) + expf(log_q);
 }
 
 // Teacher side of a row, by one warp: log p of each entry replaces its value
-// in logp[] (-inf where absent); returns sum p.
+// in logp[] (-inf where absent); returns sum p, NaN if the teacher is not a
+// number anywhere: that must reach loss and gradient, not pass for no mass.
 __device__ __forceinline__ float teacher_side(const DistillParams& p, int64_t r, float inv_tau, float* logp)
 {
     const int lane = threadIdx.x & 31;
@@ -66,7 +67,7 @@ __device__ __forceinline__ float teacher_side(const DistillParams& p, int64_t r,
         float s = 0.0f;
         for (int k = lane; k < p.k; k += 32) s += top == neg_inf() ? 0.0f : expf(logp[k] * inv_tau - top);
         s = warp_sum(s);
-        norm = s > 0.0f ? top + logf(s) : 0.0f;
+        norm = s == 0.0f ? 0.0f : top + logf(s);  // (NaN from a value that is NaN or infinite)
     }
     float sum = 0.0f;
     for (int k = lane; k < p.k; k += 32) {
@@ -168,7 +169,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
     }
     __syncthreads();
     const float sum_p = teacher[0];
-    const float p_rest = p.teacher_lse && *n_listed < p.row.vocab ? fmaxf(1.0f - sum_p, 0.0f) : 0.0f;
+    const float p_rest = p.teacher_lse && *n_listed < p.row.vocab ? max_nan(1.0f - sum_p, 0.0f) : 0.0f;
     const float mass = sum_p + p_rest;
     const int groups = S.groups();
 
@@ -242,7 +243,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
         const bool some = m_rest != neg_inf();
         const float log_q_rest = some ? (m_rest - m_all) * inv_tau + (logf(s_rest) - log_s) : neg_inf();
         q_rest = expf(log_q_rest);
-        coef = some ? (mass * q_rest - p_rest) / s_rest : 0.0f;
+        coef = some ? (mass * q_rest - p_rest) / s_rest : 0.0f * mass;
         if (rank == 0 && warp == 0) {
             float loss = 0.0f;
             for (int k = lane; k < p.k; k += 32)
@@ -250,8 +251,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
             loss = warp_sum(loss);
             if (lane == 0) {
                 loss += kl_term(p_rest, logf(p_rest), log_q_rest);
-                if (m_all == neg_inf()) loss = __int_as_float(0x7F800000);  // q is 0 everywhere
-                p.loss[r] = mass > 0.0f ? loss : 0.0f;
+                if (m_all == neg_inf()) loss = mass + __int_as_float(0x7F800000);  // q is 0 everywhere
+                p.loss[r] = mass == 0.0f ? 0.0f : loss;
                 if (p.stats) {
                     p.stats[2 * r] = m_all / p.temperature + log_s;
                     p.stats[2 * r + 1] = some ? m_rest / p.temperature + logf(s_rest) : neg_inf();
@@ -264,11 +265,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
         const float lse_rest = p.stats[2 * r + 1];
         const bool some = lse_rest != neg_inf();
         q_rest = some ? expf(lse_rest - m_all) : 0.0f;
-        coef = some ? mass * q_rest - p_rest : 0.0f;
+        coef = some ? mass * q_rest - p_rest : 0.0f * mass;
         m_rest = some ? lse_rest : 0.0f;
     }
     // a row without teacher mass, or without a finite logit, has no gradient
-    const bool none = !(mass > 0.0f) || m_all == neg_inf();
+    const bool none = mass == 0.0f || (m_all == neg_inf() && mass == mass);
     const float scale = none ? 0.0f : weight * inv_tau;
     coef *= scale;
 
