@@ -543,8 +543,9 @@ quasar_status quasar_top_logits(const void* logits, quasar_dtype dtype, int64_t 
  *   grad         [rows, vocab] of the logits' dtype, or NULL; it may be the
  *                logits themselves (same pointer and stride).
  * -inf logits are ordinary values (q = 0; a listed one with p > 0 makes the
- * loss inf; a row of nothing else has loss inf and gradient 0).  Without a
- * single entry of mass, teacher_lse NULL gives loss and gradient 0.  A NaN
+ * loss inf; a row of nothing else has loss inf and gradient 0).  A teacher
+ * without mass gives loss and gradient 0: not a single entry of mass with
+ * teacher_lse NULL, or a teacher_lse of -inf (a row of -inf).  A NaN
  * among a row's listed values or in its teacher_lse makes the row's loss and
  * gradient NaN, and so does a listed +inf (teacher_lse +inf or NULL).  Up to
  * 6.4 million fp32 or 12.8 million bf16 logits a row (UNSUPPORTED beyond).

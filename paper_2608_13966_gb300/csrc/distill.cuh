@@ -54,7 +54,9 @@ __device__ __forceinline__ float kl_term(float p, float log_p, float log_q)
 // Teacher side of a row, by one warp: log p of each entry replaces its value
 // in logp[] (-inf where absent); returns sum p, NaN if the teacher is not a
 // number anywhere: that must reach loss and gradient, not pass for no mass.
-__device__ __forceinline__ float teacher_side(const DistillParams& p, int64_t r, float inv_tau, float* logp)
+// A teacher_lse of -inf is that of a row without mass: not even the rest has
+// any (`rest` says so).
+__device__ __forceinline__ float teacher_side(const DistillParams& p, int64_t r, float inv_tau, float* logp, bool& rest)
 {
     const int lane = threadIdx.x & 31;
     float norm;
@@ -69,9 +71,11 @@ __device__ __forceinline__ float teacher_side(const DistillParams& p, int64_t r,
         s = warp_sum(s);
         norm = s == 0.0f ? 0.0f : top + logf(s);  // (NaN from a value that is NaN or infinite)
     }
+    rest = p.teacher_lse && norm != neg_inf();
     float sum = 0.0f;
     for (int k = lane; k < p.k; k += 32) {
-        logp[k] = logp[k] * inv_tau - norm;
+        const float z = logp[k] * inv_tau;
+        logp[k] = z == neg_inf() && norm == neg_inf() ? z : z - norm;
         sum += expf(logp[k]);
     }
     return warp_sum(sum);
@@ -93,7 +97,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
     float* own = logp + kMaxTop;                              // the entries' student logits
     int32_t* entry = reinterpret_cast<int32_t*>(own + kMaxTop);  // -1: absent
     float* scratch = reinterpret_cast<float*>(entry + kMaxTop);  // [2][32]
-    float* teacher = scratch + 64;                            // sum p
+    float* teacher = scratch + 64;                            // sum p, whether the rest may have mass
     float(*parts)[2] = reinterpret_cast<float(*)[2]>(teacher + 4);  // [kRowCtas]
     uint64_t* never = reinterpret_cast<uint64_t*>(parts + kRowCtas);  // nothing signals it: see quasar_debug_force_timeout
     int* n_listed = reinterpret_cast<int*>(never + 1);
@@ -160,8 +164,12 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
                      1u << (v / THREADS % kHand * 8 + (int)(s % kN)));
     }
     if (warp == THREADS / 32 - 1) {
-        const float sum = teacher_side(p, r, inv_tau, logp);
-        if (lane == 0) teacher[0] = sum;
+        bool rest;
+        const float sum = teacher_side(p, r, inv_tau, logp, rest);
+        if (lane == 0) {
+            teacher[0] = sum;
+            teacher[1] = rest ? 1.0f : 0.0f;
+        }
     }
     if (t == 0 && p.row.force_timeout_ns) {
         mbar_init(never, 1);
@@ -169,7 +177,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
     }
     __syncthreads();
     const float sum_p = teacher[0];
-    const float p_rest = p.teacher_lse && *n_listed < p.row.vocab ? max_nan(1.0f - sum_p, 0.0f) : 0.0f;
+    const float p_rest = teacher[1] != 0.0f && *n_listed < p.row.vocab ? max_nan(1.0f - sum_p, 0.0f) : 0.0f;
     const float mass = sum_p + p_rest;
     const int groups = S.groups();
 
@@ -271,7 +279,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
     // a row without teacher mass, or without a finite logit, has no gradient
     const bool none = mass == 0.0f || (m_all == neg_inf() && mass == mass);
     const float scale = none ? 0.0f : weight * inv_tau;
-    coef *= scale;
+    coef = none ? 0.0f : coef * scale;
 
     // the unlisted entries: coef 2^(x c - base), or coef e^(z - lse) from kept
     // statistics
