@@ -510,7 +510,8 @@ quasar_status quasar_activation_grad(const void* dy, int64_t ld_dy, const void* 
  *   values       [rows, k] fp32: the logits themselves (not scaled).
  *   indices      [rows, k] int32.  Equal values rank by the lowest index.
  *   lse          [rows] fp32: log sum exp(logits / temperature) over the
- *                vocabulary (-inf for a row of -inf), or NULL.
+ *                vocabulary (-inf for a row of -inf, NaN for one with a
+ *                NaN), or NULL.
  * -inf logits are ordinary values (masked entries), and a NaN ranks above
  * everything.  Rows as long as in quasar_distill_top.
  */
@@ -545,7 +546,8 @@ quasar_status quasar_top_logits(const void* logits, quasar_dtype dtype, int64_t 
  * -inf logits are ordinary values (q = 0; a listed one with p > 0 makes the
  * loss inf; a row of nothing else has loss inf and gradient 0).  A teacher
  * without mass gives loss and gradient 0: not a single entry of mass with
- * teacher_lse NULL, or a teacher_lse of -inf (a row of -inf).  A NaN
+ * teacher_lse NULL, or a teacher_lse of -inf (a row of -inf).  A NaN logit
+ * makes loss, statistics and gradient of its row NaN.  A NaN
  * among a row's listed values or in its teacher_lse makes the row's loss and
  * gradient NaN, and so does a listed +inf (teacher_lse +inf or NULL).  Up to
  * 6.4 million fp32 or 12.8 million bf16 logits a row (UNSUPPORTED beyond).

@@ -206,6 +206,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
 
     float m_rest, coef, q_rest;  // of the whole row (backward: m_rest is the rest's lse)
     float m_all, log_s = 0.0f;   // lse = m_all / tau + log_s (backward: lse = m_all)
+    bool nothing;                // every logit is -inf (a NaN beside them shows in the sum alone)
     if constexpr (!BACKWARD) {
         RunningSum run;
         for (int g = 0; g < groups; ++g) {
@@ -229,7 +230,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
         float m_in = neg_inf(), s_in = 0.0f;
         for (int k = lane; k < p.k; k += 32) m_in = fmaxf(m_in, own[k]);
         m_in = lanes_max(m_in, 0xffffffffu);
-        for (int k = lane; k < p.k; k += 32) s_in += m_in == neg_inf() ? 0.0f : exp2f((own[k] - m_in) * c2);
+        for (int k = lane; k < p.k; k += 32) s_in += own[k] == neg_inf() ? 0.0f : exp2f((own[k] - m_in) * c2);
         s_in = warp_sum(s_in);
         if (is_low(m_rest, c2)) s_rest = low_sum(S, m_rest, c2, scratch, drop);
         if (exchange) {
@@ -248,10 +249,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
         float s_all = s_rest;
         merge_sum(m_all, s_all, m_in, s_in, c2);
         log_s = logf(s_all);
-        const bool some = m_rest != neg_inf();
+        nothing = m_all == neg_inf() && s_all == 0.0f;
+        const bool some = m_rest != neg_inf() || s_rest != 0.0f;
         const float log_q_rest = some ? (m_rest - m_all) * inv_tau + (logf(s_rest) - log_s) : neg_inf();
         q_rest = expf(log_q_rest);
-        coef = some ? (mass * q_rest - p_rest) / s_rest : 0.0f * mass;
+        coef = some ? (mass * q_rest - p_rest) / s_rest : (s_all == s_all ? 0.0f * mass : s_all);
         if (rank == 0 && warp == 0) {
             float loss = 0.0f;
             for (int k = lane; k < p.k; k += 32)
@@ -259,7 +261,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
             loss = warp_sum(loss);
             if (lane == 0) {
                 loss += kl_term(p_rest, logf(p_rest), log_q_rest);
-                if (m_all == neg_inf()) loss = mass + __int_as_float(0x7F800000);  // q is 0 everywhere
+                if (nothing) loss = mass + __int_as_float(0x7F800000);  // q is 0 everywhere
                 p.loss[r] = mass == 0.0f ? 0.0f : loss;
                 if (p.stats) {
                     p.stats[2 * r] = m_all / p.temperature + log_s;
@@ -270,14 +272,15 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
         if (!grad) return;
     } else {
         m_all = p.stats[2 * r];
+        nothing = m_all == neg_inf();
         const float lse_rest = p.stats[2 * r + 1];
         const bool some = lse_rest != neg_inf();
         q_rest = some ? expf(lse_rest - m_all) : 0.0f;
-        coef = some ? mass * q_rest - p_rest : 0.0f * mass;
+        coef = some ? mass * q_rest - p_rest : (m_all == m_all ? 0.0f * mass : m_all);
         m_rest = some ? lse_rest : 0.0f;
     }
     // a row without teacher mass, or without a finite logit, has no gradient
-    const bool none = mass == 0.0f || (m_all == neg_inf() && mass == mass);
+    const bool none = mass == 0.0f || (nothing && mass == mass);
     const float scale = none ? 0.0f : weight * inv_tau;
     coef = none ? 0.0f : coef * scale;
 

@@ -261,11 +261,14 @@ struct RowStream {
 
 // Sums of exponentials are kept as (m, s), meaning sum e^(x / tau) = s e^(m /
 // tau) with m one of the logits; c = log2(e) / tau.  m = -inf: nothing was
-// added.
+// added (s = 0), or nothing but NaN (s = NaN; m does not see one).
 __device__ __forceinline__ void merge_sum(float& m, float& s, float m2, float s2, float c)
 {
     const float top = fmaxf(m, m2);
-    if (top == neg_inf()) return;
+    if (top == neg_inf()) {
+        s += s2;
+        return;
+    }
     s = s * exp2f((m - top) * c) + s2 * exp2f((m2 - top) * c);
     m = top;
 }
