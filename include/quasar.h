@@ -510,8 +510,8 @@ quasar_status quasar_activation_grad(const void* dy, int64_t ld_dy, const void* 
  *   values       [rows, k] fp32: the logits themselves (not scaled).
  *   indices      [rows, k] int32.  Equal values rank by the lowest index.
  *   lse          [rows] fp32: log sum exp(logits / temperature) over the
- *                vocabulary (-inf for a row of -inf, NaN for one with a
- *                NaN), or NULL.
+ *                vocabulary (-inf for a row of -inf, inf for one with an inf,
+ *                NaN for one with a NaN), or NULL.
  * -inf logits are ordinary values (masked entries), and a NaN ranks above
  * everything.  Rows as long as in quasar_distill_top.
  */
@@ -547,10 +547,11 @@ quasar_status quasar_top_logits(const void* logits, quasar_dtype dtype, int64_t 
  * loss inf; a row of nothing else has loss inf and gradient 0).  A teacher
  * without mass gives loss and gradient 0: not a single entry of mass with
  * teacher_lse NULL, or a teacher_lse of -inf (a row of -inf).  A NaN logit
- * makes loss, statistics and gradient of its row NaN.  A NaN
- * among a row's listed values or in its teacher_lse makes the row's loss and
- * gradient NaN, and so does a listed +inf (teacher_lse +inf or NULL).  Up to
- * 6.4 million fp32 or 12.8 million bf16 logits a row (UNSUPPORTED beyond).
+ * makes loss, statistics and gradient of its row NaN, a +inf loss and
+ * gradient.  A NaN among a row's listed values or in its teacher_lse makes
+ * loss and gradient NaN, and so does a listed +inf (teacher_lse +inf or NULL).
+ * Up to 6.4 million fp32 or 12.8 million bf16 logits a row (UNSUPPORTED
+ * beyond).
  */
 quasar_status quasar_distill_top(const void* logits, quasar_dtype dtype, int64_t ld, int64_t rows,
                                  int64_t vocab, const int32_t* indices, const float* values, int k,
@@ -560,7 +561,11 @@ quasar_status quasar_distill_top(const void* logits, quasar_dtype dtype, int64_t
 
 /* quasar_distill_top_backward -- the gradient alone, from the statistics a
  * forward call kept, where the rows' weights (the gradient that reaches each
- * row's loss) are known only later.  Arguments as above; stats is read. */
+ * row's loss) are known only later.  Arguments as above; stats is read.  The
+ * statistics are fp32: where all of a row's unlisted logits (or all of its
+ * logits) over the temperature lie beyond some 2^20 from zero, their spacing
+ * there is what this gradient is good to in the exponent; the forward call's
+ * own has no such limit. */
 quasar_status quasar_distill_top_backward(const void* logits, quasar_dtype dtype, int64_t ld,
                                           int64_t rows, int64_t vocab, const int32_t* indices,
                                           const float* values, int k, const float* teacher_lse,

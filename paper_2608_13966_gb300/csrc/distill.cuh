@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
         m_in = lanes_max(m_in, 0xffffffffu);
         for (int k = lane; k < p.k; k += 32) s_in += own[k] == neg_inf() ? 0.0f : exp2f((own[k] - m_in) * c2);
         s_in = warp_sum(s_in);
-        if (is_low(m_rest, c2)) s_rest = low_sum(S, m_rest, c2, scratch, drop);
+        if (is_far(m_rest, c2)) s_rest = far_sum(S, m_rest, c2, scratch, drop);
         if (exchange) {
             cluster_wait();  // every CTA of the row has started: its shared memory may be written
             if (t < p.row.ctas) {
@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
         m_all = m_rest;
         float s_all = s_rest;
         merge_sum(m_all, s_all, m_in, s_in, c2);
-        log_s = logf(s_all);
+        log_s = isinf(s_all) ? s_all - s_all : logf(s_all);  // (softmax of a +inf logit is NaN)
         nothing = m_all == neg_inf() && s_all == 0.0f;
         const bool some = m_rest != neg_inf() || s_rest != 0.0f;
         const float log_q_rest = some ? (m_rest - m_all) * inv_tau + (logf(s_rest) - log_s) : neg_inf();
@@ -287,9 +287,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
     // the unlisted entries: coef 2^(x c - base), or coef e^(z - lse) from kept
     // statistics
     const float base = m_rest == neg_inf() ? 0.0f : exp_base(m_rest, c2);
-    const bool low = !BACKWARD && base == kFloor;  // the subtraction first: see exp_base
-    if (!BACKWARD && !low) coef *= m_rest == neg_inf() ? 1.0f : exp_fix(m_rest, c2, base);
-    const float2 cc = make_float2(c2, c2), bb = make_float2(low ? 0.0f : -base, low ? 0.0f : -base),
+    const bool far = !BACKWARD && fabsf(base) == kFar;  // the subtraction first: see exp_base
+    if (!BACKWARD && !far) coef *= m_rest == neg_inf() ? 1.0f : exp_fix(m_rest, c2, base);
+    const float2 cc = make_float2(c2, c2), bb = make_float2(far ? 0.0f : -base, far ? 0.0f : -base),
                  kk = make_float2(coef, coef);
     // from the end of the row: what was read last is the likeliest to be in L2
     if (BACKWARD) {
@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
     for (int g = groups - 1; g >= 0; --g) {
         uint4 next[kHand];
         if (g > 0) S.load_group(next, g - 1);
-        if (BACKWARD || low) drop_group(raw, g);
+        if (BACKWARD || far) drop_group(raw, g);
         const bool whole = vectors && S.whole_group(g);
         uint4* to = reinterpret_cast<uint4*>(grad) + S.vec(g, 0);
 #pragma unroll
@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_top(const _
                     x[j] = make_float2(ex2(x[j].x), ex2(x[j].y));
                 }
             } else {
-                if (low) {
+                if (far) {
 #pragma unroll
                     for (int j = 0; j < kP; ++j) x[j] = __fadd2_rn(x[j], make_float2(-m_rest, -m_rest));
                 }

@@ -261,7 +261,8 @@ struct RowStream {
 
 // Sums of exponentials are kept as (m, s), meaning sum e^(x / tau) = s e^(m /
 // tau) with m one of the logits; c = log2(e) / tau.  m = -inf: nothing was
-// added (s = 0), or nothing but NaN (s = NaN; m does not see one).
+// added (s = 0), or nothing but NaN (s = NaN; m does not see one); m = inf: s is
+// inf, or NaN.
 __device__ __forceinline__ void merge_sum(float& m, float& s, float m2, float s2, float c)
 {
     const float top = fmaxf(m, m2);
@@ -269,7 +270,7 @@ __device__ __forceinline__ void merge_sum(float& m, float& s, float m2, float s2
         s += s2;
         return;
     }
-    s = s * exp2f((m - top) * c) + s2 * exp2f((m2 - top) * c);
+    s = (m == top ? s : s * exp2f((m - top) * c)) + (m2 == top ? s2 : s2 * exp2f((m2 - top) * c));
     m = top;
 }
 
@@ -287,19 +288,21 @@ __device__ __forceinline__ float warp_sum(float x)
 }
 
 // 2^((x - m) c) as one multiply-add and one exponential: 2^(x c - base) times
-// fix(), with base = m c as rounded and fix what that rounding took away.
-// Below kFloor the base stays there: a row masked with the type's lowest
-// value takes m c out of fp32's range.
-constexpr float kFloor = -1.2676506e30f;  // -2^100
+// fix(), with base = m c as rounded and fix what that rounding took away: at
+// most one half up to kFar, where the base stays.  Rows whose largest logit
+// lies farther out (masked with -1e10, or with the type's lowest value) take
+// the subtraction first, by is_far: a product's ulp of its own would be worth
+// powers of two there.
+constexpr float kFar = 16777216.0f;  // 2^24
 
-__device__ __forceinline__ float exp_base(float m, float c) { return fmaxf(m * c, kFloor); }
+__device__ __forceinline__ float exp_base(float m, float c) { return fminf(fmaxf(m * c, -kFar), kFar); }
 __device__ __forceinline__ float exp_fix(float m, float c, float base) { return exp2f(-fmaf(m, c, -base)); }
 
 // A thread's running sum: s = sum of 2^(x c - base).
 struct RunningSum {
     float m, base, s;
 
-    __device__ __forceinline__ RunningSum() : m(neg_inf()), base(kFloor), s(0.0f) {}
+    __device__ __forceinline__ RunningSum() : m(neg_inf()), base(-kFar), s(0.0f) {}
 
     template <typename T>
     __device__ __forceinline__ void add(const uint4 (&raw)[kHand], typename Vec16<T>::Max top, float c)
@@ -345,16 +348,16 @@ __device__ __forceinline__ void block_sum(const RunningSum& r, float c, float* s
     m = lanes_max(w, 0xffffffffu);
     const float base = exp_base(m, c);
     s = warp_sum(lane < kW ? scratch[kW + lane] * ex2(exp_base(w, c) - base) : 0.0f);
-    s = m == neg_inf() ? s : s * exp_fix(m, c, base);
+    s = isinf(m) ? s : s * exp_fix(m, c, base);
 }
 
-// Where every logit lies so far down that the base stopped at kFloor: the sum
-// again, the subtraction first.  `drop` replaces what a thread's vector (g, u) must
+// Where the largest logit lies so far out that the base stopped at kFar: the
+// sum again, the subtraction first.  `drop` replaces what a thread's vector (g, u) must
 // not count.
 // (Out of line, and its arguments by value: a reference would keep the caller's
 // variables in memory.)
 template <typename T, int THREADS, typename Drop>
-__device__ __noinline__ float low_sum(const RowStream<T, THREADS> S, float m, float c, float* scratch, Drop drop)
+__device__ __noinline__ float far_sum(const RowStream<T, THREADS> S, float m, float c, float* scratch, Drop drop)
 {
     constexpr int kP = Vec16<T>::kN / 2;
     float s = 0.0f;
@@ -376,6 +379,6 @@ __device__ __noinline__ float low_sum(const RowStream<T, THREADS> S, float m, fl
     return s;
 }
 
-__device__ __forceinline__ bool is_low(float m, float c) { return m != neg_inf() && m * c < kFloor; }
+__device__ __forceinline__ bool is_far(float m, float c) { return !isinf(m) && fabsf(m * c) > kFar; }
 
 }  // namespace quasar

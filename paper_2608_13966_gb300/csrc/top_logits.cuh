@@ -325,7 +325,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_top_logits(const __
     float m = neg_inf(), s = 0.0f;
     if (p.lse) {
         block_sum<THREADS>(run, c2, scratch, m, s);
-        if (is_low(m, c2)) s = low_sum(S, m, c2, scratch, [](uint4&, int, int) {});
+        if (is_far(m, c2)) s = far_sum(S, m, c2, scratch, [](uint4&, int, int) {});
         if (alone && t == 0)
             p.lse[r] = m == neg_inf() && s == 0.0f ? neg_inf() : m / p.temperature + logf(s);
     }
