@@ -72,7 +72,7 @@ __device__ __forceinline__ void activate(float (&v)[N], int act)
 {
     if (act == QUASAR_ACT_RELU) {
 #pragma unroll
-        for (int c = 0; c < N; ++c) v[c] = fmaxf(v[c], 0.0f);
+        for (int c = 0; c < N; ++c) v[c] = v[c] < 0.0f ? 0.0f : v[c];  // (a NaN stays one)
     } else if (act == QUASAR_ACT_SILU) {
 #pragma unroll
         for (int c = 0; c < N; ++c) v[c] *= sigmoid(v[c]);
@@ -92,7 +92,7 @@ __device__ __forceinline__ void times_slope(float (&v)[N], const float (&z)[N], 
 {
     if (act == QUASAR_ACT_RELU) {
 #pragma unroll
-        for (int c = 0; c < N; ++c) v[c] = z[c] > 0.0f ? v[c] : 0.0f;
+        for (int c = 0; c < N; ++c) v[c] = z[c] > 0.0f ? v[c] : (z[c] <= 0.0f ? 0.0f : z[c]);
     } else if (act == QUASAR_ACT_SILU) {
 #pragma unroll
         for (int c = 0; c < N; ++c) {
