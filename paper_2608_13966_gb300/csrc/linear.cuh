@@ -86,6 +86,10 @@ __device__ __forceinline__ void activate(float (&v)[N], int act)
     }
 }
 
+// Infinities brought in, where the slopes' products have their limits 0 and 1
+// (a NaN comes in too, and comes out again with the other factor).
+__device__ __forceinline__ float bring_in(float z) { return fminf(fmaxf(z, -1e30f), 1e30f); }
+
 // v *= act'(z)
 template <int N>
 __device__ __forceinline__ void times_slope(float (&v)[N], const float (&z)[N], int act)
@@ -97,14 +101,14 @@ __device__ __forceinline__ void times_slope(float (&v)[N], const float (&z)[N], 
 #pragma unroll
         for (int c = 0; c < N; ++c) {
             const float s = sigmoid(z[c]);
-            v[c] *= s * fmaf(z[c], 1.0f - s, 1.0f);
+            v[c] *= s * fmaf(bring_in(z[c]), 1.0f - s, 1.0f);
         }
     } else if (act == QUASAR_ACT_GELU) {
 #pragma unroll
         for (int c = 0; c < N; ++c) {
             float phi, density;
             normal(z[c], phi, density);
-            v[c] *= fmaf(z[c], density, phi);
+            v[c] *= fmaf(bring_in(z[c]), density, phi);
         }
     }
 }

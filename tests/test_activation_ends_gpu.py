@@ -51,3 +51,20 @@ def test_nan_goes_through_the_slope(activation):
         dx = api.linear_backward(dz, x, r, dr=False, pre_in=pre, activation_in=activation)["dx"]
         api.check_device()
         assert bool(torch.isnan(dx[tokens - 1, inputs - 2])) and int(torch.isnan(dx).sum()) == 1
+
+
+@pytest.mark.parametrize("activation,low", [("relu", 0.0), ("silu", 0.0), ("gelu", 0.0)])
+def test_an_infinite_pre_activation_has_slope_0_or_1(activation, low):
+    """A kept pre-activation past bf16's range is infinite: the slope is its limit there."""
+    far = torch.tensor([[-INF, -3e38, -200.0, 200.0, 3e38, INF, 0.5]], dtype=BF16, device="cuda")
+    got = api.activation_grad(torch.full_like(far, 2.0), far, activation)[0, :6].float()
+    assert got.tolist() == [low, low, low, 2.0, 2.0, 2.0]
+    for tokens, features, inputs in SHAPES:
+        dz, x, r = rand(tokens, features, seed=5), rand(tokens, inputs, seed=6), rand(features, inputs, seed=7)
+        pre = torch.full((tokens, inputs), INF, dtype=BF16, device="cuda")
+        pre[:, ::3] = -INF
+        plain = api.linear_backward(dz, x, r, dr=False)["dx"]
+        dx = api.linear_backward(dz, x, r, dr=False, pre_in=pre, activation_in=activation)["dx"]
+        api.check_device()
+        assert (dx[:, ::3] == 0).all()
+        assert torch.equal(dx[:, 1::3], plain[:, 1::3]) and torch.equal(dx[:, 2::3], plain[:, 2::3])
