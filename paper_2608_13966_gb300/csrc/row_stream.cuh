@@ -114,7 +114,9 @@ struct Vec16<__nv_bfloat16> {
 };
 
 // A load that is issued where it stands (the compiler would move it down to
-// its use, and the next vectors would no longer be on their way).
+// its use, and the next vectors would no longer be on their way).  An ordinary
+// load, not a read-only one: a gradient may take the logits' place within the
+// launch, each vector written after its thread has read it.
 // KEEP: the line is wanted again, and stays in L2 before others; otherwise it
 // goes first.
 template <bool KEEP>
@@ -124,13 +126,13 @@ __device__ __forceinline__ uint4 load_now(const uint4* p)
     if constexpr (KEEP)
         asm volatile(
             "{\n\t.reg .b64 keep;\n\tcreatepolicy.fractional.L2::evict_last.b64 keep, 1.0;\n\t"
-            "ld.global.nc.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], keep;\n\t}"
+            "ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], keep;\n\t}"
             : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
             : "l"(p));
     else
         asm volatile(
             "{\n\t.reg .b64 drop;\n\tcreatepolicy.fractional.L2::evict_first.b64 drop, 1.0;\n\t"
-            "ld.global.nc.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], drop;\n\t}"
+            "ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], drop;\n\t}"
             : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
             : "l"(p));
     return x;
