@@ -105,7 +105,7 @@ def load(build_if_missing: bool = True):
 
 def _ptr(x):
     """Device pointer of a tensor, an int, or None."""
-    if x is None or type(x) is int:
+    if x is None or isinstance(x, int):
         return x
     return x.data_ptr()
 
