@@ -294,7 +294,8 @@ def tensor_amax(w, stream=None):
 #
 # Matrices are 2-D CUDA tensors whose rows are contiguous (any row stride).
 # Each call takes a ``stream`` (a torch stream or a handle; None: the current
-# one); its outputs and scratch are allocated on the stream it runs on.  The
+# one); its outputs and scratch are allocated on the stream it runs on.  All of
+# its tensors lie on one device, the one that is current for that stream.  The
 # checks read each attribute once: a call with a handful of tokens runs for
 # less time on the GPU than a careless one takes on the host.
 
@@ -311,31 +312,49 @@ def _on(stream, call, *args, **kwargs):
         return call(*args, **kwargs)
 
 
-def _matrix(t, name, dtypes=_BF16S):
-    """(rows, columns, row stride) of a matrix; a single row's stride is its
-    length rounded up to what the products' operands need."""
+def _elsewhere(name, at, on):
+    return ValueError(f"{name} must be on cuda:{on}, as the call's first tensor, not on cuda:{at}")
+
+
+def _matrix(t, name, dtypes=_BF16S, on=None):
+    """(rows, columns, row stride) of a matrix (on device ``on``, if given); a
+    single row's stride is its length rounded up to what the products' operands
+    need."""
     try:
         (rows, cols), (ld, step) = t.shape, t.stride()
     except ValueError:
         raise ValueError(f"{name} must be a 2-D tensor") from None
     if step != 1 and cols > 1:
         raise ValueError(f"{name} must have contiguous rows")
-    if t.dtype not in dtypes or not t.is_cuda:
+    at = t.get_device()
+    if t.dtype not in dtypes or at < 0:
         raise ValueError(f"{name} must be a CUDA tensor of dtype {' or '.join(map(str, dtypes))}")
+    if on is not None and at != on:
+        raise _elsewhere(name, at, on)
     return rows, cols, ld if rows > 1 else -(-cols // 8) * 8
 
 
-def _like(t, name, rows, cols, dtypes=_BF16S):
+def _like(t, name, rows, cols, dtypes=_BF16S, on=None):
     """The row stride of a matrix that must have this shape."""
-    r, c, ld = _matrix(t, name, dtypes)
+    r, c, ld = _matrix(t, name, dtypes, on)
     if r != rows or c != cols:
         raise ValueError(f"{name} must have shape ({rows}, {cols}), not ({r}, {c})")
     return ld
 
 
-def _vector(t, name, n):
-    if t.shape != (n,) or t.dtype != torch.float32 or not t.is_cuda or not t.is_contiguous():
+def _vector(t, name, n, on):
+    at = t.get_device()
+    if t.shape != (n,) or t.dtype != torch.float32 or at < 0 or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous fp32 CUDA tensor of {n} values")
+    if at != on:
+        raise _elsewhere(name, at, on)
+
+
+def _current(on):
+    """The call runs on the current device: its tensors must lie there."""
+    now = torch.cuda.current_device()
+    if now != on:
+        raise ValueError(f"the tensors are on cuda:{on}, but the current device is cuda:{now}")
 
 
 def _float_code(dtype, name):
@@ -371,15 +390,17 @@ def linear(x, r, *, bias=None, activation="none", residual=None, out_dtype=torch
         return _on(stream, linear, x, r, bias=bias, activation=activation, residual=residual,
                    out_dtype=out_dtype, save_pre=save_pre)
     tokens, inputs, ld_x = _matrix(x, "x")
-    features, r_inputs, ld_r = _matrix(r, "r")
+    on = x.get_device()
+    features, r_inputs, ld_r = _matrix(r, "r", on=on)
     if r_inputs != inputs:
         raise ValueError(f"x has {inputs} inputs, r {r_inputs}")
     code, act = _float_code(out_dtype, "out_dtype"), _act_code(activation)
     ld_res = ld_pre = 0
     if bias is not None:
-        _vector(bias, "bias", features)
+        _vector(bias, "bias", features, on)
     if residual is not None:
-        ld_res = _like(residual, "residual", tokens, features, (out_dtype,))
+        ld_res = _like(residual, "residual", tokens, features, (out_dtype,), on)
+    _current(on)
     y = torch.empty((tokens, features), dtype=out_dtype, device=x.device)
     pre = None
     if save_pre:
@@ -398,7 +419,9 @@ def activation_grad(dy, pre, activation, *, stream=None):
     act = _act_code(activation)
     if activation == "none":
         pre = None
-    ld_pre = 0 if pre is None else _like(pre, "pre", rows, cols)
+    on = dy.get_device()
+    ld_pre = 0 if pre is None else _like(pre, "pre", rows, cols, on=on)
+    _current(on)
     dz, ld_dz = _rows_of_8(rows, cols, dy.device)
     _check(quasar_activation_grad(dy, ld_dy, pre, ld_pre, act, rows, cols, dz, ld_dz))
     return dz
@@ -419,16 +442,18 @@ def linear_backward(dz, x, r, *, dx=True, dr=True, bias=False, pre_in=None, acti
                    activation_in=activation_in, residual=residual, dx_dtype=dx_dtype,
                    dr_dtype=dr_dtype)
     tokens, features, ld_dz = _matrix(dz, "dz")
-    x_tokens, inputs, ld_x = _matrix(x, "x")
+    on = dz.get_device()
+    x_tokens, inputs, ld_x = _matrix(x, "x", on=on)
     if x_tokens != tokens:
         raise ValueError(f"dz has {tokens} tokens, x {x_tokens}")
-    ld_r = _like(r, "r", features, inputs)
+    ld_r = _like(r, "r", features, inputs, on=on)
     act = _act_code(activation_in)
     if (pre_in is None) != (activation_in == "none"):
         raise ValueError("pre_in and activation_in go together")
     dx_code, dr_code = _float_code(dx_dtype, "dx_dtype"), _float_code(dr_dtype, "dr_dtype")
-    ld_pre = 0 if pre_in is None else _like(pre_in, "pre_in", tokens, inputs)
-    ld_res = 0 if residual is None else _like(residual, "residual", tokens, inputs, (dx_dtype,))
+    ld_pre = 0 if pre_in is None else _like(pre_in, "pre_in", tokens, inputs, on=on)
+    ld_res = 0 if residual is None else _like(residual, "residual", tokens, inputs, (dx_dtype,), on)
+    _current(on)
     if ld_dz % 8 or dz.data_ptr() % 16:
         dz = activation_grad(dz, None, "none")
         ld_dz = _ld(dz)
@@ -462,6 +487,7 @@ def top_logits(logits, k, *, temperature=1.0, lse=True, stream=None):
     if stream is not None:
         return _on(stream, top_logits, logits, k, temperature=temperature, lse=lse)
     rows, vocab, ld = _matrix(logits, "logits", _FLOATS)
+    _current(logits.get_device())
     device = logits.device
     values = torch.empty((rows, k), dtype=torch.float32, device=device)
     indices = torch.empty((rows, k), dtype=torch.int32, device=device)
@@ -474,19 +500,24 @@ def top_logits(logits, k, *, temperature=1.0, lse=True, stream=None):
     return out
 
 
-def _teacher(rows, indices, values, teacher_lse, row_weight):
+def _teacher(rows, on, indices, values, teacher_lse, row_weight):
     """k, of a teacher's lists for this many rows."""
-    shape = indices.shape
-    if len(shape) != 2 or shape[0] != rows or indices.dtype != torch.int32 or \
-            not indices.is_cuda or not indices.is_contiguous():
+    shape, at = indices.shape, indices.get_device()
+    if len(shape) != 2 or shape[0] != rows or indices.dtype != torch.int32 or at < 0 or \
+            not indices.is_contiguous():
         raise ValueError("indices must be a contiguous int32 CUDA tensor [rows, k]")
-    if values.shape != shape or values.dtype != torch.float32 or not values.is_cuda or \
+    if at != on:
+        raise _elsewhere("indices", at, on)
+    at = values.get_device()
+    if values.shape != shape or values.dtype != torch.float32 or at < 0 or \
             not values.is_contiguous():
         raise ValueError("values must be a contiguous fp32 CUDA tensor of the shape of indices")
+    if at != on:
+        raise _elsewhere("values", at, on)
     if teacher_lse is not None:
-        _vector(teacher_lse, "teacher_lse", rows)
+        _vector(teacher_lse, "teacher_lse", rows, on)
     if row_weight is not None:
-        _vector(row_weight, "row_weight", rows)
+        _vector(row_weight, "row_weight", rows, on)
     return shape[1]
 
 
@@ -505,7 +536,9 @@ def distill_top(logits, indices, values, *, teacher_lse=None, row_weight=None, t
         return _on(stream, distill_top, logits, indices, values, teacher_lse=teacher_lse,
                    row_weight=row_weight, temperature=temperature, grad=grad, stats=stats, out=out)
     rows, vocab, ld = _matrix(logits, "logits", _FLOATS)
-    k = _teacher(rows, indices, values, teacher_lse, row_weight)
+    on = logits.get_device()
+    k = _teacher(rows, on, indices, values, teacher_lse, row_weight)
+    _current(on)
     device = logits.device
     loss = torch.empty(rows, dtype=torch.float32, device=device)
     made = {"loss": loss}
@@ -514,7 +547,7 @@ def distill_top(logits, indices, values, *, teacher_lse=None, row_weight=None, t
         if out is None:
             out, ld_out = torch.empty((rows, vocab), dtype=logits.dtype, device=device), vocab
         else:
-            ld_out = _like(out, "out", rows, vocab, (logits.dtype,))
+            ld_out = _like(out, "out", rows, vocab, (logits.dtype,), on)
         made["grad"] = out
     else:
         out = None
@@ -533,14 +566,16 @@ def distill_top_backward(logits, indices, values, stats, row_weight, *, teacher_
         return _on(stream, distill_top_backward, logits, indices, values, stats, row_weight,
                    teacher_lse=teacher_lse, temperature=temperature, out=out)
     rows, vocab, ld = _matrix(logits, "logits", _FLOATS)
-    k = _teacher(rows, indices, values, teacher_lse, row_weight)
-    _like(stats, "stats", rows, 2, (torch.float32,))
+    on = logits.get_device()
+    k = _teacher(rows, on, indices, values, teacher_lse, row_weight)
+    _like(stats, "stats", rows, 2, (torch.float32,), on)
     if not stats.is_contiguous():
         raise ValueError("stats must be contiguous")
+    _current(on)
     if out is None:
         out, ld_out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device), vocab
     else:
-        ld_out = _like(out, "out", rows, vocab, (logits.dtype,))
+        ld_out = _like(out, "out", rows, vocab, (logits.dtype,), on)
     _check(quasar_distill_top_backward(logits, _CODES[logits.dtype], ld, rows, vocab, indices,
                                        values, k, teacher_lse, stats, row_weight, temperature, out,
                                        ld_out))
