@@ -10,6 +10,7 @@
 
 #include "host.h"
 #include "linear.h"
+#include "linear_plan.h"
 #include "logits.h"
 #include "quasar.h"
 
@@ -146,38 +147,6 @@ int tile_stages(int bn, size_t* smem)
     return stages;
 }
 
-// CTAs that share a tile's reduction: as many as leave each two blocks, while
-// all clusters run at once.  A CTA's copies bound it, so a split shortens the
-// call until the SMs are full (2 against 3 CTAs a tile: 128 x 11008 x 4096
-// 23.9 and 19.5 us, 5012 x 160 x 12544 55 and 41), but clusters left over
-// start when the rest is done (5012 x 128 x 12544: 40 clusters of 6 CTAs 29.6
-// us, of 7, more than fit, 45.8, of 4 33.2).
-//
-// How many clusters fit does not follow from the SM count, as one lies within
-// a part of the device.  The device's answer counts one CTA an SM; the kernel
-// runs two, so a cluster of s takes the place of half one, or of one of half
-// the size.  That holds for every variant: one kernel is asked for all.
-quasar_status tile_split(int64_t tiles, int k_blocks, int n_sm, int* split)
-{
-    *split = 1;
-    size_t smem = 0;
-    tile_stages(128, &smem);
-    const void* fn = product_tile_kernel(128, false, false, false);
-    for (int s = std::min(8, k_blocks / 2); s > 1; --s) {
-        if (tiles * s > 2 * (int64_t)n_sm) continue;
-        int whole = 0, half = n_sm;
-        quasar_status st = host_max_clusters(fn, s, 192, smem, &whole);
-        if (st == QUASAR_OK && s > 2) st = host_max_clusters(fn, (s + 1) / 2, 192, smem, &half);
-        if (st != QUASAR_OK) return st;
-        if (tiles > std::max(2 * whole, half)) continue;
-        // no more CTAs than the longest share needs
-        while ((k_blocks + s - 2) / (s - 1) == (k_blocks + s - 1) / s) --s;
-        *split = s;
-        break;
-    }
-    return QUASAR_OK;
-}
-
 // D (rows x cols, rows contiguous) = A B^T over `depth`, then the epilogue.
 quasar_status product(const Operand& a, const Operand& b, int64_t rows, int64_t cols, int64_t depth,
                       const Epilogue& e, quasar_stream_t stream)
@@ -219,9 +188,12 @@ quasar_status product(const Operand& a, const Operand& b, int64_t rows, int64_t 
     p.tiles_row = (int)((rows + 127) / 128);
     p.tiles_col = (int)((cols + bn - 1) / bn);
     const int64_t tiles = (int64_t)p.tiles_row * p.tiles_col;
-    p.split = 1;
-    if ((st = tile_split(tiles, p.k_blocks, n_sm, &p.split)) != QUASAR_OK) return st;
     size_t smem = 0;
+    // (the answer holds for every variant: one kernel is asked for all)
+    tile_stages(128, &smem);
+    const void* asked = product_tile_kernel(128, false, false, false);
+    auto max_clusters = [&](int size, int* n) { return host_max_clusters(asked, size, 192, smem, n); };
+    if ((st = tile_split(tiles, p.k_blocks, n_sm, max_clusters, &p.split)) != QUASAR_OK) return st;
     p.stages = tile_stages(bn, &smem);
     if (tiles * p.split > (int64_t(1) << 31) - 1) return QUASAR_ERR_UNSUPPORTED;
     // parts are only worth promoting where there are several
