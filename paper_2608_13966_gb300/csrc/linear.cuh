@@ -351,7 +351,7 @@ __global__ void __launch_bounds__(192, 2) k_product_tile(const __grid_constant__
         mbar_init_fence();
     }
     if (warp == 5) tmem_alloc<1>(tmem_slot, kColumns);
-    if (warp == 4 && lane == 0) {
+    if (warp == 4 && lane == 0 && p.k_blocks > 0) {  // (an empty reduction has no maps)
         prefetch_map(&p.a);
         prefetch_map(&p.b);
     }
