@@ -447,7 +447,8 @@ typedef enum {
  * Any number of tokens, from one up; features may be odd, rows of y, pre and
  * residual may start anywhere.  tokens or features 0 is a no-op; inputs 0
  * gives z = bias.  Products are exact bf16 x bf16, accumulated in fp32.
- * Outputs must not overlap inputs, but for the residual.
+ * Outputs must share no byte with inputs, but for the residual; columns of one
+ * buffer share none.
  */
 quasar_status quasar_linear(const void* x, int64_t ld_x, const void* r, int64_t ld_r,
                             const float* bias, quasar_activation activation, const void* residual,

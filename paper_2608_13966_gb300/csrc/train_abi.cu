@@ -38,17 +38,35 @@ int64_t dtype_size(quasar_dtype d) { return d == QUASAR_BF16 ? 2 : 4; }
 bool valid_act(quasar_activation a) { return a >= QUASAR_ACT_NONE && a <= QUASAR_ACT_GELU; }
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-// Bytes a strided [rows, cols] view spans.
-size_t span(int64_t rows, int64_t cols, int64_t ld, int64_t size)
-{
-    return rows == 0 || cols == 0 ? 0 : (size_t)(((rows - 1) * ld + cols) * size);
-}
+// The bytes of a strided matrix: `width` of them in each of `rows` rows that
+// are `pitch` apart.
+struct Bytes {
+    uintptr_t at;
+    size_t rows, width, pitch;
 
-bool overlaps(const void* a, size_t na, const void* b, size_t nb)
+    Bytes(const void* p, int64_t rows_, int64_t cols, int64_t ld, int64_t size)
+        : at(reinterpret_cast<uintptr_t>(p)), rows(p ? (size_t)rows_ : 0), width((size_t)(cols * size)),
+          pitch((size_t)(ld * size))
+    {
+    }
+    Bytes(const void* p, int64_t n, int64_t size) : Bytes(p, 1, n, n, size) {}
+    size_t span() const { return rows == 0 || width == 0 ? 0 : (rows - 1) * pitch + width; }
+    bool operator==(const Bytes& o) const
+    {
+        return at == o.at && rows == o.rows && width == o.width && (rows <= 1 || pitch == o.pitch);
+    }
+};
+
+// Whether two matrices share a byte.  Columns of one buffer (the same pitch)
+// lie between each other's without: decided by where they lie in its rows.
+bool overlaps(const Bytes& a, const Bytes& b)
 {
-    if (!a || !b || na == 0 || nb == 0) return false;
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x < y + nb && y < x + na;
+    const size_t na = a.span(), nb = b.span();
+    if (na == 0 || nb == 0 || a.at >= b.at + nb || b.at >= a.at + na) return false;
+    const size_t pitch = a.rows > 1 ? a.pitch : b.pitch;
+    if ((b.rows > 1 && b.pitch != pitch) || a.width > pitch || b.width > pitch) return true;
+    const size_t from = b.at >= a.at ? (b.at - a.at) % pitch : (pitch - (a.at - b.at) % pitch) % pitch;
+    return from < a.width || from + b.width > pitch;
 }
 
 // Sizes a 2-D view may have: coordinates are 32-bit on the device, offsets 64.
@@ -260,22 +278,20 @@ quasar_status run_distill(const void* logits, quasar_dtype dtype, int64_t ld, in
         return QUASAR_ERR_INVALID_ARG;
     if (backward ? (!stats || !grad) : !loss) return QUASAR_ERR_INVALID_ARG;
     if (!aligned(grad, (uintptr_t)dtype_size(dtype))) return QUASAR_ERR_INVALID_ARG;
-    const size_t n_log = span(rows, vocab, ld, dtype_size(dtype));
-    const size_t n_grad = grad ? span(rows, vocab, ld_grad, dtype_size(dtype)) : 0;
-    const size_t n_row = (size_t)rows * 4, n_top = (size_t)rows * k * 4;
+    const Bytes b_logits(logits, rows, vocab, ld, dtype_size(dtype));
+    const Bytes b_grad(grad, rows, vocab, ld_grad, dtype_size(dtype));
     // the gradient may replace the logits, in exactly their place
-    const bool in_place = grad == logits && ld_grad == ld;
-    if (!in_place && overlaps(grad, n_grad, logits, n_log)) return QUASAR_ERR_INVALID_ARG;
-    const void* outs[] = {grad, backward ? nullptr : loss, backward ? nullptr : stats};
-    const size_t out_n[] = {n_grad, n_row, 2 * n_row};
-    const void* ins[] = {indices, values, teacher_lse, row_weight, backward ? stats : nullptr};
-    const size_t in_n[] = {n_top, n_top, n_row, n_row, 2 * n_row};
+    if (!(b_grad == b_logits) && overlaps(b_grad, b_logits)) return QUASAR_ERR_INVALID_ARG;
+    const Bytes outs[] = {b_grad, Bytes(backward ? nullptr : loss, rows, 4),
+                          Bytes(backward ? nullptr : stats, 2 * rows, 4)};
+    const Bytes ins[] = {Bytes(indices, rows * k, 4), Bytes(values, rows * k, 4), Bytes(teacher_lse, rows, 4),
+                         Bytes(row_weight, rows, 4), Bytes(backward ? stats : nullptr, 2 * rows, 4)};
     for (int i = 0; i < 3; ++i) {
-        for (int j = 0; j < 5; ++j)
-            if (overlaps(outs[i], out_n[i], ins[j], in_n[j])) return QUASAR_ERR_INVALID_ARG;
-        if (i > 0 && overlaps(outs[i], out_n[i], logits, n_log)) return QUASAR_ERR_INVALID_ARG;
+        for (const Bytes& in : ins)
+            if (overlaps(outs[i], in)) return QUASAR_ERR_INVALID_ARG;
+        if (i > 0 && overlaps(outs[i], b_logits)) return QUASAR_ERR_INVALID_ARG;
         for (int j = 0; j < i; ++j)
-            if (overlaps(outs[i], out_n[i], outs[j], out_n[j])) return QUASAR_ERR_INVALID_ARG;
+            if (overlaps(outs[i], outs[j])) return QUASAR_ERR_INVALID_ARG;
     }
     DistillParams p{};
     int threads = 0;
@@ -314,17 +330,13 @@ quasar_status quasar_linear(const void* x, int64_t ld_x, const void* r, int64_t 
     const int64_t size = dtype_size(y_dtype);
     if (!y || !aligned(y, size) || !aligned(residual, size) || !aligned(bias, 4) || !aligned(pre, 2))
         return QUASAR_ERR_INVALID_ARG;
-    const size_t n_y = span(tokens, features, ld_y, size);
-    const size_t n_pre = pre ? span(tokens, features, ld_pre, 2) : 0;
-    const size_t n_res = residual ? span(tokens, features, ld_residual, size) : 0;
-    const size_t n_x = span(tokens, inputs, ld_x, 2), n_r = span(features, inputs, ld_r, 2);
-    const size_t n_bias = bias ? (size_t)features * 4 : 0;
+    const Bytes b_y(y, tokens, features, ld_y, size), b_pre(pre, tokens, features, ld_pre, 2);
+    const Bytes b_res(residual, tokens, features, ld_residual, size), b_bias(bias, features, 4);
+    const Bytes b_x(x, tokens, inputs, ld_x, 2), b_r(r, features, inputs, ld_r, 2);
     // y may replace the residual, in exactly its place
-    const bool in_place = residual == y && ld_residual == ld_y;
-    if (overlaps(y, n_y, x, n_x) || overlaps(y, n_y, r, n_r) || overlaps(y, n_y, bias, n_bias) ||
-        (!in_place && overlaps(y, n_y, residual, n_res)) || overlaps(pre, n_pre, x, n_x) ||
-        overlaps(pre, n_pre, r, n_r) || overlaps(pre, n_pre, bias, n_bias) ||
-        overlaps(pre, n_pre, residual, n_res) || overlaps(pre, n_pre, y, n_y))
+    if (overlaps(b_y, b_x) || overlaps(b_y, b_r) || overlaps(b_y, b_bias) ||
+        (!(b_res == b_y) && overlaps(b_y, b_res)) || overlaps(b_pre, b_x) || overlaps(b_pre, b_r) ||
+        overlaps(b_pre, b_bias) || overlaps(b_pre, b_res) || overlaps(b_pre, b_y))
         return QUASAR_ERR_INVALID_ARG;
     const Epilogue e{bias, pre, ld_pre, nullptr, 0, residual, ld_residual, y, ld_y, activation,
                      y_dtype == QUASAR_F32};
@@ -356,15 +368,12 @@ quasar_status quasar_linear_grad_input(const void* dz, int64_t ld_dz, const void
     const int64_t size = dtype_size(dx_dtype);
     if (!dx || !aligned(dx, size) || !aligned(residual, size) || !aligned(pre_in, 2)) return QUASAR_ERR_INVALID_ARG;
     if (slope && !pre_in) return QUASAR_ERR_INVALID_ARG;
-    const size_t n_dx = span(tokens, inputs, ld_dx, size);
-    const size_t n_pre = pre_in ? span(tokens, inputs, ld_pre_in, 2) : 0;
-    const size_t n_res = residual ? span(tokens, inputs, ld_residual, size) : 0;
-    const bool res_in_place = residual == dx && ld_residual == ld_dx;
-    const bool pre_in_place = pre_in == dx && ld_pre_in == ld_dx && size == 2;
-    if (overlaps(dx, n_dx, dz, span(tokens, features, ld_dz, 2)) ||
-        overlaps(dx, n_dx, r, span(features, inputs, ld_r, 2)) ||
-        (!pre_in_place && overlaps(dx, n_dx, pre_in, n_pre)) ||
-        (!res_in_place && overlaps(dx, n_dx, residual, n_res)))
+    const Bytes b_dx(dx, tokens, inputs, ld_dx, size), b_pre(pre_in, tokens, inputs, ld_pre_in, 2);
+    const Bytes b_res(residual, tokens, inputs, ld_residual, size);
+    // dx may replace the residual or a bf16 pre_in, in exactly their place
+    if (overlaps(b_dx, Bytes(dz, tokens, features, ld_dz, 2)) ||
+        overlaps(b_dx, Bytes(r, features, inputs, ld_r, 2)) || (!(b_pre == b_dx) && overlaps(b_dx, b_pre)) ||
+        (!(b_res == b_dx) && overlaps(b_dx, b_res)))
         return QUASAR_ERR_INVALID_ARG;
     const Epilogue e{nullptr, nullptr, 0, slope ? pre_in : nullptr, ld_pre_in, residual, ld_residual, dx, ld_dx,
                      activation_in, dx_dtype == QUASAR_F32};
@@ -382,11 +391,10 @@ quasar_status quasar_linear_grad_weight(const void* dz, int64_t ld_dz, const voi
         return QUASAR_ERR_INVALID_ARG;
     if (features == 0) return QUASAR_OK;
     if ((dr && !aligned(dr, dtype_size(dr_dtype))) || !aligned(dbias, 4)) return QUASAR_ERR_INVALID_ARG;
-    const size_t n_dz = span(tokens, features, ld_dz, 2);
-    const size_t n_dr = dr ? span(features, inputs, ld_dr, dtype_size(dr_dtype)) : 0;
-    const size_t n_x = dr ? span(tokens, inputs, ld_x, 2) : 0, n_db = dbias ? (size_t)features * 4 : 0;
-    if (overlaps(dr, n_dr, dz, n_dz) || overlaps(dr, n_dr, x, n_x) || overlaps(dbias, n_db, dz, n_dz) ||
-        overlaps(dbias, n_db, x, n_x) || overlaps(dbias, n_db, dr, n_dr))
+    const Bytes b_dz(dz, tokens, features, ld_dz, 2), b_x(dr ? x : nullptr, tokens, inputs, ld_x, 2);
+    const Bytes b_dr(dr, features, inputs, ld_dr, dtype_size(dr_dtype)), b_dbias(dbias, features, 4);
+    if (overlaps(b_dr, b_dz) || overlaps(b_dr, b_x) || overlaps(b_dbias, b_dz) || overlaps(b_dbias, b_x) ||
+        overlaps(b_dbias, b_dr))
         return QUASAR_ERR_INVALID_ARG;
     if ((!dr || inputs == 0) && !dbias) return QUASAR_OK;
     // a few tokens: writing dr is what it takes, 20 us against the tensor cores'
@@ -424,9 +432,9 @@ quasar_status quasar_activation_grad(const void* dy, int64_t ld_dy, const void* 
     if (rows == 0 || cols == 0) return QUASAR_OK;
     if (!dy || !dz || (slope && !pre) || !aligned(dy, 2) || !aligned(dz, 2) || !aligned(pre, 2))
         return QUASAR_ERR_INVALID_ARG;
-    const size_t n_dz = span(rows, cols, ld_dz, 2);
-    if ((!(dz == dy && ld_dz == ld_dy) && overlaps(dz, n_dz, dy, span(rows, cols, ld_dy, 2))) ||
-        (slope && !(dz == pre && ld_dz == ld_pre) && overlaps(dz, n_dz, pre, span(rows, cols, ld_pre, 2))))
+    const Bytes b_dz(dz, rows, cols, ld_dz, 2), b_dy(dy, rows, cols, ld_dy, 2);
+    const Bytes b_pre(slope ? pre : nullptr, rows, cols, ld_pre, 2);
+    if ((!(b_dz == b_dy) && overlaps(b_dz, b_dy)) || (!(b_dz == b_pre) && overlaps(b_dz, b_pre)))
         return QUASAR_ERR_INVALID_ARG;
     ActGradParams p{dy, ld_dy, slope ? pre : nullptr, ld_pre, dz, ld_dz, rows, cols, activation};
     return launch(activation_grad_kernel(), &p,
@@ -442,11 +450,10 @@ quasar_status quasar_top_logits(const void* logits, quasar_dtype dtype, int64_t 
     if (rows == 0) return QUASAR_OK;
     if (!values || !indices || !aligned(values, 4) || !aligned(indices, 4) || !aligned(lse, 4))
         return QUASAR_ERR_INVALID_ARG;
-    const size_t n_log = span(rows, vocab, ld, dtype_size(dtype)), n_top = (size_t)rows * k * 4;
-    const size_t n_lse = lse ? (size_t)rows * 4 : 0;
-    if (overlaps(values, n_top, logits, n_log) || overlaps(indices, n_top, logits, n_log) ||
-        overlaps(lse, n_lse, logits, n_log) || overlaps(values, n_top, indices, n_top) ||
-        overlaps(lse, n_lse, values, n_top) || overlaps(lse, n_lse, indices, n_top))
+    const Bytes b_logits(logits, rows, vocab, ld, dtype_size(dtype)), b_lse(lse, rows, 4);
+    const Bytes b_values(values, rows * k, 4), b_indices(indices, rows * k, 4);
+    if (overlaps(b_values, b_logits) || overlaps(b_indices, b_logits) || overlaps(b_lse, b_logits) ||
+        overlaps(b_values, b_indices) || overlaps(b_lse, b_values) || overlaps(b_lse, b_indices))
         return QUASAR_ERR_INVALID_ARG;
     TopParams p{};
     int threads = 0;
