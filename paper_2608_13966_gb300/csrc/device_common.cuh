@@ -100,7 +100,8 @@ __device__ __forceinline__ void bulk_g2s(void* dst, const void* src, uint32_t by
 // Launched as a programmatic dependent, a grid starts while the one before it
 // in the stream drains: nothing of global memory is read or written before
 // this wait, which ends when that grid has completed.  The next grid may then
-// start its own prologue.
+// start its own prologue.  Such a kernel has no read-only loads: their memory
+// must not change from the kernel's start on, and they may move above the wait.
 __device__ __forceinline__ void wait_for_previous_grid()
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");

@@ -46,10 +46,10 @@ __global__ void __launch_bounds__(kOuterThreads) k_outer(const __grid_constant__
         if (whole) {
             uint2 w[2];
             if constexpr (F32) {
-                w[0] = __ldg(reinterpret_cast<const uint2*>(from + place(0)));
-                w[1] = __ldg(reinterpret_cast<const uint2*>(from + place(2)));
+                w[0] = *reinterpret_cast<const uint2*>(from + place(0));
+                w[1] = *reinterpret_cast<const uint2*>(from + place(2));
             } else {
-                const uint4 v = __ldg(reinterpret_cast<const uint4*>(from + place(0)));
+                const uint4 v = *reinterpret_cast<const uint4*>(from + place(0));
                 w[0] = make_uint2(v.x, v.y);
                 w[1] = make_uint2(v.z, v.w);
             }

@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(32 * kOneWarps) k_linear_one(const __grid_cons
 #pragma unroll
         for (int f = 0; f < kF; ++f) raw[f] = __ldcs(row[f] + v);
         float2 xs[4];
-        unpack8(__ldg(reinterpret_cast<const uint4*>(x) + v), xs);
+        unpack8(reinterpret_cast<const uint4*>(x)[v], xs);
 #pragma unroll
         for (int f = 0; f < kF; ++f) {
             float2 w[4];
