@@ -117,8 +117,9 @@ struct Vec16<__nv_bfloat16> {
 // its use, and the next vectors would no longer be on their way).  An ordinary
 // load, not a read-only one: a gradient may take the logits' place within the
 // launch, each vector written after its thread has read it.
-// KEEP: the line is wanted again, and stays in L2 before others; otherwise it
-// goes first.
+// KEEP: the line may be wanted again, and stays in L2 before others (the
+// distillation's first pass asks so whether a gradient follows or not);
+// otherwise it goes first.
 template <bool KEEP>
 __device__ __forceinline__ uint4 load_now(const uint4* p)
 {
