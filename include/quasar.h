@@ -532,9 +532,10 @@ quasar_status quasar_top_logits(const void* logits, quasar_dtype dtype, int64_t 
  *   loss = sum_k p_k log(p_k / q_k) + p_r log(p_r / q_r)
  *   grad = row_weight * d loss / d logits
  * The loss is summed as p log(p/q) - p + q, which is the same where p sums to
- * one.  A teacher_lse that is not the values' own may leave it at another sum
- * (above one, or below with the whole vocabulary listed): the loss is then
- * larger by 1 - sum p, the gradient is that of the formula.
+ * one.  teacher_lse may leave it at another sum (above one, or below with the
+ * whole vocabulary listed; by its rounding, some 1e-7, or because it belongs
+ * to other values): the loss is then larger by 1 - sum p, the gradient is that
+ * of the formula.
  *
  *   logits       [rows, vocab] bf16 or fp32; rows may start anywhere.
  *   indices      [rows, k] int32, distinct within a row.  An index outside

@@ -525,19 +525,20 @@ __global__ void __launch_bounds__(192, 2) k_product_tile(const __grid_constant__
 // into the other half while the epilogue drains this one.
 //
 // PROMOTE: fp32 results, parts of the reduction added up in registers as in
-// k_product_tile (8192 x 14336 x 4096 with parts of 512: 660 us against 515
-// us for bf16 results, of which the larger output takes 35).
+// k_product_tile (8192 x 14336 x 4096 with parts of 512: 667 us against 521
+// us for bf16 results, one input set over and over).  Its 64 sums a thread
+// leave some of the epilogue's values in local memory; with 8 warps none are,
+// and it takes 661.
 //
 // Bound by the tensor cores and the power they draw: 8192 x 14336 x 4096 with
-// bias, SiLU and kept pre-activation takes 632 us, 1.52 PFLOP/s, 0.81 of the
-// measured burst rate and 0.89 of the sustained (535 to 557 us, 1.76 PFLOP/s,
-// where one input set is used over and over).  With a short reduction, by the
-// epilogue: the weight gradient of 32 tokens, 14336 x 4096, takes 36.5 us, 3.2
-// TB/s.
+// bias, SiLU and kept pre-activation takes 615 us, 1.56 PFLOP/s, 0.83 of the
+// measured burst rate and 0.91 of the sustained (536 to 572 us, where one input
+// set is used over and over).  With a short reduction, by the epilogue: the
+// weight gradient of 32 tokens, 14336 x 4096, takes 36 to 45 us.
 //
 // Warps: 0-15 epilogue (lane quadrant w % 4, 64 columns w / 4; with 8 warps of
-// 128 columns 32 tokens' gradient took 42 us, 2560 x 2560 x 1024 with SiLU 22.5
-// against 20.9, the large products 0 to 3% less), 16 copies, 17 matrix
+// 128 columns 32 tokens' gradient took 56 us against 45, 2560 x 2560 x 1024 with
+// SiLU 19.2 against 18.5, the large products the same), 16 copies, 17 matrix
 // instructions and, in the second CTA, the drained accumulators' messages.
 constexpr int kPairCols = 256;
 constexpr int kPairEpilogue = 16;  // warps

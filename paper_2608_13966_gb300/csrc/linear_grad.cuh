@@ -155,7 +155,9 @@ __global__ void __launch_bounds__(256) k_column_sum(const __grid_constant__ Colu
     }
 }
 
-// dz = dy act'(pre), rounded once to bf16 (pre NULL: a strided copy).
+// dz = dy act'(pre), rounded once to bf16 (pre NULL: a strided copy).  One
+// element a thread, so bound by its loads' number: 4096 x 12288 takes 237 us
+// with SiLU, 1.3 TB/s, and 199 us as a copy of odd rows.
 __global__ void __launch_bounds__(256) k_activation_grad(const __grid_constant__ ActGradParams p)
 {
     wait_for_previous_grid();

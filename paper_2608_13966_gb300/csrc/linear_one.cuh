@@ -3,7 +3,7 @@
 //
 // A CTA takes 4 features and splits their rows over its 8 warps, so that the
 // 32 KB of four rows of 4,096 are all on their way at once; x comes from L1.
-// Bound by HBM: 14336 x 4096 takes 22 us, 5.3 TB/s.  (From two tokens on the
+// Bound by HBM: 14336 x 4096 takes 22.0 us, 5.3 TB/s.  (From two tokens on the
 // tensor cores' kernel is faster: see the rule in the launch.)
 #pragma once
 

@@ -11,9 +11,9 @@ namespace quasar {
 // CTAs that share a tile's reduction: as many as leave each two blocks, while
 // all clusters run at once.  A CTA's copies bound it, so a split shortens the
 // call until the SMs are full (2 against 3 CTAs a tile: 128 x 11008 x 4096
-// 23.9 and 19.5 us, 5012 x 160 x 12544 55 and 41), but clusters left over
-// start when the rest is done (5012 x 128 x 12544: 40 clusters of 6 CTAs 29.6
-// us, of 7, more than fit, 45.8, of 4 33.2).
+// 23.9 and 19.9 us with one input set over and over, 5012 x 160 x 12544 55 and
+// 42), but clusters left over start when the rest is done (5012 x 128 x 12544:
+// 40 clusters of 6 CTAs 29.8 us, of 7, more than fit, 45.8, of 4 33.2).
 //
 // How many clusters fit does not follow from the SM count, as one lies within
 // a part of the device.  max_clusters(size, &n) asks the device, whose answer

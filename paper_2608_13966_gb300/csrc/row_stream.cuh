@@ -9,7 +9,7 @@
 //
 // A row is not kept in shared memory between passes: that ties its bytes to a
 // chain of reductions and barriers, and with at most 228 KB an SM the copies
-// wait for it (the 4096 x 131072 distillation took 457 us that way, 371 so).
+// wait for it (the 4096 x 131072 distillation took 457 us that way, 372 so).
 // A second pass finds most of the row in L2.
 #pragma once
 
