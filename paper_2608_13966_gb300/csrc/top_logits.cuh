@@ -23,10 +23,10 @@
 //
 // Bound by instructions, some 11 an element at 2.6 a cycle: the top 64 of 2048
 // x 131072 bf16 rows with their log-sum-exps take 125 us, 4.3 TB/s.  The 256 of
-// 4096 x 8184 take 186 us, the 128 (128 threads a CTA) 122.  Where a row is
-// settled by bisection that is what its call waits for: of 2048 x 131072 fp32
-// rows of normal values one or two put more aside than the lists hold, and the
-// call takes 699 us.
+// 4096 x 8184 take 186 us, the 128 (128 threads a CTA) 122.  A row that is
+// settled by bisection is what its call waits for: 2048 x 131072 fp32 rows of
+// normal values take 209 us, and 755 in the batches, about every second, where
+// one or two of them put more aside than the lists hold.
 #pragma once
 
 #include "row_stream.cuh"
