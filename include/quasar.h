@@ -580,6 +580,87 @@ quasar_status quasar_distill_top_backward(const void* logits, quasar_dtype dtype
                                           quasar_stream_t stream);
 
 /*
+ * The layers between the products: embedding, layer norm and attention, with
+ * their gradients.  The conventions of the operators above hold: row-major
+ * matrices with a row stride, rows that may start anywhere unless said
+ * otherwise, fp32 sums and statistics, one rounding of an output of fewer
+ * bits, and sums in a fixed order (the same inputs give the same bits).  Calls
+ * that need scratch memory say how much in a call of their own; it is the
+ * caller's, 16-byte aligned, holds nothing before or after, and must not be
+ * used by another call until this one's work is done (calls on one stream may
+ * share it).
+ */
+
+typedef enum { QUASAR_I32 = 0, QUASAR_I64 = 1 } quasar_index_type;
+
+/*
+ * quasar_embedding -- y[t] = scale table[ids[t]] + residual[t].
+ *
+ *   ids       [tokens] int32 or int64 (ids_type).  One outside [0, vocab)
+ *             takes zeros for its row (padding).
+ *   table     [vocab, width] bf16 or fp32.
+ *   residual  [tokens, width] of y's dtype, or NULL; it may be y itself.
+ *   y         [tokens, width], dtype y_dtype (written).
+ */
+quasar_status quasar_embedding(const void* ids, quasar_index_type ids_type, int64_t tokens, const void* table,
+                               quasar_dtype table_dtype, int64_t ld_table, int64_t vocab, int64_t width, float scale,
+                               const void* residual, int64_t ld_residual, void* y, quasar_dtype y_dtype, int64_t ld_y,
+                               quasar_stream_t stream);
+
+/*
+ * quasar_embedding_backward -- dtable[v] = scale times the sum of the rows of
+ * dy (bf16 or fp32 [tokens, width]) whose id is v: the g of the reconstruction
+ * entry points.  Every row of dtable ([vocab, width], dtype dtable_dtype) is
+ * written, with zeros where no token has its id; with accumulate 1 the sums are
+ * added to what it holds, and rows without tokens are not touched.  Ids outside
+ * [0, vocab) count nowhere.
+ */
+quasar_status quasar_embedding_backward_workspace(int64_t tokens, int64_t width, int64_t* bytes);
+quasar_status quasar_embedding_backward(const void* dy, quasar_dtype dy_dtype, int64_t ld_dy, const void* ids,
+                                        quasar_index_type ids_type, int64_t tokens, int64_t vocab, int64_t width,
+                                        float scale, void* dtable, quasar_dtype dtable_dtype, int64_t ld_dtable,
+                                        int accumulate, void* workspace, int64_t workspace_bytes,
+                                        quasar_stream_t stream);
+
+/*
+ * quasar_layer_norm -- y = (x - mean) rstd weight + bias for each row, with
+ * rstd = (mean((x - mean)^2) + eps)^-1/2.  With center 0 the mean is taken as
+ * 0 (the root-mean-square norm).
+ *
+ *   x         [rows, cols] bf16 or fp32.
+ *   weight, bias  [cols] fp32; NULL: 1 and 0.
+ *   eps       finite, at least 0.  (A row without variance and eps 0 give NaN.)
+ *   y         [rows, cols], dtype y_dtype (written); it may be x itself (same
+ *             pointer, stride and dtype).
+ *   stats     [rows, 2] fp32: mean and rstd, for the backward call; or NULL.
+ * rows 0 is a no-op; cols 0 with rows is INVALID_ARG.
+ */
+quasar_status quasar_layer_norm(const void* x, quasar_dtype x_dtype, int64_t ld_x, const float* weight,
+                                const float* bias, int64_t rows, int64_t cols, int center, float eps, void* y,
+                                quasar_dtype y_dtype, int64_t ld_y, float* stats, quasar_stream_t stream);
+
+/*
+ * quasar_layer_norm_backward -- from dy (bf16 or fp32 [rows, cols]), x and the
+ * forward call's stats, with xh = (x - mean) rstd and u = dy weight:
+ *
+ *   dx       rstd (u - mean(u) - xh mean(u xh)) + residual (without mean(u)
+ *            where center is 0), dtype dx_dtype, or NULL; it may be dy, x or
+ *            the residual itself (same pointer, stride and dtype).
+ *   residual [rows, cols] of dx's dtype: the gradient that goes around the
+ *            layer, or NULL.
+ *   dweight  [cols] fp32: the sum over the rows of dy xh, or NULL.
+ *   dbias    [cols] fp32: the sum over the rows of dy, or NULL.
+ * rows 0 gives dweight and dbias of zeros.
+ */
+quasar_status quasar_layer_norm_backward_workspace(int64_t rows, int64_t cols, int64_t* bytes);
+quasar_status quasar_layer_norm_backward(const void* dy, quasar_dtype dy_dtype, int64_t ld_dy, const void* x,
+                                         quasar_dtype x_dtype, int64_t ld_x, const float* weight, const float* stats,
+                                         int64_t rows, int64_t cols, int center, const void* residual,
+                                         int64_t ld_residual, void* dx, quasar_dtype dx_dtype, int64_t ld_dx,
+                                         float* dweight, float* dbias, void* workspace, int64_t workspace_bytes,
+                                         quasar_stream_t stream);
+
+/*
  * quasar_get_device_status -- synchronises `stream`, then returns
  * QUASAR_ERR_TIMEOUT if any kernel of this library on the current device
  * recorded a timed-out wait since the previous query (and clears the record),

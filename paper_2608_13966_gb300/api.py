@@ -19,7 +19,9 @@ from .quasar import (ACTIVATIONS, BF16, F32, QuasarError, QuasarStatus, adamw_nv
                      quasar_recon_nvfp4, quasar_recon_nvfp4_batch_ex, quasar_tensor_amax,
                      quasar_activation_grad, quasar_distill_top, quasar_distill_top_backward,
                      quasar_linear, quasar_linear_grad_input, quasar_linear_grad_weight,
-                     quasar_top_logits)
+                     quasar_top_logits, I32, I64, quasar_embedding, quasar_embedding_backward,
+                     quasar_embedding_backward_workspace, quasar_layer_norm,
+                     quasar_layer_norm_backward, quasar_layer_norm_backward_workspace)
 
 
 def _check(st):
@@ -587,4 +589,143 @@ def distill_top_backward(logits, indices, values, stats, row_weight, *, teacher_
     _check(quasar_distill_top_backward(logits, _CODES[logits.dtype], ld, rows, vocab, indices,
                                        values, k, teacher_lse, stats, row_weight, temperature, out,
                                        ld_out))
+    return out
+
+
+# -- the layers between the products ---------------------------------------------
+
+_ID_CODES = {torch.int32: I32, torch.int64: I64}
+
+
+def _scratch(n, device):
+    """The workspace of one call (allocated for it, on the stream it runs on)."""
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def _ids(t, on=None):
+    """The number of a call's tokens and the code of their type."""
+    at = t.get_device()
+    if len(t.shape) != 1 or t.dtype not in _ID_CODES or at < 0 or not t.is_contiguous():
+        raise ValueError("ids must be a contiguous int32 or int64 CUDA tensor [tokens]")
+    if on is not None and at != on:
+        raise _elsewhere("ids", at, on)
+    return t.shape[0], _ID_CODES[t.dtype]
+
+
+def embedding(ids, table, *, scale=1.0, residual=None, out_dtype=torch.bfloat16, stream=None):
+    """y[t] = scale * table[ids[t]] + residual[t].
+
+    ids: int32 or int64 [tokens], one outside the table takes zeros (padding);
+    table: bf16 or fp32 [vocab, width]; residual: [tokens, width] of out_dtype
+    (positions, for one).  Returns y."""
+    if stream is not None:
+        return _on(stream, embedding, ids, table, scale=scale, residual=residual,
+                   out_dtype=out_dtype)
+    tokens, ids_code = _ids(ids)
+    on = ids.get_device()
+    vocab, width, ld = _matrix(table, "table", _FLOATS, on)
+    code = _float_code(out_dtype, "out_dtype")
+    ld_res = 0 if residual is None else _like(residual, "residual", tokens, width, (out_dtype,), on)
+    _current(on)
+    y = torch.empty((tokens, width), dtype=out_dtype, device=ids.device)
+    _check(quasar_embedding(ids, ids_code, tokens, table, _CODES[table.dtype], ld, vocab, width,
+                            scale, residual, ld_res, y, code, width))
+    return y
+
+
+def embedding_backward(dy, ids, vocab, *, scale=1.0, dtable_dtype=torch.bfloat16, into=None,
+                       stream=None):
+    """The table's gradient from dy (bf16 or fp32 [tokens, width]): scale times
+    the sum of the rows that share an id, every row of [vocab, width] written.
+    With ``into`` (bf16 or fp32 [vocab, width], a gradient of the same table)
+    the sums are added to it, and rows without tokens are not touched.  Returns
+    the gradient: the g that a reconstruction reads."""
+    if stream is not None:
+        return _on(stream, embedding_backward, dy, ids, vocab, scale=scale,
+                   dtable_dtype=dtable_dtype, into=into)
+    tokens, width, ld_dy = _matrix(dy, "dy", _FLOATS)
+    on = dy.get_device()
+    n, ids_code = _ids(ids, on)
+    if n != tokens:
+        raise ValueError(f"dy has {tokens} tokens, ids {n}")
+    if into is None:
+        code = _float_code(dtable_dtype, "dtable_dtype")
+    else:
+        ld = _like(into, "into", vocab, width, _FLOATS, on)
+        code = _CODES[into.dtype]
+    _current(on)
+    if into is None:
+        out, ld = torch.empty((vocab, width), dtype=dtable_dtype, device=dy.device), width
+    else:
+        out = into
+    need = quasar_embedding_backward_workspace(tokens, width)
+    _check(quasar_embedding_backward(dy, _CODES[dy.dtype], ld_dy, ids, ids_code, tokens, vocab,
+                                     width, scale, out, code, ld, int(into is not None),
+                                     _scratch(need, dy.device), need))
+    return out
+
+
+def layer_norm(x, weight=None, *, bias=None, center=True, eps=1e-5, out_dtype=torch.bfloat16,
+               stats=False, stream=None):
+    """y = (x - mean) rstd weight + bias over each row of x (bf16 or fp32 [rows,
+    cols]), with rstd = (mean((x - mean)^2) + eps)^-1/2; center=False: the mean is
+    taken as 0 (the root-mean-square norm).  weight, bias: fp32 [cols].  Returns
+    a dict with y and, with stats, the rows' mean and rstd (fp32 [rows, 2])."""
+    if stream is not None:
+        return _on(stream, layer_norm, x, weight, bias=bias, center=center, eps=eps,
+                   out_dtype=out_dtype, stats=stats)
+    rows, cols, ld = _matrix(x, "x", _FLOATS)
+    on = x.get_device()
+    code = _float_code(out_dtype, "out_dtype")
+    if weight is not None:
+        _vector(weight, "weight", cols, on)
+    if bias is not None:
+        _vector(bias, "bias", cols, on)
+    _current(on)
+    y = torch.empty((rows, cols), dtype=out_dtype, device=x.device)
+    out, kept = {"y": y}, None
+    if stats:
+        out["stats"] = kept = torch.empty((rows, 2), dtype=torch.float32, device=x.device)
+    _check(quasar_layer_norm(x, _CODES[x.dtype], ld, weight, bias, rows, cols, int(bool(center)), eps,
+                             y, code, cols, kept))
+    return out
+
+
+def layer_norm_backward(dy, x, weight, stats, *, center=True, dx=True, dweight=True, dbias=False,
+                        residual=None, dx_dtype=torch.bfloat16, stream=None):
+    """Gradients of ``layer_norm`` from dy (bf16 or fp32 [rows, cols]) and the
+    statistics it kept.  residual (of dx_dtype): the gradient that goes around
+    the layer, added to dx.  Returns a dict of dx, dweight and dbias (fp32
+    [cols]), those asked for; weight None: it was 1."""
+    if stream is not None:
+        return _on(stream, layer_norm_backward, dy, x, weight, stats, center=center, dx=dx,
+                   dweight=dweight, dbias=dbias, residual=residual, dx_dtype=dx_dtype)
+    rows, cols, ld_dy = _matrix(dy, "dy", _FLOATS)
+    on = dy.get_device()
+    ld_x = _like(x, "x", rows, cols, _FLOATS, on)
+    if weight is not None:
+        _vector(weight, "weight", cols, on)
+    _like(stats, "stats", rows, 2, (torch.float32,), on)
+    if not stats.is_contiguous():
+        raise ValueError("stats must be contiguous")
+    code = _float_code(dx_dtype, "dx_dtype")
+    if residual is not None and not dx:
+        raise ValueError("a residual is added to dx: it goes with dx=True")
+    ld_res = 0 if residual is None else _like(residual, "residual", rows, cols, (dx_dtype,), on)
+    _current(on)
+    device, out = dy.device, {}
+    to = dw = db = scratch = None
+    need = 0
+    if dx:
+        out["dx"] = to = torch.empty((rows, cols), dtype=dx_dtype, device=device)
+    if dweight:
+        out["dweight"] = dw = torch.empty(cols, dtype=torch.float32, device=device)
+    if dbias:
+        out["dbias"] = db = torch.empty(cols, dtype=torch.float32, device=device)
+    if dweight or dbias:
+        need = quasar_layer_norm_backward_workspace(rows, cols)
+        scratch = _scratch(need, device)
+    _check(quasar_layer_norm_backward(dy, _CODES[dy.dtype], ld_dy, x, _CODES[x.dtype], ld_x, weight,
+                                      stats, rows, cols, int(bool(center)), residual, ld_res, to, code,
+                                      cols, dw, db, scratch, need))
     return out

@@ -41,6 +41,9 @@ UNITS = [
     ("kernels_linear.cu", [], "kernels_linear.o"),
     ("kernels_linear_tile.cu", [], "kernels_linear_tile.o"),
     ("kernels_logits.cu", [], "kernels_logits.o"),
+    ("layers_abi.cu", [], "layers_abi.o"),
+    ("kernels_norm.cu", [], "kernels_norm.o"),
+    ("kernels_embedding.cu", [], "kernels_embedding.o"),
 ]
 
 

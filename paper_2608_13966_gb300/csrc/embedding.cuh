@@ -1,0 +1,294 @@
+// Embedding: rows of a table by token, and the table's gradient.
+//
+//   y[t] = scale table[id_t] + residual[t]
+//   dtable[v] = scale sum over the t with id_t = v of dy[t]
+//
+// The gradient's sums have one order, whatever the timing: the tokens are
+// sorted by id (stable, so a row's tokens stay in their order), every whole
+// chunk of 128 sorted tokens that share an id is summed first (a frequent
+// token's rows are then spread over the device), and each row of the table
+// adds up its tokens' rows and chunks.  A table's row without tokens is
+// written with zeros by the CTA that it belongs to: no pass clears the table
+// first.
+#pragma once
+
+#include "cluster.cuh"
+#include "layers.h"
+#include "row_access.cuh"
+
+namespace quasar {
+
+// Token t's row of the table, or -1.
+__device__ __forceinline__ int64_t id_at(const void* ids, int wide, int64_t t, int64_t vocab)
+{
+    const int64_t id = wide ? static_cast<const long long*>(ids)[t] : static_cast<const int*>(ids)[t];
+    return id >= 0 && id < vocab ? id : -1;
+}
+
+// 4 tokens and 2,048 columns a CTA, so that four rows are on their way at once.
+template <bool VECTORS>
+__global__ void __launch_bounds__(kEmbedThreads) k_embedding(const __grid_constant__ EmbedParams p)
+{
+    wait_for_previous_grid();
+    const int64_t t0 = (int64_t)blockIdx.x * kEmbedTokens;
+    const int64_t c0 = (int64_t)blockIdx.y * kEmbedCols, cols = p.width - c0 < kEmbedCols ? p.width - c0 : kEmbedCols;
+    Raw8<true> raw[kEmbedTokens], res[kEmbedTokens];
+#pragma unroll
+    for (int q = 0; q < kEmbedTokens; ++q) {
+        const int64_t id = t0 + q < p.tokens ? id_at(p.ids, p.ids_64, t0 + q, p.vocab) : -1;
+        load_raw<kEmbedThreads, VECTORS>(
+            raw[q], static_cast<const uint8_t*>(row_of(p.table, p.table_f32, id < 0 ? 0 : id, p.ld_table)) + c0 * (p.table_f32 ? 4 : 2),
+            p.table_f32, threadIdx.x, 0, id < 0 ? 0 : cols);
+        if (p.residual)
+            load_raw<kEmbedThreads, VECTORS>(
+                res[q], static_cast<const uint8_t*>(row_of(p.residual, p.y_f32, t0 + q, p.ld_res)) + c0 * (p.y_f32 ? 4 : 2),
+                p.y_f32, threadIdx.x, 0, t0 + q < p.tokens ? cols : 0);
+    }
+#pragma unroll
+    for (int q = 0; q < kEmbedTokens; ++q) {
+        if (t0 + q >= p.tokens) break;
+        float v[8], r[8];
+        unpack_raw(raw[q], p.table_f32, v);
+        if (p.residual) {
+            unpack_raw(res[q], p.y_f32, r);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r[i] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = fmaf(p.scale, v[i], r[i]);
+        store_row<kEmbedThreads, VECTORS>(
+            static_cast<uint8_t*>(row_of(p.y, p.y_f32, t0 + q, p.ld_y)) + c0 * (p.y_f32 ? 4 : 2), p.y_f32,
+            threadIdx.x, 0, cols, v);
+    }
+}
+
+// -- the tokens' order -------------------------------------------------------------
+
+// Stable sort of (id, place) by id, 9 bits a pass from the lowest, by one
+// cluster in one launch.  A warp keeps a contiguous share of the list; the
+// rank of an entry is what lies before its bin, before its CTA, before its
+// warp and before it in its warp.  (n is small beside the rows it sorts: a
+// token's row of 4096 is 8 KB, its entry 8 bytes a pass.)
+__global__ void __launch_bounds__(kSortThreads) k_sort_ids(const __grid_constant__ SortParams p)
+{
+    constexpr int kBins = 1 << kSortBits, kWarps = kSortThreads / 32;
+    extern __shared__ uint8_t smem_raw[];
+    uint32_t* count = reinterpret_cast<uint32_t*>(smem_raw);  // [warps][bins]
+    uint32_t* total = count + kWarps * kBins;                 // [bins], read by the cluster
+    uint32_t* scan = total + kBins;                           // [kBins / 32]
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = p.ctas > 1 ? (int)cluster_rank() : 0;
+    const int64_t gw = rank * kWarps + warp, all = (int64_t)p.ctas * kWarps;
+    const int from = (int)(p.n * gw / all), to = (int)(p.n * (gw + 1) / all);
+    uint32_t* mine = count + warp * kBins;
+    wait_for_previous_grid();
+
+    for (int pass = 0; pass < p.passes; ++pass) {
+        const int shift = pass * kSortBits;
+        const int in = (p.passes - pass) & 1, out = in ^ 1;  // (the last pass writes to 0)
+        auto load = [&](int i, uint32_t& key, uint32_t& place) {
+            key = 0, place = (uint32_t)i;
+            if (i >= to) return;
+            if (pass == 0) {
+                const int64_t id = id_at(p.ids, p.ids_64, i, p.vocab);
+                key = (uint32_t)(id < 0 ? p.vocab : id);
+            } else {
+                key = __ldcg(p.keys[in] + i);
+                place = __ldcg(p.places[in] + i);
+            }
+        };
+        for (int b = threadIdx.x; b < kWarps * kBins; b += kSortThreads) count[b] = 0;
+        __syncthreads();
+        for (int i0 = from; i0 < to; i0 += 128) {
+            uint32_t key[4], place[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) load(i0 + 32 * q + lane, key[q], place[q]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const bool live = i0 + 32 * q + lane < to;
+                const uint32_t digit = live ? key[q] >> shift & (kBins - 1) : kBins;
+                const uint32_t same = __match_any_sync(0xffffffffu, digit);
+                if (live && (same & ((1u << lane) - 1)) == 0) mine[digit] += __popc(same);
+                __syncwarp();
+            }
+        }
+        __syncthreads();
+        if (threadIdx.x < kBins) {
+            uint32_t s = 0;
+            for (int w = 0; w < kWarps; ++w) {
+                const uint32_t c = count[w * kBins + threadIdx.x];
+                count[w * kBins + threadIdx.x] = s;
+                s += c;
+            }
+            total[threadIdx.x] = s;
+        }
+        __syncthreads();
+        if (p.ctas > 1) cluster_sync();
+        uint32_t bin = 0, before = 0;  // this bin's entries: all, and in the CTAs before
+        if (threadIdx.x < kBins) {
+            for (int c = 0; c < p.ctas; ++c) {
+                uint32_t n = total[threadIdx.x];
+                if (p.ctas > 1)
+                    asm volatile("ld.shared::cluster.u32 %0, [%1];"
+                                 : "=r"(n)
+                                 : "r"(peer_addr(smem_u32(total + threadIdx.x), (uint32_t)c))
+                                 : "memory");
+                bin += n;
+                if (c < rank) before += n;
+            }
+        }
+        uint32_t upto = bin;  // inclusive sum over the bins
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
+        }
+        if (threadIdx.x < kBins && lane == 31) scan[warp] = upto;
+        __syncthreads();
+        if (threadIdx.x < kBins) {
+            uint32_t base = upto - bin + before;
+            for (int w = 0; w < warp; ++w) base += scan[w];
+            for (int w = 0; w < kWarps; ++w) count[w * kBins + threadIdx.x] += base;
+        }
+        __syncthreads();
+        for (int i0 = from; i0 < to; i0 += 128) {
+            uint32_t key[4], place[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) load(i0 + 32 * q + lane, key[q], place[q]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const bool live = i0 + 32 * q + lane < to;
+                const uint32_t digit = live ? key[q] >> shift & (kBins - 1) : kBins;
+                const uint32_t same = __match_any_sync(0xffffffffu, digit);
+                const uint32_t earlier = __popc(same & ((1u << lane) - 1));
+                const uint32_t at = live ? mine[digit] + earlier : 0;
+                __syncwarp();
+                if (live) {
+                    if (earlier == 0) mine[digit] += __popc(same);
+                    p.keys[out][at] = key[q];
+                    p.places[out][at] = place[q];
+                }
+                __syncwarp();
+            }
+        }
+        // the next pass reads what the other CTAs wrote (from L2)
+        __threadfence();
+        __syncthreads();
+        if (p.ctas > 1) cluster_sync();
+    }
+}
+
+// -- the gradient ------------------------------------------------------------------
+
+// Sums of whole chunks of sorted tokens that share an id.
+template <bool VECTORS>
+__global__ void __launch_bounds__(kEmbedThreads) k_embedding_chunks(const __grid_constant__ EmbedGradParams p)
+{
+    wait_for_previous_grid();
+    const int i0 = (int)blockIdx.x * kRunChunk;
+    const uint32_t id = p.keys[i0];
+    if (id >= p.vocab || id != p.keys[i0 + kRunChunk - 1]) return;
+    const int64_t c0 = (int64_t)blockIdx.y * kEmbedCols, cols = p.width - c0 < kEmbedCols ? p.width - c0 : kEmbedCols;
+    float sum[8] = {};
+#pragma unroll 1
+    for (int i = 0; i < kRunChunk; i += 8) {
+        Raw8<true> raw[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            load_raw<kEmbedThreads, VECTORS>(
+                raw[q], static_cast<const uint8_t*>(row_of(p.dy, p.dy_f32, p.places[i0 + i + q], p.ld_dy)) + c0 * (p.dy_f32 ? 4 : 2),
+                p.dy_f32, threadIdx.x, 0, cols);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            float v[8];
+            unpack_raw(raw[q], p.dy_f32, v);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) sum[x] += v[x];
+        }
+    }
+    float* to = p.sums + (int64_t)blockIdx.x * p.width + c0;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+        const int64_t c = row_at<kEmbedThreads, VECTORS>(threadIdx.x, 0, x);
+        if (c < cols) to[c] = sum[x];
+    }
+}
+
+// First of the sorted keys in [from, to) that is not below `key`.
+__device__ __forceinline__ int lower_bound(const uint32_t* keys, int from, int to, uint32_t key)
+{
+    while (from < to) {
+        const int mid = from + (to - from) / 2;
+        if (keys[mid] < key)
+            from = mid + 1;
+        else
+            to = mid;
+    }
+    return from;
+}
+
+// kEmbedRows rows of the table by 2,048 columns a CTA.  Bound by writing the
+// table's gradient.
+template <bool VECTORS>
+__global__ void __launch_bounds__(kEmbedThreads) k_embedding_grad(const __grid_constant__ EmbedGradParams p)
+{
+    __shared__ int ends[kEmbedRows + 1];  // where each row's tokens start
+    wait_for_previous_grid();
+    const int64_t v0 = (int64_t)blockIdx.x * kEmbedRows;
+    const int rows = (int)(p.vocab - v0 < kEmbedRows ? p.vocab - v0 : kEmbedRows);
+    const int64_t c0 = (int64_t)blockIdx.y * kEmbedCols, cols = p.width - c0 < kEmbedCols ? p.width - c0 : kEmbedCols;
+    if (threadIdx.x <= rows) ends[threadIdx.x] = lower_bound(p.keys, 0, p.n, (uint32_t)(v0 + threadIdx.x));
+    __syncthreads();
+    if (p.add && ends[0] == ends[rows]) return;
+    const int64_t dy_at = c0 * (p.dy_f32 ? 4 : 2);
+    for (int r = 0; r < rows; ++r) {
+        int i = ends[r];
+        const int end = ends[r + 1];
+        void* row = static_cast<uint8_t*>(row_of(p.dtable, p.f32, v0 + r, p.ld)) + c0 * (p.f32 ? 4 : 2);
+        if (p.add && i == end) continue;
+        float sum[8] = {};
+        while (i < end) {
+            if (i % kRunChunk == 0 && i + kRunChunk <= end) {
+                float v[8];
+                load_floats<kEmbedThreads, VECTORS>(v, p.sums + (int64_t)(i / kRunChunk) * p.width + c0, threadIdx.x, 0,
+                                                    cols, 0.0f);
+#pragma unroll
+                for (int x = 0; x < 8; ++x) sum[x] += v[x];
+                i += kRunChunk;
+                continue;
+            }
+            // up to the next chunk, four rows on their way at once
+            const int stop = min(end, (i / kRunChunk + 1) * kRunChunk);
+            for (; i < stop; i += 4) {
+                Raw8<true> raw[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    load_raw<kEmbedThreads, VECTORS>(
+                        raw[q], static_cast<const uint8_t*>(row_of(p.dy, p.dy_f32, i + q < stop ? p.places[i + q] : 0, p.ld_dy)) + dy_at,
+                        p.dy_f32, threadIdx.x, 0, i + q < stop ? cols : 0);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float v[8];
+                    unpack_raw(raw[q], p.dy_f32, v);
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) sum[x] += v[x];
+                }
+            }
+            i = stop;
+        }
+#pragma unroll
+        for (int x = 0; x < 8; ++x) sum[x] *= p.scale;
+        if (p.add) {
+            Raw8<true> raw;
+            float v[8];
+            load_raw<kEmbedThreads, VECTORS>(raw, row, p.f32, threadIdx.x, 0, cols);
+            unpack_raw(raw, p.f32, v);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) sum[x] += v[x];
+        }
+        store_row<kEmbedThreads, VECTORS>(row, p.f32, threadIdx.x, 0, cols, sum);
+    }
+}
+
+}  // namespace quasar

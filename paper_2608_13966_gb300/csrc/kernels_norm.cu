@@ -1,0 +1,76 @@
+// Instantiations of the layer norms.
+#include "layer_norm.cuh"
+
+namespace quasar {
+
+namespace {
+
+struct Shape {
+    int t, nv;  // threads a row, vectors of 8 a thread
+};
+
+// Short rows share a CTA of 256 threads; from 129 vectors on a row has a CTA.
+Shape norm_shape(int64_t cols)
+{
+    const int64_t vecs = (cols + 7) / 8;
+    if (vecs <= 8) return {8, 1};
+    if (vecs <= 16) return {8, 2};
+    if (vecs <= 32) return {32, 1};
+    if (vecs <= 64) return {32, 2};
+    if (vecs <= 128) return {32, 4};
+    if (vecs <= 256) return {256, 1};
+    if (vecs <= 512) return {512, 1};
+    if (vecs <= 1024) return {512, 2};
+    return {512, 4};
+}
+
+template <int T, int NV>
+const void* forward(bool vectors)
+{
+    return vectors ? reinterpret_cast<const void*>(&k_layer_norm<T, NV, true>)
+                   : reinterpret_cast<const void*>(&k_layer_norm<T, NV, false>);
+}
+
+template <int T, int NV>
+const void* backward(bool vectors, bool wide)
+{
+    if (vectors)
+        return wide ? reinterpret_cast<const void*>(&k_layer_norm_grad<T, NV, true, true>)
+                    : reinterpret_cast<const void*>(&k_layer_norm_grad<T, NV, true, false>);
+    return wide ? reinterpret_cast<const void*>(&k_layer_norm_grad<T, NV, false, true>)
+                : reinterpret_cast<const void*>(&k_layer_norm_grad<T, NV, false, false>);
+}
+
+}  // namespace
+
+// The kernel of rows of this length (backward: of their gradients), its
+// threads, how many rows a CTA takes at a time and how many CTAs an SM holds;
+// nullptr for rows that registers do not hold.
+const void* layer_norm_kernel(int64_t cols, bool vectors, bool grad, bool wide, int* threads, int* rows, int* per_sm)
+{
+    if (cols > kNormMostCols) return nullptr;
+    const Shape s = norm_shape(cols);
+    *threads = s.t < 256 ? 256 : s.t;
+    *rows = *threads / s.t;
+    *per_sm = s.nv == 1 ? 1024 / *threads : 512 / *threads;
+#define QUASAR_NORM(T, NV) \
+    if (s.t == T && s.nv == NV) return grad ? backward<T, NV>(vectors, wide) : forward<T, NV>(vectors);
+    QUASAR_NORM(8, 1)
+    QUASAR_NORM(8, 2)
+    QUASAR_NORM(32, 1)
+    QUASAR_NORM(32, 2)
+    QUASAR_NORM(32, 4)
+    QUASAR_NORM(256, 1)
+    QUASAR_NORM(512, 1)
+    QUASAR_NORM(512, 2)
+    QUASAR_NORM(512, 4)
+#undef QUASAR_NORM
+    return nullptr;
+}
+
+const void* layer_norm_long_kernel() { return reinterpret_cast<const void*>(&k_layer_norm_long); }
+const void* layer_norm_grad_long_kernel() { return reinterpret_cast<const void*>(&k_layer_norm_grad_long); }
+const void* layer_norm_grad_columns_kernel() { return reinterpret_cast<const void*>(&k_layer_norm_grad_columns); }
+const void* part_sum_kernel() { return reinterpret_cast<const void*>(&k_part_sum); }
+
+}  // namespace quasar

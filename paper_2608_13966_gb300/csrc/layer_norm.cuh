@@ -1,0 +1,370 @@
+// Layer normalisation and its gradients.
+//
+//   y = (x - mean) rstd w + b,   rstd = (mean((x - mean)^2) + eps)^-1/2
+//   (not centered: mean = 0 throughout, the root-mean-square norm)
+//
+//   xh = (x - mean) rstd,  u = dy w
+//   dx = rstd (u - mean(u) - xh mean(u xh)) + residual
+//   dw = sum over rows of dy xh,  db = sum over rows of dy
+//
+// Bound by memory: a row is read once and kept in registers.  T threads share
+// a row, NV times 8 elements each; 8 or 32 threads where rows are short (a CTA
+// then takes 32 or 8 of them at a time), a whole CTA else.  CTAs are
+// persistent, so that a thread's columns stay the same: their weights are read
+// once, and dw and db accumulate in registers over the CTA's rows.  The next
+// row is on its way while one is worked on.
+//
+// The variance is summed about the mean: of each warp's elements about their
+// own mean, the warps' then joined (M2 = sum M2_w + n_w (mean_w - mean)^2),
+// which takes one exchange through shared memory instead of two.
+#pragma once
+
+#include "layers.h"
+#include "row_access.cuh"
+
+namespace quasar {
+
+template <int T>
+constexpr int kNormThreads = T < 256 ? 256 : T;
+
+// Sum over the W (at most 32) threads of an aligned part of a warp.
+template <int W>
+__device__ __forceinline__ float lanes_sum(float x)
+{
+#pragma unroll
+    for (int o = W / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+
+// -- forward ---------------------------------------------------------------------
+
+// 16384 x 4096 bf16 with weight and bias: see the figures at the launch.
+template <int T, int NV, bool VECTORS>
+__global__ void __launch_bounds__(kNormThreads<T>, NV == 1 ? 1024 / kNormThreads<T> : 512 / kNormThreads<T>)
+    k_layer_norm(const __grid_constant__ NormParams p)
+{
+    constexpr int kGroups = kNormThreads<T> / T, kWarps = T / 32, kLanes = T < 32 ? T : 32;
+    __shared__ float2 red[2][T > 32 ? kWarps : 1];
+    __shared__ float counts[T > 32 ? kWarps : 1];
+    const int t = threadIdx.x % T, lane = threadIdx.x & 31;
+    const bool whole = p.cols == (int64_t)T * NV * 8;
+    const float cols = (float)p.cols;
+
+    float mine = 0.0f;  // this warp's elements (its part of the row)
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mine += row_at<T, VECTORS>(t, j, i) < p.cols ? 1.0f : 0.0f;
+    mine = lanes_sum<kLanes>(mine);
+    if (T > 32 && lane == 0) counts[threadIdx.x >> 5] = mine;
+    wait_for_previous_grid();
+
+    float w[NV][8], b[NV][8];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        load_floats<T, VECTORS>(w[j], p.weight, t, j, p.cols, 1.0f);
+        load_floats<T, VECTORS>(b[j], p.bias, t, j, p.cols, 0.0f);
+    }
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    int64_t row = (int64_t)blockIdx.x * kGroups + threadIdx.x / T;
+    Raw8<true> raw[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        load_raw<T, VECTORS>(raw[j], row_of(p.x, p.x_f32, row, p.ld_x), p.x_f32, t, j, row < p.rows ? p.cols : 0);
+    int turn = 0;
+    for (int64_t first = (int64_t)blockIdx.x * kGroups; first < p.rows; first += step, row += step, turn ^= 1) {
+        float v[NV][8];
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            unpack_raw(raw[j], p.x_f32, v[j]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[j][i];
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            load_raw<T, VECTORS>(raw[j], row_of(p.x, p.x_f32, row + step, p.ld_x), p.x_f32, t, j,
+                                 row + step < p.rows ? p.cols : 0);
+        // (divisions: a row of one value then has no variance at all)
+        float mean = p.center && mine > 0.0f ? lanes_sum<kLanes>(sum) / mine : 0.0f;
+        float m2 = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = whole || row_at<T, VECTORS>(t, j, i) < p.cols ? v[j][i] - mean : 0.0f;
+                m2 = fmaf(d, d, m2);
+            }
+        m2 = lanes_sum<kLanes>(m2);
+        if constexpr (T > 32) {
+            if (lane == 0) red[turn][threadIdx.x >> 5] = make_float2(mean, m2);
+            __syncthreads();
+            const float2 part = lane < kWarps ? red[turn][lane] : make_float2(0.0f, 0.0f);
+            const float n = lane < kWarps ? counts[lane] : 0.0f;
+            mean = lanes_sum<32>(n * part.x) / cols;
+            const float d = part.x - mean;
+            m2 = lanes_sum<32>(fmaf(n * d, d, part.y));
+        }
+        const float rstd = rsqrtf(m2 / cols + p.eps);
+        if (row < p.rows) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[j][i] = fmaf((v[j][i] - mean) * rstd, w[j][i], b[j][i]);
+                store_row<T, VECTORS>(row_of(p.y, p.y_f32, row, p.ld_y), p.y_f32, t, j, p.cols, v[j]);
+            }
+            if (p.stats && t == 0) {
+                p.stats[2 * row] = mean;
+                p.stats[2 * row + 1] = rstd;
+            }
+        }
+    }
+}
+
+// Sum over the CTA (512 threads), the same value in every thread.
+__device__ __forceinline__ float cta_sum(float x, float* red)
+{
+    x = lanes_sum<32>(x);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = x;
+    __syncthreads();
+    return lanes_sum<32>((threadIdx.x & 31) < 16 ? red[threadIdx.x & 31] : 0.0f);
+}
+
+__device__ __forceinline__ float element(const void* row, bool f32, int64_t c)
+{
+    return f32 ? static_cast<const float*>(row)[c] : __bfloat162float(static_cast<const __nv_bfloat16*>(row)[c]);
+}
+
+__device__ __forceinline__ void put_element(void* row, bool f32, int64_t c, float v)
+{
+    if (f32)
+        static_cast<float*>(row)[c] = v;
+    else
+        static_cast<__nv_bfloat16*>(row)[c] = __float2bfloat16_rn(v);
+}
+
+// Rows that registers do not hold: read once for the mean, once for the
+// variance and once for y (from L2, where they fit it).
+__global__ void __launch_bounds__(512) k_layer_norm_long(const __grid_constant__ NormParams p)
+{
+    __shared__ float red[16];
+    wait_for_previous_grid();
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        const void* x = row_of(p.x, p.x_f32, row, p.ld_x);
+        const float cols = (float)p.cols;
+        float mean = 0.0f;
+        if (p.center) {
+            float s = 0.0f;
+#pragma unroll 4
+            for (int64_t c = threadIdx.x; c < p.cols; c += 512) s += element(x, p.x_f32, c);
+            mean = cta_sum(s, red) / cols;
+        }
+        float s = 0.0f;
+#pragma unroll 4
+        for (int64_t c = threadIdx.x; c < p.cols; c += 512) {
+            const float d = element(x, p.x_f32, c) - mean;
+            s = fmaf(d, d, s);
+        }
+        const float rstd = rsqrtf(cta_sum(s, red) / cols + p.eps);
+        void* y = row_of(p.y, p.y_f32, row, p.ld_y);
+#pragma unroll 4
+        for (int64_t c = threadIdx.x; c < p.cols; c += 512)
+            put_element(y, p.y_f32, c,
+                        fmaf((element(x, p.x_f32, c) - mean) * rstd, p.weight ? p.weight[c] : 1.0f,
+                             p.bias ? p.bias[c] : 0.0f));
+        if (p.stats && threadIdx.x == 0) {
+            p.stats[2 * row] = mean;
+            p.stats[2 * row + 1] = rstd;
+        }
+    }
+}
+
+// -- backward --------------------------------------------------------------------
+
+template <int T, int NV, bool VECTORS, bool WIDE>
+__global__ void __launch_bounds__(kNormThreads<T>, NV == 1 ? 1024 / kNormThreads<T> : 512 / kNormThreads<T>)
+    k_layer_norm_grad(const __grid_constant__ NormGradParams p)
+{
+    constexpr int kGroups = kNormThreads<T> / T, kWarps = T / 32, kLanes = T < 32 ? T : 32;
+    __shared__ float2 red[2][T > 32 ? kWarps : 1];
+    __shared__ float sums[kGroups > 1 ? kGroups * T * NV * 8 : 1];
+    const int t = threadIdx.x % T, lane = threadIdx.x & 31;
+    const float per = 1.0f / (float)p.cols;
+    wait_for_previous_grid();
+
+    float w[NV][8], dw[NV][8], db[NV][8];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        load_floats<T, VECTORS>(w[j], p.weight, t, j, p.cols, 1.0f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[j][i] = db[j][i] = 0.0f;
+    }
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    int64_t row = (int64_t)blockIdx.x * kGroups + threadIdx.x / T;
+    Raw8<WIDE> raw_x[NV], raw_dy[NV];
+    float2 stat = make_float2(0.0f, 0.0f);
+    auto fetch = [&](int64_t r) {
+        const int64_t cols = r < p.rows ? p.cols : 0;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            load_raw<T, VECTORS>(raw_x[j], row_of(p.x, p.x_f32, r, p.ld_x), p.x_f32, t, j, cols);
+            load_raw<T, VECTORS>(raw_dy[j], row_of(p.dy, p.dy_f32, r, p.ld_dy), p.dy_f32, t, j, cols);
+        }
+        stat = r < p.rows ? make_float2(p.stats[2 * r], p.stats[2 * r + 1]) : make_float2(0.0f, 0.0f);
+    };
+    fetch(row);
+    int turn = 0;
+    for (int64_t first = (int64_t)blockIdx.x * kGroups; first < p.rows; first += step, row += step, turn ^= 1) {
+        const float mean = p.center ? stat.x : 0.0f, rstd = stat.y;
+        float xh[NV][8], u[NV][8];
+        float su = 0.0f, sux = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            unpack_raw(raw_x[j], p.x_f32, xh[j]);
+            unpack_raw(raw_dy[j], p.dy_f32, u[j]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                // (beyond the row: x = dy = 0, and u = 0 keeps them out of every sum)
+                xh[j][i] = (xh[j][i] - mean) * rstd;
+                dw[j][i] = fmaf(u[j][i], xh[j][i], dw[j][i]);
+                db[j][i] += u[j][i];
+                u[j][i] *= w[j][i];
+                su += u[j][i];
+                sux = fmaf(u[j][i], xh[j][i], sux);
+            }
+        }
+        fetch(row + step);
+        if (!p.dx) continue;
+        su = lanes_sum<kLanes>(su);
+        sux = lanes_sum<kLanes>(sux);
+        if constexpr (T > 32) {
+            if (lane == 0) red[turn][threadIdx.x >> 5] = make_float2(su, sux);
+            __syncthreads();
+            const float2 part = lane < kWarps ? red[turn][lane] : make_float2(0.0f, 0.0f);
+            su = lanes_sum<32>(part.x);
+            sux = lanes_sum<32>(part.y);
+        }
+        const float mu = p.center ? su * per : 0.0f, mux = sux * per;
+        if (row < p.rows) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float res[8];
+                if (p.residual) {
+                    Raw8<true> raw;
+                    load_raw<T, VECTORS>(raw, row_of(p.residual, p.dx_f32, row, p.ld_res), p.dx_f32, t, j, p.cols);
+                    unpack_raw(raw, p.dx_f32, res);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) res[i] = 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) u[j][i] = fmaf(fmaf(-xh[j][i], mux, u[j][i] - mu), rstd, res[i]);
+                store_row<T, VECTORS>(row_of(p.dx, p.dx_f32, row, p.ld_dx), p.dx_f32, t, j, p.cols, u[j]);
+            }
+        }
+    }
+    // this CTA's share of dw and db
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float* part = which ? p.part_b : p.part_w;
+        if (!part) continue;
+        float(&mine)[NV][8] = which ? db : dw;
+        part += (int64_t)blockIdx.x * p.cols;
+        if constexpr (kGroups > 1) {
+            constexpr int kSpan = T * NV * 8;
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    sums[threadIdx.x / T * kSpan + (int)row_at<T, VECTORS>(t, j, i)] = mine[j][i];
+            __syncthreads();
+            for (int c = threadIdx.x; c < p.cols; c += kNormThreads<T>) {
+                float s = sums[c];
+#pragma unroll 8
+                for (int g = 1; g < kGroups; ++g) s += sums[g * kSpan + c];
+                part[c] = s;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int64_t c = row_at<T, VECTORS>(t, j, i);
+                    if (c < p.cols) part[c] = mine[j][i];
+                }
+        }
+    }
+}
+
+// dx of rows that registers do not hold.
+__global__ void __launch_bounds__(512) k_layer_norm_grad_long(const __grid_constant__ NormGradParams p)
+{
+    __shared__ float red[16];
+    wait_for_previous_grid();
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        const void* x = row_of(p.x, p.x_f32, row, p.ld_x);
+        const void* dy = row_of(p.dy, p.dy_f32, row, p.ld_dy);
+        const float mean = p.center ? p.stats[2 * row] : 0.0f, rstd = p.stats[2 * row + 1];
+        const float per = 1.0f / (float)p.cols;
+        float su = 0.0f, sux = 0.0f;
+#pragma unroll 4
+        for (int64_t c = threadIdx.x; c < p.cols; c += 512) {
+            const float u = element(dy, p.dy_f32, c) * (p.weight ? p.weight[c] : 1.0f);
+            su += u;
+            sux = fmaf(u, (element(x, p.x_f32, c) - mean) * rstd, sux);
+        }
+        const float mu = p.center ? cta_sum(su, red) * per : 0.0f, mux = cta_sum(sux, red) * per;
+        void* dx = row_of(p.dx, p.dx_f32, row, p.ld_dx);
+#pragma unroll 4
+        for (int64_t c = threadIdx.x; c < p.cols; c += 512) {
+            const float u = element(dy, p.dy_f32, c) * (p.weight ? p.weight[c] : 1.0f);
+            const float xh = (element(x, p.x_f32, c) - mean) * rstd;
+            const float res = p.residual ? element(row_of(p.residual, p.dx_f32, row, p.ld_res), p.dx_f32, c) : 0.0f;
+            put_element(dx, p.dx_f32, c, fmaf(fmaf(-xh, mux, u - mu), rstd, res));
+        }
+    }
+}
+
+// dw and db of such rows: a column a thread, a share of the rows a CTA.
+__global__ void __launch_bounds__(256) k_layer_norm_grad_columns(const __grid_constant__ NormGradParams p)
+{
+    wait_for_previous_grid();
+    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (c >= p.cols) return;
+    float dw = 0.0f, db = 0.0f;
+#pragma unroll 4
+    for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
+        const float d = element(row_of(p.dy, p.dy_f32, row, p.ld_dy), p.dy_f32, c);
+        const float mean = p.center ? p.stats[2 * row] : 0.0f;
+        dw = fmaf(d, (element(row_of(p.x, p.x_f32, row, p.ld_x), p.x_f32, c) - mean) * p.stats[2 * row + 1], dw);
+        db += d;
+    }
+    if (p.part_w) p.part_w[(int64_t)blockIdx.y * p.cols + c] = dw;
+    if (p.part_b) p.part_b[(int64_t)blockIdx.y * p.cols + c] = db;
+}
+
+// The CTAs' shares added up, always in the same order: 32 columns a CTA, the
+// parts over its 8 warps.
+__global__ void __launch_bounds__(256) k_part_sum(const __grid_constant__ PartSumParams p)
+{
+    __shared__ float red[8][32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
+    wait_for_previous_grid();
+    const float* part = p.part[blockIdx.y];
+    float s = 0.0f;
+    if (c < p.cols) {
+#pragma unroll 8
+        for (int q = warp; q < p.parts; q += 8) s += part[q * p.cols + c];
+    }
+    red[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && c < p.cols) {
+        for (int q = 1; q < 8; ++q) s += red[q][lane];
+        p.out[blockIdx.y][c] = s;
+    }
+}
+
+}  // namespace quasar

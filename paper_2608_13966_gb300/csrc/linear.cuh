@@ -261,28 +261,6 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, const float4& x, 
     }
 }
 
-// -- waits -------------------------------------------------------------------
-
-// Wait for a phase of `bar`; gives up when limit_ns have passed or another
-// role of this CTA gave up (`*gone`), and then says so to the others.
-__device__ __forceinline__ bool role_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* gone,
-                                          uint64_t limit_ns, unsigned int* status)
-{
-    if (mbar_try_wait(bar, parity)) return true;
-    const uint64_t t0 = global_timer_ns();
-    for (;;) {
-#pragma unroll 1
-        for (int i = 0; i < 16; ++i)
-            if (mbar_try_wait(bar, parity)) return true;
-        if (*gone) return false;
-        if (global_timer_ns() - t0 > limit_ns) {
-            *gone = 1;
-            record_timeout(status);
-            return false;
-        }
-    }
-}
-
 // -- one tile per cluster ------------------------------------------------------
 
 // BN columns (tokens, for the forward product) by 128 rows per cluster, the

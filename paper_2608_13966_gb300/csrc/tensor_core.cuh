@@ -36,6 +36,16 @@ __device__ __forceinline__ void tile_g2s_pair(uint32_t dst, const CUtensorMap* m
         : "memory");
 }
 
+// 3-D tile copy: (x, y, z) from the contiguous coordinate up; x as above.
+__device__ __forceinline__ void tile_g2s_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map)
 {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
@@ -56,6 +66,13 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool mn_major)
 // Descriptor advance for the next 16 elements of K: 32 bytes along a K-major
 // row, 16 rows of 128 bytes in an MN-major block.
 __device__ __forceinline__ uint64_t k_step(bool mn_major) { return mn_major ? (2048u >> 4) : (32u >> 4); }
+
+// An MN-major tile whose blocks of 64 M or N are `rows` (of K) high.
+__device__ __forceinline__ uint64_t operand_desc_tall(uint32_t addr, uint32_t rows)
+{
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)(rows * 128u >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) |
+           (1ull << 46) | (2ull << 61);
+}
 
 // Instruction descriptor of kind::f16: bf16 operands, fp32 accumulators.
 __device__ __forceinline__ constexpr uint32_t mma_desc(int m, int n, bool a_mn, bool b_mn)
@@ -79,6 +96,17 @@ __device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uin
             "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
             "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
             : "memory");
+}
+
+// The same with A (M x 16 bf16, a row a lane, two elements a column) in tensor
+// memory.
+__device__ __forceinline__ void mma_bf16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t desc, bool add)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
+        : "memory");
 }
 
 // Arrive on `bar` when every tcgen05.mma this thread issued so far is done.
@@ -164,5 +192,74 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const float* v)
 }
 
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// 32 columns, no wait: v is defined after the next tmem_wait_ld on it.
+__device__ __forceinline__ void tmem_ld(uint32_t addr, float (&v)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
+        "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+          "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+          "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+          "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+        : "r"(addr));
+}
+
+// The loads so far are done; what v holds is used only from here on.
+__device__ __forceinline__ void tmem_wait_ld(float (&v)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]),
+      "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]),
+      "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]),
+      "+f"(v[21]), "+f"(v[22]), "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]),
+      "+f"(v[29]), "+f"(v[30]), "+f"(v[31])::"memory");
+}
+
+__device__ __forceinline__ void tmem_st(uint32_t addr, const uint32_t (&v)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
+          "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_st(uint32_t addr, const uint32_t (&v)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, "
+        "%22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(addr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
+          "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]),
+          "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]),
+          "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+        : "memory");
+}
+
+// -- waits -------------------------------------------------------------------
+
+// Wait for a phase of `bar`; gives up when limit_ns have passed or another
+// role of this CTA gave up (`*gone`), and then says so to the others.
+__device__ __forceinline__ bool role_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* gone,
+                                          uint64_t limit_ns, unsigned int* status)
+{
+    if (mbar_try_wait(bar, parity)) return true;
+    const uint64_t t0 = global_timer_ns();
+    for (;;) {
+#pragma unroll 1
+        for (int i = 0; i < 16; ++i)
+            if (mbar_try_wait(bar, parity)) return true;
+        if (*gone) return false;
+        if (global_timer_ns() - t0 > limit_ns) {
+            *gone = 1;
+            record_timeout(status);
+            return false;
+        }
+    }
+}
 
 }  // namespace quasar

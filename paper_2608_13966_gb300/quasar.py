@@ -64,6 +64,15 @@ PROTOTYPES = {
                                 _P]),
     "quasar_distill_top_backward": (_I, [_P, _I, _I64, _I64, _I64, _P, _P, _I, _P, _P, _P, _F, _P,
                                          _I64, _P]),
+    "quasar_embedding": (_I, [_P, _I, _I64, _P, _I, _I64, _I64, _I64, _F, _P, _I64, _P, _I, _I64,
+                              _P]),
+    "quasar_embedding_backward_workspace": (_I, [_I64, _I64, _P]),
+    "quasar_embedding_backward": (_I, [_P, _I, _I64, _P, _I, _I64, _I64, _I64, _F, _P, _I, _I64,
+                                       _I, _P, _I64, _P]),
+    "quasar_layer_norm": (_I, [_P, _I, _I64, _P, _P, _I64, _I64, _I, _F, _P, _I, _I64, _P, _P]),
+    "quasar_layer_norm_backward_workspace": (_I, [_I64, _I64, _P]),
+    "quasar_layer_norm_backward": (_I, [_P, _I, _I64, _P, _I, _I64, _P, _P, _I64, _I64, _I, _P,
+                                        _I64, _P, _I, _I64, _P, _P, _P, _I64, _P]),
     "quasar_get_device_status": (_I, [_P]),
     "quasar_debug_force_timeout": (None, [_I64]),
     "quasar_debug_set_stats": (None, [_P]),
@@ -462,6 +471,58 @@ def quasar_distill_top_backward(logits, dtype, ld, rows, vocab, indices, values,
     return _status((_lib or load()).quasar_distill_top_backward(
         _ptr(logits), dtype, ld, rows, vocab, _ptr(indices), _ptr(values), k, _ptr(teacher_lse),
         _ptr(stats), _ptr(row_weight), temperature, _ptr(grad), ld_grad, _stream(stream)))
+
+
+# quasar_index_type
+I32, I64 = 0, 1
+
+
+def _bytes_of(call, *sizes) -> int:
+    """What a workspace call answers."""
+    n = ctypes.c_int64()
+    st = call(*sizes, ctypes.byref(n))
+    if st:
+        raise QuasarError(st)
+    return n.value
+
+
+def quasar_embedding(ids, ids_type, tokens, table, table_dtype, ld_table, vocab, width, scale,
+                     residual, ld_residual, y, y_dtype, ld_y, stream=None) -> QuasarStatus:
+    return _status((_lib or load()).quasar_embedding(
+        _ptr(ids), ids_type, tokens, _ptr(table), table_dtype, ld_table, vocab, width, scale,
+        _ptr(residual), ld_residual, _ptr(y), y_dtype, ld_y, _stream(stream)))
+
+
+def quasar_embedding_backward_workspace(tokens, width) -> int:
+    return _bytes_of((_lib or load()).quasar_embedding_backward_workspace, tokens, width)
+
+
+def quasar_embedding_backward(dy, dy_dtype, ld_dy, ids, ids_type, tokens, vocab, width, scale,
+                              dtable, dtable_dtype, ld_dtable, accumulate, workspace,
+                              workspace_bytes, stream=None) -> QuasarStatus:
+    return _status((_lib or load()).quasar_embedding_backward(
+        _ptr(dy), dy_dtype, ld_dy, _ptr(ids), ids_type, tokens, vocab, width, scale, _ptr(dtable),
+        dtable_dtype, ld_dtable, accumulate, _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def quasar_layer_norm(x, x_dtype, ld_x, weight, bias, rows, cols, center, eps, y, y_dtype, ld_y,
+                      stats=None, stream=None) -> QuasarStatus:
+    return _status((_lib or load()).quasar_layer_norm(
+        _ptr(x), x_dtype, ld_x, _ptr(weight), _ptr(bias), rows, cols, center, eps, _ptr(y), y_dtype,
+        ld_y, _ptr(stats), _stream(stream)))
+
+
+def quasar_layer_norm_backward_workspace(rows, cols) -> int:
+    return _bytes_of((_lib or load()).quasar_layer_norm_backward_workspace, rows, cols)
+
+
+def quasar_layer_norm_backward(dy, dy_dtype, ld_dy, x, x_dtype, ld_x, weight, stats, rows, cols,
+                               center, residual, ld_residual, dx, dx_dtype, ld_dx, dweight, dbias,
+                               workspace, workspace_bytes, stream=None) -> QuasarStatus:
+    return _status((_lib or load()).quasar_layer_norm_backward(
+        _ptr(dy), dy_dtype, ld_dy, _ptr(x), x_dtype, ld_x, _ptr(weight), _ptr(stats), rows, cols,
+        center, _ptr(residual), ld_residual, _ptr(dx), dx_dtype, ld_dx, _ptr(dweight), _ptr(dbias),
+        _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 def quasar_get_device_status(stream=None) -> QuasarStatus:
