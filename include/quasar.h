@@ -661,6 +661,37 @@ quasar_status quasar_layer_norm_backward(const void* dy, quasar_dtype dy_dtype, 
                                          quasar_stream_t stream);
 
 /*
+ * quasar_attention -- y = softmax(scale q k^T) v for each head, over sequences
+ * packed along the rows.
+ *
+ *   q         [tokens, heads x head_dim] bf16.
+ *   k, v      [keys, kv_heads x head_dim] bf16; heads / kv_heads consecutive
+ *             heads of q share one of k and v.
+ *   starts    [sequences + 1] int32: sequence i has the rows starts[i] ..
+ *             starts[i + 1] - 1 of q, key_starts alike for k and v.  Both are
+ *             read on the device and must not decrease or leave the tensors
+ *             (rows outside are not accessed, whatever they hold).  NULL with
+ *             sequences 1: every row.
+ *   causal    1: a sequence's last token sees its last key, the token before it
+ *             one key less, and so on (so one token sees every key); 0: every
+ *             token sees every key of its sequence.
+ *   scale     above 0.
+ *   y         [tokens, heads x head_dim] bf16 (written).
+ *   lse       [tokens, heads] fp32: log sum exp of the scaled scores, for the
+ *             backward call; or NULL.
+ * q, k, v and y are 16-byte aligned with row strides of a multiple of 8, and so
+ * is head_dim, at most 128 (UNSUPPORTED beyond; at most 128 heads that share
+ * keys).  Columns of one buffer (a projection's result) are fine.  A token that
+ * sees no key, and a row of no sequence, has y 0 and lse -inf.  A value that is
+ * not finite reaches the rows of its sequence alone; in v it may reach those
+ * that do not see it, as 0 times it does in the formula.
+ */
+quasar_status quasar_attention(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                               int64_t tokens, int64_t keys, int64_t heads, int64_t kv_heads, int64_t head_dim,
+                               const int32_t* starts, const int32_t* key_starts, int64_t sequences, int causal,
+                               float scale, void* y, int64_t ld_y, float* lse, quasar_stream_t stream);
+
+/*
  * quasar_get_device_status -- synchronises `stream`, then returns
  * QUASAR_ERR_TIMEOUT if any kernel of this library on the current device
  * recorded a timed-out wait since the previous query (and clears the record),

@@ -19,7 +19,7 @@ from .quasar import (ACTIVATIONS, BF16, F32, QuasarError, QuasarStatus, adamw_nv
                      quasar_recon_nvfp4, quasar_recon_nvfp4_batch_ex, quasar_tensor_amax,
                      quasar_activation_grad, quasar_distill_top, quasar_distill_top_backward,
                      quasar_linear, quasar_linear_grad_input, quasar_linear_grad_weight,
-                     quasar_top_logits, I32, I64, quasar_embedding, quasar_embedding_backward,
+                     quasar_top_logits, I32, I64, quasar_attention, quasar_embedding, quasar_embedding_backward,
                      quasar_embedding_backward_workspace, quasar_layer_norm,
                      quasar_layer_norm_backward, quasar_layer_norm_backward_workspace)
 
@@ -728,4 +728,67 @@ def layer_norm_backward(dy, x, weight, stats, *, center=True, dx=True, dweight=T
     _check(quasar_layer_norm_backward(dy, _CODES[dy.dtype], ld_dy, x, _CODES[x.dtype], ld_x, weight,
                                       stats, rows, cols, int(bool(center)), residual, ld_res, to, code,
                                       cols, dw, db, scratch, need))
+    return out
+
+
+def _packed(q, k, v, head_dim, starts, key_starts):
+    """tokens, keys, heads, kv_heads, sequences and the row strides of q, k and v."""
+    tokens, q_cols, ld_q = _matrix(q, "q")
+    on = q.get_device()
+    keys, k_cols, ld_k = _matrix(k, "k", on=on)
+    ld_v = _like(v, "v", keys, k_cols, on=on)
+    if head_dim < 1 or q_cols % head_dim or k_cols % head_dim or not q_cols or not k_cols:
+        raise ValueError(f"q has {q_cols} columns and k {k_cols}: whole heads of {head_dim} are wanted")
+    if q_cols % k_cols:
+        raise ValueError(f"{q_cols // head_dim} heads cannot share {k_cols // head_dim}")
+    sequences = 1
+    if starts is not None:
+        sequences = _starts(starts, "starts", None, on)
+        if key_starts is None and tokens != keys:
+            raise ValueError("queries and keys differ in number: key_starts is needed")
+    if key_starts is not None:
+        if starts is None:
+            raise ValueError("key_starts goes with starts")
+        _starts(key_starts, "key_starts", sequences, on)
+    return tokens, keys, q_cols // head_dim, k_cols // head_dim, sequences, ld_q, ld_k, ld_v
+
+
+def _starts(t, name, sequences, on):
+    at = t.get_device()
+    if len(t.shape) != 1 or t.dtype != torch.int32 or at < 0 or not t.is_contiguous() or \
+            t.shape[0] < 1 or (sequences is not None and t.shape[0] != sequences + 1):
+        raise ValueError(f"{name} must be a contiguous int32 CUDA tensor [sequences + 1]")
+    if at != on:
+        raise _elsewhere(name, at, on)
+    return t.shape[0] - 1
+
+
+def attention(q, k, v, head_dim, *, starts=None, key_starts=None, causal=True, scale=None,
+              lse=False, stream=None):
+    """y = softmax(scale q k^T) v for each head, over sequences packed along the
+    rows.
+
+    q: bf16 [tokens, heads * head_dim]; k, v: bf16 [keys, kv_heads * head_dim]
+    (heads / kv_heads consecutive heads share one of k and v); columns of one
+    buffer are fine.  starts: int32 [sequences + 1], where each sequence's rows
+    start (None: one sequence); key_starts: the same of k and v, where it
+    differs.  causal: a sequence's last token sees its last key, so one token a
+    sequence sees every key (a cache).  scale: head_dim ** -0.5 unless given.
+    Returns a dict with y and, with lse, the rows' log sum exp of the scaled
+    scores (fp32 [tokens, heads]).  A token without keys, or of no sequence, has
+    y 0 and lse -inf."""
+    if stream is not None:
+        return _on(stream, attention, q, k, v, head_dim, starts=starts, key_starts=key_starts,
+                   causal=causal, scale=scale, lse=lse)
+    tokens, keys, heads, kv_heads, sequences, ld_q, ld_k, ld_v = _packed(q, k, v, head_dim, starts,
+                                                                        key_starts)
+    _current(q.get_device())
+    y = torch.empty((tokens, heads * head_dim), dtype=torch.bfloat16, device=q.device)
+    out, sums = {"y": y}, None
+    if lse:
+        out["lse"] = sums = torch.empty((tokens, heads), dtype=torch.float32, device=q.device)
+    _check(quasar_attention(q, ld_q, k, ld_k, v, ld_v, tokens, keys, heads, kv_heads, head_dim, starts,
+                            starts if key_starts is None else key_starts, sequences,
+                            int(bool(causal)), head_dim ** -0.5 if scale is None else scale, y,
+                            heads * head_dim, sums))
     return out

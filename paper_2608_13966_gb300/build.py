@@ -44,6 +44,8 @@ UNITS = [
     ("layers_abi.cu", [], "layers_abi.o"),
     ("kernels_norm.cu", [], "kernels_norm.o"),
     ("kernels_embedding.cu", [], "kernels_embedding.o"),
+    ("attention_abi.cu", [], "attention_abi.o"),
+    ("kernels_attention.cu", [], "kernels_attention.o"),
 ]
 
 

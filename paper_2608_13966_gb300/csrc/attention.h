@@ -1,0 +1,45 @@
+// Launch parameters of the attention kernels (shared by host and device).
+#pragma once
+
+#include <cstdint>
+#include <cuda.h>
+
+namespace quasar {
+
+constexpr int kAttnRows = 128;     // of a tile: (token, head) pairs, the lanes of tensor memory
+constexpr int kAttnKeys = 128;     // of a key tile
+constexpr int kAttnMostSplit = 8;  // CTAs of a cluster that share a row's keys
+
+// Sequences packed along the rows of q, and of k and v: sequence i has the rows
+// starts[i] .. starts[i + 1] (NULL: one sequence of all rows).
+struct AttnSequences {
+    const int* starts;
+    const int* key_starts;
+    int n;
+    int tokens;  // rows of q
+    int keys;    // rows of k, v
+};
+
+struct AttnParams {
+    CUtensorMap q;  // [tokens, heads, d]: boxes of 64 x group x tile_tokens
+    CUtensorMap k;  // [keys, kv_heads, d]: boxes of 64 x 1 x 128
+    CUtensorMap v;
+    AttnSequences s;
+    int heads;
+    int kv_heads;
+    int group;        // heads that share keys
+    int d;
+    int tile_tokens;  // kAttnRows / group
+    int causal;
+    int items;        // pairs of tiles there may be, and one (per kv head)
+    int split;
+    float scale_log2;
+    void* y;
+    int64_t ld_y;
+    float* lse;       // [tokens, heads], or NULL
+    uint64_t timeout_ns;
+    uint64_t force_timeout_ns;
+    unsigned int* status;
+};
+
+}  // namespace quasar

@@ -1,0 +1,115 @@
+// C ABI of attention.  Argument validation, launch plans and launches;
+// declarations and contracts are in include/quasar.h.
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "attention.h"
+#include "host_launch.h"
+#include "quasar.h"
+
+namespace quasar {
+const void* attention_kernel(int d);
+int attention_threads();
+size_t attention_smem(int d);
+}  // namespace quasar
+
+namespace {
+
+using namespace quasar;
+
+// [rows, heads, d] bf16 as it lies in columns of a matrix: tiles of 64 columns
+// of a head, `box_heads` heads and `box_rows` rows.
+quasar_status head_map(const void* p, int64_t rows, int64_t heads, int64_t d, int64_t ld, int box_heads, int box_rows,
+                       CUtensorMap* map)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return QUASAR_ERR_UNSUPPORTED;
+    const cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)rows};
+    const cuuint64_t strides[2] = {(cuuint64_t)d * 2, (cuuint64_t)ld * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
+    const cuuint32_t step[3] = {1, 1, 1};
+    const CUresult r =
+        encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(p), dims, strides, box, step,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? QUASAR_OK : QUASAR_ERR_INVALID_ARG;
+}
+
+bool valid_heads(int64_t heads, int64_t kv_heads, int64_t d)
+{
+    return heads >= 1 && kv_heads >= 1 && heads % kv_heads == 0 && d >= 8 && d % 8 == 0 &&
+           heads <= (int64_t(1) << 31) / d;
+}
+
+bool valid_sequences(const int32_t* starts, const int32_t* key_starts, int64_t n)
+{
+    if (n < 0 || n > (int64_t(1) << 24) || !aligned(starts, 4) || !aligned(key_starts, 4)) return false;
+    return n == 1 || (starts && key_starts);
+}
+
+}  // namespace
+
+extern "C" {
+
+quasar_status quasar_attention(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                               int64_t tokens, int64_t keys, int64_t heads, int64_t kv_heads, int64_t head_dim,
+                               const int32_t* starts, const int32_t* key_starts, int64_t sequences, int causal,
+                               float scale, void* y, int64_t ld_y, float* lse, quasar_stream_t stream)
+{
+    if (!valid_heads(heads, kv_heads, head_dim) || !valid_sequences(starts, key_starts, sequences))
+        return QUASAR_ERR_INVALID_ARG;
+    if (!valid_operand(q, tokens, heads * head_dim, ld_q) || !valid_operand(k, keys, kv_heads * head_dim, ld_k) ||
+        !valid_operand(v, keys, kv_heads * head_dim, ld_v) || !valid_operand(y, tokens, heads * head_dim, ld_y))
+        return QUASAR_ERR_INVALID_ARG;
+    if (!(scale > 0.0f) || !std::isfinite(scale) || (causal != 0 && causal != 1) || !aligned(lse, 4))
+        return QUASAR_ERR_INVALID_ARG;
+    if (head_dim > 128 || heads / kv_heads > kAttnRows) return QUASAR_ERR_UNSUPPORTED;
+    if (tokens == 0) return QUASAR_OK;
+    const Bytes b_q(q, tokens, heads * head_dim, ld_q, 2), b_k(k, keys, kv_heads * head_dim, ld_k, 2);
+    const Bytes b_v(v, keys, kv_heads * head_dim, ld_v, 2), b_y(y, tokens, heads * head_dim, ld_y, 2);
+    const Bytes b_lse(lse, tokens * heads, 4), b_s(starts, sequences + 1, 4), b_ks(key_starts, sequences + 1, 4);
+    for (const Bytes* in : {&b_q, &b_k, &b_v, &b_s, &b_ks})
+        if (overlaps(b_y, *in) || overlaps(b_lse, *in)) return QUASAR_ERR_INVALID_ARG;
+    if (overlaps(b_y, b_lse)) return QUASAR_ERR_INVALID_ARG;
+    AttnParams p{};
+    int n_sm = 0;
+    quasar_status st = host_device(&n_sm, &p.status);
+    if (st != QUASAR_OK) return st;
+    p.s = AttnSequences{starts, key_starts, (int)sequences, (int)tokens, (int)keys};
+    p.heads = (int)heads;
+    p.kv_heads = (int)kv_heads;
+    p.group = (int)(heads / kv_heads);
+    p.d = (int)head_dim;
+    p.tile_tokens = kAttnRows / p.group;
+    p.causal = causal;
+    p.scale_log2 = scale * 1.44269504f;
+    p.y = y;
+    p.ld_y = ld_y;
+    p.lse = lse;
+    p.timeout_ns = host_timeout_ns();
+    p.force_timeout_ns = host_forced_timeout_ns();
+    // sequences of n_i tokens have ceil(n_i / span) items, and one more clears
+    // the rows of none
+    const int64_t items = tokens / (2 * p.tile_tokens) + sequences + 1;
+    if (items * kv_heads * kAttnMostSplit > (int64_t(1) << 31) - 1) return QUASAR_ERR_UNSUPPORTED;
+    p.items = (int)items;
+    const int64_t work = std::max<int64_t>(1, items - 1) * kv_heads;
+    const int64_t tiles = keys / std::max<int64_t>(1, sequences) / kAttnKeys;
+    p.split = 1;
+    const void* fn = attention_kernel(p.d);
+    const size_t smem = attention_smem(p.d);
+    while (p.split < kAttnMostSplit && work * p.split * 2 <= n_sm && tiles >= 4 * p.split) p.split *= 2;
+    if ((st = head_map(q, tokens, heads, head_dim, ld_q, p.group, p.tile_tokens, &p.q)) != QUASAR_OK) return st;
+    // (without keys no copy is made: any valid map will do)
+    const bool none = keys == 0;
+    if ((st = head_map(none ? q : k, none ? tokens : keys, none ? heads : kv_heads, head_dim, none ? ld_q : ld_k, 1,
+                       kAttnKeys, &p.k)) != QUASAR_OK)
+        return st;
+    if ((st = head_map(none ? q : v, none ? tokens : keys, none ? heads : kv_heads, head_dim, none ? ld_q : ld_v, 1,
+                       kAttnKeys, &p.v)) != QUASAR_OK)
+        return st;
+    return launch(fn, &p, dim3((unsigned)(items * kv_heads * p.split)), attention_threads(), p.split, smem, stream);
+}
+
+}  // extern "C"

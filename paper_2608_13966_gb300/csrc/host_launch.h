@@ -1,6 +1,7 @@
 // Host-side checks and the launch that the operators' entry points share.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include <cstddef>
@@ -55,6 +56,12 @@ inline bool valid_shape(int64_t rows, int64_t cols, int64_t ld)
            ld <= (int64_t(1) << 36) && (rows == 0 || ld <= (int64_t(1) << 58) / rows);
 }
 
+// An operand's rows start at 16-byte boundaries (the rule of tiled copies).
+inline bool valid_operand(const void* p, int64_t rows, int64_t cols, int64_t ld)
+{
+    return valid_shape(rows, cols, ld) && (rows == 0 || cols == 0 || (p && aligned(p, 16) && ld % 8 == 0));
+}
+
 // -- launches ------------------------------------------------------------------
 
 // A programmatic dependent launch: every kernel started by it waits for the
@@ -83,6 +90,27 @@ inline quasar_status launch(const void* fn, void* params, dim3 grid, int threads
     cfg.numAttrs = cluster > 1 ? 2 : 1;
     void* args[] = {params};
     return cudaLaunchKernelExC(&cfg, fn, args) == cudaSuccess ? QUASAR_OK : QUASAR_ERR_CUDA;
+}
+
+// -- tensor maps ---------------------------------------------------------------
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                 CUtensorMapFloatOOBfill);
+
+inline EncodeTiled encode_tiled()
+{
+    static const EncodeTiled fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) !=
+                cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return fn;
 }
 
 }  // namespace quasar

@@ -1,0 +1,19 @@
+// Instantiations of the attention kernels.
+#include "attention.cuh"
+
+namespace quasar {
+
+const void* attention_kernel(int d)
+{
+    return d <= 64 ? reinterpret_cast<const void*>(&k_attention<1>) : reinterpret_cast<const void*>(&k_attention<2>);
+}
+
+int attention_threads() { return kAttnThreads; }
+
+size_t attention_smem(int d)
+{
+    const size_t tile = (size_t)(d <= 64 ? 1 : 2) * kAttnBlock;
+    return 1024 + (2 + kAttnSlots) * tile + (1 + 2 * kAttnSlots + 6 + 2) * 8 + 8 + sizeof(AttnItem) + 8 + 2 * 128 * 8;
+}
+
+}  // namespace quasar

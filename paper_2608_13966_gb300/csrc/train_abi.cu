@@ -35,25 +35,6 @@ using namespace quasar;
 
 // -- matrix products -------------------------------------------------------------
 
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
-                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                 CUtensorMapFloatOOBfill);
-
-EncodeTiled encode_tiled()
-{
-    static const EncodeTiled fn = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) !=
-                cudaSuccess ||
-            q != cudaDriverEntryPointSuccess)
-            p = nullptr;
-        return reinterpret_cast<EncodeTiled>(p);
-    }();
-    return fn;
-}
-
 // An operand as it lies in memory: bf16 [outer, inner], 64 x box_outer tiles.
 struct Operand {
     const void* p;
@@ -75,12 +56,6 @@ quasar_status tile_map(const Operand& o, int box_outer, CUtensorMap* map)
                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? QUASAR_OK : QUASAR_ERR_INVALID_ARG;
-}
-
-// An operand's rows start at 16-byte boundaries (the rule of tiled copies).
-bool valid_operand(const void* p, int64_t rows, int64_t cols, int64_t ld)
-{
-    return valid_shape(rows, cols, ld) && (rows == 0 || cols == 0 || (p && aligned(p, 16) && ld % 8 == 0));
 }
 
 // Stages of k_product_tile for bn columns: what two CTAs an SM leave each.

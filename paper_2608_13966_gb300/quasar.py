@@ -73,6 +73,8 @@ PROTOTYPES = {
     "quasar_layer_norm_backward_workspace": (_I, [_I64, _I64, _P]),
     "quasar_layer_norm_backward": (_I, [_P, _I, _I64, _P, _I, _I64, _P, _P, _I64, _I64, _I, _P,
                                         _I64, _P, _I, _I64, _P, _P, _P, _I64, _P]),
+    "quasar_attention": (_I, [_P, _I64, _P, _I64, _P, _I64, _I64, _I64, _I64, _I64, _I64, _P, _P,
+                              _I64, _I, _F, _P, _I64, _P, _P]),
     "quasar_get_device_status": (_I, [_P]),
     "quasar_debug_force_timeout": (None, [_I64]),
     "quasar_debug_set_stats": (None, [_P]),
@@ -523,6 +525,15 @@ def quasar_layer_norm_backward(dy, dy_dtype, ld_dy, x, x_dtype, ld_x, weight, st
         _ptr(dy), dy_dtype, ld_dy, _ptr(x), x_dtype, ld_x, _ptr(weight), _ptr(stats), rows, cols,
         center, _ptr(residual), ld_residual, _ptr(dx), dx_dtype, ld_dx, _ptr(dweight), _ptr(dbias),
         _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def quasar_attention(q, ld_q, k, ld_k, v, ld_v, tokens, keys, heads, kv_heads, head_dim, starts,
+                     key_starts, sequences, causal, scale, y, ld_y, lse=None,
+                     stream=None) -> QuasarStatus:
+    return _status((_lib or load()).quasar_attention(
+        _ptr(q), ld_q, _ptr(k), ld_k, _ptr(v), ld_v, tokens, keys, heads, kv_heads, head_dim,
+        _ptr(starts), _ptr(key_starts), sequences, causal, scale, _ptr(y), ld_y, _ptr(lse),
+        _stream(stream)))
 
 
 def quasar_get_device_status(stream=None) -> QuasarStatus:
