@@ -692,6 +692,28 @@ quasar_status quasar_attention(const void* q, int64_t ld_q, const void* k, int64
                                float scale, void* y, int64_t ld_y, float* lse, quasar_stream_t stream);
 
 /*
+ * quasar_attention_backward -- the gradients of quasar_attention in q, k and v
+ * from dy (the gradient at y), with the y and lse that the forward call wrote.
+ *
+ *   dy, y     [tokens, heads x head_dim] bf16, as q.
+ *   lse       [tokens, heads] fp32.
+ *   dq        [tokens, heads x head_dim] bf16 (written), or NULL.
+ *   dk, dv    [keys, kv_heads x head_dim] bf16 (written), or both NULL: sums
+ *             over the heads that share them.
+ * dq, dk and dv are aligned as q; columns of one buffer (what the projection's
+ * own backward pass reads) are fine.  Rows of no sequence, tokens that see no
+ * key and keys that no token sees have gradients 0.
+ */
+quasar_status quasar_attention_backward_workspace(int64_t tokens, int64_t heads, int64_t* bytes);
+quasar_status quasar_attention_backward(const void* dy, int64_t ld_dy, const void* q, int64_t ld_q, const void* k,
+                                        int64_t ld_k, const void* v, int64_t ld_v, const void* y, int64_t ld_y,
+                                        const float* lse, int64_t tokens, int64_t keys, int64_t heads, int64_t kv_heads,
+                                        int64_t head_dim, const int32_t* starts, const int32_t* key_starts,
+                                        int64_t sequences, int causal, float scale, void* dq, int64_t ld_dq, void* dk,
+                                        int64_t ld_dk, void* dv, int64_t ld_dv, void* workspace,
+                                        int64_t workspace_bytes, quasar_stream_t stream);
+
+/*
  * quasar_get_device_status -- synchronises `stream`, then returns
  * QUASAR_ERR_TIMEOUT if any kernel of this library on the current device
  * recorded a timed-out wait since the previous query (and clears the record),

@@ -19,7 +19,8 @@ from .quasar import (ACTIVATIONS, BF16, F32, QuasarError, QuasarStatus, adamw_nv
                      quasar_recon_nvfp4, quasar_recon_nvfp4_batch_ex, quasar_tensor_amax,
                      quasar_activation_grad, quasar_distill_top, quasar_distill_top_backward,
                      quasar_linear, quasar_linear_grad_input, quasar_linear_grad_weight,
-                     quasar_top_logits, I32, I64, quasar_attention, quasar_embedding, quasar_embedding_backward,
+                     quasar_top_logits, I32, I64, quasar_attention,
+                     quasar_attention_backward, quasar_attention_backward_workspace, quasar_embedding, quasar_embedding_backward,
                      quasar_embedding_backward_workspace, quasar_layer_norm,
                      quasar_layer_norm_backward, quasar_layer_norm_backward_workspace)
 
@@ -792,3 +793,50 @@ def attention(q, k, v, head_dim, *, starts=None, key_starts=None, causal=True, s
                             int(bool(causal)), head_dim ** -0.5 if scale is None else scale, y,
                             heads * head_dim, sums))
     return out
+
+
+def attention_backward(dy, q, k, v, y, lse, head_dim, *, starts=None, key_starts=None, causal=True,
+                       scale=None, dq=True, dkv=True, out=None, stream=None):
+    """Gradients of ``attention`` from dy (bf16, of y's shape) and the y and lse
+    that it returned, with the arguments it was called with.  Returns a dict of
+    dq and of dk and dv (sums over the heads that share them), those asked for:
+    written to ``out`` = (dq, dk, dv) if given, which may be columns of one
+    buffer (the dz of the projection that made q, k and v)."""
+    if stream is not None:
+        return _on(stream, attention_backward, dy, q, k, v, y, lse, head_dim, starts=starts,
+                   key_starts=key_starts, causal=causal, scale=scale, dq=dq, dkv=dkv, out=out)
+    tokens, keys, heads, kv_heads, sequences, ld_q, ld_k, ld_v = _packed(q, k, v, head_dim, starts,
+                                                                        key_starts)
+    on, cols, kv_cols = q.get_device(), heads * head_dim, kv_heads * head_dim
+    ld_dy = _like(dy, "dy", tokens, cols, on=on)
+    ld_y = _like(y, "y", tokens, cols, on=on)
+    _like(lse, "lse", tokens, heads, (torch.float32,), on)
+    if not lse.is_contiguous():
+        raise ValueError("lse must be contiguous")
+    if out is not None:
+        if len(out) != 3:
+            raise ValueError("out must be (dq, dk, dv)")
+        for name, wanted, t, rows, width in (("dq", dq, out[0], tokens, cols),
+                                             ("dk", dkv, out[1], keys, kv_cols),
+                                             ("dv", dkv, out[2], keys, kv_cols)):
+            if wanted:
+                _like(t, name, rows, width, on=on)
+    _current(on)
+    made, lds = {}, []
+    for i, (name, wanted, rows, width) in enumerate((("dq", dq, tokens, cols),
+                                                     ("dk", dkv, keys, kv_cols),
+                                                     ("dv", dkv, keys, kv_cols))):
+        if wanted:
+            made[name] = torch.empty((rows, width), dtype=torch.bfloat16, device=q.device) \
+                if out is None else out[i]
+            lds.append(_ld(made[name]))
+        else:
+            lds.append(0)
+    need = quasar_attention_backward_workspace(tokens, heads)
+    _check(quasar_attention_backward(dy, ld_dy, q, ld_q, k, ld_k, v, ld_v, y, ld_y, lse, tokens, keys,
+                                     heads, kv_heads, head_dim, starts,
+                                     starts if key_starts is None else key_starts, sequences,
+                                     int(bool(causal)), head_dim ** -0.5 if scale is None else scale,
+                                     made.get("dq"), lds[0], made.get("dk"), lds[1], made.get("dv"),
+                                     lds[2], _scratch(need, q.device), need))
+    return made

@@ -46,6 +46,7 @@ UNITS = [
     ("kernels_embedding.cu", [], "kernels_embedding.o"),
     ("attention_abi.cu", [], "attention_abi.o"),
     ("kernels_attention.cu", [], "kernels_attention.o"),
+    ("kernels_attention_grad.cu", [], "kernels_attention_grad.o"),
 ]
 
 

@@ -68,7 +68,7 @@ struct AttnItem {
 
 // The sequence that item `want` falls into, where a sequence of n rows has
 // ceil(n / span) items (rows of q, or of the keys).  Whole-warp call.
-__device__ __forceinline__ AttnItem find_item(const AttnSequences& s, int want, int items, int span, bool of_keys)
+__device__ __forceinline__ AttnItem find_item(const AttnSequences& s, int want, int items, int span, bool of_keys = false)
 {
     const int lane = threadIdx.x & 31;
     int before = 0;
@@ -90,8 +90,9 @@ __device__ __forceinline__ AttnItem find_item(const AttnSequences& s, int want, 
             sequence_rows(s.starts, base + l, s.tokens, a.q0, a.n);
             sequence_rows(s.key_starts, base + l, s.keys, a.k0, a.m);
             const int count = __shfl_sync(0xffffffffu, mine, l);
-            // the last item first: under a causal mask it has the most keys
-            a.index = count - 1 - (want - before - __shfl_sync(0xffffffffu, upto - mine, l));
+            // the longest first, under a causal mask: the last tokens, the first keys
+            a.index = want - before - __shfl_sync(0xffffffffu, upto - mine, l);
+            if (!of_keys) a.index = count - 1 - a.index;
             return a;
         }
         before += __shfl_sync(0xffffffffu, upto, 31);
@@ -187,7 +188,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
     wait_for_previous_grid();
     if (warp == 0) {
         const AttnItem a =
-            find_item(p.s, (int)(blockIdx.x / p.split / p.kv_heads), p.items, 2 * p.tile_tokens, false);
+            find_item(p.s, (int)(blockIdx.x / p.split / p.kv_heads), p.items, 2 * p.tile_tokens);
         if (lane == 0) *item = a;
     }
     tc_fence_before();
@@ -214,7 +215,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
         if (lane == 0) {
             if (p.force_timeout_ns) role_wait(never, 0, gone, p.force_timeout_ns, p.status);
             int it = 0;  // entries of the ring: K_0, V_0, K_1, V_1, ...
-            if (steps > 0 && !*gone) {
+            const bool rows_sent = steps > 0 && !*gone;
+            if (rows_sent) {
                 const uint32_t bytes = (uint32_t)(p.tile_tokens * p.group) * 128 * DB;
                 mbar_arrive_expect_tx(q_full, (n[0] > 0 ? bytes : 0) + (n[1] > 0 ? bytes : 0));
                 for (int i = 0; i < 2; ++i)
@@ -234,7 +236,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                                 a.k0 + (first + it / 2) * kAttnKeys, smem_u32(full + s));
             }
             if (*gone) {  // what is in flight has landed before the memory is let go
-                if (it > 0) mbar_wait_bounded(q_full, 0, p.timeout_ns);
+                if (rows_sent) mbar_wait_bounded(q_full, 0, p.timeout_ns);
                 for (int j = max(it - kAttnSlots, 0); j < it; ++j)
                     mbar_wait_bounded(full + j % kAttnSlots, (j / kAttnSlots) & 1, p.timeout_ns);
             }

@@ -42,4 +42,45 @@ struct AttnParams {
     unsigned int* status;
 };
 
+constexpr int kGradCols = 64;  // of a step of the backward kernels
+
+// One of the two backward kernels: 128 rows stay, the other side streams past
+// in steps of 64 columns.
+struct AttnGradParams {
+    CUtensorMap x1, x2;  // of the rows:  k, v (keys stay) or q, dy (queries stay)
+    CUtensorMap z1, z2;  // of the steps: q, dy            or k, v
+    AttnSequences s;
+    int heads;
+    int kv_heads;
+    int group;
+    int d;
+    int tile_tokens;     // of 128 rows of queries
+    int box_heads;       // of a step of queries
+    int step_tokens;
+    int causal;
+    int items;
+    float scale_log2;
+    float scale;
+    const float2* stats;  // [tokens, heads]: lse in bits, sum of dy y
+    void* d1;             // dk or dq
+    int64_t ld_d1;
+    void* d2;             // dv
+    int64_t ld_d2;
+    uint64_t timeout_ns;
+    uint64_t force_timeout_ns;
+    unsigned int* status;
+};
+
+struct AttnStatsParams {
+    const void* dy;
+    int64_t ld_dy;
+    const void* y;
+    int64_t ld_y;
+    const float* lse;
+    int64_t tokens;
+    int heads;
+    int d;
+    float2* stats;
+};
+
 }  // namespace quasar

@@ -75,6 +75,10 @@ PROTOTYPES = {
                                         _I64, _P, _I, _I64, _P, _P, _P, _I64, _P]),
     "quasar_attention": (_I, [_P, _I64, _P, _I64, _P, _I64, _I64, _I64, _I64, _I64, _I64, _P, _P,
                               _I64, _I, _F, _P, _I64, _P, _P]),
+    "quasar_attention_backward_workspace": (_I, [_I64, _I64, _P]),
+    "quasar_attention_backward": (_I, [_P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64,
+                                       _I64, _I64, _I64, _I64, _P, _P, _I64, _I, _F, _P, _I64, _P,
+                                       _I64, _P, _I64, _P, _I64, _P]),
     "quasar_get_device_status": (_I, [_P]),
     "quasar_debug_force_timeout": (None, [_I64]),
     "quasar_debug_set_stats": (None, [_P]),
@@ -533,6 +537,21 @@ def quasar_attention(q, ld_q, k, ld_k, v, ld_v, tokens, keys, heads, kv_heads, h
     return _status((_lib or load()).quasar_attention(
         _ptr(q), ld_q, _ptr(k), ld_k, _ptr(v), ld_v, tokens, keys, heads, kv_heads, head_dim,
         _ptr(starts), _ptr(key_starts), sequences, causal, scale, _ptr(y), ld_y, _ptr(lse),
+        _stream(stream)))
+
+
+def quasar_attention_backward_workspace(tokens, heads) -> int:
+    return _bytes_of((_lib or load()).quasar_attention_backward_workspace, tokens, heads)
+
+
+def quasar_attention_backward(dy, ld_dy, q, ld_q, k, ld_k, v, ld_v, y, ld_y, lse, tokens, keys, heads,
+                              kv_heads, head_dim, starts, key_starts, sequences, causal, scale, dq,
+                              ld_dq, dk, ld_dk, dv, ld_dv, workspace, workspace_bytes,
+                              stream=None) -> QuasarStatus:
+    return _status((_lib or load()).quasar_attention_backward(
+        _ptr(dy), ld_dy, _ptr(q), ld_q, _ptr(k), ld_k, _ptr(v), ld_v, _ptr(y), ld_y, _ptr(lse),
+        tokens, keys, heads, kv_heads, head_dim, _ptr(starts), _ptr(key_starts), sequences, causal,
+        scale, _ptr(dq), ld_dq, _ptr(dk), ld_dk, _ptr(dv), ld_dv, _ptr(workspace), workspace_bytes,
         _stream(stream)))
 
 
