@@ -194,3 +194,27 @@ def test_streams_and_graphs():
     torch.cuda.synchronize()
     for _, o in graphs:
         check(case, o, q, k, v, nq2, nk2)
+
+
+def test_a_wait_that_runs_out_is_reported():
+    """Forward and both backward kernels: their copies are never asked for."""
+    from paper_2608_13966_gb300 import quasar as Q
+
+    for case in (([300], None, 4, 2, 128, True), ([1], [3000], 8, 2, 64, True)):  # (the second: a cluster a row)
+        q, k, v, starts, key_starts, nq, nk = make(case)
+        kw = dict(starts=starts, key_starts=key_starts)
+        want = api.attention(q, k, v, case[4], lse=True, **kw)
+        back = lambda: api.attention_backward(q, q, k, v, want["y"], want["lse"], case[4], **kw)  # noqa: E731
+        grads = back()
+        api.check_device()
+        for call in (lambda: api.attention(q, k, v, case[4], **kw), back):
+            Q.quasar_debug_force_timeout(1_000_000)
+            try:
+                call()
+                assert Q.quasar_get_device_status() == Q.QuasarStatus.ERR_TIMEOUT
+            finally:
+                Q.quasar_debug_force_timeout(0)
+        assert torch.equal(api.attention(q, k, v, case[4], **kw)["y"], want["y"])
+        again = back()
+        assert all(torch.equal(again[n], grads[n]) for n in grads)
+        api.check_device()
