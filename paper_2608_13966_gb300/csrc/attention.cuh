@@ -8,8 +8,7 @@
 // products run.  For each key tile j and row tile i
 //
 //   S_i = Q_i K_j^T          in tensor memory, 128 x 128 fp32
-//   m, l, P                  a thread per row, no exchange between threads;
-//                            P in bf16 takes S's place
+//   m, l, P                  P in bf16 takes S's place
 //   O_i += P V_j             P from tensor memory, V as it lies in memory
 //
 // in one pass over the keys with the running maximum m and sum l of the
@@ -23,8 +22,11 @@
 // Where rows are few, a cluster of CTAs shares a row's keys and joins its
 // parts through distributed shared memory, in rank order.
 //
-// Warps: 0-3 and 4-7 the rows of tiles 0 and 1, 8 copies, 9 matrix
-// instructions.
+// Warps: 0-7 and 8-15 the rows of tiles 0 and 1, two threads a row, 64 keys of a
+// key tile each, that exchange their maxima (with one thread a row the 4 warps
+// of a tile spent 2,400 cycles a key tile on their dependent instructions, and
+// the tensor cores waited: 4 x 4096 causal, 32 heads of 128 over 8, 565 us);
+// 16 copies, 17 matrix instructions.
 #pragma once
 
 #include "attention.h"
@@ -33,7 +35,8 @@
 
 namespace quasar {
 
-constexpr int kAttnThreads = 320;
+constexpr int kAttnThreads = 640;  // 20 warps, two of them idle: registers move by groups of four
+constexpr int kAttnCopies = 16, kAttnProducts = 17;  // warps
 constexpr int kAttnSlots = 4;             // of the ring of key and value tiles
 constexpr float kAttnSlack = 8.0f;        // log2 of how far m may fall behind
 constexpr uint32_t kAttnBlock = kAttnRows * 128;  // bytes of 128 rows x 64 bf16
@@ -150,7 +153,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
     uint64_t* full = q_full + 1;           // [slots]
     uint64_t* empty = full + kAttnSlots;   // [slots]
     uint64_t* s_full = empty + kAttnSlots; // [2]
-    uint64_t* p_full = s_full + 2;         // [2]: 4 warps
+    uint64_t* p_full = s_full + 2;         // [2]: 8 warps
     uint64_t* o_full = p_full + 2;         // [2]
     uint64_t* drained = o_full + 2;
     uint64_t* never = drained + 1;
@@ -158,8 +161,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
     volatile uint32_t* gone = tmem_slot + 1;
     AttnItem* item = reinterpret_cast<AttnItem*>(tmem_slot + 2);
     float2* stat = reinterpret_cast<float2*>(item + 1);  // [2][128]: m and l, where CTAs share a row
+    float2* swap = stat + 256;                           // [2 turns][2 tiles][2 halves][128]
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int rank = p.split > 1 ? (int)cluster_rank() : 0;
     const int kvh = (int)(blockIdx.x / p.split) % p.kv_heads;
 
@@ -171,7 +175,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(s_full + i, 1);
-            mbar_init(p_full + i, 4);
+            mbar_init(p_full + i, 8);
             mbar_init(o_full + i, 1);
         }
         mbar_init(drained, 1);
@@ -179,8 +183,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
         *gone = 0;
         mbar_init_fence();
     }
-    if (warp == 9) tmem_alloc<1>(tmem_slot, 512);
-    if (warp == 8 && lane == 0) {
+    if (warp == kAttnProducts) tmem_alloc<1>(tmem_slot, 512);
+    if (warp == kAttnCopies && lane == 0) {
         prefetch_map(&p.q);
         prefetch_map(&p.k);
         prefetch_map(&p.v);
@@ -194,7 +198,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = uniform(*tmem_slot);
     const AttnItem a = *item;
     const int t0 = a.index * 2 * p.tile_tokens;  // first token of tile 0
 
@@ -209,304 +213,342 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
         n[0] = max(min(n[0], stop) - first, 0);
         n[1] = max(min(n[1], stop) - first, 0);
     }
+    n[0] = uniform(n[0]);
+    n[1] = uniform(n[1]);
     const int steps = max(n[0], n[1]);
 
-    if (warp == 8) {
-        if (lane == 0) {
-            if (p.force_timeout_ns) role_wait(never, 0, gone, p.force_timeout_ns, p.status);
-            int it = 0;  // entries of the ring: K_0, V_0, K_1, V_1, ...
-            const bool rows_sent = steps > 0 && !*gone;
-            if (rows_sent) {
-                const uint32_t bytes = (uint32_t)(p.tile_tokens * p.group) * 128 * DB;
-                mbar_arrive_expect_tx(q_full, (n[0] > 0 ? bytes : 0) + (n[1] > 0 ? bytes : 0));
-                for (int i = 0; i < 2; ++i)
-                    if (n[i] > 0)
-                        for (int b = 0; b < DB; ++b)
-                            tile_g2s_3d(smem_u32(smem + i * kTile + b * kAttnBlock), &p.q, 64 * b, kvh * p.group,
-                                        a.q0 + t0 + i * p.tile_tokens, smem_u32(q_full));
-            }
-            for (; it < 2 * steps && !*gone; ++it) {
-                const int s = it % kAttnSlots;
-                if (it >= kAttnSlots &&
-                    !role_wait(empty + s, (it / kAttnSlots - 1) & 1, gone, p.timeout_ns, p.status))
-                    break;
-                mbar_arrive_expect_tx(full + s, kTile);
-                for (int b = 0; b < DB; ++b)
-                    tile_g2s_3d(smem_u32(ring + s * kTile + b * kAttnBlock), it & 1 ? &p.v : &p.k, 64 * b, kvh,
-                                a.k0 + (first + it / 2) * kAttnKeys, smem_u32(full + s));
-            }
-            if (*gone) {  // what is in flight has landed before the memory is let go
-                if (rows_sent) mbar_wait_bounded(q_full, 0, p.timeout_ns);
-                for (int j = max(it - kAttnSlots, 0); j < it; ++j)
-                    mbar_wait_bounded(full + j % kAttnSlots, (j / kAttnSlots) & 1, p.timeout_ns);
-            }
-        }
-    } else if (warp == 9) {
-        constexpr uint32_t desc_s = mma_desc(kAttnRows, kAttnKeys, false, false);
-        constexpr uint32_t desc_o = mma_desc(kAttnRows, D, false, true);
-        auto wait = [&](uint64_t* bar, uint32_t parity) {
-            const bool ok = role_wait(bar, parity, gone, p.timeout_ns, p.status);
-            return __all_sync(0xffffffffu, ok);
-        };
-        auto slot = [&](int entry) { return smem_u32(ring + (entry % kAttnSlots) * kTile); };
-        auto score = [&](int i, int j) {  // S_i = Q_i K_j^T
-            if (lane == 0) {
-                const uint32_t q = smem_u32(smem + i * kTile), k = slot(2 * j);
-#pragma unroll
-                for (int b = 0; b < DB; ++b) {
-                    uint64_t da = operand_desc(q + b * kAttnBlock, false), db = operand_desc(k + b * kAttnBlock, false);
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        mma_bf16<1>(tmem + i * 128, da, db, desc_s, b + x > 0);
-                        da += k_step(false);
-                        db += k_step(false);
-                    }
-                }
-                mma_commit(smem_u32(s_full + i));
-            }
-            __syncwarp();
-        };
-        bool ok = steps == 0 || wait(q_full, 0);
-        if (steps > 0 && ok && (ok = wait(full, 0))) {
-            tc_fence_after();
-            for (int i = 0; i < 2; ++i)
-                if (n[i] > 0) score(i, 0);
-            if (lane == 0) mma_commit(smem_u32(empty));
-        }
-        for (int j = 0; j < steps && ok; ++j) {
-            const int v = 2 * j + 1, next = 2 * j + 2;
-            if (!(ok = wait(full + v % kAttnSlots, (v / kAttnSlots) & 1))) break;
-            // rows of V behind the sequence belong to another, or to nobody:
-            // their probabilities are 0, but 0 times what lies there need not be
-            const int64_t left = (int64_t)a.m - (int64_t)(first + j) * kAttnKeys;
-            if (left < kAttnKeys) {
-                for (int x = lane + (int)left * 8; x < kAttnKeys * 8; x += 32)
-#pragma unroll
-                    for (int b = 0; b < DB; ++b)
-                        *reinterpret_cast<uint4*>(ring + (v % kAttnSlots) * kTile + b * kAttnBlock + x * 16) =
-                            make_uint4(0, 0, 0, 0);
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-            }
-            for (int i = 0; i < 2 && ok; ++i) {
-                if (j < n[i]) {
-                    if (!(ok = wait(p_full + i, j & 1))) break;
-                    tc_fence_after();
-                    if (lane == 0) {
-                        uint64_t db = operand_desc_tall(slot(v), kAttnKeys);
-#pragma unroll
-                        for (int x = 0; x < kAttnKeys / 16; ++x) {
-                            mma_bf16_ts(tmem + 256 + i * 128, tmem + i * 128 + 8 * x, db, desc_o, j > 0 || x > 0);
-                            db += k_step(true);
-                        }
-                        mma_commit(smem_u32(o_full + i));
-                    }
-                    __syncwarp();
-                }
-                if (j + 1 < n[i]) {
-                    if (!(ok = wait(full + next % kAttnSlots, (next / kAttnSlots) & 1))) break;
-                    tc_fence_after();
-                    score(i, j + 1);
-                }
-            }
-            if (ok && lane == 0) {
-                mma_commit(smem_u32(empty + v % kAttnSlots));
-                if (j + 1 < steps) mma_commit(smem_u32(empty + next % kAttnSlots));
-            }
-        }
-        if (lane == 0) {
-            mma_commit(smem_u32(drained));
-            mbar_wait_bounded(drained, 0, p.timeout_ns);
-        }
-    }
-    __syncwarp();
-
-    // a thread's row: r of tile i
-    const int i = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
-    const int token = t0 + i * p.tile_tokens + r / p.group, head = kvh * p.group + r % p.group;
-    const bool live = warp < 8 && a.spares == 0 && r < p.tile_tokens * p.group && token < a.n;
-    const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    float m = minus_inf(), l = 0.0f;
-    bool ok = true;
-    if (warp < 8 && n[i] > 0) {
-        // the last key that the row sees
-        const int64_t see = !live ? -1 : (p.causal ? min((int64_t)a.m - 1, (int64_t)token + a.m - a.n) : (int64_t)a.m - 1);
-        const bool any_live = __any_sync(0xffffffffu, live);
-        const uint32_t s_at = mine + i * 128, o_at = mine + 256 + i * 128;
-        for (int j = 0; j < n[i]; ++j) {
-            ok = __all_sync(0xffffffffu, role_wait(s_full + i, j & 1, gone, p.timeout_ns, p.status));
-            if (!ok) break;
-            tc_fence_after();
-            if (any_live) {
-                float s[4][32];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld(s_at + 32 * c, s[c]);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_wait_ld(s[c]);
-                const int64_t key0 = (int64_t)(first + j) * kAttnKeys;
-                if (!__all_sync(0xffffffffu, see >= key0 + kAttnKeys - 1)) {
-                    const int upto = (int)max((int64_t)-1, min(see - key0, (int64_t)kAttnKeys));
-#pragma unroll
-                    for (int c = 0; c < kAttnKeys; ++c)
-                        if (c > upto) s[c / 32][c % 32] = minus_inf();
-                }
-                float top[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    top[c] = s[c][0];
-#pragma unroll
-                    for (int x = 1; x < 31; x += 2) top[c] = fmax3(top[c], s[c][x], s[c][x + 1]);
-                    top[c] = fmaxf(top[c], s[c][31]);
-                }
-                const float larger = fmaxf(m, fmaxf(fmax3(top[0], top[1], top[2]), top[3]) * p.scale_log2);
-                if (__any_sync(0xffffffffu, larger > m + kAttnSlack)) {
-                    const float f = larger == m ? 1.0f : exp2_fast(m - larger);
-                    l *= f;
-                    m = larger;
-                    if (j > 0) {
-                        ok = __all_sync(0xffffffffu,
-                                        role_wait(o_full + i, (j - 1) & 1, gone, p.timeout_ns, p.status));
-                        if (!ok) break;
-                        tc_fence_after();
-#pragma unroll 1
-                        for (int c = 0; c < D; c += 32) {
-                            float o[32];
-                            uint32_t w[32];
-                            tmem_ld(o_at + c, o);
-                            tmem_wait_ld(o);
-#pragma unroll
-                            for (int x = 0; x < 32; ++x) w[x] = __float_as_uint(o[x] * f);
-                            tmem_st(o_at + c, w);
-                        }
-                    }
-                }
-                const float shift = m == minus_inf() ? 0.0f : -m;
-                const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), shift2 = make_float2(shift, shift);
-                float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t w[16];
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        float2 e = __ffma2_rn(make_float2(s[c][2 * x], s[c][2 * x + 1]), scale2, shift2);
-                        e.x = exp2_fast(e.x);
-                        e.y = exp2_fast(e.y);
-                        sum[x & 1] = __fadd2_rn(sum[x & 1], e);
-                        w[x] = pack_bf16x2(e.x, e.y);
-                    }
-                    tmem_st(s_at + 16 * c, w);
-                }
-                l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-                tmem_wait_st();
-            }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_full + i);
-        }
-        if (ok) {
-            ok = __all_sync(0xffffffffu, role_wait(o_full + i, (n[i] - 1) & 1, gone, p.timeout_ns, p.status));
-            tc_fence_after();
-        }
-    }
-
-    if (p.split == 1) {
-        if (warp < 8 && a.spares == 0 && ok && __any_sync(0xffffffffu, live)) {
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-            // the rows through the query tile's memory, so that a store covers
-            // whole rows
-            uint8_t* stage = smem + i * kTile + (warp & 3) * 32 * D * 2;
-#pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
-                float o[32];
-                if (n[i] > 0) {
-                    tmem_ld(mine + 256 + i * 128 + c, o);
-                    tmem_wait_ld(o);
-                } else {
-#pragma unroll
-                    for (int x = 0; x < 32; ++x) o[x] = 0.0f;
-                }
-#pragma unroll
-                for (int x = 0; x < 32; x += 8)
-                    *reinterpret_cast<uint4*>(stage + lane * D * 2 + (((c + x) / 8) ^ (lane & 7)) * 16) =
-                        make_uint4(pack_bf16x2(o[x] * inv, o[x + 1] * inv), pack_bf16x2(o[x + 2] * inv, o[x + 3] * inv),
-                                   pack_bf16x2(o[x + 4] * inv, o[x + 5] * inv), pack_bf16x2(o[x + 6] * inv, o[x + 7] * inv));
-            }
-            if (p.lse && live)
-                p.lse[(int64_t)(a.q0 + token) * p.heads + head] = l == 0.0f ? minus_inf() : 0.69314718f * (m + log2f(l));
-            __syncwarp();
-            constexpr int kLanes = D / 8;  // of a row
-            for (int q = 0; q < 32; q += 32 / kLanes) {
-                const int row = q + lane / kLanes, chunk = lane % kLanes;
-                const int rr = (warp & 3) * 32 + row;
-                const int tok = t0 + i * p.tile_tokens + rr / p.group;
-                if (rr < p.tile_tokens * p.group && tok < a.n && chunk * 8 < p.d)
-                    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.y) + (int64_t)(a.q0 + tok) * p.ld_y +
-                                              (int64_t)(kvh * p.group + rr % p.group) * p.d + chunk * 8) =
-                        *reinterpret_cast<const uint4*>(stage + row * D * 2 + (chunk ^ (row & 7)) * 16);
-            }
-        }
-    } else if (a.spares == 0) {
-        // every product of this CTA is done: the ring's memory takes O
-        __syncthreads();
-        float* part = reinterpret_cast<float*>(ring);  // [2][128][D], vectors of 4 swizzled by row
-        if (warp < 8) {
-            stat[i * 128 + r] = make_float2(m, ok ? l : 0.0f);
-            if (n[i] > 0 && ok) {
-#pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
-                    float o[32];
-                    tmem_ld(mine + 256 + i * 128 + c, o);
-                    tmem_wait_ld(o);
-#pragma unroll
-                    for (int x = 0; x < 32; x += 4)
-                        *reinterpret_cast<float4*>(part + (size_t)(i * 128 + r) * D + (((c + x) / 4) ^ (r & 7)) * 4) =
-                            make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
-                }
-            }
-        }
-        cluster_sync();
-        constexpr int kVecs = D / 4;
-        const int rows = p.tile_tokens * p.group;
-        for (int x = rank * kAttnThreads + (int)threadIdx.x; x < 2 * rows * kVecs; x += p.split * kAttnThreads) {
-            const int tile = x / (rows * kVecs), row = x / kVecs % rows, c = x % kVecs;
-            const int tok = t0 + tile * p.tile_tokens + row / p.group;
-            if (tok >= a.n || 4 * c >= p.d) continue;
-            float top = minus_inf(), total = 0.0f;
-            float2 st[kAttnMostSplit];
-#pragma unroll
-            for (int q = 0; q < kAttnMostSplit; ++q)
-                if (q < p.split) {
-                    const uint32_t at = peer_addr(smem_u32(stat + tile * 128 + row), (uint32_t)q);
-                    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(st[q].x), "=f"(st[q].y) : "r"(at) : "memory");
-                    top = fmaxf(top, st[q].x);
-                }
-            const float shift = top == minus_inf() ? 0.0f : top;
-            float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-            for (int q = 0; q < kAttnMostSplit; ++q)
-                if (q < p.split && st[q].y != 0.0f) {  // (a part without keys left nothing)
-                    const float f = exp2_fast(st[q].x - shift);
-                    const float4 v = ld_peer4(peer_addr(smem_u32(part + (size_t)(tile * 128 + row) * D + (c ^ (row & 7)) * 4), (uint32_t)q));
-                    total = fmaf(f, st[q].y, total);
-                    o.x = fmaf(f, v.x, o.x), o.y = fmaf(f, v.y, o.y), o.z = fmaf(f, v.z, o.z), o.w = fmaf(f, v.w, o.w);
-                }
-            const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-            const int64_t to = (int64_t)(a.q0 + tok);
-            const int h = kvh * p.group + row % p.group;
-            *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.y) + to * p.ld_y + (int64_t)h * p.d + 4 * c) =
-                make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-            if (p.lse && c == 0)
-                p.lse[to * p.heads + h] = total == 0.0f ? minus_inf() : 0.69314718f * (shift + log2f(total));
-        }
-        cluster_sync();  // nobody leaves while its memory is read
-    }
     if (a.spares > 0 && rank == 0) {
         clear_rows(p.y, p.ld_y, (int64_t)kvh * p.group * p.d, p.group * p.d, p.s.starts, p.s.n, p.s.tokens, a.index, a.spares);
         clear_lse(p.lse, p.heads, kvh * p.group, p.group, p.s.starts, p.s.n, p.s.tokens, a.index, a.spares);
     }
+    // registers: 640 threads start with 96; 512 x 104 + 128 x 64 is as many
+    if (warp >= kAttnCopies) {
+        registers_down<64>();
+        if (warp == kAttnCopies) {
+            if (lane == 0) {
+                if (p.force_timeout_ns) role_wait(never, 0, gone, p.force_timeout_ns, p.status);
+                int it = 0;  // entries of the ring: K_0, V_0, K_1, V_1, ...
+                const bool rows_sent = steps > 0 && !*gone;
+                if (rows_sent) {
+                    const uint32_t bytes = (uint32_t)(p.tile_tokens * p.group) * 128 * DB;
+                    mbar_arrive_expect_tx(q_full, (n[0] > 0 ? bytes : 0) + (n[1] > 0 ? bytes : 0));
+                    for (int i = 0; i < 2; ++i)
+                        if (n[i] > 0)
+                            for (int b = 0; b < DB; ++b)
+                                tile_g2s_3d(smem_u32(smem + i * kTile + b * kAttnBlock), &p.q, 64 * b, kvh * p.group,
+                                            a.q0 + t0 + i * p.tile_tokens, smem_u32(q_full));
+                }
+                for (; it < 2 * steps && !*gone; ++it) {
+                    const int s = it % kAttnSlots;
+                    if (it >= kAttnSlots &&
+                        !role_wait(empty + s, (it / kAttnSlots - 1) & 1, gone, p.timeout_ns, p.status))
+                        break;
+                    mbar_arrive_expect_tx(full + s, kTile);
+                    for (int b = 0; b < DB; ++b)
+                        tile_g2s_3d(smem_u32(ring + s * kTile + b * kAttnBlock), it & 1 ? &p.v : &p.k, 64 * b, kvh,
+                                    a.k0 + (first + it / 2) * kAttnKeys, smem_u32(full + s));
+                }
+                if (*gone) {  // what is in flight has landed before the memory is let go
+                    if (rows_sent) mbar_wait_bounded(q_full, 0, p.timeout_ns);
+                    for (int j = max(it - kAttnSlots, 0); j < it; ++j)
+                        mbar_wait_bounded(full + j % kAttnSlots, (j / kAttnSlots) & 1, p.timeout_ns);
+                }
+            }
+        } else if (warp == kAttnProducts) {
+            constexpr uint32_t desc_s = mma_desc(kAttnRows, kAttnKeys, false, false);
+            constexpr uint32_t desc_o = mma_desc(kAttnRows, D, false, true);
+            auto wait = [&](uint64_t* bar, uint32_t parity) {
+                const bool ok = role_wait(bar, parity, gone, p.timeout_ns, p.status);
+                return __all_sync(0xffffffffu, ok);
+            };
+            auto slot = [&](int entry) { return smem_u32(ring + (entry % kAttnSlots) * kTile); };
+            auto score = [&](int i, int j) {  // S_i = Q_i K_j^T
+                if (elect_one()) {
+                    const uint32_t q = smem_u32(smem + i * kTile), k = slot(2 * j);
+#pragma unroll
+                    for (int b = 0; b < DB; ++b) {
+                        uint64_t da = operand_desc(q + b * kAttnBlock, false), db = operand_desc(k + b * kAttnBlock, false);
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            mma_bf16<1>(tmem + i * 128, da, db, desc_s, b + x > 0);
+                            da += k_step(false);
+                            db += k_step(false);
+                        }
+                    }
+                    mma_commit(smem_u32(s_full + i));
+                }
+                __syncwarp();
+            };
+            bool ok = steps == 0 || wait(q_full, 0);
+            if (steps > 0 && ok && (ok = wait(full, 0))) {
+                tc_fence_after();
+                for (int i = 0; i < 2; ++i)
+                    if (n[i] > 0) score(i, 0);
+                if (elect_one()) mma_commit(smem_u32(empty));
+            }
+            for (int j = 0; j < steps && ok; ++j) {
+                const int v = 2 * j + 1, next = 2 * j + 2;
+                if (!(ok = wait(full + v % kAttnSlots, (v / kAttnSlots) & 1))) break;
+                // rows of V behind the sequence belong to another, or to nobody:
+                // their probabilities are 0, but 0 times what lies there need not be
+                const int64_t left = (int64_t)a.m - (int64_t)(first + j) * kAttnKeys;
+                if (left < kAttnKeys) {
+                    for (int x = lane + (int)left * 8; x < kAttnKeys * 8; x += 32)
+#pragma unroll
+                        for (int b = 0; b < DB; ++b)
+                            *reinterpret_cast<uint4*>(ring + (v % kAttnSlots) * kTile + b * kAttnBlock + x * 16) =
+                                make_uint4(0, 0, 0, 0);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                }
+                for (int i = 0; i < 2 && ok; ++i) {
+                    if (j < n[i]) {
+                        if (!(ok = wait(p_full + i, j & 1))) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+                            uint64_t db = operand_desc_tall(slot(v), kAttnKeys);
+#pragma unroll
+                            for (int x = 0; x < kAttnKeys / 16; ++x) {
+                                mma_bf16_ts(tmem + 256 + i * 128, tmem + i * 128 + 8 * x, db, desc_o, j > 0 || x > 0);
+                                db += k_step(true);
+                            }
+                            mma_commit(smem_u32(o_full + i));
+                        }
+                        __syncwarp();
+                    }
+                    if (j + 1 < n[i]) {
+                        if (!(ok = wait(full + next % kAttnSlots, (next / kAttnSlots) & 1))) break;
+                        tc_fence_after();
+                        score(i, j + 1);
+                    }
+                }
+                if (ok && elect_one()) {
+                    mma_commit(smem_u32(empty + v % kAttnSlots));
+                    if (j + 1 < steps) mma_commit(smem_u32(empty + next % kAttnSlots));
+                }
+            }
+            if (elect_one()) {
+                mma_commit(smem_u32(drained));
+                mbar_wait_bounded(drained, 0, p.timeout_ns);
+            }
+        }
+        __syncwarp();
+        if (p.split > 1 && a.spares == 0) {  // the barriers of the rows' warps
+            __syncthreads();
+            cluster_sync();
+            cluster_sync();
+        }
+    } else {
+        registers_up<104>();
+        // a thread's row: r of tile i; its half of the row's keys, and of its columns
+        const int i = warp >> 3 & 1, half = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
+        const int token = t0 + i * p.tile_tokens + r / p.group, head = kvh * p.group + r % p.group;
+        const bool live = a.spares == 0 && r < p.tile_tokens * p.group && token < a.n;
+        const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        constexpr int kHalf = D / 2;
+        const uint32_t o_at = mine + 256 + i * 128 + half * kHalf;
+        float m = minus_inf(), l = 0.0f;
+        bool ok = true;
+        if (n[i] > 0) {
+            // Both warps of a row come to this barrier once a key tile and once at
+            // the end, whatever their waits gave, and leave together.
+            auto exchange = [&](int turn, float x, float& other) {
+                float2* at = swap + ((turn & 1) * 2 + i) * 256 + r;
+                at[half * 128] = make_float2(x, ok ? 1.0f : 0.0f);
+                asm volatile("bar.sync %0, 64;" ::"r"(1 + i * 4 + (warp & 3)) : "memory");
+                const float2 theirs = at[(half ^ 1) * 128];
+                other = theirs.x;
+                return ok && theirs.y != 0.0f;
+            };
+            // the last key that the row sees
+            const int64_t see = !live ? -1 : (p.causal ? min((int64_t)a.m - 1, (int64_t)token + a.m - a.n) : (int64_t)a.m - 1);
+            const bool any_live = __any_sync(0xffffffffu, live);
+            const uint32_t s_at = mine + i * 128 + half * 64, p_at = mine + i * 128 + half * 32;
+            bool together = true;
+            for (int j = 0; j < n[i]; ++j) {
+                ok = ok && __all_sync(0xffffffffu, role_wait(s_full + i, j & 1, gone, p.timeout_ns, p.status));
+                tc_fence_after();
+                float s[2][32];
+                float larger = m, other;
+                if (any_live && ok) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) tmem_ld(s_at + 32 * c, s[c]);
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) tmem_wait_ld(s[c]);
+                    const int64_t key0 = (int64_t)(first + j) * kAttnKeys + 64 * half;
+                    if (!__all_sync(0xffffffffu, see >= key0 + 63)) {
+                        const int upto = (int)max((int64_t)-1, min(see - key0, (int64_t)64));
+#pragma unroll
+                        for (int c = 0; c < 64; ++c)
+                            if (c > upto) s[c / 32][c % 32] = minus_inf();
+                    }
+                    float top[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const float* v = s[c / 2] + c % 2 * 16;
+                        top[c] = fmaxf(v[0], v[1]);
+#pragma unroll
+                        for (int x = 2; x < 16; x += 2) top[c] = fmax3(top[c], v[x], v[x + 1]);
+                    }
+                    larger = fmaxf(m, fmaxf(fmax3(top[0], top[1], top[2]), top[3]) * p.scale_log2);
+                }
+                // (the scores are in registers, both warps': P may take their place)
+                tc_fence_before();
+                together = exchange(j, larger, other);
+                if (!together) break;
+                if (any_live) {
+                    tc_fence_after();
+                    larger = fmaxf(larger, other);
+                    if (__any_sync(0xffffffffu, larger > m + kAttnSlack)) {
+                        const float f = larger == m ? 1.0f : exp2_fast(m - larger);
+                        l *= f;
+                        m = larger;
+                        if (j > 0) {
+                            ok = __all_sync(0xffffffffu,
+                                            role_wait(o_full + i, (j - 1) & 1, gone, p.timeout_ns, p.status));
+                            if (!ok) continue;
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int c = 0; c < kHalf; c += 16) {
+                                float o[16];
+                                tmem_ld16(o_at + c, o);
+#pragma unroll
+                                for (int x = 0; x < 16; ++x) o[x] *= f;
+                                tmem_st16(o_at + c, o);
+                            }
+                        }
+                    }
+                    const float shift = m == minus_inf() ? 0.0f : -m;
+                    const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), shift2 = make_float2(shift, shift);
+                    float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) {
+                            float2 e = __ffma2_rn(make_float2(s[c][2 * x], s[c][2 * x + 1]), scale2, shift2);
+                            e.x = exp2_fast(e.x);
+                            e.y = exp2_fast(e.y);
+                            sum[x & 1] = __fadd2_rn(sum[x & 1], e);
+                            w[x] = pack_bf16x2(e.x, e.y);
+                        }
+                        tmem_st(p_at + 16 * c, w);
+                    }
+                    l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                    tmem_wait_st();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full + i);
+            }
+            if (together) {
+                ok = ok && __all_sync(0xffffffffu, role_wait(o_full + i, (n[i] - 1) & 1, gone, p.timeout_ns, p.status));
+                float other;
+                ok = exchange(n[i], l, other);
+                l = half ? other + l : l + other;
+                tc_fence_after();
+            } else {
+                ok = false;
+            }
+        }
+
+        if (p.split == 1) {
+            if (a.spares == 0 && ok && __any_sync(0xffffffffu, live)) {
+                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                // the rows through the query tile's memory, so that a store covers
+                // whole rows
+                uint8_t* stage = smem + i * kTile + (warp & 3) * 32 * D * 2;
+#pragma unroll 1
+                for (int c = half * kHalf; c < (half + 1) * kHalf; c += 32) {
+                    float o[32];
+                    if (n[i] > 0) {
+                        tmem_ld(o_at + c - half * kHalf, o);
+                        tmem_wait_ld(o);
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < 32; ++x) o[x] = 0.0f;
+                    }
+#pragma unroll
+                    for (int x = 0; x < 32; x += 8)
+                        *reinterpret_cast<uint4*>(stage + lane * D * 2 + (((c + x) / 8) ^ (lane & 7)) * 16) =
+                            make_uint4(pack_bf16x2(o[x] * inv, o[x + 1] * inv), pack_bf16x2(o[x + 2] * inv, o[x + 3] * inv),
+                                       pack_bf16x2(o[x + 4] * inv, o[x + 5] * inv), pack_bf16x2(o[x + 6] * inv, o[x + 7] * inv));
+                }
+                if (p.lse && live && half == 0)
+                    p.lse[(int64_t)(a.q0 + token) * p.heads + head] = l == 0.0f ? minus_inf() : 0.69314718f * (m + log2f(l));
+                __syncwarp();
+                constexpr int kLanes = kHalf / 8;  // of a row
+                for (int q = 0; q < 32; q += 32 / kLanes) {
+                    const int row = q + lane / kLanes, chunk = half * kLanes + lane % kLanes;
+                    const int rr = (warp & 3) * 32 + row;
+                    const int tok = t0 + i * p.tile_tokens + rr / p.group;
+                    if (rr < p.tile_tokens * p.group && tok < a.n && chunk * 8 < p.d)
+                        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.y) + (int64_t)(a.q0 + tok) * p.ld_y +
+                                                  (int64_t)(kvh * p.group + rr % p.group) * p.d + chunk * 8) =
+                            *reinterpret_cast<const uint4*>(stage + row * D * 2 + (chunk ^ (row & 7)) * 16);
+                }
+            }
+        } else if (a.spares == 0) {
+            // every product of this CTA is done: the ring's memory takes O
+            __syncthreads();
+            float* part = reinterpret_cast<float*>(ring);  // [2][128][D], vectors of 4 swizzled by row
+            {
+                if (half == 0) stat[i * 128 + r] = make_float2(m, ok ? l : 0.0f);
+                if (n[i] > 0 && ok) {
+#pragma unroll 1
+                    for (int c = half * kHalf; c < (half + 1) * kHalf; c += 32) {
+                        float o[32];
+                        tmem_ld(o_at + c - half * kHalf, o);
+                        tmem_wait_ld(o);
+#pragma unroll
+                        for (int x = 0; x < 32; x += 4)
+                            *reinterpret_cast<float4*>(part + (size_t)(i * 128 + r) * D + (((c + x) / 4) ^ (r & 7)) * 4) =
+                                make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
+                    }
+                }
+            }
+            cluster_sync();
+            constexpr int kVecs = D / 4;
+            const int rows = p.tile_tokens * p.group;
+            constexpr int kMany = kAttnCopies * 32;
+            for (int x = rank * kMany + (int)threadIdx.x; x < 2 * rows * kVecs; x += p.split * kMany) {
+                const int tile = x / (rows * kVecs), row = x / kVecs % rows, c = x % kVecs;
+                const int tok = t0 + tile * p.tile_tokens + row / p.group;
+                if (tok >= a.n || 4 * c >= p.d) continue;
+                float top = minus_inf(), total = 0.0f;
+                float2 st[kAttnMostSplit];
+#pragma unroll
+                for (int q = 0; q < kAttnMostSplit; ++q)
+                    if (q < p.split) {
+                        const uint32_t at = peer_addr(smem_u32(stat + tile * 128 + row), (uint32_t)q);
+                        asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(st[q].x), "=f"(st[q].y) : "r"(at) : "memory");
+                        top = fmaxf(top, st[q].x);
+                    }
+                const float shift = top == minus_inf() ? 0.0f : top;
+                float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                for (int q = 0; q < kAttnMostSplit; ++q)
+                    if (q < p.split && st[q].y != 0.0f) {  // (a part without keys left nothing)
+                        const float f = exp2_fast(st[q].x - shift);
+                        const float4 v = ld_peer4(peer_addr(smem_u32(part + (size_t)(tile * 128 + row) * D + (c ^ (row & 7)) * 4), (uint32_t)q));
+                        total = fmaf(f, st[q].y, total);
+                        o.x = fmaf(f, v.x, o.x), o.y = fmaf(f, v.y, o.y), o.z = fmaf(f, v.z, o.z), o.w = fmaf(f, v.w, o.w);
+                    }
+                const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+                const int64_t to = (int64_t)(a.q0 + tok);
+                const int h = kvh * p.group + row % p.group;
+                *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.y) + to * p.ld_y + (int64_t)h * p.d + 4 * c) =
+                    make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+                if (p.lse && c == 0)
+                    p.lse[to * p.heads + h] = total == 0.0f ? minus_inf() : 0.69314718f * (shift + log2f(total));
+            }
+            cluster_sync();  // nobody leaves while its memory is read
+        }
+    }
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) tmem_free<1>(tmem, 512);
+    if (warp == kAttnProducts) tmem_free<1>(tmem, 512);
 }
 
 }  // namespace quasar

@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
     volatile uint32_t* gone = tmem_slot + 1;
     AttnItem* item = reinterpret_cast<AttnItem*>(tmem_slot + 2);
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int kvh = (int)blockIdx.x % p.kv_heads;
 
     if (threadIdx.x == 0) {
@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = uniform(*tmem_slot);
     const AttnItem a = *item;
     const int row0 = a.index * (KEYS ? kAttnRows : p.tile_tokens);  // first key, or token, of the rows
     const int shift = a.m - a.n;                                    // key j is seen by tokens from j - shift on
@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
             per_run = see > 0 ? (int)((see + kGradCols - 1) / kGradCols) : 0;
         }
     }
-    const int steps = per_run * runs;  // (at most tokens x heads, or keys: checked by the host)
+    const int steps = uniform(per_run * runs);  // (at most tokens x heads, or keys: checked by the host)
     // a step's first token (or key), its run, and its columns of the sequence
     auto first_of = [&](int it) { return KEYS ? (step0 + it % per_run) * p.step_tokens : it * kGradCols; };
     auto cols_of = [&](int it) {
@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
         };
         // the gradients grow by step `it`
         auto grow = [&](int it) {
-            if (lane == 0) {
+            if (elect_one()) {
                 const int s = it % kGradSlots, buf = it & 1;
                 const uint32_t z = smem_u32(ring + s * kSlot);
 #pragma unroll
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                 __syncwarp();
             }
             tc_fence_after();
-            if (lane == 0) {
+            if (elect_one()) {
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
                     const uint32_t x = smem_u32(smem + g * kRowTile), z = smem_u32(ring + s * kSlot + g * kColTile);
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
             tc_fence_after();
             grow(steps - 1);
         }
-        if (lane == 0) {  // every instruction is done before the memory is let go
+        if (elect_one()) {  // every instruction is done before the memory is let go
             mma_commit(smem_u32(acc_full));
             mbar_wait_bounded(acc_full, 0, p.timeout_ns);
         }

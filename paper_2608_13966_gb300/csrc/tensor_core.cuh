@@ -240,6 +240,41 @@ __device__ __forceinline__ void tmem_st(uint32_t addr, const uint32_t (&v)[32])
         : "memory");
 }
 
+// One lane of a converged warp.  Matrix instructions take their addresses and
+// descriptors from uniform registers: issued under `lane == 0` and with values
+// that are not known to be the warp's, each cost some 120 cycles of moves, twice
+// what a product of 128 x 128 x 16 takes.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t one;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(one));
+    return one != 0;
+}
+
+// x of lane 0: a value that all lanes hold, known to be the warp's.
+template <typename T>
+__device__ __forceinline__ T uniform(T x)
+{
+    return __shfl_sync(0xffffffffu, x, 0);
+}
+
+// Registers a thread, moved between the groups of four warps of a CTA (each
+// group as a whole): what some take the others have given, out of what the CTA
+// was launched with.
+template <int N>
+__device__ __forceinline__ void registers_up()
+{
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+template <int N>
+__device__ __forceinline__ void registers_down()
+{
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
 // -- waits -------------------------------------------------------------------
 
 // Wait for a phase of `bar`; gives up when limit_ns have passed or another
