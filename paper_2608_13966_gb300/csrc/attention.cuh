@@ -37,7 +37,7 @@ namespace quasar {
 
 constexpr int kAttnThreads = 640;  // 20 warps, two of them idle: registers move by groups of four
 constexpr int kAttnCopies = 16, kAttnProducts = 17;  // warps
-constexpr int kAttnSlots = 4;             // of the ring of key and value tiles
+constexpr int kAttnSlots = 2;             // of the ring, each a tile of values and one of keys
 constexpr float kAttnSlack = 8.0f;        // log2 of how far m may fall behind
 constexpr uint32_t kAttnBlock = kAttnRows * 128;  // bytes of 128 rows x 64 bf16
 
@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* ring = smem + 2 * kTile;
-    uint64_t* q_full = reinterpret_cast<uint64_t*>(ring + kAttnSlots * kTile);
+    uint64_t* q_full = reinterpret_cast<uint64_t*>(ring + kAttnSlots * 2 * kTile);
     uint64_t* full = q_full + 1;           // [slots]
     uint64_t* empty = full + kAttnSlots;   // [slots]
     uint64_t* s_full = empty + kAttnSlots; // [2]
@@ -226,8 +226,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
         registers_down<64>();
         if (warp == kAttnCopies) {
             if (lane == 0) {
-                if (p.force_timeout_ns) role_wait(never, 0, gone, p.force_timeout_ns, p.status);
-                int it = 0;  // entries of the ring: K_0, V_0, K_1, V_1, ...
+                if (p.force_timeout_ns) role_sleep(never, 0, gone, p.force_timeout_ns, p.status);
+                int it = 0;  // entries of the ring: K_0; V_0, K_1; V_1, K_2; ... V_last
                 const bool rows_sent = steps > 0 && !*gone;
                 if (rows_sent) {
                     const uint32_t bytes = (uint32_t)(p.tile_tokens * p.group) * 128 * DB;
@@ -238,15 +238,18 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                                 tile_g2s_3d(smem_u32(smem + i * kTile + b * kAttnBlock), &p.q, 64 * b, kvh * p.group,
                                             a.q0 + t0 + i * p.tile_tokens, smem_u32(q_full));
                 }
-                for (; it < 2 * steps && !*gone; ++it) {
+                for (; steps > 0 && it <= steps && !*gone; ++it) {
                     const int s = it % kAttnSlots;
                     if (it >= kAttnSlots &&
-                        !role_wait(empty + s, (it / kAttnSlots - 1) & 1, gone, p.timeout_ns, p.status))
+                        !role_sleep(empty + s, (it / kAttnSlots - 1) & 1, gone, p.timeout_ns, p.status))
                         break;
-                    mbar_arrive_expect_tx(full + s, kTile);
-                    for (int b = 0; b < DB; ++b)
-                        tile_g2s_3d(smem_u32(ring + s * kTile + b * kAttnBlock), it & 1 ? &p.v : &p.k, 64 * b, kvh,
-                                    a.k0 + (first + it / 2) * kAttnKeys, smem_u32(full + s));
+                    mbar_arrive_expect_tx(full + s, (it > 0 ? kTile : 0) + (it < steps ? kTile : 0));
+                    const uint32_t to = smem_u32(ring + s * 2 * kTile);
+                    const int key = a.k0 + (first + it) * kAttnKeys;
+                    for (int b = 0; b < DB; ++b) {
+                        if (it > 0) tile_g2s_3d(to + b * kAttnBlock, &p.v, 64 * b, kvh, key - kAttnKeys, smem_u32(full + s));
+                        if (it < steps) tile_g2s_3d(to + kTile + b * kAttnBlock, &p.k, 64 * b, kvh, key, smem_u32(full + s));
+                    }
                 }
                 if (*gone) {  // what is in flight has landed before the memory is let go
                     if (rows_sent) mbar_wait_bounded(q_full, 0, p.timeout_ns);
@@ -255,76 +258,60 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                 }
             }
         } else if (warp == kAttnProducts) {
+            // One thread for both tiles, first come first served: with a warp each
+            // their products share the tensor cores instruction by instruction,
+            // both end late, and 4 x 4096 took 550 us against 492.  What bounds it
+            // is this warp's own time, some 130 cycles a wait: one barrier for the
+            // values of a step and the keys of the next.
             constexpr uint32_t desc_s = mma_desc(kAttnRows, kAttnKeys, false, false);
             constexpr uint32_t desc_o = mma_desc(kAttnRows, D, false, true);
             auto wait = [&](uint64_t* bar, uint32_t parity) {
-                const bool ok = role_wait(bar, parity, gone, p.timeout_ns, p.status);
+                const bool ok = role_sleep(bar, parity, gone, p.timeout_ns, p.status);
                 return __all_sync(0xffffffffu, ok);
             };
-            auto slot = [&](int entry) { return smem_u32(ring + (entry % kAttnSlots) * kTile); };
-            auto score = [&](int i, int j) {  // S_i = Q_i K_j^T
-                if (elect_one()) {
-                    const uint32_t q = smem_u32(smem + i * kTile), k = slot(2 * j);
-#pragma unroll
-                    for (int b = 0; b < DB; ++b) {
-                        uint64_t da = operand_desc(q + b * kAttnBlock, false), db = operand_desc(k + b * kAttnBlock, false);
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            mma_bf16<1>(tmem + i * 128, da, db, desc_s, b + x > 0);
-                            da += k_step(false);
-                            db += k_step(false);
-                        }
-                    }
-                    mma_commit(smem_u32(s_full + i));
-                }
-                __syncwarp();
-            };
             bool ok = steps == 0 || wait(q_full, 0);
-            if (steps > 0 && ok && (ok = wait(full, 0))) {
-                tc_fence_after();
-                for (int i = 0; i < 2; ++i)
-                    if (n[i] > 0) score(i, 0);
-                if (elect_one()) mma_commit(smem_u32(empty));
-            }
-            for (int j = 0; j < steps && ok; ++j) {
-                const int v = 2 * j + 1, next = 2 * j + 2;
-                if (!(ok = wait(full + v % kAttnSlots, (v / kAttnSlots) & 1))) break;
+            for (int j = -1; steps > 0 && j < steps && ok; ++j) {
+                const int e = j + 1, s = e % kAttnSlots;
+                if (!(ok = wait(full + s, (e / kAttnSlots) & 1))) break;
+                uint8_t* const values = ring + s * 2 * kTile;
                 // rows of V behind the sequence belong to another, or to nobody:
                 // their probabilities are 0, but 0 times what lies there need not be
-                const int64_t left = (int64_t)a.m - (int64_t)(first + j) * kAttnKeys;
-                if (left < kAttnKeys) {
-                    for (int x = lane + (int)left * 8; x < kAttnKeys * 8; x += 32)
+                const int left = a.m - (first + j) * kAttnKeys;
+                if (j >= 0 && left < kAttnKeys) {
+                    for (int x = lane + left * 8; x < kAttnKeys * 8; x += 32)
 #pragma unroll
                         for (int b = 0; b < DB; ++b)
-                            *reinterpret_cast<uint4*>(ring + (v % kAttnSlots) * kTile + b * kAttnBlock + x * 16) =
-                                make_uint4(0, 0, 0, 0);
+                            *reinterpret_cast<uint4*>(values + b * kAttnBlock + x * 16) = make_uint4(0, 0, 0, 0);
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                 }
-                for (int i = 0; i < 2 && ok; ++i) {
-                    if (j < n[i]) {
-                        if (!(ok = wait(p_full + i, j & 1))) break;
-                        tc_fence_after();
-                        if (elect_one()) {
-                            uint64_t db = operand_desc_tall(slot(v), kAttnKeys);
+                const uint64_t dv = operand_desc_tall(smem_u32(values), kAttnKeys);
+                const uint64_t dk = operand_desc(smem_u32(values + kTile), false);
 #pragma unroll
-                            for (int x = 0; x < kAttnKeys / 16; ++x) {
-                                mma_bf16_ts(tmem + 256 + i * 128, tmem + i * 128 + 8 * x, db, desc_o, j > 0 || x > 0);
-                                db += k_step(true);
-                            }
+                for (int i = 0; i < 2; ++i) {
+                    if (j >= 0 && j < n[i] && !(ok = wait(p_full + i, j & 1))) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t s_at = tmem + i * 128, o_at = tmem + 256 + i * 128;
+                        if (j >= 0 && j < n[i]) {
+#pragma unroll
+                            for (int x = 0; x < kAttnKeys / 16; ++x)
+                                mma_bf16_ts(o_at, s_at + 8 * x, dv + x * k_step(true), desc_o, j > 0 || x > 0);
                             mma_commit(smem_u32(o_full + i));
                         }
-                        __syncwarp();
+                        if (j + 1 < n[i]) {  // S = Q K^T
+                            const uint64_t dq = operand_desc(smem_u32(smem + i * kTile), false);
+#pragma unroll
+                            for (int b = 0; b < DB; ++b)
+#pragma unroll
+                                for (int x = 0; x < 4; ++x)
+                                    mma_bf16<1>(s_at, dq + b * (kAttnBlock >> 4) + x * k_step(false),
+                                                dk + b * (kAttnBlock >> 4) + x * k_step(false), desc_s, b + x > 0);
+                            mma_commit(smem_u32(s_full + i));
+                        }
+                        if (i == 1) mma_commit(smem_u32(empty + s));
                     }
-                    if (j + 1 < n[i]) {
-                        if (!(ok = wait(full + next % kAttnSlots, (next / kAttnSlots) & 1))) break;
-                        tc_fence_after();
-                        score(i, j + 1);
-                    }
-                }
-                if (ok && elect_one()) {
-                    mma_commit(smem_u32(empty + v % kAttnSlots));
-                    if (j + 1 < steps) mma_commit(smem_u32(empty + next % kAttnSlots));
+                    __syncwarp();
                 }
             }
             if (elect_one()) {
@@ -366,7 +353,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
             const uint32_t s_at = mine + i * 128 + half * 64, p_at = mine + i * 128 + half * 32;
             bool together = true;
             for (int j = 0; j < n[i]; ++j) {
-                ok = ok && __all_sync(0xffffffffu, role_wait(s_full + i, j & 1, gone, p.timeout_ns, p.status));
+                ok = ok && __all_sync(0xffffffffu, role_sleep(s_full + i, j & 1, gone, p.timeout_ns, p.status));
                 tc_fence_after();
                 float s[2][32];
                 float larger = m, other;
@@ -405,7 +392,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                         m = larger;
                         if (j > 0) {
                             ok = __all_sync(0xffffffffu,
-                                            role_wait(o_full + i, (j - 1) & 1, gone, p.timeout_ns, p.status));
+                                            role_sleep(o_full + i, (j - 1) & 1, gone, p.timeout_ns, p.status));
                             if (!ok) continue;
                             tc_fence_after();
 #pragma unroll 1
@@ -434,15 +421,15 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                         }
                         tmem_st(p_at + 16 * c, w);
                     }
-                    l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                     tmem_wait_st();
+                    l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full + i);
             }
             if (together) {
-                ok = ok && __all_sync(0xffffffffu, role_wait(o_full + i, (n[i] - 1) & 1, gone, p.timeout_ns, p.status));
+                ok = ok && __all_sync(0xffffffffu, role_sleep(o_full + i, (n[i] - 1) & 1, gone, p.timeout_ns, p.status));
                 float other;
                 ok = exchange(n[i], l, other);
                 l = half ? other + l : l + other;

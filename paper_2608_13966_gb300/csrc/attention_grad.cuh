@@ -21,8 +21,11 @@
 // P and dS go through tensor memory as bf16, in the place of S and dP: each is
 // rounded once for its matrix product (2^-8 of it), sums are fp32.
 //
-// Warps: 0-3 and 4-7 make P and dS of every other step (a thread per row), 8
-// copies, 9 matrix instructions, 10 brings the columns' statistics (keys stay).
+// Warps: 0-7 and 8-15 make P and dS of every other step, two threads a row (with
+// one, their dependent instructions took 2,700 cycles a step, and 4 x 4096
+// causal, 32 heads of 128 over 8, 1815 us in all); 16 copies, 17 and 18 matrix
+// instructions (S and dv; dP and dk or dq), 19 brings the columns' statistics
+// (keys stay).
 // Tensor memory: two gradients of 128 columns, S and dP twice of 64.
 #pragma once
 
@@ -30,7 +33,8 @@
 
 namespace quasar {
 
-constexpr int kGradThreads = 352;
+constexpr int kGradThreads = 640;
+constexpr int kGradCopies = 16, kGradProducts = 17, kGradStats = 19;  // warps (of products two)
 constexpr int kGradSlots = 4;
 
 // The rows' statistics: 8 or 16 threads a (token, head) pair.
@@ -82,7 +86,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
     uint64_t* empty = full + kGradSlots;       // [slots]
     uint64_t* stat_full = empty + kGradSlots;  // [slots]
     uint64_t* s_full = stat_full + kGradSlots; // [2]
-    uint64_t* p_full = s_full + 2;             // [2]: 4 warps
+    uint64_t* p_full = s_full + 2;             // [2]: 8 warps
     uint64_t* acc_full = p_full + 2;
     uint64_t* never = acc_full + 1;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(never + 1);
@@ -96,20 +100,20 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
         mbar_init(x_full, 1);
         for (int s = 0; s < kGradSlots; ++s) {
             mbar_init(full + s, 1);
-            mbar_init(empty + s, 1);
+            mbar_init(empty + s, 2);
             mbar_init(stat_full + s, 1);
         }
         for (int b = 0; b < 2; ++b) {
-            mbar_init(s_full + b, 1);
-            mbar_init(p_full + b, 4);
+            mbar_init(s_full + b, 2);
+            mbar_init(p_full + b, 8);
         }
-        mbar_init(acc_full, 1);
+        mbar_init(acc_full, 2);
         mbar_init(never, 1);
         *gone = 0;
         mbar_init_fence();
     }
-    if (warp == 9) tmem_alloc<1>(tmem_slot, 512);
-    if (warp == 8 && lane == 0) {
+    if (warp == kGradProducts) tmem_alloc<1>(tmem_slot, 512);
+    if (warp == kGradCopies && lane == 0) {
         prefetch_map(&p.x1);
         prefetch_map(&p.x2);
         prefetch_map(&p.z1);
@@ -154,9 +158,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
         return KEYS ? min(p.step_tokens, a.n - f) * p.box_heads : min(kGradCols, a.m - f);
     };
 
-    if (warp == 8) {
+    if (warp == kGradCopies) {
         if (lane == 0) {
-            if (p.force_timeout_ns) role_wait(never, 0, gone, p.force_timeout_ns, p.status);
+            if (p.force_timeout_ns) role_sleep(never, 0, gone, p.force_timeout_ns, p.status);
             int it = 0;
             const bool rows_sent = steps > 0 && !*gone;
             if (rows_sent) {
@@ -170,7 +174,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
             const uint32_t bytes = 2 * DB * 128 * (KEYS ? (uint32_t)(p.step_tokens * p.box_heads) : kGradCols);
             for (; it < steps && !*gone; ++it) {
                 const int s = it % kGradSlots;
-                if (it >= kGradSlots && !role_wait(empty + s, (it / kGradSlots - 1) & 1, gone, p.timeout_ns, p.status))
+                if (it >= kGradSlots && !role_sleep(empty + s, (it / kGradSlots - 1) & 1, gone, p.timeout_ns, p.status))
                     break;
                 mbar_arrive_expect_tx(full + s, bytes);
                 for (int z = 0; z < 2; ++z)
@@ -185,27 +189,27 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                     mbar_wait_bounded(full + j % kGradSlots, (j / kGradSlots) & 1, p.timeout_ns);
             }
         }
-    } else if (warp == 9) {
+    } else if (warp - kGradProducts == 0 || warp - kGradProducts == 1) {
+        // g = 0: S = X1 Z1^T and, with P in its place, acc2 += P Z2;
+        // g = 1: dP = X2 Z2^T and, with dS in its place, acc1 += dS Z1
         constexpr uint32_t desc_s = mma_desc(kAttnRows, kGradCols, false, false);
         constexpr uint32_t desc_acc = mma_desc(kAttnRows, D, false, true);
+        const int g = warp - kGradProducts;
+        const uint32_t scores = tmem + (g ? kDp : kScores), acc = tmem + (g ? 0 : kAcc2);
         auto wait = [&](uint64_t* bar, uint32_t parity) {
-            const bool ok = role_wait(bar, parity, gone, p.timeout_ns, p.status);
+            const bool ok = role_sleep(bar, parity, gone, p.timeout_ns, p.status);
             return __all_sync(0xffffffffu, ok);
         };
-        // the gradients grow by step `it`
+        // the gradient grows by step `it`
         auto grow = [&](int it) {
             if (elect_one()) {
-                const int s = it % kGradSlots, buf = it & 1;
-                const uint32_t z = smem_u32(ring + s * kSlot);
+                const int s = it % kGradSlots;
+                if (KEYS || g == 1) {
+                    const uint64_t db = operand_desc(smem_u32(ring + s * kSlot) + (g ? 0 : kColTile), true);
+                    const uint32_t p_at = scores + (it & 1) * 64;
 #pragma unroll
-                for (int g = KEYS ? 1 : 0; g >= 0; --g) {
-                    uint64_t db = operand_desc(z + g * kColTile, true);
-#pragma unroll
-                    for (int x = 0; x < kGradCols / 16; ++x) {
-                        mma_bf16_ts(tmem + g * kAcc2, tmem + (g ? kScores : kDp) + buf * 64 + 8 * x, db, desc_acc,
-                                    it > 0 || x > 0);
-                        db += k_step(true);
-                    }
+                    for (int x = 0; x < kGradCols / 16; ++x)
+                        mma_bf16_ts(acc, p_at + x / 2 * 32 + x % 2 * 8, db + x * k_step(true), desc_acc, it > 0 || x > 0);
                 }
                 mma_commit(smem_u32(empty + s));
             }
@@ -216,6 +220,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
             const int s = it % kGradSlots, buf = it & 1;
             if (!(ok = wait(full + s, (it / kGradSlots) & 1))) break;
             // columns behind the sequence belong to another, or to nobody: zeros
+            // (both warps write them, each before its own reads)
             const int cols = cols_of(it);
             if (cols < kGradCols) {
                 for (int x = lane + cols * 8; x < kGradCols * 8; x += 32)
@@ -227,19 +232,13 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
             }
             tc_fence_after();
             if (elect_one()) {
+                const uint32_t x = smem_u32(smem + g * kRowTile), z = smem_u32(ring + s * kSlot + g * kColTile);
 #pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const uint32_t x = smem_u32(smem + g * kRowTile), z = smem_u32(ring + s * kSlot + g * kColTile);
+                for (int b = 0; b < DB; ++b) {
+                    const uint64_t da = operand_desc(x + b * kAttnBlock, false), db = operand_desc(z + b * kColBlock, false);
 #pragma unroll
-                    for (int b = 0; b < DB; ++b) {
-                        uint64_t da = operand_desc(x + b * kAttnBlock, false), db = operand_desc(z + b * kColBlock, false);
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            mma_bf16<1>(tmem + (g ? kDp : kScores) + buf * 64, da, db, desc_s, b + y > 0);
-                            da += k_step(false);
-                            db += k_step(false);
-                        }
-                    }
+                    for (int y = 0; y < 4; ++y)
+                        mma_bf16<1>(scores + buf * 64, da + y * k_step(false), db + y * k_step(false), desc_s, b + y > 0);
                 }
                 mma_commit(smem_u32(s_full + buf));
             }
@@ -258,7 +257,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
             mma_commit(smem_u32(acc_full));
             mbar_wait_bounded(acc_full, 0, p.timeout_ns);
         }
-    } else if (warp == 10) {
+    } else if (warp == kGradStats) {
         if (KEYS)
             for (int it = 0; it < steps; ++it) {
                 const int s = it % kGradSlots, cols = cols_of(it);
@@ -269,8 +268,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                     const int c = lane + 32 * q;  // behind the sequence: p = 0
                     st[q] = c < cols ? p.stats[at + (int64_t)(c / p.box_heads) * p.heads + c % p.box_heads]
                                      : make_float2(-minus_inf(), 0.0f);
+                    st[q] = make_float2(-st[q].x, -st[q].y);  // (as they are added)
                 }
-                bool ok = it < kGradSlots || role_wait(empty + s, (it / kGradSlots - 1) & 1, gone, p.timeout_ns, p.status);
+                bool ok = it < kGradSlots || role_sleep(empty + s, (it / kGradSlots - 1) & 1, gone, p.timeout_ns, p.status);
                 ok = __all_sync(0xffffffffu, ok && !*gone);
                 if (!ok) break;
 #pragma unroll
@@ -279,91 +279,96 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                 if (lane == 0) mbar_arrive(stat_full + s);
             }
     } else {
-        const int wg = warp >> 2, r = (warp & 3) * 32 + lane;
+        // turn: of every other step; half: of its columns, whose P and dS lie where
+        // this half of S and dP lay
+        const int turn = warp >> 3, half = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
         const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         // the row: key row0 + r, or (token, head)
         const int token = row0 + r / p.group, head = kvh * p.group + r % p.group;
         const bool live = a.spares == 0 && (KEYS ? row0 + r < a.m : r < p.tile_tokens * p.group && token < a.n);
         const bool any_live = __any_sync(0xffffffffu, live);
-        float2 own = make_float2(-minus_inf(), 0.0f);
-        if (!KEYS && live) own = p.stats[(int64_t)(a.q0 + token) * p.heads + head];
+        float2 own = make_float2(minus_inf(), 0.0f);  // both negative
+        if (!KEYS && live) {
+            own = p.stats[(int64_t)(a.q0 + token) * p.heads + head];
+            own = make_float2(-own.x, -own.y);
+        }
+        // of the sequence's columns, the first that sees the row's key; the last
+        // key that the row's token sees
+        const int64_t from = KEYS && p.causal ? (int64_t)row0 + r - shift : 0;
+        const int64_t upto = p.causal ? min((int64_t)a.m - 1, (int64_t)token + shift) : (int64_t)a.m - 1;
         bool ok = true;
-        for (int it = wg; it < steps; it += 2) {
+        for (int it = turn; it < steps; it += 2) {
             const int s = it % kGradSlots;
-            ok = role_wait(s_full + wg, (it / 2) & 1, gone, p.timeout_ns, p.status);
-            if (KEYS && ok) ok = role_wait(stat_full + s, (it / kGradSlots) & 1, gone, p.timeout_ns, p.status);
+            ok = role_sleep(s_full + turn, (it / 2) & 1, gone, p.timeout_ns, p.status);
+            if (KEYS && ok) ok = role_sleep(stat_full + s, (it / kGradSlots) & 1, gone, p.timeout_ns, p.status);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
             if (any_live) {
-                const uint32_t s_at = mine + kScores + wg * 64, dp_at = mine + kDp + wg * 64;
-                // the columns [lo, hi] that the row sees (or that see it)
-                int lo = 0, hi = kGradCols - 1;
+                const uint32_t s_at = mine + kScores + turn * 64 + half * 32, dp_at = mine + kDp + turn * 64 + half * 32;
+                // the columns [lo, hi] of this half that the row sees (or that see it)
+                int lo = 0, hi = 31;
                 const int f = first_of(it);
                 if (KEYS && p.causal)
-                    lo = (int)max((int64_t)0, min((int64_t)kGradCols, ((int64_t)row0 + r - shift - f) * p.box_heads));
-                if (!KEYS)
-                    hi = (int)max((int64_t)-1, min((int64_t)kGradCols - 1,
-                                                   (p.causal ? min((int64_t)a.m - 1, (int64_t)token + shift) : a.m - 1) - (int64_t)f));
-                const bool masked = !__all_sync(0xffffffffu, lo == 0 && hi == kGradCols - 1);
-                const float2* st = col_stats + s * kGradCols;
+                    lo = (int)max((int64_t)0, min((int64_t)32, (from - f) * p.box_heads - half * 32));
+                if (!KEYS) hi = (int)max((int64_t)-1, min((int64_t)31, upto - f - half * 32));
+                const bool masked = !__all_sync(0xffffffffu, lo == 0 && hi == 31);
+                const float2* st = col_stats + s * kGradCols + half * 32;
                 const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float sc[32], dp[32];
-                    tmem_ld(s_at + 32 * h, sc);
-                    tmem_ld(dp_at + 32 * h, dp);
+                    float sc[16], dp[16];
+                    tmem_ld(s_at + 16 * h, sc);
+                    tmem_ld(dp_at + 16 * h, dp);
                     tmem_wait_ld(sc);
                     tmem_wait_ld(dp);
-                    uint32_t pw[16], dw[16];
+                    uint32_t pw[8], dw[8];
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        float2 lse, delta;
+                    for (int x = 0; x < 8; ++x) {
+                        float2 lse = make_float2(own.x, own.x), delta = make_float2(own.y, own.y);
                         if (KEYS) {
-                            const float4 two = *reinterpret_cast<const float4*>(st + 32 * h + 2 * x);
-                            lse = make_float2(-two.x, -two.z);
-                            delta = make_float2(-two.y, -two.w);
-                        } else {
-                            lse = make_float2(-own.x, -own.x);
-                            delta = make_float2(-own.y, -own.y);
+                            const float4 two = *reinterpret_cast<const float4*>(st + 16 * h + 2 * x);
+                            lse = make_float2(two.x, two.z);
+                            delta = make_float2(two.y, two.w);
                         }
                         float2 e = __ffma2_rn(make_float2(sc[2 * x], sc[2 * x + 1]), scale2, lse);
                         e.x = exp2_fast(e.x);
                         e.y = exp2_fast(e.y);
                         float2 ds = __fmul2_rn(e, __fadd2_rn(make_float2(dp[2 * x], dp[2 * x + 1]), delta));
                         if (masked) {
-                            const int c = 32 * h + 2 * x;
+                            const int c = 16 * h + 2 * x;
                             if (c < lo || c > hi) e.x = 0.0f, ds.x = 0.0f;
                             if (c + 1 < lo || c + 1 > hi) e.y = 0.0f, ds.y = 0.0f;
                         }
                         pw[x] = pack_bf16x2(e.x, e.y);
                         dw[x] = pack_bf16x2(ds.x, ds.y);
                     }
-                    // (the first half's words lie in columns that are read by now)
-                    if (KEYS) tmem_st(s_at + 16 * h, pw);
-                    tmem_st(dp_at + 16 * h, dw);
+                    // (columns that this thread has read)
+                    if (KEYS) tmem_st(s_at + 8 * h, pw);
+                    tmem_st(dp_at + 8 * h, dw);
                 }
                 tmem_wait_st();
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(p_full + wg);
+            if (lane == 0) mbar_arrive(p_full + turn);
         }
         if (ok && steps > 0) {
-            ok = __all_sync(0xffffffffu, role_wait(acc_full, 0, gone, p.timeout_ns, p.status)) && !*gone;
+            ok = role_sleep(acc_full, 0, gone, p.timeout_ns, p.status) && !*gone;
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
         }
-        // dk or dq by warps 0-3, dv by warps 4-7, through the rows' memory so
-        // that a store covers whole rows
-        if (ok && any_live && (KEYS || wg == 0)) {
-            const float scale = wg == 0 ? p.scale : 1.0f;
-            uint8_t* stage = smem + wg * kRowTile + (warp & 3) * 32 * D * 2;
+        // dk or dq by warps 0-7, dv by warps 8-15, half of the columns each,
+        // through the rows' memory so that a store covers whole rows
+        if (ok && any_live && (KEYS || turn == 0)) {
+            constexpr int kHalf = D / 2;
+            const float scale = turn == 0 ? p.scale : 1.0f;
+            uint8_t* stage = smem + turn * kRowTile + (warp & 3) * 32 * D * 2;
 #pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
+            for (int c = half * kHalf; c < (half + 1) * kHalf; c += 32) {
                 float o[32];
                 if (steps > 0) {
-                    tmem_ld(mine + wg * kAcc2 + c, o);
+                    tmem_ld(mine + turn * kAcc2 + c, o);
                     tmem_wait_ld(o);
                 } else {
 #pragma unroll
@@ -376,11 +381,11 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                                    pack_bf16x2(o[x + 4] * scale, o[x + 5] * scale), pack_bf16x2(o[x + 6] * scale, o[x + 7] * scale));
             }
             __syncwarp();
-            constexpr int kLanes = D / 8;  // of a row
-            __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(wg == 0 ? p.d1 : p.d2);
-            const int64_t ld = wg == 0 ? p.ld_d1 : p.ld_d2;
+            constexpr int kLanes = kHalf / 8;  // of a row
+            __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(turn == 0 ? p.d1 : p.d2);
+            const int64_t ld = turn == 0 ? p.ld_d1 : p.ld_d2;
             for (int q = 0; q < 32; q += 32 / kLanes) {
-                const int row = q + lane / kLanes, chunk = lane % kLanes;
+                const int row = q + lane / kLanes, chunk = half * kLanes + lane % kLanes;
                 const int rr = (warp & 3) * 32 + row;
                 int64_t at;
                 bool in = chunk * 8 < p.d;
@@ -410,7 +415,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) tmem_free<1>(tmem, 512);
+    if (warp == kGradProducts) tmem_free<1>(tmem, 512);
 }
 
 }  // namespace quasar

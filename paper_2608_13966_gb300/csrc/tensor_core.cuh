@@ -240,6 +240,32 @@ __device__ __forceinline__ void tmem_st(uint32_t addr, const uint32_t (&v)[32])
         : "memory");
 }
 
+__device__ __forceinline__ void tmem_ld(uint32_t addr, float (&v)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+          "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+        : "r"(addr));
+}
+
+__device__ __forceinline__ void tmem_wait_ld(float (&v)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]),
+      "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]),
+      "+f"(v[13]), "+f"(v[14]), "+f"(v[15])::"memory");
+}
+
+__device__ __forceinline__ void tmem_st(uint32_t addr, const uint32_t (&v)[8])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+        : "memory");
+}
+
 // One lane of a converged warp.  Matrix instructions take their addresses and
 // descriptors from uniform registers: issued under `lane == 0` and with values
 // that are not known to be the warp's, each cost some 120 cycles of moves, twice
@@ -277,6 +303,20 @@ __device__ __forceinline__ void registers_down()
 
 // -- waits -------------------------------------------------------------------
 
+// A try that may suspend the thread for up to `ns` before it gives up.
+__device__ __forceinline__ bool mbar_try_wait_for(uint64_t* bar, uint32_t parity, uint32_t ns)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity), "r"(ns)
+        : "memory");
+    return ok != 0;
+}
+
 // Wait for a phase of `bar`; gives up when limit_ns have passed or another
 // role of this CTA gave up (`*gone`), and then says so to the others.
 __device__ __forceinline__ bool role_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* gone,
@@ -288,6 +328,24 @@ __device__ __forceinline__ bool role_wait(uint64_t* bar, uint32_t parity, volati
 #pragma unroll 1
         for (int i = 0; i < 16; ++i)
             if (mbar_try_wait(bar, parity)) return true;
+        if (*gone) return false;
+        if (global_timer_ns() - t0 > limit_ns) {
+            *gone = 1;
+            record_timeout(status);
+            return false;
+        }
+    }
+}
+
+// The same for warps that share their scheduler with busy ones: the thread
+// sleeps instead of asking again and again.
+__device__ __forceinline__ bool role_sleep(uint64_t* bar, uint32_t parity, volatile uint32_t* gone,
+                                           uint64_t limit_ns, unsigned int* status)
+{
+    if (mbar_try_wait_for(bar, parity, 20000)) return true;
+    const uint64_t t0 = global_timer_ns();
+    for (;;) {
+        if (mbar_try_wait_for(bar, parity, 20000)) return true;
         if (*gone) return false;
         if (global_timer_ns() - t0 > limit_ns) {
             *gone = 1;
