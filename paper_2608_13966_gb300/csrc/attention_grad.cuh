@@ -151,11 +151,21 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
         }
     }
     const int steps = uniform(per_run * runs);  // (at most tokens x heads, or keys: checked by the host)
-    // a step's first token (or key), its run, and its columns of the sequence
-    auto first_of = [&](int it) { return KEYS ? (step0 + it % per_run) * p.step_tokens : it * kGradCols; };
-    auto cols_of = [&](int it) {
-        const int f = first_of(it);
-        return KEYS ? min(p.step_tokens, a.n - f) * p.box_heads : min(kGradCols, a.m - f);
+    // A walk over the steps: their first token (or key) and run, without a
+    // division a step.
+    struct Walk {
+        int first, run, begin, end, by;
+        __device__ void next()
+        {
+            first += by;
+            if (first >= end) first = begin, ++run;
+        }
+    };
+    const Walk walk{KEYS ? step0 * p.step_tokens : 0, 0, KEYS ? step0 * p.step_tokens : 0, KEYS ? a.n : a.m,
+                    KEYS ? p.step_tokens : kGradCols};
+    // columns of a step that are the sequence's
+    auto cols_of = [&](const Walk& w) {
+        return KEYS ? min(p.step_tokens, a.n - w.first) * p.box_heads : min(kGradCols, a.m - w.first);
     };
 
     if (warp == kGradCopies) {
@@ -172,7 +182,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                                     KEYS ? kvh : kvh * p.group, (KEYS ? a.k0 : a.q0) + row0, smem_u32(x_full));
             }
             const uint32_t bytes = 2 * DB * 128 * (KEYS ? (uint32_t)(p.step_tokens * p.box_heads) : kGradCols);
-            for (; it < steps && !*gone; ++it) {
+            Walk w = walk;
+            for (; it < steps && !*gone; ++it, w.next()) {
                 const int s = it % kGradSlots;
                 if (it >= kGradSlots && !role_sleep(empty + s, (it / kGradSlots - 1) & 1, gone, p.timeout_ns, p.status))
                     break;
@@ -180,8 +191,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                 for (int z = 0; z < 2; ++z)
                     for (int b = 0; b < DB; ++b)
                         tile_g2s_3d(smem_u32(ring + s * kSlot + z * kColTile + b * kColBlock), z ? &p.z2 : &p.z1, 64 * b,
-                                    KEYS ? kvh * p.group + it / per_run * p.box_heads : kvh,
-                                    (KEYS ? a.q0 : a.k0) + first_of(it), smem_u32(full + s));
+                                    KEYS ? kvh * p.group + w.run * p.box_heads : kvh,
+                                    (KEYS ? a.q0 : a.k0) + w.first, smem_u32(full + s));
             }
             if (*gone) {  // what is in flight has landed before the memory is let go
                 if (rows_sent) mbar_wait_bounded(x_full, 0, p.timeout_ns);
@@ -216,12 +227,13 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
             __syncwarp();
         };
         bool ok = steps == 0 || wait(x_full, 0);
-        for (int it = 0; it < steps && ok; ++it) {
+        Walk w = walk;
+        for (int it = 0; it < steps && ok; ++it, w.next()) {
             const int s = it % kGradSlots, buf = it & 1;
             if (!(ok = wait(full + s, (it / kGradSlots) & 1))) break;
             // columns behind the sequence belong to another, or to nobody: zeros
             // (both warps write them, each before its own reads)
-            const int cols = cols_of(it);
+            const int cols = cols_of(w);
             if (cols < kGradCols) {
                 for (int x = lane + cols * 8; x < kGradCols * 8; x += 32)
 #pragma unroll
@@ -258,15 +270,18 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
             mbar_wait_bounded(acc_full, 0, p.timeout_ns);
         }
     } else if (warp == kGradStats) {
-        if (KEYS)
-            for (int it = 0; it < steps; ++it) {
-                const int s = it % kGradSlots, cols = cols_of(it);
-                const int64_t at = (int64_t)(a.q0 + first_of(it)) * p.heads + kvh * p.group + it / per_run * p.box_heads;
+        if (KEYS) {
+            Walk w = walk;
+            const int place[2] = {lane / p.box_heads * p.heads + lane % p.box_heads,
+                                  (lane + 32) / p.box_heads * p.heads + (lane + 32) % p.box_heads};
+            for (int it = 0; it < steps; ++it, w.next()) {
+                const int s = it % kGradSlots, cols = cols_of(w);
+                const int64_t at = (int64_t)(a.q0 + w.first) * p.heads + kvh * p.group + w.run * p.box_heads;
                 float2 st[2];
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
                     const int c = lane + 32 * q;  // behind the sequence: p = 0
-                    st[q] = c < cols ? p.stats[at + (int64_t)(c / p.box_heads) * p.heads + c % p.box_heads]
+                    st[q] = c < cols ? p.stats[at + place[q]]
                                      : make_float2(-minus_inf(), 0.0f);
                     st[q] = make_float2(-st[q].x, -st[q].y);  // (as they are added)
                 }
@@ -278,6 +293,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                 __syncwarp();
                 if (lane == 0) mbar_arrive(stat_full + s);
             }
+        }
     } else {
         // turn: of every other step; half: of its columns, whose P and dS lie where
         // this half of S and dP lay
@@ -297,7 +313,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
         const int64_t from = KEYS && p.causal ? (int64_t)row0 + r - shift : 0;
         const int64_t upto = p.causal ? min((int64_t)a.m - 1, (int64_t)token + shift) : (int64_t)a.m - 1;
         bool ok = true;
-        for (int it = turn; it < steps; it += 2) {
+        Walk w = walk;
+        if (turn) w.next();
+        for (int it = turn; it < steps; it += 2, w.next(), w.next()) {
             const int s = it % kGradSlots;
             ok = role_sleep(s_full + turn, (it / 2) & 1, gone, p.timeout_ns, p.status);
             if (KEYS && ok) ok = role_sleep(stat_full + s, (it / kGradSlots) & 1, gone, p.timeout_ns, p.status);
@@ -308,7 +326,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                 const uint32_t s_at = mine + kScores + turn * 64 + half * 32, dp_at = mine + kDp + turn * 64 + half * 32;
                 // the columns [lo, hi] of this half that the row sees (or that see it)
                 int lo = 0, hi = 31;
-                const int f = first_of(it);
+                const int f = w.first;
                 if (KEYS && p.causal)
                     lo = (int)max((int64_t)0, min((int64_t)32, (from - f) * p.box_heads - half * 32));
                 if (!KEYS) hi = (int)max((int64_t)-1, min((int64_t)31, upto - f - half * 32));

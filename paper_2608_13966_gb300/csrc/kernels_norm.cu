@@ -9,19 +9,23 @@ struct Shape {
     int t, nv;  // threads a row, vectors of 8 a thread
 };
 
-// Short rows share a CTA of 256 threads; from 129 vectors on a row has a CTA.
-Shape norm_shape(int64_t cols)
+// Short rows share a CTA of 256 threads; from 65 vectors on a row has a CTA, of
+// up to 4 vectors a thread (backward, where a vector takes more registers: 2).
+Shape norm_shape(int64_t cols, bool grad)
 {
     const int64_t vecs = (cols + 7) / 8;
     if (vecs <= 8) return {8, 1};
     if (vecs <= 16) return {8, 2};
     if (vecs <= 32) return {32, 1};
     if (vecs <= 64) return {32, 2};
-    if (vecs <= 128) return {32, 4};
-    if (vecs <= 256) return {256, 1};
-    if (vecs <= 512) return {512, 1};
-    if (vecs <= 1024) return {512, 2};
-    return {512, 4};
+    if (vecs <= 128) return {128, 1};
+    if (vecs <= 256) return {128, 2};
+    if (!grad) {
+        if (vecs <= 512) return {128, 4};
+        return vecs <= 1024 ? Shape{256, 4} : Shape{512, 4};
+    }
+    if (vecs <= 512) return {256, 2};
+    return vecs <= 1024 ? Shape{512, 2} : Shape{512, 4};
 }
 
 template <int T, int NV>
@@ -49,22 +53,29 @@ const void* backward(bool vectors, bool wide)
 const void* layer_norm_kernel(int64_t cols, bool vectors, bool grad, bool wide, int* threads, int* rows, int* per_sm)
 {
     if (cols > kNormMostCols) return nullptr;
-    const Shape s = norm_shape(cols);
-    *threads = s.t < 256 ? 256 : s.t;
+    const Shape s = norm_shape(cols, grad);
+    *threads = s.t < 128 ? 256 : s.t;
     *rows = *threads / s.t;
-    *per_sm = s.nv == 1 ? 1024 / *threads : 512 / *threads;
+    *per_sm = (s.nv == 1 ? 768 : 512) / *threads;
 #define QUASAR_NORM(T, NV) \
     if (s.t == T && s.nv == NV) return grad ? backward<T, NV>(vectors, wide) : forward<T, NV>(vectors);
+#define QUASAR_NORM_FORWARD(T, NV) \
+    if (s.t == T && s.nv == NV) return forward<T, NV>(vectors);
     QUASAR_NORM(8, 1)
     QUASAR_NORM(8, 2)
     QUASAR_NORM(32, 1)
     QUASAR_NORM(32, 2)
-    QUASAR_NORM(32, 4)
-    QUASAR_NORM(256, 1)
-    QUASAR_NORM(512, 1)
-    QUASAR_NORM(512, 2)
+    QUASAR_NORM(128, 1)
+    QUASAR_NORM(128, 2)
     QUASAR_NORM(512, 4)
+    if (grad) {
+        if (s.t == 256) return backward<256, 2>(vectors, wide);
+        return backward<512, 2>(vectors, wide);
+    }
+    QUASAR_NORM_FORWARD(128, 4)
+    QUASAR_NORM_FORWARD(256, 4)
 #undef QUASAR_NORM
+#undef QUASAR_NORM_FORWARD
     return nullptr;
 }
 

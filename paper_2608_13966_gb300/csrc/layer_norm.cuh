@@ -9,10 +9,9 @@
 //
 // Bound by memory: a row is read once and kept in registers.  T threads share
 // a row, NV times 8 elements each; 8 or 32 threads where rows are short (a CTA
-// then takes 32 or 8 of them at a time), a whole CTA else.  CTAs are
-// persistent, so that a thread's columns stay the same: their weights are read
-// once, and dw and db accumulate in registers over the CTA's rows.  The next
-// row is on its way while one is worked on.
+// then takes 32 or 8 of them at a time), a whole CTA else.  The backward
+// kernel's CTAs are persistent, so that a thread's columns stay the same and dw
+// and db accumulate in registers over the CTA's rows.
 //
 // The variance is summed about the mean: of each warp's elements about their
 // own mean, the warps' then joined (M2 = sum M2_w + n_w (mean_w - mean)^2),
@@ -25,7 +24,11 @@
 namespace quasar {
 
 template <int T>
-constexpr int kNormThreads = T < 256 ? 256 : T;
+constexpr int kNormThreads = T < 128 ? 256 : T;
+
+// CTAs an SM of the backward kernel, by its registers.
+template <int T, int NV>
+constexpr int kNormPerSm = (NV == 1 ? 768 : 512) / kNormThreads<T>;  // 512 threads have 128 each
 
 // Sum over the W (at most 32) threads of an aligned part of a warp.
 template <int W>
@@ -38,86 +41,83 @@ __device__ __forceinline__ float lanes_sum(float x)
 
 // -- forward ---------------------------------------------------------------------
 
-// 16384 x 4096 bf16 with weight and bias: see the figures at the launch.
+// Several CTAs an SM, no more than a row each in hand, keep the memory busy; the
+// weights come from L1 (kept in registers by persistent CTAs of 512 threads
+// that fetched their next row ahead, two an SM, 16384 x 4096 took 79 us).
 template <int T, int NV, bool VECTORS>
-__global__ void __launch_bounds__(kNormThreads<T>, NV == 1 ? 1024 / kNormThreads<T> : 512 / kNormThreads<T>)
-    k_layer_norm(const __grid_constant__ NormParams p)
+__global__ void __launch_bounds__(kNormThreads<T>, 1024 / kNormThreads<T>) k_layer_norm(const __grid_constant__ NormParams p)
 {
     constexpr int kGroups = kNormThreads<T> / T, kWarps = T / 32, kLanes = T < 32 ? T : 32;
-    __shared__ float2 red[2][T > 32 ? kWarps : 1];
-    __shared__ float counts[T > 32 ? kWarps : 1];
+    __shared__ float2 red[T > 32 ? kWarps : 1];
     const int t = threadIdx.x % T, lane = threadIdx.x & 31;
     const bool whole = p.cols == (int64_t)T * NV * 8;
     const float cols = (float)p.cols;
-
-    float mine = 0.0f;  // this warp's elements (its part of the row)
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) mine += row_at<T, VECTORS>(t, j, i) < p.cols ? 1.0f : 0.0f;
-    mine = lanes_sum<kLanes>(mine);
-    if (T > 32 && lane == 0) counts[threadIdx.x >> 5] = mine;
+    const int64_t row = (int64_t)blockIdx.x * kGroups + threadIdx.x / T;
+    const bool live = row < p.rows;
     wait_for_previous_grid();
 
-    float w[NV][8], b[NV][8];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        load_floats<T, VECTORS>(w[j], p.weight, t, j, p.cols, 1.0f);
-        load_floats<T, VECTORS>(b[j], p.bias, t, j, p.cols, 0.0f);
-    }
-    const int64_t step = (int64_t)gridDim.x * kGroups;
-    int64_t row = (int64_t)blockIdx.x * kGroups + threadIdx.x / T;
     Raw8<true> raw[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j)
-        load_raw<T, VECTORS>(raw[j], row_of(p.x, p.x_f32, row, p.ld_x), p.x_f32, t, j, row < p.rows ? p.cols : 0);
-    int turn = 0;
-    for (int64_t first = (int64_t)blockIdx.x * kGroups; first < p.rows; first += step, row += step, turn ^= 1) {
-        float v[NV][8];
-        float sum = 0.0f;
+        load_raw<T, VECTORS>(raw[j], row_of(p.x, p.x_f32, row, p.ld_x), p.x_f32, t, j, live ? p.cols : 0);
+    float v[NV][8];
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        unpack_raw(raw[j], p.x_f32, v[j]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += v[j][i];
+    }
+    float n = cols;  // this warp's elements (its part of the row)
+    if (T > 32) {
+        n = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            unpack_raw(raw[j], p.x_f32, v[j]);
+            const int64_t left = p.cols - row_at<T, VECTORS>(t & ~31, j, 0);
+            if (VECTORS)
+                n += (float)max((int64_t)0, min((int64_t)256, left));
+            else
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum += v[j][i];
+                for (int i = 0; i < 8; ++i) n += (float)max((int64_t)0, min((int64_t)32, left - (int64_t)i * T));
         }
+    }
+    // (divisions: a row of one value then has no variance at all)
+    float mean = p.center && n > 0.0f ? lanes_sum<kLanes>(sum) / n : 0.0f;
+    float m2 = 0.0f;
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-            load_raw<T, VECTORS>(raw[j], row_of(p.x, p.x_f32, row + step, p.ld_x), p.x_f32, t, j,
-                                 row + step < p.rows ? p.cols : 0);
-        // (divisions: a row of one value then has no variance at all)
-        float mean = p.center && mine > 0.0f ? lanes_sum<kLanes>(sum) / mine : 0.0f;
-        float m2 = 0.0f;
+    for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float d = whole || row_at<T, VECTORS>(t, j, i) < p.cols ? v[j][i] - mean : 0.0f;
-                m2 = fmaf(d, d, m2);
-            }
-        m2 = lanes_sum<kLanes>(m2);
-        if constexpr (T > 32) {
-            if (lane == 0) red[turn][threadIdx.x >> 5] = make_float2(mean, m2);
-            __syncthreads();
-            const float2 part = lane < kWarps ? red[turn][lane] : make_float2(0.0f, 0.0f);
-            const float n = lane < kWarps ? counts[lane] : 0.0f;
-            mean = lanes_sum<32>(n * part.x) / cols;
-            const float d = part.x - mean;
-            m2 = lanes_sum<32>(fmaf(n * d, d, part.y));
+        for (int i = 0; i < 8; ++i) {
+            const float d = whole || row_at<T, VECTORS>(t, j, i) < p.cols ? v[j][i] - mean : 0.0f;
+            m2 = fmaf(d, d, m2);
         }
-        const float rstd = rsqrtf(m2 / cols + p.eps);
-        if (row < p.rows) {
+    m2 = lanes_sum<kLanes>(m2);
+    if constexpr (T > 32) {
+        __shared__ float counts[kWarps];
+        if (lane == 0) red[threadIdx.x >> 5] = make_float2(mean, m2), counts[threadIdx.x >> 5] = n;
+        __syncthreads();
+        const float2 part = lane < kWarps ? red[lane] : make_float2(0.0f, 0.0f);
+        n = lane < kWarps ? counts[lane] : 0.0f;
+        mean = lanes_sum<kWarps>(n * part.x) / cols;
+        const float d = part.x - mean;
+        m2 = lanes_sum<kWarps>(fmaf(n * d, d, part.y));
+        mean = __shfl_sync(0xffffffffu, mean, 0);  // (of the lanes that hold a warp's part)
+        m2 = __shfl_sync(0xffffffffu, m2, 0);
+    }
+    const float rstd = rsqrtf(m2 / cols + p.eps);
+    if (!live) return;
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
+    for (int j = 0; j < NV; ++j) {
+        float w[8], b[8];
+        load_floats<T, VECTORS>(w, p.weight, t, j, p.cols, 1.0f);
+        load_floats<T, VECTORS>(b, p.bias, t, j, p.cols, 0.0f);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[j][i] = fmaf((v[j][i] - mean) * rstd, w[j][i], b[j][i]);
-                store_row<T, VECTORS>(row_of(p.y, p.y_f32, row, p.ld_y), p.y_f32, t, j, p.cols, v[j]);
-            }
-            if (p.stats && t == 0) {
-                p.stats[2 * row] = mean;
-                p.stats[2 * row + 1] = rstd;
-            }
-        }
+        for (int i = 0; i < 8; ++i) v[j][i] = fmaf((v[j][i] - mean) * rstd, w[i], b[i]);
+        store_row<T, VECTORS>(row_of(p.y, p.y_f32, row, p.ld_y), p.y_f32, t, j, p.cols, v[j]);
+    }
+    if (p.stats && t == 0) {
+        p.stats[2 * row] = mean;
+        p.stats[2 * row + 1] = rstd;
     }
 }
 
@@ -182,8 +182,10 @@ __global__ void __launch_bounds__(512) k_layer_norm_long(const __grid_constant__
 
 // -- backward --------------------------------------------------------------------
 
+// A row's elements stay as they lie in memory between the two passes over
+// them; dw and db take the registers.
 template <int T, int NV, bool VECTORS, bool WIDE>
-__global__ void __launch_bounds__(kNormThreads<T>, NV == 1 ? 1024 / kNormThreads<T> : 512 / kNormThreads<T>)
+__global__ void __launch_bounds__(kNormThreads<T>, kNormPerSm<T, NV>)
     k_layer_norm_grad(const __grid_constant__ NormGradParams p)
 {
     constexpr int kGroups = kNormThreads<T> / T, kWarps = T / 32, kLanes = T < 32 ? T : 32;
@@ -193,48 +195,44 @@ __global__ void __launch_bounds__(kNormThreads<T>, NV == 1 ? 1024 / kNormThreads
     const float per = 1.0f / (float)p.cols;
     wait_for_previous_grid();
 
-    float w[NV][8], dw[NV][8], db[NV][8];
+    float dw[NV][8], db[NV][8];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        load_floats<T, VECTORS>(w[j], p.weight, t, j, p.cols, 1.0f);
+    for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < 8; ++i) dw[j][i] = db[j][i] = 0.0f;
-    }
     const int64_t step = (int64_t)gridDim.x * kGroups;
     int64_t row = (int64_t)blockIdx.x * kGroups + threadIdx.x / T;
-    Raw8<WIDE> raw_x[NV], raw_dy[NV];
-    float2 stat = make_float2(0.0f, 0.0f);
-    auto fetch = [&](int64_t r) {
-        const int64_t cols = r < p.rows ? p.cols : 0;
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            load_raw<T, VECTORS>(raw_x[j], row_of(p.x, p.x_f32, r, p.ld_x), p.x_f32, t, j, cols);
-            load_raw<T, VECTORS>(raw_dy[j], row_of(p.dy, p.dy_f32, r, p.ld_dy), p.dy_f32, t, j, cols);
-        }
-        stat = r < p.rows ? make_float2(p.stats[2 * r], p.stats[2 * r + 1]) : make_float2(0.0f, 0.0f);
-    };
-    fetch(row);
     int turn = 0;
     for (int64_t first = (int64_t)blockIdx.x * kGroups; first < p.rows; first += step, row += step, turn ^= 1) {
-        const float mean = p.center ? stat.x : 0.0f, rstd = stat.y;
-        float xh[NV][8], u[NV][8];
+        const bool live = row < p.rows;
+        Raw8<WIDE> raw_x[NV], raw_dy[NV], raw_res[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            load_raw<T, VECTORS>(raw_x[j], row_of(p.x, p.x_f32, row, p.ld_x), p.x_f32, t, j, live ? p.cols : 0);
+            load_raw<T, VECTORS>(raw_dy[j], row_of(p.dy, p.dy_f32, row, p.ld_dy), p.dy_f32, t, j, live ? p.cols : 0);
+            if (p.residual)
+                load_raw<T, VECTORS>(raw_res[j], row_of(p.residual, p.dx_f32, row, p.ld_res), p.dx_f32, t, j,
+                                     live ? p.cols : 0);
+        }
+        const float mean = live && p.center ? p.stats[2 * row] : 0.0f, rstd = live ? p.stats[2 * row + 1] : 0.0f;
         float su = 0.0f, sux = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            unpack_raw(raw_x[j], p.x_f32, xh[j]);
-            unpack_raw(raw_dy[j], p.dy_f32, u[j]);
+            float x[8], u[8], w[8];
+            unpack_raw(raw_x[j], p.x_f32, x);
+            unpack_raw(raw_dy[j], p.dy_f32, u);
+            load_floats<T, VECTORS>(w, p.weight, t, j, p.cols, 1.0f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                // (beyond the row: x = dy = 0, and u = 0 keeps them out of every sum)
-                xh[j][i] = (xh[j][i] - mean) * rstd;
-                dw[j][i] = fmaf(u[j][i], xh[j][i], dw[j][i]);
-                db[j][i] += u[j][i];
-                u[j][i] *= w[j][i];
-                su += u[j][i];
-                sux = fmaf(u[j][i], xh[j][i], sux);
+                // (beyond the row dy is 0, which keeps x's part out of every sum)
+                const float xh = (x[i] - mean) * rstd;
+                dw[j][i] = fmaf(u[i], xh, dw[j][i]);
+                db[j][i] += u[i];
+                u[i] *= w[i];
+                su += u[i];
+                sux = fmaf(u[i], xh, sux);
             }
         }
-        fetch(row + step);
         if (!p.dx) continue;
         su = lanes_sum<kLanes>(su);
         sux = lanes_sum<kLanes>(sux);
@@ -246,21 +244,23 @@ __global__ void __launch_bounds__(kNormThreads<T>, NV == 1 ? 1024 / kNormThreads
             sux = lanes_sum<32>(part.y);
         }
         const float mu = p.center ? su * per : 0.0f, mux = sux * per;
-        if (row < p.rows) {
+        if (live) {
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                float res[8];
+                float x[8], u[8], w[8], res[8];
+                unpack_raw(raw_x[j], p.x_f32, x);
+                unpack_raw(raw_dy[j], p.dy_f32, u);
+                load_floats<T, VECTORS>(w, p.weight, t, j, p.cols, 1.0f);
                 if (p.residual) {
-                    Raw8<true> raw;
-                    load_raw<T, VECTORS>(raw, row_of(p.residual, p.dx_f32, row, p.ld_res), p.dx_f32, t, j, p.cols);
-                    unpack_raw(raw, p.dx_f32, res);
+                    unpack_raw(raw_res[j], p.dx_f32, res);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) res[i] = 0.0f;
                 }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) u[j][i] = fmaf(fmaf(-xh[j][i], mux, u[j][i] - mu), rstd, res[i]);
-                store_row<T, VECTORS>(row_of(p.dx, p.dx_f32, row, p.ld_dx), p.dx_f32, t, j, p.cols, u[j]);
+                for (int i = 0; i < 8; ++i)
+                    u[i] = fmaf(fmaf(-(x[i] - mean) * rstd, mux, fmaf(u[i], w[i], -mu)), rstd, res[i]);
+                store_row<T, VECTORS>(row_of(p.dx, p.dx_f32, row, p.ld_dx), p.dx_f32, t, j, p.cols, u);
             }
         }
     }

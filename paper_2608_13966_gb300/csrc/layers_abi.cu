@@ -108,8 +108,7 @@ quasar_status quasar_layer_norm(const void* x, quasar_dtype x_dtype, int64_t ld_
     if (!fn)
         return launch(layer_norm_long_kernel(), &p, dim3((unsigned)std::min<int64_t>(rows, (int64_t)n_sm * 4)), 512, 1,
                       0, stream);
-    const int64_t grid = std::min<int64_t>((rows + at_once - 1) / at_once, (int64_t)n_sm * per_sm);
-    return launch(fn, &p, dim3((unsigned)grid), threads, 1, 0, stream);
+    return launch(fn, &p, dim3((unsigned)((rows + at_once - 1) / at_once)), threads, 1, 0, stream);
 }
 
 quasar_status quasar_layer_norm_backward_workspace(int64_t rows, int64_t cols, int64_t* bytes)
@@ -174,8 +173,8 @@ quasar_status quasar_layer_norm_backward(const void* dy, quasar_dtype dy_dtype, 
                              vector_rows(residual, rows, ld_residual, dx_dtype) && vector_rows(dx, rows, ld_dx, dx_dtype) &&
                              aligned(weight, 16);
         int threads = 0, at_once = 0, per_sm = 0;
-        const void* fn = layer_norm_kernel(cols, vectors, true, x_dtype == QUASAR_F32 || dy_dtype == QUASAR_F32, &threads,
-                                           &at_once, &per_sm);
+        const bool wide = x_dtype == QUASAR_F32 || dy_dtype == QUASAR_F32 || (residual && dx_dtype == QUASAR_F32);
+        const void* fn = layer_norm_kernel(cols, vectors, true, wide, &threads, &at_once, &per_sm);
         if (fn) {
             if ((st = launch(fn, &p, dim3((unsigned)parts), threads, 1, 0, stream)) != QUASAR_OK) return st;
         } else {
