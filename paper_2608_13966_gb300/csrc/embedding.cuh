@@ -5,7 +5,7 @@
 //
 // The gradient's sums have one order, whatever the timing: the tokens are
 // sorted by id (stable, so a row's tokens stay in their order), every whole
-// chunk of 128 sorted tokens that share an id is summed first (a frequent
+// chunk of 32 sorted tokens that share an id is summed first (a frequent
 // token's rows are then spread over the device), and each row of the table
 // adds up its tokens' rows and chunks.  A table's row without tokens is
 // written with zeros by the CTA that it belongs to: no pass clears the table
@@ -26,13 +26,14 @@ __device__ __forceinline__ int64_t id_at(const void* ids, int wide, int64_t t, i
 }
 
 // 4 tokens and 2,048 columns a CTA, so that four rows are on their way at once.
-template <bool VECTORS>
+template <bool VECTORS, bool WIDE>
 __global__ void __launch_bounds__(kEmbedThreads) k_embedding(const __grid_constant__ EmbedParams p)
 {
     wait_for_previous_grid();
     const int64_t t0 = (int64_t)blockIdx.x * kEmbedTokens;
-    const int64_t c0 = (int64_t)blockIdx.y * kEmbedCols, cols = p.width - c0 < kEmbedCols ? p.width - c0 : kEmbedCols;
-    Raw8<true> raw[kEmbedTokens], res[kEmbedTokens];
+    const int64_t c0 = (int64_t)blockIdx.y * kEmbedCols;
+    const int cols = (int)(p.width - c0 < kEmbedCols ? p.width - c0 : kEmbedCols);
+    Raw8<WIDE> raw[kEmbedTokens], res[kEmbedTokens];
 #pragma unroll
     for (int q = 0; q < kEmbedTokens; ++q) {
         const int64_t id = t0 + q < p.tokens ? id_at(p.ids, p.ids_64, t0 + q, p.vocab) : -1;
@@ -181,24 +182,22 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_ids(const __grid_constant
 
 // -- the gradient ------------------------------------------------------------------
 
-// Sums of whole chunks of sorted tokens that share an id.
-template <bool VECTORS>
-__global__ void __launch_bounds__(kEmbedThreads) k_embedding_chunks(const __grid_constant__ EmbedGradParams p)
+// Where the elements of token i (of the sorted ones) lie that this CTA takes.
+__device__ __forceinline__ const void* dy_row(const EmbedGradParams& p, int i, int64_t c0)
 {
-    wait_for_previous_grid();
-    const int i0 = (int)blockIdx.x * kRunChunk;
-    const uint32_t id = p.keys[i0];
-    if (id >= p.vocab || id != p.keys[i0 + kRunChunk - 1]) return;
-    const int64_t c0 = (int64_t)blockIdx.y * kEmbedCols, cols = p.width - c0 < kEmbedCols ? p.width - c0 : kEmbedCols;
-    float sum[8] = {};
-#pragma unroll 1
-    for (int i = 0; i < kRunChunk; i += 8) {
-        Raw8<true> raw[8];
+    return static_cast<const uint8_t*>(row_of(p.dy, p.dy_f32, p.places[i], p.ld_dy)) + c0 * (p.dy_f32 ? 4 : 2);
+}
+
+// sum += the rows of tokens [i, end), eight on their way at once.
+template <bool VECTORS, bool WIDE>
+__device__ __forceinline__ void add_rows(float (&sum)[8], const EmbedGradParams& p, int i, int end, int64_t c0, int cols)
+{
+    for (; i < end; i += 8) {
+        Raw8<WIDE> raw[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q)
-            load_raw<kEmbedThreads, VECTORS>(
-                raw[q], static_cast<const uint8_t*>(row_of(p.dy, p.dy_f32, p.places[i0 + i + q], p.ld_dy)) + c0 * (p.dy_f32 ? 4 : 2),
-                p.dy_f32, threadIdx.x, 0, cols);
+            load_raw<kEmbedThreads, VECTORS>(raw[q], dy_row(p, min(i + q, end - 1), c0), p.dy_f32, threadIdx.x, 0,
+                                             i + q < end ? cols : 0);
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
             float v[8];
@@ -207,12 +206,24 @@ __global__ void __launch_bounds__(kEmbedThreads) k_embedding_chunks(const __grid
             for (int x = 0; x < 8; ++x) sum[x] += v[x];
         }
     }
+}
+
+// Sums of whole chunks of sorted tokens that share an id.  (In chunks of 128
+// the few that there are took 52 us for 16384 tokens, a batch of rows after the
+// other.)
+template <bool VECTORS, bool WIDE>
+__global__ void __launch_bounds__(kEmbedThreads) k_embedding_chunks(const __grid_constant__ EmbedGradParams p)
+{
+    wait_for_previous_grid();
+    const int i0 = (int)blockIdx.x * kRunChunk;
+    const uint32_t id = p.keys[i0];
+    if (id >= p.vocab || id != p.keys[i0 + kRunChunk - 1]) return;
+    const int64_t c0 = (int64_t)blockIdx.y * kEmbedCols;
+    const int cols = (int)(p.width - c0 < kEmbedCols ? p.width - c0 : kEmbedCols);
+    float sum[8] = {};
+    add_rows<VECTORS, WIDE>(sum, p, i0, i0 + kRunChunk, c0, cols);
     float* to = p.sums + (int64_t)blockIdx.x * p.width + c0;
-#pragma unroll
-    for (int x = 0; x < 8; ++x) {
-        const int64_t c = row_at<kEmbedThreads, VECTORS>(threadIdx.x, 0, x);
-        if (c < cols) to[c] = sum[x];
-    }
+    store_row<kEmbedThreads, VECTORS>(to, true, threadIdx.x, 0, cols, sum);
 }
 
 // First of the sorted keys in [from, to) that is not below `key`.
@@ -230,57 +241,46 @@ __device__ __forceinline__ int lower_bound(const uint32_t* keys, int from, int t
 
 // kEmbedRows rows of the table by 2,048 columns a CTA.  Bound by writing the
 // table's gradient.
-template <bool VECTORS>
+template <bool VECTORS, bool WIDE>
 __global__ void __launch_bounds__(kEmbedThreads) k_embedding_grad(const __grid_constant__ EmbedGradParams p)
 {
     __shared__ int ends[kEmbedRows + 1];  // where each row's tokens start
     wait_for_previous_grid();
     const int64_t v0 = (int64_t)blockIdx.x * kEmbedRows;
     const int rows = (int)(p.vocab - v0 < kEmbedRows ? p.vocab - v0 : kEmbedRows);
-    const int64_t c0 = (int64_t)blockIdx.y * kEmbedCols, cols = p.width - c0 < kEmbedCols ? p.width - c0 : kEmbedCols;
+    const int64_t c0 = (int64_t)blockIdx.y * kEmbedCols;
+    const int cols = (int)(p.width - c0 < kEmbedCols ? p.width - c0 : kEmbedCols);
     if (threadIdx.x <= rows) ends[threadIdx.x] = lower_bound(p.keys, 0, p.n, (uint32_t)(v0 + threadIdx.x));
     __syncthreads();
     if (p.add && ends[0] == ends[rows]) return;
-    const int64_t dy_at = c0 * (p.dy_f32 ? 4 : 2);
-    for (int r = 0; r < rows; ++r) {
-        int i = ends[r];
+    uint8_t* row = static_cast<uint8_t*>(row_of(p.dtable, p.f32, v0, p.ld)) + c0 * (p.f32 ? 4 : 2);
+    const int64_t pitch = p.ld * (p.f32 ? 4 : 2);
+    int i = ends[0];
+#pragma unroll 1
+    for (int r = 0; r < rows; ++r, row += pitch) {
         const int end = ends[r + 1];
-        void* row = static_cast<uint8_t*>(row_of(p.dtable, p.f32, v0 + r, p.ld)) + c0 * (p.f32 ? 4 : 2);
-        if (p.add && i == end) continue;
         float sum[8] = {};
-        while (i < end) {
-            if (i % kRunChunk == 0 && i + kRunChunk <= end) {
-                float v[8];
-                load_floats<kEmbedThreads, VECTORS>(v, p.sums + (int64_t)(i / kRunChunk) * p.width + c0, threadIdx.x, 0,
-                                                    cols, 0.0f);
-#pragma unroll
-                for (int x = 0; x < 8; ++x) sum[x] += v[x];
-                i += kRunChunk;
-                continue;
-            }
-            // up to the next chunk, four rows on their way at once
-            const int stop = min(end, (i / kRunChunk + 1) * kRunChunk);
-            for (; i < stop; i += 4) {
-                Raw8<true> raw[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    load_raw<kEmbedThreads, VECTORS>(
-                        raw[q], static_cast<const uint8_t*>(row_of(p.dy, p.dy_f32, i + q < stop ? p.places[i + q] : 0, p.ld_dy)) + dy_at,
-                        p.dy_f32, threadIdx.x, 0, i + q < stop ? cols : 0);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float v[8];
-                    unpack_raw(raw[q], p.dy_f32, v);
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) sum[x] += v[x];
-                }
-            }
-            i = stop;
+        if (i == end) {
+            if (!p.add) store_row<kEmbedThreads, VECTORS>(row, p.f32, threadIdx.x, 0, cols, sum);
+            continue;
         }
+        // up to the first whole chunk, the chunks, and from the last on
+        const int head = min(end, (i + kRunChunk - 1) / kRunChunk * kRunChunk);
+        add_rows<VECTORS, WIDE>(sum, p, i, head, c0, cols);
+        const int tail = max(head, end / kRunChunk * kRunChunk);
+#pragma unroll 4
+        for (int q = head / kRunChunk; q < tail / kRunChunk; ++q) {
+            float v[8];
+            load_floats<kEmbedThreads, VECTORS>(v, p.sums + (int64_t)q * p.width + c0, threadIdx.x, 0, cols, 0.0f);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) sum[x] += v[x];
+        }
+        add_rows<VECTORS, WIDE>(sum, p, tail, end, c0, cols);
+        i = end;
 #pragma unroll
         for (int x = 0; x < 8; ++x) sum[x] *= p.scale;
         if (p.add) {
-            Raw8<true> raw;
+            Raw8<WIDE> raw;
             float v[8];
             load_raw<kEmbedThreads, VECTORS>(raw, row, p.f32, threadIdx.x, 0, cols);
             unpack_raw(raw, p.f32, v);

@@ -29,10 +29,13 @@ Shape norm_shape(int64_t cols, bool grad)
 }
 
 template <int T, int NV>
-const void* forward(bool vectors)
+const void* forward(bool vectors, bool wide)
 {
-    return vectors ? reinterpret_cast<const void*>(&k_layer_norm<T, NV, true>)
-                   : reinterpret_cast<const void*>(&k_layer_norm<T, NV, false>);
+    if (vectors)
+        return wide ? reinterpret_cast<const void*>(&k_layer_norm<T, NV, true, true>)
+                    : reinterpret_cast<const void*>(&k_layer_norm<T, NV, true, false>);
+    return wide ? reinterpret_cast<const void*>(&k_layer_norm<T, NV, false, true>)
+                : reinterpret_cast<const void*>(&k_layer_norm<T, NV, false, false>);
 }
 
 template <int T, int NV>
@@ -58,9 +61,9 @@ const void* layer_norm_kernel(int64_t cols, bool vectors, bool grad, bool wide, 
     *rows = *threads / s.t;
     *per_sm = (s.nv == 1 ? 768 : 512) / *threads;
 #define QUASAR_NORM(T, NV) \
-    if (s.t == T && s.nv == NV) return grad ? backward<T, NV>(vectors, wide) : forward<T, NV>(vectors);
+    if (s.t == T && s.nv == NV) return grad ? backward<T, NV>(vectors, wide) : forward<T, NV>(vectors, wide);
 #define QUASAR_NORM_FORWARD(T, NV) \
-    if (s.t == T && s.nv == NV) return forward<T, NV>(vectors);
+    if (s.t == T && s.nv == NV) return forward<T, NV>(vectors, wide);
     QUASAR_NORM(8, 1)
     QUASAR_NORM(8, 2)
     QUASAR_NORM(32, 1)

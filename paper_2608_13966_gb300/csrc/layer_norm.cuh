@@ -44,22 +44,23 @@ __device__ __forceinline__ float lanes_sum(float x)
 // Several CTAs an SM, no more than a row each in hand, keep the memory busy; the
 // weights come from L1 (kept in registers by persistent CTAs of 512 threads
 // that fetched their next row ahead, two an SM, 16384 x 4096 took 79 us).
-template <int T, int NV, bool VECTORS>
+template <int T, int NV, bool VECTORS, bool WIDE>
 __global__ void __launch_bounds__(kNormThreads<T>, 1024 / kNormThreads<T>) k_layer_norm(const __grid_constant__ NormParams p)
 {
     constexpr int kGroups = kNormThreads<T> / T, kWarps = T / 32, kLanes = T < 32 ? T : 32;
     __shared__ float2 red[T > 32 ? kWarps : 1];
     const int t = threadIdx.x % T, lane = threadIdx.x & 31;
-    const bool whole = p.cols == (int64_t)T * NV * 8;
-    const float cols = (float)p.cols;
+    const int n_cols = (int)p.cols;  // (what registers hold)
+    const bool whole = n_cols == T * NV * 8;
+    const float cols = (float)n_cols;
     const int64_t row = (int64_t)blockIdx.x * kGroups + threadIdx.x / T;
     const bool live = row < p.rows;
     wait_for_previous_grid();
 
-    Raw8<true> raw[NV];
+    Raw8<WIDE> raw[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j)
-        load_raw<T, VECTORS>(raw[j], row_of(p.x, p.x_f32, row, p.ld_x), p.x_f32, t, j, live ? p.cols : 0);
+        load_raw<T, VECTORS>(raw[j], row_of(p.x, p.x_f32, row, p.ld_x), p.x_f32, t, j, live ? n_cols : 0);
     float v[NV][8];
     float sum = 0.0f;
 #pragma unroll
@@ -73,12 +74,12 @@ __global__ void __launch_bounds__(kNormThreads<T>, 1024 / kNormThreads<T>) k_lay
         n = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int64_t left = p.cols - row_at<T, VECTORS>(t & ~31, j, 0);
+            const int left = n_cols - row_at<T, VECTORS>(t & ~31, j, 0);
             if (VECTORS)
-                n += (float)max((int64_t)0, min((int64_t)256, left));
+                n += (float)max(0, min(256, left));
             else
 #pragma unroll
-                for (int i = 0; i < 8; ++i) n += (float)max((int64_t)0, min((int64_t)32, left - (int64_t)i * T));
+                for (int i = 0; i < 8; ++i) n += (float)max(0, min(32, left - i * T));
         }
     }
     // (divisions: a row of one value then has no variance at all)
@@ -88,7 +89,7 @@ __global__ void __launch_bounds__(kNormThreads<T>, 1024 / kNormThreads<T>) k_lay
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float d = whole || row_at<T, VECTORS>(t, j, i) < p.cols ? v[j][i] - mean : 0.0f;
+            const float d = whole || row_at<T, VECTORS>(t, j, i) < n_cols ? v[j][i] - mean : 0.0f;
             m2 = fmaf(d, d, m2);
         }
     m2 = lanes_sum<kLanes>(m2);
@@ -109,11 +110,11 @@ __global__ void __launch_bounds__(kNormThreads<T>, 1024 / kNormThreads<T>) k_lay
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         float w[8], b[8];
-        load_floats<T, VECTORS>(w, p.weight, t, j, p.cols, 1.0f);
-        load_floats<T, VECTORS>(b, p.bias, t, j, p.cols, 0.0f);
+        load_floats<T, VECTORS>(w, p.weight, t, j, n_cols, 1.0f);
+        load_floats<T, VECTORS>(b, p.bias, t, j, n_cols, 0.0f);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[j][i] = fmaf((v[j][i] - mean) * rstd, w[i], b[i]);
-        store_row<T, VECTORS>(row_of(p.y, p.y_f32, row, p.ld_y), p.y_f32, t, j, p.cols, v[j]);
+        store_row<T, VECTORS>(row_of(p.y, p.y_f32, row, p.ld_y), p.y_f32, t, j, n_cols, v[j]);
     }
     if (p.stats && t == 0) {
         p.stats[2 * row] = mean;
@@ -192,7 +193,8 @@ __global__ void __launch_bounds__(kNormThreads<T>, kNormPerSm<T, NV>)
     __shared__ float2 red[2][T > 32 ? kWarps : 1];
     __shared__ float sums[kGroups > 1 ? kGroups * T * NV * 8 : 1];
     const int t = threadIdx.x % T, lane = threadIdx.x & 31;
-    const float per = 1.0f / (float)p.cols;
+    const int n_cols = (int)p.cols;
+    const float per = 1.0f / (float)n_cols;
     wait_for_previous_grid();
 
     float dw[NV][8], db[NV][8];
@@ -208,11 +210,11 @@ __global__ void __launch_bounds__(kNormThreads<T>, kNormPerSm<T, NV>)
         Raw8<WIDE> raw_x[NV], raw_dy[NV], raw_res[NV];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            load_raw<T, VECTORS>(raw_x[j], row_of(p.x, p.x_f32, row, p.ld_x), p.x_f32, t, j, live ? p.cols : 0);
-            load_raw<T, VECTORS>(raw_dy[j], row_of(p.dy, p.dy_f32, row, p.ld_dy), p.dy_f32, t, j, live ? p.cols : 0);
+            load_raw<T, VECTORS>(raw_x[j], row_of(p.x, p.x_f32, row, p.ld_x), p.x_f32, t, j, live ? n_cols : 0);
+            load_raw<T, VECTORS>(raw_dy[j], row_of(p.dy, p.dy_f32, row, p.ld_dy), p.dy_f32, t, j, live ? n_cols : 0);
             if (p.residual)
                 load_raw<T, VECTORS>(raw_res[j], row_of(p.residual, p.dx_f32, row, p.ld_res), p.dx_f32, t, j,
-                                     live ? p.cols : 0);
+                                     live ? n_cols : 0);
         }
         const float mean = live && p.center ? p.stats[2 * row] : 0.0f, rstd = live ? p.stats[2 * row + 1] : 0.0f;
         float su = 0.0f, sux = 0.0f;
@@ -221,7 +223,7 @@ __global__ void __launch_bounds__(kNormThreads<T>, kNormPerSm<T, NV>)
             float x[8], u[8], w[8];
             unpack_raw(raw_x[j], p.x_f32, x);
             unpack_raw(raw_dy[j], p.dy_f32, u);
-            load_floats<T, VECTORS>(w, p.weight, t, j, p.cols, 1.0f);
+            load_floats<T, VECTORS>(w, p.weight, t, j, n_cols, 1.0f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 // (beyond the row dy is 0, which keeps x's part out of every sum)
@@ -250,7 +252,7 @@ __global__ void __launch_bounds__(kNormThreads<T>, kNormPerSm<T, NV>)
                 float x[8], u[8], w[8], res[8];
                 unpack_raw(raw_x[j], p.x_f32, x);
                 unpack_raw(raw_dy[j], p.dy_f32, u);
-                load_floats<T, VECTORS>(w, p.weight, t, j, p.cols, 1.0f);
+                load_floats<T, VECTORS>(w, p.weight, t, j, n_cols, 1.0f);
                 if (p.residual) {
                     unpack_raw(raw_res[j], p.dx_f32, res);
                 } else {
@@ -260,7 +262,7 @@ __global__ void __launch_bounds__(kNormThreads<T>, kNormPerSm<T, NV>)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     u[i] = fmaf(fmaf(-(x[i] - mean) * rstd, mux, fmaf(u[i], w[i], -mu)), rstd, res[i]);
-                store_row<T, VECTORS>(row_of(p.dx, p.dx_f32, row, p.ld_dx), p.dx_f32, t, j, p.cols, u);
+                store_row<T, VECTORS>(row_of(p.dx, p.dx_f32, row, p.ld_dx), p.dx_f32, t, j, n_cols, u);
             }
         }
     }
@@ -278,9 +280,9 @@ __global__ void __launch_bounds__(kNormThreads<T>, kNormPerSm<T, NV>)
             for (int j = 0; j < NV; ++j)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    sums[threadIdx.x / T * kSpan + (int)row_at<T, VECTORS>(t, j, i)] = mine[j][i];
+                    sums[threadIdx.x / T * kSpan + row_at<T, VECTORS>(t, j, i)] = mine[j][i];
             __syncthreads();
-            for (int c = threadIdx.x; c < p.cols; c += kNormThreads<T>) {
+            for (int c = threadIdx.x; c < n_cols; c += kNormThreads<T>) {
                 float s = sums[c];
 #pragma unroll 8
                 for (int g = 1; g < kGroups; ++g) s += sums[g * kSpan + c];
@@ -291,8 +293,8 @@ __global__ void __launch_bounds__(kNormThreads<T>, kNormPerSm<T, NV>)
             for (int j = 0; j < NV; ++j)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int64_t c = row_at<T, VECTORS>(t, j, i);
-                    if (c < p.cols) part[c] = mine[j][i];
+                    const int c = row_at<T, VECTORS>(t, j, i);
+                    if (c < n_cols) part[c] = mine[j][i];
                 }
         }
     }
@@ -346,10 +348,10 @@ __global__ void __launch_bounds__(256) k_layer_norm_grad_columns(const __grid_co
 }
 
 // The CTAs' shares added up, always in the same order: 32 columns a CTA, the
-// parts over its 8 warps.
-__global__ void __launch_bounds__(256) k_part_sum(const __grid_constant__ PartSumParams p)
+// parts over its 32 warps (with 8 warps 304 parts of 4096 columns took 10 us).
+__global__ void __launch_bounds__(1024) k_part_sum(const __grid_constant__ PartSumParams p)
 {
-    __shared__ float red[8][32];
+    __shared__ float red[32][33];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;
     wait_for_previous_grid();
@@ -357,14 +359,13 @@ __global__ void __launch_bounds__(256) k_part_sum(const __grid_constant__ PartSu
     float s = 0.0f;
     if (c < p.cols) {
 #pragma unroll 8
-        for (int q = warp; q < p.parts; q += 8) s += part[q * p.cols + c];
+        for (int q = warp; q < p.parts; q += 32) s += part[q * p.cols + c];
     }
     red[warp][lane] = s;
     __syncthreads();
-    if (warp == 0 && c < p.cols) {
-        for (int q = 1; q < 8; ++q) s += red[q][lane];
-        p.out[blockIdx.y][c] = s;
-    }
+    // column `warp`, its 32 sums in a tree
+    s = lanes_sum<32>(red[lane][warp]);
+    if (lane == 0 && (int64_t)blockIdx.x * 32 + warp < p.cols) p.out[blockIdx.y][(int64_t)blockIdx.x * 32 + warp] = s;
 }
 
 }  // namespace quasar

@@ -59,11 +59,11 @@ struct PartSumParams {
 constexpr int kSortBits = 9;        // of a pass
 constexpr int kSortThreads = 1024;
 constexpr int kSortCtas = 8;        // most of a cluster
-constexpr int kRunChunk = 128;      // sorted tokens summed ahead where they share an id
+constexpr int kRunChunk = 32;       // sorted tokens summed ahead where they share an id
 constexpr int kEmbedThreads = 256;
 constexpr int kEmbedCols = kEmbedThreads * 8;  // of a CTA
 constexpr int kEmbedTokens = 4;     // of a CTA of the lookup
-constexpr int kEmbedRows = 32;      // of the table, a CTA of the gradient
+constexpr int kEmbedRows = 64;      // of the table, a CTA of the gradient
 
 struct EmbedParams {
     const void* ids;

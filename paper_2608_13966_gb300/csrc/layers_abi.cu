@@ -15,11 +15,11 @@ const void* layer_norm_long_kernel();
 const void* layer_norm_grad_long_kernel();
 const void* layer_norm_grad_columns_kernel();
 const void* part_sum_kernel();
-const void* embedding_kernel(bool vectors);
+const void* embedding_kernel(bool vectors, bool wide);
 const void* sort_ids_kernel();
 size_t sort_ids_smem();
-const void* embedding_chunks_kernel(bool vectors);
-const void* embedding_grad_kernel(bool vectors);
+const void* embedding_chunks_kernel(bool vectors, bool wide);
+const void* embedding_grad_kernel(bool vectors, bool wide);
 }  // namespace quasar
 
 namespace {
@@ -104,7 +104,7 @@ quasar_status quasar_layer_norm(const void* x, quasar_dtype x_dtype, int64_t ld_
     const bool vectors = vector_rows(x, rows, ld_x, x_dtype) && vector_rows(y, rows, ld_y, y_dtype) &&
                          aligned(weight, 16) && aligned(bias, 16);
     int threads = 0, at_once = 0, per_sm = 0;
-    const void* fn = layer_norm_kernel(cols, vectors, false, false, &threads, &at_once, &per_sm);
+    const void* fn = layer_norm_kernel(cols, vectors, false, x_dtype == QUASAR_F32, &threads, &at_once, &per_sm);
     if (!fn)
         return launch(layer_norm_long_kernel(), &p, dim3((unsigned)std::min<int64_t>(rows, (int64_t)n_sm * 4)), 512, 1,
                       0, stream);
@@ -191,7 +191,7 @@ quasar_status quasar_layer_norm_backward(const void* dy, quasar_dtype dy_dtype, 
     }
     if (parts == 1 || (!dweight && !dbias)) return QUASAR_OK;
     if (!dweight) sums.part[0] = sums.part[1], sums.out[0] = sums.out[1];
-    return launch(part_sum_kernel(), &sums, dim3((unsigned)((cols + 31) / 32), dweight && dbias ? 2 : 1), 256, 1, 0,
+    return launch(part_sum_kernel(), &sums, dim3((unsigned)((cols + 31) / 32), dweight && dbias ? 2 : 1), 1024, 1, 0,
                   stream);
 }
 
@@ -217,7 +217,8 @@ quasar_status quasar_embedding(const void* ids, quasar_index_type ids_type, int6
                   residual, ld_residual, y, ld_y, y_dtype == QUASAR_F32};
     const bool vectors = vector_rows(table, vocab, ld_table, table_dtype) && vector_rows(y, tokens, ld_y, y_dtype) &&
                          vector_rows(residual, tokens, ld_residual, y_dtype);
-    return launch(embedding_kernel(vectors), &p,
+    const bool wide = table_dtype == QUASAR_F32 || (residual && y_dtype == QUASAR_F32);
+    return launch(embedding_kernel(vectors, wide), &p,
                   dim3((unsigned)((tokens + kEmbedTokens - 1) / kEmbedTokens), (unsigned)chunks), kEmbedThreads, 1, 0,
                   stream);
 }
@@ -286,11 +287,12 @@ quasar_status quasar_embedding_backward(const void* dy, quasar_dtype dy_dtype, i
     p.add = accumulate;
     const bool vectors = vector_rows(dy, tokens, ld_dy, dy_dtype) && vector_rows(dtable, vocab, ld_dtable, dtable_dtype) &&
                          width % 4 == 0;  // (the chunks' sums)
-    if (tokens >= kRunChunk && (st = launch(embedding_chunks_kernel(vectors), &p,
+    const bool wide = dy_dtype == QUASAR_F32 || (accumulate && dtable_dtype == QUASAR_F32);
+    if (tokens >= kRunChunk && (st = launch(embedding_chunks_kernel(vectors, wide), &p,
                                             dim3((unsigned)(tokens / kRunChunk), (unsigned)chunks), kEmbedThreads, 1, 0,
                                             stream)) != QUASAR_OK)
         return st;
-    return launch(embedding_grad_kernel(vectors), &p,
+    return launch(embedding_grad_kernel(vectors, wide), &p,
                   dim3((unsigned)((vocab + kEmbedRows - 1) / kEmbedRows), (unsigned)chunks), kEmbedThreads, 1, 0, stream);
 }
 

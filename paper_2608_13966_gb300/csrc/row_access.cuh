@@ -8,9 +8,9 @@ namespace quasar {
 // Elements of thread t: with VECTORS runs of 8 (rows start at 16-byte
 // boundaries), else single elements T apart.
 template <int T, bool VECTORS>
-__device__ __forceinline__ int64_t row_at(int t, int j, int i)
+__device__ __forceinline__ int row_at(int t, int j, int i)
 {
-    return VECTORS ? (int64_t)(j * T + t) * 8 + i : (int64_t)(j * 8 + i) * T + t;
+    return VECTORS ? (j * T + t) * 8 + i : (j * 8 + i) * T + t;
 }
 
 // 8 elements as they lie in memory: the raw words of a row on its way.
@@ -21,13 +21,13 @@ struct Raw8 {
 };
 
 template <int T, bool VECTORS, bool WIDE>
-__device__ __forceinline__ void load_raw(Raw8<WIDE>& r, const void* row, bool f32, int t, int j, int64_t cols)
+__device__ __forceinline__ void load_raw(Raw8<WIDE>& r, const void* row, bool f32, int t, int j, int cols)
 {
     const __nv_bfloat16* h = static_cast<const __nv_bfloat16*>(row);
     const float* f = static_cast<const float*>(row);
 #pragma unroll
     for (int q = 0; q < (WIDE ? 8 : 4); ++q) r.w[q] = 0;
-    const int64_t c0 = row_at<T, VECTORS>(t, j, 0);
+    const int c0 = row_at<T, VECTORS>(t, j, 0);
     if (VECTORS && c0 + 8 <= cols) {
         if (WIDE && f32) {
             const uint4 a = __ldcs(reinterpret_cast<const uint4*>(f + c0));
@@ -42,7 +42,7 @@ __device__ __forceinline__ void load_raw(Raw8<WIDE>& r, const void* row, bool f3
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int64_t c = row_at<T, VECTORS>(t, j, i);
+        const int c = row_at<T, VECTORS>(t, j, i);
         if (c >= cols) continue;
         if (WIDE && f32) {
             r.w[WIDE ? i : 0] = __float_as_uint(f[c]);
@@ -66,9 +66,9 @@ __device__ __forceinline__ void unpack_raw(const Raw8<WIDE>& r, bool f32, float 
 }
 
 template <int T, bool VECTORS>
-__device__ __forceinline__ void load_floats(float (&v)[8], const float* row, int t, int j, int64_t cols, float none)
+__device__ __forceinline__ void load_floats(float (&v)[8], const float* row, int t, int j, int cols, float none)
 {
-    const int64_t c0 = row_at<T, VECTORS>(t, j, 0);
+    const int c0 = row_at<T, VECTORS>(t, j, 0);
     if (VECTORS && row && c0 + 8 <= cols) {
         const float4 a = *reinterpret_cast<const float4*>(row + c0), b = *reinterpret_cast<const float4*>(row + c0 + 4);
         v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
@@ -76,17 +76,17 @@ __device__ __forceinline__ void load_floats(float (&v)[8], const float* row, int
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int64_t c = row_at<T, VECTORS>(t, j, i);
+        const int c = row_at<T, VECTORS>(t, j, i);
         v[i] = c < cols ? (row ? row[c] : none) : 0.0f;
     }
 }
 
 template <int T, bool VECTORS>
-__device__ __forceinline__ void store_row(void* row, bool f32, int t, int j, int64_t cols, const float (&v)[8])
+__device__ __forceinline__ void store_row(void* row, bool f32, int t, int j, int cols, const float (&v)[8])
 {
     __nv_bfloat16* h = static_cast<__nv_bfloat16*>(row);
     float* f = static_cast<float*>(row);
-    const int64_t c0 = row_at<T, VECTORS>(t, j, 0);
+    const int c0 = row_at<T, VECTORS>(t, j, 0);
     if (VECTORS && c0 + 8 <= cols) {
         if (f32) {
             reinterpret_cast<float4*>(f + c0)[0] = make_float4(v[0], v[1], v[2], v[3]);
@@ -99,7 +99,7 @@ __device__ __forceinline__ void store_row(void* row, bool f32, int t, int j, int
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int64_t c = row_at<T, VECTORS>(t, j, i);
+        const int c = row_at<T, VECTORS>(t, j, i);
         if (c >= cols) continue;
         if (f32)
             f[c] = v[i];

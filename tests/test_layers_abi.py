@@ -77,7 +77,7 @@ def test_embedding_backward_arguments(kw, expect):
 
 def test_embedding_workspace():
     assert Q.quasar_embedding_backward_workspace(4, 64) == 4 * 16
-    assert Q.quasar_embedding_backward_workspace(300, 7) == 4 * 1200 + 2 * 4 * 7
+    assert Q.quasar_embedding_backward_workspace(300, 7) == 4 * 1200 + 9 * 4 * 7
     with pytest.raises(Q.QuasarError):
         Q.quasar_embedding_backward_workspace(-1, 7)
 
