@@ -10,6 +10,8 @@ clears that word after synchronising the stream, and callers that must know
 their outputs are whole call it once after their last reconstruction."""
 from __future__ import annotations
 
+import functools
+
 import torch
 
 from .quasar import (ACTIVATIONS, BF16, F32, QuasarError, QuasarStatus, adamw_nvfp4_tensor_array,
@@ -598,6 +600,16 @@ def distill_top_backward(logits, indices, values, stats, row_weight, *, teacher_
 _ID_CODES = {torch.int32: I32, torch.int64: I64}
 
 
+@functools.lru_cache(maxsize=4096)
+def _norm_workspace(rows, cols, on):
+    """What the call answers for these sizes on this device (2 us a time)."""
+    return quasar_layer_norm_backward_workspace(rows, cols)
+
+
+_embedding_workspace = functools.lru_cache(maxsize=4096)(quasar_embedding_backward_workspace)
+_attention_workspace = functools.lru_cache(maxsize=4096)(quasar_attention_backward_workspace)
+
+
 def _scratch(n, device):
     """The workspace of one call (allocated for it, on the stream it runs on)."""
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
@@ -659,7 +671,7 @@ def embedding_backward(dy, ids, vocab, *, scale=1.0, dtable_dtype=torch.bfloat16
         out, ld = torch.empty((vocab, width), dtype=dtable_dtype, device=dy.device), width
     else:
         out = into
-    need = quasar_embedding_backward_workspace(tokens, width)
+    need = _embedding_workspace(tokens, width)
     _check(quasar_embedding_backward(dy, _CODES[dy.dtype], ld_dy, ids, ids_code, tokens, vocab,
                                      width, scale, out, code, ld, int(into is not None),
                                      _scratch(need, dy.device), need))
@@ -724,7 +736,7 @@ def layer_norm_backward(dy, x, weight, stats, *, center=True, dx=True, dweight=T
     if dbias:
         out["dbias"] = db = torch.empty(cols, dtype=torch.float32, device=device)
     if dweight or dbias:
-        need = quasar_layer_norm_backward_workspace(rows, cols)
+        need = _norm_workspace(rows, cols, on)
         scratch = _scratch(need, device)
     _check(quasar_layer_norm_backward(dy, _CODES[dy.dtype], ld_dy, x, _CODES[x.dtype], ld_x, weight,
                                       stats, rows, cols, int(bool(center)), residual, ld_res, to, code,
@@ -832,7 +844,7 @@ def attention_backward(dy, q, k, v, y, lse, head_dim, *, starts=None, key_starts
             lds.append(_ld(made[name]))
         else:
             lds.append(0)
-    need = quasar_attention_backward_workspace(tokens, heads)
+    need = _attention_workspace(tokens, heads)
     _check(quasar_attention_backward(dy, ld_dy, q, ld_q, k, ld_k, v, ld_v, y, ld_y, lse, tokens, keys,
                                      heads, kv_heads, head_dim, starts,
                                      starts if key_starts is None else key_starts, sequences,

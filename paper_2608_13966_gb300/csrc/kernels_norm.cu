@@ -82,6 +82,43 @@ const void* layer_norm_kernel(int64_t cols, bool vectors, bool grad, bool wide, 
     return nullptr;
 }
 
+// The kernel of rows through shared memory (rows of whole vectors of 8 that
+// start at 16-byte boundaries), its threads and CTAs an SM; nullptr for rows
+// that a warp takes, or that registers do not hold (backward from 8192 on, where
+// dw and db need them too).
+const void* layer_norm_ring_kernel(int64_t cols, bool grad, bool wide, int* threads, int* per_sm)
+{
+    if (cols % 8 != 0 || cols <= 1024 || cols > (grad ? 8192 : kNormMostCols)) return nullptr;
+#define QUASAR_RING(most, T, NV, kernel, grads)                                        \
+    if (cols <= most) {                                                                \
+        *threads = T, *per_sm = kNormRingPerSm<T, NV, grads>;                          \
+        return wide ? reinterpret_cast<const void*>(&kernel<T, NV, true>)              \
+                    : reinterpret_cast<const void*>(&kernel<T, NV, false>);            \
+    }
+    // few threads with many elements each: the reductions cost a warp as much
+    // for 1 as for 4 vectors (16384 x 4096: 512 threads of one 75 us)
+    if (grad) {
+        QUASAR_RING(2048, 128, 2, k_layer_norm_grad_ring, true)
+        QUASAR_RING(4096, 256, 2, k_layer_norm_grad_ring, true)
+        QUASAR_RING(8192, 512, 2, k_layer_norm_grad_ring, true)
+    }
+    QUASAR_RING(2048, 128, 2, k_layer_norm_ring, false)
+    QUASAR_RING(4096, 128, 4, k_layer_norm_ring, false)
+    QUASAR_RING(8192, 256, 4, k_layer_norm_ring, false)
+    QUASAR_RING(kNormMostCols, 512, 4, k_layer_norm_ring, false)
+#undef QUASAR_RING
+    return nullptr;
+}
+
+// Slots of a ring, by what the CTAs of an SM leave each other.
+int layer_norm_slots(uint32_t slot_bytes, int threads, int per_sm, size_t* smem)
+{
+    int slots = 8;
+    while (slots > 1 && norm_ring_smem(slots, slot_bytes, threads) > (size_t)216 * 1024 / per_sm) --slots;
+    *smem = norm_ring_smem(slots, slot_bytes, threads);
+    return slots;
+}
+
 const void* layer_norm_long_kernel() { return reinterpret_cast<const void*>(&k_layer_norm_long); }
 const void* layer_norm_grad_long_kernel() { return reinterpret_cast<const void*>(&k_layer_norm_grad_long); }
 const void* layer_norm_grad_columns_kernel() { return reinterpret_cast<const void*>(&k_layer_norm_grad_columns); }

@@ -26,6 +26,11 @@ namespace quasar {
 template <int T>
 constexpr int kNormThreads = T < 128 ? 256 : T;
 
+// CTAs an SM of the kernels whose rows come through shared memory: 512 threads
+// have 128 registers each (forward with two vectors a thread: 768).
+template <int T, int NV, bool GRAD>
+constexpr int kNormRingPerSm = (NV == 2 && !GRAD ? 768 : 512) / T;
+
 // CTAs an SM of the backward kernel, by its registers.
 template <int T, int NV>
 constexpr int kNormPerSm = (NV == 1 ? 768 : 512) / kNormThreads<T>;  // 512 threads have 128 each
@@ -120,6 +125,169 @@ __global__ void __launch_bounds__(kNormThreads<T>, 1024 / kNormThreads<T>) k_lay
         p.stats[2 * row] = mean;
         p.stats[2 * row + 1] = rstd;
     }
+}
+
+// -- rows through shared memory ----------------------------------------------------
+//
+// Rows of whole 16-byte vectors that start at 16-byte boundaries, longer than
+// what a warp takes: persistent CTAs keep their columns' weights in registers
+// and bulk copies bring the next rows (up to 8) into a ring.  A slot is free
+// once every thread has taken its part, which the reduction's barrier says.
+//
+// 16384 x 4096 bf16 with weight and bias: see the launch.
+
+struct NormRing {
+    uint8_t* rows;
+    uint64_t* full;         // [slots]
+    uint64_t* never;
+    volatile uint32_t* gone;
+    float2* red;            // [2][warps]
+    float* counts;          // [warps]
+    int slots;
+    uint32_t slot_bytes;
+};
+
+__host__ __device__ constexpr size_t norm_ring_smem(int slots, uint32_t slot_bytes, int threads)
+{
+    return (size_t)slots * slot_bytes + (slots + 2) * 8 + threads / 32 * 20;
+}
+
+__device__ __forceinline__ NormRing norm_ring(uint8_t* smem, int slots, uint32_t slot_bytes, int warps)
+{
+    NormRing r;
+    r.rows = smem;
+    r.full = reinterpret_cast<uint64_t*>(smem + (size_t)slots * slot_bytes);
+    r.never = r.full + slots;
+    r.gone = reinterpret_cast<volatile uint32_t*>(r.never + 1);
+    r.red = reinterpret_cast<float2*>(r.never + 2);
+    r.counts = reinterpret_cast<float*>(r.red + 2 * warps);
+    r.slots = slots;
+    r.slot_bytes = slot_bytes;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < slots; ++i) mbar_init(r.full + i, 1);
+        mbar_init(r.never, 1);
+        *r.gone = 0;
+        mbar_init_fence();
+    }
+    __syncthreads();
+    return r;
+}
+
+// A wait that ran out is said to all behind the next barrier.
+__device__ __forceinline__ void norm_wait(const NormRing& r, uint64_t* bar, uint32_t parity, uint64_t limit_ns, unsigned int* status)
+{
+    if (!mbar_wait_bounded(bar, parity, limit_ns)) {
+        *r.gone = 1;
+        record_timeout(status);
+    }
+}
+
+// Given up: what is in flight of `sent` rows has landed before the memory is
+// let go.
+__device__ __forceinline__ void norm_drain(const NormRing& r, int64_t sent, uint64_t limit_ns)
+{
+    for (int64_t k = sent > r.slots ? sent - r.slots : 0; k < sent; ++k)
+        mbar_wait_bounded(r.full + k % r.slots, (uint32_t)(k / r.slots) & 1, limit_ns);
+}
+
+template <bool WIDE>
+__device__ __forceinline__ void from_shared(Raw8<WIDE>& r, const uint8_t* row, bool f32, int c0)
+{
+#pragma unroll
+    for (int q = 0; q < (WIDE ? 8 : 4); ++q) r.w[q] = 0;
+    if (WIDE && f32) {
+        const uint4 a = *reinterpret_cast<const uint4*>(row + (size_t)c0 * 4), b = *reinterpret_cast<const uint4*>(row + (size_t)c0 * 4 + 16);
+        r.w[0] = a.x, r.w[1] = a.y, r.w[2] = a.z, r.w[3] = a.w;
+        r.w[WIDE ? 4 : 0] = b.x, r.w[WIDE ? 5 : 0] = b.y, r.w[WIDE ? 6 : 0] = b.z, r.w[WIDE ? 7 : 0] = b.w;
+    } else {
+        const uint4 a = *reinterpret_cast<const uint4*>(row + (size_t)c0 * 2);
+        r.w[0] = a.x, r.w[1] = a.y, r.w[2] = a.z, r.w[3] = a.w;
+    }
+}
+
+template <int T, int NV, bool WIDE>
+__global__ void __launch_bounds__(T, kNormRingPerSm<T, NV, false>) k_layer_norm_ring(const __grid_constant__ NormParams p)
+{
+    constexpr int kWarps = T / 32;
+    extern __shared__ __align__(16) uint8_t smem[];
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+    const int n_cols = (int)p.cols;  // a multiple of 8 (of 4 in fp32)
+    const float cols = (float)n_cols;
+    const uint32_t bytes = (uint32_t)n_cols * (p.x_f32 ? 4 : 2);
+    const NormRing ring = norm_ring(smem, p.slots, bytes, kWarps);
+    float n = 0.0f;  // this warp's elements
+#pragma unroll
+    for (int j = 0; j < NV; ++j) n += (float)max(0, min(256, n_cols - row_at<T, true>(t & ~31, j, 0)));
+    if (lane == 0) ring.counts[warp] = n;
+    wait_for_previous_grid();
+    int64_t sent = 0;  // rows asked for (thread 0)
+    auto fetch = [&](int64_t row, int slot) {
+        mbar_arrive_expect_tx(ring.full + slot, bytes);
+        bulk_g2s(ring.rows + (size_t)slot * bytes, row_of(p.x, p.x_f32, row, p.ld_x), bytes, ring.full + slot);
+        ++sent;
+    };
+    if (t == 0) {
+        if (p.force_timeout_ns) norm_wait(ring, ring.never, 0, p.force_timeout_ns, p.status);
+        int64_t row = blockIdx.x;
+        for (int s = 0; s < ring.slots && row < p.rows; ++s, row += gridDim.x) fetch(row, s);
+    }
+    float w[NV][8], b[NV][8];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        load_floats<T, true>(w[j], p.weight, t, j, n_cols, 1.0f);
+        load_floats<T, true>(b[j], p.bias, t, j, n_cols, 0.0f);
+    }
+    int slot = 0, turn = 0;
+    uint32_t parity = 0;
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
+        norm_wait(ring, ring.full + slot, parity, p.timeout_ns, p.status);
+        float v[NV][8];
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c0 = row_at<T, true>(t, j, 0);
+            Raw8<WIDE> raw{};
+            if (c0 < n_cols) from_shared(raw, ring.rows + (size_t)slot * bytes, p.x_f32, c0);
+            unpack_raw(raw, p.x_f32, v[j]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[j][i];
+        }
+        float mean = p.center && n > 0.0f ? lanes_sum<32>(sum) / n : 0.0f;
+        float m2 = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const bool in = row_at<T, true>(t, j, 0) < n_cols;  // (whole runs of 8)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = in ? v[j][i] - mean : 0.0f;
+                m2 = fmaf(d, d, m2);
+            }
+        }
+        m2 = lanes_sum<32>(m2);
+        if (lane == 0) ring.red[turn * kWarps + warp] = make_float2(mean, m2);
+        __syncthreads();
+        if (*ring.gone) break;
+        if (t == 0 && row + (int64_t)ring.slots * gridDim.x < p.rows) fetch(row + (int64_t)ring.slots * gridDim.x, slot);
+        const float2 part = lane < kWarps ? ring.red[turn * kWarps + lane] : make_float2(0.0f, 0.0f);
+        const float k = lane < kWarps ? ring.counts[lane] : 0.0f;
+        mean = lanes_sum<32>(k * part.x) / cols;
+        const float d = part.x - mean;
+        m2 = lanes_sum<32>(fmaf(k * d, d, part.y));
+        const float rstd = rsqrtf(m2 / cols + p.eps);
+        void* y = row_of(p.y, p.y_f32, row, p.ld_y);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[j][i] = fmaf((v[j][i] - mean) * rstd, w[j][i], b[j][i]);
+            store_row<T, true>(y, p.y_f32, t, j, n_cols, v[j]);
+        }
+        if (p.stats && t == 0) {
+            p.stats[2 * row] = mean;
+            p.stats[2 * row + 1] = rstd;
+        }
+        if (++slot == ring.slots) slot = 0, parity ^= 1;
+    }
+    if (*ring.gone && t == 0) norm_drain(ring, sent, p.timeout_ns);
 }
 
 // Sum over the CTA (512 threads), the same value in every thread.
@@ -297,6 +465,111 @@ __global__ void __launch_bounds__(kNormThreads<T>, kNormPerSm<T, NV>)
                     if (c < n_cols) part[c] = mine[j][i];
                 }
         }
+    }
+}
+
+template <int T, int NV, bool WIDE>
+__global__ void __launch_bounds__(T, kNormRingPerSm<T, NV, true>) k_layer_norm_grad_ring(const __grid_constant__ NormGradParams p)
+{
+    constexpr int kWarps = T / 32;
+    extern __shared__ __align__(16) uint8_t smem[];
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+    const int n_cols = (int)p.cols;
+    const float per = 1.0f / (float)n_cols;
+    // a slot: the rows of x, dy and the residual
+    const uint32_t x_bytes = (uint32_t)n_cols * (p.x_f32 ? 4 : 2), dy_bytes = (uint32_t)n_cols * (p.dy_f32 ? 4 : 2);
+    const uint32_t res_bytes = p.residual ? (uint32_t)n_cols * (p.dx_f32 ? 4 : 2) : 0;
+    const uint32_t slot_bytes = x_bytes + dy_bytes + res_bytes;
+    const NormRing ring = norm_ring(smem, p.slots, slot_bytes, kWarps);
+    wait_for_previous_grid();
+    int64_t sent = 0;
+    auto fetch = [&](int64_t row, int slot) {
+        uint8_t* to = ring.rows + (size_t)slot * slot_bytes;
+        mbar_arrive_expect_tx(ring.full + slot, slot_bytes);
+        bulk_g2s(to, row_of(p.x, p.x_f32, row, p.ld_x), x_bytes, ring.full + slot);
+        bulk_g2s(to + x_bytes, row_of(p.dy, p.dy_f32, row, p.ld_dy), dy_bytes, ring.full + slot);
+        if (res_bytes)
+            bulk_g2s(to + x_bytes + dy_bytes, row_of(p.residual, p.dx_f32, row, p.ld_res), res_bytes, ring.full + slot);
+        ++sent;
+    };
+    if (t == 0) {
+        if (p.force_timeout_ns) norm_wait(ring, ring.never, 0, p.force_timeout_ns, p.status);
+        int64_t row = blockIdx.x;
+        for (int s = 0; s < ring.slots && row < p.rows; ++s, row += gridDim.x) fetch(row, s);
+    }
+    float w[NV][8], dw[NV][8], db[NV][8];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        load_floats<T, true>(w[j], p.weight, t, j, n_cols, 1.0f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[j][i] = db[j][i] = 0.0f;
+    }
+    auto stats_of = [&](int64_t row) {
+        return row < p.rows ? make_float2(p.center ? p.stats[2 * row] : 0.0f, p.stats[2 * row + 1]) : make_float2(0.0f, 0.0f);
+    };
+    float2 next = stats_of(blockIdx.x);
+    int slot = 0, turn = 0;
+    uint32_t parity = 0;
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
+        const float mean = next.x, rstd = next.y;
+        next = stats_of(row + gridDim.x);
+        norm_wait(ring, ring.full + slot, parity, p.timeout_ns, p.status);
+        const uint8_t* at = ring.rows + (size_t)slot * slot_bytes;
+        float xh[NV][8], u[NV][8];
+        Raw8<WIDE> res[NV];
+        float su = 0.0f, sux = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c0 = row_at<T, true>(t, j, 0);
+            Raw8<WIDE> x{}, dy{};
+            res[j] = Raw8<WIDE>{};
+            if (c0 < n_cols) {
+                from_shared(x, at, p.x_f32, c0);
+                from_shared(dy, at + x_bytes, p.dy_f32, c0);
+                if (res_bytes) from_shared(res[j], at + x_bytes + dy_bytes, p.dx_f32, c0);
+            }
+            unpack_raw(x, p.x_f32, xh[j]);
+            unpack_raw(dy, p.dy_f32, u[j]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                // (beyond the row dy is 0, which keeps x's part out of every sum)
+                xh[j][i] = (xh[j][i] - mean) * rstd;
+                dw[j][i] = fmaf(u[j][i], xh[j][i], dw[j][i]);
+                db[j][i] += u[j][i];
+                u[j][i] *= w[j][i];
+                su += u[j][i];
+                sux = fmaf(u[j][i], xh[j][i], sux);
+            }
+        }
+        su = lanes_sum<32>(su);
+        sux = lanes_sum<32>(sux);
+        if (lane == 0) ring.red[turn * kWarps + warp] = make_float2(su, sux);
+        __syncthreads();  // (every thread has its part of the row: dx may take its place)
+        if (*ring.gone) break;
+        if (t == 0 && row + (int64_t)ring.slots * gridDim.x < p.rows) fetch(row + (int64_t)ring.slots * gridDim.x, slot);
+        if (p.dx) {
+            const float2 part = lane < kWarps ? ring.red[turn * kWarps + lane] : make_float2(0.0f, 0.0f);
+            const float mu = p.center ? lanes_sum<32>(part.x) * per : 0.0f, mux = lanes_sum<32>(part.y) * per;
+            void* dx = row_of(p.dx, p.dx_f32, row, p.ld_dx);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float r[8];
+                unpack_raw(res[j], p.dx_f32, r);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) u[j][i] = fmaf(fmaf(-xh[j][i], mux, u[j][i] - mu), rstd, r[i]);
+                store_row<T, true>(dx, p.dx_f32, t, j, n_cols, u[j]);
+            }
+        }
+        if (++slot == ring.slots) slot = 0, parity ^= 1;
+    }
+    if (*ring.gone) {
+        if (t == 0) norm_drain(ring, sent, p.timeout_ns);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if (p.part_w) store_row<T, true>(p.part_w + (int64_t)blockIdx.x * p.cols, true, t, j, n_cols, dw[j]);
+        if (p.part_b) store_row<T, true>(p.part_b + (int64_t)blockIdx.x * p.cols, true, t, j, n_cols, db[j]);
     }
 }
 

@@ -24,6 +24,10 @@ struct NormParams {
     int64_t ld_y;
     int y_f32;
     float* stats;         // [rows, 2]: mean, 1 / deviation; or NULL
+    int slots;            // of the ring, where rows come through shared memory
+    uint64_t timeout_ns;
+    uint64_t force_timeout_ns;
+    unsigned int* status;
 };
 
 struct NormGradParams {
@@ -45,6 +49,10 @@ struct NormGradParams {
     int dx_f32;
     float* part_w;         // [CTAs of rows, cols] partial sums, or NULL
     float* part_b;
+    int slots;
+    uint64_t timeout_ns;
+    uint64_t force_timeout_ns;
+    unsigned int* status;
 };
 
 struct PartSumParams {

@@ -11,6 +11,8 @@
 
 namespace quasar {
 const void* layer_norm_kernel(int64_t cols, bool vectors, bool grad, bool wide, int* threads, int* rows, int* per_sm);
+const void* layer_norm_ring_kernel(int64_t cols, bool grad, bool wide, int* threads, int* per_sm);
+int layer_norm_slots(uint32_t slot_bytes, int threads, int per_sm, size_t* smem);
 const void* layer_norm_long_kernel();
 const void* layer_norm_grad_long_kernel();
 const void* layer_norm_grad_columns_kernel();
@@ -49,7 +51,9 @@ quasar_status norm_parts(int64_t rows, int64_t cols, int64_t* parts)
     unsigned int* status = nullptr;
     const quasar_status st = host_device(&n_sm, &status);
     if (st != QUASAR_OK) return st;
-    if (layer_norm_kernel(cols, true, true, false, &threads, &at_once, &per_sm))
+    if (layer_norm_ring_kernel(cols, true, false, &threads, &per_sm))  // (whichever kernel it will be)
+        *parts = std::min<int64_t>(rows, (int64_t)n_sm * per_sm);
+    else if (layer_norm_kernel(cols, true, true, false, &threads, &at_once, &per_sm))
         *parts = std::min<int64_t>((rows + at_once - 1) / at_once, (int64_t)n_sm * per_sm);
     else
         *parts = std::min(rows, kColumnParts);
@@ -100,11 +104,19 @@ quasar_status quasar_layer_norm(const void* x, quasar_dtype x_dtype, int64_t ld_
     const quasar_status st = host_device(&n_sm, &status);
     if (st != QUASAR_OK) return st;
     NormParams p{x, ld_x, x_dtype == QUASAR_F32, weight, bias, rows, cols, center, eps,
-                 y, ld_y, y_dtype == QUASAR_F32, stats};
+                 y, ld_y, y_dtype == QUASAR_F32, stats, 0, host_timeout_ns(), host_forced_timeout_ns(), status};
     const bool vectors = vector_rows(x, rows, ld_x, x_dtype) && vector_rows(y, rows, ld_y, y_dtype) &&
                          aligned(weight, 16) && aligned(bias, 16);
     int threads = 0, at_once = 0, per_sm = 0;
-    const void* fn = layer_norm_kernel(cols, vectors, false, x_dtype == QUASAR_F32, &threads, &at_once, &per_sm);
+    const bool wide = x_dtype == QUASAR_F32;
+    if (vectors) {
+        if (const void* ring = layer_norm_ring_kernel(cols, false, wide, &threads, &per_sm)) {
+            size_t smem = 0;
+            p.slots = layer_norm_slots((uint32_t)(cols * dtype_size(x_dtype)), threads, per_sm, &smem);
+            return launch(ring, &p, dim3((unsigned)std::min<int64_t>(rows, (int64_t)n_sm * per_sm)), threads, 1, smem, stream);
+        }
+    }
+    const void* fn = layer_norm_kernel(cols, vectors, false, wide, &threads, &at_once, &per_sm);
     if (!fn)
         return launch(layer_norm_long_kernel(), &p, dim3((unsigned)std::min<int64_t>(rows, (int64_t)n_sm * 4)), 512, 1,
                       0, stream);
@@ -163,7 +175,9 @@ quasar_status quasar_layer_norm_backward(const void* dy, quasar_dtype dy_dtype, 
         if (overlaps(b_ws, b)) return QUASAR_ERR_INVALID_ARG;
     NormGradParams p{dy,   ld_dy,  dy_dtype == QUASAR_F32, x,        ld_x,        x_dtype == QUASAR_F32,
                      weight, stats, rows, cols, center, residual, ld_residual, dx, ld_dx, dx_dtype == QUASAR_F32,
-                     nullptr, nullptr};
+                     nullptr, nullptr, 0, host_timeout_ns(), host_forced_timeout_ns(), nullptr};
+    int n_sm = 0;
+    if ((st = host_device(&n_sm, &p.status)) != QUASAR_OK) return st;
     float* const partial = static_cast<float*>(workspace);
     if (dweight) p.part_w = parts <= 1 ? dweight : partial;
     if (dbias) p.part_b = parts <= 1 ? dbias : partial + parts * cols;
@@ -174,8 +188,14 @@ quasar_status quasar_layer_norm_backward(const void* dy, quasar_dtype dy_dtype, 
                              aligned(weight, 16);
         int threads = 0, at_once = 0, per_sm = 0;
         const bool wide = x_dtype == QUASAR_F32 || dy_dtype == QUASAR_F32 || (residual && dx_dtype == QUASAR_F32);
-        const void* fn = layer_norm_kernel(cols, vectors, true, wide, &threads, &at_once, &per_sm);
-        if (fn) {
+        const void* ring = vectors ? layer_norm_ring_kernel(cols, true, wide, &threads, &per_sm) : nullptr;
+        const void* fn = ring ? nullptr : layer_norm_kernel(cols, vectors, true, wide, &threads, &at_once, &per_sm);
+        if (ring) {
+            size_t smem = 0;
+            const int64_t bytes = cols * (dtype_size(x_dtype) + dtype_size(dy_dtype) + (residual ? dtype_size(dx_dtype) : 0));
+            p.slots = layer_norm_slots((uint32_t)bytes, threads, per_sm, &smem);
+            if ((st = launch(ring, &p, dim3((unsigned)parts), threads, 1, smem, stream)) != QUASAR_OK) return st;
+        } else if (fn) {
             if ((st = launch(fn, &p, dim3((unsigned)parts), threads, 1, 0, stream)) != QUASAR_OK) return st;
         } else {
             // (the columns' sums first: dx may take dy's or x's place)

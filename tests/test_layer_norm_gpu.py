@@ -195,3 +195,51 @@ def test_streams_and_graphs():
     torch.cuda.synchronize()
     for _, o in graphs:
         assert all(torch.equal(o[k], want[k]) for k in want)
+
+
+def test_a_wait_that_runs_out_is_reported():
+    from paper_2608_13966_gb300 import quasar as Q
+
+    for rows in (3, 5000):
+        x, dy = made(rows, 4096, BF16), made(rows, 4096, BF16, seed=3)
+        want = api.layer_norm(x, stats=True)
+        grads = api.layer_norm_backward(dy, x, None, want["stats"], dbias=True)
+        api.check_device()
+        for call in (lambda: api.layer_norm(x), lambda: api.layer_norm_backward(dy, x, None, want["stats"])):
+            Q.quasar_debug_force_timeout(1_000_000)
+            try:
+                call()
+                assert Q.quasar_get_device_status() == Q.QuasarStatus.ERR_TIMEOUT
+            finally:
+                Q.quasar_debug_force_timeout(0)
+        assert torch.equal(api.layer_norm(x)["y"], want["y"])
+        again = api.layer_norm_backward(dy, x, None, want["stats"], dbias=True)
+        assert all(torch.equal(again[k], grads[k]) for k in grads)
+        api.check_device()
+
+
+@pytest.mark.parametrize("cols", [64, 1003, 2048, 8192, 16384, 20000])
+def test_in_place(cols):
+    """y in x's place; dx in dy's, x's or the residual's; guards around them stay."""
+    from paper_2608_13966_gb300 import quasar as Q
+
+    rows, ld = 700, cols + 8
+    def wide(seed, dtype=BF16):
+        t = torch.full((rows, ld), 99.0, dtype=dtype, device="cuda")
+        t[:, :cols] = made(rows, cols, dtype, seed=seed)
+        return t
+    x = wide(0)
+    o = api.layer_norm(x[:, :cols], stats=True)
+    assert Q.quasar_layer_norm(x, Q.BF16, ld, None, None, rows, cols, 1, 1e-5, x, Q.BF16, ld) == Q.QuasarStatus.OK
+    assert torch.equal(x[:, :cols], o["y"]) and (x[:, cols:] == 99).all()
+    need = Q.quasar_layer_norm_backward_workspace(rows, cols)
+    ws = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
+    for place in range(3):
+        x, dy, res = wide(0), wide(3), wide(4)
+        want = api.layer_norm_backward(dy[:, :cols], x[:, :cols], None, o["stats"], dbias=True, residual=res[:, :cols])
+        dw, db = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+        dx = (dy, x, res)[place]
+        assert Q.quasar_layer_norm_backward(dy, Q.BF16, ld, x, Q.BF16, ld, None, o["stats"], rows, cols, 1, res, ld, dx,
+                                            Q.BF16, ld, dw, db, ws, need) == Q.QuasarStatus.OK
+        assert torch.equal(dx[:, :cols], want["dx"]) and (dx[:, cols:] == 99).all()
+        assert torch.equal(dw, want["dweight"]) and torch.equal(db, want["dbias"])
