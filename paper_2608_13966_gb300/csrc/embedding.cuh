@@ -78,35 +78,47 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_ids(const __grid_constant
     uint32_t* count = reinterpret_cast<uint32_t*>(smem_raw);  // [warps][bins]
     uint32_t* total = count + kWarps * kBins;                 // [bins], read by the cluster
     uint32_t* scan = total + kBins;                           // [kBins / 32]
+    uint32_t* halves = scan + kBins / 32;                     // [bins]
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = p.ctas > 1 ? (int)cluster_rank() : 0;
     const int64_t gw = rank * kWarps + warp, all = (int64_t)p.ctas * kWarps;
     const int from = (int)(p.n * gw / all), to = (int)(p.n * (gw + 1) / all);
+    const bool held = to - from <= 128;  // 4 entries a lane, kept between a pass's two walks
     uint32_t* mine = count + warp * kBins;
+    // a bin's column of counts, half of the warps each
+    const int bin = threadIdx.x % kBins, part = threadIdx.x / kBins;
+    static_assert(kSortThreads == 2 * kBins, "two threads a bin");
+    uint32_t* column = count + part * (kWarps / 2) * kBins + bin;
     wait_for_previous_grid();
 
     for (int pass = 0; pass < p.passes; ++pass) {
         const int shift = pass * kSortBits;
         const int in = (p.passes - pass) & 1, out = in ^ 1;  // (the last pass writes to 0)
-        auto load = [&](int i, uint32_t& key, uint32_t& place) {
-            key = 0, place = (uint32_t)i;
-            if (i >= to) return;
-            if (pass == 0) {
-                const int64_t id = id_at(p.ids, p.ids_64, i, p.vocab);
-                key = (uint32_t)(id < 0 ? p.vocab : id);
-            } else {
-                key = __ldcg(p.keys[in] + i);
-                place = __ldcg(p.places[in] + i);
-            }
-        };
-        for (int b = threadIdx.x; b < kWarps * kBins; b += kSortThreads) count[b] = 0;
-        __syncthreads();
-        for (int i0 = from; i0 < to; i0 += 128) {
-            uint32_t key[4], place[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) load(i0 + 32 * q + lane, key[q], place[q]);
+        uint32_t key[4], place[4];
+        auto load = [&](int i0) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
+                const int i = i0 + 32 * q + lane;
+                key[q] = 0, place[q] = (uint32_t)i;
+                if (i >= to) continue;
+                if (pass == 0) {
+                    const int64_t id = id_at(p.ids, p.ids_64, i, p.vocab);
+                    key[q] = (uint32_t)(id < 0 ? p.vocab : id);
+                } else {
+                    key[q] = __ldcg(p.keys[in] + i);
+                    place[q] = __ldcg(p.places[in] + i);
+                }
+            }
+        };
+        for (int b = threadIdx.x; b < kWarps * kBins / 4; b += kSortThreads)
+            reinterpret_cast<uint4*>(count)[b] = make_uint4(0, 0, 0, 0);
+        load(from);
+        __syncthreads();
+        for (int i0 = from; i0 < to; i0 += 128) {
+            if (i0 > from) load(i0);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (i0 + 32 * q >= to) break;
                 const bool live = i0 + 32 * q + lane < to;
                 const uint32_t digit = live ? key[q] >> shift & (kBins - 1) : kBins;
                 const uint32_t same = __match_any_sync(0xffffffffu, digit);
@@ -115,50 +127,57 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_ids(const __grid_constant
             }
         }
         __syncthreads();
-        if (threadIdx.x < kBins) {
-            uint32_t s = 0;
-            for (int w = 0; w < kWarps; ++w) {
-                const uint32_t c = count[w * kBins + threadIdx.x];
-                count[w * kBins + threadIdx.x] = s;
-                s += c;
-            }
-            total[threadIdx.x] = s;
+        // a bin's counts become what its warps before have
+        uint32_t sum = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps / 2; ++w) {
+            const uint32_t c = column[w * kBins];
+            column[w * kBins] = sum;
+            sum += c;
         }
+        if (part == 0) halves[bin] = sum;
+        __syncthreads();
+        if (part == 1) total[bin] = halves[bin] + sum;
         __syncthreads();
         if (p.ctas > 1) cluster_sync();
-        uint32_t bin = 0, before = 0;  // this bin's entries: all, and in the CTAs before
-        if (threadIdx.x < kBins) {
-            for (int c = 0; c < p.ctas; ++c) {
-                uint32_t n = total[threadIdx.x];
-                if (p.ctas > 1)
+        uint32_t whole = 0, before = 0;  // this bin's entries: all, and in the CTAs before
+        if (p.ctas > 1) {
+            uint32_t n[kSortCtas];
+#pragma unroll
+            for (int c = 0; c < kSortCtas; ++c) {
+                n[c] = 0;
+                if (c < p.ctas)
                     asm volatile("ld.shared::cluster.u32 %0, [%1];"
-                                 : "=r"(n)
-                                 : "r"(peer_addr(smem_u32(total + threadIdx.x), (uint32_t)c))
+                                 : "=r"(n[c])
+                                 : "r"(peer_addr(smem_u32(total + bin), (uint32_t)c))
                                  : "memory");
-                bin += n;
-                if (c < rank) before += n;
             }
+#pragma unroll
+            for (int c = 0; c < kSortCtas; ++c) {
+                whole += n[c];
+                if (c < rank) before += n[c];
+            }
+        } else {
+            whole = total[bin];
         }
-        uint32_t upto = bin;  // inclusive sum over the bins
+        uint32_t upto = whole;  // inclusive sum over the bins
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
             if (lane >= o) upto += x;
         }
-        if (threadIdx.x < kBins && lane == 31) scan[warp] = upto;
+        if (part == 0 && lane == 31) scan[warp] = upto;
         __syncthreads();
-        if (threadIdx.x < kBins) {
-            uint32_t base = upto - bin + before;
-            for (int w = 0; w < warp; ++w) base += scan[w];
-            for (int w = 0; w < kWarps; ++w) count[w * kBins + threadIdx.x] += base;
-        }
+        uint32_t base = upto - whole + before + (part ? halves[bin] : 0);
+        for (int w = 0; w < bin / 32; ++w) base += scan[w];
+#pragma unroll
+        for (int w = 0; w < kWarps / 2; ++w) column[w * kBins] += base;
         __syncthreads();
         for (int i0 = from; i0 < to; i0 += 128) {
-            uint32_t key[4], place[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) load(i0 + 32 * q + lane, key[q], place[q]);
+            if (!held) load(i0);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
+                if (i0 + 32 * q >= to) break;
                 const bool live = i0 + 32 * q + lane < to;
                 const uint32_t digit = live ? key[q] >> shift & (kBins - 1) : kBins;
                 const uint32_t same = __match_any_sync(0xffffffffu, digit);
@@ -182,24 +201,21 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_ids(const __grid_constant
 
 // -- the gradient ------------------------------------------------------------------
 
-// Where the elements of token i (of the sorted ones) lie that this CTA takes.
-__device__ __forceinline__ const void* dy_row(const EmbedGradParams& p, int i, int64_t c0)
+// sum += the rows of the tokens places[i] .. places[end - 1], N on their way at
+// once.
+template <int N, bool VECTORS, bool WIDE>
+__device__ __forceinline__ void add_rows(float (&sum)[8], const EmbedGradParams& p, const uint32_t* places, int i, int end,
+                                         int64_t c0, int cols)
 {
-    return static_cast<const uint8_t*>(row_of(p.dy, p.dy_f32, p.places[i], p.ld_dy)) + c0 * (p.dy_f32 ? 4 : 2);
-}
-
-// sum += the rows of tokens [i, end), eight on their way at once.
-template <bool VECTORS, bool WIDE>
-__device__ __forceinline__ void add_rows(float (&sum)[8], const EmbedGradParams& p, int i, int end, int64_t c0, int cols)
-{
-    for (; i < end; i += 8) {
-        Raw8<WIDE> raw[8];
+    const uint8_t* dy = static_cast<const uint8_t*>(p.dy) + c0 * (p.dy_f32 ? 4 : 2);
+    for (; i < end; i += N) {
+        Raw8<WIDE> raw[N];
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
-            load_raw<kEmbedThreads, VECTORS>(raw[q], dy_row(p, min(i + q, end - 1), c0), p.dy_f32, threadIdx.x, 0,
-                                             i + q < end ? cols : 0);
+        for (int q = 0; q < N; ++q)
+            load_raw<kEmbedThreads, VECTORS>(raw[q], row_of(static_cast<const void*>(dy), p.dy_f32, places[min(i + q, end - 1)], p.ld_dy),
+                                             p.dy_f32, threadIdx.x, 0, i + q < end ? cols : 0);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
+        for (int q = 0; q < N; ++q) {
             float v[8];
             unpack_raw(raw[q], p.dy_f32, v);
 #pragma unroll
@@ -214,14 +230,17 @@ __device__ __forceinline__ void add_rows(float (&sum)[8], const EmbedGradParams&
 template <bool VECTORS, bool WIDE>
 __global__ void __launch_bounds__(kEmbedThreads) k_embedding_chunks(const __grid_constant__ EmbedGradParams p)
 {
+    __shared__ uint32_t places[kRunChunk];
     wait_for_previous_grid();
     const int i0 = (int)blockIdx.x * kRunChunk;
     const uint32_t id = p.keys[i0];
+    if (threadIdx.x < kRunChunk) places[threadIdx.x] = p.places[i0 + threadIdx.x];
     if (id >= p.vocab || id != p.keys[i0 + kRunChunk - 1]) return;
+    __syncthreads();
     const int64_t c0 = (int64_t)blockIdx.y * kEmbedCols;
     const int cols = (int)(p.width - c0 < kEmbedCols ? p.width - c0 : kEmbedCols);
     float sum[8] = {};
-    add_rows<VECTORS, WIDE>(sum, p, i0, i0 + kRunChunk, c0, cols);
+    add_rows<WIDE ? 8 : 16, VECTORS, WIDE>(sum, p, places, 0, kRunChunk, c0, cols);
     float* to = p.sums + (int64_t)blockIdx.x * p.width + c0;
     store_row<kEmbedThreads, VECTORS>(to, true, threadIdx.x, 0, cols, sum);
 }
@@ -253,20 +272,35 @@ __global__ void __launch_bounds__(kEmbedThreads) k_embedding_grad(const __grid_c
     if (threadIdx.x <= rows) ends[threadIdx.x] = lower_bound(p.keys, 0, p.n, (uint32_t)(v0 + threadIdx.x));
     __syncthreads();
     if (p.add && ends[0] == ends[rows]) return;
-    uint8_t* row = static_cast<uint8_t*>(row_of(p.dtable, p.f32, v0, p.ld)) + c0 * (p.f32 ? 4 : 2);
+    uint8_t* const first = static_cast<uint8_t*>(row_of(p.dtable, p.f32, v0, p.ld)) + c0 * (p.f32 ? 4 : 2);
     const int64_t pitch = p.ld * (p.f32 ? 4 : 2);
+    if (!p.add) {  // the rows without tokens
+        uint8_t* row = first;
+        if (VECTORS && (int)threadIdx.x * 8 + 8 <= cols) {
+            row += threadIdx.x * (p.f32 ? 32 : 16);
+            const uint4 zero = make_uint4(0, 0, 0, 0);
+#pragma unroll 4
+            for (int r = 0; r < rows; ++r, row += pitch)
+                if (ends[r] == ends[r + 1]) {
+                    __stcs(reinterpret_cast<uint4*>(row), zero);
+                    if (p.f32) __stcs(reinterpret_cast<uint4*>(row) + 1, zero);
+                }
+        } else {
+            const float zeros[8] = {};
+            for (int r = 0; r < rows; ++r, row += pitch)
+                if (ends[r] == ends[r + 1]) store_row<kEmbedThreads, VECTORS>(row, p.f32, threadIdx.x, 0, cols, zeros);
+        }
+    }
     int i = ends[0];
 #pragma unroll 1
-    for (int r = 0; r < rows; ++r, row += pitch) {
+    for (int r = 0; r < rows; ++r) {
         const int end = ends[r + 1];
+        if (i == end) continue;
+        uint8_t* const row = first + r * pitch;
         float sum[8] = {};
-        if (i == end) {
-            if (!p.add) store_row<kEmbedThreads, VECTORS>(row, p.f32, threadIdx.x, 0, cols, sum);
-            continue;
-        }
         // up to the first whole chunk, the chunks, and from the last on
         const int head = min(end, (i + kRunChunk - 1) / kRunChunk * kRunChunk);
-        add_rows<VECTORS, WIDE>(sum, p, i, head, c0, cols);
+        add_rows<8, VECTORS, WIDE>(sum, p, p.places, i, head, c0, cols);
         const int tail = max(head, end / kRunChunk * kRunChunk);
 #pragma unroll 4
         for (int q = head / kRunChunk; q < tail / kRunChunk; ++q) {
@@ -275,7 +309,7 @@ __global__ void __launch_bounds__(kEmbedThreads) k_embedding_grad(const __grid_c
 #pragma unroll
             for (int x = 0; x < 8; ++x) sum[x] += v[x];
         }
-        add_rows<VECTORS, WIDE>(sum, p, tail, end, c0, cols);
+        add_rows<8, VECTORS, WIDE>(sum, p, p.places, tail, end, c0, cols);
         i = end;
 #pragma unroll
         for (int x = 0; x < 8; ++x) sum[x] *= p.scale;

@@ -21,7 +21,7 @@ const void* sort_ids_kernel() { return reinterpret_cast<const void*>(&k_sort_ids
 
 size_t sort_ids_smem()
 {
-    return ((size_t)(kSortThreads / 32) * (1 << kSortBits) + (1 << kSortBits) + (1 << kSortBits) / 32) * 4;
+    return ((size_t)(kSortThreads / 32) * (1 << kSortBits) + 2 * (1 << kSortBits) + (1 << kSortBits) / 32) * 4;
 }
 
 }  // namespace quasar
