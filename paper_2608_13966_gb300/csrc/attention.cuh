@@ -19,8 +19,10 @@
 // P is rounded to bf16 for the matrix product (half a step, 2^-9 relative at
 // most, independent from key to key); l is the sum before the rounding.
 //
-// Where rows are few, a cluster of CTAs shares a row's keys and joins its
-// parts through distributed shared memory, in rank order.
+// Where rows are few, a cluster of CTAs shares a row's keys, and where there are
+// rows for one tile alone, the tiles are twins: the same rows, every other key
+// tile each.  The parts are joined through (distributed) shared memory, always
+// in the same order.
 //
 // Warps: 0-7 and 8-15 the rows of tiles 0 and 1, two threads a row, 64 keys of a
 // key tile each, that exchange their maxima (with one thread a row the 4 warps
@@ -202,20 +204,31 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
     const AttnItem a = *item;
     const int t0 = a.index * 2 * p.tile_tokens;  // first token of tile 0
 
-    // this CTA's key tiles: of tile i, n_i from `first` on
-    int first = 0, n[2] = {0, 0};
+    // This CTA's key tiles: `count` from `first` on; tile i takes n_i of them
+    // (twins: every other one).  They come as entries of the ring, a key tile
+    // with the values of the one `lag` before it.
+    int first = 0, count = 0, n[2] = {0, 0};
+    bool twins = false;
     if (a.spares == 0) {
         n[0] = key_tiles(a, t0, t0 + p.tile_tokens, p.causal);
         n[1] = key_tiles(a, t0 + p.tile_tokens, t0 + 2 * p.tile_tokens, p.causal);
+        twins = a.n - t0 <= p.tile_tokens && n[0] > 1;
         const int most = max(n[0], n[1]);
         first = (int)((int64_t)most * rank / p.split);
-        const int stop = (int)((int64_t)most * (rank + 1) / p.split);
-        n[0] = max(min(n[0], stop) - first, 0);
-        n[1] = max(min(n[1], stop) - first, 0);
+        count = (int)((int64_t)most * (rank + 1) / p.split) - first;
+        if (twins) {
+            n[0] = (count + 1) / 2;
+            n[1] = count / 2;
+        } else {
+            n[0] = max(min(n[0] - first, count), 0);
+            n[1] = max(min(n[1] - first, count), 0);
+        }
     }
     n[0] = uniform(n[0]);
     n[1] = uniform(n[1]);
-    const int steps = max(n[0], n[1]);
+    twins = uniform((int)twins) != 0;
+    const int lag = twins ? 2 : 1;
+    const int steps = max(n[0], n[1]), entries = uniform(steps > 0 ? count + lag : 0);
 
     if (a.spares > 0 && rank == 0) {
         clear_rows(p.y, p.ld_y, (int64_t)kvh * p.group * p.d, p.group * p.d, p.s.starts, p.s.n, p.s.tokens, a.index, a.spares);
@@ -227,28 +240,29 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
         if (warp == kAttnCopies) {
             if (lane == 0) {
                 if (p.force_timeout_ns) role_sleep(never, 0, gone, p.force_timeout_ns, p.status);
-                int it = 0;  // entries of the ring: K_0; V_0, K_1; V_1, K_2; ... V_last
+                int it = 0;
                 const bool rows_sent = steps > 0 && !*gone;
                 if (rows_sent) {
                     const uint32_t bytes = (uint32_t)(p.tile_tokens * p.group) * 128 * DB;
-                    mbar_arrive_expect_tx(q_full, (n[0] > 0 ? bytes : 0) + (n[1] > 0 ? bytes : 0));
+                    mbar_arrive_expect_tx(q_full, (n[0] > 0 ? bytes : 0) + (n[1] > 0 && !twins ? bytes : 0));
                     for (int i = 0; i < 2; ++i)
-                        if (n[i] > 0)
+                        if (n[i] > 0 && !(twins && i == 1))
                             for (int b = 0; b < DB; ++b)
                                 tile_g2s_3d(smem_u32(smem + i * kTile + b * kAttnBlock), &p.q, 64 * b, kvh * p.group,
                                             a.q0 + t0 + i * p.tile_tokens, smem_u32(q_full));
                 }
-                for (; steps > 0 && it <= steps && !*gone; ++it) {
+                for (; it < entries && !*gone; ++it) {
                     const int s = it % kAttnSlots;
                     if (it >= kAttnSlots &&
                         !role_sleep(empty + s, (it / kAttnSlots - 1) & 1, gone, p.timeout_ns, p.status))
                         break;
-                    mbar_arrive_expect_tx(full + s, (it > 0 ? kTile : 0) + (it < steps ? kTile : 0));
+                    const bool values = it >= lag, keys = it < count;
+                    mbar_arrive_expect_tx(full + s, (values ? kTile : 0) + (keys ? kTile : 0));
                     const uint32_t to = smem_u32(ring + s * 2 * kTile);
                     const int key = a.k0 + (first + it) * kAttnKeys;
                     for (int b = 0; b < DB; ++b) {
-                        if (it > 0) tile_g2s_3d(to + b * kAttnBlock, &p.v, 64 * b, kvh, key - kAttnKeys, smem_u32(full + s));
-                        if (it < steps) tile_g2s_3d(to + kTile + b * kAttnBlock, &p.k, 64 * b, kvh, key, smem_u32(full + s));
+                        if (values) tile_g2s_3d(to + b * kAttnBlock, &p.v, 64 * b, kvh, key - lag * kAttnKeys, smem_u32(full + s));
+                        if (keys) tile_g2s_3d(to + kTile + b * kAttnBlock, &p.k, 64 * b, kvh, key, smem_u32(full + s));
                     }
                 }
                 if (*gone) {  // what is in flight has landed before the memory is let go
@@ -270,14 +284,14 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                 return __all_sync(0xffffffffu, ok);
             };
             bool ok = steps == 0 || wait(q_full, 0);
-            for (int j = -1; steps > 0 && j < steps && ok; ++j) {
-                const int e = j + 1, s = e % kAttnSlots;
+            for (int e = 0; e < entries && ok; ++e) {
+                const int s = e % kAttnSlots;
                 if (!(ok = wait(full + s, (e / kAttnSlots) & 1))) break;
                 uint8_t* const values = ring + s * 2 * kTile;
                 // rows of V behind the sequence belong to another, or to nobody:
                 // their probabilities are 0, but 0 times what lies there need not be
-                const int left = a.m - (first + j) * kAttnKeys;
-                if (j >= 0 && left < kAttnKeys) {
+                const int left = a.m - (first + e - lag) * kAttnKeys;
+                if (e >= lag && left < kAttnKeys) {
                     for (int x = lane + left * 8; x < kAttnKeys * 8; x += 32)
 #pragma unroll
                         for (int b = 0; b < DB; ++b)
@@ -289,6 +303,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                 const uint64_t dk = operand_desc(smem_u32(values + kTile), false);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
+                    if (twins && i != (e & 1)) continue;
+                    const int j = (twins ? e >> 1 : e) - 1;  // of the values, in the tile's own steps
                     if (j >= 0 && j < n[i] && !(ok = wait(p_full + i, j & 1))) break;
                     tc_fence_after();
                     if (elect_one()) {
@@ -300,7 +316,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                             mma_commit(smem_u32(o_full + i));
                         }
                         if (j + 1 < n[i]) {  // S = Q K^T
-                            const uint64_t dq = operand_desc(smem_u32(smem + i * kTile), false);
+                            const uint64_t dq = operand_desc(smem_u32(smem + (twins ? 0 : i) * kTile), false);
 #pragma unroll
                             for (int b = 0; b < DB; ++b)
 #pragma unroll
@@ -309,7 +325,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                                                 dk + b * (kAttnBlock >> 4) + x * k_step(false), desc_s, b + x > 0);
                             mma_commit(smem_u32(s_full + i));
                         }
-                        if (i == 1) mma_commit(smem_u32(empty + s));
+                        if (i == 1 || twins) mma_commit(smem_u32(empty + s));
                     }
                     __syncwarp();
                 }
@@ -320,16 +336,16 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
             }
         }
         __syncwarp();
-        if (p.split > 1 && a.spares == 0) {  // the barriers of the rows' warps
+        if ((p.split > 1 || twins) && a.spares == 0) {  // the barriers of the rows' warps
             __syncthreads();
-            cluster_sync();
-            cluster_sync();
+            p.split > 1 ? cluster_sync() : __syncthreads();
+            if (p.split > 1) cluster_sync();
         }
     } else {
         registers_up<104>();
         // a thread's row: r of tile i; its half of the row's keys, and of its columns
         const int i = warp >> 3 & 1, half = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
-        const int token = t0 + i * p.tile_tokens + r / p.group, head = kvh * p.group + r % p.group;
+        const int token = t0 + (twins ? 0 : i) * p.tile_tokens + r / p.group, head = kvh * p.group + r % p.group;
         const bool live = a.spares == 0 && r < p.tile_tokens * p.group && token < a.n;
         const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         constexpr int kHalf = D / 2;
@@ -362,7 +378,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                     for (int c = 0; c < 2; ++c) tmem_ld(s_at + 32 * c, s[c]);
 #pragma unroll
                     for (int c = 0; c < 2; ++c) tmem_wait_ld(s[c]);
-                    const int64_t key0 = (int64_t)(first + j) * kAttnKeys + 64 * half;
+                    const int64_t key0 = (int64_t)(first + (twins ? 2 * j + i : j)) * kAttnKeys + 64 * half;
                     if (!__all_sync(0xffffffffu, see >= key0 + 63)) {
                         const int upto = (int)max((int64_t)-1, min(see - key0, (int64_t)64));
 #pragma unroll
@@ -439,7 +455,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
             }
         }
 
-        if (p.split == 1) {
+        if (p.split == 1 && !twins) {
             if (a.spares == 0 && ok && __any_sync(0xffffffffu, live)) {
                 const float inv = l == 0.0f ? 0.0f : 1.0f / l;
                 // the rows through the query tile's memory, so that a store covers
@@ -494,33 +510,43 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                     }
                 }
             }
-            cluster_sync();
-            constexpr int kVecs = D / 4;
+            p.split > 1 ? cluster_sync() : __syncthreads();
+            constexpr int kVecs = D / 4, kMany = kAttnCopies * 32;
             const int rows = p.tile_tokens * p.group;
-            constexpr int kMany = kAttnCopies * 32;
-            for (int x = rank * kMany + (int)threadIdx.x; x < 2 * rows * kVecs; x += p.split * kMany) {
+            auto peer = [&](const void* x, int q) {
+                return p.split > 1 ? peer_addr(smem_u32(x), (uint32_t)q) : smem_u32(x);
+            };
+            for (int x = rank * kMany + (int)threadIdx.x; x < (twins ? 1 : 2) * rows * kVecs; x += p.split * kMany) {
                 const int tile = x / (rows * kVecs), row = x / kVecs % rows, c = x % kVecs;
                 const int tok = t0 + tile * p.tile_tokens + row / p.group;
                 if (tok >= a.n || 4 * c >= p.d) continue;
                 float top = minus_inf(), total = 0.0f;
-                float2 st[kAttnMostSplit];
+                float2 st[kAttnMostSplit][2];
 #pragma unroll
                 for (int q = 0; q < kAttnMostSplit; ++q)
-                    if (q < p.split) {
-                        const uint32_t at = peer_addr(smem_u32(stat + tile * 128 + row), (uint32_t)q);
-                        asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(st[q].x), "=f"(st[q].y) : "r"(at) : "memory");
-                        top = fmaxf(top, st[q].x);
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        st[q][w] = make_float2(minus_inf(), 0.0f);
+                        if (q >= p.split || (w == 1 && !twins)) continue;
+                        asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];"
+                                     : "=f"(st[q][w].x), "=f"(st[q][w].y)
+                                     : "r"(peer(stat + (tile + w) * 128 + row, q))
+                                     : "memory");
+                        top = fmaxf(top, st[q][w].x);
                     }
                 const float shift = top == minus_inf() ? 0.0f : top;
                 float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
                 for (int q = 0; q < kAttnMostSplit; ++q)
-                    if (q < p.split && st[q].y != 0.0f) {  // (a part without keys left nothing)
-                        const float f = exp2_fast(st[q].x - shift);
-                        const float4 v = ld_peer4(peer_addr(smem_u32(part + (size_t)(tile * 128 + row) * D + (c ^ (row & 7)) * 4), (uint32_t)q));
-                        total = fmaf(f, st[q].y, total);
-                        o.x = fmaf(f, v.x, o.x), o.y = fmaf(f, v.y, o.y), o.z = fmaf(f, v.z, o.z), o.w = fmaf(f, v.w, o.w);
-                    }
+#pragma unroll
+                    for (int w = 0; w < 2; ++w)
+                        if (st[q][w].y != 0.0f) {  // (a part without keys left nothing)
+                            const float f = exp2_fast(st[q][w].x - shift);
+                            const float4 v =
+                                ld_peer4(peer(part + (size_t)((tile + w) * 128 + row) * D + (c ^ (row & 7)) * 4, q));
+                            total = fmaf(f, st[q][w].y, total);
+                            o.x = fmaf(f, v.x, o.x), o.y = fmaf(f, v.y, o.y), o.z = fmaf(f, v.z, o.z), o.w = fmaf(f, v.w, o.w);
+                        }
                 const float inv = total == 0.0f ? 0.0f : 1.0f / total;
                 const int64_t to = (int64_t)(a.q0 + tok);
                 const int h = kvh * p.group + row % p.group;
@@ -529,7 +555,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                 if (p.lse && c == 0)
                     p.lse[to * p.heads + h] = total == 0.0f ? minus_inf() : 0.69314718f * (shift + log2f(total));
             }
-            cluster_sync();  // nobody leaves while its memory is read
+            if (p.split > 1) cluster_sync();  // nobody leaves while its memory is read
         }
     }
     __syncwarp();

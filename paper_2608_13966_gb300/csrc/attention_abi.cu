@@ -103,7 +103,7 @@ quasar_status quasar_attention(const void* q, int64_t ld_q, const void* k, int64
     p.split = 1;
     const void* fn = attention_kernel(p.d);
     const size_t smem = attention_smem(p.d);
-    while (p.split < kAttnMostSplit && work * p.split * 2 <= n_sm && tiles >= 4 * p.split) p.split *= 2;
+    while (p.split < kAttnMostSplit && work * p.split < n_sm && tiles >= 4 * p.split) p.split *= 2;
     if ((st = head_map(q, tokens, heads, head_dim, ld_q, p.group, p.tile_tokens, &p.q)) != QUASAR_OK) return st;
     // (without keys no copy is made: any valid map will do)
     const bool none = keys == 0;
