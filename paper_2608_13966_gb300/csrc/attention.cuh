@@ -8,7 +8,7 @@
 // products run.  For each key tile j and row tile i
 //
 //   S_i = Q_i K_j^T          in tensor memory, 128 x 128 fp32
-//   m, l, P                  P in bf16 takes S's place
+//   m, l, P                  P in bf16 takes S's place, each half in its half
 //   O_i += P V_j             P from tensor memory, V as it lies in memory
 //
 // in one pass over the keys with the running maximum m and sum l of the
@@ -37,7 +37,7 @@
 
 namespace quasar {
 
-constexpr int kAttnThreads = 640;  // 20 warps, two of them idle: registers move by groups of four
+constexpr int kAttnThreads = 576;
 constexpr int kAttnCopies = 16, kAttnProducts = 17;  // warps
 constexpr int kAttnSlots = 2;             // of the ring, each a tile of values and one of keys
 constexpr float kAttnSlack = 8.0f;        // log2 of how far m may fall behind
@@ -234,9 +234,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
         clear_rows(p.y, p.ld_y, (int64_t)kvh * p.group * p.d, p.group * p.d, p.s.starts, p.s.n, p.s.tokens, a.index, a.spares);
         clear_lse(p.lse, p.heads, kvh * p.group, p.group, p.s.starts, p.s.n, p.s.tokens, a.index, a.spares);
     }
-    // registers: 640 threads start with 96; 512 x 104 + 128 x 64 is as many
     if (warp >= kAttnCopies) {
-        registers_down<64>();
         if (warp == kAttnCopies) {
             if (lane == 0) {
                 if (p.force_timeout_ns) role_sleep(never, 0, gone, p.force_timeout_ns, p.status);
@@ -312,7 +310,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                         if (j >= 0 && j < n[i]) {
 #pragma unroll
                             for (int x = 0; x < kAttnKeys / 16; ++x)
-                                mma_bf16_ts(o_at, s_at + 8 * x, dv + x * k_step(true), desc_o, j > 0 || x > 0);
+                                mma_bf16_ts(o_at, s_at + x / 4 * 64 + x % 4 * 8, dv + x * k_step(true), desc_o, j > 0 || x > 0);
                             mma_commit(smem_u32(o_full + i));
                         }
                         if (j + 1 < n[i]) {  // S = Q K^T
@@ -342,7 +340,6 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
             if (p.split > 1) cluster_sync();
         }
     } else {
-        registers_up<104>();
         // a thread's row: r of tile i; its half of the row's keys, and of its columns
         const int i = warp >> 3 & 1, half = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
         const int token = t0 + (twins ? 0 : i) * p.tile_tokens + r / p.group, head = kvh * p.group + r % p.group;
@@ -363,46 +360,49 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                 other = theirs.x;
                 return ok && theirs.y != 0.0f;
             };
-            // the last key that the row sees
-            const int64_t see = !live ? -1 : (p.causal ? min((int64_t)a.m - 1, (int64_t)token + a.m - a.n) : (int64_t)a.m - 1);
+            // the last key that the row sees (rows of nobody mask nothing)
+            const int64_t see = !live ? (int64_t)1 << 40 : (p.causal ? min((int64_t)a.m - 1, (int64_t)token + a.m - a.n) : (int64_t)a.m - 1);
             const bool any_live = __any_sync(0xffffffffu, live);
-            const uint32_t s_at = mine + i * 128 + half * 64, p_at = mine + i * 128 + half * 32;
+            const uint32_t s_at = mine + i * 128 + half * 64, p_at = s_at;
             bool together = true;
             for (int j = 0; j < n[i]; ++j) {
                 ok = ok && __all_sync(0xffffffffu, role_sleep(s_full + i, j & 1, gone, p.timeout_ns, p.status));
                 tc_fence_after();
-                float s[2][32];
                 float larger = m, other;
+                const int64_t key0 = (int64_t)(first + (twins ? 2 * j + i : j)) * kAttnKeys + 64 * half;
+                const bool masked = !__all_sync(0xffffffffu, see >= key0 + 63);
+                const int upto = (int)max((int64_t)-1, min(see - key0, (int64_t)64));
+                auto scores = [&](int c, float (&s)[32]) {  // 32 of this half's, where the row sees them
+                    tmem_ld(s_at + 32 * c, s);
+                    tmem_wait_ld(s);
+                    if (masked) {
+#pragma unroll
+                        for (int x = 0; x < 32; ++x)
+                            if (32 * c + x > upto) s[x] = minus_inf();
+                    }
+                };
                 if (any_live && ok) {
+                    float top[2];
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) tmem_ld(s_at + 32 * c, s[c]);
+                    for (int c = 0; c < 2; ++c) {
+                        float s[32];
+                        scores(c, s);
+                        float t[4];
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) tmem_wait_ld(s[c]);
-                    const int64_t key0 = (int64_t)(first + (twins ? 2 * j + i : j)) * kAttnKeys + 64 * half;
-                    if (!__all_sync(0xffffffffu, see >= key0 + 63)) {
-                        const int upto = (int)max((int64_t)-1, min(see - key0, (int64_t)64));
+                        for (int q = 0; q < 4; ++q) {
+                            t[q] = fmaxf(s[8 * q], s[8 * q + 1]);
 #pragma unroll
-                        for (int c = 0; c < 64; ++c)
-                            if (c > upto) s[c / 32][c % 32] = minus_inf();
+                            for (int x = 2; x < 8; x += 2) t[q] = fmax3(t[q], s[8 * q + x], s[8 * q + x + 1]);
+                        }
+                        top[c] = fmaxf(fmax3(t[0], t[1], t[2]), t[3]);
                     }
-                    float top[4];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const float* v = s[c / 2] + c % 2 * 16;
-                        top[c] = fmaxf(v[0], v[1]);
-#pragma unroll
-                        for (int x = 2; x < 16; x += 2) top[c] = fmax3(top[c], v[x], v[x + 1]);
-                    }
-                    larger = fmaxf(m, fmaxf(fmax3(top[0], top[1], top[2]), top[3]) * p.scale_log2);
+                    larger = fmaxf(m, fmaxf(top[0], top[1]) * p.scale_log2);
                 }
-                // (the scores are in registers, both warps': P may take their place)
-                tc_fence_before();
                 together = exchange(j, larger, other);
                 if (!together) break;
                 if (any_live) {
-                    tc_fence_after();
                     larger = fmaxf(larger, other);
-                    if (__any_sync(0xffffffffu, larger > m + kAttnSlack)) {
+                    if (__any_sync(0xffffffffu, live && larger > m + kAttnSlack)) {
                         const float f = larger == m ? 1.0f : exp2_fast(m - larger);
                         l *= f;
                         m = larger;
@@ -426,10 +426,14 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                     float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
+                        // (read again: kept from the maximum on, 64 scores leave
+                        // too few registers for what follows)
+                        float s[32];
+                        scores(c, s);
                         uint32_t w[16];
 #pragma unroll
                         for (int x = 0; x < 16; ++x) {
-                            float2 e = __ffma2_rn(make_float2(s[c][2 * x], s[c][2 * x + 1]), scale2, shift2);
+                            float2 e = __ffma2_rn(make_float2(s[2 * x], s[2 * x + 1]), scale2, shift2);
                             e.x = exp2_fast(e.x);
                             e.y = exp2_fast(e.y);
                             sum[x & 1] = __fadd2_rn(sum[x & 1], e);

@@ -286,21 +286,6 @@ __device__ __forceinline__ T uniform(T x)
     return __shfl_sync(0xffffffffu, x, 0);
 }
 
-// Registers a thread, moved between the groups of four warps of a CTA (each
-// group as a whole): what some take the others have given, out of what the CTA
-// was launched with.
-template <int N>
-__device__ __forceinline__ void registers_up()
-{
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
-}
-
-template <int N>
-__device__ __forceinline__ void registers_down()
-{
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
-}
-
 // -- waits -------------------------------------------------------------------
 
 // A try that may suspend the thread for up to `ns` before it gives up.
