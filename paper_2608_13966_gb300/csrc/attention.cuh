@@ -28,7 +28,7 @@
 // key tile each, that exchange their maxima (with one thread a row the 4 warps
 // of a tile spent 2,400 cycles a key tile on their dependent instructions, and
 // the tensor cores waited: 4 x 4096 causal, 32 heads of 128 over 8, 565 us);
-// 16 copies, 17 matrix instructions.
+// 16 copies, 17 matrix instructions, 18 looks up the items.
 #pragma once
 
 #include "attention.h"
@@ -37,8 +37,8 @@
 
 namespace quasar {
 
-constexpr int kAttnThreads = 576;
-constexpr int kAttnCopies = 16, kAttnProducts = 17;  // warps
+constexpr int kAttnThreads = 608;
+constexpr int kAttnRowWarps = 16, kAttnCopies = 16, kAttnProducts = 17, kAttnItems = 18;  // warps
 constexpr int kAttnSlots = 2;             // of the ring, each a tile of values and one of keys
 constexpr float kAttnSlack = 8.0f;        // log2 of how far m may fall behind
 constexpr uint32_t kAttnBlock = kAttnRows * 128;  // bytes of 128 rows x 64 bf16
@@ -108,7 +108,7 @@ __device__ __forceinline__ AttnItem find_item(const AttnSequences& s, int want, 
 // Zeros in the columns [c0, c0 + width) of the rows that no sequence has, the
 // spare items taking turns.  (bf16, 16-byte aligned)
 __device__ __forceinline__ void clear_rows(void* out, int64_t ld, int64_t c0, int width, const int* starts, int n_seq,
-                                           int rows, int index, int spares)
+                                           int rows, int index, int spares, int thread, int threads)
 {
     if (!out) return;
     const int first = starts ? min(max(starts[0], 0), rows) : 0;
@@ -117,19 +117,19 @@ __device__ __forceinline__ void clear_rows(void* out, int64_t ld, int64_t c0, in
     for (int64_t r = index; r < (int64_t)first + (rows - last); r += spares) {
         const int64_t row = r < first ? r : r - first + last;
         uint4* p = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(out) + row * ld + c0);
-        for (int v = threadIdx.x; v < vecs; v += blockDim.x) p[v] = make_uint4(0, 0, 0, 0);
+        for (int v = thread; v < vecs; v += threads) p[v] = make_uint4(0, 0, 0, 0);
     }
 }
 
 __device__ __forceinline__ void clear_lse(float* lse, int heads, int h0, int group, const int* starts, int n_seq,
-                                          int rows, int index, int spares)
+                                          int rows, int index, int spares, int thread, int threads)
 {
     if (!lse) return;
     const int first = starts ? min(max(starts[0], 0), rows) : 0;
     const int last = starts ? max(first, min(max(starts[n_seq], 0), rows)) : rows;
     for (int64_t r = index; r < (int64_t)first + (rows - last); r += spares) {
         const int64_t row = r < first ? r : r - first + last;
-        for (int h = threadIdx.x; h < group; h += blockDim.x) lse[row * heads + h0 + h] = minus_inf();
+        for (int h = thread; h < group; h += threads) lse[row * heads + h0 + h] = minus_inf();
     }
 }
 
@@ -142,7 +142,50 @@ __device__ __forceinline__ int key_tiles(const AttnItem& a, int t0, int t1, bool
     return see > 0 ? (int)((see + kAttnKeys - 1) / kAttnKeys) : 0;
 }
 
+// What every role of a CTA knows of an item: its rows, and its key tiles:
+// `count` from `first` on, of which tile i takes n_i (twins: every other one).
+// They come as entries of the ring, a key tile with the values of the one `lag`
+// before it.
+struct AttnWork {
+    AttnItem a;
+    int kvh;
+    int t0;  // first token of tile 0
+    int first, count, n[2];
+    int twins, lag, entries;
+};
+
+__device__ __forceinline__ AttnWork attention_work(const AttnParams& p, int which, int rank)
+{
+    AttnWork w{};
+    w.kvh = which % p.kv_heads;
+    w.a = find_item(p.s, which / p.kv_heads, p.items, 2 * p.tile_tokens);
+    w.t0 = w.a.index * 2 * p.tile_tokens;
+    w.lag = 1;
+    if (w.a.spares > 0) return w;
+    w.n[0] = key_tiles(w.a, w.t0, w.t0 + p.tile_tokens, p.causal);
+    w.n[1] = key_tiles(w.a, w.t0 + p.tile_tokens, w.t0 + 2 * p.tile_tokens, p.causal);
+    w.twins = !p.persistent && w.a.n - w.t0 <= p.tile_tokens && w.n[0] > 1;
+    const int most = max(w.n[0], w.n[1]);
+    w.first = (int)((int64_t)most * rank / p.split);
+    w.count = (int)((int64_t)most * (rank + 1) / p.split) - w.first;
+    if (w.twins) {
+        w.lag = 2;
+        w.n[0] = (w.count + 1) / 2;
+        w.n[1] = w.count / 2;
+    } else {
+        w.n[0] = max(min(w.n[0] - w.first, w.count), 0);
+        w.n[1] = max(min(w.n[1] - w.first, w.count), 0);
+    }
+    w.entries = max(w.n[0], w.n[1]) > 0 ? w.count + w.lag : 0;
+    return w;
+}
+
 // D = 64 DB columns; a head of d columns is completed with zeros.
+//
+// A CTA walks over items (or, where CTAs share rows, has one): while one's last
+// products run and its rows are written, the next one's tiles are on their way
+// and its first products follow at once.  With a CTA an item, starting and
+// ending took some 17,000 cycles of each, a quarter of 4 x 4096.
 template <int DB>
 __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_constant__ AttnParams p)
 {
@@ -152,25 +195,35 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* ring = smem + 2 * kTile;
     uint64_t* q_full = reinterpret_cast<uint64_t*>(ring + kAttnSlots * 2 * kTile);
-    uint64_t* full = q_full + 1;           // [slots]
+    uint64_t* q_empty = q_full + 1;
+    uint64_t* full = q_empty + 1;          // [slots]
     uint64_t* empty = full + kAttnSlots;   // [slots]
     uint64_t* s_full = empty + kAttnSlots; // [2]
     uint64_t* p_full = s_full + 2;         // [2]: 8 warps
     uint64_t* o_full = p_full + 2;         // [2]
-    uint64_t* drained = o_full + 2;
+    uint64_t* o_empty = o_full + 2;        // [2]: 8 warps
+    uint64_t* item_full = o_empty + 2;     // [2]
+    uint64_t* item_empty = item_full + 2;  // [2]: the other warps
+    uint64_t* drained = item_empty + 2;
     uint64_t* never = drained + 1;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(never + 1);
     volatile uint32_t* gone = tmem_slot + 1;
-    AttnItem* item = reinterpret_cast<AttnItem*>(tmem_slot + 2);
-    float2* stat = reinterpret_cast<float2*>(item + 1);  // [2][128]: m and l, where CTAs share a row
-    float2* swap = stat + 256;                           // [2 turns][2 tiles][2 halves][128]
+    float2* stat = reinterpret_cast<float2*>(tmem_slot + 2);  // [2][128]: m and l, where rows have parts
+    float2* swap = stat + 256;                                // [2 turns][2 tiles][2 halves][128]
+    AttnWork* items = reinterpret_cast<AttnWork*>(swap + 1024);  // [2]
 
     const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int rank = p.split > 1 ? (int)cluster_rank() : 0;
-    const int kvh = (int)(blockIdx.x / p.split) % p.kv_heads;
+    // the items of this CTA: every grid's width one, and back the next time
+    // (neighbours have nearly the same number of keys)
+    const int width = (int)(gridDim.x / p.split), mine = (int)(blockIdx.x / p.split);
+    const int total = p.items * p.kv_heads;
+    auto which = [&](int k) { return k * width + (k & 1 ? width - 1 - mine : mine); };
+    const int turns = (total + width - 1) / width;
 
     if (threadIdx.x == 0) {
         mbar_init(q_full, 1);
+        mbar_init(q_empty, 1);
         for (int s = 0; s < kAttnSlots; ++s) {
             mbar_init(full + s, 1);
             mbar_init(empty + s, 1);
@@ -179,6 +232,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
             mbar_init(s_full + i, 1);
             mbar_init(p_full + i, 8);
             mbar_init(o_full + i, 1);
+            mbar_init(o_empty + i, 8);
+            mbar_init(item_full + i, 1);
+            mbar_init(item_empty + i, kAttnRowWarps + 2);
         }
         mbar_init(drained, 1);
         mbar_init(never, 1);
@@ -191,104 +247,100 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
         prefetch_map(&p.k);
         prefetch_map(&p.v);
     }
-    wait_for_previous_grid();
-    if (warp == 0) {
-        const AttnItem a =
-            find_item(p.s, (int)(blockIdx.x / p.split / p.kv_heads), p.items, 2 * p.tile_tokens);
-        if (lane == 0) *item = a;
-    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    wait_for_previous_grid();
     const uint32_t tmem = uniform(*tmem_slot);
-    const AttnItem a = *item;
-    const int t0 = a.index * 2 * p.tile_tokens;  // first token of tile 0
+    auto wait = [&](uint64_t* bar, uint32_t parity) {  // the warp's, with one outcome
+        const bool ok = role_sleep(bar, parity, gone, p.timeout_ns, p.status);
+        return __all_sync(0xffffffffu, ok);
+    };
+    // item k, once it is known; its place is for k + 2 when all have let it go
+    auto take = [&](int k) { return wait(item_full + (k & 1), (k >> 1) & 1); };
+    auto release = [&](int k) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(item_empty + (k & 1));
+    };
 
-    // This CTA's key tiles: `count` from `first` on; tile i takes n_i of them
-    // (twins: every other one).  They come as entries of the ring, a key tile
-    // with the values of the one `lag` before it.
-    int first = 0, count = 0, n[2] = {0, 0};
-    bool twins = false;
-    if (a.spares == 0) {
-        n[0] = key_tiles(a, t0, t0 + p.tile_tokens, p.causal);
-        n[1] = key_tiles(a, t0 + p.tile_tokens, t0 + 2 * p.tile_tokens, p.causal);
-        twins = a.n - t0 <= p.tile_tokens && n[0] > 1;
-        const int most = max(n[0], n[1]);
-        first = (int)((int64_t)most * rank / p.split);
-        count = (int)((int64_t)most * (rank + 1) / p.split) - first;
-        if (twins) {
-            n[0] = (count + 1) / 2;
-            n[1] = count / 2;
-        } else {
-            n[0] = max(min(n[0] - first, count), 0);
-            n[1] = max(min(n[1] - first, count), 0);
-        }
-    }
-    n[0] = uniform(n[0]);
-    n[1] = uniform(n[1]);
-    twins = uniform((int)twins) != 0;
-    const int lag = twins ? 2 : 1;
-    const int steps = max(n[0], n[1]), entries = uniform(steps > 0 ? count + lag : 0);
-
-    if (a.spares > 0 && rank == 0) {
-        clear_rows(p.y, p.ld_y, (int64_t)kvh * p.group * p.d, p.group * p.d, p.s.starts, p.s.n, p.s.tokens, a.index, a.spares);
-        clear_lse(p.lse, p.heads, kvh * p.group, p.group, p.s.starts, p.s.n, p.s.tokens, a.index, a.spares);
-    }
-    if (warp >= kAttnCopies) {
-        if (warp == kAttnCopies) {
+    if (warp == kAttnItems) {
+        for (int k = 0; k < turns && which(k) < total; ++k) {
+            const AttnWork w = attention_work(p, which(k), rank);
+            if (k >= 2 && !wait(item_empty + (k & 1), ((k >> 1) - 1) & 1)) break;
             if (lane == 0) {
-                if (p.force_timeout_ns) role_sleep(never, 0, gone, p.force_timeout_ns, p.status);
-                int it = 0;
-                const bool rows_sent = steps > 0 && !*gone;
-                if (rows_sent) {
-                    const uint32_t bytes = (uint32_t)(p.tile_tokens * p.group) * 128 * DB;
-                    mbar_arrive_expect_tx(q_full, (n[0] > 0 ? bytes : 0) + (n[1] > 0 && !twins ? bytes : 0));
-                    for (int i = 0; i < 2; ++i)
-                        if (n[i] > 0 && !(twins && i == 1))
-                            for (int b = 0; b < DB; ++b)
-                                tile_g2s_3d(smem_u32(smem + i * kTile + b * kAttnBlock), &p.q, 64 * b, kvh * p.group,
-                                            a.q0 + t0 + i * p.tile_tokens, smem_u32(q_full));
-                }
-                for (; it < entries && !*gone; ++it) {
-                    const int s = it % kAttnSlots;
-                    if (it >= kAttnSlots &&
-                        !role_sleep(empty + s, (it / kAttnSlots - 1) & 1, gone, p.timeout_ns, p.status))
-                        break;
-                    const bool values = it >= lag, keys = it < count;
+                items[k & 1] = w;
+                mbar_arrive(item_full + (k & 1));
+            }
+            __syncwarp();
+        }
+    } else if (warp == kAttnCopies) {
+        bool ok = true;
+        if (p.force_timeout_ns) ok = __all_sync(0xffffffffu, role_sleep(never, 0, gone, p.force_timeout_ns, p.status));
+        int it = 0, queries = 0;  // entries of the ring and sets of queries so far
+        for (int k = 0; k < turns && which(k) < total && ok; ++k) {
+            if (!(ok = take(k))) break;
+            const AttnWork w = items[k & 1];
+            release(k);
+            if (w.entries == 0) continue;
+            if (queries > 0 && !(ok = wait(q_empty, (queries - 1) & 1))) break;
+            if (lane == 0) {
+                const uint32_t bytes = (uint32_t)(p.tile_tokens * p.group) * 128 * DB;
+                const bool both = w.n[1] > 0 && !w.twins;
+                mbar_arrive_expect_tx(q_full, (w.n[0] > 0 ? bytes : 0) + (both ? bytes : 0));
+                for (int i = 0; i < 2; ++i)
+                    if (i ? both : w.n[0] > 0)
+                        for (int b = 0; b < DB; ++b)
+                            tile_g2s_3d(smem_u32(smem + i * kTile + b * kAttnBlock), &p.q, 64 * b, w.kvh * p.group,
+                                        w.a.q0 + w.t0 + i * p.tile_tokens, smem_u32(q_full));
+            }
+            ++queries;
+            for (int e = 0; e < w.entries; ++e, ++it) {
+                const int s = it % kAttnSlots;
+                if (it >= kAttnSlots && !(ok = wait(empty + s, (it / kAttnSlots - 1) & 1))) break;
+                if (lane == 0) {
+                    const bool values = e >= w.lag, keys = e < w.count;
                     mbar_arrive_expect_tx(full + s, (values ? kTile : 0) + (keys ? kTile : 0));
                     const uint32_t to = smem_u32(ring + s * 2 * kTile);
-                    const int key = a.k0 + (first + it) * kAttnKeys;
+                    const int key = w.a.k0 + (w.first + e) * kAttnKeys;
                     for (int b = 0; b < DB; ++b) {
-                        if (values) tile_g2s_3d(to + b * kAttnBlock, &p.v, 64 * b, kvh, key - lag * kAttnKeys, smem_u32(full + s));
-                        if (keys) tile_g2s_3d(to + kTile + b * kAttnBlock, &p.k, 64 * b, kvh, key, smem_u32(full + s));
+                        if (values)
+                            tile_g2s_3d(to + b * kAttnBlock, &p.v, 64 * b, w.kvh, key - w.lag * kAttnKeys, smem_u32(full + s));
+                        if (keys) tile_g2s_3d(to + kTile + b * kAttnBlock, &p.k, 64 * b, w.kvh, key, smem_u32(full + s));
                     }
                 }
-                if (*gone) {  // what is in flight has landed before the memory is let go
-                    if (rows_sent) mbar_wait_bounded(q_full, 0, p.timeout_ns);
-                    for (int j = max(it - kAttnSlots, 0); j < it; ++j)
-                        mbar_wait_bounded(full + j % kAttnSlots, (j / kAttnSlots) & 1, p.timeout_ns);
-                }
+                __syncwarp();
             }
-        } else if (warp == kAttnProducts) {
-            // One thread for both tiles, first come first served: with a warp each
-            // their products share the tensor cores instruction by instruction,
-            // both end late, and 4 x 4096 took 550 us against 492.  What bounds it
-            // is this warp's own time, some 130 cycles a wait: one barrier for the
-            // values of a step and the keys of the next.
-            constexpr uint32_t desc_s = mma_desc(kAttnRows, kAttnKeys, false, false);
-            constexpr uint32_t desc_o = mma_desc(kAttnRows, D, false, true);
-            auto wait = [&](uint64_t* bar, uint32_t parity) {
-                const bool ok = role_sleep(bar, parity, gone, p.timeout_ns, p.status);
-                return __all_sync(0xffffffffu, ok);
-            };
-            bool ok = steps == 0 || wait(q_full, 0);
-            for (int e = 0; e < entries && ok; ++e) {
-                const int s = e % kAttnSlots;
-                if (!(ok = wait(full + s, (e / kAttnSlots) & 1))) break;
+        }
+        if (*gone && lane == 0) {  // what is in flight has landed before the memory is let go
+            if (queries > 0) mbar_wait_bounded(q_full, (queries - 1) & 1, p.timeout_ns);
+            for (int j = max(it - kAttnSlots, 0); j < it; ++j)
+                mbar_wait_bounded(full + j % kAttnSlots, (j / kAttnSlots) & 1, p.timeout_ns);
+        }
+    } else if (warp == kAttnProducts) {
+        // One thread for both tiles, first come first served: with a warp each
+        // their products share the tensor cores instruction by instruction,
+        // both end late, and 4 x 4096 took 550 us against 492.
+        constexpr uint32_t desc_s = mma_desc(kAttnRows, kAttnKeys, false, false);
+        constexpr uint32_t desc_o = mma_desc(kAttnRows, D, false, true);
+        int it = 0, queries = 0, done[2] = {0, 0}, outs[2] = {0, 0};  // steps and rows of outputs of a tile
+        bool ok = true;
+        for (int k = 0; k < turns && which(k) < total && ok; ++k) {
+            if (!(ok = take(k))) break;
+            const AttnWork w = items[k & 1];
+            release(k);
+            const int entries = uniform(w.entries), count = uniform(w.count), lag = uniform(w.lag);
+            const int n[2] = {uniform(w.n[0]), uniform(w.n[1])};
+            const bool twins = uniform(w.twins) != 0;
+            if (entries == 0) continue;
+            if (!(ok = wait(q_full, queries & 1))) break;
+            ++queries;
+            for (int e = 0; e < entries && ok; ++e, ++it) {
+                const int s = it % kAttnSlots;
+                if (!(ok = wait(full + s, (it / kAttnSlots) & 1))) break;
                 uint8_t* const values = ring + s * 2 * kTile;
                 // rows of V behind the sequence belong to another, or to nobody:
                 // their probabilities are 0, but 0 times what lies there need not be
-                const int left = a.m - (first + e - lag) * kAttnKeys;
+                const int left = w.a.m - (w.first + e - lag) * kAttnKeys;
                 if (e >= lag && left < kAttnKeys) {
                     for (int x = lane + left * 8; x < kAttnKeys * 8; x += 32)
 #pragma unroll
@@ -303,17 +355,22 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                 for (int i = 0; i < 2; ++i) {
                     if (twins && i != (e & 1)) continue;
                     const int j = (twins ? e >> 1 : e) - 1;  // of the values, in the tile's own steps
-                    if (j >= 0 && j < n[i] && !(ok = wait(p_full + i, j & 1))) break;
+                    const bool grow = j >= 0 && j < n[i], score = j + 1 < n[i];
+                    if (grow) {
+                        if (!(ok = wait(p_full + i, (done[i] + j) & 1))) break;
+                        // the rows of the item before have been read
+                        if (j == 0 && outs[i] > 0 && !(ok = wait(o_empty + i, (outs[i] - 1) & 1))) break;
+                    }
                     tc_fence_after();
                     if (elect_one()) {
                         const uint32_t s_at = tmem + i * 128, o_at = tmem + 256 + i * 128;
-                        if (j >= 0 && j < n[i]) {
+                        if (grow) {
 #pragma unroll
                             for (int x = 0; x < kAttnKeys / 16; ++x)
                                 mma_bf16_ts(o_at, s_at + x / 4 * 64 + x % 4 * 8, dv + x * k_step(true), desc_o, j > 0 || x > 0);
                             mma_commit(smem_u32(o_full + i));
                         }
-                        if (j + 1 < n[i]) {  // S = Q K^T
+                        if (score) {  // S = Q K^T
                             const uint64_t dq = operand_desc(smem_u32(smem + (twins ? 0 : i) * kTile), false);
 #pragma unroll
                             for (int b = 0; b < DB; ++b)
@@ -323,153 +380,181 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                                                 dk + b * (kAttnBlock >> 4) + x * k_step(false), desc_s, b + x > 0);
                             mma_commit(smem_u32(s_full + i));
                         }
-                        if (i == 1 || twins) mma_commit(smem_u32(empty + s));
+                        if (i == 1 || twins) {
+                            mma_commit(smem_u32(empty + s));
+                            if (e == count - 1) mma_commit(smem_u32(q_empty));
+                        }
                     }
                     __syncwarp();
                 }
             }
-            if (elect_one()) {
-                mma_commit(smem_u32(drained));
-                mbar_wait_bounded(drained, 0, p.timeout_ns);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                done[i] += n[i];
+                outs[i] += n[i] > 0;
             }
+        }
+        if (elect_one()) {
+            mma_commit(smem_u32(drained));
+            mbar_wait_bounded(drained, 0, p.timeout_ns);
         }
         __syncwarp();
-        if ((p.split > 1 || twins) && a.spares == 0) {  // the barriers of the rows' warps
-            __syncthreads();
-            p.split > 1 ? cluster_sync() : __syncthreads();
-            if (p.split > 1) cluster_sync();
-        }
     } else {
         // a thread's row: r of tile i; its half of the row's keys, and of its columns
-        const int i = warp >> 3 & 1, half = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
-        const int token = t0 + (twins ? 0 : i) * p.tile_tokens + r / p.group, head = kvh * p.group + r % p.group;
-        const bool live = a.spares == 0 && r < p.tile_tokens * p.group && token < a.n;
-        const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         constexpr int kHalf = D / 2;
-        const uint32_t o_at = mine + 256 + i * 128 + half * kHalf;
-        float m = minus_inf(), l = 0.0f;
+        const int i = warp >> 3 & 1, half = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t s_at = lanes + i * 128 + half * 64, o_at = lanes + 256 + i * 128 + half * kHalf;
+        int done = 0, swaps = 0;  // steps and exchanges so far
+        uint32_t agreed = 0;
         bool ok = true;
-        if (n[i] > 0) {
-            // Both warps of a row come to this barrier once a key tile and once at
-            // the end, whatever their waits gave, and leave together.
-            auto exchange = [&](int turn, float x, float& other) {
-                float2* at = swap + ((turn & 1) * 2 + i) * 256 + r;
-                at[half * 128] = make_float2(x, ok ? 1.0f : 0.0f);
-                asm volatile("bar.sync %0, 64;" ::"r"(1 + i * 4 + (warp & 3)) : "memory");
-                const float2 theirs = at[(half ^ 1) * 128];
-                other = theirs.x;
-                return ok && theirs.y != 0.0f;
-            };
-            // the last key that the row sees (rows of nobody mask nothing)
-            const int64_t see = !live ? (int64_t)1 << 40 : (p.causal ? min((int64_t)a.m - 1, (int64_t)token + a.m - a.n) : (int64_t)a.m - 1);
-            const bool any_live = __any_sync(0xffffffffu, live);
-            const uint32_t s_at = mine + i * 128 + half * 64, p_at = s_at;
-            bool together = true;
-            for (int j = 0; j < n[i]; ++j) {
-                ok = ok && __all_sync(0xffffffffu, role_sleep(s_full + i, j & 1, gone, p.timeout_ns, p.status));
-                tc_fence_after();
-                float larger = m, other;
-                const int64_t key0 = (int64_t)(first + (twins ? 2 * j + i : j)) * kAttnKeys + 64 * half;
-                const bool masked = !__all_sync(0xffffffffu, see >= key0 + 63);
-                const int upto = (int)max((int64_t)-1, min(see - key0, (int64_t)64));
-                auto scores = [&](int c, float (&s)[32]) {  // 32 of this half's, where the row sees them
-                    tmem_ld(s_at + 32 * c, s);
-                    tmem_wait_ld(s);
-                    if (masked) {
-#pragma unroll
-                        for (int x = 0; x < 32; ++x)
-                            if (32 * c + x > upto) s[x] = minus_inf();
-                    }
-                };
-                if (any_live && ok) {
-                    float top[2];
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        float s[32];
-                        scores(c, s);
-                        float t[4];
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            t[q] = fmaxf(s[8 * q], s[8 * q + 1]);
-#pragma unroll
-                            for (int x = 2; x < 8; x += 2) t[q] = fmax3(t[q], s[8 * q + x], s[8 * q + x + 1]);
-                        }
-                        top[c] = fmaxf(fmax3(t[0], t[1], t[2]), t[3]);
-                    }
-                    larger = fmaxf(m, fmaxf(top[0], top[1]) * p.scale_log2);
+        // Both warps of a row come to this barrier at the same places, whatever
+        // their waits gave, and leave together.
+        auto exchange = [&](float x, float& other) {
+            float2* at = swap + ((swaps & 1) * 2 + i) * 256 + r;
+            ++swaps;
+            at[half * 128] = make_float2(x, ok ? 1.0f : 0.0f);
+            asm volatile("bar.sync %0, 64;" ::"r"(1 + i * 4 + (warp & 3)) : "memory");
+            const float2 theirs = at[(half ^ 1) * 128];
+            other = theirs.x;
+            return ok && theirs.y != 0.0f;
+        };
+        bool synced = false;
+        for (int k = 0; k < turns && which(k) < total; ++k) {
+            // (an item that one of them did not get, or did not finish, ends it for all)
+            ok = ok && take(k);
+            asm volatile(
+                "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+                "bar.red.and.pred q, 9, 512, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                : "=r"(agreed)
+                : "r"((uint32_t)ok)
+                : "memory");
+            ok = agreed != 0;
+            if (!ok) break;
+            const AttnWork& w = items[k & 1];
+            const AttnItem& a = w.a;
+            if (a.spares > 0) {
+                if (rank == 0) {
+                    clear_rows(p.y, p.ld_y, (int64_t)w.kvh * p.group * p.d, p.group * p.d, p.s.starts, p.s.n, p.s.tokens,
+                               a.index, a.spares, threadIdx.x, kAttnRowWarps * 32);
+                    clear_lse(p.lse, p.heads, w.kvh * p.group, p.group, p.s.starts, p.s.n, p.s.tokens, a.index, a.spares,
+                              threadIdx.x, kAttnRowWarps * 32);
                 }
-                together = exchange(j, larger, other);
-                if (!together) break;
-                if (any_live) {
-                    larger = fmaxf(larger, other);
-                    if (__any_sync(0xffffffffu, live && larger > m + kAttnSlack)) {
-                        const float f = larger == m ? 1.0f : exp2_fast(m - larger);
-                        l *= f;
-                        m = larger;
-                        if (j > 0) {
-                            ok = __all_sync(0xffffffffu,
-                                            role_sleep(o_full + i, (j - 1) & 1, gone, p.timeout_ns, p.status));
-                            if (!ok) continue;
-                            tc_fence_after();
-#pragma unroll 1
-                            for (int c = 0; c < kHalf; c += 16) {
-                                float o[16];
-                                tmem_ld16(o_at + c, o);
+                release(k);
+                continue;
+            }
+            const int token = w.t0 + (w.twins ? 0 : i) * p.tile_tokens + r / p.group, head = w.kvh * p.group + r % p.group;
+            const bool live = r < p.tile_tokens * p.group && token < a.n;
+            const bool any_live = __any_sync(0xffffffffu, live);
+            const int n = w.n[i];
+            float m = minus_inf(), l = 0.0f;
+            if (n > 0) {
+                // the last key that the row sees (rows of nobody mask nothing)
+                const int64_t see = !live ? (int64_t)1 << 40 : (p.causal ? min((int64_t)a.m - 1, (int64_t)token + a.m - a.n) : (int64_t)a.m - 1);
+                bool together = true;
+                for (int j = 0; j < n; ++j) {
+                    ok = ok && wait(s_full + i, (done + j) & 1);
+                    tc_fence_after();
+                    float larger = m, other;
+                    const int64_t key0 = (int64_t)(w.first + (w.twins ? 2 * j + i : j)) * kAttnKeys + 64 * half;
+                    const bool masked = !__all_sync(0xffffffffu, see >= key0 + 63);
+                    const int upto = (int)max((int64_t)-1, min(see - key0, (int64_t)64));
+                    auto scores = [&](int c, float (&s)[32]) {  // 32 of this half's, where the row sees them
+                        tmem_ld(s_at + 32 * c, s);
+                        tmem_wait_ld(s);
+                        if (masked) {
 #pragma unroll
-                                for (int x = 0; x < 16; ++x) o[x] *= f;
-                                tmem_st16(o_at + c, o);
+                            for (int x = 0; x < 32; ++x)
+                                if (32 * c + x > upto) s[x] = minus_inf();
+                        }
+                    };
+                    if (any_live && ok) {
+                        float top[2];
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            float s[32];
+                            scores(c, s);
+                            float t[4];
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                t[q] = fmaxf(s[8 * q], s[8 * q + 1]);
+#pragma unroll
+                                for (int x = 2; x < 8; x += 2) t[q] = fmax3(t[q], s[8 * q + x], s[8 * q + x + 1]);
+                            }
+                            top[c] = fmaxf(fmax3(t[0], t[1], t[2]), t[3]);
+                        }
+                        larger = fmaxf(m, fmaxf(top[0], top[1]) * p.scale_log2);
+                    }
+                    together = exchange(larger, other);
+                    if (!together) break;
+                    if (any_live) {
+                        larger = fmaxf(larger, other);
+                        if (__any_sync(0xffffffffu, live && larger > m + kAttnSlack)) {
+                            const float f = larger == m ? 1.0f : exp2_fast(m - larger);
+                            l *= f;
+                            m = larger;
+                            if (j > 0) {
+                                ok = wait(o_full + i, (done + j - 1) & 1);
+                                if (!ok) continue;
+                                tc_fence_after();
+#pragma unroll 1
+                                for (int c = 0; c < kHalf; c += 16) {
+                                    float o[16];
+                                    tmem_ld16(o_at + c, o);
+#pragma unroll
+                                    for (int x = 0; x < 16; ++x) o[x] *= f;
+                                    tmem_st16(o_at + c, o);
+                                }
                             }
                         }
-                    }
-                    const float shift = m == minus_inf() ? 0.0f : -m;
-                    const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), shift2 = make_float2(shift, shift);
-                    float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+                        const float shift = m == minus_inf() ? 0.0f : -m;
+                        const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), shift2 = make_float2(shift, shift);
+                        float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        // (read again: kept from the maximum on, 64 scores leave
-                        // too few registers for what follows)
-                        float s[32];
-                        scores(c, s);
-                        uint32_t w[16];
+                        for (int c = 0; c < 2; ++c) {
+                            // (read again: kept from the maximum on, 64 scores leave
+                            // too few registers for what follows)
+                            float s[32];
+                            scores(c, s);
+                            uint32_t x16[16];
 #pragma unroll
-                        for (int x = 0; x < 16; ++x) {
-                            float2 e = __ffma2_rn(make_float2(s[2 * x], s[2 * x + 1]), scale2, shift2);
-                            e.x = exp2_fast(e.x);
-                            e.y = exp2_fast(e.y);
-                            sum[x & 1] = __fadd2_rn(sum[x & 1], e);
-                            w[x] = pack_bf16x2(e.x, e.y);
+                            for (int x = 0; x < 16; ++x) {
+                                float2 e = __ffma2_rn(make_float2(s[2 * x], s[2 * x + 1]), scale2, shift2);
+                                e.x = exp2_fast(e.x);
+                                e.y = exp2_fast(e.y);
+                                sum[x & 1] = __fadd2_rn(sum[x & 1], e);
+                                x16[x] = pack_bf16x2(e.x, e.y);
+                            }
+                            tmem_st(s_at + 16 * c, x16);
                         }
-                        tmem_st(p_at + 16 * c, w);
+                        tmem_wait_st();
+                        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                     }
-                    tmem_wait_st();
-                    l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(p_full + i);
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(p_full + i);
+                if (together) {
+                    ok = ok && wait(o_full + i, (done + n - 1) & 1);
+                    float other;
+                    ok = exchange(l, other);
+                    l = half ? other + l : l + other;
+                    tc_fence_after();
+                } else {
+                    ok = false;
+                }
+                done += n;
             }
-            if (together) {
-                ok = ok && __all_sync(0xffffffffu, role_sleep(o_full + i, (n[i] - 1) & 1, gone, p.timeout_ns, p.status));
-                float other;
-                ok = exchange(n[i], l, other);
-                l = half ? other + l : l + other;
-                tc_fence_after();
-            } else {
-                ok = false;
-            }
-        }
-
-        if (p.split == 1 && !twins) {
-            if (a.spares == 0 && ok && __any_sync(0xffffffffu, live)) {
+            const bool whole = p.split == 1 && !w.twins;  // the row has one part
+            if (whole && ok && any_live) {
                 const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-                // the rows through the query tile's memory, so that a store covers
-                // whole rows
-                uint8_t* stage = smem + i * kTile + (warp & 3) * 32 * D * 2;
+                __nv_bfloat16* const y =
+                    static_cast<__nv_bfloat16*>(p.y) + (int64_t)(a.q0 + token) * p.ld_y + (int64_t)head * p.d + half * kHalf;
 #pragma unroll 1
-                for (int c = half * kHalf; c < (half + 1) * kHalf; c += 32) {
+                for (int c = 0; c < kHalf; c += 32) {
                     float o[32];
-                    if (n[i] > 0) {
-                        tmem_ld(o_at + c - half * kHalf, o);
+                    if (n > 0) {
+                        tmem_ld(o_at + c, o);
                         tmem_wait_ld(o);
                     } else {
 #pragma unroll
@@ -477,94 +562,99 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                     }
 #pragma unroll
                     for (int x = 0; x < 32; x += 8)
-                        *reinterpret_cast<uint4*>(stage + lane * D * 2 + (((c + x) / 8) ^ (lane & 7)) * 16) =
-                            make_uint4(pack_bf16x2(o[x] * inv, o[x + 1] * inv), pack_bf16x2(o[x + 2] * inv, o[x + 3] * inv),
-                                       pack_bf16x2(o[x + 4] * inv, o[x + 5] * inv), pack_bf16x2(o[x + 6] * inv, o[x + 7] * inv));
+                        if (live && half * kHalf + c + x < p.d)
+                            *reinterpret_cast<uint4*>(y + c + x) =
+                                make_uint4(pack_bf16x2(o[x] * inv, o[x + 1] * inv), pack_bf16x2(o[x + 2] * inv, o[x + 3] * inv),
+                                           pack_bf16x2(o[x + 4] * inv, o[x + 5] * inv), pack_bf16x2(o[x + 6] * inv, o[x + 7] * inv));
                 }
                 if (p.lse && live && half == 0)
                     p.lse[(int64_t)(a.q0 + token) * p.heads + head] = l == 0.0f ? minus_inf() : 0.69314718f * (m + log2f(l));
-                __syncwarp();
-                constexpr int kLanes = kHalf / 8;  // of a row
-                for (int q = 0; q < 32; q += 32 / kLanes) {
-                    const int row = q + lane / kLanes, chunk = half * kLanes + lane % kLanes;
-                    const int rr = (warp & 3) * 32 + row;
-                    const int tok = t0 + i * p.tile_tokens + rr / p.group;
-                    if (rr < p.tile_tokens * p.group && tok < a.n && chunk * 8 < p.d)
-                        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.y) + (int64_t)(a.q0 + tok) * p.ld_y +
-                                                  (int64_t)(kvh * p.group + rr % p.group) * p.d + chunk * 8) =
-                            *reinterpret_cast<const uint4*>(stage + row * D * 2 + (chunk ^ (row & 7)) * 16);
-                }
             }
-        } else if (a.spares == 0) {
-            // every product of this CTA is done: the ring's memory takes O
-            __syncthreads();
-            float* part = reinterpret_cast<float*>(ring);  // [2][128][D], vectors of 4 swizzled by row
-            {
+            if (n > 0) {  // the outputs are read: the next item's may grow
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(o_empty + i);
+            }
+            if (!whole) {
+                // (one item, then: every product of this CTA is done, and the
+                // ring's memory takes O)
+                asm volatile("bar.sync 9, 512;" ::: "memory");
+                float* part = reinterpret_cast<float*>(ring);  // [2][128][D], vectors of 4 swizzled by row
                 if (half == 0) stat[i * 128 + r] = make_float2(m, ok ? l : 0.0f);
-                if (n[i] > 0 && ok) {
+                if (n > 0 && ok) {
 #pragma unroll 1
-                    for (int c = half * kHalf; c < (half + 1) * kHalf; c += 32) {
+                    for (int c = 0; c < kHalf; c += 32) {
                         float o[32];
-                        tmem_ld(o_at + c - half * kHalf, o);
+                        tmem_ld(o_at + c, o);
                         tmem_wait_ld(o);
 #pragma unroll
                         for (int x = 0; x < 32; x += 4)
-                            *reinterpret_cast<float4*>(part + (size_t)(i * 128 + r) * D + (((c + x) / 4) ^ (r & 7)) * 4) =
+                            *reinterpret_cast<float4*>(part + (size_t)(i * 128 + r) * D +
+                                                       (((half * kHalf + c + x) / 4) ^ (r & 7)) * 4) =
                                 make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
                     }
                 }
-            }
-            p.split > 1 ? cluster_sync() : __syncthreads();
-            constexpr int kVecs = D / 4, kMany = kAttnCopies * 32;
-            const int rows = p.tile_tokens * p.group;
-            auto peer = [&](const void* x, int q) {
-                return p.split > 1 ? peer_addr(smem_u32(x), (uint32_t)q) : smem_u32(x);
-            };
-            for (int x = rank * kMany + (int)threadIdx.x; x < (twins ? 1 : 2) * rows * kVecs; x += p.split * kMany) {
-                const int tile = x / (rows * kVecs), row = x / kVecs % rows, c = x % kVecs;
-                const int tok = t0 + tile * p.tile_tokens + row / p.group;
-                if (tok >= a.n || 4 * c >= p.d) continue;
-                float top = minus_inf(), total = 0.0f;
-                float2 st[kAttnMostSplit][2];
+                if (p.split > 1) {
+                    cluster_sync();
+                    synced = true;
+                } else {
+                    asm volatile("bar.sync 9, 512;" ::: "memory");
+                }
+                constexpr int kVecs = D / 4, kMany = kAttnRowWarps * 32;
+                const int rows = p.tile_tokens * p.group;
+                auto peer = [&](const void* x, int q) {
+                    return p.split > 1 ? peer_addr(smem_u32(x), (uint32_t)q) : smem_u32(x);
+                };
+                for (int x = rank * kMany + (int)threadIdx.x; x < (w.twins ? 1 : 2) * rows * kVecs; x += p.split * kMany) {
+                    const int tile = x / (rows * kVecs), row = x / kVecs % rows, c = x % kVecs;
+                    const int tok = w.t0 + tile * p.tile_tokens + row / p.group;
+                    if (tok >= a.n || 4 * c >= p.d) continue;
+                    float top = minus_inf(), total_l = 0.0f;
+                    float2 st[kAttnMostSplit][2];
 #pragma unroll
-                for (int q = 0; q < kAttnMostSplit; ++q)
+                    for (int q = 0; q < kAttnMostSplit; ++q)
 #pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        st[q][w] = make_float2(minus_inf(), 0.0f);
-                        if (q >= p.split || (w == 1 && !twins)) continue;
-                        asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];"
-                                     : "=f"(st[q][w].x), "=f"(st[q][w].y)
-                                     : "r"(peer(stat + (tile + w) * 128 + row, q))
-                                     : "memory");
-                        top = fmaxf(top, st[q][w].x);
-                    }
-                const float shift = top == minus_inf() ? 0.0f : top;
-                float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-                for (int q = 0; q < kAttnMostSplit; ++q)
-#pragma unroll
-                    for (int w = 0; w < 2; ++w)
-                        if (st[q][w].y != 0.0f) {  // (a part without keys left nothing)
-                            const float f = exp2_fast(st[q][w].x - shift);
-                            const float4 v =
-                                ld_peer4(peer(part + (size_t)((tile + w) * 128 + row) * D + (c ^ (row & 7)) * 4, q));
-                            total = fmaf(f, st[q][w].y, total);
-                            o.x = fmaf(f, v.x, o.x), o.y = fmaf(f, v.y, o.y), o.z = fmaf(f, v.z, o.z), o.w = fmaf(f, v.w, o.w);
+                        for (int z = 0; z < 2; ++z) {
+                            st[q][z] = make_float2(minus_inf(), 0.0f);
+                            if (q >= p.split || (z == 1 && !w.twins)) continue;
+                            asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];"
+                                         : "=f"(st[q][z].x), "=f"(st[q][z].y)
+                                         : "r"(peer(stat + (tile + z) * 128 + row, q))
+                                         : "memory");
+                            top = fmaxf(top, st[q][z].x);
                         }
-                const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-                const int64_t to = (int64_t)(a.q0 + tok);
-                const int h = kvh * p.group + row % p.group;
-                *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.y) + to * p.ld_y + (int64_t)h * p.d + 4 * c) =
-                    make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-                if (p.lse && c == 0)
-                    p.lse[to * p.heads + h] = total == 0.0f ? minus_inf() : 0.69314718f * (shift + log2f(total));
+                    const float shift = top == minus_inf() ? 0.0f : top;
+                    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                    for (int q = 0; q < kAttnMostSplit; ++q)
+#pragma unroll
+                        for (int z = 0; z < 2; ++z)
+                            if (st[q][z].y != 0.0f) {  // (a part without keys left nothing)
+                                const float f = exp2_fast(st[q][z].x - shift);
+                                const float4 v =
+                                    ld_peer4(peer(part + (size_t)((tile + z) * 128 + row) * D + (c ^ (row & 7)) * 4, q));
+                                total_l = fmaf(f, st[q][z].y, total_l);
+                                o.x = fmaf(f, v.x, o.x), o.y = fmaf(f, v.y, o.y), o.z = fmaf(f, v.z, o.z), o.w = fmaf(f, v.w, o.w);
+                            }
+                    const float inv = total_l == 0.0f ? 0.0f : 1.0f / total_l;
+                    const int64_t to = (int64_t)(a.q0 + tok);
+                    const int h = w.kvh * p.group + row % p.group;
+                    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.y) + to * p.ld_y + (int64_t)h * p.d + 4 * c) =
+                        make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+                    if (p.lse && c == 0)
+                        p.lse[to * p.heads + h] = total_l == 0.0f ? minus_inf() : 0.69314718f * (shift + log2f(total_l));
+                }
             }
-            if (p.split > 1) cluster_sync();  // nobody leaves while its memory is read
+            release(k);
         }
+        __syncwarp();
+        if (p.split > 1 && !synced) cluster_sync();
     }
     __syncwarp();
+    if (p.split > 1 && warp >= kAttnRowWarps) cluster_sync();  // (the one that the rows' warps have had)
     tc_fence_before();
     __syncthreads();
+    if (p.split > 1) cluster_sync();  // nobody leaves while its memory is read
     if (warp == kAttnProducts) tmem_free<1>(tmem, 512);
 }
 

@@ -104,6 +104,9 @@ quasar_status quasar_attention(const void* q, int64_t ld_q, const void* k, int64
     const void* fn = attention_kernel(p.d);
     const size_t smem = attention_smem(p.d);
     while (p.split < kAttnMostSplit && work * p.split < n_sm && tiles >= 4 * p.split) p.split *= 2;
+    // more items than SMs, of more than a tile each: a CTA an SM walks over them
+    p.persistent = work > n_sm && tokens > sequences * p.tile_tokens;
+    const int64_t ctas = p.persistent ? std::min<int64_t>(n_sm, items * kv_heads) : items * kv_heads * p.split;
     if ((st = head_map(q, tokens, heads, head_dim, ld_q, p.group, p.tile_tokens, &p.q)) != QUASAR_OK) return st;
     // (without keys no copy is made: any valid map will do)
     const bool none = keys == 0;
@@ -113,7 +116,7 @@ quasar_status quasar_attention(const void* q, int64_t ld_q, const void* k, int64
     if ((st = head_map(none ? q : v, none ? tokens : keys, none ? heads : kv_heads, head_dim, none ? ld_q : ld_v, 1,
                        kAttnKeys, &p.v)) != QUASAR_OK)
         return st;
-    return launch(fn, &p, dim3((unsigned)(items * kv_heads * p.split)), attention_threads(), p.split, smem, stream);
+    return launch(fn, &p, dim3((unsigned)ctas), attention_threads(), p.split, smem, stream);
 }
 
 quasar_status quasar_attention_backward_workspace(int64_t tokens, int64_t heads, int64_t* bytes)

@@ -423,11 +423,13 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
     }
     if (a.spares > 0) {
         if (KEYS) {
-            clear_rows(p.d1, p.ld_d1, (int64_t)kvh * p.d, p.d, p.s.key_starts, p.s.n, p.s.keys, a.index, a.spares);
-            clear_rows(p.d2, p.ld_d2, (int64_t)kvh * p.d, p.d, p.s.key_starts, p.s.n, p.s.keys, a.index, a.spares);
+            clear_rows(p.d1, p.ld_d1, (int64_t)kvh * p.d, p.d, p.s.key_starts, p.s.n, p.s.keys, a.index, a.spares,
+                       threadIdx.x, kGradThreads);
+            clear_rows(p.d2, p.ld_d2, (int64_t)kvh * p.d, p.d, p.s.key_starts, p.s.n, p.s.keys, a.index, a.spares,
+                       threadIdx.x, kGradThreads);
         } else {
             clear_rows(p.d1, p.ld_d1, (int64_t)kvh * p.group * p.d, p.group * p.d, p.s.starts, p.s.n, p.s.tokens, a.index,
-                       a.spares);
+                       a.spares, threadIdx.x, kGradThreads);
         }
     }
     __syncwarp();
