@@ -208,9 +208,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
     uint64_t* never = drained + 1;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(never + 1);
     volatile uint32_t* gone = tmem_slot + 1;
-    float2* stat = reinterpret_cast<float2*>(tmem_slot + 2);  // [2][128]: m and l, where rows have parts
+    float2* stat = reinterpret_cast<float2*>(never + 3);      // [2][128]: m and l, where rows have parts (16-byte aligned)
     float2* swap = stat + 256;                                // [2 turns][2 tiles][2 halves][128]
-    AttnWork* items = reinterpret_cast<AttnWork*>(swap + 1024);  // [2]
+    uint8_t* stages = reinterpret_cast<uint8_t*>(swap + 1024);   // 1 KB a warp of rows
+    AttnWork* items = reinterpret_cast<AttnWork*>(stages + kAttnRowWarps * 1024);  // [2]
 
     const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int rank = p.split > 1 ? (int)cluster_rank() : 0;
@@ -421,15 +422,22 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
         };
         bool synced = false;
         for (int k = 0; k < turns && which(k) < total; ++k) {
-            // (an item that one of them did not get, or did not finish, ends it for all)
+            // (an item that one of them did not get, or did not finish, ends it for
+            // both warps of a row, and for all where they will meet)
             ok = ok && take(k);
-            asm volatile(
-                "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
-                "bar.red.and.pred q, 9, 512, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                : "=r"(agreed)
-                : "r"((uint32_t)ok)
-                : "memory");
-            ok = agreed != 0;
+            if (p.persistent) {
+                float nothing;
+                ok = exchange(0.0f, nothing);
+            } else {
+                asm volatile(
+                    "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+                    "bar.red.and.pred q, 9, 512, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                    : "=r"(agreed)
+                    : "r"((uint32_t)ok)
+                    : "memory");
+                ok = agreed != 0;
+            }
+            ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             const AttnWork& w = items[k & 1];
             const AttnItem& a = w.a;
@@ -548,9 +556,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
             const bool whole = p.split == 1 && !w.twins;  // the row has one part
             if (whole && ok && any_live) {
                 const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-                __nv_bfloat16* const y =
-                    static_cast<__nv_bfloat16*>(p.y) + (int64_t)(a.q0 + token) * p.ld_y + (int64_t)head * p.d + half * kHalf;
-#pragma unroll 1
+                uint32_t out[kHalf / 2];
+#pragma unroll
                 for (int c = 0; c < kHalf; c += 32) {
                     float o[32];
                     if (n > 0) {
@@ -561,11 +568,31 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                         for (int x = 0; x < 32; ++x) o[x] = 0.0f;
                     }
 #pragma unroll
-                    for (int x = 0; x < 32; x += 8)
-                        if (live && half * kHalf + c + x < p.d)
-                            *reinterpret_cast<uint4*>(y + c + x) =
-                                make_uint4(pack_bf16x2(o[x] * inv, o[x + 1] * inv), pack_bf16x2(o[x + 2] * inv, o[x + 3] * inv),
-                                           pack_bf16x2(o[x + 4] * inv, o[x + 5] * inv), pack_bf16x2(o[x + 6] * inv, o[x + 7] * inv));
+                    for (int x = 0; x < 32; x += 2) out[(c + x) / 2] = pack_bf16x2(o[x] * inv, o[x + 1] * inv);
+                }
+                // 1 KB of rows at a time through shared memory, so that a store
+                // covers whole lines (a row a thread took 4,000 cycles an item)
+                constexpr int kVecs = kHalf / 8, kRows = 64 / kVecs;  // 16-byte vectors of a row; rows at a time
+                uint8_t* const stage = stages + warp * 1024;
+#pragma unroll 1
+                for (int q = 0; q < 32; q += kRows) {
+                    __syncwarp();
+                    if (lane >= q && lane < q + kRows) {
+#pragma unroll
+                        for (int c = 0; c < kVecs; ++c)
+                            *reinterpret_cast<uint4*>(stage + ((lane - q) * kVecs + (c ^ (lane & (kVecs - 1)))) * 16) =
+                                make_uint4(out[4 * c], out[4 * c + 1], out[4 * c + 2], out[4 * c + 3]);
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int z = lane; z < 64; z += 32) {
+                        const int row = q + z / kVecs, c = z % kVecs;
+                        const int rr = (warp & 3) * 32 + row, tok = w.t0 + i * p.tile_tokens + rr / p.group;
+                        if (rr < p.tile_tokens * p.group && tok < a.n && half * kHalf + 8 * c < p.d)
+                            *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.y) + (int64_t)(a.q0 + tok) * p.ld_y +
+                                                      (int64_t)(w.kvh * p.group + rr % p.group) * p.d + half * kHalf + 8 * c) =
+                                *reinterpret_cast<const uint4*>(stage + (z / kVecs * kVecs + (c ^ (row & (kVecs - 1)))) * 16);
+                    }
                 }
                 if (p.lse && live && half == 0)
                     p.lse[(int64_t)(a.q0 + token) * p.heads + head] = l == 0.0f ? minus_inf() : 0.69314718f * (m + log2f(l));
