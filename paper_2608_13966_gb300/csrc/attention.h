@@ -43,10 +43,10 @@ struct AttnParams {
     unsigned int* status;
 };
 
-constexpr int kGradCols = 64;  // of a step of the backward kernels
+constexpr int kGradCols = 128;  // of a step of the backward kernels
 
 // One of the two backward kernels: 128 rows stay, the other side streams past
-// in steps of 64 columns.
+// in steps of 128 columns.
 struct AttnGradParams {
     CUtensorMap x1, x2;  // of the rows:  k, v (keys stay) or q, dy (queries stay)
     CUtensorMap z1, z2;  // of the steps: q, dy            or k, v
@@ -55,9 +55,7 @@ struct AttnGradParams {
     int kv_heads;
     int group;
     int d;
-    int tile_tokens;     // of 128 rows of queries
-    int box_heads;       // of a step of queries
-    int step_tokens;
+    int tile_tokens;     // of 128 rows, or columns, of queries
     int causal;
     int items;
     float scale_log2;

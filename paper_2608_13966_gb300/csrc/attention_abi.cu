@@ -174,8 +174,6 @@ quasar_status quasar_attention_backward(const void* dy, int64_t ld_dy, const voi
     p.group = (int)(heads / kv_heads);
     p.d = (int)head_dim;
     p.tile_tokens = kAttnRows / p.group;
-    for (p.box_heads = std::min(p.group, kGradCols); p.group % p.box_heads != 0;) --p.box_heads;
-    p.step_tokens = kGradCols / p.box_heads;
     p.causal = causal;
     p.scale = scale;
     p.scale_log2 = scale * 1.44269504f;
@@ -183,10 +181,9 @@ quasar_status quasar_attention_backward(const void* dy, int64_t ld_dy, const voi
     p.timeout_ns = host_timeout_ns();
     p.force_timeout_ns = host_forced_timeout_ns();
     const int64_t key_items = keys / kAttnRows + sequences + 1, query_items = tokens / p.tile_tokens + sequences + 1;
-    const int64_t steps = (tokens / p.step_tokens + 1) * (p.group / p.box_heads);
     constexpr int64_t kMost = (int64_t(1) << 31) - 1;
     const int lanes = p.d <= 64 ? 8 : 16;
-    if (key_items * kv_heads > kMost || query_items * kv_heads > kMost || steps > kMost ||
+    if (key_items * kv_heads > kMost || query_items * kv_heads > kMost ||
         tokens * heads > kMost * 256 / lanes)
         return QUASAR_ERR_UNSUPPORTED;
     const size_t smem = attention_grad_smem(p.d);
@@ -208,8 +205,8 @@ quasar_status quasar_attention_backward(const void* dy, int64_t ld_dy, const voi
         p.d1 = dk, p.ld_d1 = ld_dk, p.d2 = dv, p.ld_d2 = ld_dv;
         if ((st = map(true, k, ld_k, 1, kAttnRows, &p.x1)) != QUASAR_OK ||
             (st = map(true, v, ld_v, 1, kAttnRows, &p.x2)) != QUASAR_OK ||
-            (st = map(false, q, ld_q, p.box_heads, p.step_tokens, &p.z1)) != QUASAR_OK ||
-            (st = map(false, dy, ld_dy, p.box_heads, p.step_tokens, &p.z2)) != QUASAR_OK ||
+            (st = map(false, q, ld_q, p.group, p.tile_tokens, &p.z1)) != QUASAR_OK ||
+            (st = map(false, dy, ld_dy, p.group, p.tile_tokens, &p.z2)) != QUASAR_OK ||
             (st = launch(attention_grad_kernel(p.d, true), &p, dim3((unsigned)(key_items * kv_heads)),
                          attention_grad_threads(), 1, smem, stream)) != QUASAR_OK)
             return st;

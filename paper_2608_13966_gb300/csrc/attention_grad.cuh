@@ -6,7 +6,7 @@
 //
 // Two kernels of one form, so that every sum has one owner and one order (no
 // atomics, no second copy of dq): 128 rows stay in shared memory, the other
-// side streams past in steps of 64 columns, and the gradients of the rows grow
+// side streams past in steps of 128 columns, and the gradients of the rows grow
 // in tensor memory.
 //
 //   keys stay:    S = K Q^T, dP = V dY^T (transposed scores), dv += P dY, dk += dS Q
@@ -21,21 +21,27 @@
 // P and dS go through tensor memory as bf16, in the place of S and dP: each is
 // rounded once for its matrix product (2^-8 of it), sums are fp32.
 //
-// Warps: 0-7 and 8-15 make P and dS of every other step, two threads a row (with
-// one, their dependent instructions took 2,700 cycles a step, and 4 x 4096
-// causal, 32 heads of 128 over 8, 1815 us in all); 16 copies, 17 and 18 matrix
-// instructions (S and dv; dP and dk or dq), 19 brings the columns' statistics
-// (keys stay).
-// Tensor memory: two gradients of 128 columns, S and dP twice of 64.
+// The matrix instructions are one thread's, in an order that leaves the rows'
+// warps the time of two products for P and as long for dS:
+//
+//   keys stay:    dv(j), S(j+1), dk(j), dP(j+1)
+//   queries stay: S(j+1), dP(j+1), dq(j)          (dP in two places in turn)
+//
+// (In steps of 64 columns, S and dP of two steps at a time, the tensor cores'
+// reading of shared memory took 1.26 as long and the chain of a step was not
+// hidden: 4 x 4096 causal, 32 heads of 128 over 8, 1710 us.)
+//
+// Warps: 0-15 make P and dS, four threads a row; 16 copies, 17 matrix
+// instructions, 18 brings the columns' statistics (keys stay).
 #pragma once
 
 #include "attention.cuh"
 
 namespace quasar {
 
-constexpr int kGradThreads = 640;
-constexpr int kGradCopies = 16, kGradProducts = 17, kGradStats = 19;  // warps (of products two)
-constexpr int kGradSlots = 4;
+constexpr int kGradThreads = 608;
+constexpr int kGradRowWarps = 16, kGradCopies = 16, kGradProducts = 17, kGradStats = 18;  // warps
+constexpr int kGradSlots1 = 3, kGradSlots2 = 2;  // of the rings of z1 (which waits for the step's end) and z2
 
 // The rows' statistics: 8 or 16 threads a (token, head) pair.
 template <int LANES>
@@ -68,47 +74,60 @@ __global__ void __launch_bounds__(256) k_attention_stats(const __grid_constant__
     }
 }
 
+__host__ __device__ constexpr size_t attention_grad_bytes(int blocks)
+{
+    return (size_t)(2 + kGradSlots1 + kGradSlots2) * blocks * kAttnBlock + 2 * kGradCols * 8 +
+           (1 + 2 * kGradSlots1 + 2 * kGradSlots2 + 2 * 2 + 2 + 2 + 1) * 8 + sizeof(AttnItem) + 8;
+}
+
 template <int DB, bool KEYS>
 __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid_constant__ AttnGradParams p)
 {
     constexpr int D = 64 * DB;
-    constexpr uint32_t kRowTile = DB * kAttnBlock;        // bytes of the rows' x1 or x2
-    constexpr uint32_t kColBlock = kGradCols * 128;
-    constexpr uint32_t kColTile = DB * kColBlock;         // of a step's z1 or z2
-    constexpr uint32_t kSlot = 2 * kColTile;
-    constexpr uint32_t kAcc2 = 128, kScores = 256, kDp = 384;  // columns of tensor memory
-    extern __shared__ uint8_t smem_raw[];
+    constexpr uint32_t kTile = DB * kAttnBlock;  // bytes of 128 rows
+    // columns of tensor memory: the gradients from 0 (and 128), the scores, dP
+    constexpr uint32_t kAcc2 = 128, kScores = KEYS ? 256 : 128;
+    auto dp_at = [](int j) { return KEYS ? 384u : 256u + (j & 1) * 128u; };
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint8_t* ring = smem + 2 * kRowTile;
-    float2* col_stats = reinterpret_cast<float2*>(ring + kGradSlots * kSlot);  // [slots][64]
-    uint64_t* x_full = reinterpret_cast<uint64_t*>(col_stats + kGradSlots * kGradCols);
-    uint64_t* full = x_full + 1;               // [slots]
-    uint64_t* empty = full + kGradSlots;       // [slots]
-    uint64_t* stat_full = empty + kGradSlots;  // [slots]
-    uint64_t* s_full = stat_full + kGradSlots; // [2]
-    uint64_t* p_full = s_full + 2;             // [2]: 8 warps
-    uint64_t* acc_full = p_full + 2;
-    uint64_t* never = acc_full + 1;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(never + 1);
+    uint8_t* ring1 = smem + 2 * kTile;
+    uint8_t* ring2 = ring1 + kGradSlots1 * kTile;
+    float2* col_stats = reinterpret_cast<float2*>(ring2 + kGradSlots2 * kTile);  // [2][128], negative
+    uint64_t* x_full = reinterpret_cast<uint64_t*>(col_stats + 2 * kGradCols);
+    uint64_t* full1 = x_full + 1;               // [slots1]
+    uint64_t* empty1 = full1 + kGradSlots1;
+    uint64_t* full2 = empty1 + kGradSlots1;     // [slots2]
+    uint64_t* empty2 = full2 + kGradSlots2;
+    uint64_t* stat_full = empty2 + kGradSlots2; // [2]
+    uint64_t* dp_full = stat_full + 2;          // [2]
+    uint64_t* ds_full = dp_full + 2;            // [2]: the rows' warps
+    uint64_t* s_full = ds_full + 2;
+    uint64_t* p_full = s_full + 1;              // the rows' warps: the scores are read, P is in their place
+    uint64_t* acc_full = p_full + 1;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_full + 1);
     volatile uint32_t* gone = tmem_slot + 1;
     AttnItem* item = reinterpret_cast<AttnItem*>(tmem_slot + 2);
 
     const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int kvh = (int)blockIdx.x % p.kv_heads;
 
+    uint32_t given;
+    asm volatile("mov.u32 %0, %%dynamic_smem_size;" : "=r"(given));
+    if (smem + attention_grad_bytes(DB) > smem_raw + given) {  // (it starts at a multiple of 1024, as declared)
+        if (threadIdx.x == 0) record_timeout(p.status);
+        return;
+    }
     if (threadIdx.x == 0) {
         mbar_init(x_full, 1);
-        for (int s = 0; s < kGradSlots; ++s) {
-            mbar_init(full + s, 1);
-            mbar_init(empty + s, 2);
-            mbar_init(stat_full + s, 1);
-        }
+        for (int s = 0; s < 2 * kGradSlots1 + 2 * kGradSlots2; ++s) mbar_init(full1 + s, 1);
         for (int b = 0; b < 2; ++b) {
-            mbar_init(s_full + b, 2);
-            mbar_init(p_full + b, 8);
+            mbar_init(stat_full + b, 1);
+            mbar_init(dp_full + b, 1);
+            mbar_init(ds_full + b, kGradRowWarps);
         }
-        mbar_init(acc_full, 2);
-        mbar_init(never, 1);
+        mbar_init(s_full, 1);
+        mbar_init(p_full, kGradRowWarps);
+        mbar_init(acc_full, 1);
         *gone = 0;
         mbar_init_fence();
     }
@@ -132,173 +151,167 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
     const int row0 = a.index * (KEYS ? kAttnRows : p.tile_tokens);  // first key, or token, of the rows
     const int shift = a.m - a.n;                                    // key j is seen by tokens from j - shift on
 
-    // Steps.  Keys stay: for each run of box_heads heads the tokens from the
-    // first that sees a key of the tile.  Queries stay: the keys that the last
-    // token sees.
-    int per_run = 0, runs = 1, step0 = 0;
+    // Steps.  Keys stay: the tokens from the first that sees a key of the tile.
+    // Queries stay: the keys that the last token sees.
+    const int by = KEYS ? p.tile_tokens : kGradCols;  // tokens, or keys, of a step
+    int begin = 0, end = 0;                           // of the sequence's tokens, or keys
     if (a.spares == 0) {
         if (KEYS) {
             const int64_t sees = p.causal ? max((int64_t)0, (int64_t)row0 - shift) : 0;
-            if (sees < a.n) {
-                step0 = (int)(sees / p.step_tokens);
-                per_run = (a.n + p.step_tokens - 1) / p.step_tokens - step0;
-            }
-            runs = p.group / p.box_heads;
+            if (sees < a.n) begin = (int)sees / by * by, end = a.n;
         } else {
-            const int last = min(row0 + p.tile_tokens, a.n) - 1;
-            const int64_t see = p.causal ? min((int64_t)a.m, (int64_t)last + 1 + shift) : a.m;
-            per_run = see > 0 ? (int)((see + kGradCols - 1) / kGradCols) : 0;
+            const int64_t last = min((int64_t)row0 + p.tile_tokens, (int64_t)a.n) - 1;
+            end = (int)max((int64_t)0, p.causal ? min((int64_t)a.m, last + 1 + shift) : (int64_t)a.m);
         }
     }
-    const int steps = uniform(per_run * runs);  // (at most tokens x heads, or keys: checked by the host)
-    // A walk over the steps: their first token (or key) and run, without a
-    // division a step.
-    struct Walk {
-        int first, run, begin, end, by;
-        __device__ void next()
-        {
-            first += by;
-            if (first >= end) first = begin, ++run;
-        }
-    };
-    const Walk walk{KEYS ? step0 * p.step_tokens : 0, 0, KEYS ? step0 * p.step_tokens : 0, KEYS ? a.n : a.m,
-                    KEYS ? p.step_tokens : kGradCols};
-    // columns of a step that are the sequence's
-    auto cols_of = [&](const Walk& w) {
-        return KEYS ? min(p.step_tokens, a.n - w.first) * p.box_heads : min(kGradCols, a.m - w.first);
+    const int steps = uniform((end - begin + by - 1) / by);
+    const int limit = KEYS ? a.n : a.m;  // columns behind it are not the sequence's
+    auto cols_of = [&](int j) { return KEYS ? min(by, limit - begin - j * by) * p.group : min(by, limit - j * by); };
+    auto wait = [&](uint64_t* bar, uint32_t parity) {  // the warp's, with one outcome
+        const bool ok = role_sleep(bar, parity, gone, p.timeout_ns, p.status);
+        return __all_sync(0xffffffffu, ok);
     };
 
     if (warp == kGradCopies) {
         if (lane == 0) {
-            if (p.force_timeout_ns) role_sleep(never, 0, gone, p.force_timeout_ns, p.status);
-            int it = 0;
+            // (no copy asked for: nothing else goes on)
+            if (p.force_timeout_ns) role_sleep(acc_full, 0, gone, p.force_timeout_ns, p.status);
+            int sent1 = 0, sent2 = 0;
             const bool rows_sent = steps > 0 && !*gone;
             if (rows_sent) {
                 const uint32_t rows = KEYS ? kAttnRows : (uint32_t)(p.tile_tokens * p.group);
                 mbar_arrive_expect_tx(x_full, 2 * rows * 128 * DB);
                 for (int x = 0; x < 2; ++x)
                     for (int b = 0; b < DB; ++b)
-                        tile_g2s_3d(smem_u32(smem + x * kRowTile + b * kAttnBlock), x ? &p.x2 : &p.x1, 64 * b,
+                        tile_g2s_3d(smem_u32(smem + x * kTile + b * kAttnBlock), x ? &p.x2 : &p.x1, 64 * b,
                                     KEYS ? kvh : kvh * p.group, (KEYS ? a.k0 : a.q0) + row0, smem_u32(x_full));
             }
-            const uint32_t bytes = 2 * DB * 128 * (KEYS ? (uint32_t)(p.step_tokens * p.box_heads) : kGradCols);
-            Walk w = walk;
-            for (; it < steps && !*gone; ++it, w.next()) {
-                const int s = it % kGradSlots;
-                if (it >= kGradSlots && !role_sleep(empty + s, (it / kGradSlots - 1) & 1, gone, p.timeout_ns, p.status))
+            const uint32_t bytes = DB * 128 * (KEYS ? (uint32_t)(p.tile_tokens * p.group) : kGradCols);
+            for (int j = 0; j < steps && !*gone; ++j) {
+                const int at = (KEYS ? a.q0 : a.k0) + begin + j * by, head = KEYS ? kvh * p.group : kvh;
+                const int s1 = j % kGradSlots1, s2 = j % kGradSlots2;
+                if (j >= kGradSlots1 && !role_sleep(empty1 + s1, (j / kGradSlots1 - 1) & 1, gone, p.timeout_ns, p.status))
                     break;
-                mbar_arrive_expect_tx(full + s, bytes);
-                for (int z = 0; z < 2; ++z)
-                    for (int b = 0; b < DB; ++b)
-                        tile_g2s_3d(smem_u32(ring + s * kSlot + z * kColTile + b * kColBlock), z ? &p.z2 : &p.z1, 64 * b,
-                                    KEYS ? kvh * p.group + w.run * p.box_heads : kvh,
-                                    (KEYS ? a.q0 : a.k0) + w.first, smem_u32(full + s));
+                mbar_arrive_expect_tx(full1 + s1, bytes);
+                for (int b = 0; b < DB; ++b)
+                    tile_g2s_3d(smem_u32(ring1 + s1 * kTile + b * kAttnBlock), &p.z1, 64 * b, head, at, smem_u32(full1 + s1));
+                ++sent1;
+                if (j >= kGradSlots2 && !role_sleep(empty2 + s2, (j / kGradSlots2 - 1) & 1, gone, p.timeout_ns, p.status))
+                    break;
+                mbar_arrive_expect_tx(full2 + s2, bytes);
+                for (int b = 0; b < DB; ++b)
+                    tile_g2s_3d(smem_u32(ring2 + s2 * kTile + b * kAttnBlock), &p.z2, 64 * b, head, at, smem_u32(full2 + s2));
+                ++sent2;
             }
             if (*gone) {  // what is in flight has landed before the memory is let go
                 if (rows_sent) mbar_wait_bounded(x_full, 0, p.timeout_ns);
-                for (int j = max(it - kGradSlots, 0); j < it; ++j)
-                    mbar_wait_bounded(full + j % kGradSlots, (j / kGradSlots) & 1, p.timeout_ns);
+                for (int j = max(sent1 - kGradSlots1, 0); j < sent1; ++j)
+                    mbar_wait_bounded(full1 + j % kGradSlots1, (j / kGradSlots1) & 1, p.timeout_ns);
+                for (int j = max(sent2 - kGradSlots2, 0); j < sent2; ++j)
+                    mbar_wait_bounded(full2 + j % kGradSlots2, (j / kGradSlots2) & 1, p.timeout_ns);
             }
         }
-    } else if (warp - kGradProducts == 0 || warp - kGradProducts == 1) {
-        // g = 0: S = X1 Z1^T and, with P in its place, acc2 += P Z2;
-        // g = 1: dP = X2 Z2^T and, with dS in its place, acc1 += dS Z1
+    } else if (warp == kGradProducts) {
         constexpr uint32_t desc_s = mma_desc(kAttnRows, kGradCols, false, false);
         constexpr uint32_t desc_acc = mma_desc(kAttnRows, D, false, true);
-        const int g = warp - kGradProducts;
-        const uint32_t scores = tmem + (g ? kDp : kScores), acc = tmem + (g ? 0 : kAcc2);
-        auto wait = [&](uint64_t* bar, uint32_t parity) {
-            const bool ok = role_sleep(bar, parity, gone, p.timeout_ns, p.status);
-            return __all_sync(0xffffffffu, ok);
-        };
-        // the gradient grows by step `it`
-        auto grow = [&](int it) {
-            if (elect_one()) {
-                const int s = it % kGradSlots;
-                if (KEYS || g == 1) {
-                    const uint64_t db = operand_desc(smem_u32(ring + s * kSlot) + (g ? 0 : kColTile), true);
-                    const uint32_t p_at = scores + (it & 1) * 64;
+        // columns behind the sequence belong to another, or to nobody: zeros
+        auto blank = [&](uint8_t* z, int j) {
+            const int cols = cols_of(j);
+            if (cols >= kGradCols) return;
+            for (int x = lane + cols * 8; x < kGradCols * 8; x += 32)
 #pragma unroll
-                    for (int x = 0; x < kGradCols / 16; ++x)
-                        mma_bf16_ts(acc, p_at + x / 2 * 32 + x % 2 * 8, db + x * k_step(true), desc_acc, it > 0 || x > 0);
-                }
-                mma_commit(smem_u32(empty + s));
-            }
+                for (int b = 0; b < DB; ++b)
+                    *reinterpret_cast<uint4*>(z + b * kAttnBlock + x * 16) = make_uint4(0, 0, 0, 0);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
         };
-        bool ok = steps == 0 || wait(x_full, 0);
-        Walk w = walk;
-        for (int it = 0; it < steps && ok; ++it, w.next()) {
-            const int s = it % kGradSlots, buf = it & 1;
-            if (!(ok = wait(full + s, (it / kGradSlots) & 1))) break;
-            // columns behind the sequence belong to another, or to nobody: zeros
-            // (both warps write them, each before its own reads)
-            const int cols = cols_of(w);
-            if (cols < kGradCols) {
-                for (int x = lane + cols * 8; x < kGradCols * 8; x += 32)
-#pragma unroll
-                    for (int b = 0; b < 2 * DB; ++b)
-                        *reinterpret_cast<uint4*>(ring + s * kSlot + b * kColBlock + x * 16) = make_uint4(0, 0, 0, 0);
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-            }
-            tc_fence_after();
+        // 128 x 128 scores: rows of x by columns of z
+        auto scores = [&](uint32_t to, const uint8_t* x, const uint8_t* z, uint64_t* done, uint64_t* free) {
             if (elect_one()) {
-                const uint32_t x = smem_u32(smem + g * kRowTile), z = smem_u32(ring + s * kSlot + g * kColTile);
+                const uint64_t dx = operand_desc(smem_u32(x), false), dz = operand_desc(smem_u32(z), false);
 #pragma unroll
-                for (int b = 0; b < DB; ++b) {
-                    const uint64_t da = operand_desc(x + b * kAttnBlock, false), db = operand_desc(z + b * kColBlock, false);
+                for (int b = 0; b < DB; ++b)
 #pragma unroll
                     for (int y = 0; y < 4; ++y)
-                        mma_bf16<1>(scores + buf * 64, da + y * k_step(false), db + y * k_step(false), desc_s, b + y > 0);
-                }
-                mma_commit(smem_u32(s_full + buf));
+                        mma_bf16<1>(tmem + to, dx + b * (kAttnBlock >> 4) + y * k_step(false),
+                                    dz + b * (kAttnBlock >> 4) + y * k_step(false), desc_s, b + y > 0);
+                mma_commit(smem_u32(done));
+                if (free) mma_commit(smem_u32(free));
             }
             __syncwarp();
-            if (it > 0) {
-                if (!(ok = wait(p_full + (buf ^ 1), ((it - 1) / 2) & 1))) break;
-                tc_fence_after();
-                grow(it - 1);
+        };
+        // a gradient grows by the probabilities (or dS) at `from` times z
+        auto grow = [&](uint32_t acc, uint32_t from, const uint8_t* z, bool add, uint64_t* free) {
+            if (elect_one()) {
+                const uint64_t dz = operand_desc_tall(smem_u32(z), kGradCols);
+#pragma unroll
+                for (int x = 0; x < kGradCols / 16; ++x)
+                    mma_bf16_ts(tmem + acc, tmem + from + x / 2 * 32 + x % 2 * 8, dz + x * k_step(true), desc_acc,
+                                add || x > 0);
+                mma_commit(smem_u32(free));
             }
-        }
-        if (steps > 0 && ok && (ok = wait(p_full + ((steps - 1) & 1), ((steps - 1) / 2) & 1))) {
+            __syncwarp();
+        };
+        auto score_s = [&](int j) {  // S(j)
+            uint8_t* const z = ring1 + j % kGradSlots1 * kTile;
+            if (!wait(full1 + j % kGradSlots1, (j / kGradSlots1) & 1)) return false;
+            blank(z, j);
             tc_fence_after();
-            grow(steps - 1);
+            scores(kScores, smem, z, s_full, nullptr);
+            return true;
+        };
+        auto score_dp = [&](int j) {  // dP(j)
+            uint8_t* const z = ring2 + j % kGradSlots2 * kTile;
+            if (!wait(full2 + j % kGradSlots2, (j / kGradSlots2) & 1)) return false;
+            blank(z, j);
+            tc_fence_after();
+            scores(dp_at(j), smem + kTile, z, dp_full + (j & 1), KEYS ? nullptr : empty2 + j % kGradSlots2);
+            return true;
+        };
+        bool ok = steps == 0 || (wait(x_full, 0) && score_s(0) && score_dp(0));
+        for (int j = 0; j < steps && ok; ++j) {
+            if (!(ok = wait(p_full, j & 1))) break;
+            tc_fence_after();
+            if (KEYS) grow(kAcc2, kScores, ring2 + j % kGradSlots2 * kTile, j > 0, empty2 + j % kGradSlots2);
+            if (j + 1 < steps && !(ok = score_s(j + 1))) break;
+            if (!KEYS && j + 1 < steps && !(ok = score_dp(j + 1))) break;
+            if (!(ok = wait(ds_full + (j & 1), (j >> 1) & 1))) break;
+            tc_fence_after();
+            grow(0, dp_at(j), ring1 + j % kGradSlots1 * kTile, j > 0, empty1 + j % kGradSlots1);
+            if (KEYS && j + 1 < steps && !(ok = score_dp(j + 1))) break;
         }
         if (elect_one()) {  // every instruction is done before the memory is let go
             mma_commit(smem_u32(acc_full));
             mbar_wait_bounded(acc_full, 0, p.timeout_ns);
         }
+        __syncwarp();
     } else if (warp == kGradStats) {
         if (KEYS) {
-            Walk w = walk;
-            const int place[2] = {lane / p.box_heads * p.heads + lane % p.box_heads,
-                                  (lane + 32) / p.box_heads * p.heads + (lane + 32) % p.box_heads};
-            for (int it = 0; it < steps; ++it, w.next()) {
-                const int s = it % kGradSlots, cols = cols_of(w);
-                const int64_t at = (int64_t)(a.q0 + w.first) * p.heads + kvh * p.group + w.run * p.box_heads;
-                float2 st[2];
+            int place[4];  // of the columns lane, lane + 32, ... in a row of statistics
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const int c = lane + 32 * q;  // behind the sequence: p = 0
-                    st[q] = c < cols ? p.stats[at + place[q]]
-                                     : make_float2(-minus_inf(), 0.0f);
-                    st[q] = make_float2(-st[q].x, -st[q].y);  // (as they are added)
-                }
-                bool ok = it < kGradSlots || role_sleep(empty + s, (it / kGradSlots - 1) & 1, gone, p.timeout_ns, p.status);
-                ok = __all_sync(0xffffffffu, ok && !*gone);
-                if (!ok) break;
+            for (int q = 0; q < 4; ++q)
+                place[q] = (lane + 32 * q) / p.group * p.heads + (lane + 32 * q) % p.group;
+            for (int j = 0; j < steps; ++j) {
+                const int64_t at = (int64_t)(a.q0 + begin + j * by) * p.heads + kvh * p.group;
+                const int cols = cols_of(j);
+                float2 st[4];
 #pragma unroll
-                for (int q = 0; q < 2; ++q) col_stats[s * kGradCols + lane + 32 * q] = st[q];
+                for (int q = 0; q < 4; ++q)  // (behind the sequence: p = 0)
+                    st[q] = lane + 32 * q < cols ? p.stats[at + place[q]] : make_float2(-minus_inf(), 0.0f);
+                if (j >= 2 && !wait(ds_full + (j & 1), ((j >> 1) - 1) & 1)) break;
+#pragma unroll
+                for (int q = 0; q < 4; ++q)  // (as they are added)
+                    col_stats[(j & 1) * kGradCols + lane + 32 * q] = make_float2(-st[q].x, -st[q].y);
                 __syncwarp();
-                if (lane == 0) mbar_arrive(stat_full + s);
+                if (lane == 0) mbar_arrive(stat_full + (j & 1));
             }
         }
     } else {
-        // turn: of every other step; half: of its columns, whose P and dS lie where
-        // this half of S and dP lay
-        const int turn = warp >> 3, half = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
+        // a thread's row, and its quarter of a step's columns, whose P and dS lie
+        // where this quarter of S and dP lay
+        const int quarter = warp >> 2, r = (warp & 3) * 32 + lane;
         const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t s_at = mine + kScores + quarter * 32;
         // the row: key row0 + r, or (token, head)
         const int token = row0 + r / p.group, head = kvh * p.group + r % p.group;
         const bool live = a.spares == 0 && (KEYS ? row0 + r < a.m : r < p.tile_tokens * p.group && token < a.n);
@@ -308,68 +321,81 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
             own = p.stats[(int64_t)(a.q0 + token) * p.heads + head];
             own = make_float2(-own.x, -own.y);
         }
-        // of the sequence's columns, the first that sees the row's key; the last
+        // of the sequence's tokens, the first that sees the row's key; the last
         // key that the row's token sees
         const int64_t from = KEYS && p.causal ? (int64_t)row0 + r - shift : 0;
         const int64_t upto = p.causal ? min((int64_t)a.m - 1, (int64_t)token + shift) : (int64_t)a.m - 1;
+        const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
         bool ok = true;
-        Walk w = walk;
-        if (turn) w.next();
-        for (int it = turn; it < steps; it += 2, w.next(), w.next()) {
-            const int s = it % kGradSlots;
-            ok = role_sleep(s_full + turn, (it / 2) & 1, gone, p.timeout_ns, p.status);
-            if (KEYS && ok) ok = role_sleep(stat_full + s, (it / kGradSlots) & 1, gone, p.timeout_ns, p.status);
-            ok = __all_sync(0xffffffffu, ok);
+        for (int j = 0; j < steps; ++j) {
+            ok = wait(s_full, j & 1);
+            if (KEYS && ok) ok = wait(stat_full + (j & 1), (j >> 1) & 1);
+            if (!ok) break;
+            tc_fence_after();
+            const float2* st = col_stats + (j & 1) * kGradCols + quarter * 32;
+            float2 e[16];
+            if (any_live) {
+                // the columns [lo, hi] of this quarter that the row sees (or that see it)
+                int lo = 0, hi = 31;
+                const int64_t f = begin + (int64_t)j * by;
+                if (KEYS && p.causal)
+                    lo = (int)max((int64_t)0, min((int64_t)32, (from - f) * p.group - quarter * 32));
+                if (!KEYS) hi = (int)max((int64_t)-1, min((int64_t)31, upto - f - quarter * 32));
+                const bool masked = !__all_sync(0xffffffffu, lo == 0 && hi == 31);
+                float s[32];
+                tmem_ld(s_at, s);
+                tmem_wait_ld(s);
+#pragma unroll
+                for (int x = 0; x < 16; ++x) {
+                    float2 lse = make_float2(own.x, own.x);
+                    if (KEYS) lse = make_float2(st[2 * x].x, st[2 * x + 1].x);
+                    e[x] = __ffma2_rn(make_float2(s[2 * x], s[2 * x + 1]), scale2, lse);
+                    e[x].x = exp2_fast(e[x].x);
+                    e[x].y = exp2_fast(e[x].y);
+                }
+                if (masked) {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        if (2 * x < lo || 2 * x > hi) e[x].x = 0.0f;
+                        if (2 * x + 1 < lo || 2 * x + 1 > hi) e[x].y = 0.0f;
+                    }
+                }
+                if (KEYS) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) w[x] = pack_bf16x2(e[x].x, e[x].y);
+                    tmem_st(s_at, w);
+                    tmem_wait_st();
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full);
+            ok = wait(dp_full + (j & 1), (j >> 1) & 1);
             if (!ok) break;
             tc_fence_after();
             if (any_live) {
-                const uint32_t s_at = mine + kScores + turn * 64 + half * 32, dp_at = mine + kDp + turn * 64 + half * 32;
-                // the columns [lo, hi] of this half that the row sees (or that see it)
-                int lo = 0, hi = 31;
-                const int f = w.first;
-                if (KEYS && p.causal)
-                    lo = (int)max((int64_t)0, min((int64_t)32, (from - f) * p.box_heads - half * 32));
-                if (!KEYS) hi = (int)max((int64_t)-1, min((int64_t)31, upto - f - half * 32));
-                const bool masked = !__all_sync(0xffffffffu, lo == 0 && hi == 31);
-                const float2* st = col_stats + s * kGradCols + half * 32;
-                const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
+                const uint32_t at = mine + dp_at(j) + quarter * 32;
+                float dp[32];
+                uint32_t w[16];
+                tmem_ld(at, dp);
+                tmem_wait_ld(dp);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float sc[16], dp[16];
-                    tmem_ld(s_at + 16 * h, sc);
-                    tmem_ld(dp_at + 16 * h, dp);
-                    tmem_wait_ld(sc);
-                    tmem_wait_ld(dp);
-                    uint32_t pw[8], dw[8];
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) {
-                        float2 lse = make_float2(own.x, own.x), delta = make_float2(own.y, own.y);
-                        if (KEYS) {
-                            const float4 two = *reinterpret_cast<const float4*>(st + 16 * h + 2 * x);
-                            lse = make_float2(two.x, two.z);
-                            delta = make_float2(two.y, two.w);
-                        }
-                        float2 e = __ffma2_rn(make_float2(sc[2 * x], sc[2 * x + 1]), scale2, lse);
-                        e.x = exp2_fast(e.x);
-                        e.y = exp2_fast(e.y);
-                        float2 ds = __fmul2_rn(e, __fadd2_rn(make_float2(dp[2 * x], dp[2 * x + 1]), delta));
-                        if (masked) {
-                            const int c = 16 * h + 2 * x;
-                            if (c < lo || c > hi) e.x = 0.0f, ds.x = 0.0f;
-                            if (c + 1 < lo || c + 1 > hi) e.y = 0.0f, ds.y = 0.0f;
-                        }
-                        pw[x] = pack_bf16x2(e.x, e.y);
-                        dw[x] = pack_bf16x2(ds.x, ds.y);
-                    }
-                    // (columns that this thread has read)
-                    if (KEYS) tmem_st(s_at + 8 * h, pw);
-                    tmem_st(dp_at + 8 * h, dw);
+                for (int x = 0; x < 16; ++x) {
+                    float2 delta = make_float2(own.y, own.y);
+                    if (KEYS) delta = make_float2(st[2 * x].y, st[2 * x + 1].y);
+                    float2 ds = __fmul2_rn(e[x], __fadd2_rn(make_float2(dp[2 * x], dp[2 * x + 1]), delta));
+                    // (0 times what need not be finite)
+                    if (e[x].x == 0.0f) ds.x = 0.0f;
+                    if (e[x].y == 0.0f) ds.y = 0.0f;
+                    w[x] = pack_bf16x2(ds.x, ds.y);
                 }
+                tmem_st(at, w);
                 tmem_wait_st();
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(p_full + turn);
+            if (lane == 0) mbar_arrive(ds_full + (j & 1));
         }
         if (ok && steps > 0) {
             ok = role_sleep(acc_full, 0, gone, p.timeout_ns, p.status) && !*gone;
@@ -378,10 +404,11 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
         }
         // dk or dq by warps 0-7, dv by warps 8-15, half of the columns each,
         // through the rows' memory so that a store covers whole rows
+        const int turn = warp >> 3, half = warp >> 2 & 1;
         if (ok && any_live && (KEYS || turn == 0)) {
             constexpr int kHalf = D / 2;
             const float scale = turn == 0 ? p.scale : 1.0f;
-            uint8_t* stage = smem + turn * kRowTile + (warp & 3) * 32 * D * 2;
+            uint8_t* stage = smem + turn * kTile + (warp & 3) * 32 * D * 2;
 #pragma unroll 1
             for (int c = half * kHalf; c < (half + 1) * kHalf; c += 32) {
                 float o[32];

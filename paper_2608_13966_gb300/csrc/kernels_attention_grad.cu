@@ -20,11 +20,10 @@ const void* attention_grad_kernel(int d, bool keys)
 
 int attention_grad_threads() { return kGradThreads; }
 
+// (the memory starts at a multiple of 1024; where there is room, without relying on it)
 size_t attention_grad_smem(int d)
 {
-    const size_t block = (size_t)(d <= 64 ? 1 : 2) * 128;
-    return 1024 + 2 * kAttnRows * block + kGradSlots * (2 * kGradCols * block + kGradCols * 8) +
-           (1 + 3 * kGradSlots + 4 + 2) * 8 + 8 + sizeof(AttnItem) + 8;
+    return d <= 64 ? 1024 + attention_grad_bytes(1) : attention_grad_bytes(2);
 }
 
 }  // namespace quasar
