@@ -92,8 +92,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* ring1 = smem + 2 * kTile;
     uint8_t* ring2 = ring1 + kGradSlots1 * kTile;
-    float2* col_stats = reinterpret_cast<float2*>(ring2 + kGradSlots2 * kTile);  // [2][128], negative
-    uint64_t* x_full = reinterpret_cast<uint64_t*>(col_stats + 2 * kGradCols);
+    float* col_stats = reinterpret_cast<float*>(ring2 + kGradSlots2 * kTile);  // [2][lse, D][128], negative
+    uint64_t* x_full = reinterpret_cast<uint64_t*>(col_stats + 4 * kGradCols);
     uint64_t* full1 = x_full + 1;               // [slots1]
     uint64_t* empty1 = full1 + kGradSlots1;
     uint64_t* full2 = empty1 + kGradSlots1;     // [slots2]
@@ -252,34 +252,68 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
             }
             __syncwarp();
         };
-        auto score_s = [&](int j) {  // S(j)
-            uint8_t* const z = ring1 + j % kGradSlots1 * kTile;
-            if (!wait(full1 + j % kGradSlots1, (j / kGradSlots1) & 1)) return false;
-            blank(z, j);
-            tc_fence_after();
-            scores(kScores, smem, z, s_full, nullptr);
+        // A place of a ring, walked without divisions (a wait and what goes with
+        // it is in the way of the tensor cores, instruction by instruction).
+        struct Place {
+            int slot, phase;
+            __device__ void next(int slots)
+            {
+                if (++slot == slots) slot = 0, phase ^= 1;
+            }
+        };
+        Place z1{0, 0}, z2{0, 0};  // of the next S and dP
+        const bool blanks = by * (KEYS ? p.group : 1) < kGradCols;  // (in every step)
+        auto come1 = [&](int j) {  // z1 of step j has come
+            if (!wait(full1 + z1.slot, z1.phase)) return false;
+            if (blanks || j == steps - 1) blank(ring1 + z1.slot * kTile, j);
             return true;
         };
-        auto score_dp = [&](int j) {  // dP(j)
-            uint8_t* const z = ring2 + j % kGradSlots2 * kTile;
-            if (!wait(full2 + j % kGradSlots2, (j / kGradSlots2) & 1)) return false;
-            blank(z, j);
-            tc_fence_after();
-            scores(dp_at(j), smem + kTile, z, dp_full + (j & 1), KEYS ? nullptr : empty2 + j % kGradSlots2);
+        auto come2 = [&](int j) {
+            if (!wait(full2 + z2.slot, z2.phase)) return false;
+            if (blanks || j == steps - 1) blank(ring2 + z2.slot * kTile, j);
             return true;
         };
-        bool ok = steps == 0 || (wait(x_full, 0) && score_s(0) && score_dp(0));
+        auto score_s = [&]() {
+            scores(kScores, smem, ring1 + z1.slot * kTile, s_full, nullptr);
+            z1.next(kGradSlots1);
+        };
+        auto score_dp = [&](int j) {
+            scores(dp_at(j), smem + kTile, ring2 + z2.slot * kTile, dp_full + (j & 1), KEYS ? nullptr : empty2 + z2.slot);
+            z2.next(kGradSlots2);
+        };
+        bool ok = steps == 0 || (wait(x_full, 0) && come1(0) && come2(0));
+        if (steps > 0 && ok) {
+            tc_fence_after();
+            score_s();
+            score_dp(0);
+        }
+        int old1 = 0;
         for (int j = 0; j < steps && ok; ++j) {
-            if (!(ok = wait(p_full, j & 1))) break;
-            tc_fence_after();
-            if (KEYS) grow(kAcc2, kScores, ring2 + j % kGradSlots2 * kTile, j > 0, empty2 + j % kGradSlots2);
-            if (j + 1 < steps && !(ok = score_s(j + 1))) break;
-            if (!KEYS && j + 1 < steps && !(ok = score_dp(j + 1))) break;
+            const bool more = j + 1 < steps;
+            if (KEYS) {
+                // (two products at a time, their operands waited for before them)
+                if (more && !(ok = come1(j + 1))) break;
+                if (!(ok = wait(p_full, j & 1))) break;
+                tc_fence_after();
+                grow(kAcc2, kScores, ring2 + (j & 1) * kTile, j > 0, empty2 + (j & 1));
+                if (more) score_s();
+                if (more && !(ok = come2(j + 1))) break;
+            } else {
+                if (!(ok = wait(p_full, j & 1))) break;
+                if (more && !(ok = come1(j + 1))) break;
+                tc_fence_after();
+                if (more) score_s();
+                if (more && !(ok = come2(j + 1))) break;
+                tc_fence_after();
+                if (more) score_dp(j + 1);
+            }
             if (!(ok = wait(ds_full + (j & 1), (j >> 1) & 1))) break;
             tc_fence_after();
-            grow(0, dp_at(j), ring1 + j % kGradSlots1 * kTile, j > 0, empty1 + j % kGradSlots1);
-            if (KEYS && j + 1 < steps && !(ok = score_dp(j + 1))) break;
+            grow(0, dp_at(j), ring1 + old1 * kTile, j > 0, empty1 + old1);
+            if (++old1 == kGradSlots1) old1 = 0;
+            if (KEYS && more) score_dp(j + 1);
         }
+        static_assert(kGradSlots2 == 2, "z2 of step j is in place j & 1");
         if (elect_one()) {  // every instruction is done before the memory is let go
             mma_commit(smem_u32(acc_full));
             mbar_wait_bounded(acc_full, 0, p.timeout_ns);
@@ -300,8 +334,11 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                     st[q] = lane + 32 * q < cols ? p.stats[at + place[q]] : make_float2(-minus_inf(), 0.0f);
                 if (j >= 2 && !wait(ds_full + (j & 1), ((j >> 1) - 1) & 1)) break;
 #pragma unroll
-                for (int q = 0; q < 4; ++q)  // (as they are added)
-                    col_stats[(j & 1) * kGradCols + lane + 32 * q] = make_float2(-st[q].x, -st[q].y);
+                for (int q = 0; q < 4; ++q) {  // (as they are added)
+                    float* const to = col_stats + (j & 1) * 2 * kGradCols + lane + 32 * q;
+                    to[0] = -st[q].x;
+                    to[kGradCols] = -st[q].y;
+                }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(stat_full + (j & 1));
             }
@@ -332,8 +369,10 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
             if (KEYS && ok) ok = wait(stat_full + (j & 1), (j >> 1) & 1);
             if (!ok) break;
             tc_fence_after();
-            const float2* st = col_stats + (j & 1) * kGradCols + quarter * 32;
+            // (four at a time: a load of each took the LSU longer than all else)
+            const float4* st = reinterpret_cast<const float4*>(col_stats + (j & 1) * 2 * kGradCols + quarter * 32);
             float2 e[16];
+            bool masked = false;
             if (any_live) {
                 // the columns [lo, hi] of this quarter that the row sees (or that see it)
                 int lo = 0, hi = 31;
@@ -341,17 +380,20 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                 if (KEYS && p.causal)
                     lo = (int)max((int64_t)0, min((int64_t)32, (from - f) * p.group - quarter * 32));
                 if (!KEYS) hi = (int)max((int64_t)-1, min((int64_t)31, upto - f - quarter * 32));
-                const bool masked = !__all_sync(0xffffffffu, lo == 0 && hi == 31);
+                masked = !__all_sync(0xffffffffu, lo == 0 && hi == 31) || cols_of(j) < kGradCols;
                 float s[32];
                 tmem_ld(s_at, s);
                 tmem_wait_ld(s);
 #pragma unroll
-                for (int x = 0; x < 16; ++x) {
-                    float2 lse = make_float2(own.x, own.x);
-                    if (KEYS) lse = make_float2(st[2 * x].x, st[2 * x + 1].x);
-                    e[x] = __ffma2_rn(make_float2(s[2 * x], s[2 * x + 1]), scale2, lse);
+                for (int x = 0; x < 16; x += 2) {
+                    float4 lse = make_float4(own.x, own.x, own.x, own.x);
+                    if (KEYS) lse = st[x / 2];
+                    e[x] = __ffma2_rn(make_float2(s[2 * x], s[2 * x + 1]), scale2, make_float2(lse.x, lse.y));
+                    e[x + 1] = __ffma2_rn(make_float2(s[2 * x + 2], s[2 * x + 3]), scale2, make_float2(lse.z, lse.w));
                     e[x].x = exp2_fast(e[x].x);
                     e[x].y = exp2_fast(e[x].y);
+                    e[x + 1].x = exp2_fast(e[x + 1].x);
+                    e[x + 1].y = exp2_fast(e[x + 1].y);
                 }
                 if (masked) {
 #pragma unroll
@@ -381,14 +423,18 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                 tmem_ld(at, dp);
                 tmem_wait_ld(dp);
 #pragma unroll
-                for (int x = 0; x < 16; ++x) {
-                    float2 delta = make_float2(own.y, own.y);
-                    if (KEYS) delta = make_float2(st[2 * x].y, st[2 * x + 1].y);
-                    float2 ds = __fmul2_rn(e[x], __fadd2_rn(make_float2(dp[2 * x], dp[2 * x + 1]), delta));
-                    // (0 times what need not be finite)
-                    if (e[x].x == 0.0f) ds.x = 0.0f;
-                    if (e[x].y == 0.0f) ds.y = 0.0f;
-                    w[x] = pack_bf16x2(ds.x, ds.y);
+                for (int x = 0; x < 16; x += 2) {
+                    float4 delta = make_float4(own.y, own.y, own.y, own.y);
+                    if (KEYS) delta = st[kGradCols / 4 + x / 2];
+                    float2 ds[2] = {
+                        __fmul2_rn(e[x], __fadd2_rn(make_float2(dp[2 * x], dp[2 * x + 1]), make_float2(delta.x, delta.y))),
+                        __fmul2_rn(e[x + 1], __fadd2_rn(make_float2(dp[2 * x + 2], dp[2 * x + 3]), make_float2(delta.z, delta.w)))};
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        w[x + y] = pack_bf16x2(ds[y].x, ds[y].y);
+                        // (0 times what need not be finite)
+                        if (masked) w[x + y] &= (e[x + y].x == 0.0f ? 0u : 0xFFFFu) | (e[x + y].y == 0.0f ? 0u : 0xFFFF0000u);
+                    }
                 }
                 tmem_st(at, w);
                 tmem_wait_st();
