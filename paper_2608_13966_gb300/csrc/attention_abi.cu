@@ -218,7 +218,7 @@ quasar_status quasar_attention_backward(const void* dy, int64_t ld_dy, const voi
             (st = map(false, dy, ld_dy, p.group, p.tile_tokens, &p.x2)) != QUASAR_OK ||
             (st = map(true, k, ld_k, 1, kGradCols, &p.z1)) != QUASAR_OK ||
             (st = map(true, v, ld_v, 1, kGradCols, &p.z2)) != QUASAR_OK ||
-            (st = launch(attention_grad_kernel(p.d, false), &p, dim3((unsigned)(query_items * kv_heads)),
+            (st = launch(attention_grad_kernel(p.d, false), &p, dim3((unsigned)std::min<int64_t>(n_sm, query_items * kv_heads)),
                          attention_grad_threads(), 1, smem, stream)) != QUASAR_OK)
             return st;
     }
