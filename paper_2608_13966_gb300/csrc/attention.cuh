@@ -72,35 +72,43 @@ struct AttnItem {
 };
 
 // The sequence that item `want` falls into, where a sequence of n rows has
-// ceil(n / span) items (rows of q, or of the keys).  Whole-warp call.
+// ceil(n / span) items (rows of q, or of the keys).  Whole-warp call; 128
+// sequences are read at a time.
 __device__ __forceinline__ AttnItem find_item(const AttnSequences& s, int want, int items, int span, bool of_keys = false)
 {
     const int lane = threadIdx.x & 31;
     int before = 0;
-    for (int base = 0; base < s.n; base += 32) {
-        int from = 0, n = 0;
-        if (base + lane < s.n)
-            sequence_rows(of_keys ? s.key_starts : s.starts, base + lane, of_keys ? s.keys : s.tokens, from, n);
-        const int mine = (int)(((int64_t)n + span - 1) / span);
-        int upto = mine;
+    for (int base = 0; base < s.n; base += 128) {
+        int mine[4];
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int x = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += x;
+        for (int q = 0; q < 4; ++q) {
+            int from = 0, n = 0;
+            if (base + 32 * q + lane < s.n)
+                sequence_rows(of_keys ? s.key_starts : s.starts, base + 32 * q + lane, of_keys ? s.keys : s.tokens, from, n);
+            mine[q] = (int)(((int64_t)n + span - 1) / span);
         }
-        const unsigned hit = __ballot_sync(0xffffffffu, before + upto > want);
-        if (hit) {
-            const int l = __ffs(hit) - 1;
-            AttnItem a{};
-            sequence_rows(s.starts, base + l, s.tokens, a.q0, a.n);
-            sequence_rows(s.key_starts, base + l, s.keys, a.k0, a.m);
-            const int count = __shfl_sync(0xffffffffu, mine, l);
-            // the longest first, under a causal mask: the last tokens, the first keys
-            a.index = want - before - __shfl_sync(0xffffffffu, upto - mine, l);
-            if (!of_keys) a.index = count - 1 - a.index;
-            return a;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            int upto = mine[q];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int x = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += x;
+            }
+            const unsigned hit = __ballot_sync(0xffffffffu, before + upto > want);
+            if (hit) {
+                const int l = __ffs(hit) - 1;
+                AttnItem a{};
+                sequence_rows(s.starts, base + 32 * q + l, s.tokens, a.q0, a.n);
+                sequence_rows(s.key_starts, base + 32 * q + l, s.keys, a.k0, a.m);
+                const int count = __shfl_sync(0xffffffffu, mine[q], l);
+                // the longest first, under a causal mask: the last tokens, the first keys
+                a.index = want - before - __shfl_sync(0xffffffffu, upto - mine[q], l);
+                if (!of_keys) a.index = count - 1 - a.index;
+                return a;
+            }
+            before += __shfl_sync(0xffffffffu, upto, 31);
         }
-        before += __shfl_sync(0xffffffffu, upto, 31);
     }
     return AttnItem{0, 0, 0, 0, want - before, items - before};
 }

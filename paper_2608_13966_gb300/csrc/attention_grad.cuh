@@ -518,26 +518,31 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                 tc_fence_after();
                 if (any_live) {
                     const uint32_t at = mine + dp_at(g) + quarter * 32;
-                    float dp[32];
-                    uint32_t words[16];
-                    tmem_ld(at, dp);
-                    tmem_wait_ld(dp);
 #pragma unroll
-                    for (int x = 0; x < 16; x += 2) {
-                        float4 delta = make_float4(own.y, own.y, own.y, own.y);
-                        if (KEYS) delta = st[kGradCols / 4 + x / 2];
-                        float2 ds[2] = {
-                            __fmul2_rn(e[x], __fadd2_rn(make_float2(dp[2 * x], dp[2 * x + 1]), make_float2(delta.x, delta.y))),
-                            __fmul2_rn(e[x + 1], __fadd2_rn(make_float2(dp[2 * x + 2], dp[2 * x + 3]), make_float2(delta.z, delta.w)))};
+                    for (int h = 0; h < 16; h += 8) {  // (16 columns at a time: registers)
+                        float dp[16];
+                        uint32_t words[8];
+                        tmem_ld(at + 2 * h, dp);
+                        tmem_wait_ld(dp);
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            words[x + y] = pack_bf16x2(ds[y].x, ds[y].y);
-                            // (0 times what need not be finite)
-                            if (masked)
-                                words[x + y] &= (e[x + y].x == 0.0f ? 0u : 0xFFFFu) | (e[x + y].y == 0.0f ? 0u : 0xFFFF0000u);
+                        for (int x = 0; x < 8; x += 2) {
+                            float4 delta = make_float4(own.y, own.y, own.y, own.y);
+                            if (KEYS) delta = st[kGradCols / 4 + (h + x) / 2];
+                            float2 ds[2] = {
+                                __fmul2_rn(e[h + x], __fadd2_rn(make_float2(dp[2 * x], dp[2 * x + 1]), make_float2(delta.x, delta.y))),
+                                __fmul2_rn(e[h + x + 1],
+                                           __fadd2_rn(make_float2(dp[2 * x + 2], dp[2 * x + 3]), make_float2(delta.z, delta.w)))};
+#pragma unroll
+                            for (int y = 0; y < 2; ++y) {
+                                words[x + y] = pack_bf16x2(ds[y].x, ds[y].y);
+                                // (0 times what need not be finite)
+                                if (masked)
+                                    words[x + y] &= (e[h + x + y].x == 0.0f ? 0u : 0xFFFFu) |
+                                                    (e[h + x + y].y == 0.0f ? 0u : 0xFFFF0000u);
+                            }
                         }
+                        tmem_st(at + h, words);
                     }
-                    tmem_st(at, words);
                     tmem_wait_st();
                 }
                 tc_fence_before();

@@ -167,6 +167,61 @@ def test_empty():
     assert (o["y"] == 0).all() and (o["lse"] == -math.inf).all()
 
 
+@pytest.mark.parametrize("many", [300, 3001])
+def test_many_sequences(many):
+    """One to three tokens a sequence, up to 40 keys."""
+    g = torch.Generator()
+    g.manual_seed(many)
+    nq = torch.randint(0, 4, (many,), generator=g).tolist()
+    nk = [n + extra for n, extra in zip(nq, torch.randint(0, 38, (many,), generator=g).tolist())]
+    case = (nq, nk, 4, 2, 64, True)
+    q, k, v, starts, key_starts, *_ = make(case)
+    o = api.attention(q, k, v, 64, starts=starts, key_starts=key_starts, lse=True)
+    back = api.attention_backward(q, q, k, v, o["y"], o["lse"], 64, starts=starts, key_starts=key_starts)
+    api.check_device()
+    some = set(torch.randint(0, many, (40,), generator=g).tolist()) | {0, many - 1}
+    for i, (rq, rk) in enumerate(each(nq, nk)):
+        if i not in some or rq.start == rq.stop:
+            continue
+        y, lse, e_y, e_lse = ref.forward(q[rq], k[rk], v[rk], 64, 2, True, 0.125)
+        assert ((o["y"][rq].double() - y).abs() <= e_y + ref.HALF * (y.abs() + e_y)).all()
+        want = ref.backward(q[rq], q[rq], k[rk], v[rk], 64, 2, True, 0.125)
+        for name, rows, x, e in (("dq", rq, want[0], want[3]), ("dk", rk, want[1], want[4]), ("dv", rk, want[2], want[5])):
+            assert ((back[name][rows].double() - x).abs() <= e + ref.HALF * (x.abs() + e)).all(), name
+
+
+def test_far_rows():
+    """Rows beyond 2^31 elements of a buffer: a long cache, one head of it wide.  (How many CTAs
+    share a row's keys goes by the cache's rows, so sums have another order than over the
+    sequence's own rows alone, and both are held to fp64.)"""
+    rows, width = 560000, 4096
+    cache = torch.empty(rows, width, dtype=BF16, device="cuda")
+    case = ([70], [200], 2, 1, 64, True)
+    q, k, v, *_ = make(case)
+    kk, vv = cache[:, 128:192], cache[:, 4032:]
+    kk[-200:], vv[-200:] = k, v
+    starts, key_starts = ref.starts_of([70]), torch.tensor([rows - 200, rows], dtype=torch.int32, device="cuda")
+    o = api.attention(q, kk, vv, 64, starts=starts, key_starts=key_starts, lse=True)
+    check(case, o, q, k, v, [70], [200])
+    back = api.attention_backward(q, q, kk, vv, o["y"], o["lse"], 64, starts=starts, key_starts=key_starts)
+    want = ref.backward(q, q, k, v, 64, 1, True, 0.125)
+    for name, x, e in zip(("dq", "dk", "dv"), want[:3], want[3:]):
+        got = back[name][-x.shape[0]:].double()
+        assert ((got - x).abs() <= e + ref.HALF * (x.abs() + e)).all(), name
+        assert (back[name][:-x.shape[0]] == 0).all()
+
+
+def test_a_long_sequence():
+    """20,001 tokens of one head against fp64 at some of its rows, and in one piece with itself."""
+    case = ([20001], None, 1, 1, 64, True)
+    q, k, v, *_ = make(case)
+    o = api.attention(q, k, v, 64, lse=True)
+    for rows in (slice(0, 130), slice(9990, 10010), slice(19900, 20001)):
+        y, lse, e_y, e_lse = ref.forward(q[rows], k[:rows.stop], v[:rows.stop], 64, 1, True, 0.125)
+        assert ((o["y"][rows].double() - y).abs() <= e_y + ref.HALF * (y.abs() + e_y)).all()
+        assert ((o["lse"][rows].double() - lse).abs() <= e_lse).all()
+
+
 def test_streams_and_graphs():
     case = ([1, 1, 1, 300], [2000, 700, 129, 300], 8, 2, 128, True)
     q, k, v, starts, key_starts, nq, nk = make(case)
