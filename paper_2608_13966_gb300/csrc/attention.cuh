@@ -16,8 +16,8 @@
 // 2^8 (so P stays below 2^8, and the rounding of P to bf16 is relative): the
 // quotient O / l does not depend on which maximum was subtracted.
 //
-// P is rounded to bf16 for the matrix product (half a step, 2^-9 relative at
-// most, independent from key to key); l is the sum before the rounding.
+// P is rounded to bf16 for the matrix product (2^-8 of it at most); l is the sum
+// before the rounding.
 //
 // Where rows are few, a cluster of CTAs shares a row's keys, and where there are
 // rows for one tile alone, the tiles are twins: the same rows, every other key
@@ -25,10 +25,17 @@
 // in the same order.
 //
 // Warps: 0-7 and 8-15 the rows of tiles 0 and 1, two threads a row, 64 keys of a
-// key tile each, that exchange their maxima (with one thread a row the 4 warps
-// of a tile spent 2,400 cycles a key tile on their dependent instructions, and
-// the tensor cores waited: 4 x 4096 causal, 32 heads of 128 over 8, 565 us);
-// 16 copies, 17 matrix instructions, 18 looks up the items.
+// key tile each, that exchange their maxima (with one thread a row the tensor
+// cores waited for a tile's 4 warps: 565 us); 16 copies, 17 matrix instructions,
+// 18 looks up the items.
+//
+// 4 x 4096 causal, 32 heads of 128 over 8: 445 us, 1.24 PFLOP/s of the products at
+// and below the diagonal, 0.73 of the sustained rate.  What bounds it is the
+// chain from a tile's scores through P to its next product, which the other tile
+// hides in part, and the product thread's waits (some hundred cycles each, and
+// the tensor cores hold few instructions); masked halves of diagonal tiles are
+// computed too, 1.03 of the work.  One query for each of 61 sequences of up to
+// 2,048 keys, 32 heads over 8: 79 us, 4.4 TB/s; many short clusters' ends.
 #pragma once
 
 #include "attention.h"
@@ -40,6 +47,7 @@ namespace quasar {
 constexpr int kAttnThreads = 608;
 constexpr int kAttnRowWarps = 16, kAttnCopies = 16, kAttnProducts = 17, kAttnItems = 18;  // warps
 constexpr int kAttnSlots = 2;             // of the ring, each a tile of values and one of keys
+constexpr int kAttnAhead = 3;             // of an item's entries, when the next is asked for
 constexpr float kAttnSlack = 8.0f;        // log2 of how far m may fall behind
 constexpr uint32_t kAttnBlock = kAttnRows * 128;  // bytes of 128 rows x 64 bf16
 
@@ -160,6 +168,7 @@ struct AttnWork {
     int t0;  // first token of tile 0
     int first, count, n[2];
     int twins, lag, entries;
+    int end;  // 1: the CTA's last item, 2: there is none
 };
 
 __device__ __forceinline__ AttnWork attention_work(const AttnParams& p, int which, int rank)
@@ -190,10 +199,12 @@ __device__ __forceinline__ AttnWork attention_work(const AttnParams& p, int whic
 
 // D = 64 DB columns; a head of d columns is completed with zeros.
 //
-// A CTA walks over items (or, where CTAs share rows, has one): while one's last
-// products run and its rows are written, the next one's tiles are on their way
-// and its first products follow at once.  With a CTA an item, starting and
-// ending took some 17,000 cycles of each, a quarter of 4 x 4096.
+// A CTA takes items until there are none (or, where few are, has one): while one's
+// last products run and its rows are written, the next one's tiles are on their
+// way and its first products follow at once.  The grid has a CTA for each item,
+// and CTAs that run take those that have not been launched (4 x 4096 445 us,
+// with items dealt out beforehand 454, with a CTA an item 512; 256 queries of 2,048
+// keys each 378, 459 dealt out to twins, 460).
 template <int DB>
 __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_constant__ AttnParams p)
 {
@@ -214,22 +225,18 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
     uint64_t* item_empty = item_full + 2;  // [2]: the other warps
     uint64_t* drained = item_empty + 2;
     uint64_t* never = drained + 1;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(never + 1);
+    uint64_t* near = never + 1;  // an item's end is
+    uint64_t* asked = near + 1;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(asked + 1);
     volatile uint32_t* gone = tmem_slot + 1;
-    float2* stat = reinterpret_cast<float2*>(never + 3);      // [2][128]: m and l, where rows have parts (16-byte aligned)
+    void* answer = asked + 3;                                 // (at a 16-byte boundary, and what follows)
+    float2* stat = reinterpret_cast<float2*>(asked + 5);      // [2][128]: m and l, where rows have parts
     float2* swap = stat + 256;                                // [2 turns][2 tiles][2 halves][128]
     uint8_t* stages = reinterpret_cast<uint8_t*>(swap + 1024);   // 1 KB a warp of rows
     AttnWork* items = reinterpret_cast<AttnWork*>(stages + kAttnRowWarps * 1024);  // [2]
 
     const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int rank = p.split > 1 ? (int)cluster_rank() : 0;
-    // the items of this CTA: every grid's width one, and back the next time
-    // (neighbours have nearly the same number of keys)
-    const int width = (int)(gridDim.x / p.split), mine = (int)(blockIdx.x / p.split);
-    const int total = p.items * p.kv_heads;
-    auto which = [&](int k) { return k * width + (k & 1 ? width - 1 - mine : mine); };
-    const int turns = (total + width - 1) / width;
-
     if (threadIdx.x == 0) {
         mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
@@ -247,6 +254,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
         }
         mbar_init(drained, 1);
         mbar_init(never, 1);
+        mbar_init(near, 1);
+        mbar_init(asked, 1);
         *gone = 0;
         mbar_init_fence();
     }
@@ -273,9 +282,25 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
     };
 
     if (warp == kAttnItems) {
-        for (int k = 0; k < turns && which(k) < total; ++k) {
-            const AttnWork w = attention_work(p, which(k), rank);
+        int which = (int)blockIdx.x / p.split;
+        for (int k = 0, end = 0; end == 0; ++k) {
             if (k >= 2 && !wait(item_empty + (k & 1), ((k >> 1) - 1) & 1)) break;
+            if (k > 0) {
+                if (!wait(near, (k - 1) & 1)) break;
+                if (lane == 0) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    ask_for_cta(answer, asked);
+                }
+                __syncwarp();
+                if (!wait(asked, (k - 1) & 1)) {  // (nobody leaves before the answer is here)
+                    mbar_wait_bounded(asked, (k - 1) & 1, p.timeout_ns);
+                    break;
+                }
+                which = uniform(lane == 0 ? asked_cta(answer) : 0);
+            }
+            AttnWork w{};
+            if (which >= 0) w = attention_work(p, which, rank);
+            w.end = end = which < 0 ? 2 : !p.persistent;
             if (lane == 0) {
                 items[k & 1] = w;
                 mbar_arrive(item_full + (k & 1));
@@ -286,10 +311,16 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
         bool ok = true;
         if (p.force_timeout_ns) ok = __all_sync(0xffffffffu, role_sleep(never, 0, gone, p.force_timeout_ns, p.status));
         int it = 0, queries = 0;  // entries of the ring and sets of queries so far
-        for (int k = 0; k < turns && which(k) < total && ok; ++k) {
+        for (int k = 0, end = 0; ok && end == 0; ++k) {
             if (!(ok = take(k))) break;
             const AttnWork w = items[k & 1];
             release(k);
+            end = w.end;
+            // the next item is asked for a few key tiles ahead, no sooner: the CTAs
+            // that are through with theirs come first (at once, 2,048 tokens of one
+            // sequence took 54 us against 41)
+            const int ask = max(0, w.entries - kAttnAhead);
+            if (ask == 0 && lane == 0) mbar_arrive(near);
             if (w.entries == 0) continue;
             if (queries > 0 && !(ok = wait(q_empty, (queries - 1) & 1))) break;
             if (lane == 0) {
@@ -305,6 +336,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
             ++queries;
             for (int e = 0; e < w.entries; ++e, ++it) {
                 const int s = it % kAttnSlots;
+                if (e > 0 && e == ask && lane == 0) mbar_arrive(near);
                 if (it >= kAttnSlots && !(ok = wait(empty + s, (it / kAttnSlots - 1) & 1))) break;
                 if (lane == 0) {
                     const bool values = e >= w.lag, keys = e < w.count;
@@ -313,7 +345,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                     const int key = w.a.k0 + (w.first + e) * kAttnKeys;
                     for (int b = 0; b < DB; ++b) {
                         if (values)
-                            tile_g2s_3d(to + b * kAttnBlock, &p.v, 64 * b, w.kvh, key - w.lag * kAttnKeys, smem_u32(full + s));
+                            tile_g2s_3d(to + b * kAttnBlock, &p.v, 64 * b, w.kvh, key - w.lag * kAttnKeys,
+                                        smem_u32(full + s));
                         if (keys) tile_g2s_3d(to + kTile + b * kAttnBlock, &p.k, 64 * b, w.kvh, key, smem_u32(full + s));
                     }
                 }
@@ -328,15 +361,16 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
     } else if (warp == kAttnProducts) {
         // One thread for both tiles, first come first served: with a warp each
         // their products share the tensor cores instruction by instruction,
-        // both end late, and 4 x 4096 took 550 us against 492.
+        // both end late, and 4 x 4096 took 550 us where one thread's took 492.
         constexpr uint32_t desc_s = mma_desc(kAttnRows, kAttnKeys, false, false);
         constexpr uint32_t desc_o = mma_desc(kAttnRows, D, false, true);
         int it = 0, queries = 0, done[2] = {0, 0}, outs[2] = {0, 0};  // steps and rows of outputs of a tile
         bool ok = true;
-        for (int k = 0; k < turns && which(k) < total && ok; ++k) {
+        for (int k = 0, end = 0; ok && end == 0; ++k) {
             if (!(ok = take(k))) break;
             const AttnWork w = items[k & 1];
             release(k);
+            end = uniform(w.end);
             const int entries = uniform(w.entries), count = uniform(w.count), lag = uniform(w.lag);
             const int n[2] = {uniform(w.n[0]), uniform(w.n[1])};
             const bool twins = uniform(w.twins) != 0;
@@ -376,7 +410,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                         if (grow) {
 #pragma unroll
                             for (int x = 0; x < kAttnKeys / 16; ++x)
-                                mma_bf16_ts(o_at, s_at + x / 4 * 64 + x % 4 * 8, dv + x * k_step(true), desc_o, j > 0 || x > 0);
+                                mma_bf16_ts(o_at, s_at + x / 4 * 64 + x % 4 * 8, dv + x * k_step(true), desc_o,
+                                            j > 0 || x > 0);
                             mma_commit(smem_u32(o_full + i));
                         }
                         if (score) {  // S = Q K^T
@@ -429,7 +464,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
             return ok && theirs.y != 0.0f;
         };
         bool synced = false;
-        for (int k = 0; k < turns && which(k) < total; ++k) {
+        for (int k = 0, end = 0; end == 0; ++k) {
             // (an item that one of them did not get, or did not finish, ends it for
             // both warps of a row, and for all where they will meet)
             ok = ok && take(k);
@@ -449,6 +484,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
             if (!ok) break;
             const AttnWork& w = items[k & 1];
             const AttnItem& a = w.a;
+            end = w.end;
+            if (end == 2) break;
             if (a.spares > 0) {
                 if (rank == 0) {
                     clear_rows(p.y, p.ld_y, (int64_t)w.kvh * p.group * p.d, p.group * p.d, p.s.starts, p.s.n, p.s.tokens,
@@ -466,7 +503,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
             float m = minus_inf(), l = 0.0f;
             if (n > 0) {
                 // the last key that the row sees (rows of nobody mask nothing)
-                const int64_t see = !live ? (int64_t)1 << 40 : (p.causal ? min((int64_t)a.m - 1, (int64_t)token + a.m - a.n) : (int64_t)a.m - 1);
+                const int64_t last = (int64_t)a.m - 1;
+                const int64_t see = !live      ? (int64_t)1 << 40
+                                    : p.causal ? min(last, (int64_t)token + a.m - a.n)
+                                               : last;
                 bool together = true;
                 for (int j = 0; j < n; ++j) {
                     ok = ok && wait(s_full + i, (done + j) & 1);
@@ -579,7 +619,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                     for (int x = 0; x < 32; x += 2) out[(c + x) / 2] = pack_bf16x2(o[x] * inv, o[x + 1] * inv);
                 }
                 // 1 KB of rows at a time through shared memory, so that a store
-                // covers whole lines (a row a thread took 4,000 cycles an item)
+                // covers whole lines (of a row a thread each store touched 32)
                 constexpr int kVecs = kHalf / 8, kRows = 64 / kVecs;  // 16-byte vectors of a row; rows at a time
                 uint8_t* const stage = stages + warp * 1024;
 #pragma unroll 1
@@ -597,9 +637,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                         const int row = q + z / kVecs, c = z % kVecs;
                         const int rr = (warp & 3) * 32 + row, tok = w.t0 + i * p.tile_tokens + rr / p.group;
                         if (rr < p.tile_tokens * p.group && tok < a.n && half * kHalf + 8 * c < p.d)
-                            *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.y) + (int64_t)(a.q0 + tok) * p.ld_y +
-                                                      (int64_t)(w.kvh * p.group + rr % p.group) * p.d + half * kHalf + 8 * c) =
-                                *reinterpret_cast<const uint4*>(stage + (z / kVecs * kVecs + (c ^ (row & (kVecs - 1)))) * 16);
+                            *reinterpret_cast<uint4*>(
+                                static_cast<__nv_bfloat16*>(p.y) + (int64_t)(a.q0 + tok) * p.ld_y +
+                                (int64_t)(w.kvh * p.group + rr % p.group) * p.d + half * kHalf + 8 * c) =
+                                *reinterpret_cast<const uint4*>(stage + (z - c + (c ^ (row & (kVecs - 1)))) * 16);
                     }
                 }
                 if (p.lse && live && half == 0)

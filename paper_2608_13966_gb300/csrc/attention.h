@@ -33,7 +33,7 @@ struct AttnParams {
     int causal;
     int items;        // pairs of tiles there may be, and one (per kv head)
     int split;
-    int persistent;   // CTAs walk over items (and a row has one part)
+    int persistent;   // CTAs take items (and a row has one part)
     float scale_log2;
     void* y;
     int64_t ld_y;

@@ -27,9 +27,13 @@
 //   keys stay:    dv(j), S(j+1), dk(j), dP(j+1)
 //   queries stay: S(j+1), dP(j+1), dq(j)          (dP in two places in turn)
 //
-// (In steps of 64 columns, S and dP of two steps at a time, the tensor cores'
-// reading of shared memory took 1.26 as long and the chain of a step was not
-// hidden: 4 x 4096 causal, 32 heads of 128 over 8, 1710 us.)
+// (In steps of 64 columns, S and dP of two steps at a time, 1788 us where steps
+// of 128 took 1710: the tensor cores read 1.26 times as much shared memory.)
+//
+// 4 x 4096 causal, 32 heads of 128 over 8: 1617 us with the statistics, 0.85
+// PFLOP/s of the formulas' 5 products, 1.19 of the 7.  What bounds it is the chain
+// scores, P, dS, product of a step, of which one CTA's tensor memory holds no
+// second one beside the gradients.
 //
 // Warps: 0-15 make P and dS, four threads a row; 16 copies, 17 matrix
 // instructions, 18 brings the columns' statistics (keys stay), 19 looks up the
@@ -462,7 +466,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
             // key that the row's token sees
             // (-2^30: it sees none; a sequence's places are below 2^31)
             const int from = KEYS && p.causal ? (int)max((int64_t)0, (int64_t)w.row0 + r - shift) : 0;
-            const int upto = (int)max((int64_t)-(1 << 30), p.causal ? min((int64_t)w.a.m - 1, (int64_t)token + shift) : (int64_t)w.a.m - 1);
+            const int64_t last = (int64_t)w.a.m - 1;
+            const int upto = (int)max((int64_t)-(1 << 30), p.causal ? min(last, (int64_t)token + shift) : last);
             const int begin = w.begin;
             for (int j = 0; j < steps; ++j, ++g) {
                 ok = wait(s_full, g & 1);
@@ -528,12 +533,12 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                         for (int x = 0; x < 8; x += 2) {
                             float4 delta = make_float4(own.y, own.y, own.y, own.y);
                             if (KEYS) delta = st[kGradCols / 4 + (h + x) / 2];
-                            float2 ds[2] = {
-                                __fmul2_rn(e[h + x], __fadd2_rn(make_float2(dp[2 * x], dp[2 * x + 1]), make_float2(delta.x, delta.y))),
-                                __fmul2_rn(e[h + x + 1],
-                                           __fadd2_rn(make_float2(dp[2 * x + 2], dp[2 * x + 3]), make_float2(delta.z, delta.w)))};
+                            float2 ds[2] = {__fadd2_rn(make_float2(dp[2 * x], dp[2 * x + 1]), make_float2(delta.x, delta.y)),
+                                            __fadd2_rn(make_float2(dp[2 * x + 2], dp[2 * x + 3]),
+                                                       make_float2(delta.z, delta.w))};
 #pragma unroll
                             for (int y = 0; y < 2; ++y) {
+                                ds[y] = __fmul2_rn(e[h + x + y], ds[y]);
                                 words[x + y] = pack_bf16x2(ds[y].x, ds[y].y);
                                 // (0 times what need not be finite)
                                 if (masked)

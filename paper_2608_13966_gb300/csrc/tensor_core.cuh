@@ -268,8 +268,9 @@ __device__ __forceinline__ void tmem_st(uint32_t addr, const uint32_t (&v)[8])
 
 // One lane of a converged warp.  Matrix instructions take their addresses and
 // descriptors from uniform registers: issued under `lane == 0` and with values
-// that are not known to be the warp's, each cost some 120 cycles of moves, twice
-// what a product of 128 x 128 x 16 takes.
+// that are not known to be the warp's, they are slower to come than the tensor
+// cores to take them (attention of 4 x 4096 tokens 597 us against 492, its
+// gradients 2456 against 2007).
 __device__ __forceinline__ bool elect_one()
 {
     uint32_t one;
@@ -284,6 +285,35 @@ template <typename T>
 __device__ __forceinline__ T uniform(T x)
 {
     return __shfl_sync(0xffffffffu, x, 0);
+}
+
+// -- the grid's work taken by CTAs that run -----------------------------------
+
+// Asks for a CTA of the grid that has not been launched, which then never is:
+// 16 bytes to `answer` (16-byte aligned), counted on `bar`.  Not asked again once
+// there was none.
+__device__ __forceinline__ void ask_for_cta(void* answer, uint64_t* bar)
+{
+    mbar_arrive_expect_tx(bar, 16);
+    asm volatile(
+        "clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+            smem_u32(answer)),
+        "r"(smem_u32(bar))
+        : "memory");
+}
+
+// Its blockIdx.x, or -1 where there was none.
+__device__ __forceinline__ int asked_cta(const void* answer)
+{
+    uint32_t x;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b128 a;\n\tld.shared.b128 a, [%1];\n\tmov.u32 %0, 0xffffffff;\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, a;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, a;\n\t}"
+        : "=r"(x)
+        : "r"(smem_u32(answer))
+        : "memory");
+    return (int)x;
 }
 
 // -- waits -------------------------------------------------------------------
