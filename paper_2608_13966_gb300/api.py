@@ -826,7 +826,7 @@ def attention_backward(dy, q, k, v, y, lse, head_dim, *, starts=None, key_starts
     if not lse.is_contiguous():
         raise ValueError("lse must be contiguous")
     if out is not None:
-        if len(out) != 3:
+        if not isinstance(out, (tuple, list)) or len(out) != 3:
             raise ValueError("out must be (dq, dk, dv)")
         for name, wanted, t, rows, width in (("dq", dq, out[0], tokens, cols),
                                              ("dk", dkv, out[1], keys, kv_cols),

@@ -21,21 +21,22 @@
 //
 // Where rows are few, a cluster of CTAs shares a row's keys, and where there are
 // rows for one tile alone, the tiles are twins: the same rows, every other key
-// tile each.  The parts are joined through (distributed) shared memory, always
-// in the same order.
+// tile each.  Twins are joined in tensor memory, the parts of a cluster's CTAs
+// through distributed shared memory, always in the same order.
 //
 // Warps: 0-7 and 8-15 the rows of tiles 0 and 1, two threads a row, 64 keys of a
 // key tile each, that exchange their maxima (with one thread a row the tensor
 // cores waited for a tile's 4 warps: 565 us); 16 copies, 17 matrix instructions,
 // 18 looks up the items.
 //
-// 4 x 4096 causal, 32 heads of 128 over 8: 445 us, 1.24 PFLOP/s of the products at
-// and below the diagonal, 0.73 of the sustained rate.  What bounds it is the
+// 4 x 4096 causal, 32 heads of 128 over 8: 440 us, 1.25 PFLOP/s of the products at
+// and below the diagonal, 0.74 of the sustained rate.  What bounds it is the
 // chain from a tile's scores through P to its next product, which the other tile
 // hides in part, and the product thread's waits (some hundred cycles each, and
 // the tensor cores hold few instructions); masked halves of diagonal tiles are
 // computed too, 1.03 of the work.  One query for each of 61 sequences of up to
-// 2,048 keys, 32 heads over 8: 79 us, 4.4 TB/s; many short clusters' ends.
+// 2,048 keys, 32 heads over 8: 79 us, 4.5 TB/s, bound by the last of 3.2 items an SM
+// (256 sequences of 2,048 keys 346 us, 6.2 TB/s).
 #pragma once
 
 #include "attention.h"
@@ -181,7 +182,7 @@ __device__ __forceinline__ AttnWork attention_work(const AttnParams& p, int whic
     if (w.a.spares > 0) return w;
     w.n[0] = key_tiles(w.a, w.t0, w.t0 + p.tile_tokens, p.causal);
     w.n[1] = key_tiles(w.a, w.t0 + p.tile_tokens, w.t0 + 2 * p.tile_tokens, p.causal);
-    w.twins = !p.persistent && w.a.n - w.t0 <= p.tile_tokens && w.n[0] > 1;
+    w.twins = w.a.n - w.t0 <= p.tile_tokens && w.n[0] > 1;
     const int most = max(w.n[0], w.n[1]);
     w.first = (int)((int64_t)most * rank / p.split);
     w.count = (int)((int64_t)most * (rank + 1) / p.split) - w.first;
@@ -202,9 +203,10 @@ __device__ __forceinline__ AttnWork attention_work(const AttnParams& p, int whic
 // A CTA takes items until there are none (or, where few are, has one): while one's
 // last products run and its rows are written, the next one's tiles are on their
 // way and its first products follow at once.  The grid has a CTA for each item,
-// and CTAs that run take those that have not been launched (4 x 4096 445 us,
-// with items dealt out beforehand 454, with a CTA an item 512; 256 queries of 2,048
-// keys each 378, 459 dealt out to twins, 460).
+// and CTAs that run take those that have not been launched (4 x 4096 440 us; with
+// items dealt out beforehand 454, though one sequence of 2,048 40 as now; with a CTA
+// an item 512; 256 queries of 2,048 keys 346, with a CTA an item 460, without
+// twins 378).
 template <int DB>
 __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_constant__ AttnParams p)
 {
@@ -226,7 +228,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
     uint64_t* drained = item_empty + 2;
     uint64_t* never = drained + 1;
     uint64_t* near = never + 1;  // an item's end is
-    uint64_t* asked = near + 1;
+    uint64_t* join = near + 1;   // [4]: twin 1 of 32 rows is done
+    uint64_t* asked = join + 4;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(asked + 1);
     volatile uint32_t* gone = tmem_slot + 1;
     void* answer = asked + 3;                                 // (at a 16-byte boundary, and what follows)
@@ -256,6 +259,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
         mbar_init(never, 1);
         mbar_init(near, 1);
         mbar_init(asked, 1);
+        for (int i = 0; i < 4; ++i) mbar_init(join + i, 1);
         *gone = 0;
         mbar_init_fence();
     }
@@ -449,7 +453,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
         const int i = warp >> 3 & 1, half = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t s_at = lanes + i * 128 + half * 64, o_at = lanes + 256 + i * 128 + half * kHalf;
-        int done = 0, swaps = 0;  // steps and exchanges so far
+        int done = 0, swaps = 0, joins = 0;  // steps, exchanges and joined twins so far
         uint32_t agreed = 0;
         bool ok = true;
         // Both warps of a row come to this barrier at the same places, whatever
@@ -601,8 +605,42 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                 }
                 done += n;
             }
-            const bool whole = p.split == 1 && !w.twins;  // the row has one part
-            if (whole && ok && any_live) {
+            const bool whole = p.split == 1;  // the row has no parts in other CTAs
+            const bool joined = whole && w.twins;
+            if (joined) {  // twin 1 leaves its sums to twin 0, where they lie
+                if (i == 1) {
+                    if (half == 0) {
+                        stat[128 + r] = make_float2(m, l);
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0 && ok) mbar_arrive(join + (warp & 3));
+                    }
+                } else {
+                    ok = ok && wait(join + (warp & 3), joins & 1);
+                    tc_fence_after();
+                    if (ok && any_live) {
+                        const float2 twin = stat[128 + r];
+                        const float top = fmaxf(m, twin.x), shift = top == minus_inf() ? 0.0f : top;
+                        const float mine = exp2_fast(m - shift), theirs = exp2_fast(twin.x - shift);
+                        const bool none = l == 0.0f, no_twin = twin.y == 0.0f;  // (what is not seen left nothing)
+#pragma unroll 1
+                        for (int c = 0; c < kHalf; c += 16) {
+                            float o[16], z[16];
+                            tmem_ld16(o_at + c, o);
+                            tmem_ld16(o_at + 128 + c, z);
+#pragma unroll
+                            for (int x = 0; x < 16; ++x)
+                                o[x] = fmaf(theirs, no_twin ? 0.0f : z[x], mine * (none ? 0.0f : o[x]));
+                            tmem_st16(o_at + c, o);
+                        }
+                        tmem_wait_st();
+                        l = fmaf(mine, l, theirs * twin.y);
+                        m = top;
+                    }
+                }
+                ++joins;
+            }
+            if (whole && ok && any_live && !(joined && i == 1)) {
                 const float inv = l == 0.0f ? 0.0f : 1.0f / l;
                 uint32_t out[kHalf / 2];
 #pragma unroll
@@ -649,7 +687,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
             if (n > 0) {  // the outputs are read: the next item's may grow
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(o_empty + i);
+                if (lane == 0 && !(joined && i == 1)) {
+                    mbar_arrive(o_empty + i);
+                    if (joined) mbar_arrive(o_empty + 1);
+                }
             }
             if (!whole) {
                 // (one item, then: every product of this CTA is done, and the
@@ -670,17 +711,11 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                                 make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
                     }
                 }
-                if (p.split > 1) {
-                    cluster_sync();
-                    synced = true;
-                } else {
-                    asm volatile("bar.sync 9, 512;" ::: "memory");
-                }
+                cluster_sync();
+                synced = true;
                 constexpr int kVecs = D / 4, kMany = kAttnRowWarps * 32;
                 const int rows = p.tile_tokens * p.group;
-                auto peer = [&](const void* x, int q) {
-                    return p.split > 1 ? peer_addr(smem_u32(x), (uint32_t)q) : smem_u32(x);
-                };
+                auto peer = [&](const void* x, int q) { return peer_addr(smem_u32(x), (uint32_t)q); };
                 for (int x = rank * kMany + (int)threadIdx.x; x < (w.twins ? 1 : 2) * rows * kVecs; x += p.split * kMany) {
                     const int tile = x / (rows * kVecs), row = x / kVecs % rows, c = x % kVecs;
                     const int tok = w.t0 + tile * p.tile_tokens + row / p.group;

@@ -98,13 +98,13 @@ quasar_status quasar_attention(const void* q, int64_t ld_q, const void* k, int64
     const int64_t items = tokens / (2 * p.tile_tokens) + sequences + 1;
     if (items * kv_heads * kAttnMostSplit > (int64_t(1) << 31) - 1) return QUASAR_ERR_UNSUPPORTED;
     p.items = (int)items;
-    const int64_t work = std::max<int64_t>(1, items - 1) * kv_heads;
+    const int64_t work = std::max<int64_t>(1, items - 1) * kv_heads;  // (the one more aside)
     const int64_t tiles = keys / std::max<int64_t>(1, sequences) / kAttnKeys;
     p.split = 1;
     const void* fn = attention_kernel(p.d);
     const size_t smem = attention_smem(p.d);
     // more items than SMs: their CTAs take them from one another (not so, 16 x 512
-    // tokens 107 us against 78, 512 queries of 512 keys 472 against 246).  Fewer:
+    // tokens 107 us against 78, 512 queries of 512 keys 472 against 229).  Fewer:
     // as many CTAs share one's keys as fill the device, four key tiles each (two:
     // two queries of 1,024 keys 22.7 us against 12.3; eight: 13.9)
     p.persistent = work > n_sm;
@@ -221,7 +221,7 @@ quasar_status quasar_attention_backward(const void* dy, int64_t ld_dy, const voi
             (st = map(false, dy, ld_dy, p.group, p.tile_tokens, &p.x2)) != QUASAR_OK ||
             (st = map(true, k, ld_k, 1, kGradCols, &p.z1)) != QUASAR_OK ||
             (st = map(true, v, ld_v, 1, kGradCols, &p.z2)) != QUASAR_OK ||
-            (st = launch(attention_grad_kernel(p.d, false), &p, dim3((unsigned)std::min<int64_t>(n_sm, query_items * kv_heads)),
+            (st = launch(attention_grad_kernel(p.d, false), &p, dim3((unsigned)(query_items * kv_heads)),
                          attention_grad_threads(), 1, smem, stream)) != QUASAR_OK)
             return st;
     }

@@ -30,7 +30,7 @@
 // (In steps of 64 columns, S and dP of two steps at a time, 1788 us where steps
 // of 128 took 1710: the tensor cores read 1.26 times as much shared memory.)
 //
-// 4 x 4096 causal, 32 heads of 128 over 8: 1617 us with the statistics, 0.85
+// 4 x 4096 causal, 32 heads of 128 over 8: 1620 us with the statistics, 0.85
 // PFLOP/s of the formulas' 5 products, 1.19 of the 7.  What bounds it is the chain
 // scores, P, dS, product of a step, of which one CTA's tensor memory holds no
 // second one beside the gradients.
@@ -46,6 +46,7 @@ namespace quasar {
 
 constexpr int kGradThreads = 640;
 constexpr int kGradRowWarps = 16, kGradCopies = 16, kGradProducts = 17, kGradStats = 18, kGradItems = 19;  // warps
+constexpr int kGradAhead = 3;  // of an item's steps, when the next is asked for
 constexpr int kGradSlots1 = 3, kGradSlots2 = 2;  // of the rings of z1 (which waits for the step's end) and z2
 
 // The rows' statistics: 8 or 16 threads a (token, head) pair.
@@ -88,6 +89,7 @@ struct GradWork {
     int row0;   // first key, or token, of the rows
     int begin;  // first token, or key, of the steps
     int steps;
+    int end;    // there is no item
 };
 
 template <bool KEYS>
@@ -114,11 +116,14 @@ __device__ __forceinline__ GradWork grad_work(const AttnGradParams& p, int which
 __host__ __device__ constexpr size_t attention_grad_bytes(int blocks)
 {
     return (size_t)(2 + kGradSlots1 + kGradSlots2) * blocks * kAttnBlock + 2 * 2 * kGradCols * 4 +
-           (2 + 2 * kGradSlots1 + 2 * kGradSlots2 + 2 * 3 + 2 + 2 + 4 + 3) * 8 + 2 * sizeof(GradWork);
+           (2 + 2 * kGradSlots1 + 2 * kGradSlots2 + 2 * 3 + 2 + 2 + 4 + 8) * 8 + 2 * sizeof(GradWork);
 }
 
-// A CTA an SM walks over the items: the next one's tiles are on their way, and
-// its first scores are made, while the gradients of one are written.
+// The grid has a CTA for each item, and CTAs that run take those that have not
+// been launched: the next one's tiles are on their way, and its first scores are
+// made, while the gradients of one are written (with items dealt out beforehand
+// for queries and a CTA an item for keys, 13 sequences of up to 501 tokens, 12 heads
+// of 64, took 64 us against 58; 4 x 4096 the same).
 template <int DB, bool KEYS>
 __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid_constant__ AttnGradParams p)
 {
@@ -149,15 +154,14 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
     uint64_t* item_empty = item_full + 2;       // [2]: the warps that take items
     uint64_t* drained = item_empty + 2;
     uint64_t* never = drained + 1;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(never + 1);
+    uint64_t* near = never + 1;                 // an item's end is
+    uint64_t* asked = near + 1;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(asked + 1);
     volatile uint32_t* gone = tmem_slot + 1;
-    GradWork* items = reinterpret_cast<GradWork*>(never + 2);  // [2]
+    void* answer = asked + 2 + (asked - x_full & 1);  // (x_full is at a 16-byte boundary)
+    GradWork* items = reinterpret_cast<GradWork*>(asked + 5);  // [2]
 
     const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
-    // the items of this CTA: every grid's width one, and back the next time
-    const int width = (int)gridDim.x, total = p.items * p.kv_heads, turns = (total + width - 1) / width;
-    auto which = [&](int k) { return k * width + (k & 1 ? width - 1 - (int)blockIdx.x : (int)blockIdx.x); };
-
     uint32_t given;
     asm volatile("mov.u32 %0, %%dynamic_smem_size;" : "=r"(given));
     if (smem + attention_grad_bytes(DB) > smem_raw + given) {  // (it starts at a multiple of 1024, as declared)
@@ -181,6 +185,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
         mbar_init(acc_empty, kGradRowWarps);
         mbar_init(drained, 1);
         mbar_init(never, 1);
+        mbar_init(near, 1);
+        mbar_init(asked, 1);
         *gone = 0;
         mbar_init_fence();
     }
@@ -219,9 +225,25 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
     static_assert(kGradSlots2 == 2, "z2 of a step is in place g & 1");
 
     if (warp == kGradItems) {
-        for (int k = 0; k < turns && which(k) < total; ++k) {
-            const GradWork w = grad_work<KEYS>(p, which(k));
+        int which = (int)blockIdx.x;
+        for (int k = 0; which >= 0; ++k) {
             if (k >= 2 && !wait(item_empty + (k & 1), ((k >> 1) - 1) & 1)) break;
+            if (k > 0) {
+                if (!wait(near, (k - 1) & 1)) break;
+                if (lane == 0) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    ask_for_cta(answer, asked);
+                }
+                __syncwarp();
+                if (!wait(asked, (k - 1) & 1)) {  // (nobody leaves before the answer is here)
+                    mbar_wait_bounded(asked, (k - 1) & 1, p.timeout_ns);
+                    break;
+                }
+                which = uniform(lane == 0 ? asked_cta(answer) : 0);
+            }
+            GradWork w{};
+            if (which >= 0) w = grad_work<KEYS>(p, which);
+            w.end = which < 0;
             if (lane == 0) {
                 items[k & 1] = w;
                 mbar_arrive(item_full + (k & 1));
@@ -235,10 +257,15 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
         Place z1{0, 1}, z2{0, 1};            // (the phase of a place's release before)
         const uint32_t x_bytes = 2 * DB * 128 * (KEYS ? kAttnRows : (uint32_t)(p.tile_tokens * p.group));
         const uint32_t z_bytes = DB * 128 * (KEYS ? (uint32_t)(p.tile_tokens * p.group) : kGradCols);
-        for (int k = 0; k < turns && which(k) < total && ok; ++k) {
+        for (int k = 0, end = 0; ok && !end; ++k) {
             if (!(ok = take(k))) break;
             const GradWork w = items[k & 1];
             release(k);
+            end = w.end;
+            // the next item is asked for a few steps ahead, no sooner: the CTAs that
+            // are through with theirs come first
+            const int ask = max(0, w.steps - kGradAhead);
+            if (ask == 0 && lane == 0) mbar_arrive(near);
             if (w.steps == 0) continue;
             if (sets > 0 && !(ok = wait(x_empty, (sets - 1) & 1))) break;
             ++sets;
@@ -252,6 +279,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
             int at = (KEYS ? w.a.q0 : w.a.k0) + w.begin;
             const int head = KEYS ? w.kvh * p.group : w.kvh;
             for (int j = 0; j < w.steps && ok; ++j, at += by) {
+                if (j > 0 && j == ask && lane == 0) mbar_arrive(near);
                 if (sent1 >= kGradSlots1 && !(ok = wait(empty1 + z1.slot, z1.phase))) break;
                 if (lane == 0) {
                     mbar_arrive_expect_tx(full1 + z1.slot, z_bytes);
@@ -324,10 +352,11 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
         Place z1{0, 0}, z2{0, 0};  // of the next S and dP
         int old1 = 0, sets = 0, g = 0;  // z1 of the step that ends; items with steps; steps so far
         bool ok = true;
-        for (int k = 0; k < turns && which(k) < total && ok; ++k) {
+        for (int k = 0, end = 0; ok && !end; ++k) {
             if (!(ok = take(k))) break;
             const GradWork w = items[k & 1];
             release(k);
+            end = uniform(w.end);
             const int steps = uniform(w.steps);
             if (steps == 0) continue;
             // columns of a step that are the sequence's
@@ -403,10 +432,11 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                 place[q] = (lane + 32 * q) / p.group * p.heads + (lane + 32 * q) % p.group;
             bool ok = true;
             int g = 0;
-            for (int k = 0; k < turns && which(k) < total && ok; ++k) {
+            for (int k = 0, end = 0; ok && !end; ++k) {
                 if (!(ok = take(k))) break;
                 const GradWork w = items[k & 1];
                 release(k);
+                end = w.end;
                 for (int j = 0; j < w.steps; ++j, ++g) {
                     const int64_t at = (int64_t)(w.a.q0 + w.begin + j * by) * p.heads + w.kvh * p.group;
                     const int cols = min(by, w.a.n - w.begin - j * by) * p.group;
@@ -435,9 +465,10 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
         const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
         bool ok = true;
         int sets = 0, g = 0;
-        for (int k = 0; k < turns && which(k) < total && ok; ++k) {
+        for (int k = 0; ok; ++k) {
             if (!(ok = take(k))) break;
             const GradWork& w = items[k & 1];
+            if (w.end) break;
             if (w.a.spares > 0) {
                 constexpr int kMany = kGradRowWarps * 32;
                 if (KEYS) {
