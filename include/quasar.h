@@ -675,7 +675,7 @@ quasar_status quasar_layer_norm_backward(const void* dy, quasar_dtype dy_dtype, 
  *   causal    1: a sequence's last token sees its last key, the token before it
  *             one key less, and so on (so one token sees every key); 0: every
  *             token sees every key of its sequence.
- *   scale     above 0.
+ *   scale     above 0, and finite times log2(e) too.
  *   y         [tokens, heads x head_dim] bf16 (written).
  *   lse       [tokens, heads] fp32: log sum exp of the scaled scores, for the
  *             backward call; or NULL.

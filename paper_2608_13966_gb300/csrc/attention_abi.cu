@@ -22,6 +22,8 @@ namespace {
 
 using namespace quasar;
 
+constexpr float kLog2e = 1.44269504f;
+
 // [rows, heads, d] bf16 as it lies in columns of a matrix: tiles of 64 columns
 // of a head, `box_heads` heads and `box_rows` rows.
 quasar_status head_map(const void* p, int64_t rows, int64_t heads, int64_t d, int64_t ld, int box_heads, int box_rows,
@@ -66,7 +68,7 @@ quasar_status quasar_attention(const void* q, int64_t ld_q, const void* k, int64
     if (!valid_operand(q, tokens, heads * head_dim, ld_q) || !valid_operand(k, keys, kv_heads * head_dim, ld_k) ||
         !valid_operand(v, keys, kv_heads * head_dim, ld_v) || !valid_operand(y, tokens, heads * head_dim, ld_y))
         return QUASAR_ERR_INVALID_ARG;
-    if (!(scale > 0.0f) || !std::isfinite(scale) || (causal != 0 && causal != 1) || !aligned(lse, 4))
+    if (!(scale > 0.0f) || !std::isfinite(scale * kLog2e) || (causal != 0 && causal != 1) || !aligned(lse, 4))
         return QUASAR_ERR_INVALID_ARG;
     if (head_dim > 128 || heads / kv_heads > kAttnRows) return QUASAR_ERR_UNSUPPORTED;
     if (tokens == 0) return QUASAR_OK;
@@ -87,7 +89,7 @@ quasar_status quasar_attention(const void* q, int64_t ld_q, const void* k, int64
     p.d = (int)head_dim;
     p.tile_tokens = kAttnRows / p.group;
     p.causal = causal;
-    p.scale_log2 = scale * 1.44269504f;
+    p.scale_log2 = scale * kLog2e;
     p.y = y;
     p.ld_y = ld_y;
     p.lse = lse;
@@ -107,8 +109,14 @@ quasar_status quasar_attention(const void* q, int64_t ld_q, const void* k, int64
     // tokens 107 us against 78, 512 queries of 512 keys 472 against 229).  Fewer:
     // as many CTAs share one's keys as fill the device, four key tiles each (two:
     // two queries of 1,024 keys 22.7 us against 12.3; eight: 13.9)
-    p.persistent = work > n_sm;
-    while (p.split < kAttnMostSplit && work * p.split < n_sm && tiles >= 4 * p.split) p.split *= 2;
+    // The tensor core cuts off what a product has below 2^-25 of the sum so far, of
+    // many keys alike a little each time: values of 1.99 over 2^20 keys came out
+    // 0.8% low, over 2^22 3.9%.  From 2^19 keys a sequence on (on average), always as many CTAs as
+    // there may be, with a sum each (2,048 tokens over 2^18 keys would take 7.7 ms
+    // against 6.9).
+    const bool far = tiles >= kAttnFarTiles;
+    p.persistent = work > n_sm && !far;
+    while (p.split < kAttnMostSplit && (far || work * p.split < n_sm) && tiles >= 4 * p.split) p.split *= 2;
     const int64_t ctas = items * kv_heads * p.split;
     if ((st = head_map(q, tokens, heads, head_dim, ld_q, p.group, p.tile_tokens, &p.q)) != QUASAR_OK) return st;
     // (without keys no copy is made: any valid map will do)
@@ -148,7 +156,7 @@ quasar_status quasar_attention_backward(const void* dy, int64_t ld_dy, const voi
     if ((dq && !valid_operand(dq, tokens, cols, ld_dq)) ||
         (dk && (!valid_operand(dk, keys, kv_cols, ld_dk) || !valid_operand(dv, keys, kv_cols, ld_dv))))
         return QUASAR_ERR_INVALID_ARG;
-    if (!(scale > 0.0f) || !std::isfinite(scale) || (causal != 0 && causal != 1)) return QUASAR_ERR_INVALID_ARG;
+    if (!(scale > 0.0f) || !std::isfinite(scale * kLog2e) || (causal != 0 && causal != 1)) return QUASAR_ERR_INVALID_ARG;
     if (!aligned(lse, 4) || (tokens > 0 && !lse)) return QUASAR_ERR_INVALID_ARG;
     if (head_dim > 128 || heads / kv_heads > kAttnRows) return QUASAR_ERR_UNSUPPORTED;
     const int64_t need = 8 * tokens * heads;
@@ -179,7 +187,7 @@ quasar_status quasar_attention_backward(const void* dy, int64_t ld_dy, const voi
     p.tile_tokens = kAttnRows / p.group;
     p.causal = causal;
     p.scale = scale;
-    p.scale_log2 = scale * 1.44269504f;
+    p.scale_log2 = scale * kLog2e;
     p.stats = static_cast<const float2*>(workspace);
     p.timeout_ns = host_timeout_ns();
     p.force_timeout_ns = host_forced_timeout_ns();

@@ -207,6 +207,12 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
         const bool ok = role_sleep(bar, parity, gone, p.timeout_ns, p.status);
         return __all_sync(0xffffffffu, ok);
     };
+    // (an item of many keys may take longer than any one step of it may; the other
+    // warps' waits end this one too)
+    auto wait_long = [&](uint64_t* bar, uint32_t parity) {
+        const bool ok = role_sleep(bar, parity, gone, 64 * p.timeout_ns, p.status);
+        return __all_sync(0xffffffffu, ok);
+    };
     // item k, once it is known; its place is for k + 2 when all have let it go
     auto take = [&](int k) { return wait(item_full + (k & 1), (k >> 1) & 1); };
     auto release = [&](int k) {
@@ -227,9 +233,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
     if (warp == kGradItems) {
         int which = (int)blockIdx.x;
         for (int k = 0; which >= 0; ++k) {
-            if (k >= 2 && !wait(item_empty + (k & 1), ((k >> 1) - 1) & 1)) break;
+            if (k >= 2 && !wait_long(item_empty + (k & 1), ((k >> 1) - 1) & 1)) break;
             if (k > 0) {
-                if (!wait(near, (k - 1) & 1)) break;
+                if (!wait_long(near, (k - 1) & 1)) break;
                 if (lane == 0) {
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     ask_for_cta(answer, asked);

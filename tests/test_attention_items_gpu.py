@@ -1,4 +1,6 @@
 """Attention of more items than the device holds at a time: CTAs take them from those not launched."""
+import math
+
 import pytest
 import torch
 
@@ -76,6 +78,34 @@ def test_only_their_columns_are_written():
         inner(whole)[:] = 7.25
         assert (whole == 7.25).all()
     assert torch.equal(lse[1:-1], o["lse"]) and (lse[0] == 7.25).all() and (lse[-1] == 7.25).all()
+
+
+def test_an_item_longer_than_a_wait():
+    """One of 600 sequences has 2.6e8 keys, which take a CTA over a second: that is no time-out.  With
+    q of zeros and values of ones for 2^20 keys and zeros behind, every sum is exact: lse is
+    log(2.6e8) but for some roundings of 20, and y their share, rounded to bf16 (twice: as a quotient,
+    and as stored).  The others have a token and a key each."""
+    far, tokens, others = 260_000_000, 256, 599
+    k = torch.zeros(far + others, 8, dtype=BF16, device="cuda")
+    k[:1 << 20] = 1
+    k[far:] = 3
+    q = torch.zeros(tokens + others, 8, dtype=BF16, device="cuda")
+    starts, key_starts = ref.starts_of([tokens] + [1] * others), ref.starts_of([far] + [1] * others)
+    o = api.attention(q, k, k, 8, starts=starts, key_starts=key_starts, causal=False, lse=True)
+    api.check_device()
+    assert ((o["lse"][:tokens].double() - math.log(far)).abs() <= 8 * 20 * 2.0 ** -24).all()
+    want = (1 << 20) / far
+    assert ((o["y"][:tokens].double() - want).abs() <= (2.0 ** -8 + 2.0 ** -20) * want).all()
+    assert (o["y"][tokens:] == 3).all() and (o["lse"][tokens:] == 0).all()
+
+
+def test_far_more_keys_than_a_sum_holds():
+    """2^21 keys alike, of values with eight bits: what the tensor core cuts off of each stays below
+    the rounding of y."""
+    v = torch.full((1 << 21, 8), 255 / 128, dtype=BF16, device="cuda")
+    for tokens in (3, 152 * 256):
+        y = api.attention(torch.zeros(tokens, 8, dtype=BF16, device="cuda"), v, v, 8, causal=False)["y"]
+        assert ((y.double() - 255 / 128).abs() <= 2.0 ** -8 * 2).all()
 
 
 def test_a_wait_that_runs_out_is_reported():

@@ -167,6 +167,7 @@ SHARED = [
     (dict(scale=0.0), INVALID),
     (dict(scale=-1.0), INVALID),
     (dict(scale=INF), INVALID),
+    (dict(scale=3e38), INVALID),  # not finite in bits
     (dict(scale=NAN), INVALID),
     (dict(lse=G + 2), INVALID),
     (dict(tokens=-1), INVALID),
