@@ -47,7 +47,10 @@ namespace quasar {
 
 constexpr int kAttnThreads = 608;
 constexpr int kAttnRowWarps = 16, kAttnCopies = 16, kAttnProducts = 17, kAttnItems = 18;  // warps
-constexpr int kAttnSlots = 2;             // of the ring, each a tile of values and one of keys
+// Places of the ring, each a tile of values and one of keys: 128 KB (heads of 64 with
+// two: 128 queries of 2,048 keys, 32 heads over 8, 125 us against 104).
+template <int DB>
+constexpr int kAttnSlots = DB == 1 ? 4 : 2;
 constexpr int kAttnAhead = 3;             // of an item's entries, when the next is asked for
 constexpr float kAttnSlack = 8.0f;        // log2 of how far m may fall behind
 constexpr uint32_t kAttnBlock = kAttnRows * 128;  // bytes of 128 rows x 64 bf16
@@ -212,14 +215,15 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
 {
     constexpr int D = 64 * DB;
     constexpr uint32_t kTile = DB * kAttnBlock;  // bytes of a tile of q, k or v
+    constexpr int kSlots = kAttnSlots<DB>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* ring = smem + 2 * kTile;
-    uint64_t* q_full = reinterpret_cast<uint64_t*>(ring + kAttnSlots * 2 * kTile);
+    uint64_t* q_full = reinterpret_cast<uint64_t*>(ring + kSlots * 2 * kTile);
     uint64_t* q_empty = q_full + 1;
     uint64_t* full = q_empty + 1;          // [slots]
-    uint64_t* empty = full + kAttnSlots;   // [slots]
-    uint64_t* s_full = empty + kAttnSlots; // [2]
+    uint64_t* empty = full + kSlots;       // [slots]
+    uint64_t* s_full = empty + kSlots;     // [2]
     uint64_t* p_full = s_full + 2;         // [2]: 8 warps
     uint64_t* o_full = p_full + 2;         // [2]
     uint64_t* o_empty = o_full + 2;        // [2]: 8 warps
@@ -243,7 +247,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
     if (threadIdx.x == 0) {
         mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
-        for (int s = 0; s < kAttnSlots; ++s) {
+        for (int s = 0; s < kSlots; ++s) {
             mbar_init(full + s, 1);
             mbar_init(empty + s, 1);
         }
@@ -345,9 +349,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
             }
             ++queries;
             for (int e = 0; e < w.entries; ++e, ++it) {
-                const int s = it % kAttnSlots;
+                const int s = it % kSlots;
                 if (e > 0 && e == ask && lane == 0) mbar_arrive(near);
-                if (it >= kAttnSlots && !(ok = wait(empty + s, (it / kAttnSlots - 1) & 1))) break;
+                if (it >= kSlots && !(ok = wait(empty + s, (it / kSlots - 1) & 1))) break;
                 if (lane == 0) {
                     const bool values = e >= w.lag, keys = e < w.count;
                     mbar_arrive_expect_tx(full + s, (values ? kTile : 0) + (keys ? kTile : 0));
@@ -365,8 +369,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
         }
         if (*gone && lane == 0) {  // what is in flight has landed before the memory is let go
             if (queries > 0) mbar_wait_bounded(q_full, (queries - 1) & 1, p.timeout_ns);
-            for (int j = max(it - kAttnSlots, 0); j < it; ++j)
-                mbar_wait_bounded(full + j % kAttnSlots, (j / kAttnSlots) & 1, p.timeout_ns);
+            for (int j = max(it - kSlots, 0); j < it; ++j)
+                mbar_wait_bounded(full + j % kSlots, (j / kSlots) & 1, p.timeout_ns);
         }
     } else if (warp == kAttnProducts) {
         // One thread for both tiles, first come first served: with a warp each
@@ -388,8 +392,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
             if (!(ok = wait(q_full, queries & 1))) break;
             ++queries;
             for (int e = 0; e < entries && ok; ++e, ++it) {
-                const int s = it % kAttnSlots;
-                if (!(ok = wait(full + s, (it / kAttnSlots) & 1))) break;
+                const int s = it % kSlots;
+                if (!(ok = wait(full + s, (it / kSlots) & 1))) break;
                 uint8_t* const values = ring + s * 2 * kTile;
                 // rows of V behind the sequence belong to another, or to nobody:
                 // their probabilities are 0, but 0 times what lies there need not be

@@ -12,8 +12,8 @@ int attention_threads() { return kAttnThreads; }
 
 size_t attention_smem(int d)
 {
-    const size_t tile = (size_t)(d <= 64 ? 1 : 2) * kAttnBlock;
-    return 1024 + (2 + 2 * kAttnSlots) * tile + (2 * kAttnSlots + 26) * 8 + 10 * 128 * 8 + kAttnRowWarps * 1024 +
+    const size_t tile = (size_t)(d <= 64 ? 1 : 2) * kAttnBlock, slots = d <= 64 ? kAttnSlots<1> : kAttnSlots<2>;
+    return 1024 + (2 + 2 * slots) * tile + (2 * slots + 26) * 8 + 10 * 128 * 8 + kAttnRowWarps * 1024 +
            2 * sizeof(AttnWork);
 }
 
