@@ -755,7 +755,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                                 const float4 v =
                                     ld_peer4(peer(part + (size_t)((tile + z) * 128 + row) * D + (c ^ (row & 7)) * 4, q));
                                 total_l = fmaf(f, st[q][z].y, total_l);
-                                o.x = fmaf(f, v.x, o.x), o.y = fmaf(f, v.y, o.y), o.z = fmaf(f, v.z, o.z), o.w = fmaf(f, v.w, o.w);
+                                o.x = fmaf(f, v.x, o.x), o.y = fmaf(f, v.y, o.y);
+                                o.z = fmaf(f, v.z, o.z), o.w = fmaf(f, v.w, o.w);
                             }
                     const float inv = total_l == 0.0f ? 0.0f : 1.0f / total_l;
                     const int64_t to = (int64_t)(a.q0 + tok);

@@ -328,7 +328,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
             __syncwarp();
         };
         // 128 x 128 scores: rows of x by columns of z
-        auto scores = [&](uint32_t to, const uint8_t* x, const uint8_t* z, uint64_t* done, uint64_t* free, uint64_t* rows_free) {
+        auto scores = [&](uint32_t to, const uint8_t* x, const uint8_t* z, uint64_t* done, uint64_t* free,
+                          uint64_t* rows_free) {
             if (elect_one()) {
                 const uint64_t dx = operand_desc(smem_u32(x), false), dz = operand_desc(smem_u32(z), false);
 #pragma unroll

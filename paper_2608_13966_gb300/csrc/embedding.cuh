@@ -217,7 +217,9 @@ __device__ __forceinline__ void add_rows(float (&sum)[8], const EmbedGradParams&
         Raw8<WIDE> raw[N];
 #pragma unroll
         for (int q = 0; q < N; ++q)
-            load_raw<kEmbedThreads, VECTORS>(raw[q], row_of(static_cast<const void*>(dy), p.dy_f32, places[min(i + q, end - 1)], p.ld_dy),
+            load_raw<kEmbedThreads, VECTORS>(raw[q],
+                                             row_of(static_cast<const void*>(dy), p.dy_f32,
+                                                    places[min(i + q, end - 1)], p.ld_dy),
                                              p.dy_f32, threadIdx.x, 0, i + q < end ? cols : 0);
 #pragma unroll
         for (int q = 0; q < N; ++q) {

@@ -475,7 +475,8 @@ __global__ void __launch_bounds__(kNormThreads<T>, kNormPerSm<T, NV>)
 }
 
 template <int T, int NV, bool WIDE>
-__global__ void __launch_bounds__(T, kNormRingPerSm<T, NV, true>) k_layer_norm_grad_ring(const __grid_constant__ NormGradParams p)
+__global__ void __launch_bounds__(T, kNormRingPerSm<T, NV, true>)
+    k_layer_norm_grad_ring(const __grid_constant__ NormGradParams p)
 {
     constexpr int kWarps = T / 32;
     extern __shared__ __align__(16) uint8_t smem[];
@@ -511,7 +512,8 @@ __global__ void __launch_bounds__(T, kNormRingPerSm<T, NV, true>) k_layer_norm_g
         for (int i = 0; i < 8; ++i) dw[j][i] = db[j][i] = 0.0f;
     }
     auto stats_of = [&](int64_t row) {
-        return row < p.rows ? make_float2(p.center ? p.stats[2 * row] : 0.0f, p.stats[2 * row + 1]) : make_float2(0.0f, 0.0f);
+        if (row >= p.rows) return make_float2(0.0f, 0.0f);
+        return make_float2(p.center ? p.stats[2 * row] : 0.0f, p.stats[2 * row + 1]);
     };
     float2 next = stats_of(blockIdx.x);
     int slot = 0, turn = 0;

@@ -113,7 +113,8 @@ quasar_status quasar_layer_norm(const void* x, quasar_dtype x_dtype, int64_t ld_
         if (const void* ring = layer_norm_ring_kernel(cols, false, wide, &threads, &per_sm)) {
             size_t smem = 0;
             p.slots = layer_norm_slots((uint32_t)(cols * dtype_size(x_dtype)), threads, per_sm, &smem);
-            return launch(ring, &p, dim3((unsigned)std::min<int64_t>(rows, (int64_t)n_sm * per_sm)), threads, 1, smem, stream);
+            return launch(ring, &p, dim3((unsigned)std::min<int64_t>(rows, (int64_t)n_sm * per_sm)), threads, 1, smem,
+                          stream);
         }
     }
     const void* fn = layer_norm_kernel(cols, vectors, false, wide, &threads, &at_once, &per_sm);
@@ -192,7 +193,8 @@ quasar_status quasar_layer_norm_backward(const void* dy, quasar_dtype dy_dtype, 
         const void* fn = ring ? nullptr : layer_norm_kernel(cols, vectors, true, wide, &threads, &at_once, &per_sm);
         if (ring) {
             size_t smem = 0;
-            const int64_t bytes = cols * (dtype_size(x_dtype) + dtype_size(dy_dtype) + (residual ? dtype_size(dx_dtype) : 0));
+            const int64_t bytes =
+                cols * (dtype_size(x_dtype) + dtype_size(dy_dtype) + (residual ? dtype_size(dx_dtype) : 0));
             p.slots = layer_norm_slots((uint32_t)bytes, threads, per_sm, &smem);
             if ((st = launch(ring, &p, dim3((unsigned)parts), threads, 1, smem, stream)) != QUASAR_OK) return st;
         } else if (fn) {
