@@ -574,10 +574,26 @@ __global__ void __launch_bounds__(T, kNormRingPerSm<T, NV, true>)
         if (t == 0) norm_drain(ring, sent, p.timeout_ns);
         return;
     }
+    // (of one row they are the caller's dweight and dbias, which start at any float)
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        if (p.part_w) store_row<T, true>(p.part_w + (int64_t)blockIdx.x * p.cols, true, t, j, n_cols, dw[j]);
-        if (p.part_b) store_row<T, true>(p.part_b + (int64_t)blockIdx.x * p.cols, true, t, j, n_cols, db[j]);
+    for (int which = 0; which < 2; ++which) {
+        float* part = which ? p.part_b : p.part_w;
+        if (!part) continue;
+        float(&mine)[NV][8] = which ? db : dw;
+        const bool vectors = (reinterpret_cast<uintptr_t>(part) & 15) == 0;
+        part += (int64_t)blockIdx.x * p.cols;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (vectors) {
+                store_row<T, true>(part, true, t, j, n_cols, mine[j]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int c = row_at<T, true>(t, j, i);
+                    if (c < n_cols) part[c] = mine[j][i];
+                }
+            }
+        }
     }
 }
 
