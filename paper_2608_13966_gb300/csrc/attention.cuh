@@ -19,6 +19,14 @@
 // P is rounded to bf16 for the matrix product (2^-8 of it at most); l is the sum
 // before the rounding.
 //
+// The tensor core cuts off what a product has below 2^-23 of the sum that it is added
+// to, of many keys alike a little each time: in one sum values of 1.99 over 2^20 keys came
+// out 0.8% low, over 2^22 3.9%.  So O grows by 1,024 key tiles at a time (8,192
+// products, 2^-10 of a sum at most), each with a maximum and an l of its own, and what they
+// leave is joined in fp32 in the thread's local memory.  Where k has no more rows than
+// that (131,072) a kernel without this code runs (256 single tokens over 2,048 keys
+// each: 357 us without, 361 with it).
+//
 // Where rows are few, a cluster of CTAs shares a row's keys, and where there are
 // rows for one tile alone, the tiles are twins: the same rows, every other key
 // tile each.  Twins are joined in tensor memory, the parts of a cluster's CTAs
@@ -201,6 +209,33 @@ __device__ __forceinline__ AttnWork attention_work(const AttnParams& p, int whic
     return w;
 }
 
+// What a row has summed of some key tiles (O's columns, l and its maximum) joined to
+// what it has of those before; O, l and m then start again or, behind the last tiles,
+// hold it all.
+template <int COLUMNS>
+__device__ __forceinline__ float2 join_tiles(float* before, uint32_t o_at, float m, float l, bool first, bool last)
+{
+    const float top = first ? m : fmaxf(m, before[COLUMNS + 1]), shift = top == minus_inf() ? 0.0f : top;
+    const float old = first ? 0.0f : exp2_fast(before[COLUMNS + 1] - shift), now = exp2_fast(m - shift);
+#pragma unroll 1
+    for (int c = 0; c < COLUMNS; c += 16) {
+        float o[16];
+        tmem_ld16(o_at + c, o);
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+            const float sum = first ? o[x] : fmaf(o[x], now, before[c + x] * old);
+            before[c + x] = sum;
+            o[x] = last ? sum : 0.0f;
+        }
+        tmem_st16(o_at + c, o);
+    }
+    tmem_wait_st();
+    l = first ? l : fmaf(l, now, before[COLUMNS] * old);
+    before[COLUMNS] = l;
+    before[COLUMNS + 1] = top;
+    return last ? make_float2(top, l) : make_float2(minus_inf(), 0.0f);
+}
+
 // D = 64 DB columns; a head of d columns is completed with zeros.
 //
 // A CTA takes items until there are none (or, where few are, has one): while one's
@@ -210,7 +245,9 @@ __device__ __forceinline__ AttnWork attention_work(const AttnParams& p, int whic
 // items dealt out beforehand 454, though one sequence of 2,048 40 as now; with a CTA
 // an item 512; 256 queries of 2,048 keys 346, with a CTA an item 460, without
 // twins 378).
-template <int DB>
+//
+// FAR: a sequence may have more key tiles than one sum takes.
+template <int DB, bool FAR>
 __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_constant__ AttnParams p)
 {
     constexpr int D = 64 * DB;
@@ -515,6 +552,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
             const bool any_live = __any_sync(0xffffffffu, live);
             const int n = w.n[i];
             float m = minus_inf(), l = 0.0f;
+            [[maybe_unused]] float before[FAR ? kHalf + 2 : 1];  // (indexed: in local memory)
             if (n > 0) {
                 // the last key that the row sees (rows of nobody mask nothing)
                 const int64_t last = (int64_t)a.m - 1;
@@ -522,6 +560,15 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                                     : p.causal ? min(last, (int64_t)token + a.m - a.n)
                                                : last;
                 bool together = true;
+                [[maybe_unused]] auto join = [&](int upto) {  // the tiles before `upto`, whose products are done
+                    if constexpr (FAR) {
+                        if (!ok || !any_live) return;
+                        tc_fence_after();
+                        const float2 ml = join_tiles<kHalf>(before, o_at, m, l, upto == kAttnFold, upto == n);
+                        m = ml.x, l = ml.y;
+                        tc_fence_before();
+                    }
+                };
                 for (int j = 0; j < n; ++j) {
                     ok = ok && wait(s_full + i, (done + j) & 1);
                     tc_fence_after();
@@ -603,9 +650,14 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(p_full + i);
+                    if (FAR && (j + 1) % kAttnFold == 0 && j + 1 < n) {
+                        ok = ok && wait(o_full + i, (done + j) & 1);
+                        join(j + 1);
+                    }
                 }
                 if (together) {
                     ok = ok && wait(o_full + i, (done + n - 1) & 1);
+                    if (FAR && n > kAttnFold) join(n);
                     float other;
                     ok = exchange(l, other);
                     l = half ? other + l : l + other;

@@ -9,7 +9,7 @@ namespace quasar {
 constexpr int kAttnRows = 128;     // of a tile: (token, head) pairs, the lanes of tensor memory
 constexpr int kAttnKeys = 128;     // of a key tile
 constexpr int kAttnMostSplit = 8;  // CTAs of a cluster that share a row's keys
-constexpr int kAttnFarTiles = 4096;  // key tiles of a sequence that is always shared
+constexpr int kAttnFold = 1024;    // key tiles of one sum of a row
 
 // Sequences packed along the rows of q, and of k and v: sequence i has the rows
 // starts[i] .. starts[i + 1] (NULL: one sequence of all rows).

@@ -9,7 +9,7 @@
 #include "quasar.h"
 
 namespace quasar {
-const void* attention_kernel(int d);
+const void* attention_kernel(int d, bool far);
 int attention_threads();
 size_t attention_smem(int d);
 const void* attention_stats_kernel(int d);
@@ -103,20 +103,14 @@ quasar_status quasar_attention(const void* q, int64_t ld_q, const void* k, int64
     const int64_t work = std::max<int64_t>(1, items - 1) * kv_heads;  // (the one more aside)
     const int64_t tiles = keys / std::max<int64_t>(1, sequences) / kAttnKeys;
     p.split = 1;
-    const void* fn = attention_kernel(p.d);
+    const void* fn = attention_kernel(p.d, keys > (int64_t)kAttnFold * kAttnKeys);  // (no sequence has more)
     const size_t smem = attention_smem(p.d);
     // more items than SMs: their CTAs take them from one another (not so, 16 x 512
     // tokens 107 us against 78, 512 queries of 512 keys 472 against 229).  Fewer:
     // as many CTAs share one's keys as fill the device, four key tiles each (two:
     // two queries of 1,024 keys 22.7 us against 12.3; eight: 13.9)
-    // The tensor core cuts off what a product has below 2^-25 of the sum so far, of
-    // many keys alike a little each time: values of 1.99 over 2^20 keys came out
-    // 0.8% low, over 2^22 3.9%.  From 2^19 keys a sequence on (on average), always as many CTAs as
-    // there may be, with a sum each (2,048 tokens over 2^18 keys would take 7.7 ms
-    // against 6.9).
-    const bool far = tiles >= kAttnFarTiles;
-    p.persistent = work > n_sm && !far;
-    while (p.split < kAttnMostSplit && (far || work * p.split < n_sm) && tiles >= 4 * p.split) p.split *= 2;
+    p.persistent = work > n_sm;
+    while (p.split < kAttnMostSplit && work * p.split < n_sm && tiles >= 4 * p.split) p.split *= 2;
     const int64_t ctas = items * kv_heads * p.split;
     if ((st = head_map(q, tokens, heads, head_dim, ld_q, p.group, p.tile_tokens, &p.q)) != QUASAR_OK) return st;
     // (without keys no copy is made: any valid map will do)

@@ -3,9 +3,13 @@
 
 namespace quasar {
 
-const void* attention_kernel(int d)
+const void* attention_kernel(int d, bool far)
 {
-    return d <= 64 ? reinterpret_cast<const void*>(&k_attention<1>) : reinterpret_cast<const void*>(&k_attention<2>);
+    if (d <= 64)
+        return far ? reinterpret_cast<const void*>(&k_attention<1, true>)
+                   : reinterpret_cast<const void*>(&k_attention<1, false>);
+    return far ? reinterpret_cast<const void*>(&k_attention<2, true>)
+               : reinterpret_cast<const void*>(&k_attention<2, false>);
 }
 
 int attention_threads() { return kAttnThreads; }
