@@ -44,7 +44,8 @@ struct AttnParams {
     unsigned int* status;
 };
 
-constexpr int kGradCols = 128;  // of a step of the backward kernels
+constexpr int kGradCols = 128;   // of a step of the backward kernels
+constexpr int kGradFold = 1024;  // steps of one sum
 
 // One of the two backward kernels: 128 rows stay, the other side streams past
 // in steps of 128 columns.

@@ -13,7 +13,7 @@ const void* attention_kernel(int d, bool far);
 int attention_threads();
 size_t attention_smem(int d);
 const void* attention_stats_kernel(int d);
-const void* attention_grad_kernel(int d, bool keys);
+const void* attention_grad_kernel(int d, bool keys, bool far);
 int attention_grad_threads();
 size_t attention_grad_smem(int d);
 }  // namespace quasar
@@ -212,7 +212,7 @@ quasar_status quasar_attention_backward(const void* dy, int64_t ld_dy, const voi
             (st = map(true, v, ld_v, 1, kAttnRows, &p.x2)) != QUASAR_OK ||
             (st = map(false, q, ld_q, p.group, p.tile_tokens, &p.z1)) != QUASAR_OK ||
             (st = map(false, dy, ld_dy, p.group, p.tile_tokens, &p.z2)) != QUASAR_OK ||
-            (st = launch(attention_grad_kernel(p.d, true), &p, dim3((unsigned)(key_items * kv_heads)),
+            (st = launch(attention_grad_kernel(p.d, true, tokens > (int64_t)kGradFold * p.tile_tokens), &p, dim3((unsigned)(key_items * kv_heads)),
                          attention_grad_threads(), 1, smem, stream)) != QUASAR_OK)
             return st;
     }
@@ -223,7 +223,7 @@ quasar_status quasar_attention_backward(const void* dy, int64_t ld_dy, const voi
             (st = map(false, dy, ld_dy, p.group, p.tile_tokens, &p.x2)) != QUASAR_OK ||
             (st = map(true, k, ld_k, 1, kGradCols, &p.z1)) != QUASAR_OK ||
             (st = map(true, v, ld_v, 1, kGradCols, &p.z2)) != QUASAR_OK ||
-            (st = launch(attention_grad_kernel(p.d, false), &p, dim3((unsigned)(query_items * kv_heads)),
+            (st = launch(attention_grad_kernel(p.d, false, keys > (int64_t)kGradFold * kGradCols), &p, dim3((unsigned)(query_items * kv_heads)),
                          attention_grad_threads(), 1, smem, stream)) != QUASAR_OK)
             return st;
     }

@@ -19,7 +19,11 @@
 // Rows and columns of queries are (token, head) pairs, the heads that share keys
 // side by side, so dk and dv of shared keys are one sum over all of their heads.
 // P and dS go through tensor memory as bf16, in the place of S and dP: each is
-// rounded once for its matrix product (2^-8 of it), sums are fp32.
+// rounded once for its matrix product (2^-8 of it), sums are fp32.  The tensor core
+// cuts off what a product has below 2^-23 of the sum that it is added to, so one sum takes
+// 1,024 steps (8,192 products, 2^-10 of it at most); what it has come to is then added to
+// the thread's own in local memory (dv of 2^21 rows alike came out 1.6% low in one sum).  Where
+// no sequence can have as many steps a kernel without this code runs.
 //
 // The matrix instructions are one thread's, in an order that leaves the rows'
 // warps the time of two products for P and as long for dS:
@@ -124,7 +128,9 @@ __host__ __device__ constexpr size_t attention_grad_bytes(int blocks)
 // made, while the gradients of one are written (with a CTA an item, keys
 // and queries of 64 x 256 tokens, 16 heads of 128, took 202 and 191 us against 142
 // and 130; of 4 x 4096, 32 heads over 8, 900 and 864 against 877 and 763).
-template <int DB, bool KEYS>
+//
+// FAR: an item may have more steps than one sum takes.
+template <int DB, bool KEYS, bool FAR>
 __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid_constant__ AttnGradParams p)
 {
     constexpr int D = 64 * DB;
@@ -357,7 +363,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
             __syncwarp();
         };
         Place z1{0, 0}, z2{0, 0};  // of the next S and dP
-        int old1 = 0, sets = 0, g = 0;  // z1 of the step that ends; items with steps; steps so far
+        int old1 = 0, sets = 0, sums = 0, g = 0;  // z1 of the step that ends; items with steps; sums, steps so far
         bool ok = true;
         for (int k = 0, end = 0; ok && !end; ++k) {
             if (!(ok = take(k))) break;
@@ -395,14 +401,15 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
             for (int j = 0; j < steps; ++j) {
                 const bool more = j + 1 < steps;
                 const int gj = g + j;
-                // the gradients of the item before have been read
-                if (j == 0 && sets > 0 && !(ok = wait(acc_empty, (sets - 1) & 1))) break;
+                // the gradients of the item before, or of the sum before, have been read
+                const bool first = FAR ? j % kGradFold == 0 : j == 0;
+                if (first && sums > 0 && !(ok = wait(acc_empty, (sums - 1) & 1))) break;
                 if (KEYS) {
                     // (two products at a time, their operands waited for before them)
                     if (more && !(ok = come1(j + 1))) break;
                     if (!(ok = wait(p_full, gj & 1))) break;
                     tc_fence_after();
-                    grow(kAcc2, kScores, ring2 + (gj & 1) * kTile, j > 0, empty2 + (gj & 1));
+                    grow(kAcc2, kScores, ring2 + (gj & 1) * kTile, !first, empty2 + (gj & 1));
                     if (more) score_s();
                     if (more && !(ok = come2(j + 1))) break;
                 } else {
@@ -416,14 +423,20 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                 }
                 if (!(ok = wait(ds_full + (gj & 1), (gj >> 1) & 1))) break;
                 tc_fence_after();
-                grow(0, dp_at(gj), ring1 + old1 * kTile, j > 0, empty1 + old1);
+                grow(0, dp_at(gj), ring1 + old1 * kTile, !first, empty1 + old1);
                 if (++old1 == kGradSlots1) old1 = 0;
+                if (FAR && more && (j + 1) % kGradFold == 0) {  // a sum is full
+                    if (elect_one()) mma_commit(smem_u32(acc_full));
+                    __syncwarp();
+                    ++sums;
+                }
                 if (KEYS && more) score_dp(j + 1);
             }
             if (!ok) break;
             if (elect_one()) mma_commit(smem_u32(acc_full));
             __syncwarp();
             ++sets;
+            ++sums;
             g += steps;
         }
         if (elect_one()) {  // every instruction is done before the memory is let go
@@ -470,8 +483,14 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
         const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t s_at = mine + kScores + quarter * 32;
         const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
+        // keys stay: dk by warps 0-7, dv by warps 8-15, half of the columns each;
+        // queries stay: a quarter of the columns of dq each
+        constexpr int kSpan = KEYS ? D / 2 : D / 4;
+        const bool second = KEYS && warp >= 8;
+        const int c0 = KEYS ? (quarter & 1) * kSpan : quarter * kSpan;
+        const uint32_t acc_at = mine + (second ? kAcc2 : 0) + c0;
         bool ok = true;
-        int sets = 0, g = 0;
+        int sums = 0, g = 0;
         for (int k = 0; ok; ++k) {
             if (!(ok = take(k))) break;
             const GradWork& w = items[k & 1];
@@ -507,6 +526,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
             const int64_t last = (int64_t)w.a.m - 1;
             const int upto = (int)max((int64_t)-(1 << 30), p.causal ? min(last, (int64_t)token + shift) : last);
             const int begin = w.begin;
+            [[maybe_unused]] float before[FAR ? kSpan : 1];  // the gradients of the sums before (in local memory)
             for (int j = 0; j < steps; ++j, ++g) {
                 ok = wait(s_full, g & 1);
                 if (KEYS && ok) ok = wait(stat_full + (g & 1), (g >> 1) & 1);
@@ -591,28 +611,42 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(ds_full + (g & 1));
+                if (FAR && (j + 1) % kGradFold == 0 && j + 1 < steps) {  // a sum is full
+                    if (!(ok = wait(acc_full, sums & 1))) break;
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c = 0; c < kSpan; c += 16) {
+                        float o[16];
+                        tmem_ld16(acc_at + c, o);
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) before[c + x] = j < kGradFold ? o[x] : before[c + x] + o[x];
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(acc_empty);
+                    ++sums;
+                }
             }
             if (!ok) break;
             if (steps > 0) {
-                if (!(ok = wait(acc_full, sets & 1))) break;
+                if (!(ok = wait(acc_full, sums & 1))) break;
                 tc_fence_after();
             }
-            // keys stay: dk by warps 0-7, dv by warps 8-15, half of the columns
-            // each; queries stay: a quarter of the columns of dq each
-            constexpr int kSpan = KEYS ? D / 2 : D / 4;
-            const bool second = KEYS && warp >= 8;
-            const int c0 = KEYS ? (quarter & 1) * kSpan : quarter * kSpan;
             const float scale = second ? 1.0f : p.scale;
             uint32_t out[kSpan / 2];
 #pragma unroll
             for (int c = 0; c < kSpan; c += 16) {
                 float o[16];
                 if (steps > 0) {
-                    tmem_ld(mine + (second ? kAcc2 : 0) + c0 + c, o);
+                    tmem_ld(acc_at + c, o);
                     tmem_wait_ld(o);
                 } else {
 #pragma unroll
                     for (int x = 0; x < 16; ++x) o[x] = 0.0f;
+                }
+                if (FAR && steps > kGradFold) {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) o[x] += before[c + x];
                 }
 #pragma unroll
                 for (int x = 0; x < 16; x += 2) out[(c + x) / 2] = pack_bf16x2(o[x] * scale, o[x + 1] * scale);
@@ -621,7 +655,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(acc_empty);
-                ++sets;
+                ++sums;
             }
             if (live) {
                 __nv_bfloat16* const to =

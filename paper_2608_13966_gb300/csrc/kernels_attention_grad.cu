@@ -9,13 +9,17 @@ const void* attention_stats_kernel(int d)
                    : reinterpret_cast<const void*>(&k_attention_stats<16>);
 }
 
-const void* attention_grad_kernel(int d, bool keys)
+template <int DB, bool KEYS>
+static const void* grad_kernel(bool far)
 {
-    if (d <= 64)
-        return keys ? reinterpret_cast<const void*>(&k_attention_grad<1, true>)
-                    : reinterpret_cast<const void*>(&k_attention_grad<1, false>);
-    return keys ? reinterpret_cast<const void*>(&k_attention_grad<2, true>)
-                : reinterpret_cast<const void*>(&k_attention_grad<2, false>);
+    return far ? reinterpret_cast<const void*>(&k_attention_grad<DB, KEYS, true>)
+               : reinterpret_cast<const void*>(&k_attention_grad<DB, KEYS, false>);
+}
+
+const void* attention_grad_kernel(int d, bool keys, bool far)
+{
+    if (d <= 64) return keys ? grad_kernel<1, true>(far) : grad_kernel<1, false>(far);
+    return keys ? grad_kernel<2, true>(far) : grad_kernel<2, false>(far);
 }
 
 int attention_grad_threads() { return kGradThreads; }
