@@ -718,6 +718,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) k_attention(const __grid_cons
 #pragma unroll
                     for (int x = 0; x < 32; x += 2) out[(c + x) / 2] = pack_bf16x2(o[x] * inv, o[x + 1] * inv);
                 }
+                if (l == 0.0f) {  // (0 times values that need not be finite)
+#pragma unroll
+                    for (int x = 0; x < kHalf / 2; ++x) out[x] = 0;
+                }
                 // 1 KB of rows at a time through shared memory, so that a store
                 // covers whole lines (of a row a thread each store touched 32)
                 constexpr int kVecs = kHalf / 8, kRows = 64 / kVecs;  // 16-byte vectors of a row; rows at a time

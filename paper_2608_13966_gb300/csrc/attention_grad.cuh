@@ -651,6 +651,10 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_attention_grad(const __grid
 #pragma unroll
                 for (int x = 0; x < 16; x += 2) out[(c + x) / 2] = pack_bf16x2(o[x] * scale, o[x + 1] * scale);
             }
+            if (!KEYS && upto < 0) {  // it sees no key: 0, and not 0 times keys that need not be finite
+#pragma unroll
+                for (int x = 0; x < kSpan / 2; ++x) out[x] = 0;
+            }
             if (steps > 0) {  // read: the next item's may grow
                 tc_fence_before();
                 __syncwarp();
