@@ -684,7 +684,9 @@ quasar_status quasar_layer_norm_backward(const void* dy, quasar_dtype dy_dtype, 
  * keys).  Columns of one buffer (a projection's result) are fine.  A token that
  * sees no key, and a row of no sequence, has y 0 and lse -inf.  A value that is
  * not finite reaches the rows of its sequence alone; in v it may reach those
- * that see other keys and not its own, as 0 times it does in the formula.
+ * that see other keys and not its own, as 0 times it does in the formula.  Sums
+ * over keys (and over rows, for the gradients) are fp32, made by the matrix cores
+ * up to 131072 terms at a time, which cuts off at most 2^-10 of their sizes.
  */
 quasar_status quasar_attention(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
                                int64_t tokens, int64_t keys, int64_t heads, int64_t kv_heads, int64_t head_dim,

@@ -37,14 +37,16 @@
 // cores waited for a tile's 4 warps: 565 us); 16 copies, 17 matrix instructions,
 // 18 looks up the items.
 //
-// 4 x 4096 causal, 32 heads of 128 over 8: 440 us, 1.25 PFLOP/s of the products at
-// and below the diagonal, 0.74 of the sustained rate.  What bounds it is the
+// 4 x 4096 causal, 32 heads of 128 over 8: 452 us, 1.22 PFLOP/s of the products at
+// and below the diagonal, 0.72 of the sustained rate.  What bounds it is the
 // chain from a tile's scores through P to its next product, which the other tile
 // hides in part, and the product thread's waits (some hundred cycles each, and
 // the tensor cores hold few instructions); masked halves of diagonal tiles are
 // computed too, 1.03 of the work.  One query for each of 61 sequences of up to
-// 2,048 keys, 32 heads over 8: 79 us, 4.5 TB/s, bound by the last of 3.2 items an SM
-// (256 sequences of 2,048 keys 346 us, 6.2 TB/s).
+// 2,048 keys, 32 heads over 8: 73 us, 4.5 TB/s, bound by the last of 3.2 items an SM
+// (256 sequences of 2,048 keys 354 us, 6.1 TB/s).  For each of 8 sequences of up to 16,384
+// keys: 77 us, 4.6 TB/s: 64 items are fewer than the SMs, so clusters of four CTAs have one
+// each, 256 CTAs for 152 SMs, whose second round starts when the first has ended.
 #pragma once
 
 #include "attention.h"
@@ -241,10 +243,10 @@ __device__ __forceinline__ float2 join_tiles(float* before, uint32_t o_at, float
 // A CTA takes items until there are none (or, where few are, has one): while one's
 // last products run and its rows are written, the next one's tiles are on their
 // way and its first products follow at once.  The grid has a CTA for each item,
-// and CTAs that run take those that have not been launched (4 x 4096 440 us; with
-// items dealt out beforehand 454, though one sequence of 2,048 40 as now; with a CTA
-// an item 512; 256 queries of 2,048 keys 346, with a CTA an item 460, without
-// twins 378).
+// and CTAs that run take those that have not been launched (replayed side by side,
+// 4 x 4096 440 us; with items dealt out beforehand 454, though one sequence of 2,048 40
+// as now; with a CTA an item 512; 256 queries of 2,048 keys 346, with a CTA an item
+// 460, without twins 378).
 //
 // FAR: a sequence may have more key tiles than one sum takes.
 template <int DB, bool FAR>

@@ -34,8 +34,8 @@
 // (In steps of 64 columns, S and dP of two steps at a time, 1788 us where steps
 // of 128 took 1710: the tensor cores read 1.26 times as much shared memory.)
 //
-// 4 x 4096 causal, 32 heads of 128 over 8: 1620 us with the statistics, 0.85
-// PFLOP/s of the formulas' 5 products, 1.19 of the 7.  What bounds it is the chain
+// 4 x 4096 causal, 32 heads of 128 over 8: 1610 us with the statistics, 0.85
+// PFLOP/s of the formulas' 5 products, 1.20 of the 7.  What bounds it is the chain
 // scores, P, dS, product of a step, of which one CTA's tensor memory holds no
 // second one beside the gradients.
 //

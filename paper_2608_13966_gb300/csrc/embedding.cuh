@@ -264,8 +264,13 @@ __device__ __forceinline__ int lower_bound(const uint32_t* keys, int from, int t
     return from;
 }
 
-// kEmbedRows rows of the table by 2,048 columns a CTA.  Bound by writing the
-// table's gradient.
+// kEmbedRows rows of the table by 2,048 columns a CTA.  Where most of a large
+// table's rows have no token, bound by writing the gradient (131072 x 4096 bf16,
+// 16384 tokens: 214 us, 5.2 TB/s of DRAM).  Rows that have tokens come one after the
+// other, each a wait for its places and then for its rows of dy: 16384 tokens over
+// every row of 4096 x 4096 140 us with the sort, 150 over 192 x 256 (3 CTAs) 103 us.
+// 8003 x 1003 fp32 has 126 CTAs, fewer than the SMs, and stores single elements: 33 us
+// with the sort, where its bytes take 5.
 template <bool VECTORS, bool WIDE>
 __global__ void __launch_bounds__(kEmbedThreads) k_embedding_grad(const __grid_constant__ EmbedGradParams p)
 {

@@ -84,8 +84,12 @@ const void* layer_norm_kernel(int64_t cols, bool vectors, bool grad, bool wide, 
 
 // The kernel of rows through shared memory (rows of whole vectors of 8 that
 // start at 16-byte boundaries), its threads and CTAs an SM; nullptr for rows
-// that a warp takes, or that registers do not hold (backward from 8192 on, where
-// dw and db need them too).
+// that a warp takes, or that registers do not hold (backward beyond 8192, where
+// dw and db need them too: k_layer_norm_grad has such rows, with 348 to 808 bytes of
+// spills a thread and no row on its way; 4096 x 16384 bf16 164 us, 2.5 TB/s, against
+// 82, 4.9 TB/s, for 8192 x 8192 here).  Rows that are not whole vectors take the
+// register kernels by single elements: 16384 x 4099 bf16 219 us forward and 310
+// back, against 51 and 79 for 4096 columns.
 const void* layer_norm_ring_kernel(int64_t cols, bool grad, bool wide, int* threads, int* per_sm)
 {
     if (cols % 8 != 0 || cols <= 1024 || cols > (grad ? 8192 : kNormMostCols)) return nullptr;
